@@ -287,6 +287,35 @@ int rlkv_paged_append(rlkv_paged* cache, int layer, const int* slots, int n, con
  * [n_tokens][kv_heads][head_dim]. */
 int rlkv_paged_prefill(rlkv_paged* cache, int layer, int slot, const void* k, const void* v,
                        int n_tokens, void* stream);
+/* Rotary position embedding on the way into the paged cache.  (The paper's models rotate queries and keys
+ * by their position; with these calls the projections' output goes into the cache in one launch.)
+ *
+ * rlkv_rotary_table fills `table` (device fp32 [positions][rot_dim / 2][2], 16-byte aligned) with cos and sin
+ * of position * inv_freq[j], computed in 64 bits.  inv_freq: HOST double [rot_dim / 2], whatever scaling the
+ * model uses already in it; rot_dim even, at most 128.  The launch goes to the GPU that holds `table`. */
+int rlkv_rotary_table(const double* inv_freq, int rot_dim, int positions, void* table, void* stream);
+/* The rotation of the cache's rotated calls from now on: element pairs j of the first rot_dim elements of a
+ * head -- (j, j + rot_dim / 2), or (2j, 2j + 1) if interleaved -- are turned by the angle in row t of the table for
+ * the token that becomes token t of its sequence.  rot_dim: a multiple of 16, at most head_dim; elements past it
+ * stay as they are.  The table (as above, `positions` rows) is the caller's and has to outlive the calls;
+ * NULL: no rotation is set (the rotated calls then return RLKV_EINVAL). */
+int rlkv_paged_set_rotary(rlkv_paged* cache, const void* table, int positions, int rot_dim, int interleaved);
+/* rlkv_paged_append on keys rotated by their position, the queries of the same tokens rotated in the same
+ * launch.  q: device bf16 [n][q_heads][head_dim]; k, v: [n][kv_heads][head_dim]; tokens are *_stride elements
+ * apart (a multiple of 8; 0: contiguous), so that slices of one projection's output can be given as they are.
+ * q_out: device bf16, contiguous: the rotated queries, for rlkv_paged_decode_attention; it may be q itself where
+ * q is contiguous, and overlaps no other argument.  q and q_out may both be NULL.  Products are computed in fp32
+ * and rounded once: q_out and 16-bit rows to bf16, 8-bit rows to the code of the fp32 value.  Values are stored
+ * as rlkv_paged_append stores them.  RLKV_EINVAL if no rotation is set or a token lies past the table. */
+int rlkv_paged_append_rotated(rlkv_paged* cache, int layer, const int* slots, int n, const void* q, int64_t q_stride,
+                              const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out,
+                              void* stream);
+/* rlkv_paged_prefill in the same way: n_tokens tokens of one sequence.  k_out (device bf16, contiguous
+ * [n_tokens][kv_heads][head_dim], or NULL; it may be k itself where k is contiguous): the rotated keys of the
+ * whole prompt, for rlkv_prompt_attention. */
+int rlkv_paged_prefill_rotated(rlkv_paged* cache, int layer, int slot, const void* q, int64_t q_stride, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride, int n_tokens, void* q_out,
+                               void* k_out, void* stream);
 /* Decode attention for n sequences of one layer, each over its own length, one launch for both
  * head classes and all lengths.  q: device bf16 [n][q_heads][head_dim]; out: device fp32
  * [n][q_heads][head_dim]; entry i belongs to slots[i] (HOST int[n]).  RLKV_EEMPTY if a listed
@@ -312,6 +341,15 @@ int rlkv_paged_step(rlkv_paged* cache, const int* slots, int n, const void* k, c
 int rlkv_paged_set_step_mode(rlkv_paged* cache, int mode);
 /* As rlkv_set_output_bf16, for rlkv_paged_decode_attention and rlkv_paged_step. */
 int rlkv_paged_set_output_bf16(rlkv_paged* cache, int on);
+/* The scores of rlkv_paged_decode_attention and rlkv_paged_step from now on, for models that cap them or encode
+ * positions in them:
+ *     score = softcap * tanh(x / softcap) - slopes[layer][j] * (tokens from the key to the query),
+ * x = q.k / sqrt(head_dim), for query head j.  softcap 0: x as it is; else 1e-3 to 1e6.  slopes: HOST float
+ * [layers][q_heads], magnitudes up to 1e6, copied, or NULL: no distance term.  Distances are those of the tokens,
+ * whatever ring slot a compressed head keeps a key in.  Synchronous where slopes are given (it waits for the device);
+ * not during a stream capture.  A captured graph keeps the softcap of its capture and reads the slopes set last.
+ * RLKV_EINVAL (nothing changed) for other values. */
+int rlkv_paged_set_scores(rlkv_paged* cache, float softcap, const float* slopes);
 int rlkv_paged_length(const rlkv_paged* cache, int layer, int slot, int* len_out);
 /* Pages on the free list and pages in total. */
 int rlkv_paged_pages(const rlkv_paged* cache, int* free_out, int* total_out);
@@ -337,6 +375,49 @@ int rlkv_paged_kernel_status(rlkv_paged* cache, int* status_out);
 int rlkv_debug_paged_schedule(const int* lens, int n, int n_full, int n_comp, int cap, int ctas,
                               int item_tiles, int* n_items_out, int* delivered_out,
                               int* expected_out, int* complete_out);
+
+/* ---- attention over whole prompts -------------------------------------------------------------------
+ * What a prompt (or a training sample) needs before its tokens are decoded: every token attends the tokens
+ * before it, with the head classes of the caches.  Documents are packed behind one another: document d holds the
+ * queries q_starts[d] .. q_starts[d+1]-1 and the keys k_starts[d] .. k_starts[d+1]-1 and sees no other document.
+ * With qn queries and kn keys, query i of a document stands at position pos = i + kn - qn and key j at position j (so
+ * a prompt may come in pieces: the last qn tokens as queries, all kn as keys).  The query sees key j iff
+ *     j < max(pos + 1, prefix[d])   and, unless its KV head is full,   j < sink or j > pos - window.
+ * prefix: the first prefix[d] keys are seen by every query of the document, from both sides.  The window is the cache's:
+ * what a compressed head would retain when token pos is the newest.  Over the visible keys
+ *     score = softcap * tanh(x / softcap) - slopes[layer][j] * |pos - position of the key|,  x = q.k / sqrt(head_dim),
+ *     out = softmax(score) . V,  lse = log sum exp(score).
+ * A query that sees no key gets out = 0 and lse = -infinity.  Tokens behind the last document belong to none: their
+ * rows of out, lse, dq, dk, dv are left as they are, and whatever their rows of q, k, v, dout hold has no effect on
+ * others; nor do the rows of one document on another's.  Values of a document's own rows are assumed finite.
+ *
+ * The mixed attention of Eq. 1 over a prompt is two of these (all heads full; all heads compressed), blended by the
+ * gates; its gradients are two backward calls on the weighted dout. */
+typedef struct rlkv_prompt rlkv_prompt;
+/* head_is_full: HOST [layers*kv_heads], slopes: HOST float [layers][q_heads] or NULL, both copied; softcap and slopes as
+ * for rlkv_paged_set_scores.  max_tokens: most q_tokens of a call (it sizes the backward pass's scratch, max_tokens *
+ * q_heads floats of device memory).  Shape limits are those of rlkv_cache_create.  Synchronous. */
+int rlkv_prompt_create(rlkv_prompt** out, int layers, int kv_heads, int q_heads, int head_dim, int max_tokens,
+                       const uint8_t* head_is_full, int sink, int window, float softcap, const float* slopes);
+int rlkv_prompt_destroy(rlkv_prompt* prompt);
+/* q: device bf16 [q_tokens][q_heads][head_dim]; k, v: [k_tokens][kv_heads][head_dim]; tokens *_stride elements apart (a
+ * multiple of 8, at most 2^30; 0: contiguous).  q_starts, k_starts: DEVICE int32 [n_docs + 1], ascending, read when the
+ * kernels run (k_starts NULL: the same as q_starts); ranges are clipped to the tensors.  n_docs: 1 to 65535.  prefix: DEVICE
+ * int32 [n_docs] or NULL.  out: device bf16 [q_tokens][q_heads][head_dim] (fp32 accumulation, rounded once); lse: device fp32
+ * [q_tokens][q_heads], or NULL.  Calls on one handle must be ordered, as for a cache. */
+int rlkv_prompt_attention(rlkv_prompt* prompt, int layer, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                          const void* v, int64_t v_stride, int q_tokens, int k_tokens, const int* q_starts,
+                          const int* k_starts, int n_docs, const int* prefix, void* out, float* lse, void* stream);
+/* The gradients, from the forward call's arguments and results and dout (device bf16, as out): dq as out, dk and dv device
+ * bf16 [k_tokens][kv_heads][head_dim] (summed over the query heads of a KV head), each rounded once.  Every sum has a fixed
+ * order: the same call gives the same bits. */
+int rlkv_prompt_attention_backward(rlkv_prompt* prompt, int layer, const void* q, int64_t q_stride, const void* k,
+                                   int64_t k_stride, const void* v, int64_t v_stride, int q_tokens, int k_tokens,
+                                   const int* q_starts, const int* k_starts, int n_docs, const int* prefix,
+                                   const void* out, const float* lse, const void* dout, void* dq, void* dk, void* dv,
+                                   void* stream);
+/* As rlkv_kernel_status. */
+int rlkv_prompt_kernel_status(rlkv_prompt* prompt, int* status_out);
 
 /* ---- introspection (host-side bookkeeping; no GPU work unless stated) ---- */
 int rlkv_length(const rlkv_cache* cache, int layer, int* len_out);

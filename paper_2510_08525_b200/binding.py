@@ -20,7 +20,7 @@ RLKV_OK, RLKV_EINVAL, RLKV_EFULL, RLKV_EEMPTY, RLKV_ENOMEM, RLKV_ECUDA, RLKV_EKE
 RLKV_ESCRATCH = -7
 
 # name -> (restype, argtypes); one entry per symbol declared in include/rlkv.h
-_vp, _ci, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+_vp, _ci, _sz, _i64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_int64
 SIGNATURES = {
     "rlkv_cache_size": (_ci, [_ci, _ci, _ci, _ci, _ci, _ci, _vp, _ci, _ci, ctypes.POINTER(_sz)]),
     "rlkv_cache_create": (_ci, [ctypes.POINTER(_vp), _ci, _ci, _ci, _ci, _ci, _ci, _vp, _ci, _ci, _vp, _sz]),
@@ -65,6 +65,11 @@ SIGNATURES = {
     "rlkv_paged_seq_close": (_ci, [_vp, _ci]),
     "rlkv_paged_append": (_ci, [_vp, _ci, _vp, _ci, _vp, _vp, _vp]),
     "rlkv_paged_prefill": (_ci, [_vp, _ci, _ci, _vp, _vp, _ci, _vp]),
+    "rlkv_paged_set_scores": (_ci, [_vp, ctypes.c_float, _vp]),
+    "rlkv_rotary_table": (_ci, [_vp, _ci, _ci, _vp, _vp]),
+    "rlkv_paged_set_rotary": (_ci, [_vp, _vp, _ci, _ci, _ci]),
+    "rlkv_paged_append_rotated": (_ci, [_vp, _ci, _vp, _ci, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
+    "rlkv_paged_prefill_rotated": (_ci, [_vp, _ci, _ci, _vp, _i64, _vp, _i64, _vp, _i64, _ci, _vp, _vp, _vp]),
     "rlkv_paged_decode_attention": (_ci, [_vp, _ci, _vp, _ci, _vp, _vp, _vp]),
     "rlkv_paged_step": (_ci, [_vp, _vp, _ci, _vp, _vp, _vp, _vp, _vp]),
     "rlkv_paged_length": (_ci, [_vp, _ci, _ci, ctypes.POINTER(_ci)]),
@@ -72,6 +77,12 @@ SIGNATURES = {
     "rlkv_paged_step_bytes": (_ci, [_vp, _ci, _vp, _ci, ctypes.POINTER(ctypes.c_uint64)]),
     "rlkv_paged_debug_export_head": (_ci, [_vp, _ci, _ci, _ci, _vp, _vp, ctypes.POINTER(_ci), _vp]),
     "rlkv_paged_kernel_status": (_ci, [_vp, ctypes.POINTER(_ci)]),
+    "rlkv_prompt_create": (_ci, [ctypes.POINTER(_vp), _ci, _ci, _ci, _ci, _ci, _vp, _ci, _ci, ctypes.c_float, _vp]),
+    "rlkv_prompt_destroy": (_ci, [_vp]),
+    "rlkv_prompt_attention": (_ci, [_vp, _ci, _vp, _i64, _vp, _i64, _vp, _i64, _ci, _ci, _vp, _vp, _ci, _vp, _vp, _vp, _vp]),
+    "rlkv_prompt_attention_backward": (_ci, [_vp, _ci, _vp, _i64, _vp, _i64, _vp, _i64, _ci, _ci, _vp, _vp, _ci, _vp, _vp, _vp, _vp,
+                                             _vp, _vp, _vp, _vp]),
+    "rlkv_prompt_kernel_status": (_ci, [_vp, ctypes.POINTER(_ci)]),
     "rlkv_debug_paged_schedule": (_ci, [_vp, _ci, _ci, _ci, _ci, _ci, _ci, ctypes.POINTER(_ci), _vp, _vp, _vp]),
 }
 
@@ -420,6 +431,42 @@ def rlkv_paged_prefill(cache, layer, slot, k, v, n_tokens, stream=None) -> None:
     _check(lib.rlkv_paged_prefill(cache, layer, slot, _ptr(k), _ptr(v), n_tokens, _stream(stream)))
 
 
+def _rows(x):
+    """(address, elements from token to token) of a [tokens][heads][head_dim] tensor, which may be a slice of a
+    wider projection; an address alone stands for contiguous tokens."""
+    if x is None or isinstance(x, (int, np.ndarray)):
+        return _ptr(x), 0
+    if x.dim() != 3 or x.stride(2) != 1 or x.stride(1) != x.shape[2]:
+        raise ValueError("tokens must be [tokens][heads][head_dim] with contiguous heads")
+    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else 0
+
+
+def rlkv_paged_set_scores(cache, softcap, slopes=None) -> None:
+    """slopes: host, [layers][q_heads] (the caller's to get right: the handle knows its own shape), or None."""
+    s = None if slopes is None else np.ascontiguousarray(slopes, dtype=np.float32)
+    _check(lib.rlkv_paged_set_scores(cache, float(softcap), 0 if s is None else s.ctypes.data))
+
+
+def rlkv_rotary_table(inv_freq, positions, table, stream=None) -> None:
+    f = np.ascontiguousarray(inv_freq, dtype=np.float64)
+    _check(lib.rlkv_rotary_table(f.ctypes.data, 2 * f.size, positions, _ptr(table), _stream(stream)))
+
+
+def rlkv_paged_set_rotary(cache, table, positions, rot_dim, interleaved=False) -> None:
+    _check(lib.rlkv_paged_set_rotary(cache, _ptr(table), positions, rot_dim, int(bool(interleaved))))
+
+
+def rlkv_paged_append_rotated(cache, layer, slots, q, k, v, q_out, stream=None) -> None:
+    s = np.ascontiguousarray(slots, dtype=np.int32)
+    _check(lib.rlkv_paged_append_rotated(cache, layer, s.ctypes.data, s.size, *_rows(q), *_rows(k), *_rows(v), _ptr(q_out),
+                                         _stream(stream)))
+
+
+def rlkv_paged_prefill_rotated(cache, layer, slot, q, k, v, n_tokens, q_out, k_out=None, stream=None) -> None:
+    _check(lib.rlkv_paged_prefill_rotated(cache, layer, slot, *_rows(q), *_rows(k), *_rows(v), n_tokens, _ptr(q_out),
+                                          _ptr(k_out), _stream(stream)))
+
+
 def rlkv_paged_decode_attention(cache, layer, slots, q, out, stream=None) -> None:
     s = _slots(slots)
     _check(lib.rlkv_paged_decode_attention(cache, layer, s.ctypes.data, s.size, _ptr(q), _ptr(out), _stream(stream)))
@@ -465,6 +512,53 @@ def rlkv_paged_debug_export_head(cache, layer, slot, kv_head, max_rows, head_dim
 def rlkv_paged_kernel_status(cache) -> int:
     out = _ci(0)
     _check(lib.rlkv_paged_kernel_status(cache, ctypes.byref(out)))
+    return int(out.value)
+
+
+# ---- attention over whole prompts ---------------------------------------------------------------
+
+
+def rlkv_prompt_create(layers, kv_heads, q_heads, head_dim, max_tokens, head_is_full, sink, window, softcap=0.0, slopes=None) -> int:
+    m = _mask(head_is_full)
+    if m.size != layers * kv_heads:
+        raise ValueError("head_is_full must have layers*kv_heads entries")
+    s = None if slopes is None else np.ascontiguousarray(slopes, dtype=np.float32)
+    if s is not None and s.size != layers * q_heads:
+        raise ValueError("slopes must have layers*q_heads entries")
+    handle = _vp(0)
+    _check(lib.rlkv_prompt_create(ctypes.byref(handle), layers, kv_heads, q_heads, head_dim, max_tokens, m.ctypes.data, sink,
+                                  window, float(softcap), 0 if s is None else s.ctypes.data))
+    return int(handle.value)
+
+
+def rlkv_prompt_destroy(prompt) -> None:
+    _check(lib.rlkv_prompt_destroy(prompt))
+
+
+def _prompt_args(q, k, v, q_starts, k_starts, prefix):
+    n_docs = q_starts.numel() - 1
+    if k_starts is not None and k_starts.numel() != n_docs + 1 or prefix is not None and prefix.numel() != n_docs:
+        raise ValueError("k_starts must have as many entries as q_starts, prefix one less")
+    if any(x is not None and x.element_size() != 4 for x in (q_starts, k_starts, prefix)):
+        raise ValueError("q_starts, k_starts and prefix are int32")
+    return (*_rows(q), *_rows(k), *_rows(v), q.shape[0], k.shape[0], _ptr(q_starts), _ptr(k_starts), n_docs, _ptr(prefix))
+
+
+def rlkv_prompt_attention(prompt, layer, q, k, v, q_starts, k_starts, prefix, out, lse, stream=None) -> None:
+    """q, k, v: [tokens][heads][head_dim], possibly slices of one projection's output; q_starts, k_starts, prefix: int32."""
+    _check(lib.rlkv_prompt_attention(prompt, layer, *_prompt_args(q, k, v, q_starts, k_starts, prefix), _ptr(out), _ptr(lse),
+                                     _stream(stream)))
+
+
+def rlkv_prompt_attention_backward(prompt, layer, q, k, v, q_starts, k_starts, prefix, out, lse, dout, dq, dk, dv,
+                                   stream=None) -> None:
+    _check(lib.rlkv_prompt_attention_backward(prompt, layer, *_prompt_args(q, k, v, q_starts, k_starts, prefix), _ptr(out),
+                                              _ptr(lse), _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv), _stream(stream)))
+
+
+def rlkv_prompt_kernel_status(prompt) -> int:
+    out = _ci(0)
+    _check(lib.rlkv_prompt_kernel_status(prompt, ctypes.byref(out)))
     return int(out.value)
 
 

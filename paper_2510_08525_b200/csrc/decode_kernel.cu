@@ -257,7 +257,7 @@ struct SegInfo {
     int uid, tile, band;   // the unit, the segment's first tile inside it, the band
     int tiles, len;        // tiles and valid rows of the unit
     int qrow, head, layer; // where its query and output rows are; its KV head; its layer (paged whole step)
-    int pad;
+    int n;                 // paged cache: tokens of the unit's sequence
 };
 constexpr int kSegRing = 8;  // segment descriptors in flight between producer and consumers
 
@@ -560,6 +560,45 @@ __device__ __forceinline__ void merge_units(const float* partials, float* out, i
 // the longest sequence); producer and consumers both leave out a unit's tiles past its own length and
 // realign the slot counter at every segment, and the producer looks a full unit's rows up in the
 // sequence's page table, whose entries for a segment it fetches with one bulk copy.
+
+// How a lane of a SCORED kernel turns the product q.k of one head with the key in row r of a unit into a
+// score in the log2 domain: cap * tanh(x / cap) - slope * (tokens between the query and the key), x = q.k /
+// sqrt(D).  tanh is computed from one exp2 and one division, 1 - 2 / (1 + e^2z): off by about 2^-22 of the cap
+// where the approximate tanh instruction would be off by 2^-11 of it, too much in an exponent.
+struct ScoreRule {
+    float s, cap2, slope2;  // factor of q.k; cap and slope times log2(e) (slope2 0: no distance term, cap2 0: no cap)
+    int last, sink, wrap;   // distance of row r: last - r, but newest - r of a ring row, plus the window where it is negative
+    int newest;
+    __device__ __forceinline__ float score(float qk, int r) const
+    {
+        float y = qk * s;
+        if (cap2 != 0.f) y = cap2 - __fdividef(2.f * cap2, 1.f + exp2f(y));  // (s then holds 2 log2(e) / cap as well)
+        if (slope2 != 0.f) {
+            int dist = last - r;
+            if (r >= sink) dist = newest - r + (r > newest ? wrap : 0);
+            y = fmaf(-slope2, (float)dist, y);
+        }
+        return y;
+    }
+};
+__device__ __forceinline__ ScoreRule score_rule(const PagedArgs& pg, float scale_log2, int layer, int q_heads, int q_head, int n,
+                                                bool full_unit)
+{
+    ScoreRule rule;
+    rule.cap2 = pg.softcap * 1.4426950408889634f;
+    rule.s = pg.softcap != 0.f ? 2.f * scale_log2 / pg.softcap : scale_log2;  // 2 z log2(e), z = x / cap
+    rule.slope2 = pg.slopes ? __ldg(pg.slopes + (size_t)layer * q_heads + q_head) * 1.4426950408889634f : 0.f;
+    rule.last = n - 1;
+    // a full head, or a ring that has not wrapped: row r is token r.  Else row sink + i holds the newest token that
+    // is congruent to i modulo the window (counted from the sink)
+    const int window = pg.cap - pg.sink;
+    const bool ring = !full_unit && n > pg.cap;
+    rule.sink = ring ? pg.sink : 0x7fffffff;
+    rule.newest = ring ? pg.sink + (n - 1 - pg.sink) % window : 0;
+    rule.wrap = window;
+    return rule;
+}
+
 struct NoPagedArgs {};
 template <int MODE>
 struct ExtraArgs {
@@ -578,7 +617,9 @@ struct ExtraArgs<kModeStep> {
     typedef StepArgs type;
 };
 
-template <int D, int NG, int MODE>
+// SCORED (paged cache): scores are capped by a tanh and lowered by the distance between query and key
+// (rlkv_paged_set_scores); a template parameter, so that plain scores pay nothing for it.
+template <int D, int NG, int MODE, bool SCORED = false>
 __global__ void __launch_bounds__(Smem<D, NG>::kThreads, 1)
 decode_kernel(const __grid_constant__ DecodeArgs args, const __grid_constant__ CUtensorMap tmap, const int stages,
               const __grid_constant__ typename ExtraArgs<MODE>::type extra)
@@ -790,6 +831,18 @@ decode_kernel(const __grid_constant__ DecodeArgs args, const __grid_constant__ C
                     const bool fp8_unit = FP8;  // every unit of an 8-bit cache is pages of E4M3 codes
                     int seg_eff = seg_tiles;  // tiles of the segment that exist (the producer announces no segment without any)
                     if (PAGED) seg_eff = max(0, min(seg_tiles, (u.len + kTile - 1) / kTile - u.pos.tile));
+                    // how this lane's heads turn a product q.k into a score: 8-bit cache heads 2tq and 2tq + 1,
+                    // else head `quad`
+                    ScoreRule rule, rule1;
+                    if constexpr (SCORED) {
+                        const int h0 = FP8 ? 2 * tq : quad;
+                        const float kscale = !FP8 ? 1.f
+                                             : pg->step.n_layers > 1 ? __ldg(pg->scales + u.layer * pg->step.kv_heads + u.head)
+                                                                     : pg->k_scale[u.head];
+                        const bool full_unit = u.pos.uid < sc.U;
+                        rule = score_rule(*pg, a.scale_log2 * kscale, u.layer, a.q_heads, u.head * G + min(h0, G - 1), sg.n, full_unit);
+                        if (FP8) rule1 = score_rule(*pg, a.scale_log2 * kscale, u.layer, a.q_heads, u.head * G + min(h0 + 1, G - 1), sg.n, full_unit);
+                    }
                     // skip the empty slots the producer issued to line the slot counter up with x (a new item
                     // may start anywhere; tiles a paged unit does not have shift the counter against x)
                     for (int pad = ((x - cnt) % NG + NG) % NG; alive && pad > 0; --pad, next_slot()) {
@@ -893,12 +946,20 @@ decode_kernel(const __grid_constant__ DecodeArgs args, const __grid_constant__ C
                                         e4m3x4_to_f16x2x2(kf[kp][3], a1, a3);  // set B, chunk 2kp + 1
                                         mma_f16(so, a0, a1, a2, a3, qa[2 * kp + 1][0], qa[2 * kp + 1][1]);
                                     }
+                                    // row `quad` of set A is token 4(quad/2) + quad%2 of the warp's 16, of set B two on
+                                    const int tokA = wig * 16 + 4 * (quad >> 1) + (quad & 1);
+                                    if constexpr (SCORED) {
+                                        const int row = (u.pos.tile + i + sb) * kTile + tokA;
+                                        sc8[sb][0] = rule.score(se[0] + so[0], row);
+                                        sc8[sb][1] = rule1.score(se[1] + so[1], row);
+                                        sc8[sb][2] = rule.score(se[2] + so[2], row + 2);
+                                        sc8[sb][3] = rule1.score(se[3] + so[3], row + 2);
+                                    } else {
                                     sc8[sb][0] = (se[0] + so[0]) * sl2;
                                     sc8[sb][1] = (se[1] + so[1]) * sl2;
                                     sc8[sb][2] = (se[2] + so[2]) * sl2;
                                     sc8[sb][3] = (se[3] + so[3]) * sl2;
-                                    // row `quad` of set A is token 4(quad/2) + quad%2 of the warp's 16, of set B two on
-                                    const int tokA = wig * 16 + 4 * (quad >> 1) + (quad & 1);
+                                    }
                                     if (tokA >= valid_sb) sc8[sb][0] = sc8[sb][1] = -INFINITY;
                                     if (tokA + 2 >= valid_sb) sc8[sb][2] = sc8[sb][3] = -INFINITY;
                                 }
@@ -989,11 +1050,19 @@ decode_kernel(const __grid_constant__ DecodeArgs args, const __grid_constant__ C
                             }
                             // this lane: head `quad`, tokens wig*16 + {2tq, 2tq+1, 8+2tq, 9+2tq}
                             float sc4[4];
+                            const int tok0 = wig * 16 + 2 * tq;
+                            if constexpr (SCORED) {
+                                const int row = (u.pos.tile + i) * kTile + tok0;
+                                sc4[0] = rule.score(s0[0] + s2[0], row);
+                                sc4[1] = rule.score(s0[1] + s2[1], row + 1);
+                                sc4[2] = rule.score(s1[0] + s3[0], row + 8);
+                                sc4[3] = rule.score(s1[1] + s3[1], row + 9);
+                            } else {
                             sc4[0] = (s0[0] + s2[0]) * a.scale_log2;
                             sc4[1] = (s0[1] + s2[1]) * a.scale_log2;
                             sc4[2] = (s1[0] + s3[0]) * a.scale_log2;
                             sc4[3] = (s1[1] + s3[1]) * a.scale_log2;
-                            const int tok0 = wig * 16 + 2 * tq;
+                            }
                             if (tok0 >= valid) sc4[0] = -INFINITY;
                             if (tok0 + 1 >= valid) sc4[1] = -INFINITY;
                             if (tok0 + 8 >= valid) sc4[2] = -INFINITY;
@@ -1178,6 +1247,7 @@ decode_kernel(const __grid_constant__ DecodeArgs args, const __grid_constant__ C
                 sg.qrow = u.qrow;
                 sg.head = u.head;
                 sg.layer = u.layer;
+                if (SCORED && item >= 0) sg.n = pg->seq_len[u.b];
                 mbar_arrive(smem_u32(seg_full + di));  // release: the descriptor is visible to the waiters
                 if (++di == kSegRing) {
                     di = 0;
@@ -1646,7 +1716,7 @@ decode_kernel(const __grid_constant__ DecodeArgs args, const __grid_constant__ C
     if (trace && tid == 0) my_trace[3] = global_timer_ns();
 }
 
-template <int D, int NG, int MODE>
+template <int D, int NG, int MODE, bool SCORED = false>
 cudaError_t launch_one(const DecodeArgs& a, const CUtensorMap& tmap, int grid, int stages, cudaStream_t stream,
                        bool overlap, const typename ExtraArgs<MODE>::type& extra)
 {
@@ -1661,7 +1731,7 @@ cudaError_t launch_one(const DecodeArgs& a, const CUtensorMap& tmap, int grid, i
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = overlap ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, decode_kernel<D, NG, MODE>, a, tmap, stages, extra);
+    return cudaLaunchKernelEx(&cfg, decode_kernel<D, NG, MODE, SCORED>, a, tmap, stages, extra);
 }
 
 template <int D, int NG>
@@ -1676,6 +1746,14 @@ cudaError_t prepare_one()
     if (e != cudaSuccess) return e;
     if (D == 128 && NG == 2) {  // 8-bit pages: head_dim 128, two consumer groups only
         e = cudaFuncSetAttribute(decode_kernel<128, 2, kModePagedFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 kMaxDynamicSmem);
+        if (e != cudaSuccess) return e;
+        e = cudaFuncSetAttribute(decode_kernel<128, 2, kModePagedFp8, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 kMaxDynamicSmem);
+        if (e != cudaSuccess) return e;
+    }
+    if (NG == 2) {  // the paged cache runs with two consumer groups
+        e = cudaFuncSetAttribute(decode_kernel<D, 2, kModePaged, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  kMaxDynamicSmem);
         if (e != cudaSuccess) return e;
     }
@@ -1725,7 +1803,13 @@ cudaError_t launch_decode(const DecodeArgs& a, const CUtensorMap* tmap, int head
     if (mode == kModeStep && !step) return cudaErrorInvalidValue;
     if (mode == kModePagedFp8) {
         if (!paged8 || head_dim != 128 || groups != 2) return cudaErrorInvalidValue;
+        if (paged8->pa.scored) return launch_one<128, 2, kModePagedFp8, true>(a, *tmap, grid, stages, stream, overlap, *paged8);
         return launch_one<128, 2, kModePagedFp8>(a, *tmap, grid, stages, stream, overlap, *paged8);
+    }
+    if (mode == kModePaged && paged->scored) {
+        if (groups != 2) return cudaErrorInvalidValue;
+        return head_dim == 128 ? launch_one<128, 2, kModePaged, true>(a, *tmap, grid, stages, stream, overlap, *paged)
+                               : launch_one<64, 2, kModePaged, true>(a, *tmap, grid, stages, stream, overlap, *paged);
     }
     if (head_dim == 128) {
         if (groups == 1) return launch_either<128, 1>(a, *tmap, grid, stages, stream, overlap, mode, paged, step);

@@ -350,6 +350,11 @@ struct PagedArgs {
     // ring0_8 + (s * n_comp + c) * ring_tiles on (ring row r in page r / 64, row r % 64).
     // x_hat = value(code) * scale with one scale per KV head (indexed by head) for K, V.
     int page0_8, ring0_8, ring_tiles;
+    // scores (rlkv_paged_set_scores): capped by softcap where it is not 0, lowered by slope * distance where
+    // slopes (device, [q_heads] of the launch's first layer, layer after layer) is not null; scored: either is set
+    int sink, scored;
+    float softcap;
+    const float* slopes;
     float k_scale[kMaxKvHeads], v_scale[kMaxKvHeads];
     int seq_len[kMaxPagedBatch];
     unsigned short seq_slot[kMaxPagedBatch];
@@ -657,5 +662,26 @@ struct PagedAppendArgs {
     unsigned short slot[kMaxPagedBatch];
 };
 cudaError_t launch_paged_append(const PagedAppendArgs& a, cudaStream_t stream);
+
+// The same append with the position rotation on the way (rows.k, rows.v and q `stride` elements from token to
+// token; rows.entry_stride is unused).  q may be null (no queries to turn), k_out may be null.
+struct RotatedAppendArgs {
+    PagedAppendArgs rows;
+    const __nv_bfloat16* q;     // [n][q_heads][head_dim]
+    __nv_bfloat16* q_out;       // contiguous
+    __nv_bfloat16* k_out;       // the rotated keys, contiguous [n][kv_heads][head_dim]
+    const float* table;         // [positions][rot / 2] (cos, sin)
+    long long q_stride, k_stride, v_stride;
+    int q_heads, rot, interleaved;
+};
+cudaError_t launch_rotated_append(const RotatedAppendArgs& a, cudaStream_t stream);
+
+constexpr int kMaxRotaryPairs = 64;
+struct RotaryTableArgs {
+    float2* table;
+    int positions, pairs;
+    double inv_freq[kMaxRotaryPairs];
+};
+cudaError_t launch_rotary_table(const RotaryTableArgs& a, cudaStream_t stream);
 
 }  // namespace rlkv

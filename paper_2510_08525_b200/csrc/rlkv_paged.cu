@@ -16,6 +16,7 @@
 //   tables      int32 slot_of_head[layers][kv_heads]
 //   page table  int32 [max_seqs][table_stride]   (written by the append kernels)
 //   layer desc  LayerDesc[layers]  (where each layer's regions start; for the step's append launch)
+//   slopes      float [layers][q_heads]  (rlkv_paged_set_scores)
 //   tickets     int32 [2][kMaxPagedBatch * kv_heads]
 //   status      int32 kernel status word, then two work-claim counters
 //   partials    float [2][max_slots][partial_floats]
@@ -56,12 +57,16 @@ struct rlkv_paged {
     std::vector<int> table;       // [max_seqs][table_stride], -1 = no page
     std::vector<int> free_pages;  // stack of physical pages
     std::vector<uint8_t> open;    // [max_seqs]
-    size_t off_pool, off_tables, off_head_table, off_layer_desc, off_page_table, off_tickets, off_status, off_partials, total;
+    size_t off_pool, off_tables, off_head_table, off_layer_desc, off_slopes, off_page_table, off_tickets, off_status, off_partials, total;
     unsigned int claims[2];
     uint8_t* dev_base;
     bool owns_buffer;
     CUtensorMap tmap;
     uint64_t launches;
+    const float* rotary;          // rlkv_paged_set_rotary: the caller's table of angles (device), null: none set
+    int rotary_rows, rotary_dim, rotary_interleaved;
+    float softcap;                // rlkv_paged_set_scores: 0 no cap
+    bool biased;                  // and whether scores are lowered by distance (slopes at off_slopes)
 };
 
 namespace {
@@ -165,6 +170,8 @@ int make_paged_layout(rlkv_paged& p, const uint8_t* mask, int max_seq_len)
     off = align_up(off + (size_t)p.layers * p.kv_heads * sizeof(int), 1024);
     p.off_layer_desc = off;
     off = align_up(off + (size_t)p.layers * sizeof(LayerDesc), 1024);
+    p.off_slopes = off;
+    off = align_up(off + (size_t)p.layers * p.q_heads * sizeof(float), 1024);
     p.off_page_table = off;
     off = align_up(off + (size_t)p.max_seqs * p.table_stride * sizeof(int), 1024);
     p.off_tickets = off;
@@ -284,6 +291,8 @@ static int paged_create(rlkv_paged** out, int layers, int kv_heads, int q_heads,
     p->max_seqs = max_seqs; p->n_pages = n_pages; p->sink = sink; p->window = window; p->max_seq_len = max_seq_len;
     p->claims[0] = p->claims[1] = 0; p->launches = 0; p->dev_base = nullptr; p->owns_buffer = false; p->out_bf16 = 0;
     p->step_mode = 0;
+    p->softcap = 0.f; p->biased = false;
+    p->rotary = nullptr; p->rotary_rows = p->rotary_dim = p->rotary_interleaved = 0;
     p->fp8 = fp8;
     if (fp8) {
         p->k_scale.assign(k_scale, k_scale + (size_t)layers * kv_heads);
@@ -410,7 +419,10 @@ int rlkv_paged_seq_close(rlkv_paged* p, int slot)
     return RLKV_OK;
 }
 
-int rlkv_paged_append(rlkv_paged* p, int layer, const int* slots, int n, const void* k, const void* v, void* stream)
+// One token for each of n sequences: what rlkv_paged_append and its rotated form share.  `rot`: the rotation
+// (null: none), whose `rows` are filled here.
+static int paged_append(rlkv_paged* p, int layer, const int* slots, int n, const void* k, const void* v, void* stream,
+                        RotatedAppendArgs* rot)
 {
     if (!valid_layer(p, layer) || !k || !v || !aligned16(k) || !aligned16(v)) return RLKV_EINVAL;
     int rc = check_slots(p, slots, n);
@@ -422,12 +434,14 @@ int rlkv_paged_append(rlkv_paged* p, int layer, const int* slots, int n, const v
     for (int i = 0; i < n; ++i) {
         const int t = len[slots[i]];
         if (t >= p->max_seq_len) return RLKV_EFULL;
+        if (rot && t >= p->rotary_rows) return RLKV_EINVAL;
         if (p->table[(size_t)slots[i] * p->table_stride + t / kTile] < 0) ++need;
     }
     if (need > (int)p->free_pages.size()) return RLKV_EFULL;
     DeviceGuard g(p->device);
     if (!g.ok) return RLKV_ECUDA;
-    PagedAppendArgs a;
+    PagedAppendArgs plain;
+    PagedAppendArgs& a = rot ? rot->rows : plain;
     fill_append_args(p, layer, k, v, a);
     a.prefill = 0;
     a.n = n;
@@ -444,15 +458,97 @@ int rlkv_paged_append(rlkv_paged* p, int layer, const int* slots, int n, const v
         a.t[i] = t;
         a.page[i] = entry;
     }
-    RLKV_CUDA(launch_paged_append(a, static_cast<cudaStream_t>(stream)));
+    if (rot) RLKV_CUDA(launch_rotated_append(*rot, static_cast<cudaStream_t>(stream)));
+    else RLKV_CUDA(launch_paged_append(a, static_cast<cudaStream_t>(stream)));
     for (int i = 0; i < n; ++i) len[slots[i]] += 1;
     p->launches++;
     return RLKV_OK;
 }
 
+int rlkv_paged_append(rlkv_paged* p, int layer, const int* slots, int n, const void* k, const void* v, void* stream)
+{
+    return paged_append(p, layer, slots, n, k, v, stream, nullptr);
+}
+
+int rlkv_rotary_table(const double* inv_freq, int rot_dim, int positions, void* table, void* stream)
+{
+    if (!inv_freq || !table || !aligned16(table) || rot_dim < 2 || rot_dim % 2 || rot_dim / 2 > kMaxRotaryPairs || positions < 1)
+        return RLKV_EINVAL;
+    cudaPointerAttributes at;
+    if (cudaPointerGetAttributes(&at, table) != cudaSuccess || at.type != cudaMemoryTypeDevice) {
+        cudaGetLastError();
+        return RLKV_EINVAL;
+    }
+    DeviceGuard g(at.device);
+    if (!g.ok) return RLKV_ECUDA;
+    RotaryTableArgs a;
+    a.table = static_cast<float2*>(table);
+    a.positions = positions;
+    a.pairs = rot_dim / 2;
+    for (int j = 0; j < kMaxRotaryPairs; ++j) a.inv_freq[j] = j < a.pairs ? inv_freq[j] : 0.0;
+    RLKV_CUDA(launch_rotary_table(a, static_cast<cudaStream_t>(stream)));
+    return RLKV_OK;
+}
+
+int rlkv_paged_set_rotary(rlkv_paged* p, const void* table, int positions, int rot_dim, int interleaved)
+{
+    if (!p) return RLKV_EINVAL;
+    if (table && (!aligned16(table) || positions < 1 || rot_dim < 16 || rot_dim % 16 || rot_dim > p->head_dim)) return RLKV_EINVAL;
+    p->rotary = static_cast<const float*>(table);
+    p->rotary_rows = table ? positions : 0;
+    p->rotary_dim = rot_dim;
+    p->rotary_interleaved = interleaved ? 1 : 0;
+    return RLKV_OK;
+}
+
+// The arguments of a rotated append that the two forms share; a stride of 0 stands for contiguous tokens.
+static int rotation_args(const rlkv_paged* p, const void* q, int64_t q_stride, int64_t k_stride, int64_t v_stride, void* q_out,
+                         void* k_out, RotatedAppendArgs& r)
+{
+    if (!p || !p->rotary || !q != !q_out || !aligned16(q) || !aligned16(q_out) || !aligned16(k_out)) return RLKV_EINVAL;
+    const int64_t q_row = (int64_t)p->q_heads * p->head_dim, kv_row = (int64_t)p->kv_heads * p->head_dim;
+    if (!q_stride) q_stride = q_row;
+    if (!k_stride) k_stride = kv_row;
+    if (!v_stride) v_stride = kv_row;
+    if (q_stride < q_row || k_stride < kv_row || v_stride < kv_row || q_stride % 8 || k_stride % 8 || v_stride % 8) return RLKV_EINVAL;
+    r.q = static_cast<const __nv_bfloat16*>(q);
+    r.q_out = static_cast<__nv_bfloat16*>(q_out);
+    r.k_out = static_cast<__nv_bfloat16*>(k_out);
+    r.table = p->rotary;
+    r.q_stride = q_stride;
+    r.k_stride = k_stride;
+    r.v_stride = v_stride;
+    r.q_heads = p->q_heads;
+    r.rot = p->rotary_dim;
+    r.interleaved = p->rotary_interleaved;
+    return RLKV_OK;
+}
+
+int rlkv_paged_append_rotated(rlkv_paged* p, int layer, const int* slots, int n, const void* q, int64_t q_stride, const void* k,
+                              int64_t k_stride, const void* v, int64_t v_stride, void* q_out, void* stream)
+{
+    RotatedAppendArgs r;
+    const int rc = rotation_args(p, q, q_stride, k_stride, v_stride, q_out, nullptr, r);
+    if (rc) return rc;
+    return paged_append(p, layer, slots, n, k, v, stream, &r);
+}
+
+static int paged_prefill(rlkv_paged* p, int layer, int slot, const void* k, const void* v, int n_tokens, long long entry_stride,
+                         void* stream, RotatedAppendArgs* rot);
+
 int rlkv_paged_prefill(rlkv_paged* p, int layer, int slot, const void* k, const void* v, int n_tokens, void* stream)
 {
     return rlkv::paged_prefill_strided(p, layer, slot, k, v, n_tokens, p ? (long long)p->kv_heads * p->head_dim : 0, stream);
+}
+
+int rlkv_paged_prefill_rotated(rlkv_paged* p, int layer, int slot, const void* q, int64_t q_stride, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride, int n_tokens, void* q_out, void* k_out,
+                               void* stream)
+{
+    RotatedAppendArgs r;
+    const int rc = rotation_args(p, q, q_stride, k_stride, v_stride, q_out, k_out, r);
+    if (rc) return rc;
+    return paged_prefill(p, layer, slot, k, v, n_tokens, (long long)p->kv_heads * p->head_dim, stream, &r);
 }
 
 }  // extern "C"
@@ -462,12 +558,20 @@ int rlkv_paged_prefill(rlkv_paged* p, int layer, int slot, const void* k, const 
 int rlkv::paged_prefill_strided(rlkv_paged* p, int layer, int slot, const void* k, const void* v, int n_tokens,
                                 long long entry_stride, void* stream)
 {
+    return paged_prefill(p, layer, slot, k, v, n_tokens, entry_stride, stream, nullptr);
+}
+
+// `rot`: the rotation, with strides of its own for q, k and v (null: none).
+static int paged_prefill(rlkv_paged* p, int layer, int slot, const void* k, const void* v, int n_tokens, long long entry_stride,
+                         void* stream, RotatedAppendArgs* rot)
+{
     if (!valid_layer(p, layer) || !valid_slot(p, slot) || !k || !v || !aligned16(k) || !aligned16(v) || n_tokens < 1 ||
         entry_stride < (long long)p->kv_heads * p->head_dim || entry_stride % 8 != 0)
         return RLKV_EINVAL;
     int* len = len_of(p, layer);
     const int t0 = len[slot];
     if ((long long)t0 + n_tokens > p->max_seq_len) return RLKV_EFULL;
+    if (rot && (long long)t0 + n_tokens > p->rotary_rows) return RLKV_EINVAL;
     const int first = t0 / kTile, last = (t0 + n_tokens - 1) / kTile;
     int* row = p->table.data() + (size_t)slot * p->table_stride;
     int need = 0;
@@ -483,16 +587,17 @@ int rlkv::paged_prefill_strided(rlkv_paged* p, int layer, int slot, const void* 
         }
     // launches of at most kMaxAppendPages pages each: every launch equals that many single appends,
     // bit for bit, and the launches run in order, so the whole equals n_tokens single appends
-    const size_t row_elems = (size_t)entry_stride;
+    const size_t k_row = (size_t)(rot ? rot->k_stride : entry_stride), v_row = (size_t)(rot ? rot->v_stride : entry_stride);
     for (int done = 0; done < n_tokens;) {
         const int t = t0 + done;
         const int page0 = t / kTile;
         int count = n_tokens - done;
         const int room = (page0 + kMaxAppendPages) * kTile - t;  // tokens up to the end of the last page the args can name
         if (count > room) count = room;
-        PagedAppendArgs a;
-        fill_append_args(p, layer, static_cast<const __nv_bfloat16*>(k) + (size_t)done * row_elems,
-                         static_cast<const __nv_bfloat16*>(v) + (size_t)done * row_elems, a);
+        PagedAppendArgs plain;
+        PagedAppendArgs& a = rot ? rot->rows : plain;
+        fill_append_args(p, layer, static_cast<const __nv_bfloat16*>(k) + (size_t)done * k_row,
+                         static_cast<const __nv_bfloat16*>(v) + (size_t)done * v_row, a);
         a.prefill = 1;
         a.entry_stride = entry_stride;
         a.n = count;
@@ -500,7 +605,16 @@ int rlkv::paged_prefill_strided(rlkv_paged* p, int layer, int slot, const void* 
         a.first_page = page0;
         a.slot[0] = (unsigned short)slot;
         for (int i = page0; i <= (t + count - 1) / kTile; ++i) a.page[i - page0] = row[i];
-        RLKV_CUDA(launch_paged_append(a, static_cast<cudaStream_t>(stream)));
+        if (rot) {
+            RLKV_CUDA(launch_rotated_append(*rot, static_cast<cudaStream_t>(stream)));
+            if (rot->q) {
+                rot->q += (size_t)count * rot->q_stride;
+                rot->q_out += (size_t)count * p->q_heads * p->head_dim;
+            }
+            if (rot->k_out) rot->k_out += (size_t)count * p->kv_heads * p->head_dim;
+        } else {
+            RLKV_CUDA(launch_paged_append(a, static_cast<cudaStream_t>(stream)));
+        }
         p->launches++;
         done += count;
     }
@@ -631,6 +745,10 @@ static int paged_decode(rlkv_paged* p, int layer, const int* slots, int n, const
         pa.seq_len[i] = i < n ? len[slots[i]] : 0;
         pa.seq_slot[i] = (unsigned short)(i < n ? slots[i] : 0);
     }
+    pa.sink = p->sink;
+    pa.softcap = p->softcap;
+    pa.slopes = p->biased ? dev_at<float>(p, p->off_slopes) + (size_t)layer * p->q_heads : nullptr;
+    pa.scored = p->softcap != 0.f || p->biased;
     pa.page0_8 = (int)p->page0_8[layer];
     pa.ring0_8 = (int)p->ring0_8[layer];
     pa.ring_tiles = p->rows_comp / kTile;
@@ -741,6 +859,27 @@ int rlkv_paged_set_output_bf16(rlkv_paged* p, int on)
 {
     if (!p) return RLKV_EINVAL;
     p->out_bf16 = on ? 1 : 0;
+    return RLKV_OK;
+}
+
+int rlkv_paged_set_scores(rlkv_paged* p, float softcap, const float* slopes)
+{
+    if (!p || !(softcap >= 0.f) || (softcap != 0.f && (softcap < 1e-3f || softcap > 1e6f))) return RLKV_EINVAL;
+    const size_t count = (size_t)p->layers * p->q_heads;
+    bool biased = false;
+    if (slopes)
+        for (size_t i = 0; i < count; ++i) {
+            if (!(fabsf(slopes[i]) <= 1e6f)) return RLKV_EINVAL;
+            if (slopes[i] != 0.f) biased = true;
+        }
+    DeviceGuard g(p->device);
+    if (!g.ok) return RLKV_ECUDA;
+    if (biased) {
+        RLKV_CUDA(cudaDeviceSynchronize());  // launches in flight read the slopes they were given
+        RLKV_CUDA(cudaMemcpy(p->dev_base + p->off_slopes, slopes, count * sizeof(float), cudaMemcpyHostToDevice));
+    }
+    p->softcap = softcap;
+    p->biased = biased;
     return RLKV_OK;
 }
 

@@ -162,14 +162,6 @@ __global__ void __launch_bounds__(256) prompt_keys_kernel(const __grid_constant_
 
 }  // namespace
 
-cudaError_t launch_prompt_forward(const PromptArgs& a, int head_dim, cudaStream_t stream)
-{
-    const dim3 grid((a.q_tokens + 7) / 8, a.q_heads);
-    if (head_dim == 128) prompt_rows_kernel<128, false><<<grid, 256, 0, stream>>>(a);
-    else prompt_rows_kernel<64, false><<<grid, 256, 0, stream>>>(a);
-    return cudaGetLastError();
-}
-
 cudaError_t launch_prompt_backward(const PromptArgs& a, int head_dim, cudaStream_t stream)
 {
     const dim3 rows((a.q_tokens + 7) / 8, a.q_heads), keys((a.k_tokens + 7) / 8, a.kv_heads);

@@ -73,6 +73,35 @@ int fill_prompt_args(const rlkv_prompt* p, int layer, const void* q, int64_t q_s
     return RLKV_OK;
 }
 
+// Tensor map over [tokens][heads][head_dim], tokens `stride` elements apart: boxes of 64 elements of one head of
+// `box_tokens` tokens, 128-byte swizzle.  Tokens past the end read as zero.
+int encode_heads_map(CUtensorMap* map, const void* base, int tokens, int heads, int head_dim, int64_t stride, int box_tokens)
+{
+    typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                      const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                      CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static void* volatile fn = nullptr;  // (two threads that look it up at once find the same)
+    if (!fn) {
+        void* found = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        RLKV_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &found, cudaEnableDefault, &q));
+        if (!found || q != cudaDriverEntryPointSuccess) return cuda_fail(cudaErrorNotSupported, "cuTensorMapEncodeTiled lookup");
+        fn = found;
+    }
+    const cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)tokens};
+    const cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t box[3] = {64, 1, (cuuint32_t)box_tokens};
+    const cuuint32_t one[3] = {1, 1, 1};
+    const CUresult r = reinterpret_cast<EncodeTiledFn>(fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides,
+                                                           box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        snprintf(g_cuda_text, sizeof g_cuda_text, "cuTensorMapEncodeTiled (prompt) failed with CUresult %d", (int)r);
+        return RLKV_ECUDA;
+    }
+    return RLKV_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -115,6 +144,7 @@ int rlkv_prompt_create(rlkv_prompt** out, int layers, int kv_heads, int q_heads,
     p->dev_base = static_cast<uint8_t*>(mem);
     e = cudaMemset(mem, 0, p->off_delta);
     if (e == cudaSuccess && biased) e = cudaMemcpy(p->dev_base + p->off_slopes, slopes, count * sizeof(float), cudaMemcpyHostToDevice);
+    if (e == cudaSuccess) e = prepare_prompt_kernels(head_dim);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();  // the memset is done before a call on any stream
     if (e != cudaSuccess) {
         cudaFree(mem);
@@ -145,7 +175,12 @@ int rlkv_prompt_attention(rlkv_prompt* p, int layer, const void* q, int64_t q_st
     if (rc) return rc;
     DeviceGuard g(p->device);
     if (!g.ok) return RLKV_ECUDA;
-    RLKV_CUDA(launch_prompt_forward(a, p->head_dim, static_cast<cudaStream_t>(stream)));
+    CUtensorMap map_q, map_k, map_v;
+    int e = encode_heads_map(&map_q, q, q_tokens, p->q_heads, p->head_dim, a.q_stride, 128);
+    if (!e) e = encode_heads_map(&map_k, k, k_tokens, p->kv_heads, p->head_dim, a.k_stride, 128);
+    if (!e) e = encode_heads_map(&map_v, v, k_tokens, p->kv_heads, p->head_dim, a.v_stride, 128);
+    if (e) return e;
+    RLKV_CUDA(launch_prompt_forward(a, map_q, map_k, map_v, p->head_dim, static_cast<cudaStream_t>(stream)));
     return RLKV_OK;
 }
 

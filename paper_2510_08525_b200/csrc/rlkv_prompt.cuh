@@ -41,7 +41,65 @@ __device__ __forceinline__ DocRange doc_range(const PromptArgs& a, int d)
     return r;
 }
 
-cudaError_t launch_prompt_forward(const PromptArgs& a, int head_dim, cudaStream_t stream);
+// Status codes of prompt attention (device error word): which wait ran out.
+enum : int { kPromptWaitLoad = 101, kPromptWaitProduct = 102, kPromptWaitSoftmax = 103, kPromptWaitStage = 104, kPromptWaitDrain = 105,
+             kPromptSmemMisaligned = 106 };
+
+// Tiles of `rows` queries, numbered from the LAST tile of the last document backwards (a causal document's last
+// tiles are its longest, and the longest are best started first).  Called by one whole warp; returns false where
+// there are no more than `index` tiles.  A lane counts the tiles of eight neighbouring documents per round.
+__device__ __forceinline__ bool find_tile(const PromptArgs& a, bool keys, int rows, int index, int& doc, int& tile)
+{
+    const int lane = threadIdx.x & 31;
+    int left = index;
+    for (int top = a.n_docs; top > 0; top -= 256) {
+        int n[8], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int d = top - 1 - lane * 8 - i;
+            n[i] = 0;
+            if (d >= 0) {
+                const DocRange r = doc_range(a, d);
+                n[i] = ((keys ? r.kn : r.qn) + rows - 1) / rows;
+            }
+            sum += n[i];
+        }
+        int upto = sum;  // inclusive scan over the lanes
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, upto > left);
+        if (hit) {
+            const int owner = __ffs(hit) - 1;
+            int d = 0, t = 0;
+            if (lane == owner) {
+                int rest = left - (upto - sum), i = 0;
+                while (rest >= n[i]) rest -= n[i++];
+                d = top - 1 - lane * 8 - i;
+                t = n[i] - 1 - rest;
+            }
+            doc = __shfl_sync(0xffffffffu, d, owner);
+            tile = __shfl_sync(0xffffffffu, t, owner);
+            return true;
+        }
+        left -= __shfl_sync(0xffffffffu, upto, 31);
+    }
+    return false;
+}
+
+// Bits c of 32 with lo <= c < hi.
+__device__ __forceinline__ uint32_t range_bits(int lo, int hi)
+{
+    const uint32_t below_hi = hi >= 32 ? ~0u : hi <= 0 ? 0u : (1u << hi) - 1u;
+    const uint32_t below_lo = lo >= 32 ? ~0u : lo <= 0 ? 0u : (1u << lo) - 1u;
+    return below_hi & ~below_lo;
+}
+
+cudaError_t launch_prompt_forward(const PromptArgs& a, const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
+                                  int head_dim, cudaStream_t stream);
+cudaError_t prepare_prompt_kernels(int head_dim);
 cudaError_t launch_prompt_backward(const PromptArgs& a, int head_dim, cudaStream_t stream);
 
 }  // namespace rlkv

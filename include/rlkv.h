@@ -396,7 +396,7 @@ int rlkv_debug_paged_schedule(const int* lens, int n, int n_full, int n_comp, in
 typedef struct rlkv_prompt rlkv_prompt;
 /* head_is_full: HOST [layers*kv_heads], slopes: HOST float [layers][q_heads] or NULL, both copied; softcap and slopes as
  * for rlkv_paged_set_scores.  max_tokens: most q_tokens of a call (it sizes the backward pass's scratch, max_tokens *
- * q_heads floats of device memory).  Shape limits are those of rlkv_cache_create.  Synchronous. */
+ * q_heads * 8 bytes of device memory).  Shape limits are those of rlkv_cache_create.  Synchronous. */
 int rlkv_prompt_create(rlkv_prompt** out, int layers, int kv_heads, int q_heads, int head_dim, int max_tokens,
                        const uint8_t* head_is_full, int sink, int window, float softcap, const float* slopes);
 int rlkv_prompt_destroy(rlkv_prompt* prompt);

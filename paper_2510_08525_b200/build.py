@@ -9,7 +9,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "librlkv.so")
 SOURCES = ["rlkv_api.cu", "rlkv_paged.cu", "rlkv_prompt.cu", "append_kernel.cu", "rotary_kernel.cu", "decode_kernel.cu",
-           "prompt_forward.cu", "prompt_kernel.cu", "probe_kernel.cu"]
+           "prompt_forward.cu", "prompt_backward.cu", "probe_kernel.cu"]
 HEADERS = ["rlkv_internal.cuh", "rlkv_host.cuh", "rlkv_prompt.cuh", "tcgen05.cuh", os.path.join("..", "..", "include", "rlkv.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]

@@ -1,0 +1,726 @@
+// The backward pass of prompt attention on the tensor cores, in three launches without atomics:
+//
+//   stats   D_i = sum over head_dim of dout * out, stored with lse (log2 domain) per head and query
+//   keys    one CTA per 128 keys of a KV head: over the queries that see them (64 at a time, every query head of the
+//           group), S^T = K.Q^T and dP^T = V.dO^T, then dV += P^T.dO and dK += dS^T.Q
+//   rows    one CTA per 256 queries of a head: over their keys (64 at a time), S = Q.K^T and dP = dO.V^T, then
+//           dQ += dS.K
+//
+// S and dP are computed twice, seven products where five would do, and in return every gradient is summed by one CTA
+// in a fixed order: no atomics on dQ, no fp32 copy of it in memory, the same bits on every run.  P and dS are written
+// to tensor memory as bf16 over S and dP and are the A operand of the second products straight from there.  Two
+// warpgroups alternate -- over query tiles in `keys`, over 128-row sub-tiles in `rows` -- so that one's products run
+// beside the other's arithmetic.
+#include "rlkv_prompt.cuh"
+#include "tcgen05.cuh"
+
+namespace rlkv {
+namespace {
+
+using namespace tc;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kRows = 128;  // rows of a product's result: keys (keys kernel) or queries (rows kernel)
+constexpr int kCols = 64;   // its columns: queries or keys
+constexpr int kRowBlock = kRows * 128, kColBlock = kCols * 128;  // bytes of a block of 64 elements of so many rows
+constexpr int kThreads = 384;
+
+// ---- D and lse ---------------------------------------------------------------------------------------
+
+// One warp per head and 32 queries; half a warp reads a row.  Stored head by head, so that the keys kernel reads
+// consecutive queries.  A query that sees nothing gets lse = +infinity: its P is then exp2(s - infinity) = 0.
+template <int D>
+__global__ void __launch_bounds__(256) prompt_stats_kernel(const __grid_constant__ PromptArgs a)
+{
+    constexpr int E = D / 16;  // elements of a lane
+    const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
+    const int h = blockIdx.y * 8 + (threadIdx.x >> 5);
+    if (h >= a.q_heads) return;
+    const int t0 = blockIdx.x * 32;
+    float mine = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+        const int t = t0 + 2 * i + half;
+        float s = 0.f;
+        if (t < a.q_tokens) {
+            const long long at = ((long long)t * a.q_heads + h) * D + l16 * E;
+            __nv_bfloat162 x[E / 2], y[E / 2];
+            if (E == 8) {
+                *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(a.out + at);
+                *reinterpret_cast<uint4*>(y) = *reinterpret_cast<const uint4*>(a.dout + at);
+            } else {
+                *reinterpret_cast<uint2*>(x) = *reinterpret_cast<const uint2*>(a.out + at);
+                *reinterpret_cast<uint2*>(y) = *reinterpret_cast<const uint2*>(a.dout + at);
+            }
+#pragma unroll
+            for (int e = 0; e < E / 2; ++e) {
+                const float2 u = __bfloat1622float2(x[e]), w = __bfloat1622float2(y[e]);
+                s = fmaf(u.x, w.x, s);
+                s = fmaf(u.y, w.y, s);
+            }
+        }
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        const float even = __shfl_sync(0xffffffffu, s, 0), odd = __shfl_sync(0xffffffffu, s, 16);
+        if (lane == 2 * i) mine = even;
+        if (lane == 2 * i + 1) mine = odd;
+    }
+    const int t = t0 + lane;
+    if (t < a.q_tokens) {
+        const float lse = a.lse[(long long)t * a.q_heads + h];
+        a.stats[(long long)h * a.q_tokens + t] = make_float2(lse == -INFINITY ? INFINITY : lse * kLog2e, mine);
+    }
+}
+
+// ---- what both kernels do with a score ------------------------------------------------------------------
+
+struct ScoreConst {
+    float sl2, cap2, zs;  // scale * log2(e); cap * log2(e); scale / cap
+};
+
+// 32 products q.k -> scores in the log2 domain, and (CAP) the slopes of the cap, 1 - tanh^2.  `big`: some |z| of the
+// warp is beyond the series.
+template <bool CAP>
+__device__ __forceinline__ void capped(const ScoreConst& k, bool vote, float (&s)[32], float (&f)[CAP ? 32 : 1])
+{
+    if constexpr (!CAP) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) s[c] *= k.sl2;
+    } else {
+        float big = 0.f;
+#pragma unroll
+        for (int c = 0; c < 32; ++c) big = fmaxf(big, fabsf(s[c]));
+        if (__any_sync(0xffffffffu, vote && big * k.zs > 0.3f)) {
+            const float e2 = 2.f * kLog2e * k.zs;
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+                const float t = 1.f - __fdividef(2.f, 1.f + ex2(s[c] * e2));
+                s[c] = t * k.cap2;
+                f[c] = fmaf(-t, t, 1.f);
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+                const float z = s[c] * k.zs, y = z * z;
+                const float t = z * fmaf(y, fmaf(y, fmaf(y, fmaf(y, 62.f / 2835, -17.f / 315), 2.f / 15), -1.f / 3), 1.f);
+                s[c] = t * k.cap2;
+                f[c] = fmaf(-t, t, 1.f);
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ void load32(uint32_t addr, float (&s)[32])
+{
+    tmem_ld32(addr, s);
+    wait_ld();
+#pragma unroll
+    for (int c = 0; c < 32; ++c) asm volatile("" : "+f"(s[c]));  // nothing of it is used before the wait
+}
+
+__device__ __forceinline__ void store_row(__nv_bfloat16* dst, uint32_t src, int cols, float scale, bool any, bool mine)
+{
+    for (int c = 0; c < cols; c += 32) {
+        float o[32];
+        if (any) load32(src + c, o);
+        else
+            for (int i = 0; i < 32; ++i) o[i] = 0.f;
+        if (mine) {
+            uint4* p = reinterpret_cast<uint4*>(dst + c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                p[i] = make_uint4(bf16x2(o[8 * i] * scale, o[8 * i + 1] * scale), bf16x2(o[8 * i + 2] * scale, o[8 * i + 3] * scale),
+                                  bf16x2(o[8 * i + 4] * scale, o[8 * i + 5] * scale), bf16x2(o[8 * i + 6] * scale, o[8 * i + 7] * scale));
+        }
+    }
+}
+
+// rows x 64 elements of one head from token `token` on: boxes of 64 tokens, D / 64 of them side by side.
+template <int D>
+__device__ __forceinline__ void load_rows(uint32_t dst, int rows, const CUtensorMap* map, int head, int token, uint32_t bar)
+{
+    for (int b = 0; b < D / 64; ++b)
+        for (int r = 0; r < rows; r += 64) load_box(dst + b * rows * 128 + r * 128, map, b * 64, head, token + r, bar);
+}
+
+// ---- dK and dV ------------------------------------------------------------------------------------------
+
+template <int D>
+struct Keys {
+    static constexpr int kRowTile = kRows * D * 2, kColTile = kCols * D * 2;
+    static constexpr int kStages = 4;  // (even: a stage is always used by the same warpgroup)
+    static constexpr int kStats = 2 * kRowTile + kStages * 2 * kColTile;
+    static constexpr int kSmem = kStats + kStages * kCols * 8 + 1024;
+};
+
+struct KeysShared {
+    uint64_t kv_full, full[4], empty[4], ready[4], sd_full[2], pds_full[2], done, drain;
+    uint32_t tmem;
+    int abort, valid;
+    int k0, rows, j0, q0, qn, off, prefix, u0, n_u;  // the CTA's keys; first query tile that sees them, and how many
+};
+
+template <int D, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(kThreads, 1)
+prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do)
+{
+    using F = Keys<D>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    float2* stats = reinterpret_cast<float2*>(smem + F::kStats);
+    KeysShared& sh = *reinterpret_cast<KeysShared*>(smem + F::kStats + F::kStages * kCols * 8);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int kv_head = blockIdx.x % a.kv_heads;
+    const bool full_head = a.full[kv_head] != 0;
+    volatile int* abort_flag = &sh.abort;
+
+    if ((smem_u32(smem) & 1023u) != 0) {
+        if (tid == 0) atomicCAS(a.status, 0, kPromptSmemMisaligned);
+        return;
+    }
+    if (warp == 0) {
+        int doc = 0, tile = 0;
+        const bool valid = find_tile(a, true, kRows, blockIdx.x / a.kv_heads, doc, tile);
+        if (lane == 0) {
+            sh.valid = valid;
+            sh.abort = 0;
+            if (valid) {
+                const DocRange r = doc_range(a, doc);
+                tile = (r.kn + kRows - 1) / kRows - 1 - tile;  // a document's first keys are seen by the most queries
+                const int j0 = tile * kRows, j1 = min(j0 + kRows, r.kn), off = r.kn - r.qn;
+                sh.k0 = r.k0 + j0;
+                sh.rows = j1 - j0;
+                sh.j0 = j0;
+                sh.q0 = r.q0;
+                sh.qn = r.qn;
+                sh.off = off;
+                sh.prefix = r.prefix;
+                // queries lower .. upper-1 see some key of the tile
+                const int lower = j0 < r.prefix ? 0 : max(0, j0 - off);
+                const int upper = full_head || j0 < a.sink ? r.qn : min(r.qn, j1 - 1 + a.window - off);
+                sh.u0 = lower / kCols;
+                sh.n_u = upper > lower ? (upper + kCols - 1) / kCols - sh.u0 : 0;
+            }
+            mbar_init(smem_u32(&sh.kv_full), 1);
+            for (int i = 0; i < F::kStages; ++i) {
+                mbar_init(smem_u32(&sh.full[i]), 1);
+                mbar_init(smem_u32(&sh.empty[i]), 1);
+                mbar_init(smem_u32(&sh.ready[i]), 1);
+            }
+            for (int w = 0; w < 2; ++w) {
+                mbar_init(smem_u32(&sh.sd_full[w]), 1);
+                mbar_init(smem_u32(&sh.pds_full[w]), 4);
+            }
+            mbar_init(smem_u32(&sh.done), 1);
+            mbar_init(smem_u32(&sh.drain), 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+    }
+    __syncthreads();
+    if (!sh.valid) return;
+    if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 512);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = sh.tmem, dV = tmem + 256, dK = tmem + 256 + D;
+    const uint32_t k_smem = smem_u32(smem), v_smem = k_smem + F::kRowTile, ring = v_smem + F::kRowTile;
+    const int n_u = sh.n_u, steps = n_u * a.group;  // step n: query tile u0 + n % n_u of query head n / n_u of the group
+
+    if (warp < 8) {
+        // ------------------------------------------------------------------ P and dS, one thread per key
+        const int w = warp >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t S = tmem + lanes + w * 128, dP = S + 64;
+        const int j = sh.j0 + row, j_last = sh.j0 + sh.rows - 1;
+        const bool mine = row < sh.rows;
+        // the key is seen from positions lo .. hi-1
+        const int lo = j < sh.prefix ? INT_MIN / 2 : j, hi = full_head || j < a.sink ? INT_MAX / 2 : j + a.window;
+        const ScoreConst sc{a.scale * kLog2e, a.softcap * kLog2e, CAP ? a.scale / a.softcap : 0.f};
+        bool ok = true;
+        int g = 0, u = w;  // of step n
+        while (n_u > 0 && u >= n_u) { u -= n_u; ++g; }
+        for (int n = w; ok && n < steps; n += 2) {
+            const int st = n % F::kStages;
+            ok = wait(smem_u32(&sh.ready[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad) &&
+                 wait(smem_u32(&sh.sd_full[w]), n >> 1 & 1, abort_flag, a.status, kPromptWaitProduct);
+            if (!ok) break;
+            fence_after();
+            const float4* stat = reinterpret_cast<const float4*>(stats + st * kCols);
+            const int p0 = (sh.u0 + u) * kCols + sh.off;  // position of column 0
+            const bool past = p0 >= j_last;               // every query at or behind every key
+            const bool plain = (past || j_last < sh.prefix) && (full_head || j_last < a.sink || p0 + kCols - 1 < sh.j0 + a.window);
+            const float slope2 = BIAS ? a.slopes[kv_head * a.group + g] * kLog2e : 0.f;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                float s[32], f[CAP ? 32 : 1];
+                load32(S + half * 32, s);
+                capped<CAP>(sc, mine, s, f);
+                const int d0 = p0 + half * 32 - j;  // distance of column 0
+                if (BIAS) {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) s[c] = fmaf(-slope2, fabsf((float)(d0 + c)), s[c]);
+                }
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) {
+                    const float4 x = stat[half * 16 + c / 2];  // (lse, D) of two queries
+                    s[c] = ex2(s[c] - x.x);
+                    s[c + 1] = ex2(s[c + 1] - x.z);
+                }
+                if (!plain) {
+                    const uint32_t see = range_bits(lo - j - d0, hi - j - d0);
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) s[c] = see >> c & 1 ? s[c] : 0.f;
+                }
+                uint32_t packed[16];
+#pragma unroll
+                for (int c = 0; c < 16; ++c) packed[c] = bf16x2(s[2 * c], s[2 * c + 1]);
+                tmem_st16(S + half * 16, packed);
+                float d[32];
+                load32(dP + half * 32, d);
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) {
+                    const float4 x = stat[half * 16 + c / 2];
+                    d[c] = s[c] * (d[c] - x.y);
+                    d[c + 1] = s[c + 1] * (d[c + 1] - x.w);
+                    if constexpr (CAP) {
+                        d[c] *= f[c];
+                        d[c + 1] *= f[c + 1];
+                    }
+                    packed[c / 2] = bf16x2(d[c], d[c + 1]);
+                }
+                tmem_st16(dP + half * 16, packed);
+            }
+            wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.pds_full[w]));
+            u += 2;
+            while (u >= n_u) { u -= n_u; ++g; }
+        }
+        if (ok && steps > 0) {
+            ok = wait(smem_u32(&sh.done), 0, abort_flag, a.status, kPromptWaitProduct);
+            fence_after();
+        }
+        if (ok) {
+            const long long at = ((long long)(sh.k0 + row) * a.kv_heads + kv_head) * D;
+            if (w == 0) store_row(a.dv + at, dV + lanes, D, 1.f, steps > 0, mine);
+            else store_row(a.dk + at, dK + lanes, D, a.scale, steps > 0, mine);
+        }
+    } else if (warp == 8) {
+        // ------------------------------------------------------------------ tile loads
+        if (lane == 0 && steps > 0) {
+            mbar_expect_tx(smem_u32(&sh.kv_full), 2 * F::kRowTile);
+            load_rows<D>(k_smem, kRows, &map_k, kv_head, sh.k0, smem_u32(&sh.kv_full));
+            load_rows<D>(v_smem, kRows, &map_v, kv_head, sh.k0, smem_u32(&sh.kv_full));
+            int n = 0, g = 0, u = 0;
+            bool ok = true;
+            for (; n < steps; ++n) {
+                const int st = n % F::kStages;
+                ok = wait(smem_u32(&sh.empty[st]), (n / F::kStages & 1) ^ 1, abort_flag, a.status, kPromptWaitStage);
+                if (!ok) break;
+                const uint32_t bar = smem_u32(&sh.full[st]), dst = ring + st * 2 * F::kColTile;
+                mbar_expect_tx(bar, 2 * F::kColTile);
+                const int token = sh.q0 + (sh.u0 + u) * kCols;
+                load_rows<D>(dst, kCols, &map_q, kv_head * a.group + g, token, bar);
+                load_rows<D>(dst + F::kColTile, kCols, &map_do, kv_head * a.group + g, token, bar);
+                if (++u == n_u) { u = 0; ++g; }
+            }
+            if (!ok || *abort_flag) {  // nothing of this CTA's copies may be in flight when it ends
+                wait(smem_u32(&sh.kv_full), 0, nullptr, a.status, kPromptWaitDrain);
+                for (int i = max(0, n - F::kStages); i < n; ++i)
+                    wait(smem_u32(&sh.full[i % F::kStages]), i / F::kStages & 1, nullptr, a.status, kPromptWaitDrain);
+            }
+        }
+    } else if (warp == 9) {
+        // ------------------------------------------------------------------ matrix products
+        if (lane == 0 && steps > 0) {
+            constexpr uint32_t kScores = instr_desc(kRows, kCols, false), kGrads = instr_desc(kRows, D, true);
+            auto first_products = [&](int n) {
+                const int st = n % F::kStages;
+                if (!wait(smem_u32(&sh.full[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad) ||
+                    !wait(smem_u32(&sh.ready[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad))
+                    return false;
+                const uint32_t q = ring + st * 2 * F::kColTile, o = q + F::kColTile, d = tmem + (n & 1) * 128;
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x) {
+                    const uint32_t ra = x / 4 * kRowBlock + x % 4 * 32, cb = x / 4 * kColBlock + x % 4 * 32;
+                    mma_ss(d, smem_desc(k_smem + ra), smem_desc(q + cb), kScores, x > 0);
+                }
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x) {
+                    const uint32_t ra = x / 4 * kRowBlock + x % 4 * 32, cb = x / 4 * kColBlock + x % 4 * 32;
+                    mma_ss(d + 64, smem_desc(v_smem + ra), smem_desc(o + cb), kScores, x > 0);
+                }
+                commit(smem_u32(&sh.sd_full[n & 1]));
+                return true;
+            };
+            bool ok = wait(smem_u32(&sh.kv_full), 0, abort_flag, a.status, kPromptWaitLoad) && first_products(0);
+            if (ok && steps > 1) ok = first_products(1);
+            for (int n = 0; ok && n < steps; ++n) {
+                const int st = n % F::kStages, w = n & 1;
+                ok = wait(smem_u32(&sh.pds_full[w]), n >> 1 & 1, abort_flag, a.status, kPromptWaitSoftmax);
+                if (!ok) break;
+                fence_after();
+                const uint32_t q = ring + st * 2 * F::kColTile, o = q + F::kColTile, d = tmem + w * 128;
+#pragma unroll
+                for (int x = 0; x < kCols / 16; ++x) mma_ts(dV, d + x * 8, smem_desc(o + x * 2048, kColBlock), kGrads, n > 0 || x > 0);
+#pragma unroll
+                for (int x = 0; x < kCols / 16; ++x) mma_ts(dK, d + 64 + x * 8, smem_desc(q + x * 2048, kColBlock), kGrads, n > 0 || x > 0);
+                commit(smem_u32(&sh.empty[st]));
+                if (n + 2 < steps) ok = first_products(n + 2);
+            }
+            commit(smem_u32(&sh.done));
+            commit(smem_u32(&sh.drain));
+            wait(smem_u32(&sh.drain), 0, nullptr, a.status, kPromptWaitDrain);
+        }
+    } else if (warp == 10) {
+        // ------------------------------------------------------------------ lse and D of the query tiles; rows behind the
+        // last query: lse +infinity (P = 0), and zeros for what another document or nobody holds there (0 * NaN)
+        int g = 0, u = 0;
+        auto fetch = [&](float2 (&x)[2]) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int q = (sh.u0 + u) * kCols + lane + 32 * i;
+                x[i] = q < sh.qn ? a.stats[(long long)(kv_head * a.group + g) * a.q_tokens + sh.q0 + q] : make_float2(INFINITY, 0.f);
+            }
+        };
+        float2 next[2];
+        if (steps > 0) fetch(next);
+        for (int n = 0; n < steps; ++n) {
+            const int st = n % F::kStages, valid = sh.qn - (sh.u0 + u) * kCols;
+            const float2 now[2] = {next[0], next[1]};
+            if (++u == n_u) { u = 0; ++g; }
+            if (n + 1 < steps) fetch(next);
+            if (!wait(smem_u32(&sh.empty[st]), (n / F::kStages & 1) ^ 1, abort_flag, a.status, kPromptWaitStage)) break;
+            stats[st * kCols + lane] = now[0];
+            stats[st * kCols + lane + 32] = now[1];
+            if (!wait(smem_u32(&sh.full[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad)) break;
+            if (valid < kCols) {
+                uint8_t* x = smem + 2 * F::kRowTile + st * 2 * F::kColTile;
+                for (int i = valid * 8 + lane; i < kCols * 8; i += 32)
+                    for (int b = 0; b < 2 * D / 64; ++b) *reinterpret_cast<uint4*>(x + b * kColBlock + i * 16) = make_uint4(0, 0, 0, 0);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.ready[st]));
+        }
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == 9) {
+        __syncwarp();
+        tmem_free(tmem, 512);
+    }
+}
+
+// ---- dQ ----------------------------------------------------------------------------------------------------
+
+template <int D>
+struct RowsK {
+    static constexpr int kRowTile = kRows * D * 2, kColTile = kCols * D * 2;
+    static constexpr int kStages = D == 128 ? 3 : 6;
+    static constexpr int kSmem = 4 * kRowTile + kStages * 2 * kColTile + 1024;
+};
+
+struct RowsShared {
+    uint64_t q_full, full[6], empty[6], sd_full[2], ds_full[2], done, clean, drain;
+    uint32_t tmem;
+    int abort, valid;
+    int q0, rows, pos0, k0, kn, prefix, a_end, b0, n_tiles;  // as in the forward pass, key tiles of 64
+};
+
+template <int D, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(kThreads, 1)
+prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do)
+{
+    using F = RowsK<D>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    RowsShared& sh = *reinterpret_cast<RowsShared*>(smem + 4 * F::kRowTile + F::kStages * 2 * F::kColTile);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int head = blockIdx.x % a.q_heads, kv_head = head / a.group;
+    const bool full_head = a.full[kv_head] != 0;
+    volatile int* abort_flag = &sh.abort;
+
+    if ((smem_u32(smem) & 1023u) != 0) {
+        if (tid == 0) atomicCAS(a.status, 0, kPromptSmemMisaligned);
+        return;
+    }
+    if (warp == 0) {
+        int doc = 0, tile = 0;
+        const bool valid = find_tile(a, false, 2 * kRows, blockIdx.x / a.q_heads, doc, tile);
+        if (lane == 0) {
+            sh.valid = valid;
+            sh.abort = 0;
+            if (valid) {
+                const DocRange r = doc_range(a, doc);
+                sh.q0 = r.q0 + tile * 2 * kRows;
+                sh.rows = min(2 * kRows, r.qn - tile * 2 * kRows);
+                sh.pos0 = tile * 2 * kRows + r.kn - r.qn;
+                sh.k0 = r.k0;
+                sh.kn = r.kn;
+                sh.prefix = r.prefix;
+                const int hi = min(r.kn, max(sh.pos0 + sh.rows, r.prefix));
+                const int end = hi > 0 ? (hi + kCols - 1) / kCols : 0;
+                int a_end = end, b0 = end;
+                if (!full_head) {
+                    a_end = min(end, (min(a.sink, max(hi, 0)) + kCols - 1) / kCols);
+                    b0 = max(a_end, max(0, sh.pos0 - a.window + 1) / kCols);
+                }
+                sh.a_end = a_end;
+                sh.b0 = b0;
+                sh.n_tiles = a_end + max(0, end - b0);
+            }
+            mbar_init(smem_u32(&sh.q_full), 1);
+            for (int i = 0; i < F::kStages; ++i) {
+                mbar_init(smem_u32(&sh.full[i]), 1);
+                mbar_init(smem_u32(&sh.empty[i]), 1);
+            }
+            for (int w = 0; w < 2; ++w) {
+                mbar_init(smem_u32(&sh.sd_full[w]), 1);
+                mbar_init(smem_u32(&sh.ds_full[w]), 4);
+            }
+            mbar_init(smem_u32(&sh.done), 1);
+            mbar_init(smem_u32(&sh.clean), 1);
+            mbar_init(smem_u32(&sh.drain), 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+    }
+    __syncthreads();
+    if (!sh.valid) return;
+    if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 512);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = sh.tmem;
+    const int n_tiles = sh.n_tiles, a_end = sh.a_end, b0 = sh.b0, kn = sh.kn, prefix = sh.prefix;
+    const uint32_t q_smem = smem_u32(smem), o_smem = q_smem + 2 * F::kRowTile, ring = q_smem + 4 * F::kRowTile;
+    const int n_sub = sh.rows > kRows ? 2 : 1;
+    auto tile_at = [&](int j) { return j < a_end ? j : b0 + j - a_end; };
+    auto needed = [&](int w, int t) {  // does any query of sub-tile w see a key of tile t?
+        if (w >= n_sub) return false;
+        const int first = sh.pos0 + w * kRows, last = first + min(kRows, sh.rows - w * kRows) - 1, start = t * kCols;
+        if (start >= min(kn, max(last + 1, prefix))) return false;
+        return full_head || start < a.sink || start + kCols > first - a.window + 1;
+    };
+
+    if (warp < 8) {
+        // ------------------------------------------------------------------ P and dS, one thread per query
+        const int w = warp >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t S = tmem + lanes + w * 128, dP = S + 64;
+        const int first = sh.pos0 + w * kRows, pos = first + row, last = first + kRows - 1;
+        const bool mine = w * kRows + row < sh.rows;
+        const int hi = min(kn, max(pos + 1, prefix)), lo = full_head ? 0 : pos - a.window + 1, sink = full_head ? 0 : min(a.sink, hi);
+        const ScoreConst sc{a.scale * kLog2e, a.softcap * kLog2e, CAP ? a.scale / a.softcap : 0.f};
+        const float slope2 = BIAS ? a.slopes[head] * kLog2e : 0.f;
+        const int q = sh.q0 + w * kRows + row;
+        const float2 stat = mine ? a.stats[(long long)head * a.q_tokens + q] : make_float2(INFINITY, 0.f);
+        bool ok = true;
+        int done = 0;
+        for (int j = 0; ok && j < n_tiles; ++j) {
+            const int t = tile_at(j), start = t * kCols;
+            if (!needed(w, t)) continue;
+            ok = wait(smem_u32(&sh.sd_full[w]), done & 1, abort_flag, a.status, kPromptWaitProduct);
+            if (!ok) break;
+            fence_after();
+            const bool plain = start + kCols <= kn && (start + kCols <= first + 1 || start + kCols <= prefix) &&
+                               (full_head || start + kCols <= a.sink || start > last - a.window);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                float s[32], f[CAP ? 32 : 1];
+                load32(S + half * 32, s);
+                capped<CAP>(sc, mine, s, f);
+                const int c0 = start + half * 32;
+                if (BIAS) {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) s[c] = fmaf(-slope2, fabsf((float)(pos - c0 - c)), s[c]);
+                }
+#pragma unroll
+                for (int c = 0; c < 32; ++c) s[c] = ex2(s[c] - stat.x);
+                if (!plain) {
+                    const uint32_t see = range_bits(lo - c0, hi - c0) | range_bits(0, sink - c0);
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) s[c] = see >> c & 1 ? s[c] : 0.f;
+                }
+                float d[32];
+                load32(dP + half * 32, d);
+                uint32_t packed[16];
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) {
+                    d[c] = s[c] * (d[c] - stat.y);
+                    d[c + 1] = s[c + 1] * (d[c + 1] - stat.y);
+                    if constexpr (CAP) {
+                        d[c] *= f[c];
+                        d[c + 1] *= f[c + 1];
+                    }
+                    packed[c / 2] = bf16x2(d[c], d[c + 1]);
+                }
+                tmem_st16(dP + half * 16, packed);
+            }
+            wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.ds_full[w]));
+            ++done;
+        }
+        if (ok && n_tiles > 0) {
+            ok = wait(smem_u32(&sh.done), 0, abort_flag, a.status, kPromptWaitProduct);
+            fence_after();
+        }
+        if (ok && w < n_sub)
+            store_row(a.dq + ((long long)q * a.q_heads + head) * D, tmem + lanes + 256 + w * D, D, a.scale, done > 0, mine);
+    } else if (warp == 8) {
+        // ------------------------------------------------------------------ tile loads
+        if (lane == 0 && n_tiles > 0) {
+            mbar_expect_tx(smem_u32(&sh.q_full), 2 * n_sub * F::kRowTile);
+            for (int w = 0; w < n_sub; ++w) {
+                load_rows<D>(q_smem + w * F::kRowTile, kRows, &map_q, head, sh.q0 + w * kRows, smem_u32(&sh.q_full));
+                load_rows<D>(o_smem + w * F::kRowTile, kRows, &map_do, head, sh.q0 + w * kRows, smem_u32(&sh.q_full));
+            }
+            int j = 0;
+            bool ok = true;
+            for (; j < n_tiles; ++j) {
+                const int st = j % F::kStages;
+                ok = wait(smem_u32(&sh.empty[st]), (j / F::kStages & 1) ^ 1, abort_flag, a.status, kPromptWaitStage);
+                if (!ok) break;
+                const uint32_t bar = smem_u32(&sh.full[st]), dst = ring + st * 2 * F::kColTile;
+                mbar_expect_tx(bar, 2 * F::kColTile);
+                const int token = sh.k0 + tile_at(j) * kCols;
+                load_rows<D>(dst, kCols, &map_k, kv_head, token, bar);
+                load_rows<D>(dst + F::kColTile, kCols, &map_v, kv_head, token, bar);
+            }
+            if (!ok || *abort_flag) {  // nothing of this CTA's copies may be in flight when it ends
+                wait(smem_u32(&sh.q_full), 0, nullptr, a.status, kPromptWaitDrain);
+                for (int i = max(0, j - F::kStages); i < j; ++i)
+                    wait(smem_u32(&sh.full[i % F::kStages]), i / F::kStages & 1, nullptr, a.status, kPromptWaitDrain);
+            }
+        }
+        __syncwarp();
+        // rows behind the last key: only the last tile can hold any
+        const int end = n_tiles - 1, rows = n_tiles > 0 ? kn - tile_at(end) * kCols : kCols;
+        if (rows < kCols && !*abort_flag &&
+            wait(smem_u32(&sh.full[end % F::kStages]), end / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad)) {
+            uint8_t* x = smem + 4 * F::kRowTile + end % F::kStages * 2 * F::kColTile;
+            for (int i = rows * 8 + lane; i < kCols * 8; i += 32)
+                for (int b = 0; b < 2 * D / 64; ++b) *reinterpret_cast<uint4*>(x + b * kColBlock + i * 16) = make_uint4(0, 0, 0, 0);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.clean));
+        }
+    } else if (warp == 9) {
+        // ------------------------------------------------------------------ matrix products
+        if (lane == 0 && n_tiles > 0) {
+            constexpr uint32_t kScores = instr_desc(kRows, kCols, false), kGrads = instr_desc(kRows, D, true);
+            int used[2] = {0, 0};
+            auto loaded = [&](int j) {
+                return wait(smem_u32(&sh.full[j % F::kStages]), j / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad) &&
+                       ((tile_at(j) + 1) * kCols <= kn || wait(smem_u32(&sh.clean), 0, abort_flag, a.status, kPromptWaitLoad));
+            };
+            auto first_products = [&](int w, int j) {
+                const uint32_t k = ring + j % F::kStages * 2 * F::kColTile, v = k + F::kColTile, d = tmem + w * 128;
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x) {
+                    const uint32_t ra = x / 4 * kRowBlock + x % 4 * 32 + w * F::kRowTile, cb = x / 4 * kColBlock + x % 4 * 32;
+                    mma_ss(d, smem_desc(q_smem + ra), smem_desc(k + cb), kScores, x > 0);
+                }
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x) {
+                    const uint32_t ra = x / 4 * kRowBlock + x % 4 * 32 + w * F::kRowTile, cb = x / 4 * kColBlock + x % 4 * 32;
+                    mma_ss(d + 64, smem_desc(o_smem + ra), smem_desc(v + cb), kScores, x > 0);
+                }
+                commit(smem_u32(&sh.sd_full[w]));
+            };
+            bool ok = wait(smem_u32(&sh.q_full), 0, abort_flag, a.status, kPromptWaitLoad) && loaded(0);
+            if (ok)
+                for (int w = 0; w < 2; ++w)
+                    if (needed(w, tile_at(0))) first_products(w, 0);
+            for (int j = 0; ok && j < n_tiles; ++j) {
+                const int st = j % F::kStages;
+                if (j + 1 < n_tiles) ok = loaded(j + 1);
+                for (int w = 0; ok && w < 2; ++w) {
+                    if (needed(w, tile_at(j))) {
+                        ok = wait(smem_u32(&sh.ds_full[w]), used[w] & 1, abort_flag, a.status, kPromptWaitSoftmax);
+                        if (!ok) break;
+                        fence_after();
+                        const uint32_t k = ring + st * 2 * F::kColTile;
+#pragma unroll
+                        for (int x = 0; x < kCols / 16; ++x)
+                            mma_ts(tmem + 256 + w * D, tmem + w * 128 + 64 + x * 8, smem_desc(k + x * 2048, kColBlock), kGrads, used[w] > 0 || x > 0);
+                        ++used[w];
+                    }
+                    if (w == 1) commit(smem_u32(&sh.empty[st]));
+                    if (j + 1 < n_tiles && needed(w, tile_at(j + 1))) first_products(w, j + 1);
+                }
+            }
+            commit(smem_u32(&sh.done));
+            commit(smem_u32(&sh.drain));
+            wait(smem_u32(&sh.drain), 0, nullptr, a.status, kPromptWaitDrain);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == 9) {
+        __syncwarp();
+        tmem_free(tmem, 512);
+    }
+}
+
+struct Maps {
+    const CUtensorMap &q, &k, &v, &dout;
+};
+
+template <int D, bool CAP, bool BIAS>
+cudaError_t launch_one(const PromptArgs& a, const Maps& m, cudaStream_t stream)
+{
+    const long long k_tiles = (long long)a.k_tokens / kRows + (a.n_docs < a.k_tokens ? a.n_docs : a.k_tokens);
+    const long long q_tiles = (long long)a.q_tokens / (2 * kRows) + (a.n_docs < a.q_tokens ? a.n_docs : a.q_tokens);
+    const dim3 stats((a.q_tokens + 31) / 32, (a.q_heads + 7) / 8);
+    prompt_stats_kernel<D><<<stats, 256, 0, stream>>>(a);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    prompt_keys_kernel<D, CAP, BIAS><<<(unsigned)(k_tiles * a.kv_heads), kThreads, Keys<D>::kSmem, stream>>>(a, m.q, m.k, m.v, m.dout);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    prompt_rows_kernel<D, CAP, BIAS><<<(unsigned)(q_tiles * a.q_heads), kThreads, RowsK<D>::kSmem, stream>>>(a, m.q, m.k, m.v, m.dout);
+    return cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch_dim(const PromptArgs& a, const Maps& m, cudaStream_t stream)
+{
+    if (a.softcap != 0.f) return a.slopes ? launch_one<D, true, true>(a, m, stream) : launch_one<D, true, false>(a, m, stream);
+    return a.slopes ? launch_one<D, false, true>(a, m, stream) : launch_one<D, false, false>(a, m, stream);
+}
+
+template <int D, bool CAP, bool BIAS>
+cudaError_t prepare_one()
+{
+    const cudaError_t e = cudaFuncSetAttribute(prompt_keys_kernel<D, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, Keys<D>::kSmem);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(prompt_rows_kernel<D, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsK<D>::kSmem);
+}
+
+template <int D>
+cudaError_t prepare_dim()
+{
+    cudaError_t e = prepare_one<D, false, false>();
+    if (e == cudaSuccess) e = prepare_one<D, false, true>();
+    if (e == cudaSuccess) e = prepare_one<D, true, false>();
+    return e == cudaSuccess ? prepare_one<D, true, true>() : e;
+}
+
+}  // namespace
+
+cudaError_t launch_prompt_backward(const PromptArgs& a, const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
+                                   const CUtensorMap& map_do, int head_dim, cudaStream_t stream)
+{
+    const Maps m{map_q, map_k, map_v, map_do};
+    return head_dim == 128 ? launch_dim<128>(a, m, stream) : launch_dim<64>(a, m, stream);
+}
+
+cudaError_t prepare_prompt_backward(int head_dim) { return head_dim == 128 ? prepare_dim<128>() : prepare_dim<64>(); }
+
+}  // namespace rlkv

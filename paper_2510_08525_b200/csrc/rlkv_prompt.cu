@@ -16,8 +16,8 @@ struct rlkv_prompt {
     float softcap;
     bool biased;
     std::vector<uint8_t> is_full;  // [layers*kv_heads]
-    uint8_t* dev_base;             // status, then slopes [layers][q_heads], then delta [max_tokens][q_heads]
-    size_t off_slopes, off_delta;
+    uint8_t* dev_base;             // status, then slopes [layers][q_heads], then stats (float2) [q_heads][max_tokens]
+    size_t off_slopes, off_stats;
 };
 
 namespace {
@@ -67,7 +67,7 @@ int fill_prompt_args(const rlkv_prompt* p, int layer, const void* q, int64_t q_s
     a.slopes = p->biased ? reinterpret_cast<const float*>(p->dev_base + p->off_slopes) + (size_t)layer * p->q_heads : nullptr;
     a.out = static_cast<__nv_bfloat16*>(const_cast<void*>(out));
     a.lse = const_cast<float*>(lse);
-    a.delta = reinterpret_cast<float*>(p->dev_base + p->off_delta);
+    a.stats = reinterpret_cast<float2*>(p->dev_base + p->off_stats);
     a.status = reinterpret_cast<int*>(p->dev_base);
     for (int h = 0; h < p->kv_heads; ++h) a.full[h] = p->is_full[(size_t)layer * p->kv_heads + h] ? 1 : 0;
     return RLKV_OK;
@@ -134,17 +134,18 @@ int rlkv_prompt_create(rlkv_prompt** out, int layers, int kv_heads, int q_heads,
         return RLKV_ENOMEM;
     }
     p->off_slopes = 1024;
-    p->off_delta = align_up(p->off_slopes + count * sizeof(float), 1024);
-    const size_t total = p->off_delta + (size_t)max_tokens * q_heads * sizeof(float);
+    p->off_stats = align_up(p->off_slopes + count * sizeof(float), 1024);
+    const size_t total = p->off_stats + (size_t)max_tokens * q_heads * sizeof(float2);
     cudaError_t e = cudaGetDevice(&p->device);
     if (e != cudaSuccess) { delete p; return cuda_fail(e, "device query"); }
     void* mem = nullptr;
     e = cudaMalloc(&mem, total);
     if (e != cudaSuccess) { cudaGetLastError(); delete p; return RLKV_ENOMEM; }
     p->dev_base = static_cast<uint8_t*>(mem);
-    e = cudaMemset(mem, 0, p->off_delta);
+    e = cudaMemset(mem, 0, p->off_stats);
     if (e == cudaSuccess && biased) e = cudaMemcpy(p->dev_base + p->off_slopes, slopes, count * sizeof(float), cudaMemcpyHostToDevice);
     if (e == cudaSuccess) e = prepare_prompt_kernels(head_dim);
+    if (e == cudaSuccess) e = prepare_prompt_backward(head_dim);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();  // the memset is done before a call on any stream
     if (e != cudaSuccess) {
         cudaFree(mem);
@@ -200,7 +201,13 @@ int rlkv_prompt_attention_backward(rlkv_prompt* p, int layer, const void* q, int
     a.dv = static_cast<__nv_bfloat16*>(dv);
     DeviceGuard g(p->device);
     if (!g.ok) return RLKV_ECUDA;
-    RLKV_CUDA(launch_prompt_backward(a, p->head_dim, static_cast<cudaStream_t>(stream)));
+    CUtensorMap map_q, map_k, map_v, map_do;
+    int e = encode_heads_map(&map_q, q, q_tokens, p->q_heads, p->head_dim, a.q_stride, 64);
+    if (!e) e = encode_heads_map(&map_k, k, k_tokens, p->kv_heads, p->head_dim, a.k_stride, 64);
+    if (!e) e = encode_heads_map(&map_v, v, k_tokens, p->kv_heads, p->head_dim, a.v_stride, 64);
+    if (!e) e = encode_heads_map(&map_do, dout, q_tokens, p->q_heads, p->head_dim, (int64_t)p->q_heads * p->head_dim, 64);
+    if (e) return e;
+    RLKV_CUDA(launch_prompt_backward(a, map_q, map_k, map_v, map_do, p->head_dim, static_cast<cudaStream_t>(stream)));
     return RLKV_OK;
 }
 

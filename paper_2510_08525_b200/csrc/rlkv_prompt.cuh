@@ -1,6 +1,8 @@
 // Internal definitions of prompt attention (rlkv_prompt_*): shared by its host side and its kernels.
 #pragma once
 
+#include <limits.h>
+
 #include "rlkv_internal.cuh"
 
 namespace rlkv {
@@ -20,7 +22,7 @@ struct PromptArgs {
     float* lse;                          // [q_tokens][q_heads], may be null in the forward pass
     const __nv_bfloat16* dout;
     __nv_bfloat16 *dq, *dk, *dv;
-    float* delta;                        // scratch, [q_tokens][q_heads]: sum over head_dim of dout * out
+    float2* stats;                       // scratch, [q_heads][q_tokens]: lse * log2(e), sum over head_dim of dout * out
     int* status;
     unsigned char full[kMaxKvHeads];     // 1: the KV head sees every key, 0: sink and window only
 };
@@ -100,6 +102,8 @@ __device__ __forceinline__ uint32_t range_bits(int lo, int hi)
 cudaError_t launch_prompt_forward(const PromptArgs& a, const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
                                   int head_dim, cudaStream_t stream);
 cudaError_t prepare_prompt_kernels(int head_dim);
-cudaError_t launch_prompt_backward(const PromptArgs& a, int head_dim, cudaStream_t stream);
+cudaError_t launch_prompt_backward(const PromptArgs& a, const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
+                                   const CUtensorMap& map_do, int head_dim, cudaStream_t stream);
+cudaError_t prepare_prompt_backward(int head_dim);
 
 }  // namespace rlkv

@@ -25,6 +25,7 @@ using namespace tc;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kRows = 128;          // queries of a sub-tile, keys of a tile
+constexpr int kPolyPairs = 4;      // the exponential unit alone would need as long as the tensor core
 constexpr int kBlock = kRows * 128; // bytes of a [128 rows][64 elements] block
 
 template <int D>
@@ -36,11 +37,49 @@ struct Fwd {
 };
 
 struct FwdShared {
-    uint64_t q_full, full[10], empty[10], s_full[2], p_full[2], pv_done[2], clean, drain;
+    uint64_t q_full, full[10], empty[10], s_full[2], p_full[2][2], pv_done[2], clean, drain;
     uint32_t tmem;
     int abort, valid;
-    int q0, rows, pos0, k0, kn, prefix, a_end, b0, n_tiles;  // the CTA's queries; its key tiles: 0 .. a_end-1, then from b0 on
+    int q0, rows, pos0, k0, kn, prefix;    // the CTA's queries, its document's keys
+    int a_end, b0, n_tiles;                // its key tiles: 0 .. a_end-1, then from b0 on
+    int sub_a[2], sub_b[2], sub_e[2];      // those a sub-tile needs: 0 .. a-1 and b .. e-1
 };
+
+// P = 2^(s factor - base) of a row's 128 scores, as bf16 to tensor memory, and their sums; POLY > 0: one pair in POLY on
+// the FMA pipe.  64 keys at a time, so that the product starts on the first.
+template <int POLY>
+__device__ __forceinline__ void exponentials(float (&s)[kRows], float factor, float base, float2 (&sum)[2], uint32_t P, uint64_t* done, int lane)
+{
+    const float2 factor2 = make_float2(factor, factor), base2 = make_float2(-base, -base);
+#pragma unroll
+    for (int c = 0; c < kRows; c += 32) {
+        uint32_t packed[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            const float2 x = fma2(make_float2(s[c + i], s[c + i + 1]), factor2, base2);
+            s[c + i] = x.x;
+            s[c + i + 1] = x.y;
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            float2 p = make_float2(s[c + i], s[c + i + 1]);
+            if (POLY > 0 && i / 2 % (POLY > 0 ? POLY : 1) == POLY - 1) p = exp2_fma(p);
+            else p = make_float2(ex2(p.x), ex2(p.y));
+            s[c + i] = p.x;
+            s[c + i + 1] = p.y;
+            packed[i / 2] = bf16x2(p.x, p.y);
+        }
+        tmem_st16(P + c / 2, packed);
+        if (c % 64 == 32) {
+            wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(done + c / 64));
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < kRows; c += 2) sum[c / 2 & 1] = add2(sum[c / 2 & 1], make_float2(s[c], s[c + 1]));
+}
 
 template <int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(Fwd<D>::kThreads, 1)
@@ -50,7 +89,7 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
     using F = Fwd<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     FwdShared& sh = *reinterpret_cast<FwdShared*>(smem + (2 + F::kStages) * F::kTileBytes);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int head = blockIdx.x % a.q_heads, kv_head = head / a.group;
     const bool full_head = a.full[kv_head] != 0;
     volatile int* abort_flag = &sh.abort;
@@ -83,6 +122,14 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
                 sh.a_end = a_end;
                 sh.b0 = b0;
                 sh.n_tiles = a_end + max(0, end - b0);
+                for (int w = 0; w < 2; ++w) {
+                    const int rows = min(kRows, sh.rows - w * kRows), first = sh.pos0 + w * kRows;
+                    const int seen = rows > 0 ? max(0, min(r.kn, max(first + rows, r.prefix))) : 0;
+                    const int e = (seen + kRows - 1) / kRows;
+                    sh.sub_a[w] = full_head ? e : min(e, (a.sink + kRows - 1) / kRows);
+                    sh.sub_b[w] = max(sh.sub_a[w], max(0, first - a.window + 1) / kRows);
+                    sh.sub_e[w] = max(e, sh.sub_b[w]);
+                }
             }
             mbar_init(smem_u32(&sh.q_full), 1);
             for (int i = 0; i < F::kStages; ++i) {
@@ -91,7 +138,8 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
             }
             for (int w = 0; w < 2; ++w) {
                 mbar_init(smem_u32(&sh.s_full[w]), 1);
-                mbar_init(smem_u32(&sh.p_full[w]), 4);
+                mbar_init(smem_u32(&sh.p_full[w][0]), 4);
+                mbar_init(smem_u32(&sh.p_full[w][1]), 4);
                 mbar_init(smem_u32(&sh.pv_done[w]), 1);
             }
             mbar_init(smem_u32(&sh.clean), 1);
@@ -110,14 +158,6 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
     const uint32_t q_smem = smem_u32(smem), ring = q_smem + 2 * F::kTileBytes;
     const int n_sub = sh.rows > kRows ? 2 : 1;
     auto tile_at = [&](int j) { return j < a_end ? j : b0 + j - a_end; };
-    // does any query of sub-tile w see a key of tile t?
-    auto needed = [&](int w, int t) {
-        if (w >= n_sub) return false;
-        const int first = sh.pos0 + w * kRows, last = first + min(kRows, sh.rows - w * kRows) - 1, start = t * kRows;
-        if (start >= min(kn, max(last + 1, prefix))) return false;
-        return full_head || start < a.sink || start + kRows > first - a.window + 1;
-    };
-
     // (launched with 384 x 168 = 64512 registers: 256 x 216 + 128 x 72)
     if (warp < 8) more_registers<216>();
     else fewer_registers<72>();
@@ -132,13 +172,13 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
         const int hi = min(kn, max(pos + 1, prefix)), lo = full_head ? 0 : pos - a.window + 1, sink = full_head ? 0 : min(a.sink, hi);
         const float sl2 = a.scale * kLog2e, factor = CAP || BIAS ? 1.f : sl2;
         const float slope2 = BIAS ? a.slopes[head] * kLog2e : 0.f;
+        const int sub_a = sh.sub_a[w], sub_b = sh.sub_b[w], sub_e = sh.sub_e[w];
         float m = -INFINITY, l = 0.f;
         int done = 0;  // tiles of this sub-tile so far
         bool ok = true;
         if (w < n_sub)
-            for (int j = 0; ok && j < n_tiles; ++j) {
-                const int t = tile_at(j), start = t * kRows;
-                if (!needed(w, t)) continue;
+            for (int t = sub_a > 0 ? 0 : sub_b; t < sub_e; t = t + 1 == sub_a ? sub_b : t + 1) {
+                const int start = t * kRows;
                 ok = wait(smem_u32(&sh.s_full[w]), done & 1, abort_flag, a.status, kPromptWaitProduct);
                 if (!ok) break;
                 fence_after();
@@ -225,23 +265,11 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
                     }
                 }
                 const float base = m == -INFINITY ? 0.f : m;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < kRows; c += 32) {
-                    uint32_t packed[16];
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        const float p0 = ex2(fmaf(s[c + i], factor, -base)), p1 = ex2(fmaf(s[c + i + 1], factor, -base));
-                        sum[i / 2 & 3] += p0 + p1;
-                        packed[i / 2] = bf16x2(p0, p1);
-                    }
-                    tmem_st16(S + c / 2, packed);
-                }
-                wait_st();
-                fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh.p_full[w]));
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                // (where every key is seen: the FMA pipe's exponential wants finite arguments)
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                if (plain) exponentials<kPolyPairs>(s, factor, base, sum, S, sh.p_full[w], lane);
+                else exponentials<0>(s, factor, base, sum, S, sh.p_full[w], lane);
+                l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 ++done;
             }
         if (ok && w < n_sub) {
@@ -316,55 +344,70 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
         }
     } else if (warp == 9) {
         // ------------------------------------------------------------------ matrix products
-        if (lane == 0 && n_tiles > 0) {
+        if (n_tiles > 0) {
             constexpr uint32_t kQK = instr_desc(kRows, kRows, false), kPV = instr_desc(kRows, D, true);
             bool ok = true;
             int used[2] = {0, 0};  // P tiles of the sub-tile multiplied so far
+            const int sub_a[2] = {sh.sub_a[0], sh.sub_a[1]}, sub_b[2] = {sh.sub_b[0], sh.sub_b[1]}, sub_e[2] = {sh.sub_e[0], sh.sub_e[1]};
+            auto needed = [&](int w, int t) { return t < sub_a[w] || (t >= sub_b[w] && t < sub_e[w]); };
             auto stage = [&](int i) { return ring + i % F::kStages * F::kTileBytes; };
             auto loaded = [&](int i) {
-                return wait(smem_u32(&sh.full[i % F::kStages]), i / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad);
+                return wait_warp(smem_u32(&sh.full[i % F::kStages]), i / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad);
+            };
+            auto signal = [&](uint64_t* bar) {
+                if (elect_one()) commit(smem_u32(bar));
             };
             auto scores = [&](int w, int j) {
-                const uint32_t q = q_smem + w * F::kTileBytes, k = stage(2 * j);
+                const uint64_t q = smem_desc(q_smem + w * F::kTileBytes), k = smem_desc(stage(2 * j));
+                if (elect_one()) {
 #pragma unroll
-                for (int x = 0; x < D / 16; ++x) {
-                    const uint32_t off = x / 4 * kBlock + x % 4 * 32;
-                    mma_ss(tmem + w * kRows, smem_desc(q + off), smem_desc(k + off), kQK, x > 0);
+                    for (int x = 0; x < D / 16; ++x) {
+                        const uint32_t off = (x / 4 * kBlock + x % 4 * 32) >> 4;
+                        mma_ss(tmem + w * kRows, q + off, k + off, kQK, x > 0);
+                    }
+                    commit(smem_u32(&sh.s_full[w]));
                 }
-                commit(smem_u32(&sh.s_full[w]));
             };
-            ok = wait(smem_u32(&sh.q_full), 0, abort_flag, a.status, kPromptWaitLoad) && loaded(0);
+            ok = wait_warp(smem_u32(&sh.q_full), 0, abort_flag, a.status, kPromptWaitLoad) && loaded(0);
             if (ok) {
                 for (int w = 0; w < 2; ++w)
                     if (needed(w, tile_at(0))) scores(w, 0);
-                commit(smem_u32(&sh.empty[0]));
+                signal(&sh.empty[0]);
             }
             for (int j = 0; ok && j < n_tiles; ++j) {
                 const int t = tile_at(j);
                 ok = loaded(2 * j + 1);
-                if (ok && (t + 1) * kRows > kn) ok = wait(smem_u32(&sh.clean), 0, abort_flag, a.status, kPromptWaitLoad);
+                if (ok && (t + 1) * kRows > kn) ok = wait_warp(smem_u32(&sh.clean), 0, abort_flag, a.status, kPromptWaitLoad);
                 if (ok && j + 1 < n_tiles) ok = loaded(2 * j + 2);
-                for (int w = 0; ok && w < 2; ++w) {
-                    if (needed(w, t)) {
-                        ok = wait(smem_u32(&sh.p_full[w]), used[w] & 1, abort_flag, a.status, kPromptWaitSoftmax);
-                        if (!ok) break;
-                        fence_after();
-                        const uint32_t v = stage(2 * j + 1);
 #pragma unroll
-                        for (int x = 0; x < kRows / 16; ++x)
-                            mma_ts(tmem + 2 * kRows + w * D, tmem + w * kRows + x * 8, smem_desc(v + x * 2048, kBlock), kPV,
-                                   used[w] > 0 || x > 0);
-                        commit(smem_u32(&sh.pv_done[w]));
+                for (int w = 0; w < 2; ++w) {
+                    if (!ok) break;
+                    if (needed(w, t)) {
+                        const uint64_t v = smem_desc(stage(2 * j + 1), kBlock);
+                        for (int half = 0; half < 2; ++half) {
+                            ok = wait_warp(smem_u32(&sh.p_full[w][half]), used[w] & 1, abort_flag, a.status, kPromptWaitSoftmax);
+                            if (!ok) break;
+                            fence_after();
+                            if (elect_one()) {
+#pragma unroll
+                                for (int x = 0; x < kRows / 32; ++x) {
+                                    const int y = half * (kRows / 32) + x;
+                                    mma_ts(tmem + 2 * kRows + w * D, tmem + w * kRows + y * 8, v + (y * 2048 >> 4), kPV, used[w] > 0 || y > 0);
+                                }
+                            }
+                        }
+                        if (!ok) break;
+                        signal(&sh.pv_done[w]);
                         ++used[w];
                     }
-                    if (w == 1) commit(smem_u32(&sh.empty[(2 * j + 1) % F::kStages]));
+                    if (w == 1) signal(&sh.empty[(2 * j + 1) % F::kStages]);
                     if (j + 1 < n_tiles && needed(w, tile_at(j + 1))) scores(w, j + 1);
                 }
-                if (ok && j + 1 < n_tiles) commit(smem_u32(&sh.empty[(2 * j + 2) % F::kStages]));
+                if (ok && j + 1 < n_tiles) signal(&sh.empty[(2 * j + 2) % F::kStages]);
             }
             // every product is done before tensor memory is given back
-            commit(smem_u32(&sh.drain));
-            wait(smem_u32(&sh.drain), 0, nullptr, a.status, kPromptWaitDrain);
+            signal(&sh.drain);
+            wait_warp(smem_u32(&sh.drain), 0, nullptr, a.status, kPromptWaitDrain);
         }
     }
     fence_before();

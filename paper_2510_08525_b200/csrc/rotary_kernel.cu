@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kPiece = 16;  // elements one thread turns: eight pairs, so two 16-byte loads and one 64-byte table read
 
-// Where a K (kv = 0) or V (kv = 1) row of entry e lands.
+// Where the K (kv = 0) or V (kv = 1) row of a token lands; `slot`: the head's place among the heads of its class.
 struct RowPlace {
     bool stored;           // false: the prompt evicts the token before it ends
     __nv_bfloat16* row;    // 16-bit row
@@ -23,10 +23,9 @@ struct RowPlace {
     int prow;
 };
 
-__device__ __forceinline__ RowPlace place_of(const PagedAppendArgs& a, int e, int h, int kv, int seq, int t, int page)
+__device__ __forceinline__ RowPlace place_of(const PagedAppendArgs& a, int slot, int kv, int seq, int t, int page)
 {
     RowPlace p{true, nullptr, nullptr, 0};
-    const int slot = a.slot_of_head[h];
     int phys = 0;
     if (slot < 0) {
         if (a.prefill && !(t < a.sink || t >= a.t0 + a.n - a.window)) {
@@ -46,6 +45,13 @@ __device__ __forceinline__ RowPlace place_of(const PagedAppendArgs& a, int e, in
         p.row = a.pool + row * a.head_dim;
     }
     return p;
+}
+
+__device__ __forceinline__ void rotate(float& u, float& v, float2 cs)
+{
+    const float x = u, y = v;
+    u = fmaf(x, cs.x, -__fmul_rn(y, cs.y));
+    v = fmaf(y, cs.x, __fmul_rn(x, cs.y));
 }
 
 __device__ __forceinline__ void unpack8(const uint4& bits, float (&x)[8])
@@ -77,81 +83,111 @@ __device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv)
     return bits;
 }
 
-// One thread: one piece of one head of one token.  Heads are numbered q heads, K heads, V heads.
-__global__ void __launch_bounds__(256) rotated_append_kernel(const __grid_constant__ RotatedAppendArgs r)
+// A block takes 256 / PIECES tokens and `heads` of the heads (numbered q heads, K heads, V heads).  A thread keeps
+// one piece of one token: its eight angles stay in registers over the heads, whose loads are issued four at a time.
+template <int PIECES>
+__global__ void __launch_bounds__(256) rotated_append_kernel(const __grid_constant__ RotatedAppendArgs r, const int heads)
 {
+    constexpr int kTokens = 256 / PIECES, kBatch = 4;
     const PagedAppendArgs& a = r.rows;
-    const int pieces = a.head_dim / kPiece;
     const int q_heads = r.q ? r.q_heads : 0, rows = q_heads + 2 * a.kv_heads;
-    const unsigned total = (unsigned)a.n * rows * pieces;
-    for (unsigned i = blockIdx.x * blockDim.x + threadIdx.x; i < total; i += gridDim.x * blockDim.x) {
-        const unsigned w = i / pieces;
-        const int piece = i - w * pieces;
-        const int e = w / rows, hh = w - e * rows;
+    const int head0 = blockIdx.y * heads, head1 = min(rows, head0 + heads);
+    // pieces of one row in neighbouring lanes; the transposed V codes of an 8-bit page the other way round: tokens in
+    // neighbouring lanes write neighbouring bytes
+    const int v_turned = a.pool8 ? max(head0, q_heads + a.kv_heads) : head1;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        const int from = pass ? v_turned : head0, to = pass ? head1 : min(head1, v_turned);
+        if (from >= to) continue;
+        const int piece = pass ? threadIdx.x / kTokens : threadIdx.x % PIECES;
+        const int e = blockIdx.x * kTokens + (pass ? threadIdx.x % kTokens : threadIdx.x / PIECES);
+        if (e >= a.n) continue;
         const int seq = a.prefill ? a.slot[0] : a.slot[e];
         const int t = a.prefill ? a.t0 + e : a.t[e];
-        const bool is_q = hh < q_heads;
-        const int kv = !is_q && hh - q_heads >= a.kv_heads;
-        const int h = is_q ? hh : hh - q_heads - kv * a.kv_heads;
+        const int page = a.page[a.prefill ? t / kTile - a.first_page : e];
         // the piece's two runs of eight elements: the two halves of eight pairs, or sixteen in a row
-        const bool turn = !kv && piece * kPiece < r.rot;
-        const bool halves = turn && !r.interleaved;
-        const int c0 = halves ? piece * 8 : piece * kPiece, c1 = halves ? c0 + r.rot / 2 : c0 + 8;
-        const __nv_bfloat16* src = (is_q ? r.q + (long long)e * r.q_stride : kv ? a.v + (long long)e * r.v_stride
-                                                                                : a.k + (long long)e * r.k_stride) + h * a.head_dim;
-        uint4 b0 = *reinterpret_cast<const uint4*>(src + c0), b1 = *reinterpret_cast<const uint4*>(src + c1);
-        float x0[8], x1[8];
-        unpack8(b0, x0);
-        unpack8(b1, x1);
-        if (turn) {
-            const float4* cs = reinterpret_cast<const float4*>(r.table + (long long)t * r.rot + piece * kPiece);  // (cos, sin) of eight pairs
-            float2 f[8];
+        const bool turned = piece * kPiece < r.rot;
+        float2 f[8];
+        if (turned && from < q_heads + a.kv_heads) {
+            const float4* cs = reinterpret_cast<const float4*>(r.table + (long long)t * r.rot + piece * kPiece);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float4 v = __ldg(cs + j);
                 f[2 * j] = make_float2(v.x, v.y);
                 f[2 * j + 1] = make_float2(v.z, v.w);
             }
+        }
+        for (int base = from; base < to; base += kBatch) {
+            uint4 b[kBatch][2];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float& p = r.interleaved ? (j < 4 ? x0[2 * j] : x1[2 * j - 8]) : x0[j];
-                float& s = r.interleaved ? (j < 4 ? x0[2 * j + 1] : x1[2 * j - 7]) : x1[j];
-                const float u = p, v = s;
-                p = fmaf(u, f[j].x, -__fmul_rn(v, f[j].y));
-                s = fmaf(v, f[j].x, __fmul_rn(u, f[j].y));
+            for (int x = 0; x < kBatch; ++x) {
+                const int hh = base + x;
+                if (hh < to) {
+                    const bool is_q = hh < q_heads, is_v = hh >= q_heads + a.kv_heads;
+                    const int h = is_q ? hh : hh - q_heads - (is_v ? a.kv_heads : 0);
+                    const bool halves = turned && !is_v && !r.interleaved;
+                    const int c0 = halves ? piece * 8 : piece * kPiece, c1 = halves ? c0 + r.rot / 2 : c0 + 8;
+                    const __nv_bfloat16* src = (is_q ? r.q + e * r.q_stride : is_v ? a.v + e * r.v_stride : a.k + e * r.k_stride) + h * a.head_dim;
+                    b[x][0] = *reinterpret_cast<const uint4*>(src + c0);
+                    b[x][1] = *reinterpret_cast<const uint4*>(src + c1);
+                }
             }
-            b0 = pack8(x0);
-            b1 = pack8(x1);
-        }
-        if (is_q || (!kv && r.k_out)) {
-            __nv_bfloat16* dst = (is_q ? r.q_out + ((long long)e * q_heads + h) * a.head_dim
-                                       : r.k_out + ((long long)e * a.kv_heads + h) * a.head_dim);
-            *reinterpret_cast<uint4*>(dst + c0) = b0;
-            *reinterpret_cast<uint4*>(dst + c1) = b1;
-            if (is_q) continue;
-        }
-        const int page = a.page[a.prefill ? t / kTile - a.first_page : e];
-        if (!kv && piece == 0 && a.slot_of_head[h] == 0) a.page_table[(size_t)seq * a.table_stride + t / kTile] = page;
-        const RowPlace p = place_of(a, e, h, kv, seq, t, page);
-        if (!p.stored) continue;
-        if (!a.pool8) {
-            *reinterpret_cast<uint4*>(p.row + c0) = b0;
-            *reinterpret_cast<uint4*>(p.row + c1) = b1;
-            continue;
-        }
-        const float inv = (kv ? a.v_inv : a.k_inv)[h];
-        const uint2 k0 = codes8(x0, inv), k1 = codes8(x1, inv);
-        if (!kv) {
-            *reinterpret_cast<uint2*>(p.page8 + p.prow * 128 + c0) = k0;
-            *reinterpret_cast<uint2*>(p.page8 + p.prow * 128 + c1) = k1;
-        } else {  // V codes lie transposed behind the K codes
-            unsigned char* col = p.page8 + kTile * 128 + p.prow;
-            const unsigned char* u0 = reinterpret_cast<const unsigned char*>(&k0);
-            const unsigned char* u1 = reinterpret_cast<const unsigned char*>(&k1);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                col[(c0 + j) * kTile] = u0[j];
-                col[(c1 + j) * kTile] = u1[j];
+            for (int x = 0; x < kBatch; ++x) {
+                const int hh = base + x;
+                if (hh >= to) break;
+                const bool is_q = hh < q_heads, is_v = hh >= q_heads + a.kv_heads;
+                const int h = is_q ? hh : hh - q_heads - (is_v ? a.kv_heads : 0);
+                const bool turn = turned && !is_v, halves = turn && !r.interleaved;
+                const int c0 = halves ? piece * 8 : piece * kPiece, c1 = halves ? c0 + r.rot / 2 : c0 + 8;
+                float x0[8], x1[8];
+                unpack8(b[x][0], x0);
+                unpack8(b[x][1], x1);
+                if (turn) {
+                    if (r.interleaved) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            rotate(x0[2 * j], x0[2 * j + 1], f[j]);
+                            rotate(x1[2 * j], x1[2 * j + 1], f[4 + j]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) rotate(x0[j], x1[j], f[j]);
+                    }
+                    b[x][0] = pack8(x0);
+                    b[x][1] = pack8(x1);
+                }
+                if (is_q || (!is_v && r.k_out)) {
+                    __nv_bfloat16* dst = is_q ? r.q_out + ((long long)e * q_heads + h) * a.head_dim
+                                              : r.k_out + ((long long)e * a.kv_heads + h) * a.head_dim;
+                    *reinterpret_cast<uint4*>(dst + c0) = b[x][0];
+                    *reinterpret_cast<uint4*>(dst + c1) = b[x][1];
+                    if (is_q) continue;
+                }
+                const int slot = a.slot_of_head[h];
+                if (!is_v && piece == 0 && slot == 0) a.page_table[(size_t)seq * a.table_stride + t / kTile] = page;
+                const RowPlace p = place_of(a, slot, is_v, seq, t, page);
+                if (!p.stored) continue;
+                if (!a.pool8) {
+                    *reinterpret_cast<uint4*>(p.row + c0) = b[x][0];
+                    *reinterpret_cast<uint4*>(p.row + c1) = b[x][1];
+                    continue;
+                }
+                const float inv = (is_v ? a.v_inv : a.k_inv)[h];
+                const uint2 k0 = codes8(x0, inv), k1 = codes8(x1, inv);
+                if (!is_v) {
+                    *reinterpret_cast<uint2*>(p.page8 + p.prow * 128 + c0) = k0;
+                    *reinterpret_cast<uint2*>(p.page8 + p.prow * 128 + c1) = k1;
+                } else {  // V codes lie transposed behind the K codes
+                    unsigned char* col = p.page8 + kTile * 128 + p.prow;
+                    const unsigned char* u0 = reinterpret_cast<const unsigned char*>(&k0);
+                    const unsigned char* u1 = reinterpret_cast<const unsigned char*>(&k1);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        col[(c0 + j) * kTile] = u0[j];
+                        col[(c1 + j) * kTile] = u1[j];
+                    }
+                }
             }
         }
     }
@@ -180,8 +216,15 @@ unsigned blocks_for(long long threads, int most)
 
 cudaError_t launch_rotated_append(const RotatedAppendArgs& a, cudaStream_t stream)
 {
-    const long long threads = (long long)a.rows.n * ((a.q ? a.q_heads : 0) + 2 * a.rows.kv_heads) * (a.rows.head_dim / kPiece);
-    rotated_append_kernel<<<blocks_for(threads, 148 * 128), 256, 0, stream>>>(a);
+    const int pieces = a.rows.head_dim / kPiece, tokens = 256 / pieces;
+    const int rows = (a.q ? a.q_heads : 0) + 2 * a.rows.kv_heads, tiles = (a.rows.n + tokens - 1) / tokens;
+    // heads per block: enough blocks to fill the GPU first (few tokens: one head a block, the launch is all latency),
+    // then as many heads as share one load of the angles
+    int heads = 1;
+    while (heads < 8 && (long long)tiles * ((rows + 2 * heads - 1) / (2 * heads)) >= 148 * 8) heads *= 2;
+    const dim3 grid(tiles, (rows + heads - 1) / heads);
+    if (pieces == 8) rotated_append_kernel<8><<<grid, 256, 0, stream>>>(a, heads);
+    else rotated_append_kernel<4><<<grid, 256, 0, stream>>>(a, heads);
     return cudaGetLastError();
 }
 

@@ -68,6 +68,25 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
     return wait_slow(bar, parity, abort_flag, status, code);
 }
 
+// The whole warp waits; the answer is the same in every lane (control flow after it stays uniform).
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code)
+{
+    return __all_sync(0xffffffffu, wait(bar, parity, abort_flag, status, code));
+}
+
+// One lane of a converged warp, always the same.  Products are issued under it in warp-uniform code, so that their
+// descriptors live in uniform registers: issued by `if (lane == 0)` each took about 100 cycles, longer than it ran.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t leader;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(leader)
+        :
+        : "memory");
+    return leader != 0;
+}
+
 // A box of 64 elements (128 bytes, 128-byte swizzle) x 1 head x some tokens of a [tokens][heads][head_dim] tensor.
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int element, int head, int token, uint32_t bar)
 {
@@ -179,6 +198,50 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi)
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+// 2^x on the FMA pipe, for finite x up to about 120 (2^-126 below that): x = n + f with |f| <= 1/2, a polynomial of
+// degree 4 in f (fitted to the smallest largest relative error, 2.6e-6), and n added to its exponent.
+__device__ __forceinline__ float2 exp2_fma(float2 x)
+{
+    const float2 magic = make_float2(12582912.f, 12582912.f);  // 1.5 * 2^23: the sum's low bits are round(x)
+    x.x = fmaxf(x.x, -126.f);
+    x.y = fmaxf(x.y, -126.f);
+    const float2 n = add2(x, magic);
+    const float2 f = add2(x, fma2(n, make_float2(-1.f, -1.f), magic));
+    float2 p = fma2(f, make_float2(0.00957010059f, 0.00957010059f), make_float2(0.0559178602f, 0.0559178602f));
+    p = fma2(p, f, make_float2(0.240247449f, 0.240247449f));
+    p = fma2(p, f, make_float2(0.693121815f, 0.693121815f));
+    p = fma2(p, f, make_float2(0.999999261f, 0.999999261f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(n.x) << 23)),
+                       __int_as_float(__float_as_int(p.y) + (__float_as_int(n.y) << 23)));
 }
 
 }  // namespace tc

@@ -169,7 +169,7 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     extern __shared__ __align__(1024) uint8_t smem[];
     float2* stats = reinterpret_cast<float2*>(smem + F::kStats);
     KeysShared& sh = *reinterpret_cast<KeysShared*>(smem + F::kStats + F::kStages * kCols * 8);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int kv_head = blockIdx.x % a.kv_heads;
     const bool full_head = a.full[kv_head] != 0;
     volatile int* abort_flag = &sh.abort;
@@ -333,45 +333,51 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         }
     } else if (warp == 9) {
         // ------------------------------------------------------------------ matrix products
-        if (lane == 0 && steps > 0) {
+        if (steps > 0) {
             constexpr uint32_t kScores = instr_desc(kRows, kCols, false), kGrads = instr_desc(kRows, D, true);
+            const uint64_t k_desc = smem_desc(k_smem), v_desc = smem_desc(v_smem);
+            auto signal = [&](uint64_t* bar) {
+                if (elect_one()) commit(smem_u32(bar));
+            };
             auto first_products = [&](int n) {
                 const int st = n % F::kStages;
-                if (!wait(smem_u32(&sh.full[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad) ||
-                    !wait(smem_u32(&sh.ready[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad))
+                if (!wait_warp(smem_u32(&sh.full[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad) ||
+                    !wait_warp(smem_u32(&sh.ready[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad))
                     return false;
-                const uint32_t q = ring + st * 2 * F::kColTile, o = q + F::kColTile, d = tmem + (n & 1) * 128;
+                const uint64_t q = smem_desc(ring + st * 2 * F::kColTile), o = smem_desc(ring + st * 2 * F::kColTile + F::kColTile);
+                const uint32_t d = tmem + (n & 1) * 128;
+                if (elect_one()) {
 #pragma unroll
-                for (int x = 0; x < D / 16; ++x) {
-                    const uint32_t ra = x / 4 * kRowBlock + x % 4 * 32, cb = x / 4 * kColBlock + x % 4 * 32;
-                    mma_ss(d, smem_desc(k_smem + ra), smem_desc(q + cb), kScores, x > 0);
-                }
+                    for (int x = 0; x < D / 16; ++x)
+                        mma_ss(d, k_desc + ((x / 4 * kRowBlock + x % 4 * 32) >> 4), q + ((x / 4 * kColBlock + x % 4 * 32) >> 4), kScores, x > 0);
 #pragma unroll
-                for (int x = 0; x < D / 16; ++x) {
-                    const uint32_t ra = x / 4 * kRowBlock + x % 4 * 32, cb = x / 4 * kColBlock + x % 4 * 32;
-                    mma_ss(d + 64, smem_desc(v_smem + ra), smem_desc(o + cb), kScores, x > 0);
+                    for (int x = 0; x < D / 16; ++x)
+                        mma_ss(d + 64, v_desc + ((x / 4 * kRowBlock + x % 4 * 32) >> 4), o + ((x / 4 * kColBlock + x % 4 * 32) >> 4), kScores, x > 0);
+                    commit(smem_u32(&sh.sd_full[n & 1]));
                 }
-                commit(smem_u32(&sh.sd_full[n & 1]));
                 return true;
             };
-            bool ok = wait(smem_u32(&sh.kv_full), 0, abort_flag, a.status, kPromptWaitLoad) && first_products(0);
+            bool ok = wait_warp(smem_u32(&sh.kv_full), 0, abort_flag, a.status, kPromptWaitLoad) && first_products(0);
             if (ok && steps > 1) ok = first_products(1);
             for (int n = 0; ok && n < steps; ++n) {
                 const int st = n % F::kStages, w = n & 1;
-                ok = wait(smem_u32(&sh.pds_full[w]), n >> 1 & 1, abort_flag, a.status, kPromptWaitSoftmax);
+                ok = wait_warp(smem_u32(&sh.pds_full[w]), n >> 1 & 1, abort_flag, a.status, kPromptWaitSoftmax);
                 if (!ok) break;
                 fence_after();
-                const uint32_t q = ring + st * 2 * F::kColTile, o = q + F::kColTile, d = tmem + w * 128;
+                const uint64_t q = smem_desc(ring + st * 2 * F::kColTile, kColBlock), o = smem_desc(ring + st * 2 * F::kColTile + F::kColTile, kColBlock);
+                const uint32_t d = tmem + w * 128;
+                if (elect_one()) {
 #pragma unroll
-                for (int x = 0; x < kCols / 16; ++x) mma_ts(dV, d + x * 8, smem_desc(o + x * 2048, kColBlock), kGrads, n > 0 || x > 0);
+                    for (int x = 0; x < kCols / 16; ++x) mma_ts(dV, d + x * 8, o + (x * 2048 >> 4), kGrads, n > 0 || x > 0);
 #pragma unroll
-                for (int x = 0; x < kCols / 16; ++x) mma_ts(dK, d + 64 + x * 8, smem_desc(q + x * 2048, kColBlock), kGrads, n > 0 || x > 0);
-                commit(smem_u32(&sh.empty[st]));
+                    for (int x = 0; x < kCols / 16; ++x) mma_ts(dK, d + 64 + x * 8, q + (x * 2048 >> 4), kGrads, n > 0 || x > 0);
+                    commit(smem_u32(&sh.empty[st]));
+                }
                 if (n + 2 < steps) ok = first_products(n + 2);
             }
-            commit(smem_u32(&sh.done));
-            commit(smem_u32(&sh.drain));
-            wait(smem_u32(&sh.drain), 0, nullptr, a.status, kPromptWaitDrain);
+            signal(&sh.done);
+            signal(&sh.drain);
+            wait_warp(smem_u32(&sh.drain), 0, nullptr, a.status, kPromptWaitDrain);
         }
     } else if (warp == 10) {
         // ------------------------------------------------------------------ lse and D of the query tiles; rows behind the
@@ -427,7 +433,7 @@ struct RowsShared {
     uint64_t q_full, full[6], empty[6], sd_full[2], ds_full[2], done, clean, drain;
     uint32_t tmem;
     int abort, valid;
-    int q0, rows, pos0, k0, kn, prefix, a_end, b0, n_tiles;  // as in the forward pass, key tiles of 64
+    int q0, rows, pos0, k0, kn, prefix, a_end, b0, n_tiles, sub_a[2], sub_b[2], sub_e[2];  // as in the forward pass, key tiles of 64
 };
 
 template <int D, bool CAP, bool BIAS>
@@ -438,7 +444,7 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     using F = RowsK<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     RowsShared& sh = *reinterpret_cast<RowsShared*>(smem + 4 * F::kRowTile + F::kStages * 2 * F::kColTile);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int head = blockIdx.x % a.q_heads, kv_head = head / a.group;
     const bool full_head = a.full[kv_head] != 0;
     volatile int* abort_flag = &sh.abort;
@@ -471,6 +477,14 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 sh.a_end = a_end;
                 sh.b0 = b0;
                 sh.n_tiles = a_end + max(0, end - b0);
+                for (int w = 0; w < 2; ++w) {
+                    const int rows = min(kRows, sh.rows - w * kRows), first = sh.pos0 + w * kRows;
+                    const int seen = rows > 0 ? max(0, min(r.kn, max(first + rows, r.prefix))) : 0;
+                    const int e = (seen + kCols - 1) / kCols;
+                    sh.sub_a[w] = full_head ? e : min(e, (a.sink + kCols - 1) / kCols);
+                    sh.sub_b[w] = max(sh.sub_a[w], max(0, first - a.window + 1) / kCols);
+                    sh.sub_e[w] = max(e, sh.sub_b[w]);
+                }
             }
             mbar_init(smem_u32(&sh.q_full), 1);
             for (int i = 0; i < F::kStages; ++i) {
@@ -498,12 +512,6 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     const uint32_t q_smem = smem_u32(smem), o_smem = q_smem + 2 * F::kRowTile, ring = q_smem + 4 * F::kRowTile;
     const int n_sub = sh.rows > kRows ? 2 : 1;
     auto tile_at = [&](int j) { return j < a_end ? j : b0 + j - a_end; };
-    auto needed = [&](int w, int t) {  // does any query of sub-tile w see a key of tile t?
-        if (w >= n_sub) return false;
-        const int first = sh.pos0 + w * kRows, last = first + min(kRows, sh.rows - w * kRows) - 1, start = t * kCols;
-        if (start >= min(kn, max(last + 1, prefix))) return false;
-        return full_head || start < a.sink || start + kCols > first - a.window + 1;
-    };
 
     if (warp < 8) {
         // ------------------------------------------------------------------ P and dS, one thread per query
@@ -519,9 +527,9 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const float2 stat = mine ? a.stats[(long long)head * a.q_tokens + q] : make_float2(INFINITY, 0.f);
         bool ok = true;
         int done = 0;
-        for (int j = 0; ok && j < n_tiles; ++j) {
-            const int t = tile_at(j), start = t * kCols;
-            if (!needed(w, t)) continue;
+        const int sub_a = sh.sub_a[w], sub_b = sh.sub_b[w], sub_e = sh.sub_e[w];
+        for (int t = sub_a > 0 ? 0 : sub_b; t < sub_e; t = t + 1 == sub_a ? sub_b : t + 1) {
+            const int start = t * kCols;
             ok = wait(smem_u32(&sh.sd_full[w]), done & 1, abort_flag, a.status, kPromptWaitProduct);
             if (!ok) break;
             fence_after();
@@ -611,52 +619,61 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         }
     } else if (warp == 9) {
         // ------------------------------------------------------------------ matrix products
-        if (lane == 0 && n_tiles > 0) {
+        if (n_tiles > 0) {
             constexpr uint32_t kScores = instr_desc(kRows, kCols, false), kGrads = instr_desc(kRows, D, true);
             int used[2] = {0, 0};
+            const int sub_a[2] = {sh.sub_a[0], sh.sub_a[1]}, sub_b[2] = {sh.sub_b[0], sh.sub_b[1]}, sub_e[2] = {sh.sub_e[0], sh.sub_e[1]};
+            auto needed = [&](int w, int t) { return t < sub_a[w] || (t >= sub_b[w] && t < sub_e[w]); };
+            auto signal = [&](uint64_t* bar) {
+                if (elect_one()) commit(smem_u32(bar));
+            };
             auto loaded = [&](int j) {
-                return wait(smem_u32(&sh.full[j % F::kStages]), j / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad) &&
-                       ((tile_at(j) + 1) * kCols <= kn || wait(smem_u32(&sh.clean), 0, abort_flag, a.status, kPromptWaitLoad));
+                return wait_warp(smem_u32(&sh.full[j % F::kStages]), j / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad) &&
+                       ((tile_at(j) + 1) * kCols <= kn || wait_warp(smem_u32(&sh.clean), 0, abort_flag, a.status, kPromptWaitLoad));
             };
             auto first_products = [&](int w, int j) {
-                const uint32_t k = ring + j % F::kStages * 2 * F::kColTile, v = k + F::kColTile, d = tmem + w * 128;
+                const uint64_t k = smem_desc(ring + j % F::kStages * 2 * F::kColTile), v = smem_desc(ring + j % F::kStages * 2 * F::kColTile + F::kColTile);
+                const uint64_t q = smem_desc(q_smem + w * F::kRowTile), o = smem_desc(o_smem + w * F::kRowTile);
+                const uint32_t d = tmem + w * 128;
+                if (elect_one()) {
 #pragma unroll
-                for (int x = 0; x < D / 16; ++x) {
-                    const uint32_t ra = x / 4 * kRowBlock + x % 4 * 32 + w * F::kRowTile, cb = x / 4 * kColBlock + x % 4 * 32;
-                    mma_ss(d, smem_desc(q_smem + ra), smem_desc(k + cb), kScores, x > 0);
-                }
+                    for (int x = 0; x < D / 16; ++x)
+                        mma_ss(d, q + ((x / 4 * kRowBlock + x % 4 * 32) >> 4), k + ((x / 4 * kColBlock + x % 4 * 32) >> 4), kScores, x > 0);
 #pragma unroll
-                for (int x = 0; x < D / 16; ++x) {
-                    const uint32_t ra = x / 4 * kRowBlock + x % 4 * 32 + w * F::kRowTile, cb = x / 4 * kColBlock + x % 4 * 32;
-                    mma_ss(d + 64, smem_desc(o_smem + ra), smem_desc(v + cb), kScores, x > 0);
+                    for (int x = 0; x < D / 16; ++x)
+                        mma_ss(d + 64, o + ((x / 4 * kRowBlock + x % 4 * 32) >> 4), v + ((x / 4 * kColBlock + x % 4 * 32) >> 4), kScores, x > 0);
+                    commit(smem_u32(&sh.sd_full[w]));
                 }
-                commit(smem_u32(&sh.sd_full[w]));
             };
-            bool ok = wait(smem_u32(&sh.q_full), 0, abort_flag, a.status, kPromptWaitLoad) && loaded(0);
+            bool ok = wait_warp(smem_u32(&sh.q_full), 0, abort_flag, a.status, kPromptWaitLoad) && loaded(0);
             if (ok)
                 for (int w = 0; w < 2; ++w)
                     if (needed(w, tile_at(0))) first_products(w, 0);
             for (int j = 0; ok && j < n_tiles; ++j) {
                 const int st = j % F::kStages;
                 if (j + 1 < n_tiles) ok = loaded(j + 1);
-                for (int w = 0; ok && w < 2; ++w) {
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    if (!ok) break;
                     if (needed(w, tile_at(j))) {
-                        ok = wait(smem_u32(&sh.ds_full[w]), used[w] & 1, abort_flag, a.status, kPromptWaitSoftmax);
+                        ok = wait_warp(smem_u32(&sh.ds_full[w]), used[w] & 1, abort_flag, a.status, kPromptWaitSoftmax);
                         if (!ok) break;
                         fence_after();
-                        const uint32_t k = ring + st * 2 * F::kColTile;
+                        const uint64_t k = smem_desc(ring + st * 2 * F::kColTile, kColBlock);
+                        if (elect_one()) {
 #pragma unroll
-                        for (int x = 0; x < kCols / 16; ++x)
-                            mma_ts(tmem + 256 + w * D, tmem + w * 128 + 64 + x * 8, smem_desc(k + x * 2048, kColBlock), kGrads, used[w] > 0 || x > 0);
+                            for (int x = 0; x < kCols / 16; ++x)
+                                mma_ts(tmem + 256 + w * D, tmem + w * 128 + 64 + x * 8, k + (x * 2048 >> 4), kGrads, used[w] > 0 || x > 0);
+                        }
                         ++used[w];
                     }
-                    if (w == 1) commit(smem_u32(&sh.empty[st]));
+                    if (w == 1) signal(&sh.empty[st]);
                     if (j + 1 < n_tiles && needed(w, tile_at(j + 1))) first_products(w, j + 1);
                 }
             }
-            commit(smem_u32(&sh.done));
-            commit(smem_u32(&sh.drain));
-            wait(smem_u32(&sh.drain), 0, nullptr, a.status, kPromptWaitDrain);
+            signal(&sh.done);
+            signal(&sh.drain);
+            wait_warp(smem_u32(&sh.drain), 0, nullptr, a.status, kPromptWaitDrain);
         }
     }
     fence_before();

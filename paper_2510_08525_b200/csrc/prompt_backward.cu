@@ -74,63 +74,21 @@ __global__ void __launch_bounds__(256) prompt_stats_kernel(const __grid_constant
 
 // ---- what both kernels do with a score ------------------------------------------------------------------
 
-struct ScoreConst {
-    float sl2, cap2, zs;  // scale * log2(e); cap * log2(e); scale / cap
-};
-
-// 32 products q.k -> scores in the log2 domain, and (CAP) the slopes of the cap, 1 - tanh^2.  `big`: some |z| of the
-// warp is beyond the series.
+// 32 products q.k -> scores in the log2 domain, and (CAP) the slopes of the cap, 1 - tanh^2.
 template <bool CAP>
-__device__ __forceinline__ void capped(const ScoreConst& k, bool vote, float (&s)[32], float (&f)[CAP ? 32 : 1])
+__device__ __forceinline__ void capped(const Cap& cap, float sl2, bool vote, float (&s)[32], float (&f)[CAP ? 32 : 1])
 {
     if constexpr (!CAP) {
 #pragma unroll
-        for (int c = 0; c < 32; ++c) s[c] *= k.sl2;
+        for (int c = 0; c < 32; ++c) s[c] *= sl2;
     } else {
-        float big = 0.f;
+        cap.apply(s, vote);
+        const float2 k = make_float2(-1.f / (cap.cap2 * cap.cap2), -1.f / (cap.cap2 * cap.cap2));
 #pragma unroll
-        for (int c = 0; c < 32; ++c) big = fmaxf(big, fabsf(s[c]));
-        if (__any_sync(0xffffffffu, vote && big * k.zs > 0.3f)) {
-            const float e2 = 2.f * kLog2e * k.zs;
-#pragma unroll
-            for (int c = 0; c < 32; ++c) {
-                const float t = 1.f - __fdividef(2.f, 1.f + ex2(s[c] * e2));
-                s[c] = t * k.cap2;
-                f[c] = fmaf(-t, t, 1.f);
-            }
-        } else {
-#pragma unroll
-            for (int c = 0; c < 32; ++c) {
-                const float z = s[c] * k.zs, y = z * z;
-                const float t = z * fmaf(y, fmaf(y, fmaf(y, fmaf(y, 62.f / 2835, -17.f / 315), 2.f / 15), -1.f / 3), 1.f);
-                s[c] = t * k.cap2;
-                f[c] = fmaf(-t, t, 1.f);
-            }
-        }
-    }
-}
-
-__device__ __forceinline__ void load32(uint32_t addr, float (&s)[32])
-{
-    tmem_ld32(addr, s);
-    wait_ld();
-#pragma unroll
-    for (int c = 0; c < 32; ++c) asm volatile("" : "+f"(s[c]));  // nothing of it is used before the wait
-}
-
-__device__ __forceinline__ void store_row(__nv_bfloat16* dst, uint32_t src, int cols, float scale, bool any, bool mine)
-{
-    for (int c = 0; c < cols; c += 32) {
-        float o[32];
-        if (any) load32(src + c, o);
-        else
-            for (int i = 0; i < 32; ++i) o[i] = 0.f;
-        if (mine) {
-            uint4* p = reinterpret_cast<uint4*>(dst + c);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                p[i] = make_uint4(bf16x2(o[8 * i] * scale, o[8 * i + 1] * scale), bf16x2(o[8 * i + 2] * scale, o[8 * i + 3] * scale),
-                                  bf16x2(o[8 * i + 4] * scale, o[8 * i + 5] * scale), bf16x2(o[8 * i + 6] * scale, o[8 * i + 7] * scale));
+        for (int c = 0; c < 32; c += 2) {
+            const float2 x = make_float2(s[c], s[c + 1]), y = fma2(mul2(x, x), k, make_float2(1.f, 1.f));
+            f[c] = y.x;
+            f[c + 1] = y.y;
         }
     }
 }
@@ -183,7 +141,6 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const bool valid = find_tile(a, true, kRows, blockIdx.x / a.kv_heads, doc, tile);
         if (lane == 0) {
             sh.valid = valid;
-            sh.abort = 0;
             if (valid) {
                 const DocRange r = doc_range(a, doc);
                 tile = (r.kn + kRows - 1) / kRows - 1 - tile;  // a document's first keys are seen by the most queries
@@ -201,6 +158,14 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 sh.u0 = lower / kCols;
                 sh.n_u = upper > lower ? (upper + kCols - 1) / kCols - sh.u0 : 0;
             }
+        }
+    } else if (warp == 8) {
+        if (lane == 0) {
+            prefetch_map(&map_q);
+            prefetch_map(&map_k);
+            prefetch_map(&map_v);
+            prefetch_map(&map_do);
+            sh.abort = 0;
             mbar_init(smem_u32(&sh.kv_full), 1);
             for (int i = 0; i < F::kStages; ++i) {
                 mbar_init(smem_u32(&sh.full[i]), 1);
@@ -215,14 +180,18 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             mbar_init(smem_u32(&sh.drain), 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
+    } else if (warp == 9) {
+        tmem_alloc(smem_u32(&sh.tmem), 512);
+        fence_before();
     }
     __syncthreads();
-    if (!sh.valid) return;
-    if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 512);
-    fence_before();
-    __syncthreads();
     fence_after();
-    const uint32_t tmem = sh.tmem, dV = tmem + 256, dK = tmem + 256 + D;
+    const uint32_t tmem = sh.tmem;
+    if (!sh.valid) {
+        if (warp == 9) tmem_free(tmem, 512);
+        return;
+    }
+    const uint32_t dV = tmem + 256, dK = tmem + 256 + D;
     const uint32_t k_smem = smem_u32(smem), v_smem = k_smem + F::kRowTile, ring = v_smem + F::kRowTile;
     const int n_u = sh.n_u, steps = n_u * a.group;  // step n: query tile u0 + n % n_u of query head n / n_u of the group
 
@@ -235,7 +204,8 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const bool mine = row < sh.rows;
         // the key is seen from positions lo .. hi-1
         const int lo = j < sh.prefix ? INT_MIN / 2 : j, hi = full_head || j < a.sink ? INT_MAX / 2 : j + a.window;
-        const ScoreConst sc{a.scale * kLog2e, a.softcap * kLog2e, CAP ? a.scale / a.softcap : 0.f};
+        const Cap cap(CAP ? a.softcap : 1.f, a.scale);
+        const float sl2 = a.scale * kLog2e;
         bool ok = true;
         int g = 0, u = w;  // of step n
         while (n_u > 0 && u >= n_u) { u -= n_u; ++g; }
@@ -253,8 +223,8 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 float s[32], f[CAP ? 32 : 1];
-                load32(S + half * 32, s);
-                capped<CAP>(sc, mine, s, f);
+                tmem_read32(S + half * 32, s);
+                capped<CAP>(cap, sl2, mine, s, f);
                 const int d0 = p0 + half * 32 - j;  // distance of column 0
                 if (BIAS) {
 #pragma unroll
@@ -276,7 +246,7 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 for (int c = 0; c < 16; ++c) packed[c] = bf16x2(s[2 * c], s[2 * c + 1]);
                 tmem_st16(S + half * 16, packed);
                 float d[32];
-                load32(dP + half * 32, d);
+                tmem_read32(dP + half * 32, d);
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
                     const float4 x = stat[half * 16 + c / 2];
@@ -302,9 +272,11 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             fence_after();
         }
         if (ok) {
-            const long long at = ((long long)(sh.k0 + row) * a.kv_heads + kv_head) * D;
-            if (w == 0) store_row(a.dv + at, dV + lanes, D, 1.f, steps > 0, mine);
-            else store_row(a.dk + at, dK + lanes, D, a.scale, steps > 0, mine);
+            // through shared memory: the keys' tile for dV, the values' for dK (neither is needed any more)
+            const int part = (warp & 3) * 32;
+            const long long at = ((long long)(sh.k0 + part) * a.kv_heads + kv_head) * D;
+            write_rows<D>(smem + w * F::kRowTile + part * D * 2, (w == 0 ? dV : dK) + lanes, w == 0 ? 1.f : a.scale, steps > 0,
+                          (w == 0 ? a.dv : a.dk) + at, (long long)a.kv_heads * D, sh.rows - part, lane);
         }
     } else if (warp == 8) {
         // ------------------------------------------------------------------ tile loads
@@ -432,8 +404,8 @@ struct RowsK {
 struct RowsShared {
     uint64_t q_full, full[6], empty[6], sd_full[2], ds_full[2], done, clean, drain;
     uint32_t tmem;
-    int abort, valid;
-    int q0, rows, pos0, k0, kn, prefix, a_end, b0, n_tiles, sub_a[2], sub_b[2], sub_e[2];  // as in the forward pass, key tiles of 64
+    int abort;
+    RowTile at;  // as in the forward pass, key tiles of 64
 };
 
 template <int D, bool CAP, bool BIAS>
@@ -445,8 +417,6 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     extern __shared__ __align__(1024) uint8_t smem[];
     RowsShared& sh = *reinterpret_cast<RowsShared*>(smem + 4 * F::kRowTile + F::kStages * 2 * F::kColTile);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-    const int head = blockIdx.x % a.q_heads, kv_head = head / a.group;
-    const bool full_head = a.full[kv_head] != 0;
     volatile int* abort_flag = &sh.abort;
 
     if ((smem_u32(smem) & 1023u) != 0) {
@@ -454,38 +424,14 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         return;
     }
     if (warp == 0) {
-        int doc = 0, tile = 0;
-        const bool valid = find_tile(a, false, 2 * kRows, blockIdx.x / a.q_heads, doc, tile);
+        find_row_tile(a, kCols, sh.at);
+    } else if (warp == 8) {
         if (lane == 0) {
-            sh.valid = valid;
+            prefetch_map(&map_q);
+            prefetch_map(&map_k);
+            prefetch_map(&map_v);
+            prefetch_map(&map_do);
             sh.abort = 0;
-            if (valid) {
-                const DocRange r = doc_range(a, doc);
-                sh.q0 = r.q0 + tile * 2 * kRows;
-                sh.rows = min(2 * kRows, r.qn - tile * 2 * kRows);
-                sh.pos0 = tile * 2 * kRows + r.kn - r.qn;
-                sh.k0 = r.k0;
-                sh.kn = r.kn;
-                sh.prefix = r.prefix;
-                const int hi = min(r.kn, max(sh.pos0 + sh.rows, r.prefix));
-                const int end = hi > 0 ? (hi + kCols - 1) / kCols : 0;
-                int a_end = end, b0 = end;
-                if (!full_head) {
-                    a_end = min(end, (min(a.sink, max(hi, 0)) + kCols - 1) / kCols);
-                    b0 = max(a_end, max(0, sh.pos0 - a.window + 1) / kCols);
-                }
-                sh.a_end = a_end;
-                sh.b0 = b0;
-                sh.n_tiles = a_end + max(0, end - b0);
-                for (int w = 0; w < 2; ++w) {
-                    const int rows = min(kRows, sh.rows - w * kRows), first = sh.pos0 + w * kRows;
-                    const int seen = rows > 0 ? max(0, min(r.kn, max(first + rows, r.prefix))) : 0;
-                    const int e = (seen + kCols - 1) / kCols;
-                    sh.sub_a[w] = full_head ? e : min(e, (a.sink + kCols - 1) / kCols);
-                    sh.sub_b[w] = max(sh.sub_a[w], max(0, first - a.window + 1) / kCols);
-                    sh.sub_e[w] = max(e, sh.sub_b[w]);
-                }
-            }
             mbar_init(smem_u32(&sh.q_full), 1);
             for (int i = 0; i < F::kStages; ++i) {
                 mbar_init(smem_u32(&sh.full[i]), 1);
@@ -500,17 +446,21 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             mbar_init(smem_u32(&sh.drain), 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
+    } else if (warp == 9) {
+        tmem_alloc(smem_u32(&sh.tmem), 512);
+        fence_before();
     }
-    __syncthreads();
-    if (!sh.valid) return;
-    if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 512);
-    fence_before();
     __syncthreads();
     fence_after();
     const uint32_t tmem = sh.tmem;
-    const int n_tiles = sh.n_tiles, a_end = sh.a_end, b0 = sh.b0, kn = sh.kn, prefix = sh.prefix;
+    if (!sh.at.valid) {
+        if (warp == 9) tmem_free(tmem, 512);
+        return;
+    }
+    const int n_tiles = sh.at.n_tiles, a_end = sh.at.a_end, b0 = sh.at.b0, kn = sh.at.kn, prefix = sh.at.prefix;
+    const int n_sub = sh.at.n_sub, kv_head = sh.at.kv_head;
+    const bool full_head = a.full[kv_head] != 0;
     const uint32_t q_smem = smem_u32(smem), o_smem = q_smem + 2 * F::kRowTile, ring = q_smem + 4 * F::kRowTile;
-    const int n_sub = sh.rows > kRows ? 2 : 1;
     auto tile_at = [&](int j) { return j < a_end ? j : b0 + j - a_end; };
 
     if (warp < 8) {
@@ -518,16 +468,17 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const int w = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t S = tmem + lanes + w * 128, dP = S + 64;
-        const int first = sh.pos0 + w * kRows, pos = first + row, last = first + kRows - 1;
-        const bool mine = w * kRows + row < sh.rows;
+        const int first = sh.at.pos0[w], pos = first + row, last = first + kRows - 1, head = sh.at.head[w];
+        const bool mine = row < sh.at.rows[w];
         const int hi = min(kn, max(pos + 1, prefix)), lo = full_head ? 0 : pos - a.window + 1, sink = full_head ? 0 : min(a.sink, hi);
-        const ScoreConst sc{a.scale * kLog2e, a.softcap * kLog2e, CAP ? a.scale / a.softcap : 0.f};
+        const Cap cap(CAP ? a.softcap : 1.f, a.scale);
+        const float sl2 = a.scale * kLog2e;
         const float slope2 = BIAS ? a.slopes[head] * kLog2e : 0.f;
-        const int q = sh.q0 + w * kRows + row;
+        const int q = sh.at.q0[w] + row;
         const float2 stat = mine ? a.stats[(long long)head * a.q_tokens + q] : make_float2(INFINITY, 0.f);
         bool ok = true;
         int done = 0;
-        const int sub_a = sh.sub_a[w], sub_b = sh.sub_b[w], sub_e = sh.sub_e[w];
+        const int sub_a = sh.at.sub_a[w], sub_b = sh.at.sub_b[w], sub_e = sh.at.sub_e[w];
         for (int t = sub_a > 0 ? 0 : sub_b; t < sub_e; t = t + 1 == sub_a ? sub_b : t + 1) {
             const int start = t * kCols;
             ok = wait(smem_u32(&sh.sd_full[w]), done & 1, abort_flag, a.status, kPromptWaitProduct);
@@ -538,8 +489,8 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 float s[32], f[CAP ? 32 : 1];
-                load32(S + half * 32, s);
-                capped<CAP>(sc, mine, s, f);
+                tmem_read32(S + half * 32, s);
+                capped<CAP>(cap, sl2, mine, s, f);
                 const int c0 = start + half * 32;
                 if (BIAS) {
 #pragma unroll
@@ -553,7 +504,7 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     for (int c = 0; c < 32; ++c) s[c] = see >> c & 1 ? s[c] : 0.f;
                 }
                 float d[32];
-                load32(dP + half * 32, d);
+                tmem_read32(dP + half * 32, d);
                 uint32_t packed[16];
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
@@ -577,15 +528,18 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             ok = wait(smem_u32(&sh.done), 0, abort_flag, a.status, kPromptWaitProduct);
             fence_after();
         }
-        if (ok && w < n_sub)
-            store_row(a.dq + ((long long)q * a.q_heads + head) * D, tmem + lanes + 256 + w * D, D, a.scale, done > 0, mine);
+        if (ok && w < n_sub) {  // through shared memory: the sub-tile's queries are not needed any more
+            const int part = (warp & 3) * 32;
+            write_rows<D>(smem + w * F::kRowTile + part * D * 2, tmem + lanes + 256 + w * D, a.scale, done > 0,
+                          a.dq + ((long long)(sh.at.q0[w] + part) * a.q_heads + head) * D, (long long)a.q_heads * D, sh.at.rows[w] - part, lane);
+        }
     } else if (warp == 8) {
         // ------------------------------------------------------------------ tile loads
         if (lane == 0 && n_tiles > 0) {
             mbar_expect_tx(smem_u32(&sh.q_full), 2 * n_sub * F::kRowTile);
             for (int w = 0; w < n_sub; ++w) {
-                load_rows<D>(q_smem + w * F::kRowTile, kRows, &map_q, head, sh.q0 + w * kRows, smem_u32(&sh.q_full));
-                load_rows<D>(o_smem + w * F::kRowTile, kRows, &map_do, head, sh.q0 + w * kRows, smem_u32(&sh.q_full));
+                load_rows<D>(q_smem + w * F::kRowTile, kRows, &map_q, sh.at.head[w], sh.at.q0[w], smem_u32(&sh.q_full));
+                load_rows<D>(o_smem + w * F::kRowTile, kRows, &map_do, sh.at.head[w], sh.at.q0[w], smem_u32(&sh.q_full));
             }
             int j = 0;
             bool ok = true;
@@ -595,7 +549,7 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 if (!ok) break;
                 const uint32_t bar = smem_u32(&sh.full[st]), dst = ring + st * 2 * F::kColTile;
                 mbar_expect_tx(bar, 2 * F::kColTile);
-                const int token = sh.k0 + tile_at(j) * kCols;
+                const int token = sh.at.k0 + tile_at(j) * kCols;
                 load_rows<D>(dst, kCols, &map_k, kv_head, token, bar);
                 load_rows<D>(dst + F::kColTile, kCols, &map_v, kv_head, token, bar);
             }
@@ -622,7 +576,7 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         if (n_tiles > 0) {
             constexpr uint32_t kScores = instr_desc(kRows, kCols, false), kGrads = instr_desc(kRows, D, true);
             int used[2] = {0, 0};
-            const int sub_a[2] = {sh.sub_a[0], sh.sub_a[1]}, sub_b[2] = {sh.sub_b[0], sh.sub_b[1]}, sub_e[2] = {sh.sub_e[0], sh.sub_e[1]};
+            const int sub_a[2] = {sh.at.sub_a[0], sh.at.sub_a[1]}, sub_b[2] = {sh.at.sub_b[0], sh.at.sub_b[1]}, sub_e[2] = {sh.at.sub_e[0], sh.at.sub_e[1]};
             auto needed = [&](int w, int t) { return t < sub_a[w] || (t >= sub_b[w] && t < sub_e[w]); };
             auto signal = [&](uint64_t* bar) {
                 if (elect_one()) commit(smem_u32(bar));
@@ -693,7 +647,6 @@ template <int D, bool CAP, bool BIAS>
 cudaError_t launch_one(const PromptArgs& a, const Maps& m, cudaStream_t stream)
 {
     const long long k_tiles = (long long)a.k_tokens / kRows + (a.n_docs < a.k_tokens ? a.n_docs : a.k_tokens);
-    const long long q_tiles = (long long)a.q_tokens / (2 * kRows) + (a.n_docs < a.q_tokens ? a.n_docs : a.q_tokens);
     const dim3 stats((a.q_tokens + 31) / 32, (a.q_heads + 7) / 8);
     prompt_stats_kernel<D><<<stats, 256, 0, stream>>>(a);
     cudaError_t e = cudaGetLastError();
@@ -701,7 +654,7 @@ cudaError_t launch_one(const PromptArgs& a, const Maps& m, cudaStream_t stream)
     prompt_keys_kernel<D, CAP, BIAS><<<(unsigned)(k_tiles * a.kv_heads), kThreads, Keys<D>::kSmem, stream>>>(a, m.q, m.k, m.v, m.dout);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    prompt_rows_kernel<D, CAP, BIAS><<<(unsigned)(q_tiles * a.q_heads), kThreads, RowsK<D>::kSmem, stream>>>(a, m.q, m.k, m.v, m.dout);
+    prompt_rows_kernel<D, CAP, BIAS><<<(unsigned)row_tile_blocks(a), kThreads, RowsK<D>::kSmem, stream>>>(a, m.q, m.k, m.v, m.dout);
     return cudaGetLastError();
 }
 

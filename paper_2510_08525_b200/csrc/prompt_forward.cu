@@ -1,7 +1,7 @@
 // The forward pass of prompt attention on the tensor cores.
 //
-// One CTA takes 256 queries of one head of one document -- two sub-tiles of 128 rows -- and walks the 128-key tiles
-// that any of them sees.  Per key tile and sub-tile: S = Q.K^T (128 x 128, both operands in shared memory, fp32 in
+// One CTA takes two sub-tiles of 128 query rows -- the same queries of two heads of a KV head where the heads pair up,
+// else 256 queries of one head -- and walks the 128-key tiles that any of them sees.  Per key tile and sub-tile: S = Q.K^T (128 x 128, both operands in shared memory, fp32 in
 // tensor memory); a warpgroup, one thread per query row, turns S into P = exp2(s - m) and writes it as bf16 over S;
 // O += P.V with P read from tensor memory.  Two sub-tiles so that one's products run while the other's softmax does.
 //
@@ -25,7 +25,6 @@ using namespace tc;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kRows = 128;          // queries of a sub-tile, keys of a tile
-constexpr int kPolyPairs = 4;      // the exponential unit alone would need as long as the tensor core
 constexpr int kBlock = kRows * 128; // bytes of a [128 rows][64 elements] block
 
 template <int D>
@@ -39,15 +38,13 @@ struct Fwd {
 struct FwdShared {
     uint64_t q_full, full[10], empty[10], s_full[2], p_full[2][2], pv_done[2], clean, drain;
     uint32_t tmem;
-    int abort, valid;
-    int q0, rows, pos0, k0, kn, prefix;    // the CTA's queries, its document's keys
-    int a_end, b0, n_tiles;                // its key tiles: 0 .. a_end-1, then from b0 on
-    int sub_a[2], sub_b[2], sub_e[2];      // those a sub-tile needs: 0 .. a-1 and b .. e-1
+    int abort;
+    RowTile at;
 };
 
-// P = 2^(s factor - base) of a row's 128 scores, as bf16 to tensor memory, and their sums; POLY > 0: one pair in POLY on
-// the FMA pipe.  64 keys at a time, so that the product starts on the first.
-template <int POLY>
+// P = 2^(s factor - base) of a row's 128 scores, as bf16 to tensor memory, and their sums.  64 keys at a time, so that
+// the product starts on the first.  (A polynomial on the FMA pipe for a quarter or half of the exponentials, to spare the
+// exponential unit, measured 4 to 8 % slower: with one warp per scheduler and sub-tile it is the instructions that count.)
 __device__ __forceinline__ void exponentials(float (&s)[kRows], float factor, float base, float2 (&sum)[2], uint32_t P, uint64_t* done, int lane)
 {
     const float2 factor2 = make_float2(factor, factor), base2 = make_float2(-base, -base);
@@ -62,12 +59,9 @@ __device__ __forceinline__ void exponentials(float (&s)[kRows], float factor, fl
         }
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
-            float2 p = make_float2(s[c + i], s[c + i + 1]);
-            if (POLY > 0 && i / 2 % (POLY > 0 ? POLY : 1) == POLY - 1) p = exp2_fma(p);
-            else p = make_float2(ex2(p.x), ex2(p.y));
-            s[c + i] = p.x;
-            s[c + i + 1] = p.y;
-            packed[i / 2] = bf16x2(p.x, p.y);
+            s[c + i] = ex2(s[c + i]);
+            s[c + i + 1] = ex2(s[c + i + 1]);
+            packed[i / 2] = bf16x2(s[c + i], s[c + i + 1]);
         }
         tmem_st16(P + c / 2, packed);
         if (c % 64 == 32) {
@@ -90,8 +84,6 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
     extern __shared__ __align__(1024) uint8_t smem[];
     FwdShared& sh = *reinterpret_cast<FwdShared*>(smem + (2 + F::kStages) * F::kTileBytes);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-    const int head = blockIdx.x % a.q_heads, kv_head = head / a.group;
-    const bool full_head = a.full[kv_head] != 0;
     volatile int* abort_flag = &sh.abort;
 
     if ((smem_u32(smem) & 1023u) != 0) {
@@ -99,38 +91,13 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
         return;
     }
     if (warp == 0) {
-        int doc = 0, tile = 0;
-        const bool valid = find_tile(a, false, 2 * kRows, blockIdx.x / a.q_heads, doc, tile);
+        find_row_tile(a, kRows, sh.at);
+    } else if (warp == 8) {
         if (lane == 0) {
-            sh.valid = valid;
+            prefetch_map(&map_q);
+            prefetch_map(&map_k);
+            prefetch_map(&map_v);
             sh.abort = 0;
-            if (valid) {
-                const DocRange r = doc_range(a, doc);
-                sh.q0 = r.q0 + tile * 2 * kRows;
-                sh.rows = min(2 * kRows, r.qn - tile * 2 * kRows);
-                sh.pos0 = tile * 2 * kRows + r.kn - r.qn;
-                sh.k0 = r.k0;
-                sh.kn = r.kn;
-                sh.prefix = r.prefix;
-                const int hi = min(r.kn, max(sh.pos0 + sh.rows, r.prefix));
-                const int end = hi > 0 ? (hi + kRows - 1) / kRows : 0;
-                int a_end = end, b0 = end;
-                if (!full_head) {
-                    a_end = min(end, (min(a.sink, max(hi, 0)) + kRows - 1) / kRows);
-                    b0 = max(a_end, max(0, sh.pos0 - a.window + 1) / kRows);
-                }
-                sh.a_end = a_end;
-                sh.b0 = b0;
-                sh.n_tiles = a_end + max(0, end - b0);
-                for (int w = 0; w < 2; ++w) {
-                    const int rows = min(kRows, sh.rows - w * kRows), first = sh.pos0 + w * kRows;
-                    const int seen = rows > 0 ? max(0, min(r.kn, max(first + rows, r.prefix))) : 0;
-                    const int e = (seen + kRows - 1) / kRows;
-                    sh.sub_a[w] = full_head ? e : min(e, (a.sink + kRows - 1) / kRows);
-                    sh.sub_b[w] = max(sh.sub_a[w], max(0, first - a.window + 1) / kRows);
-                    sh.sub_e[w] = max(e, sh.sub_b[w]);
-                }
-            }
             mbar_init(smem_u32(&sh.q_full), 1);
             for (int i = 0; i < F::kStages; ++i) {
                 mbar_init(smem_u32(&sh.full[i]), 1);
@@ -146,33 +113,37 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
             mbar_init(smem_u32(&sh.drain), 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
+    } else if (warp == 9) {
+        tmem_alloc(smem_u32(&sh.tmem), 512);
+        fence_before();
     }
-    __syncthreads();
-    if (!sh.valid) return;
-    if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 512);
-    fence_before();
     __syncthreads();
     fence_after();
     const uint32_t tmem = sh.tmem;
-    const int n_tiles = sh.n_tiles, a_end = sh.a_end, b0 = sh.b0, kn = sh.kn, prefix = sh.prefix;
+    if (!sh.at.valid) {
+        if (warp == 9) tmem_free(tmem, 512);
+        return;
+    }
+    const int n_tiles = sh.at.n_tiles, a_end = sh.at.a_end, b0 = sh.at.b0, kn = sh.at.kn, prefix = sh.at.prefix;
+    const int n_sub = sh.at.n_sub, kv_head = sh.at.kv_head;
+    const bool full_head = a.full[kv_head] != 0;
     const uint32_t q_smem = smem_u32(smem), ring = q_smem + 2 * F::kTileBytes;
-    const int n_sub = sh.rows > kRows ? 2 : 1;
     auto tile_at = [&](int j) { return j < a_end ? j : b0 + j - a_end; };
-    // (launched with 384 x 168 = 64512 registers: 256 x 216 + 128 x 72)
-    if (warp < 8) more_registers<216>();
-    else fewer_registers<72>();
+    // (launched with 384 x 168 = 64512 registers: 256 x 232 + 128 x 40)
+    if (warp < 8) more_registers<232>();
+    else fewer_registers<40>();
     if (warp < 8) {
         // ------------------------------------------------------------------ softmax
         const int w = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t S = tmem + lanes + w * kRows, O = tmem + lanes + 2 * kRows + w * D;
-        const int pos = sh.pos0 + w * kRows + row;
-        const bool mine = w * kRows + row < sh.rows;  // else the row is another document's, or behind the last one
-        const int first = sh.pos0 + w * kRows, last = first + kRows - 1;
+        const int first = sh.at.pos0[w], last = first + kRows - 1, pos = first + row, head = sh.at.head[w];
+        const bool mine = row < sh.at.rows[w];  // else the row is another document's, or behind the last one
         const int hi = min(kn, max(pos + 1, prefix)), lo = full_head ? 0 : pos - a.window + 1, sink = full_head ? 0 : min(a.sink, hi);
         const float sl2 = a.scale * kLog2e, factor = CAP || BIAS ? 1.f : sl2;
         const float slope2 = BIAS ? a.slopes[head] * kLog2e : 0.f;
-        const int sub_a = sh.sub_a[w], sub_b = sh.sub_b[w], sub_e = sh.sub_e[w];
+        const int sub_a = sh.at.sub_a[w], sub_b = sh.at.sub_b[w], sub_e = sh.at.sub_e[w];
+        const Cap cap(CAP ? a.softcap : 1.f, a.scale);
         float m = -INFINITY, l = 0.f;
         int done = 0;  // tiles of this sub-tile so far
         bool ok = true;
@@ -204,24 +175,7 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
 #pragma unroll
                         for (int c = 0; c < kRows; ++c) s[c] = see[c / 32] >> (c & 31) & 1 ? s[c] : 0.f;
                     }
-                    // cap tanh(z) in the log2 domain.  Small z (most scores are far below the cap): the Taylor series,
-                    // off by 1e-8 of z at 0.3, on the FMA pipe; else 1 - 2 / (1 + e^2z) with its exp2 and division
-                    const float cap2 = a.softcap * kLog2e, zs = a.scale / a.softcap;
-                    float big = 0.f;
-#pragma unroll
-                    for (int c = 0; c < kRows; ++c) big = fmaxf(big, fabsf(s[c]));
-                    if (__any_sync(0xffffffffu, mine && big * zs > 0.3f)) {
-                        const float e2 = 2.f * kLog2e * zs;
-#pragma unroll
-                        for (int c = 0; c < kRows; ++c) s[c] = cap2 - __fdividef(2.f * cap2, 1.f + ex2(s[c] * e2));
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < kRows; ++c) {
-                            const float z = s[c] * zs, y = z * z;
-                            const float f = fmaf(y, fmaf(y, fmaf(y, fmaf(y, 62.f / 2835, -17.f / 315), 2.f / 15), -1.f / 3), 1.f);
-                            s[c] = z * cap2 * f;
-                        }
-                    }
+                    cap.apply(s, mine);
                 }
                 if (BIAS) {
                     if (causal_past) {  // -slope (pos - start - c): linear in the column
@@ -265,43 +219,23 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
                     }
                 }
                 const float base = m == -INFINITY ? 0.f : m;
-                // (where every key is seen: the FMA pipe's exponential wants finite arguments)
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                if (plain) exponentials<kPolyPairs>(s, factor, base, sum, S, sh.p_full[w], lane);
-                else exponentials<0>(s, factor, base, sum, S, sh.p_full[w], lane);
+                exponentials(s, factor, base, sum, S, sh.p_full[w], lane);
                 l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 ++done;
             }
         if (ok && w < n_sub) {
-            const long long at = (long long)(sh.q0 + w * kRows + row) * a.q_heads + head;
             if (done > 0) {
                 ok = wait(smem_u32(&sh.pv_done[w]), (done - 1) & 1, abort_flag, a.status, kPromptWaitProduct);
                 fence_after();
             }
             if (ok) {
-                const float inv = l > 0.f ? 1.f / l : 0.f;
-                if (mine && a.lse) a.lse[at] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
-#pragma unroll
-                for (int c = 0; c < D; c += 32) {
-                    float o[32];
-                    if (done > 0) {
-                        tmem_ld32(O + c, o);
-                        wait_ld();
-                    }
-                    uint32_t x[16];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        asm volatile("" : "+f"(o[i]));
-                        if (inv == 0.f) o[i] = 0.f;  // a row that sees nothing
-                    }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = bf16x2(o[2 * i] * inv, o[2 * i + 1] * inv);
-                    if (mine) {
-                        uint4* dst = reinterpret_cast<uint4*>(a.out + at * D + c);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) dst[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-                    }
-                }
+                const float inv = l > 0.f ? 1.f / l : 0.f;  // (0: a row that sees nothing)
+                const long long q0 = sh.at.q0[w];
+                if (mine && a.lse) a.lse[(q0 + row) * a.q_heads + head] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                // through shared memory (the sub-tile's queries are not needed any more), so that whole rows go out
+                write_rows<D>(smem + w * F::kTileBytes + (warp & 3) * 32 * D * 2, O, inv, done > 0, a.out + (q0 + (warp & 3) * 32) * a.q_heads * D + head * D,
+                              (long long)a.q_heads * D, sh.at.rows[w] - (warp & 3) * 32, lane);
             }
         }
     } else if (warp == 8) {
@@ -310,7 +244,7 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
             mbar_expect_tx(smem_u32(&sh.q_full), n_sub * F::kTileBytes);
             for (int w = 0; w < n_sub; ++w)
                 for (int b = 0; b < D / 64; ++b)
-                    load_box(q_smem + w * F::kTileBytes + b * kBlock, &map_q, b * 64, head, sh.q0 + w * kRows, smem_u32(&sh.q_full));
+                    load_box(q_smem + w * F::kTileBytes + b * kBlock, &map_q, b * 64, sh.at.head[w], sh.at.q0[w], smem_u32(&sh.q_full));
             int issued = 0;
             bool ok = true;
             for (; issued < 2 * n_tiles; ++issued) {
@@ -318,7 +252,7 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
                 ok = wait(smem_u32(&sh.empty[slot]), (issued / F::kStages & 1) ^ 1, abort_flag, a.status, kPromptWaitStage);
                 if (!ok) break;
                 mbar_expect_tx(smem_u32(&sh.full[slot]), F::kTileBytes);
-                const int token = sh.k0 + tile_at(issued >> 1) * kRows;
+                const int token = sh.at.k0 + tile_at(issued >> 1) * kRows;
                 for (int b = 0; b < D / 64; ++b)
                     load_box(ring + slot * F::kTileBytes + b * kBlock, issued & 1 ? &map_v : &map_k, b * 64, kv_head, token,
                              smem_u32(&sh.full[slot]));
@@ -348,7 +282,7 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
             constexpr uint32_t kQK = instr_desc(kRows, kRows, false), kPV = instr_desc(kRows, D, true);
             bool ok = true;
             int used[2] = {0, 0};  // P tiles of the sub-tile multiplied so far
-            const int sub_a[2] = {sh.sub_a[0], sh.sub_a[1]}, sub_b[2] = {sh.sub_b[0], sh.sub_b[1]}, sub_e[2] = {sh.sub_e[0], sh.sub_e[1]};
+            const int sub_a[2] = {sh.at.sub_a[0], sh.at.sub_a[1]}, sub_b[2] = {sh.at.sub_b[0], sh.at.sub_b[1]}, sub_e[2] = {sh.at.sub_e[0], sh.at.sub_e[1]};
             auto needed = [&](int w, int t) { return t < sub_a[w] || (t >= sub_b[w] && t < sub_e[w]); };
             auto stage = [&](int i) { return ring + i % F::kStages * F::kTileBytes; };
             auto loaded = [&](int i) {
@@ -422,8 +356,7 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
 template <int D, bool CAP, bool BIAS>
 cudaError_t launch_one(const PromptArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t stream)
 {
-    const long long tiles = (long long)a.q_tokens / (2 * kRows) + (a.n_docs < a.q_tokens ? a.n_docs : a.q_tokens);
-    prompt_forward_kernel<D, CAP, BIAS><<<(unsigned)(tiles * a.q_heads), Fwd<D>::kThreads, Fwd<D>::kSmem, stream>>>(a, q, k, v);
+    prompt_forward_kernel<D, CAP, BIAS><<<(unsigned)row_tile_blocks(a), Fwd<D>::kThreads, Fwd<D>::kSmem, stream>>>(a, q, k, v);
     return cudaGetLastError();
 }
 

@@ -53,6 +53,12 @@ enum : int { kPromptWaitLoad = 101, kPromptWaitProduct = 102, kPromptWaitSoftmax
 __device__ __forceinline__ bool find_tile(const PromptArgs& a, bool keys, int rows, int index, int& doc, int& tile)
 {
     const int lane = threadIdx.x & 31;
+    if (a.n_docs == 1) {
+        const DocRange r = doc_range(a, 0);
+        doc = 0;
+        tile = ((keys ? r.kn : r.qn) + rows - 1) / rows - 1 - index;
+        return tile >= 0;
+    }
     int left = index;
     for (int top = a.n_docs; top > 0; top -= 256) {
         int n[8], sum = 0;
@@ -89,6 +95,59 @@ __device__ __forceinline__ bool find_tile(const PromptArgs& a, bool keys, int ro
         left -= __shfl_sync(0xffffffffu, upto, 31);
     }
     return false;
+}
+
+// The queries of a CTA of the forward or rows kernel: two sub-tiles of up to 128, and the key tiles they see.  Where the
+// query heads of a KV head pair up, the sub-tiles are the same 128 queries of two heads (both read the same keys to
+// the last one, and short documents waste less of a tile); else 256 queries of one head.
+struct RowTile {
+    int valid, kv_head, n_sub;
+    int head[2], q0[2], rows[2], pos0[2];  // per sub-tile: head, first packed query, how many, position of the first
+    int k0, kn, prefix;                    // the document's keys
+    int a_end, b0, n_tiles;                // key tiles of the CTA: 0 .. a_end-1, then from b0 on
+    int sub_a[2], sub_b[2], sub_e[2];      // those a sub-tile needs: 0 .. a-1 and b .. e-1
+};
+__host__ __device__ inline bool heads_pair(int group) { return group % 2 == 0; }
+inline long long row_tile_blocks(const PromptArgs& a)
+{
+    const bool pair = heads_pair(a.group);
+    return ((long long)a.q_tokens / (pair ? 128 : 256) + (a.n_docs < a.q_tokens ? a.n_docs : a.q_tokens)) * (pair ? a.q_heads / 2 : a.q_heads);
+}
+// One whole warp; `keys`: keys of a tile.
+__device__ __forceinline__ void find_row_tile(const PromptArgs& a, int keys, RowTile& t)
+{
+    const bool pair = heads_pair(a.group);
+    const int units = pair ? a.q_heads / 2 : a.q_heads, span = pair ? 128 : 256;
+    int doc = 0, tile = 0;
+    const bool valid = find_tile(a, false, span, blockIdx.x / units, doc, tile);
+    if ((threadIdx.x & 31) != 0) return;
+    t.valid = valid;
+    if (!valid) return;
+    const DocRange r = doc_range(a, doc);
+    const int unit = blockIdx.x % units, first = tile * span;
+    t.k0 = r.k0;
+    t.kn = r.kn;
+    t.prefix = r.prefix;
+    t.n_sub = pair || r.qn - first > 128 ? 2 : 1;
+    t.kv_head = (pair ? 2 * unit : unit) / a.group;
+    const bool full = a.full[t.kv_head] != 0;
+    int hi = 0;
+    for (int w = 0; w < 2; ++w) {
+        const int from = first + (pair ? 0 : w * 128);
+        t.head[w] = pair ? 2 * unit + w : unit;
+        t.q0[w] = r.q0 + from;
+        t.rows[w] = max(0, min(128, r.qn - from));
+        t.pos0[w] = from + r.kn - r.qn;
+        const int seen = t.rows[w] > 0 ? max(0, min(r.kn, max(t.pos0[w] + t.rows[w], r.prefix))) : 0;
+        const int e = (seen + keys - 1) / keys;
+        t.sub_a[w] = full ? e : min(e, (a.sink + keys - 1) / keys);
+        t.sub_b[w] = max(t.sub_a[w], max(0, t.pos0[w] - a.window + 1) / keys);
+        t.sub_e[w] = max(e, t.sub_b[w]);
+        hi = max(hi, e);
+    }
+    t.a_end = full ? hi : min(hi, (a.sink + keys - 1) / keys);
+    t.b0 = full ? hi : max(t.a_end, max(0, t.pos0[0] - a.window + 1) / keys);
+    t.n_tiles = t.a_end + max(0, hi - t.b0);
 }
 
 // Bits c of 32 with lo <= c < hi.

@@ -96,6 +96,8 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
         : "memory");
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
 // Registers of a warpgroup's threads from here on (every warp of it executes this).
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -187,6 +189,15 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const float* r)
         : "memory");
 }
 
+// 32 columns, usable at once.
+__device__ __forceinline__ void tmem_read32(uint32_t addr, float (&s)[32])
+{
+    tmem_ld32(addr, s);
+    wait_ld();
+#pragma unroll
+    for (int c = 0; c < 32; ++c) asm volatile("" : "+f"(s[c]));  // nothing of it is used before the wait
+}
+
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
@@ -227,22 +238,75 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
-// 2^x on the FMA pipe, for finite x up to about 120 (2^-126 below that): x = n + f with |f| <= 1/2, a polynomial of
-// degree 4 in f (fitted to the smallest largest relative error, 2.6e-6), and n added to its exponent.
-__device__ __forceinline__ float2 exp2_fma(float2 x)
+
+// A warp's 32 result rows of D columns in tensor memory, times `scale` (each row its own), rounded to bf16, to rows
+// `stride` elements apart, the first `valid` of them.  `stage`: the warp's 32 * D * 2 bytes of shared memory: a thread
+// holds one row, and storing it as it is would touch 32 rows per instruction.  `any` false: zeros.
+template <int D>
+__device__ __forceinline__ void write_rows(uint8_t* stage, uint32_t src, float scale, bool any, __nv_bfloat16* dst, long long stride, int valid, int lane)
 {
-    const float2 magic = make_float2(12582912.f, 12582912.f);  // 1.5 * 2^23: the sum's low bits are round(x)
-    x.x = fmaxf(x.x, -126.f);
-    x.y = fmaxf(x.y, -126.f);
-    const float2 n = add2(x, magic);
-    const float2 f = add2(x, fma2(n, make_float2(-1.f, -1.f), magic));
-    float2 p = fma2(f, make_float2(0.00957010059f, 0.00957010059f), make_float2(0.0559178602f, 0.0559178602f));
-    p = fma2(p, f, make_float2(0.240247449f, 0.240247449f));
-    p = fma2(p, f, make_float2(0.693121815f, 0.693121815f));
-    p = fma2(p, f, make_float2(0.999999261f, 0.999999261f));
-    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(n.x) << 23)),
-                       __int_as_float(__float_as_int(p.y) + (__float_as_int(n.y) << 23)));
+    constexpr int kChunks = D / 8, kPerStore = 32 / kChunks;  // 16-byte pieces of a row, rows per store instruction
+#pragma unroll
+    for (int c = 0; c < D; c += 32) {
+        float o[32];
+        if (any) tmem_read32(src + c, o);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = any && scale != 0.f ? o[i] * scale : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4*>(stage + lane * D * 2 + (((c / 8 + i) ^ (lane & 7)) << 4)) =
+                make_uint4(bf16x2(o[8 * i], o[8 * i + 1]), bf16x2(o[8 * i + 2], o[8 * i + 3]), bf16x2(o[8 * i + 4], o[8 * i + 5]),
+                           bf16x2(o[8 * i + 6], o[8 * i + 7]));
+    }
+    __syncwarp();
+#pragma unroll 4
+    for (int r = lane / kChunks; r < 32; r += kPerStore)
+        if (r < valid)
+            *reinterpret_cast<uint4*>(dst + r * stride + lane % kChunks * 8) =
+                *reinterpret_cast<const uint4*>(stage + r * D * 2 + (((lane % kChunks) ^ (r & 7)) << 4));
 }
+
+// cap * tanh(x * scale / cap), in the log2 domain.  Where every |z| = |x| scale / cap of a warp's scores is at most 0.4
+// (most are far below the cap), tanh z = z f(z^2) with a polynomial f of four terms fitted to the smallest largest
+// relative error, 1e-7 -- five pairwise instructions for two scores -- ; else 1 - 2 / (1 + e^2z) with its exponential
+// and division.
+struct Cap {
+    float cap2, e2, limit, k0, k1, k2, k3;  // cap * log2(e); 2 log2(e) scale / cap; 0.4 cap / scale; f's coefficients in x
+    __device__ __forceinline__ Cap(float cap, float scale)
+    {
+        const float z = scale / cap;
+        cap2 = cap * 1.4426950408889634f;
+        e2 = 2.f * 1.4426950408889634f * z;
+        limit = 0.4f / z;
+        k0 = 0.999999902f * cap2 * z;
+        k1 = -0.333313625f * cap2 * z * z * z;
+        k2 = 0.132709767f * cap2 * z * z * z * z * z;
+        k3 = -0.0475536035f * cap2 * z * z * z * z * z * z * z;
+    }
+    // N scores of a row in place; `vote`: whether the row has a say in how its warp computes them.
+    template <int N>
+    __device__ __forceinline__ void apply(float (&s)[N], bool vote) const
+    {
+        float big = 0.f;
+#pragma unroll
+        for (int c = 0; c < N; c += 2) big = fmaxf(fmaxf(big, fabsf(s[c])), fabsf(s[c + 1]));
+        if (__any_sync(0xffffffffu, vote && big > limit)) {
+#pragma unroll
+            for (int c = 0; c < N; ++c) s[c] = cap2 - __fdividef(2.f * cap2, 1.f + ex2(s[c] * e2));
+        } else {
+#pragma unroll
+            for (int c = 0; c < N; c += 2) {
+                const float2 x = make_float2(s[c], s[c + 1]), y = mul2(x, x);
+                float2 f = fma2(make_float2(k3, k3), y, make_float2(k2, k2));
+                f = fma2(f, y, make_float2(k1, k1));
+                f = fma2(f, y, make_float2(k0, k0));
+                f = mul2(f, x);
+                s[c] = f.x;
+                s[c + 1] = f.y;
+            }
+        }
+    }
+};
 
 }  // namespace tc
 }  // namespace rlkv

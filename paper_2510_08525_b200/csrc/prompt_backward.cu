@@ -1,10 +1,10 @@
 // The backward pass of prompt attention on the tensor cores, in three launches without atomics:
 //
 //   stats   D_i = sum over head_dim of dout * out, stored with lse (log2 domain) per head and query
-//   keys    one CTA per 128 keys of a KV head: over the queries that see them (64 at a time, every query head of the
-//           group), S^T = K.Q^T and dP^T = V.dO^T, then dV += P^T.dO and dK += dS^T.Q
-//   rows    one CTA per 256 queries of a head: over their keys (64 at a time), S = Q.K^T and dP = dO.V^T, then
-//           dQ += dS.K
+//   rows    one CTA per 256 query rows (two heads, or one): over their keys (64 at a time), S = Q.K^T and dP = dO.V^T,
+//           then dQ += dS.K.  It also corrects D: out was rounded to bf16, and sum_j P (dP - D) is what that changed
+//   keys    one CTA (or one per part of the query heads, in a cluster that adds them up) per 128 keys of a KV head: over
+//           the queries that see them (64 at a time), S^T = K.Q^T and dP^T = V.dO^T, then dV += P^T.dO and dK += dS^T.Q
 //
 // S and dP are computed twice, seven products where five would do, and in return every gradient is summed by one CTA
 // in a fixed order: no atomics on dQ, no fp32 copy of it in memory, the same bits on every run.  P and dS are written
@@ -27,21 +27,21 @@ constexpr int kThreads = 384;
 
 // ---- D and lse ---------------------------------------------------------------------------------------
 
-// One warp per head and 32 queries; half a warp reads a row.  Stored head by head, so that the keys kernel reads
-// consecutive queries.  A query that sees nothing gets lse = +infinity: its P is then exp2(s - infinity) = 0.
+// One warp per head and eight queries, half a warp per row, all loads at once.  Stored head by head, so that the keys
+// kernel reads consecutive queries.  A query that sees nothing gets lse = +infinity: its P is then exp2(s - infinity) = 0.
 template <int D>
 __global__ void __launch_bounds__(256) prompt_stats_kernel(const __grid_constant__ PromptArgs a)
 {
-    constexpr int E = D / 16;  // elements of a lane
+    constexpr int E = D / 16, kTokens = 8;  // elements of a lane, queries of a warp
     const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
     const int h = blockIdx.y * 8 + (threadIdx.x >> 5);
     if (h >= a.q_heads) return;
-    const int t0 = blockIdx.x * 32;
-    float mine = 0.f;
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
+    const int t0 = blockIdx.x * kTokens;
+    float sum[kTokens / 2];
+#pragma unroll
+    for (int i = 0; i < kTokens / 2; ++i) {
         const int t = t0 + 2 * i + half;
-        float s = 0.f;
+        sum[i] = 0.f;
         if (t < a.q_tokens) {
             const long long at = ((long long)t * a.q_heads + h) * D + l16 * E;
             __nv_bfloat162 x[E / 2], y[E / 2];
@@ -55,21 +55,23 @@ __global__ void __launch_bounds__(256) prompt_stats_kernel(const __grid_constant
 #pragma unroll
             for (int e = 0; e < E / 2; ++e) {
                 const float2 u = __bfloat1622float2(x[e]), w = __bfloat1622float2(y[e]);
-                s = fmaf(u.x, w.x, s);
-                s = fmaf(u.y, w.y, s);
+                sum[i] = fmaf(u.x, w.x, sum[i]);
+                sum[i] = fmaf(u.y, w.y, sum[i]);
             }
         }
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        const float even = __shfl_sync(0xffffffffu, s, 0), odd = __shfl_sync(0xffffffffu, s, 16);
-        if (lane == 2 * i) mine = even;
-        if (lane == 2 * i + 1) mine = odd;
     }
     const int t = t0 + lane;
-    if (t < a.q_tokens) {
-        const float lse = a.lse[(long long)t * a.q_heads + h];
-        a.stats[(long long)h * a.q_tokens + t] = make_float2(lse == -INFINITY ? INFINITY : lse * kLog2e, mine);
+    const float lse = lane < kTokens && t < a.q_tokens ? a.lse[(long long)t * a.q_heads + h] : 0.f;
+    float mine = 0.f;
+#pragma unroll
+    for (int i = 0; i < kTokens / 2; ++i) {
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+        const float x = __shfl_sync(0xffffffffu, sum[i], lane & 1 ? 16 : 0);
+        if (lane / 2 == i) mine = x;
     }
+    if (lane < kTokens && t < a.q_tokens)
+        a.stats[(long long)h * a.q_tokens + t] = make_float2(lse == -INFINITY ? INFINITY : lse * kLog2e, mine);
 }
 
 // ---- what both kernels do with a score ------------------------------------------------------------------
@@ -121,14 +123,16 @@ struct KeysShared {
 template <int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do)
+                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const int split)
 {
     using F = Keys<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     float2* stats = reinterpret_cast<float2*>(smem + F::kStats);
     KeysShared& sh = *reinterpret_cast<KeysShared*>(smem + F::kStats + F::kStages * kCols * 8);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-    const int kv_head = blockIdx.x % a.kv_heads;
+    // `split` CTAs, a cluster, share the query heads of a KV head
+    const int rank = blockIdx.x % split, block = blockIdx.x / split, kv_head = block % a.kv_heads;
+    const int heads = a.group / split, head0 = kv_head * a.group + rank * heads;
     const bool full_head = a.full[kv_head] != 0;
     volatile int* abort_flag = &sh.abort;
 
@@ -138,7 +142,7 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     }
     if (warp == 0) {
         int doc = 0, tile = 0;
-        const bool valid = find_tile(a, true, kRows, blockIdx.x / a.kv_heads, doc, tile);
+        const bool valid = find_tile(a, true, kRows, block / a.kv_heads, doc, tile);
         if (lane == 0) {
             sh.valid = valid;
             if (valid) {
@@ -193,7 +197,7 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     }
     const uint32_t dV = tmem + 256, dK = tmem + 256 + D;
     const uint32_t k_smem = smem_u32(smem), v_smem = k_smem + F::kRowTile, ring = v_smem + F::kRowTile;
-    const int n_u = sh.n_u, steps = n_u * a.group;  // step n: query tile u0 + n % n_u of query head n / n_u of the group
+    const int n_u = sh.n_u, steps = n_u * heads;  // step n: query tile u0 + n % n_u of query head head0 + n / n_u
 
     if (warp < 8) {
         // ------------------------------------------------------------------ P and dS, one thread per key
@@ -219,7 +223,7 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const int p0 = (sh.u0 + u) * kCols + sh.off;  // position of column 0
             const bool past = p0 >= j_last;               // every query at or behind every key
             const bool plain = (past || j_last < sh.prefix) && (full_head || j_last < a.sink || p0 + kCols - 1 < sh.j0 + a.window);
-            const float slope2 = BIAS ? a.slopes[kv_head * a.group + g] * kLog2e : 0.f;
+            const float slope2 = BIAS ? a.slopes[head0 + g] * kLog2e : 0.f;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 float s[32], f[CAP ? 32 : 1];
@@ -271,12 +275,26 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             ok = wait(smem_u32(&sh.done), 0, abort_flag, a.status, kPromptWaitProduct);
             fence_after();
         }
-        if (ok) {
+        const int part = (warp & 3) * 32;
+        if (ok && split == 1) {
             // through shared memory: the keys' tile for dV, the values' for dK (neither is needed any more)
-            const int part = (warp & 3) * 32;
             const long long at = ((long long)(sh.k0 + part) * a.kv_heads + kv_head) * D;
             write_rows<D>(smem + w * F::kRowTile + part * D * 2, (w == 0 ? dV : dK) + lanes, w == 0 ? 1.f : a.scale, steps > 0,
                           (w == 0 ? a.dv : a.dk) + at, (long long)a.kv_heads * D, sh.rows - part, lane);
+        } else if (ok) {
+            // this CTA's share of the sums in fp32, for the cluster to add up: dV over the K and V tiles, dK over the ring
+            uint8_t* mine_rows = smem + w * 2 * F::kRowTile + row * D * 4;
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+                float o[32];
+                if (steps > 0) tmem_read32((w == 0 ? dV : dK) + lanes + c, o);
+                else
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) o[x] = 0.f;
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    *reinterpret_cast<float4*>(mine_rows + (((c / 4 + x) ^ (lane & 7)) << 4)) = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+            }
         }
     } else if (warp == 8) {
         // ------------------------------------------------------------------ tile loads
@@ -293,8 +311,8 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 const uint32_t bar = smem_u32(&sh.full[st]), dst = ring + st * 2 * F::kColTile;
                 mbar_expect_tx(bar, 2 * F::kColTile);
                 const int token = sh.q0 + (sh.u0 + u) * kCols;
-                load_rows<D>(dst, kCols, &map_q, kv_head * a.group + g, token, bar);
-                load_rows<D>(dst + F::kColTile, kCols, &map_do, kv_head * a.group + g, token, bar);
+                load_rows<D>(dst, kCols, &map_q, head0 + g, token, bar);
+                load_rows<D>(dst + F::kColTile, kCols, &map_do, head0 + g, token, bar);
                 if (++u == n_u) { u = 0; ++g; }
             }
             if (!ok || *abort_flag) {  // nothing of this CTA's copies may be in flight when it ends
@@ -359,7 +377,7 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int q = (sh.u0 + u) * kCols + lane + 32 * i;
-                x[i] = q < sh.qn ? a.stats[(long long)(kv_head * a.group + g) * a.q_tokens + sh.q0 + q] : make_float2(INFINITY, 0.f);
+                x[i] = q < sh.qn ? a.stats[(long long)(head0 + g) * a.q_tokens + sh.q0 + q] : make_float2(INFINITY, 0.f);
             }
         };
         float2 next[2];
@@ -389,6 +407,32 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     if (warp == 9) {
         __syncwarp();
         tmem_free(tmem, 512);
+    }
+    if (split > 1) {
+        // every CTA of the cluster adds up every split-th row of dV and dK, over the CTAs in order of their rank
+        // (where a wait ran out the sums are as wrong as the status word says)
+        cluster_sync();
+        if (warp < 8) {
+            const int w = warp >> 2;
+            for (int row = (warp & 3) * split + rank; row < sh.rows; row += 4 * split) {
+                constexpr int kLanes = D / 4;  // four elements a lane
+                if (lane < kLanes) {
+                    const uint32_t at = smem_u32(smem) + w * 2 * F::kRowTile + row * D * 4 + ((lane ^ (row & 7)) << 4);
+                    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int r = 0; r < split; ++r) {
+                        const float4 x = load_cluster(at, r);
+                        sum.x += x.x;
+                        sum.y += x.y;
+                        sum.z += x.z;
+                        sum.w += x.w;
+                    }
+                    const float scale = w == 0 ? 1.f : a.scale;
+                    __nv_bfloat16* dst = (w == 0 ? a.dv : a.dk) + ((long long)(sh.k0 + row) * a.kv_heads + kv_head) * D + lane * 4;
+                    *reinterpret_cast<uint2*>(dst) = make_uint2(bf16x2(sum.x * scale, sum.y * scale), bf16x2(sum.z * scale, sum.w * scale));
+                }
+            }
+        }
+        cluster_sync();  // nobody leaves while its rows are read
     }
 }
 
@@ -475,7 +519,9 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const float sl2 = a.scale * kLog2e;
         const float slope2 = BIAS ? a.slopes[head] * kLog2e : 0.f;
         const int q = sh.at.q0[w] + row;
-        const float2 stat = mine ? a.stats[(long long)head * a.q_tokens + q] : make_float2(INFINITY, 0.f);
+        float2* stat_at = a.stats + (long long)head * a.q_tokens + q;
+        const float2 stat = mine ? *stat_at : make_float2(INFINITY, 0.f);
+        float2 excess = make_float2(0.f, 0.f);  // sum of P (dP - D): zero but for the rounding of `out` that D comes from
         bool ok = true;
         int done = 0;
         const int sub_a = sh.at.sub_a[w], sub_b = sh.at.sub_b[w], sub_e = sh.at.sub_e[w];
@@ -508,8 +554,10 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 uint32_t packed[16];
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
-                    d[c] = s[c] * (d[c] - stat.y);
-                    d[c + 1] = s[c + 1] * (d[c + 1] - stat.y);
+                    const float2 ds = mul2(make_float2(s[c], s[c + 1]), add2(make_float2(d[c], d[c + 1]), make_float2(-stat.y, -stat.y)));
+                    excess = add2(excess, ds);
+                    d[c] = ds.x;
+                    d[c + 1] = ds.y;
                     if constexpr (CAP) {
                         d[c] *= f[c];
                         d[c + 1] *= f[c + 1];
@@ -528,6 +576,7 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             ok = wait(smem_u32(&sh.done), 0, abort_flag, a.status, kPromptWaitProduct);
             fence_after();
         }
+        if (ok && mine && w < n_sub) stat_at->y = stat.y + excess.x + excess.y;  // for the keys kernel
         if (ok && w < n_sub) {  // through shared memory: the sub-tile's queries are not needed any more
             const int part = (warp & 3) * 32;
             write_rows<D>(smem + w * F::kRowTile + part * D * 2, tmem + lanes + 256 + w * D, a.scale, done > 0,
@@ -646,16 +695,31 @@ struct Maps {
 template <int D, bool CAP, bool BIAS>
 cudaError_t launch_one(const PromptArgs& a, const Maps& m, cudaStream_t stream)
 {
-    const long long k_tiles = (long long)a.k_tokens / kRows + (a.n_docs < a.k_tokens ? a.n_docs : a.k_tokens);
-    const dim3 stats((a.q_tokens + 31) / 32, (a.q_heads + 7) / 8);
+    const dim3 stats((a.q_tokens + 7) / 8, (a.q_heads + 7) / 8);
     prompt_stats_kernel<D><<<stats, 256, 0, stream>>>(a);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    prompt_keys_kernel<D, CAP, BIAS><<<(unsigned)(k_tiles * a.kv_heads), kThreads, Keys<D>::kSmem, stream>>>(a, m.q, m.k, m.v, m.dout);
+    prompt_rows_kernel<D, CAP, BIAS><<<(unsigned)row_tile_blocks(a), kThreads, RowsK<D>::kSmem, stream>>>(a, m.q, m.k, m.v, m.dout);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    prompt_rows_kernel<D, CAP, BIAS><<<(unsigned)row_tile_blocks(a), kThreads, RowsK<D>::kSmem, stream>>>(a, m.q, m.k, m.v, m.dout);
-    return cudaGetLastError();
+    // Few key tiles: the query heads of a KV head go to several CTAs, as many (a divisor of the group) as leave no more than
+    // four per SM.  A causal document's first key tile is seen by all its queries, so this also evens out the CTAs' work.
+    const long long tiles = ((long long)a.k_tokens / kRows + (a.n_docs < a.k_tokens ? a.n_docs : a.k_tokens)) * a.kv_heads;
+    int split = 1;
+    for (int x = 2; x <= a.group; ++x)
+        if (a.group % x == 0 && tiles * x <= 4 * 148) split = x;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * split));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Keys<D>::kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = split > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, prompt_keys_kernel<D, CAP, BIAS>, a, m.q, m.k, m.v, m.dout, split);
 }
 
 template <int D>

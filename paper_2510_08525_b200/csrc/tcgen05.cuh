@@ -96,6 +96,24 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
         : "memory");
 }
 
+// ---- a cluster's CTAs ---------------------------------------------------------------------------------
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// Four floats at the same place of CTA `rank`'s shared memory.
+__device__ __forceinline__ float4 load_cluster(uint32_t addr, int rank)
+{
+    float4 x;
+    asm volatile(
+        "{\n\t.reg .b32 p;\n\tmapa.shared::cluster.u32 p, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [p];\n\t}"
+        : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w)
+        : "r"(addr), "r"(rank)
+        : "memory");
+    return x;
+}
+
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
 // Registers of a warpgroup's threads from here on (every warp of it executes this).

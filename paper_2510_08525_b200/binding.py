@@ -131,6 +131,10 @@ def _ptr(x) -> int:
 def _stream(s) -> int:
     if s is None:
         import torch
+        # the raw handle: building the Stream object takes several microseconds, as long as a small call
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return raw(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(s, int):
         return s
@@ -436,9 +440,11 @@ def _rows(x):
     wider projection; an address alone stands for contiguous tokens."""
     if x is None or isinstance(x, (int, np.ndarray)):
         return _ptr(x), 0
-    if x.dim() != 3 or x.stride(2) != 1 or x.stride(1) != x.shape[2]:
+    n, _, dim = x.shape  # ValueError where it has other than three dimensions
+    token, head, one = x.stride()
+    if one != 1 or head != dim:
         raise ValueError("tokens must be [tokens][heads][head_dim] with contiguous heads")
-    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else 0
+    return x.data_ptr(), token if n > 1 else 0
 
 
 def rlkv_paged_set_scores(cache, softcap, slopes=None) -> None:

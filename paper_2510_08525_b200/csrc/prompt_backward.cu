@@ -1,16 +1,14 @@
 // The backward pass of prompt attention on the tensor cores, in three launches without atomics:
 //
 //   stats   D_i = sum over head_dim of dout * out, stored with lse (log2 domain) per head and query
-//   rows    one CTA per 256 query rows (two heads, or one): over their keys (64 at a time), S = Q.K^T and dP = dO.V^T,
-//           then dQ += dS.K.  It also corrects D: out was rounded to bf16, and sum_j P (dP - D) is what that changed
+//   rows    one CTA per 256 query rows (two heads, or one): over their keys, S = Q.K^T and dP = dO.V^T, then dQ += dS.K.
+//           It also corrects D: out was rounded to bf16, and sum_j P (dP - D) is what that changed
 //   keys    one CTA (or one per part of the query heads, in a cluster that adds them up) per 128 keys of a KV head: over
-//           the queries that see them (64 at a time), S^T = K.Q^T and dP^T = V.dO^T, then dV += P^T.dO and dK += dS^T.Q
+//           the queries that see them, S^T = K.Q^T and dP^T = V.dO^T, then dV += P^T.dO and dK += dS^T.Q
 //
 // S and dP are computed twice, seven products where five would do, and in return every gradient is summed by one CTA
 // in a fixed order: no atomics on dQ, no fp32 copy of it in memory, the same bits on every run.  P and dS are written
-// to tensor memory as bf16 over S and dP and are the A operand of the second products straight from there.  Two
-// warpgroups alternate -- over query tiles in `keys`, over 128-row sub-tiles in `rows` -- so that one's products run
-// beside the other's arithmetic.
+// to tensor memory as bf16 over S and dP and are the A operand of the second products straight from there.
 #include "rlkv_prompt.cuh"
 #include "tcgen05.cuh"
 
@@ -20,9 +18,8 @@ namespace {
 using namespace tc;
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kRows = 128;  // rows of a product's result: keys (keys kernel) or queries (rows kernel)
-constexpr int kCols = 64;   // its columns: queries or keys
-constexpr int kRowBlock = kRows * 128, kColBlock = kCols * 128;  // bytes of a block of 64 elements of so many rows
+constexpr int kTok = 128;            // tokens of a tile, of queries and of keys
+constexpr int kBlock = kTok * 128;  // bytes of a block of 64 elements of its rows
 constexpr int kThreads = 384;
 
 // ---- D and lse ---------------------------------------------------------------------------------------
@@ -95,26 +92,70 @@ __device__ __forceinline__ void capped(const Cap& cap, float sl2, bool vote, flo
     }
 }
 
-// rows x 64 elements of one head from token `token` on: boxes of 64 tokens, D / 64 of them side by side.
+// A tile of 128 tokens of one head from token `token` on: D / 64 blocks of [128 rows][128 bytes].
 template <int D>
-__device__ __forceinline__ void load_rows(uint32_t dst, int rows, const CUtensorMap* map, int head, int token, uint32_t bar)
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int head, int token, uint32_t bar)
 {
-    for (int b = 0; b < D / 64; ++b)
-        for (int r = 0; r < rows; r += 64) load_box(dst + b * rows * 128 + r * 128, map, b * 64, head, token + r, bar);
+    for (int b = 0; b < D / 64; ++b) load_box(dst + b * kBlock, map, b * 64, head, token, bar);
+}
+
+// Zeros over rows `from` .. 127 of BLOCKS blocks; visible to the products of whoever the caller tells afterwards.
+template <int BLOCKS>
+__device__ __forceinline__ void clear_rows(uint8_t* tile, int from, int lane)
+{
+    for (int i = from * 8 + lane; i < kTok * 8; i += 32)
+        for (int b = 0; b < BLOCKS; ++b) *reinterpret_cast<uint4*>(tile + b * kBlock + i * 16) = make_uint4(0, 0, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+
+__device__ __forceinline__ void signal(uint64_t* bar)
+{
+    if (elect_one()) commit(smem_u32(bar));
+}
+// d (128 x 128) = A.B^T of two tiles, over head_dim; `bar` is told when it is done.
+template <int D>
+__device__ __forceinline__ void scores(uint32_t d, uint32_t a_smem, uint32_t b_smem, uint64_t* bar)
+{
+    const uint64_t x = smem_desc(a_smem), y = smem_desc(b_smem);
+    if (elect_one()) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            const uint32_t off = (i / 4 * kBlock + i % 4 * 32) >> 4;
+            mma_ss(d, x + off, y + off, instr_desc(kTok, kTok, false), i > 0);
+        }
+        commit(smem_u32(bar));
+    }
+}
+// d (128 x D) += A.B, over 128 tokens: A is bf16 in tensor memory, the second 64 tokens' columns at `second`, B a tile.
+template <int D>
+__device__ __forceinline__ void gradient(uint32_t d, uint32_t a_tmem, int second, uint32_t b_smem, bool add)
+{
+    const uint64_t y = smem_desc(b_smem, kBlock);
+    if (elect_one()) {
+#pragma unroll
+        for (int i = 0; i < kTok / 16; ++i)
+            mma_ts(d, a_tmem + (i < 4 ? i * 8 : second + (i - 4) * 8), y + (i * 2048 >> 4), instr_desc(kTok, D, true), add || i > 0);
+    }
 }
 
 // ---- dK and dV ------------------------------------------------------------------------------------------
+//
+// One tile of 128 queries at a time, both warpgroups on it (64 columns each).  The products of a tile are issued as
+//   dV(n) += P.dO | S(n+1) | dK(n) += dS.Q | dP(n+1)
+// so that one of them always runs beside the arithmetic on P and dS: S(n+1) may overwrite P(n) once dV(n) has read it,
+// dP(n+1) overwrites dS(n) after dK(n).  (Tiles of 64 queries, two in flight, left the tensor core waiting for shared
+// memory: with N = 64 a product reads 6 KB of operands per 32 cycles, where 128 bytes per cycle is what there is.)
 
 template <int D>
 struct Keys {
-    static constexpr int kRowTile = kRows * D * 2, kColTile = kCols * D * 2;
-    static constexpr int kStages = 4;  // (even: a stage is always used by the same warpgroup)
-    static constexpr int kStats = 2 * kRowTile + kStages * 2 * kColTile;
-    static constexpr int kSmem = kStats + kStages * kCols * 8 + 1024;
+    static constexpr int kTile = kTok * D * 2;
+    static constexpr int kStages = D == 128 ? 2 : 4;  // Q and dO tiles
+    static constexpr int kStats = (2 + 2 * kStages) * kTile;
+    static constexpr int kSmem = kStats + kStages * kTok * 8 + 1024;
 };
 
 struct KeysShared {
-    uint64_t kv_full, full[4], empty[4], ready[4], sd_full[2], pds_full[2], done, drain;
+    uint64_t kv_full, full[4], empty[4], ready[4], s_full, p_full, dp_full, ds_full, done, drain;
     uint32_t tmem;
     int abort, valid;
     int k0, rows, j0, q0, qn, off, prefix, u0, n_u;  // the CTA's keys; first query tile that sees them, and how many
@@ -128,7 +169,7 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     using F = Keys<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     float2* stats = reinterpret_cast<float2*>(smem + F::kStats);
-    KeysShared& sh = *reinterpret_cast<KeysShared*>(smem + F::kStats + F::kStages * kCols * 8);
+    KeysShared& sh = *reinterpret_cast<KeysShared*>(smem + F::kStats + F::kStages * kTok * 8);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     // `split` CTAs, a cluster, share the query heads of a KV head
     const int rank = blockIdx.x % split, block = blockIdx.x / split, kv_head = block % a.kv_heads;
@@ -142,13 +183,13 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     }
     if (warp == 0) {
         int doc = 0, tile = 0;
-        const bool valid = find_tile(a, true, kRows, block / a.kv_heads, doc, tile);
+        const bool valid = find_tile(a, true, kTok, block / a.kv_heads, doc, tile);
         if (lane == 0) {
             sh.valid = valid;
             if (valid) {
                 const DocRange r = doc_range(a, doc);
-                tile = (r.kn + kRows - 1) / kRows - 1 - tile;  // a document's first keys are seen by the most queries
-                const int j0 = tile * kRows, j1 = min(j0 + kRows, r.kn), off = r.kn - r.qn;
+                tile = (r.kn + kTok - 1) / kTok - 1 - tile;  // a document's first keys are seen by the most queries
+                const int j0 = tile * kTok, j1 = min(j0 + kTok, r.kn), off = r.kn - r.qn;
                 sh.k0 = r.k0 + j0;
                 sh.rows = j1 - j0;
                 sh.j0 = j0;
@@ -159,8 +200,8 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 // queries lower .. upper-1 see some key of the tile
                 const int lower = j0 < r.prefix ? 0 : max(0, j0 - off);
                 const int upper = full_head || j0 < a.sink ? r.qn : min(r.qn, j1 - 1 + a.window - off);
-                sh.u0 = lower / kCols;
-                sh.n_u = upper > lower ? (upper + kCols - 1) / kCols - sh.u0 : 0;
+                sh.u0 = lower / kTok;
+                sh.n_u = upper > lower ? (upper + kTok - 1) / kTok - sh.u0 : 0;
             }
         }
     } else if (warp == 8) {
@@ -176,10 +217,10 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 mbar_init(smem_u32(&sh.empty[i]), 1);
                 mbar_init(smem_u32(&sh.ready[i]), 1);
             }
-            for (int w = 0; w < 2; ++w) {
-                mbar_init(smem_u32(&sh.sd_full[w]), 1);
-                mbar_init(smem_u32(&sh.pds_full[w]), 4);
-            }
+            mbar_init(smem_u32(&sh.s_full), 1);
+            mbar_init(smem_u32(&sh.p_full), 8);
+            mbar_init(smem_u32(&sh.dp_full), 1);
+            mbar_init(smem_u32(&sh.ds_full), 8);
             mbar_init(smem_u32(&sh.done), 1);
             mbar_init(smem_u32(&sh.drain), 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -195,15 +236,14 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         if (warp == 9) tmem_free(tmem, 512);
         return;
     }
-    const uint32_t dV = tmem + 256, dK = tmem + 256 + D;
-    const uint32_t k_smem = smem_u32(smem), v_smem = k_smem + F::kRowTile, ring = v_smem + F::kRowTile;
+    const uint32_t dP = tmem + kTok, dV = tmem + 256, dK = tmem + 256 + D;  // S at column 0
+    const uint32_t k_smem = smem_u32(smem), v_smem = k_smem + F::kTile, ring = v_smem + F::kTile;
     const int n_u = sh.n_u, steps = n_u * heads;  // step n: query tile u0 + n % n_u of query head head0 + n / n_u
 
     if (warp < 8) {
-        // ------------------------------------------------------------------ P and dS, one thread per key
+        // ------------------------------------------------------------------ P and dS, one thread per key and 64 queries
         const int w = warp >> 2, row = (warp & 3) * 32 + lane;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t S = tmem + lanes + w * 128, dP = S + 64;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, mine_s = tmem + lanes + w * 64, mine_dp = dP + lanes + w * 64;
         const int j = sh.j0 + row, j_last = sh.j0 + sh.rows - 1;
         const bool mine = row < sh.rows;
         // the key is seen from positions lo .. hi-1
@@ -211,65 +251,69 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const Cap cap(CAP ? a.softcap : 1.f, a.scale);
         const float sl2 = a.scale * kLog2e;
         bool ok = true;
-        int g = 0, u = w;  // of step n
-        while (n_u > 0 && u >= n_u) { u -= n_u; ++g; }
-        for (int n = w; ok && n < steps; n += 2) {
+        int g = 0, u = 0;  // of step n
+        for (int n = 0; n < steps; ++n) {
             const int st = n % F::kStages;
             ok = wait(smem_u32(&sh.ready[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad) &&
-                 wait(smem_u32(&sh.sd_full[w]), n >> 1 & 1, abort_flag, a.status, kPromptWaitProduct);
+                 wait(smem_u32(&sh.s_full), n & 1, abort_flag, a.status, kPromptWaitProduct);
             if (!ok) break;
             fence_after();
-            const float4* stat = reinterpret_cast<const float4*>(stats + st * kCols);
-            const int p0 = (sh.u0 + u) * kCols + sh.off;  // position of column 0
-            const bool past = p0 >= j_last;               // every query at or behind every key
-            const bool plain = (past || j_last < sh.prefix) && (full_head || j_last < a.sink || p0 + kCols - 1 < sh.j0 + a.window);
+            const float4* stat = reinterpret_cast<const float4*>(stats + st * kTok + w * 64);
+            const int p0 = (sh.u0 + u) * kTok + sh.off + w * 64;  // position of this thread's first query
+            const bool plain = (p0 >= j_last || j_last < sh.prefix) && (full_head || j_last < a.sink || p0 + 63 < sh.j0 + a.window);
             const float slope2 = BIAS ? a.slopes[head0 + g] * kLog2e : 0.f;
+            float s[2][32], f[2][CAP ? 32 : 1];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                float s[32], f[CAP ? 32 : 1];
-                tmem_read32(S + half * 32, s);
-                capped<CAP>(cap, sl2, mine, s, f);
-                const int d0 = p0 + half * 32 - j;  // distance of column 0
+                tmem_read32(mine_s + half * 32, s[half]);
+                capped<CAP>(cap, sl2, mine, s[half], f[half]);
+                const int d0 = p0 + half * 32 - j;  // distance of the first
                 if (BIAS) {
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) s[c] = fmaf(-slope2, fabsf((float)(d0 + c)), s[c]);
+                    for (int c = 0; c < 32; ++c) s[half][c] = fmaf(-slope2, fabsf((float)(d0 + c)), s[half][c]);
                 }
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
                     const float4 x = stat[half * 16 + c / 2];  // (lse, D) of two queries
-                    s[c] = ex2(s[c] - x.x);
-                    s[c + 1] = ex2(s[c + 1] - x.z);
+                    s[half][c] = ex2(s[half][c] - x.x);
+                    s[half][c + 1] = ex2(s[half][c + 1] - x.z);
                 }
                 if (!plain) {
                     const uint32_t see = range_bits(lo - j - d0, hi - j - d0);
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) s[c] = see >> c & 1 ? s[c] : 0.f;
+                    for (int c = 0; c < 32; ++c) s[half][c] = see >> c & 1 ? s[half][c] : 0.f;
                 }
                 uint32_t packed[16];
 #pragma unroll
-                for (int c = 0; c < 16; ++c) packed[c] = bf16x2(s[2 * c], s[2 * c + 1]);
-                tmem_st16(S + half * 16, packed);
-                float d[32];
-                tmem_read32(dP + half * 32, d);
-#pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    const float4 x = stat[half * 16 + c / 2];
-                    d[c] = s[c] * (d[c] - x.y);
-                    d[c + 1] = s[c + 1] * (d[c + 1] - x.w);
-                    if constexpr (CAP) {
-                        d[c] *= f[c];
-                        d[c + 1] *= f[c + 1];
-                    }
-                    packed[c / 2] = bf16x2(d[c], d[c + 1]);
-                }
-                tmem_st16(dP + half * 16, packed);
+                for (int c = 0; c < 16; ++c) packed[c] = bf16x2(s[half][2 * c], s[half][2 * c + 1]);
+                tmem_st16(mine_s + half * 16, packed);  // (over this warpgroup's own columns of S)
             }
             wait_st();
             fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh.pds_full[w]));
-            u += 2;
-            while (u >= n_u) { u -= n_u; ++g; }
+            if (lane == 0) mbar_arrive(smem_u32(&sh.p_full));
+            ok = wait(smem_u32(&sh.dp_full), n & 1, abort_flag, a.status, kPromptWaitProduct);
+            if (!ok) break;
+            fence_after();
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                float d[32];
+                tmem_read32(mine_dp + half * 32, d);
+                uint32_t packed[16];
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) {
+                    const float4 x = stat[half * 16 + c / 2];
+                    float2 ds = mul2(make_float2(s[half][c], s[half][c + 1]), add2(make_float2(d[c], d[c + 1]), make_float2(-x.y, -x.w)));
+                    if constexpr (CAP) ds = mul2(ds, make_float2(f[half][c], f[half][c + 1]));
+                    packed[c / 2] = bf16x2(ds.x, ds.y);
+                }
+                tmem_st16(mine_dp + half * 16, packed);
+            }
+            wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.ds_full));
+            if (++u == n_u) { u = 0; ++g; }
         }
         if (ok && steps > 0) {
             ok = wait(smem_u32(&sh.done), 0, abort_flag, a.status, kPromptWaitProduct);
@@ -279,11 +323,11 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         if (ok && split == 1) {
             // through shared memory: the keys' tile for dV, the values' for dK (neither is needed any more)
             const long long at = ((long long)(sh.k0 + part) * a.kv_heads + kv_head) * D;
-            write_rows<D>(smem + w * F::kRowTile + part * D * 2, (w == 0 ? dV : dK) + lanes, w == 0 ? 1.f : a.scale, steps > 0,
+            write_rows<D>(smem + w * F::kTile + part * D * 2, (w == 0 ? dV : dK) + lanes, w == 0 ? 1.f : a.scale, steps > 0,
                           (w == 0 ? a.dv : a.dk) + at, (long long)a.kv_heads * D, sh.rows - part, lane);
         } else if (ok) {
             // this CTA's share of the sums in fp32, for the cluster to add up: dV over the K and V tiles, dK over the ring
-            uint8_t* mine_rows = smem + w * 2 * F::kRowTile + row * D * 4;
+            uint8_t* mine_rows = smem + w * 2 * F::kTile + row * D * 4;
 #pragma unroll
             for (int c = 0; c < D; c += 32) {
                 float o[32];
@@ -299,20 +343,20 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     } else if (warp == 8) {
         // ------------------------------------------------------------------ tile loads
         if (lane == 0 && steps > 0) {
-            mbar_expect_tx(smem_u32(&sh.kv_full), 2 * F::kRowTile);
-            load_rows<D>(k_smem, kRows, &map_k, kv_head, sh.k0, smem_u32(&sh.kv_full));
-            load_rows<D>(v_smem, kRows, &map_v, kv_head, sh.k0, smem_u32(&sh.kv_full));
+            mbar_expect_tx(smem_u32(&sh.kv_full), 2 * F::kTile);
+            load_tile<D>(k_smem, &map_k, kv_head, sh.k0, smem_u32(&sh.kv_full));
+            load_tile<D>(v_smem, &map_v, kv_head, sh.k0, smem_u32(&sh.kv_full));
             int n = 0, g = 0, u = 0;
             bool ok = true;
             for (; n < steps; ++n) {
                 const int st = n % F::kStages;
                 ok = wait(smem_u32(&sh.empty[st]), (n / F::kStages & 1) ^ 1, abort_flag, a.status, kPromptWaitStage);
                 if (!ok) break;
-                const uint32_t bar = smem_u32(&sh.full[st]), dst = ring + st * 2 * F::kColTile;
-                mbar_expect_tx(bar, 2 * F::kColTile);
-                const int token = sh.q0 + (sh.u0 + u) * kCols;
-                load_rows<D>(dst, kCols, &map_q, head0 + g, token, bar);
-                load_rows<D>(dst + F::kColTile, kCols, &map_do, head0 + g, token, bar);
+                const uint32_t bar = smem_u32(&sh.full[st]), dst = ring + st * 2 * F::kTile;
+                mbar_expect_tx(bar, 2 * F::kTile);
+                const int token = sh.q0 + (sh.u0 + u) * kTok;
+                load_tile<D>(dst, &map_q, head0 + g, token, bar);
+                load_tile<D>(dst + F::kTile, &map_do, head0 + g, token, bar);
                 if (++u == n_u) { u = 0; ++g; }
             }
             if (!ok || *abort_flag) {  // nothing of this CTA's copies may be in flight when it ends
@@ -324,46 +368,34 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     } else if (warp == 9) {
         // ------------------------------------------------------------------ matrix products
         if (steps > 0) {
-            constexpr uint32_t kScores = instr_desc(kRows, kCols, false), kGrads = instr_desc(kRows, D, true);
-            const uint64_t k_desc = smem_desc(k_smem), v_desc = smem_desc(v_smem);
-            auto signal = [&](uint64_t* bar) {
-                if (elect_one()) commit(smem_u32(bar));
-            };
-            auto first_products = [&](int n) {
+            auto loaded = [&](int n) {
                 const int st = n % F::kStages;
-                if (!wait_warp(smem_u32(&sh.full[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad) ||
-                    !wait_warp(smem_u32(&sh.ready[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad))
-                    return false;
-                const uint64_t q = smem_desc(ring + st * 2 * F::kColTile), o = smem_desc(ring + st * 2 * F::kColTile + F::kColTile);
-                const uint32_t d = tmem + (n & 1) * 128;
-                if (elect_one()) {
-#pragma unroll
-                    for (int x = 0; x < D / 16; ++x)
-                        mma_ss(d, k_desc + ((x / 4 * kRowBlock + x % 4 * 32) >> 4), q + ((x / 4 * kColBlock + x % 4 * 32) >> 4), kScores, x > 0);
-#pragma unroll
-                    for (int x = 0; x < D / 16; ++x)
-                        mma_ss(d + 64, v_desc + ((x / 4 * kRowBlock + x % 4 * 32) >> 4), o + ((x / 4 * kColBlock + x % 4 * 32) >> 4), kScores, x > 0);
-                    commit(smem_u32(&sh.sd_full[n & 1]));
-                }
-                return true;
+                return wait_warp(smem_u32(&sh.full[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad) &&
+                       wait_warp(smem_u32(&sh.ready[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad);
             };
-            bool ok = wait_warp(smem_u32(&sh.kv_full), 0, abort_flag, a.status, kPromptWaitLoad) && first_products(0);
-            if (ok && steps > 1) ok = first_products(1);
+            auto q_at = [&](int n) { return ring + n % F::kStages * 2 * F::kTile; };
+            bool ok = wait_warp(smem_u32(&sh.kv_full), 0, abort_flag, a.status, kPromptWaitLoad) && loaded(0);
+            if (ok) {
+                scores<D>(tmem, k_smem, q_at(0), &sh.s_full);
+                scores<D>(dP, v_smem, q_at(0) + F::kTile, &sh.dp_full);
+            }
             for (int n = 0; ok && n < steps; ++n) {
-                const int st = n % F::kStages, w = n & 1;
-                ok = wait_warp(smem_u32(&sh.pds_full[w]), n >> 1 & 1, abort_flag, a.status, kPromptWaitSoftmax);
+                ok = wait_warp(smem_u32(&sh.p_full), n & 1, abort_flag, a.status, kPromptWaitSoftmax);
                 if (!ok) break;
                 fence_after();
-                const uint64_t q = smem_desc(ring + st * 2 * F::kColTile, kColBlock), o = smem_desc(ring + st * 2 * F::kColTile + F::kColTile, kColBlock);
-                const uint32_t d = tmem + w * 128;
-                if (elect_one()) {
-#pragma unroll
-                    for (int x = 0; x < kCols / 16; ++x) mma_ts(dV, d + x * 8, o + (x * 2048 >> 4), kGrads, n > 0 || x > 0);
-#pragma unroll
-                    for (int x = 0; x < kCols / 16; ++x) mma_ts(dK, d + 64 + x * 8, q + (x * 2048 >> 4), kGrads, n > 0 || x > 0);
-                    commit(smem_u32(&sh.empty[st]));
+                gradient<D>(dV, tmem, 64, q_at(n) + F::kTile, n > 0);
+                const bool more = n + 1 < steps;
+                if (more) {
+                    ok = loaded(n + 1);
+                    if (!ok) break;
+                    scores<D>(tmem, k_smem, q_at(n + 1), &sh.s_full);
                 }
-                if (n + 2 < steps) ok = first_products(n + 2);
+                ok = wait_warp(smem_u32(&sh.ds_full), n & 1, abort_flag, a.status, kPromptWaitSoftmax);
+                if (!ok) break;
+                fence_after();
+                gradient<D>(dK, dP, 64, q_at(n), n > 0);
+                signal(&sh.empty[n % F::kStages]);
+                if (more) scores<D>(dP, v_smem, q_at(n + 1) + F::kTile, &sh.dp_full);
             }
             signal(&sh.done);
             signal(&sh.drain);
@@ -373,30 +405,27 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         // ------------------------------------------------------------------ lse and D of the query tiles; rows behind the
         // last query: lse +infinity (P = 0), and zeros for what another document or nobody holds there (0 * NaN)
         int g = 0, u = 0;
-        auto fetch = [&](float2 (&x)[2]) {
+        auto fetch = [&](float2 (&x)[4]) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int q = (sh.u0 + u) * kCols + lane + 32 * i;
+            for (int i = 0; i < 4; ++i) {
+                const int q = (sh.u0 + u) * kTok + lane + 32 * i;
                 x[i] = q < sh.qn ? a.stats[(long long)(head0 + g) * a.q_tokens + sh.q0 + q] : make_float2(INFINITY, 0.f);
             }
         };
-        float2 next[2];
+        float2 next[4];
         if (steps > 0) fetch(next);
         for (int n = 0; n < steps; ++n) {
-            const int st = n % F::kStages, valid = sh.qn - (sh.u0 + u) * kCols;
-            const float2 now[2] = {next[0], next[1]};
+            const int st = n % F::kStages, valid = sh.qn - (sh.u0 + u) * kTok;
+            float2 now[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) now[i] = next[i];
             if (++u == n_u) { u = 0; ++g; }
             if (n + 1 < steps) fetch(next);
             if (!wait(smem_u32(&sh.empty[st]), (n / F::kStages & 1) ^ 1, abort_flag, a.status, kPromptWaitStage)) break;
-            stats[st * kCols + lane] = now[0];
-            stats[st * kCols + lane + 32] = now[1];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) stats[st * kTok + lane + 32 * i] = now[i];
             if (!wait(smem_u32(&sh.full[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad)) break;
-            if (valid < kCols) {
-                uint8_t* x = smem + 2 * F::kRowTile + st * 2 * F::kColTile;
-                for (int i = valid * 8 + lane; i < kCols * 8; i += 32)
-                    for (int b = 0; b < 2 * D / 64; ++b) *reinterpret_cast<uint4*>(x + b * kColBlock + i * 16) = make_uint4(0, 0, 0, 0);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            }
+            if (valid < kTok) clear_rows<2 * D / 64>(smem + (2 + 2 * st) * F::kTile, valid, lane);
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.ready[st]));
         }
@@ -417,7 +446,7 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             for (int row = (warp & 3) * split + rank; row < sh.rows; row += 4 * split) {
                 constexpr int kLanes = D / 4;  // four elements a lane
                 if (lane < kLanes) {
-                    const uint32_t at = smem_u32(smem) + w * 2 * F::kRowTile + row * D * 4 + ((lane ^ (row & 7)) << 4);
+                    const uint32_t at = smem_u32(smem) + w * 2 * F::kTile + row * D * 4 + ((lane ^ (row & 7)) << 4);
                     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
                     for (int r = 0; r < split; ++r) {
                         const float4 x = load_cluster(at, r);
@@ -437,19 +466,24 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
 }
 
 // ---- dQ ----------------------------------------------------------------------------------------------------
+//
+// Tiles of 128 keys; each of the two sub-tiles has ONE block of 128 columns in tensor memory, which holds S, then dP (once
+// the threads have taken S into registers), then dS.  The products of a tile are issued as
+//   dQ0(j) | S0(j+1) | dQ1(j) | S1(j+1) | dP0(j+1) | dP1(j+1)
+// and each sub-tile's arithmetic runs beside the other's products.
 
 template <int D>
 struct RowsK {
-    static constexpr int kRowTile = kRows * D * 2, kColTile = kCols * D * 2;
-    static constexpr int kStages = D == 128 ? 3 : 6;
-    static constexpr int kSmem = 4 * kRowTile + kStages * 2 * kColTile + 1024;
+    static constexpr int kTile = kTok * D * 2;
+    static constexpr int kValues = D == 128 ? 1 : 2;  // V tiles in flight (two K tiles: K is needed again for dQ)
+    static constexpr int kSmem = (4 + 2 + kValues) * kTile + 1024;
 };
 
 struct RowsShared {
-    uint64_t q_full, full[6], empty[6], sd_full[2], ds_full[2], done, clean, drain;
+    uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], s_read[2], dp_full[2], ds_full[2], done, clean[2], drain;
     uint32_t tmem;
     int abort;
-    RowTile at;  // as in the forward pass, key tiles of 64
+    RowTile at;
 };
 
 template <int D, bool CAP, bool BIAS>
@@ -459,7 +493,7 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
 {
     using F = RowsK<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
-    RowsShared& sh = *reinterpret_cast<RowsShared*>(smem + 4 * F::kRowTile + F::kStages * 2 * F::kColTile);
+    RowsShared& sh = *reinterpret_cast<RowsShared*>(smem + (6 + F::kValues) * F::kTile);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     volatile int* abort_flag = &sh.abort;
 
@@ -468,7 +502,7 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         return;
     }
     if (warp == 0) {
-        find_row_tile(a, kCols, sh.at);
+        find_row_tile(a, kTok, sh.at);
     } else if (warp == 8) {
         if (lane == 0) {
             prefetch_map(&map_q);
@@ -477,16 +511,18 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             prefetch_map(&map_do);
             sh.abort = 0;
             mbar_init(smem_u32(&sh.q_full), 1);
-            for (int i = 0; i < F::kStages; ++i) {
-                mbar_init(smem_u32(&sh.full[i]), 1);
-                mbar_init(smem_u32(&sh.empty[i]), 1);
-            }
-            for (int w = 0; w < 2; ++w) {
-                mbar_init(smem_u32(&sh.sd_full[w]), 1);
-                mbar_init(smem_u32(&sh.ds_full[w]), 4);
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(smem_u32(&sh.k_full[i]), 1);
+                mbar_init(smem_u32(&sh.k_empty[i]), 1);
+                mbar_init(smem_u32(&sh.v_full[i]), 1);
+                mbar_init(smem_u32(&sh.v_empty[i]), 1);
+                mbar_init(smem_u32(&sh.s_full[i]), 1);
+                mbar_init(smem_u32(&sh.s_read[i]), 4);
+                mbar_init(smem_u32(&sh.dp_full[i]), 1);
+                mbar_init(smem_u32(&sh.ds_full[i]), 4);
+                mbar_init(smem_u32(&sh.clean[i]), 1);
             }
             mbar_init(smem_u32(&sh.done), 1);
-            mbar_init(smem_u32(&sh.clean), 1);
             mbar_init(smem_u32(&sh.drain), 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
@@ -504,67 +540,81 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     const int n_tiles = sh.at.n_tiles, a_end = sh.at.a_end, b0 = sh.at.b0, kn = sh.at.kn, prefix = sh.at.prefix;
     const int n_sub = sh.at.n_sub, kv_head = sh.at.kv_head;
     const bool full_head = a.full[kv_head] != 0;
-    const uint32_t q_smem = smem_u32(smem), o_smem = q_smem + 2 * F::kRowTile, ring = q_smem + 4 * F::kRowTile;
+    const uint32_t q_smem = smem_u32(smem), o_smem = q_smem + 2 * F::kTile, k_smem = q_smem + 4 * F::kTile, v_smem = q_smem + 6 * F::kTile;
     auto tile_at = [&](int j) { return j < a_end ? j : b0 + j - a_end; };
-
+    // (launched with 384 x 168 = 64512 registers: 256 x 232 + 128 x 40)
+    if (warp < 8) more_registers<232>();
+    else fewer_registers<40>();
     if (warp < 8) {
         // ------------------------------------------------------------------ P and dS, one thread per query
         const int w = warp >> 2, row = (warp & 3) * 32 + lane;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t S = tmem + lanes + w * 128, dP = S + 64;
-        const int first = sh.at.pos0[w], pos = first + row, last = first + kRows - 1, head = sh.at.head[w];
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, S = tmem + lanes + w * kTok;
+        const int first = sh.at.pos0[w], pos = first + row, last = first + kTok - 1, head = sh.at.head[w];
         const bool mine = row < sh.at.rows[w];
         const int hi = min(kn, max(pos + 1, prefix)), lo = full_head ? 0 : pos - a.window + 1, sink = full_head ? 0 : min(a.sink, hi);
         const Cap cap(CAP ? a.softcap : 1.f, a.scale);
         const float sl2 = a.scale * kLog2e;
         const float slope2 = BIAS ? a.slopes[head] * kLog2e : 0.f;
-        const int q = sh.at.q0[w] + row;
-        float2* stat_at = a.stats + (long long)head * a.q_tokens + q;
+        float2* stat_at = a.stats + (long long)head * a.q_tokens + sh.at.q0[w] + row;
         const float2 stat = mine ? *stat_at : make_float2(INFINITY, 0.f);
         float2 excess = make_float2(0.f, 0.f);  // sum of P (dP - D): zero but for the rounding of `out` that D comes from
         bool ok = true;
         int done = 0;
         const int sub_a = sh.at.sub_a[w], sub_b = sh.at.sub_b[w], sub_e = sh.at.sub_e[w];
         for (int t = sub_a > 0 ? 0 : sub_b; t < sub_e; t = t + 1 == sub_a ? sub_b : t + 1) {
-            const int start = t * kCols;
-            ok = wait(smem_u32(&sh.sd_full[w]), done & 1, abort_flag, a.status, kPromptWaitProduct);
+            const int start = t * kTok;
+            ok = wait(smem_u32(&sh.s_full[w]), done & 1, abort_flag, a.status, kPromptWaitProduct);
             if (!ok) break;
             fence_after();
-            const bool plain = start + kCols <= kn && (start + kCols <= first + 1 || start + kCols <= prefix) &&
-                               (full_head || start + kCols <= a.sink || start > last - a.window);
+            float s[kTok];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                float s[32], f[CAP ? 32 : 1];
-                tmem_read32(S + half * 32, s);
-                capped<CAP>(cap, sl2, mine, s, f);
-                const int c0 = start + half * 32;
+            for (int c = 0; c < 4; ++c) tmem_ld32(S + c * 32, s + c * 32);
+            wait_ld();
+#pragma unroll
+            for (int c = 0; c < kTok; ++c) asm volatile("" : "+f"(s[c]));  // nothing of the above is used before the wait
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.s_read[w]));
+            const bool plain = start + kTok <= kn && (start + kTok <= first + 1 || start + kTok <= prefix) &&
+                               (full_head || start + kTok <= a.sink || start > last - a.window);
+            // 32 scores -> P (with CAP after dP is there: its slopes would not fit in registers beside P)
+            auto probabilities = [&](float (&x)[32], float (&f)[CAP ? 32 : 1], int c0) {
+                capped<CAP>(cap, sl2, mine, x, f);
                 if (BIAS) {
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) s[c] = fmaf(-slope2, fabsf((float)(pos - c0 - c)), s[c]);
+                    for (int c = 0; c < 32; ++c) x[c] = fmaf(-slope2, fabsf((float)(pos - c0 - c)), x[c]);
                 }
 #pragma unroll
-                for (int c = 0; c < 32; ++c) s[c] = ex2(s[c] - stat.x);
+                for (int c = 0; c < 32; ++c) x[c] = ex2(x[c] - stat.x);
                 if (!plain) {
                     const uint32_t see = range_bits(lo - c0, hi - c0) | range_bits(0, sink - c0);
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) s[c] = see >> c & 1 ? s[c] : 0.f;
+                    for (int c = 0; c < 32; ++c) x[c] = see >> c & 1 ? x[c] : 0.f;
                 }
-                float d[32];
-                tmem_read32(dP + half * 32, d);
+            };
+            if constexpr (!CAP) {
+                float none[1];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) probabilities(reinterpret_cast<float(&)[32]>(s[c * 32]), none, start + c * 32);
+            }
+            ok = wait(smem_u32(&sh.dp_full[w]), done & 1, abort_flag, a.status, kPromptWaitProduct);
+            if (!ok) break;
+            fence_after();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float(&p)[32] = reinterpret_cast<float(&)[32]>(s[q * 32]);
+                float f[CAP ? 32 : 1], d[32];
+                if constexpr (CAP) probabilities(p, f, start + q * 32);
+                tmem_read32(S + q * 32, d);
                 uint32_t packed[16];
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
-                    const float2 ds = mul2(make_float2(s[c], s[c + 1]), add2(make_float2(d[c], d[c + 1]), make_float2(-stat.y, -stat.y)));
+                    float2 ds = mul2(make_float2(p[c], p[c + 1]), add2(make_float2(d[c], d[c + 1]), make_float2(-stat.y, -stat.y)));
                     excess = add2(excess, ds);
-                    d[c] = ds.x;
-                    d[c + 1] = ds.y;
-                    if constexpr (CAP) {
-                        d[c] *= f[c];
-                        d[c + 1] *= f[c + 1];
-                    }
-                    packed[c / 2] = bf16x2(d[c], d[c + 1]);
+                    if constexpr (CAP) ds = mul2(ds, make_float2(f[c], f[c + 1]));
+                    packed[c / 2] = bf16x2(ds.x, ds.y);
                 }
-                tmem_st16(dP + half * 16, packed);
+                tmem_st16(S + q * 16, packed);
             }
             wait_st();
             fence_before();
@@ -579,82 +629,93 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         if (ok && mine && w < n_sub) stat_at->y = stat.y + excess.x + excess.y;  // for the keys kernel
         if (ok && w < n_sub) {  // through shared memory: the sub-tile's queries are not needed any more
             const int part = (warp & 3) * 32;
-            write_rows<D>(smem + w * F::kRowTile + part * D * 2, tmem + lanes + 256 + w * D, a.scale, done > 0,
+            write_rows<D>(smem + w * F::kTile + part * D * 2, tmem + lanes + 256 + w * D, a.scale, done > 0,
                           a.dq + ((long long)(sh.at.q0[w] + part) * a.q_heads + head) * D, (long long)a.q_heads * D, sh.at.rows[w] - part, lane);
         }
     } else if (warp == 8) {
         // ------------------------------------------------------------------ tile loads
         if (lane == 0 && n_tiles > 0) {
-            mbar_expect_tx(smem_u32(&sh.q_full), 2 * n_sub * F::kRowTile);
+            mbar_expect_tx(smem_u32(&sh.q_full), 2 * n_sub * F::kTile);
             for (int w = 0; w < n_sub; ++w) {
-                load_rows<D>(q_smem + w * F::kRowTile, kRows, &map_q, sh.at.head[w], sh.at.q0[w], smem_u32(&sh.q_full));
-                load_rows<D>(o_smem + w * F::kRowTile, kRows, &map_do, sh.at.head[w], sh.at.q0[w], smem_u32(&sh.q_full));
+                load_tile<D>(q_smem + w * F::kTile, &map_q, sh.at.head[w], sh.at.q0[w], smem_u32(&sh.q_full));
+                load_tile<D>(o_smem + w * F::kTile, &map_do, sh.at.head[w], sh.at.q0[w], smem_u32(&sh.q_full));
             }
-            int j = 0;
+            int n_k = 0, n_v = 0;
             bool ok = true;
-            for (; j < n_tiles; ++j) {
-                const int st = j % F::kStages;
-                ok = wait(smem_u32(&sh.empty[st]), (j / F::kStages & 1) ^ 1, abort_flag, a.status, kPromptWaitStage);
+            for (int j = 0; ok && j < n_tiles; ++j) {
+                const int token = sh.at.k0 + tile_at(j) * kTok;
+                ok = wait(smem_u32(&sh.k_empty[j % 2]), (j / 2 & 1) ^ 1, abort_flag, a.status, kPromptWaitStage);
                 if (!ok) break;
-                const uint32_t bar = smem_u32(&sh.full[st]), dst = ring + st * 2 * F::kColTile;
-                mbar_expect_tx(bar, 2 * F::kColTile);
-                const int token = sh.at.k0 + tile_at(j) * kCols;
-                load_rows<D>(dst, kCols, &map_k, kv_head, token, bar);
-                load_rows<D>(dst + F::kColTile, kCols, &map_v, kv_head, token, bar);
+                mbar_expect_tx(smem_u32(&sh.k_full[j % 2]), F::kTile);
+                load_tile<D>(k_smem + j % 2 * F::kTile, &map_k, kv_head, token, smem_u32(&sh.k_full[j % 2]));
+                ++n_k;
+                const int v = j % F::kValues;
+                ok = wait(smem_u32(&sh.v_empty[v]), (j / F::kValues & 1) ^ 1, abort_flag, a.status, kPromptWaitStage);
+                if (!ok) break;
+                mbar_expect_tx(smem_u32(&sh.v_full[v]), F::kTile);
+                load_tile<D>(v_smem + v * F::kTile, &map_v, kv_head, token, smem_u32(&sh.v_full[v]));
+                ++n_v;
             }
             if (!ok || *abort_flag) {  // nothing of this CTA's copies may be in flight when it ends
                 wait(smem_u32(&sh.q_full), 0, nullptr, a.status, kPromptWaitDrain);
-                for (int i = max(0, j - F::kStages); i < j; ++i)
-                    wait(smem_u32(&sh.full[i % F::kStages]), i / F::kStages & 1, nullptr, a.status, kPromptWaitDrain);
+                for (int i = max(0, n_k - 2); i < n_k; ++i) wait(smem_u32(&sh.k_full[i % 2]), i / 2 & 1, nullptr, a.status, kPromptWaitDrain);
+                for (int i = max(0, n_v - F::kValues); i < n_v; ++i)
+                    wait(smem_u32(&sh.v_full[i % F::kValues]), i / F::kValues & 1, nullptr, a.status, kPromptWaitDrain);
             }
         }
         __syncwarp();
-        // rows behind the last key: only the last tile can hold any
-        const int end = n_tiles - 1, rows = n_tiles > 0 ? kn - tile_at(end) * kCols : kCols;
-        if (rows < kCols && !*abort_flag &&
-            wait(smem_u32(&sh.full[end % F::kStages]), end / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad)) {
-            uint8_t* x = smem + 4 * F::kRowTile + end % F::kStages * 2 * F::kColTile;
-            for (int i = rows * 8 + lane; i < kCols * 8; i += 32)
-                for (int b = 0; b < 2 * D / 64; ++b) *reinterpret_cast<uint4*>(x + b * kColBlock + i * 16) = make_uint4(0, 0, 0, 0);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        // rows behind the last key: only the last tiles can hold any.  (This warp may wait for them: it has seen their
+        // slots' earlier copies consumed)
+        const int end = n_tiles - 1, rows = n_tiles > 0 ? kn - tile_at(end) * kTok : kTok;
+        if (rows < kTok) {
+            if (!*abort_flag && wait(smem_u32(&sh.k_full[end % 2]), end / 2 & 1, abort_flag, a.status, kPromptWaitLoad)) {
+                clear_rows<D / 64>(smem + (4 + end % 2) * F::kTile, rows, lane);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.clean[0]));
+            }
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh.clean));
+            const int v = end % F::kValues;
+            if (!*abort_flag && wait(smem_u32(&sh.v_full[v]), end / F::kValues & 1, abort_flag, a.status, kPromptWaitLoad)) {
+                clear_rows<D / 64>(smem + (6 + v) * F::kTile, rows, lane);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.clean[1]));
+            }
         }
     } else if (warp == 9) {
         // ------------------------------------------------------------------ matrix products
         if (n_tiles > 0) {
-            constexpr uint32_t kScores = instr_desc(kRows, kCols, false), kGrads = instr_desc(kRows, D, true);
-            int used[2] = {0, 0};
+            int used[2] = {0, 0}, read[2] = {0, 0};  // tiles of a sub-tile whose dS was multiplied, whose S was taken
             const int sub_a[2] = {sh.at.sub_a[0], sh.at.sub_a[1]}, sub_b[2] = {sh.at.sub_b[0], sh.at.sub_b[1]}, sub_e[2] = {sh.at.sub_e[0], sh.at.sub_e[1]};
             auto needed = [&](int w, int t) { return t < sub_a[w] || (t >= sub_b[w] && t < sub_e[w]); };
-            auto signal = [&](uint64_t* bar) {
-                if (elect_one()) commit(smem_u32(bar));
+            auto cleaned = [&](int j, int which) {
+                return (tile_at(j) + 1) * kTok <= kn || wait_warp(smem_u32(&sh.clean[which]), 0, abort_flag, a.status, kPromptWaitLoad);
             };
-            auto loaded = [&](int j) {
-                return wait_warp(smem_u32(&sh.full[j % F::kStages]), j / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad) &&
-                       ((tile_at(j) + 1) * kCols <= kn || wait_warp(smem_u32(&sh.clean), 0, abort_flag, a.status, kPromptWaitLoad));
-            };
-            auto first_products = [&](int w, int j) {
-                const uint64_t k = smem_desc(ring + j % F::kStages * 2 * F::kColTile), v = smem_desc(ring + j % F::kStages * 2 * F::kColTile + F::kColTile);
-                const uint64_t q = smem_desc(q_smem + w * F::kRowTile), o = smem_desc(o_smem + w * F::kRowTile);
-                const uint32_t d = tmem + w * 128;
-                if (elect_one()) {
+            auto k_loaded = [&](int j) { return wait_warp(smem_u32(&sh.k_full[j % 2]), j / 2 & 1, abort_flag, a.status, kPromptWaitLoad) && cleaned(j, 0); };
+            // dP of both sub-tiles, each once its threads hold S
+            auto value_products = [&](int j) {
+                const int v = j % F::kValues;
+                if (!wait_warp(smem_u32(&sh.v_full[v]), j / F::kValues & 1, abort_flag, a.status, kPromptWaitLoad) || !cleaned(j, 1)) return false;
 #pragma unroll
-                    for (int x = 0; x < D / 16; ++x)
-                        mma_ss(d, q + ((x / 4 * kRowBlock + x % 4 * 32) >> 4), k + ((x / 4 * kColBlock + x % 4 * 32) >> 4), kScores, x > 0);
-#pragma unroll
-                    for (int x = 0; x < D / 16; ++x)
-                        mma_ss(d + 64, o + ((x / 4 * kRowBlock + x % 4 * 32) >> 4), v + ((x / 4 * kColBlock + x % 4 * 32) >> 4), kScores, x > 0);
-                    commit(smem_u32(&sh.sd_full[w]));
-                }
-            };
-            bool ok = wait_warp(smem_u32(&sh.q_full), 0, abort_flag, a.status, kPromptWaitLoad) && loaded(0);
-            if (ok)
                 for (int w = 0; w < 2; ++w)
-                    if (needed(w, tile_at(0))) first_products(w, 0);
+                    if (needed(w, tile_at(j))) {
+                        if (!wait_warp(smem_u32(&sh.s_read[w]), read[w] & 1, abort_flag, a.status, kPromptWaitSoftmax)) return false;
+                        fence_after();
+                        ++read[w];
+                        scores<D>(tmem + w * kTok, o_smem + w * F::kTile, v_smem + v * F::kTile, &sh.dp_full[w]);
+                    }
+                signal(&sh.v_empty[v]);
+                return true;
+            };
+            bool ok = wait_warp(smem_u32(&sh.q_full), 0, abort_flag, a.status, kPromptWaitLoad) && k_loaded(0);
+            if (ok) {
+#pragma unroll
+                for (int w = 0; w < 2; ++w)
+                    if (needed(w, tile_at(0))) scores<D>(tmem + w * kTok, q_smem + w * F::kTile, k_smem, &sh.s_full[w]);
+                ok = value_products(0);
+            }
             for (int j = 0; ok && j < n_tiles; ++j) {
-                const int st = j % F::kStages;
-                if (j + 1 < n_tiles) ok = loaded(j + 1);
+                const bool more = j + 1 < n_tiles;
+                if (more) ok = k_loaded(j + 1);
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
                     if (!ok) break;
@@ -662,17 +723,13 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                         ok = wait_warp(smem_u32(&sh.ds_full[w]), used[w] & 1, abort_flag, a.status, kPromptWaitSoftmax);
                         if (!ok) break;
                         fence_after();
-                        const uint64_t k = smem_desc(ring + st * 2 * F::kColTile, kColBlock);
-                        if (elect_one()) {
-#pragma unroll
-                            for (int x = 0; x < kCols / 16; ++x)
-                                mma_ts(tmem + 256 + w * D, tmem + w * 128 + 64 + x * 8, k + (x * 2048 >> 4), kGrads, used[w] > 0 || x > 0);
-                        }
+                        gradient<D>(tmem + 256 + w * D, tmem + w * kTok, 32, k_smem + j % 2 * F::kTile, used[w] > 0);
                         ++used[w];
                     }
-                    if (w == 1) signal(&sh.empty[st]);
-                    if (j + 1 < n_tiles && needed(w, tile_at(j + 1))) first_products(w, j + 1);
+                    if (w == 1) signal(&sh.k_empty[j % 2]);
+                    if (more && needed(w, tile_at(j + 1))) scores<D>(tmem + w * kTok, q_smem + w * F::kTile, k_smem + (j + 1) % 2 * F::kTile, &sh.s_full[w]);
                 }
+                if (ok && more) ok = value_products(j + 1);
             }
             signal(&sh.done);
             signal(&sh.drain);
@@ -704,7 +761,7 @@ cudaError_t launch_one(const PromptArgs& a, const Maps& m, cudaStream_t stream)
     if (e != cudaSuccess) return e;
     // Few key tiles: the query heads of a KV head go to several CTAs, as many (a divisor of the group) as leave no more than
     // four per SM.  A causal document's first key tile is seen by all its queries, so this also evens out the CTAs' work.
-    const long long tiles = ((long long)a.k_tokens / kRows + (a.n_docs < a.k_tokens ? a.n_docs : a.k_tokens)) * a.kv_heads;
+    const long long tiles = ((long long)a.k_tokens / kTok + (a.n_docs < a.k_tokens ? a.n_docs : a.k_tokens)) * a.kv_heads;
     int split = 1;
     for (int x = 2; x <= a.group; ++x)
         if (a.group % x == 0 && tiles * x <= 4 * 148) split = x;

@@ -202,10 +202,10 @@ int rlkv_prompt_attention_backward(rlkv_prompt* p, int layer, const void* q, int
     DeviceGuard g(p->device);
     if (!g.ok) return RLKV_ECUDA;
     CUtensorMap map_q, map_k, map_v, map_do;
-    int e = encode_heads_map(&map_q, q, q_tokens, p->q_heads, p->head_dim, a.q_stride, 64);
-    if (!e) e = encode_heads_map(&map_k, k, k_tokens, p->kv_heads, p->head_dim, a.k_stride, 64);
-    if (!e) e = encode_heads_map(&map_v, v, k_tokens, p->kv_heads, p->head_dim, a.v_stride, 64);
-    if (!e) e = encode_heads_map(&map_do, dout, q_tokens, p->q_heads, p->head_dim, (int64_t)p->q_heads * p->head_dim, 64);
+    int e = encode_heads_map(&map_q, q, q_tokens, p->q_heads, p->head_dim, a.q_stride, 128);
+    if (!e) e = encode_heads_map(&map_k, k, k_tokens, p->kv_heads, p->head_dim, a.k_stride, 128);
+    if (!e) e = encode_heads_map(&map_v, v, k_tokens, p->kv_heads, p->head_dim, a.v_stride, 128);
+    if (!e) e = encode_heads_map(&map_do, dout, q_tokens, p->q_heads, p->head_dim, (int64_t)p->q_heads * p->head_dim, 128);
     if (e) return e;
     RLKV_CUDA(launch_prompt_backward(a, map_q, map_k, map_v, map_do, p->head_dim, static_cast<cudaStream_t>(stream)));
     return RLKV_OK;

@@ -9,6 +9,8 @@
 // S and dP are computed twice, seven products where five would do, and in return every gradient is summed by one CTA
 // in a fixed order: no atomics on dQ, no fp32 copy of it in memory, the same bits on every run.  P and dS are written
 // to tensor memory as bf16 over S and dP and are the A operand of the second products straight from there.
+#include <type_traits>
+
 #include "rlkv_prompt.cuh"
 #include "tcgen05.cuh"
 
@@ -21,6 +23,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTok = 128;            // tokens of a tile, of queries and of keys
 constexpr int kBlock = kTok * 128;  // bytes of a block of 64 elements of its rows
 constexpr int kThreads = 384;
+constexpr int kPolyKeys = 0, kPolyRows = 0;  // one pair in so many on the FMA pipe
 
 // ---- D and lse ---------------------------------------------------------------------------------------
 
@@ -73,22 +76,25 @@ __global__ void __launch_bounds__(256) prompt_stats_kernel(const __grid_constant
 
 // ---- what both kernels do with a score ------------------------------------------------------------------
 
-// 32 products q.k -> scores in the log2 domain, and (CAP) the slopes of the cap, 1 - tanh^2.
-template <bool CAP>
-__device__ __forceinline__ void capped(const Cap& cap, float sl2, bool vote, float (&s)[32], float (&f)[CAP ? 32 : 1])
+// N products q.k -> scores in the log2 domain over `factor` (with neither cap nor bias the products are left as they
+// are, the factor is applied with the exponent), and (CAP) the slopes of the cap, 1 - tanh^2.  `dist0`: distance of the
+// first score, `step`: +1 or -1 from one to the next.
+template <bool CAP, bool BIAS, int N>
+__device__ __forceinline__ void finish_scores(const Cap& cap, float sl2, float slope2, int dist0, int step, bool vote, float (&s)[N], float (&f)[CAP ? N : 1])
 {
-    if constexpr (!CAP) {
-#pragma unroll
-        for (int c = 0; c < 32; ++c) s[c] *= sl2;
-    } else {
+    if constexpr (CAP) {
         cap.apply(s, vote);
         const float2 k = make_float2(-1.f / (cap.cap2 * cap.cap2), -1.f / (cap.cap2 * cap.cap2));
 #pragma unroll
-        for (int c = 0; c < 32; c += 2) {
+        for (int c = 0; c < N; c += 2) {
             const float2 x = make_float2(s[c], s[c + 1]), y = fma2(mul2(x, x), k, make_float2(1.f, 1.f));
             f[c] = y.x;
             f[c + 1] = y.y;
         }
+    }
+    if constexpr (BIAS) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] = fmaf(-slope2, fabsf((float)(dist0 + step * c)), CAP ? s[c] : s[c] * sl2);
     }
 }
 
@@ -168,7 +174,7 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
 {
     using F = Keys<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
-    float2* stats = reinterpret_cast<float2*>(smem + F::kStats);
+    float* stats = reinterpret_cast<float*>(smem + F::kStats);  // per stage: -lse of 128 queries, then their -D
     KeysShared& sh = *reinterpret_cast<KeysShared*>(smem + F::kStats + F::kStages * kTok * 8);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     // `split` CTAs, a cluster, share the query heads of a KV head
@@ -258,35 +264,48 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                  wait(smem_u32(&sh.s_full), n & 1, abort_flag, a.status, kPromptWaitProduct);
             if (!ok) break;
             fence_after();
-            const float4* stat = reinterpret_cast<const float4*>(stats + st * kTok + w * 64);
+            const float4* minus_lse = reinterpret_cast<const float4*>(stats + st * 2 * kTok + w * 64);
+            const float4* minus_d = minus_lse + kTok / 4;
             const int p0 = (sh.u0 + u) * kTok + sh.off + w * 64;  // position of this thread's first query
             const bool plain = (p0 >= j_last || j_last < sh.prefix) && (full_head || j_last < a.sink || p0 + 63 < sh.j0 + a.window);
             const float slope2 = BIAS ? a.slopes[head0 + g] * kLog2e : 0.f;
-            float s[2][32], f[2][CAP ? 32 : 1];
+            float s[64], f[CAP ? 64 : 1];
+            tmem_ld32(mine_s, s);
+            tmem_ld32(mine_s + 32, s + 32);
+            wait_ld();
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                tmem_read32(mine_s + half * 32, s[half]);
-                capped<CAP>(cap, sl2, mine, s[half], f[half]);
-                const int d0 = p0 + half * 32 - j;  // distance of the first
-                if (BIAS) {
+            for (int c = 0; c < 64; ++c) asm volatile("" : "+f"(s[c]));  // nothing of it is used before the wait
+            finish_scores<CAP, BIAS>(cap, sl2, slope2, p0 - j, 1, mine, s, f);
+            const float2 factor = CAP || BIAS ? make_float2(1.f, 1.f) : make_float2(sl2, sl2);
+            auto exponentials = [&](auto poly) {
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) s[half][c] = fmaf(-slope2, fabsf((float)(d0 + c)), s[half][c]);
+                for (int c = 0; c < 64; c += 4) {
+                    const float4 x = minus_lse[c / 4];
+                    const float2 y = exp2_pair<decltype(poly)::value>(fma2(make_float2(s[c], s[c + 1]), factor, make_float2(x.x, x.y)), c / 2);
+                    const float2 z = exp2_pair<decltype(poly)::value>(fma2(make_float2(s[c + 2], s[c + 3]), factor, make_float2(x.z, x.w)), c / 2 + 1);
+                    s[c] = y.x;
+                    s[c + 1] = y.y;
+                    s[c + 2] = z.x;
+                    s[c + 3] = z.y;
                 }
+            };
+            if (plain) {
+                exponentials(std::integral_constant<int, kPolyKeys>());
+            } else {
+                exponentials(std::integral_constant<int, 0>());
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    const float4 x = stat[half * 16 + c / 2];  // (lse, D) of two queries
-                    s[half][c] = ex2(s[half][c] - x.x);
-                    s[half][c + 1] = ex2(s[half][c + 1] - x.z);
-                }
-                if (!plain) {
-                    const uint32_t see = range_bits(lo - j - d0, hi - j - d0);
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t see = range_bits(lo - p0 - h * 32, hi - p0 - h * 32);
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) s[half][c] = see >> c & 1 ? s[half][c] : 0.f;
+                    for (int c = 0; c < 32; ++c) s[h * 32 + c] = see >> c & 1 ? s[h * 32 + c] : 0.f;
                 }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
                 uint32_t packed[16];
 #pragma unroll
-                for (int c = 0; c < 16; ++c) packed[c] = bf16x2(s[half][2 * c], s[half][2 * c + 1]);
-                tmem_st16(mine_s + half * 16, packed);  // (over this warpgroup's own columns of S)
+                for (int c = 0; c < 16; ++c) packed[c] = bf16x2(s[h * 32 + 2 * c], s[h * 32 + 2 * c + 1]);
+                tmem_st16(mine_s + h * 16, packed);  // (over this warpgroup's own columns of S)
             }
             wait_st();
             fence_before();
@@ -296,18 +315,24 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             if (!ok) break;
             fence_after();
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
+            for (int h = 0; h < 2; ++h) {
                 float d[32];
-                tmem_read32(mine_dp + half * 32, d);
+                tmem_read32(mine_dp + h * 32, d);
                 uint32_t packed[16];
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    const float4 x = stat[half * 16 + c / 2];
-                    float2 ds = mul2(make_float2(s[half][c], s[half][c + 1]), add2(make_float2(d[c], d[c + 1]), make_float2(-x.y, -x.w)));
-                    if constexpr (CAP) ds = mul2(ds, make_float2(f[half][c], f[half][c + 1]));
-                    packed[c / 2] = bf16x2(ds.x, ds.y);
+                for (int c = 0; c < 32; c += 4) {
+                    const float4 x = minus_d[h * 8 + c / 4];
+                    const int e = h * 32 + c;
+                    float2 y = mul2(make_float2(s[e], s[e + 1]), add2(make_float2(d[c], d[c + 1]), make_float2(x.x, x.y)));
+                    float2 z = mul2(make_float2(s[e + 2], s[e + 3]), add2(make_float2(d[c + 2], d[c + 3]), make_float2(x.z, x.w)));
+                    if constexpr (CAP) {
+                        y = mul2(y, make_float2(f[e], f[e + 1]));
+                        z = mul2(z, make_float2(f[e + 2], f[e + 3]));
+                    }
+                    packed[c / 2] = bf16x2(y.x, y.y);
+                    packed[c / 2 + 1] = bf16x2(z.x, z.y);
                 }
-                tmem_st16(mine_dp + half * 16, packed);
+                tmem_st16(mine_dp + h * 16, packed);
             }
             wait_st();
             fence_before();
@@ -423,7 +448,10 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             if (n + 1 < steps) fetch(next);
             if (!wait(smem_u32(&sh.empty[st]), (n / F::kStages & 1) ^ 1, abort_flag, a.status, kPromptWaitStage)) break;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) stats[st * kTok + lane + 32 * i] = now[i];
+            for (int i = 0; i < 4; ++i) {
+                stats[st * 2 * kTok + lane + 32 * i] = -now[i].x;
+                stats[st * 2 * kTok + kTok + lane + 32 * i] = -now[i].y;
+            }
             if (!wait(smem_u32(&sh.full[st]), n / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad)) break;
             if (valid < kTok) clear_rows<2 * D / 64>(smem + (2 + 2 * st) * F::kTile, valid, lane);
             __syncwarp();
@@ -578,15 +606,16 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const bool plain = start + kTok <= kn && (start + kTok <= first + 1 || start + kTok <= prefix) &&
                                (full_head || start + kTok <= a.sink || start > last - a.window);
             // 32 scores -> P (with CAP after dP is there: its slopes would not fit in registers beside P)
-            auto probabilities = [&](float (&x)[32], float (&f)[CAP ? 32 : 1], int c0) {
-                capped<CAP>(cap, sl2, mine, x, f);
-                if (BIAS) {
+            const float2 factor = CAP || BIAS ? make_float2(1.f, 1.f) : make_float2(sl2, sl2), minus_lse = make_float2(-stat.x, -stat.x);
+            auto probabilities = [&](float (&x)[32], float (&f)[CAP ? 32 : 1], int c0, auto poly) {
+                finish_scores<CAP, BIAS>(cap, sl2, slope2, pos - c0, -1, mine, x, f);
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) x[c] = fmaf(-slope2, fabsf((float)(pos - c0 - c)), x[c]);
+                for (int c = 0; c < 32; c += 2) {
+                    const float2 y = exp2_pair<decltype(poly)::value>(fma2(make_float2(x[c], x[c + 1]), factor, minus_lse), c / 2);
+                    x[c] = y.x;
+                    x[c + 1] = y.y;
                 }
-#pragma unroll
-                for (int c = 0; c < 32; ++c) x[c] = ex2(x[c] - stat.x);
-                if (!plain) {
+                if (decltype(poly)::value == 0 && !plain) {
                     const uint32_t see = range_bits(lo - c0, hi - c0) | range_bits(0, sink - c0);
 #pragma unroll
                     for (int c = 0; c < 32; ++c) x[c] = see >> c & 1 ? x[c] : 0.f;
@@ -594,8 +623,13 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             };
             if constexpr (!CAP) {
                 float none[1];
+                if (plain) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) probabilities(reinterpret_cast<float(&)[32]>(s[c * 32]), none, start + c * 32);
+                    for (int c = 0; c < 4; ++c) probabilities(reinterpret_cast<float(&)[32]>(s[c * 32]), none, start + c * 32, std::integral_constant<int, kPolyRows>());
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) probabilities(reinterpret_cast<float(&)[32]>(s[c * 32]), none, start + c * 32, std::integral_constant<int, 0>());
+                }
             }
             ok = wait(smem_u32(&sh.dp_full[w]), done & 1, abort_flag, a.status, kPromptWaitProduct);
             if (!ok) break;
@@ -604,7 +638,7 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             for (int q = 0; q < 4; ++q) {
                 float(&p)[32] = reinterpret_cast<float(&)[32]>(s[q * 32]);
                 float f[CAP ? 32 : 1], d[32];
-                if constexpr (CAP) probabilities(p, f, start + q * 32);
+                if constexpr (CAP) probabilities(p, f, start + q * 32, std::integral_constant<int, 0>());
                 tmem_read32(S + q * 32, d);
                 uint32_t packed[16];
 #pragma unroll
@@ -684,52 +718,78 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     } else if (warp == 9) {
         // ------------------------------------------------------------------ matrix products
         if (n_tiles > 0) {
-            int used[2] = {0, 0}, read[2] = {0, 0};  // tiles of a sub-tile whose dS was multiplied, whose S was taken
+            // Each sub-tile goes its own way -- S, dP once its threads hold S, dQ once they have written dS -- and whatever is
+            // ready first is issued first: in a fixed order of the two one would wait for the other's arithmetic.
             const int sub_a[2] = {sh.at.sub_a[0], sh.at.sub_a[1]}, sub_b[2] = {sh.at.sub_b[0], sh.at.sub_b[1]}, sub_e[2] = {sh.at.sub_e[0], sh.at.sub_e[1]};
-            auto needed = [&](int w, int t) { return t < sub_a[w] || (t >= sub_b[w] && t < sub_e[w]); };
-            auto cleaned = [&](int j, int which) {
-                return (tile_at(j) + 1) * kTok <= kn || wait_warp(smem_u32(&sh.clean[which]), 0, abort_flag, a.status, kPromptWaitLoad);
-            };
-            auto k_loaded = [&](int j) { return wait_warp(smem_u32(&sh.k_full[j % 2]), j / 2 & 1, abort_flag, a.status, kPromptWaitLoad) && cleaned(j, 0); };
-            // dP of both sub-tiles, each once its threads hold S
-            auto value_products = [&](int j) {
-                const int v = j % F::kValues;
-                if (!wait_warp(smem_u32(&sh.v_full[v]), j / F::kValues & 1, abort_flag, a.status, kPromptWaitLoad) || !cleaned(j, 1)) return false;
+            enum { kNextS, kNextDp, kNextDq, kNothing };  // the product that comes next
+            int tile[2], next[2], done[2] = {0, 0}, passed_k[2], passed_v[2], freed_k = 0, freed_v = 0;
+            // (the CTA's running number of a tile, which its K and V slots go by)
+            auto number = [&](int t) { return t < a_end ? t : a_end + t - b0; };
 #pragma unroll
-                for (int w = 0; w < 2; ++w)
-                    if (needed(w, tile_at(j))) {
-                        if (!wait_warp(smem_u32(&sh.s_read[w]), read[w] & 1, abort_flag, a.status, kPromptWaitSoftmax)) return false;
-                        fence_after();
-                        ++read[w];
-                        scores<D>(tmem + w * kTok, o_smem + w * F::kTile, v_smem + v * F::kTile, &sh.dp_full[w]);
-                    }
-                signal(&sh.v_empty[v]);
-                return true;
-            };
-            bool ok = wait_warp(smem_u32(&sh.q_full), 0, abort_flag, a.status, kPromptWaitLoad) && k_loaded(0);
-            if (ok) {
-#pragma unroll
-                for (int w = 0; w < 2; ++w)
-                    if (needed(w, tile_at(0))) scores<D>(tmem + w * kTok, q_smem + w * F::kTile, k_smem, &sh.s_full[w]);
-                ok = value_products(0);
+            for (int w = 0; w < 2; ++w) {
+                tile[w] = sub_a[w] > 0 ? 0 : sub_b[w];
+                next[w] = tile[w] < sub_e[w] ? kNextS : kNothing;
+                passed_k[w] = passed_v[w] = next[w] == kNothing ? n_tiles : number(tile[w]);
             }
-            for (int j = 0; ok && j < n_tiles; ++j) {
-                const bool more = j + 1 < n_tiles;
-                if (more) ok = k_loaded(j + 1);
+            auto ready = [&](uint64_t* bar, int parity) { return __all_sync(0xffffffffu, mbar_try_wait(smem_u32(bar), parity & 1)); };
+            // rows behind the last key have been cleared
+            auto cleaned = [&](int t, int which) { return (t + 1) * kTok <= kn || ready(&sh.clean[which], 0); };
+            bool ok = wait_warp(smem_u32(&sh.q_full), 0, abort_flag, a.status, kPromptWaitLoad);
+            uint64_t idle_since = 0;
+            while (ok && (next[0] != kNothing || next[1] != kNothing)) {
+                bool moved = false;
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
-                    if (!ok) break;
-                    if (needed(w, tile_at(j))) {
-                        ok = wait_warp(smem_u32(&sh.ds_full[w]), used[w] & 1, abort_flag, a.status, kPromptWaitSoftmax);
-                        if (!ok) break;
+                    const int t = tile[w], j = number(t), after = t + 1 == sub_a[w] ? sub_b[w] : t + 1;
+                    const int after_j = after < sub_e[w] ? number(after) : n_tiles;
+                    if (next[w] == kNextS) {
+                        // (a slot's phase says which tile it holds only once the one before it has been given back)
+                        if (freed_k < j - 1 || !ready(&sh.k_full[j % 2], j / 2) || !cleaned(t, 0)) continue;
+                        scores<D>(tmem + w * kTok, q_smem + w * F::kTile, k_smem + j % 2 * F::kTile, &sh.s_full[w]);
+                        next[w] = kNextDp;
+                    } else if (next[w] == kNextDp) {
+                        const int v = j % F::kValues;
+                        if (freed_v < j - F::kValues + 1 || !ready(&sh.s_read[w], done[w]) || !ready(&sh.v_full[v], j / F::kValues) || !cleaned(t, 1)) continue;
                         fence_after();
-                        gradient<D>(tmem + 256 + w * D, tmem + w * kTok, 32, k_smem + j % 2 * F::kTile, used[w] > 0);
-                        ++used[w];
+                        scores<D>(tmem + w * kTok, o_smem + w * F::kTile, v_smem + v * F::kTile, &sh.dp_full[w]);
+                        next[w] = kNextDq;
+                        passed_v[w] = after_j;
+                    } else if (next[w] == kNextDq) {
+                        if (!ready(&sh.ds_full[w], done[w])) continue;
+                        fence_after();
+                        gradient<D>(tmem + 256 + w * D, tmem + w * kTok, 32, k_smem + j % 2 * F::kTile, done[w] > 0);
+                        ++done[w];
+                        passed_k[w] = after_j;
+                        tile[w] = after;
+                        next[w] = after_j < n_tiles ? kNextS : kNothing;
+                        // (the next S at once where its keys are there: the two sub-tiles then stay out of step, and one's
+                        // arithmetic runs beside the other's products)
+                        if (after_j < n_tiles && freed_k >= after_j - 1 && ready(&sh.k_full[after_j % 2], after_j / 2) && cleaned(after, 0)) {
+                            scores<D>(tmem + w * kTok, q_smem + w * F::kTile, k_smem + after_j % 2 * F::kTile, &sh.s_full[w]);
+                            next[w] = kNextDp;
+                        }
+                    } else {
+                        continue;
                     }
-                    if (w == 1) signal(&sh.k_empty[j % 2]);
-                    if (more && needed(w, tile_at(j + 1))) scores<D>(tmem + w * kTok, q_smem + w * F::kTile, k_smem + (j + 1) % 2 * F::kTile, &sh.s_full[w]);
+                    moved = true;
+                    // slots that neither sub-tile needs any more
+                    for (; freed_k < min(passed_k[0], passed_k[1]); ++freed_k) signal(&sh.k_empty[freed_k % 2]);
+                    for (; freed_v < min(passed_v[0], passed_v[1]); ++freed_v) signal(&sh.v_empty[freed_v % F::kValues]);
                 }
-                if (ok && more) ok = value_products(j + 1);
+                if (moved) {
+                    idle_since = 0;
+                } else {
+                    const uint64_t now = __shfl_sync(0xffffffffu, now_ns(), 0);
+                    if (idle_since == 0) idle_since = now;
+                    if (now - idle_since > kWaitNs) {
+                        if (lane == 0) {
+                            *abort_flag = 1;
+                            atomicCAS(a.status, 0, kPromptWaitSoftmax);
+                        }
+                        ok = false;
+                    }
+                    if (__any_sync(0xffffffffu, *abort_flag != 0)) ok = false;
+                }
             }
             signal(&sh.done);
             signal(&sh.drain);

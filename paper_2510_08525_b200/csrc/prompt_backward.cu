@@ -9,8 +9,6 @@
 // S and dP are computed twice, seven products where five would do, and in return every gradient is summed by one CTA
 // in a fixed order: no atomics on dQ, no fp32 copy of it in memory, the same bits on every run.  P and dS are written
 // to tensor memory as bf16 over S and dP and are the A operand of the second products straight from there.
-#include <type_traits>
-
 #include "rlkv_prompt.cuh"
 #include "tcgen05.cuh"
 
@@ -23,7 +21,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTok = 128;            // tokens of a tile, of queries and of keys
 constexpr int kBlock = kTok * 128;  // bytes of a block of 64 elements of its rows
 constexpr int kThreads = 384;
-constexpr int kPolyKeys = 0, kPolyRows = 0;  // one pair in so many on the FMA pipe
 
 // ---- D and lse ---------------------------------------------------------------------------------------
 
@@ -277,22 +274,17 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             for (int c = 0; c < 64; ++c) asm volatile("" : "+f"(s[c]));  // nothing of it is used before the wait
             finish_scores<CAP, BIAS>(cap, sl2, slope2, p0 - j, 1, mine, s, f);
             const float2 factor = CAP || BIAS ? make_float2(1.f, 1.f) : make_float2(sl2, sl2);
-            auto exponentials = [&](auto poly) {
 #pragma unroll
-                for (int c = 0; c < 64; c += 4) {
-                    const float4 x = minus_lse[c / 4];
-                    const float2 y = exp2_pair<decltype(poly)::value>(fma2(make_float2(s[c], s[c + 1]), factor, make_float2(x.x, x.y)), c / 2);
-                    const float2 z = exp2_pair<decltype(poly)::value>(fma2(make_float2(s[c + 2], s[c + 3]), factor, make_float2(x.z, x.w)), c / 2 + 1);
-                    s[c] = y.x;
-                    s[c + 1] = y.y;
-                    s[c + 2] = z.x;
-                    s[c + 3] = z.y;
-                }
-            };
-            if (plain) {
-                exponentials(std::integral_constant<int, kPolyKeys>());
-            } else {
-                exponentials(std::integral_constant<int, 0>());
+            for (int c = 0; c < 64; c += 4) {
+                const float4 x = minus_lse[c / 4];
+                const float2 y = fma2(make_float2(s[c], s[c + 1]), factor, make_float2(x.x, x.y));
+                const float2 z = fma2(make_float2(s[c + 2], s[c + 3]), factor, make_float2(x.z, x.w));
+                s[c] = ex2(y.x);
+                s[c + 1] = ex2(y.y);
+                s[c + 2] = ex2(z.x);
+                s[c + 3] = ex2(z.y);
+            }
+            if (!plain) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const uint32_t see = range_bits(lo - p0 - h * 32, hi - p0 - h * 32);
@@ -607,15 +599,15 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                                (full_head || start + kTok <= a.sink || start > last - a.window);
             // 32 scores -> P (with CAP after dP is there: its slopes would not fit in registers beside P)
             const float2 factor = CAP || BIAS ? make_float2(1.f, 1.f) : make_float2(sl2, sl2), minus_lse = make_float2(-stat.x, -stat.x);
-            auto probabilities = [&](float (&x)[32], float (&f)[CAP ? 32 : 1], int c0, auto poly) {
+            auto probabilities = [&](float (&x)[32], float (&f)[CAP ? 32 : 1], int c0) {
                 finish_scores<CAP, BIAS>(cap, sl2, slope2, pos - c0, -1, mine, x, f);
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
-                    const float2 y = exp2_pair<decltype(poly)::value>(fma2(make_float2(x[c], x[c + 1]), factor, minus_lse), c / 2);
-                    x[c] = y.x;
-                    x[c + 1] = y.y;
+                    const float2 y = fma2(make_float2(x[c], x[c + 1]), factor, minus_lse);
+                    x[c] = ex2(y.x);
+                    x[c + 1] = ex2(y.y);
                 }
-                if (decltype(poly)::value == 0 && !plain) {
+                if (!plain) {
                     const uint32_t see = range_bits(lo - c0, hi - c0) | range_bits(0, sink - c0);
 #pragma unroll
                     for (int c = 0; c < 32; ++c) x[c] = see >> c & 1 ? x[c] : 0.f;
@@ -623,13 +615,8 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             };
             if constexpr (!CAP) {
                 float none[1];
-                if (plain) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) probabilities(reinterpret_cast<float(&)[32]>(s[c * 32]), none, start + c * 32, std::integral_constant<int, kPolyRows>());
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) probabilities(reinterpret_cast<float(&)[32]>(s[c * 32]), none, start + c * 32, std::integral_constant<int, 0>());
-                }
+                for (int c = 0; c < 4; ++c) probabilities(reinterpret_cast<float(&)[32]>(s[c * 32]), none, start + c * 32);
             }
             ok = wait(smem_u32(&sh.dp_full[w]), done & 1, abort_flag, a.status, kPromptWaitProduct);
             if (!ok) break;
@@ -638,7 +625,7 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             for (int q = 0; q < 4; ++q) {
                 float(&p)[32] = reinterpret_cast<float(&)[32]>(s[q * 32]);
                 float f[CAP ? 32 : 1], d[32];
-                if constexpr (CAP) probabilities(p, f, start + q * 32, std::integral_constant<int, 0>());
+                if constexpr (CAP) probabilities(p, f, start + q * 32);
                 tmem_read32(S + q * 32, d);
                 uint32_t packed[16];
 #pragma unroll

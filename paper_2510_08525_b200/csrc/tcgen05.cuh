@@ -240,30 +240,6 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
     return d;
 }
 
-// 2^x on the FMA pipe, for finite x up to about 120 (2^-126 below that range): x = n + f with |f| <= 1/2, a polynomial of
-// degree 4 in f (fitted to the smallest largest relative error, 2.6e-6), and n added to its exponent.
-__device__ __forceinline__ float2 exp2_fma(float2 x)
-{
-    const float2 magic = make_float2(12582912.f, 12582912.f);  // 1.5 * 2^23: the sum's low bits are round(x)
-    x.x = fmaxf(x.x, -126.f);
-    x.y = fmaxf(x.y, -126.f);
-    const float2 n = add2(x, magic);
-    const float2 f = add2(x, fma2(n, make_float2(-1.f, -1.f), magic));
-    float2 p = fma2(f, make_float2(0.00957010059f, 0.00957010059f), make_float2(0.0559178602f, 0.0559178602f));
-    p = fma2(p, f, make_float2(0.240247449f, 0.240247449f));
-    p = fma2(p, f, make_float2(0.693121815f, 0.693121815f));
-    p = fma2(p, f, make_float2(0.999999261f, 0.999999261f));
-    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(n.x) << 23)),
-                       __int_as_float(__float_as_int(p.y) + (__float_as_int(n.y) << 23)));
-}
-// 2^x, one pair in POLY of a run of pairs (`i`: which) on the FMA pipe; POLY 0: none.
-template <int POLY>
-__device__ __forceinline__ float2 exp2_pair(float2 x, int i)
-{
-    if (POLY > 0 && i % (POLY > 0 ? POLY : 1) == POLY - 1) return exp2_fma(x);
-    return make_float2(ex2(x.x), ex2(x.y));
-}
-
 // 32 columns, usable at once.
 __device__ __forceinline__ void tmem_read32(uint32_t addr, float (&s)[32])
 {

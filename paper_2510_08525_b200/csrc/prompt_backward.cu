@@ -185,12 +185,12 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         return;
     }
     if (warp == 0) {
-        int doc = 0, tile = 0;
-        const bool valid = find_tile(a, true, kTok, block / a.kv_heads, doc, tile);
+        int tile = 0;
+        DocRange r;
+        const bool valid = find_tile(a, true, kTok, block / a.kv_heads, r, tile);
         if (lane == 0) {
             sh.valid = valid;
             if (valid) {
-                const DocRange r = doc_range(a, doc);
                 tile = (r.kn + kTok - 1) / kTok - 1 - tile;  // a document's first keys are seen by the most queries
                 const int j0 = tile * kTok, j1 = min(j0 + kTok, r.kn), off = r.kn - r.qn;
                 sh.k0 = r.k0 + j0;

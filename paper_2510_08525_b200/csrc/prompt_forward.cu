@@ -6,7 +6,7 @@
 // O += P.V with P read from tensor memory.  Two sub-tiles so that one's products run while the other's softmax does.
 //
 //   warps 0-3, 4-7   softmax of sub-tile 0 / 1, and its output rows at the end
-//   warp 8           TMA: Q once, then K and V tiles in turn through one ring; clears the V rows behind the document's
+//   warp 8           TMA: Q once, then K and V tiles in turn through one ring; clears the rows behind the document's
 //                    last key (0 * NaN of a neighbour would be NaN)
 //   warp 9           issues every tcgen05.mma (in order, so S of the next tile may overwrite P of this one)
 //
@@ -36,7 +36,7 @@ struct Fwd {
 };
 
 struct FwdShared {
-    uint64_t q_full, full[10], empty[10], s_full[2], p_full[2][2], pv_done[2], clean, drain;
+    uint64_t q_full, full[10], empty[10], s_full[2], p_full[2][2], pv_done[2], clean[2], drain;
     uint32_t tmem;
     int abort;
     RowTile at;
@@ -109,7 +109,8 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
                 mbar_init(smem_u32(&sh.p_full[w][1]), 4);
                 mbar_init(smem_u32(&sh.pv_done[w]), 1);
             }
-            mbar_init(smem_u32(&sh.clean), 1);
+            mbar_init(smem_u32(&sh.clean[0]), 1);
+            mbar_init(smem_u32(&sh.clean[1]), 1);
             mbar_init(smem_u32(&sh.drain), 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
@@ -169,12 +170,8 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
                         see[c] = mine ? range_bits(lo - start - c * 32, hi - start - c * 32) | range_bits(0, sink - start - c * 32) : 0u;
                 }
                 if (CAP) {
-                    // what the row does not see has no say in how its warp computes the cap (nothing another document holds
-                    // may change a bit of this one's result)
-                    if (!plain) {
-#pragma unroll
-                        for (int c = 0; c < kRows; ++c) s[c] = see[c / 32] >> (c & 31) & 1 ? s[c] : 0.f;
-                    }
+                    // (rows behind the document's last key read as zero, so nothing another document holds has a say in how
+                    // the warp computes the cap)
                     cap.apply(s, mine);
                 }
                 if (BIAS) {
@@ -264,18 +261,20 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
             }
         }
         __syncwarp();
-        // the last tile copied is V's last; it is the only one that can reach past the keys.  (This warp may wait for it:
-        // it has seen the stage's earlier copies consumed)
-        const int last = 2 * n_tiles - 1, rows = n_tiles > 0 ? kn - tile_at(n_tiles - 1) * kRows : kRows;
-        if (rows < kRows && !*abort_flag &&
-            wait(smem_u32(&sh.full[last % F::kStages]), last / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad)) {
-            uint8_t* v = smem + (2 + last % F::kStages) * F::kTileBytes;
-            for (int x = rows * 8 + lane; x < kRows * 8; x += 32)
-                for (int b = 0; b < D / 64; ++b) *reinterpret_cast<uint4*>(v + b * kBlock + x * 16) = make_uint4(0, 0, 0, 0);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh.clean));
-        }
+        // rows behind the document's last key: only the last K and V tiles can hold any.  (This warp may wait for them: it has
+        // seen their stages' earlier copies consumed)
+        const int rows = n_tiles > 0 ? kn - tile_at(n_tiles - 1) * kRows : kRows;
+        if (rows < kRows)
+            for (int v = 0; v < 2; ++v) {
+                const int last = 2 * n_tiles - 2 + v;
+                if (*abort_flag || !wait(smem_u32(&sh.full[last % F::kStages]), last / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad)) break;
+                uint8_t* x = smem + (2 + last % F::kStages) * F::kTileBytes;
+                for (int i = rows * 8 + lane; i < kRows * 8; i += 32)
+                    for (int b = 0; b < D / 64; ++b) *reinterpret_cast<uint4*>(x + b * kBlock + i * 16) = make_uint4(0, 0, 0, 0);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.clean[v]));
+            }
     } else if (warp == 9) {
         // ------------------------------------------------------------------ matrix products
         if (n_tiles > 0) {
@@ -285,8 +284,10 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
             const int sub_a[2] = {sh.at.sub_a[0], sh.at.sub_a[1]}, sub_b[2] = {sh.at.sub_b[0], sh.at.sub_b[1]}, sub_e[2] = {sh.at.sub_e[0], sh.at.sub_e[1]};
             auto needed = [&](int w, int t) { return t < sub_a[w] || (t >= sub_b[w] && t < sub_e[w]); };
             auto stage = [&](int i) { return ring + i % F::kStages * F::kTileBytes; };
+            // K (even) and V tiles in turn; the last two once the rows behind the last key have been cleared
             auto loaded = [&](int i) {
-                return wait_warp(smem_u32(&sh.full[i % F::kStages]), i / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad);
+                return wait_warp(smem_u32(&sh.full[i % F::kStages]), i / F::kStages & 1, abort_flag, a.status, kPromptWaitLoad) &&
+                       ((tile_at(i >> 1) + 1) * kRows <= kn || wait_warp(smem_u32(&sh.clean[i & 1]), 0, abort_flag, a.status, kPromptWaitLoad));
             };
             auto signal = [&](uint64_t* bar) {
                 if (elect_one()) commit(smem_u32(bar));
@@ -311,7 +312,6 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
             for (int j = 0; ok && j < n_tiles; ++j) {
                 const int t = tile_at(j);
                 ok = loaded(2 * j + 1);
-                if (ok && (t + 1) * kRows > kn) ok = wait_warp(smem_u32(&sh.clean), 0, abort_flag, a.status, kPromptWaitLoad);
                 if (ok && j + 1 < n_tiles) ok = loaded(2 * j + 2);
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {

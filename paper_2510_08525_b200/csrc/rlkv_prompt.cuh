@@ -47,37 +47,56 @@ __device__ __forceinline__ DocRange doc_range(const PromptArgs& a, int d)
 enum : int { kPromptWaitLoad = 101, kPromptWaitProduct = 102, kPromptWaitSoftmax = 103, kPromptWaitStage = 104, kPromptWaitDrain = 105,
              kPromptSmemMisaligned = 106 };
 
-// Tiles of `rows` queries, numbered from the LAST tile of the last document backwards (a causal document's last
-// tiles are its longest, and the longest are best started first).  Called by one whole warp; returns false where
-// there are no more than `index` tiles.  A lane counts the tiles of eight neighbouring documents per round.
-__device__ __forceinline__ bool find_tile(const PromptArgs& a, bool keys, int rows, int index, int& doc, int& tile)
+// Tiles of `rows` queries (or keys), numbered from the LAST tile of the last document backwards (a causal document's last
+// tiles are its longest, and the longest are best started first).  Called by one whole warp; returns false where there
+// are no more than `index` tiles, else tile `tile` of the document in `range`.
+__device__ __forceinline__ bool find_tile(const PromptArgs& a, bool keys, int rows, int index, DocRange& range, int& tile)
 {
     const int lane = threadIdx.x & 31;
+    auto tiles_of = [&](const DocRange& r) { return ((keys ? r.kn : r.qn) + rows - 1) / rows; };
     if (a.n_docs == 1) {
-        const DocRange r = doc_range(a, 0);
-        doc = 0;
-        tile = ((keys ? r.kn : r.qn) + rows - 1) / rows - 1 - index;
+        range = doc_range(a, 0);
+        tile = tiles_of(range) - 1 - index;
         return tile >= 0;
     }
+    auto scan = [&](int x) {  // inclusive, over the lanes
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        return x;
+    };
     int left = index;
-    for (int top = a.n_docs; top > 0; top -= 256) {
+    if (a.n_docs <= 64) {  // a document per lane: one trip to memory, the range comes from its lane
+        for (int top = a.n_docs; top > 0; top -= 32) {
+            const int d = top - 1 - lane;
+            const DocRange r = d >= 0 ? doc_range(a, d) : DocRange{0, 0, 0, 0, 0};
+            const int n = tiles_of(r), upto = scan(n);
+            const unsigned hit = __ballot_sync(0xffffffffu, upto > left);
+            if (hit) {
+                const int owner = __ffs(hit) - 1;
+                range.q0 = __shfl_sync(0xffffffffu, r.q0, owner);
+                range.qn = __shfl_sync(0xffffffffu, r.qn, owner);
+                range.k0 = __shfl_sync(0xffffffffu, r.k0, owner);
+                range.kn = __shfl_sync(0xffffffffu, r.kn, owner);
+                range.prefix = __shfl_sync(0xffffffffu, r.prefix, owner);
+                tile = __shfl_sync(0xffffffffu, upto, owner) - 1 - left;
+                return true;
+            }
+            left -= __shfl_sync(0xffffffffu, upto, 31);
+        }
+        return false;
+    }
+    for (int top = a.n_docs; top > 0; top -= 256) {  // eight neighbouring documents per lane
         int n[8], sum = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int d = top - 1 - lane * 8 - i;
-            n[i] = 0;
-            if (d >= 0) {
-                const DocRange r = doc_range(a, d);
-                n[i] = ((keys ? r.kn : r.qn) + rows - 1) / rows;
-            }
+            n[i] = d >= 0 ? tiles_of(doc_range(a, d)) : 0;
             sum += n[i];
         }
-        int upto = sum;  // inclusive scan over the lanes
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += x;
-        }
+        const int upto = scan(sum);
         const unsigned hit = __ballot_sync(0xffffffffu, upto > left);
         if (hit) {
             const int owner = __ffs(hit) - 1;
@@ -88,7 +107,7 @@ __device__ __forceinline__ bool find_tile(const PromptArgs& a, bool keys, int ro
                 d = top - 1 - lane * 8 - i;
                 t = n[i] - 1 - rest;
             }
-            doc = __shfl_sync(0xffffffffu, d, owner);
+            range = doc_range(a, __shfl_sync(0xffffffffu, d, owner));
             tile = __shfl_sync(0xffffffffu, t, owner);
             return true;
         }
@@ -118,12 +137,12 @@ __device__ __forceinline__ void find_row_tile(const PromptArgs& a, int keys, Row
 {
     const bool pair = heads_pair(a.group);
     const int units = pair ? a.q_heads / 2 : a.q_heads, span = pair ? 128 : 256;
-    int doc = 0, tile = 0;
-    const bool valid = find_tile(a, false, span, blockIdx.x / units, doc, tile);
+    int tile = 0;
+    DocRange r;
+    const bool valid = find_tile(a, false, span, blockIdx.x / units, r, tile);
     if ((threadIdx.x & 31) != 0) return;
     t.valid = valid;
     if (!valid) return;
-    const DocRange r = doc_range(a, doc);
     const int unit = blockIdx.x % units, first = tile * span;
     t.k0 = r.k0;
     t.kn = r.kn;

@@ -297,7 +297,7 @@ int rlkv_rotary_table(const double* inv_freq, int rot_dim, int positions, void* 
 /* The rotation of the cache's rotated calls from now on: element pairs j of the first rot_dim elements of a
  * head -- (j, j + rot_dim / 2), or (2j, 2j + 1) if interleaved -- are turned by the angle in row t of the table for
  * the token that becomes token t of its sequence.  rot_dim: a multiple of 16, at most head_dim; elements past it
- * stay as they are.  The table (as above, `positions` rows) is the caller's and has to outlive the calls;
+ * stay as they are.  The table (as above, `positions` rows, on the cache's GPU) is the caller's and has to outlive the calls;
  * NULL: no rotation is set (the rotated calls then return RLKV_EINVAL). */
 int rlkv_paged_set_rotary(rlkv_paged* cache, const void* table, int positions, int rot_dim, int interleaved);
 /* rlkv_paged_append on keys rotated by their position, the queries of the same tokens rotated in the same

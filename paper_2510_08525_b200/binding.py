@@ -435,11 +435,17 @@ def rlkv_paged_prefill(cache, layer, slot, k, v, n_tokens, stream=None) -> None:
     _check(lib.rlkv_paged_prefill(cache, layer, slot, _ptr(k), _ptr(v), n_tokens, _stream(stream)))
 
 
+def _on_device(x) -> bool:
+    return not isinstance(x, np.ndarray) and x.is_cuda
+
+
 def _rows(x):
     """(address, elements from token to token) of a [tokens][heads][head_dim] tensor, which may be a slice of a
     wider projection; an address alone stands for contiguous tokens."""
-    if x is None or isinstance(x, (int, np.ndarray)):
-        return _ptr(x), 0
+    if x is None or isinstance(x, int):
+        return x or 0, 0
+    if not _on_device(x):
+        raise ValueError("a tensor in device memory is wanted")
     n, _, dim = x.shape  # ValueError where it has other than three dimensions
     token, head, one = x.stride()
     if one != 1 or head != dim:
@@ -542,6 +548,8 @@ def rlkv_prompt_destroy(prompt) -> None:
 
 
 def _prompt_args(q, k, v, q_starts, k_starts, prefix):
+    if any(x is not None and not _on_device(x) for x in (q_starts, k_starts, prefix)):
+        raise ValueError("q_starts, k_starts and prefix are read on the device")
     n_docs = q_starts.numel() - 1
     if k_starts is not None and k_starts.numel() != n_docs + 1 or prefix is not None and prefix.numel() != n_docs:
         raise ValueError("k_starts must have as many entries as q_starts, prefix one less")

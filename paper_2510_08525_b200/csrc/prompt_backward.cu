@@ -21,6 +21,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTok = 128;            // tokens of a tile, of queries and of keys
 constexpr int kBlock = kTok * 128;  // bytes of a block of 64 elements of its rows
 constexpr int kThreads = 384;
+constexpr int kFewKeys = 2048;
 
 // ---- D and lse ---------------------------------------------------------------------------------------
 
@@ -138,6 +139,23 @@ __device__ __forceinline__ void gradient(uint32_t d, uint32_t a_tmem, int second
 #pragma unroll
         for (int i = 0; i < kTok / 16; ++i)
             mma_ts(d, a_tmem + (i < 4 ? i * 8 : second + (i - 4) * 8), y + (i * 2048 >> 4), instr_desc(kTok, D, true), add || i > 0);
+    }
+}
+
+// The same for an A of 32-token blocks, 32 columns apart: 16 columns of rounded values and, `in_two`, 16 more of what the
+// rounding left.
+template <int D>
+__device__ __forceinline__ void gradient_blocks(uint32_t d, uint32_t a_tmem, uint32_t b_smem, bool in_two, bool add)
+{
+    const uint64_t y = smem_desc(b_smem, kBlock);
+    if (elect_one()) {
+#pragma unroll
+        for (int i = 0; i < kTok / 16; ++i)
+            mma_ts(d, a_tmem + i / 2 * 32 + i % 2 * 8, y + (i * 2048 >> 4), instr_desc(kTok, D, true), add || i > 0);
+        if (in_two) {
+#pragma unroll 1  // (unrolled too, the descriptors of both loops would not fit this warp's registers)
+            for (int i = 0; i < kTok / 16; ++i) mma_ts(d, a_tmem + i / 2 * 32 + i % 2 * 8 + 16, y + (i * 2048 >> 4), instr_desc(kTok, D, true), true);
+        }
     }
 }
 
@@ -560,6 +578,11 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     const int n_tiles = sh.at.n_tiles, a_end = sh.at.a_end, b0 = sh.at.b0, kn = sh.at.kn, prefix = sh.at.prefix;
     const int n_sub = sh.at.n_sub, kv_head = sh.at.kv_head;
     const bool full_head = a.full[kv_head] != 0;
+    // Where a query sees few keys, what the rounding of `out` did to D weighs as much in dQ as the rounding of dS: dS then
+    // goes into its product in two bf16 parts, and dQ is off by 2.3e-3 of its norm instead of 2.8e-3 (documents of a few
+    // hundred tokens; one rounding of the exact gradient to bf16: 1.7e-3).  With thousands of keys D is near enough (2.4e-3
+    // without) and the fourth product would cost a quarter of the kernel's time (8192 tokens: 680 -> 857 us).
+    const bool in_two = (full_head ? kn : min(kn, a.sink + a.window)) <= kFewKeys;
     const uint32_t q_smem = smem_u32(smem), o_smem = q_smem + 2 * F::kTile, k_smem = q_smem + 4 * F::kTile, v_smem = q_smem + 6 * F::kTile;
     auto tile_at = [&](int j) { return j < a_end ? j : b0 + j - a_end; };
     // (launched with 384 x 168 = 64512 registers: 256 x 232 + 128 x 40)
@@ -634,8 +657,16 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     excess = add2(excess, ds);
                     if constexpr (CAP) ds = mul2(ds, make_float2(f[c], f[c + 1]));
                     packed[c / 2] = bf16x2(ds.x, ds.y);
+                    p[c] = ds.x;
+                    p[c + 1] = ds.y;
                 }
-                tmem_st16(S + q * 16, packed);
+                tmem_st16(S + q * 32, packed);
+                if (in_two) {
+#pragma unroll
+                    for (int c = 0; c < 16; ++c)
+                        packed[c] = bf16x2(p[2 * c] - __uint_as_float(packed[c] << 16), p[2 * c + 1] - __uint_as_float(packed[c] & 0xffff0000u));
+                    tmem_st16(S + q * 32 + 16, packed);
+                }
             }
             wait_st();
             fence_before();
@@ -744,7 +775,7 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     } else if (next[w] == kNextDq) {
                         if (!ready(&sh.ds_full[w], done[w])) continue;
                         fence_after();
-                        gradient<D>(tmem + 256 + w * D, tmem + w * kTok, 32, k_smem + j % 2 * F::kTile, done[w] > 0);
+                        gradient_blocks<D>(tmem + 256 + w * D, tmem + w * kTok, k_smem + j % 2 * F::kTile, in_two, done[w] > 0);
                         ++done[w];
                         passed_k[w] = after_j;
                         tile[w] = after;

@@ -494,6 +494,13 @@ int rlkv_paged_set_rotary(rlkv_paged* p, const void* table, int positions, int r
 {
     if (!p) return RLKV_EINVAL;
     if (table && (!aligned16(table) || positions < 1 || rot_dim < 16 || rot_dim % 16 || rot_dim > p->head_dim)) return RLKV_EINVAL;
+    if (table) {
+        cudaPointerAttributes at;
+        if (cudaPointerGetAttributes(&at, table) != cudaSuccess || at.type != cudaMemoryTypeDevice || at.device != p->device) {
+            cudaGetLastError();
+            return RLKV_EINVAL;
+        }
+    }
     p->rotary = static_cast<const float*>(table);
     p->rotary_rows = table ? positions : 0;
     p->rotary_dim = rot_dim;

@@ -176,6 +176,48 @@ def test_documents_do_not_touch_one_another(rl, cuda_device):
     assert rl.rlkv_prompt_kernel_status(p.h) == 0
 
 
+@pytest.mark.parametrize("n_docs,Hkv,Hq,D", [(31, 2, 4, 64), (64, 1, 7, 64), (65, 2, 4, 128), (700, 1, 2, 64)])
+def test_many_documents(rl, cuda_device, n_docs, Hkv, Hq, D):
+    """Short and empty documents, more than a warp's lanes and more than a round of the search."""
+    dev = cuda_device
+    lq = [(i * 37) % 13 if i % 50 else 150 for i in range(n_docs)]
+    lk = [n + 3 * (i % 3) for i, n in enumerate(lq)]
+    c = dict(mask=[1, 0][:Hkv], sink=2, window=5, cap=0.0, slopes=None, prefix=None)
+    nq, nk = sum(lq), sum(lk)
+    p = Prompt(rl, 1, Hkv, Hq, D, nq, c["mask"], 2, 5)
+    q, k, v, dout = inputs(nq, nk, Hq, Hkv, D, 17, dev)
+    got = call(rl, p.h, 0, q, k, v, starts(lq, dev), starts(lk, dev), None, dout)
+    want, tol = reference(c, q, k, v, lq, lk, dout)
+    check(got, want, tol, nq, nk)
+    assert rl.rlkv_prompt_kernel_status(p.h) == 0
+
+
+def test_long_document_and_window(rl, cuda_device):
+    """Many key tiles: the ring of K and V tiles goes round, sums over query heads go through one CTA's ring too."""
+    dev, Hkv, Hq, D, n = cuda_device, 2, 4, 128, 5000
+    c = dict(mask=[1, 0], sink=200, window=1000, cap=0.0, slopes=None, prefix=None)
+    p = Prompt(rl, 1, Hkv, Hq, D, n, c["mask"], 200, 1000)
+    q, k, v, dout = inputs(n, n, Hq, Hkv, D, 19, dev)
+    got = call(rl, p.h, 0, q, k, v, starts([n], dev), None, None, dout)
+    want, tol = reference(c, q, k, v, [n], [n], dout)
+    check(got, want, tol, n, n)
+
+
+def test_large_scores(rl, cuda_device):
+    """One key takes nearly all of a row's weight, later keys raise the running maximum again and again."""
+    dev, Hkv, Hq, D, n = cuda_device, 1, 2, 64, 700
+    p = Prompt(rl, 1, Hkv, Hq, D, n, [1], 4, 60)
+    q, k, v, dout = inputs(n, n, Hq, Hkv, D, 23, dev)
+    k = (k.float() * torch.linspace(0.1, 12, n, device=dev)[:, None, None]).to(torch.bfloat16)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device=dev)
+    rl.rlkv_prompt_attention(p.h, 0, q, k, v, starts([n], dev), None, None, out, lse)
+    c = dict(mask=[1], sink=4, window=60, cap=0.0, slopes=None, prefix=None)
+    want, tol = reference(c, q, k, v, [n], [n], dout)
+    # scores up to about 400 / 8: fp32 products are off by up to 64 * 2^-24 of the sum of magnitudes, 2e-4 in the exponent at most
+    assert bool(((out.double() - want["out"]).abs() <= tol["out"] + 4e-4 * want["out"].abs() + 1e-3 * tol["out"]).all())
+    assert bool(((lse.double() - want["lse"]).abs() <= 1e-3).all())
+
+
 def test_last_row_is_the_decode_step(rl, cuda_device):
     """The last query of a prompt sees what the cache retains: prompt attention, paged decode and the mixed call agree."""
     import paper_2510_08525_b200.harness as hz
@@ -319,6 +361,10 @@ def test_refusals(rl, cuda_device):
     refused(0, q, k[:0], v[:0], qs, None, None, out, lse)
     with pytest.raises(ValueError):
         rl.rlkv_prompt_attention(p.h, 0, q, k, v, qs.long(), None, None, out, lse)
+    with pytest.raises(ValueError):
+        rl.rlkv_prompt_attention(p.h, 0, q, k, v, qs.cpu(), None, None, out, lse)        # read on the device
+    with pytest.raises(ValueError):
+        rl.rlkv_prompt_attention(p.h, 0, q.cpu(), k, v, qs, None, None, out, lse)
     with pytest.raises(ValueError):
         rl.rlkv_prompt_attention(p.h, 0, q, k, v, qs, starts([1, 2], dev), None, out, lse)
     with pytest.raises(ValueError):

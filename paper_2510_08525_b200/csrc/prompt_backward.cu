@@ -130,19 +130,19 @@ __device__ __forceinline__ void scores(uint32_t d, uint32_t a_smem, uint32_t b_s
         commit(smem_u32(bar));
     }
 }
-// d (128 x D) += A.B, over 128 tokens: A is bf16 in tensor memory, the second 64 tokens' columns at `second`, B a tile.
+// d (128 x D) += A.B over 64 tokens: two runs of 32, 64 tokens apart in the tile B and `apart` columns in A, which is bf16 in
+// tensor memory.
 template <int D>
-__device__ __forceinline__ void gradient(uint32_t d, uint32_t a_tmem, int second, uint32_t b_smem, bool add)
+__device__ __forceinline__ void gradient_half(uint32_t d, uint32_t a_tmem, int apart, uint32_t b_smem, bool add)
 {
     const uint64_t y = smem_desc(b_smem, kBlock);
     if (elect_one()) {
 #pragma unroll
-        for (int i = 0; i < kTok / 16; ++i)
-            mma_ts(d, a_tmem + (i < 4 ? i * 8 : second + (i - 4) * 8), y + (i * 2048 >> 4), instr_desc(kTok, D, true), add || i > 0);
+        for (int i = 0; i < 4; ++i)
+            mma_ts(d, a_tmem + i / 2 * apart + i % 2 * 8, y + ((i / 2 * 64 + i % 2 * 16) * 128 >> 4), instr_desc(kTok, D, true), add || i > 0);
     }
 }
-
-// The same for an A of 32-token blocks, 32 columns apart: 16 columns of rounded values and, `in_two`, 16 more of what the
+// d (128 x D) += A.B over a tile's 128 tokens, A in 32-token blocks 32 columns apart: 16 columns of rounded values and, `in_two`, 16 more of what the
 // rounding left.
 template <int D>
 __device__ __forceinline__ void gradient_blocks(uint32_t d, uint32_t a_tmem, uint32_t b_smem, bool in_two, bool add)
@@ -176,7 +176,7 @@ struct Keys {
 };
 
 struct KeysShared {
-    uint64_t kv_full, full[4], empty[4], ready[4], s_full, p_full, dp_full, ds_full, done, drain;
+    uint64_t kv_full, full[4], empty[4], ready[4], s_full, p_full[2], dp_full, ds_full, done, drain;
     uint32_t tmem;
     int abort, valid;
     int k0, rows, j0, q0, qn, off, prefix, u0, n_u;  // the CTA's keys; first query tile that sees them, and how many
@@ -239,7 +239,8 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 mbar_init(smem_u32(&sh.ready[i]), 1);
             }
             mbar_init(smem_u32(&sh.s_full), 1);
-            mbar_init(smem_u32(&sh.p_full), 8);
+            mbar_init(smem_u32(&sh.p_full[0]), 8);
+            mbar_init(smem_u32(&sh.p_full[1]), 8);
             mbar_init(smem_u32(&sh.dp_full), 1);
             mbar_init(smem_u32(&sh.ds_full), 8);
             mbar_init(smem_u32(&sh.done), 1);
@@ -292,35 +293,34 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             for (int c = 0; c < 64; ++c) asm volatile("" : "+f"(s[c]));  // nothing of it is used before the wait
             finish_scores<CAP, BIAS>(cap, sl2, slope2, p0 - j, 1, mine, s, f);
             const float2 factor = CAP || BIAS ? make_float2(1.f, 1.f) : make_float2(sl2, sl2);
-#pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                const float4 x = minus_lse[c / 4];
-                const float2 y = fma2(make_float2(s[c], s[c + 1]), factor, make_float2(x.x, x.y));
-                const float2 z = fma2(make_float2(s[c + 2], s[c + 3]), factor, make_float2(x.z, x.w));
-                s[c] = ex2(y.x);
-                s[c + 1] = ex2(y.y);
-                s[c + 2] = ex2(z.x);
-                s[c + 3] = ex2(z.y);
-            }
-            if (!plain) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t see = range_bits(lo - p0 - h * 32, hi - p0 - h * 32);
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) s[h * 32 + c] = see >> c & 1 ? s[h * 32 + c] : 0.f;
-                }
-            }
+            // 32 queries at a time, so that dV starts on the first
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                float* p = s + h * 32;
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) {
+                    const float4 x = minus_lse[h * 8 + c / 4];
+                    const float2 y = fma2(make_float2(p[c], p[c + 1]), factor, make_float2(x.x, x.y));
+                    const float2 z = fma2(make_float2(p[c + 2], p[c + 3]), factor, make_float2(x.z, x.w));
+                    p[c] = ex2(y.x);
+                    p[c + 1] = ex2(y.y);
+                    p[c + 2] = ex2(z.x);
+                    p[c + 3] = ex2(z.y);
+                }
+                if (!plain) {
+                    const uint32_t see = range_bits(lo - p0 - h * 32, hi - p0 - h * 32);
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) p[c] = see >> c & 1 ? p[c] : 0.f;
+                }
                 uint32_t packed[16];
 #pragma unroll
-                for (int c = 0; c < 16; ++c) packed[c] = bf16x2(s[h * 32 + 2 * c], s[h * 32 + 2 * c + 1]);
+                for (int c = 0; c < 16; ++c) packed[c] = bf16x2(p[2 * c], p[2 * c + 1]);
                 tmem_st16(mine_s + h * 16, packed);  // (over this warpgroup's own columns of S)
+                wait_st();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.p_full[h]));
             }
-            wait_st();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh.p_full));
             ok = wait(smem_u32(&sh.dp_full), n & 1, abort_flag, a.status, kPromptWaitProduct);
             if (!ok) break;
             fence_after();
@@ -415,10 +415,13 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 scores<D>(dP, v_smem, q_at(0) + F::kTile, &sh.dp_full);
             }
             for (int n = 0; ok && n < steps; ++n) {
-                ok = wait_warp(smem_u32(&sh.p_full), n & 1, abort_flag, a.status, kPromptWaitSoftmax);
+                for (int h = 0; h < 2; ++h) {
+                    ok = wait_warp(smem_u32(&sh.p_full[h]), n & 1, abort_flag, a.status, kPromptWaitSoftmax);
+                    if (!ok) break;
+                    fence_after();
+                    gradient_half<D>(dV, tmem + h * 16, 64, q_at(n) + F::kTile + h * 32 * 128, n > 0 || h > 0);
+                }
                 if (!ok) break;
-                fence_after();
-                gradient<D>(dV, tmem, 64, q_at(n) + F::kTile, n > 0);
                 const bool more = n + 1 < steps;
                 if (more) {
                     ok = loaded(n + 1);
@@ -428,7 +431,8 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 ok = wait_warp(smem_u32(&sh.ds_full), n & 1, abort_flag, a.status, kPromptWaitSoftmax);
                 if (!ok) break;
                 fence_after();
-                gradient<D>(dK, dP, 64, q_at(n), n > 0);
+                gradient_half<D>(dK, dP, 64, q_at(n), n > 0);
+                gradient_half<D>(dK, dP + 16, 64, q_at(n) + 32 * 128, true);
                 signal(&sh.empty[n % F::kStages]);
                 if (more) scores<D>(dP, v_smem, q_at(n + 1) + F::kTile, &sh.dp_full);
             }

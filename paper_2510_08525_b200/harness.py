@@ -149,6 +149,29 @@ class PagedCache:
     def prefill(self, layer, slot, k, v):
         rl.rlkv_paged_prefill(self.handle, layer, slot, k, v, k.shape[0])
 
+    def set_rotary(self, table, rot_dim, interleaved=False):
+        """table: fp32 [positions][rot_dim / 2][2] (rotary_table); it is kept alive with the cache."""
+        rl.rlkv_paged_set_rotary(self.handle, table, table.shape[0], rot_dim, interleaved)
+        self._rotary = table
+
+    def append_rotated(self, layer, slots, q, k, v):
+        """Appends the keys rotated by their position; returns the rotated queries."""
+        q_out = torch.empty((len(slots), self.q_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
+        rl.rlkv_paged_append_rotated(self.handle, layer, slots, q, k, v, q_out)
+        return q_out
+
+    def prefill_rotated(self, layer, slot, q, k, v):
+        """The same for a prompt; returns the rotated queries and keys, for PromptAttention."""
+        q_out = torch.empty((q.shape[0], self.q_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
+        k_out = torch.empty((k.shape[0], self.kv_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
+        rl.rlkv_paged_prefill_rotated(self.handle, layer, slot, q, k, v, k.shape[0], q_out, k_out)
+        return q_out, k_out
+
+    def set_scores(self, softcap=0.0, slopes=None):
+        if slopes is not None and np.size(slopes) != self.layers * self.q_heads:
+            raise ValueError("slopes must have layers*q_heads entries")
+        rl.rlkv_paged_set_scores(self.handle, softcap, slopes)
+
     def decode(self, layer, slots, q, out=None):
         if out is None:
             out = torch.empty((len(slots), self.q_heads, self.head_dim), dtype=torch.float32, device=self.device)
@@ -170,6 +193,47 @@ class PagedCache:
 
     def status(self) -> int:
         return rl.rlkv_paged_kernel_status(self.handle)
+
+
+def rotary_table(positions, rot_dim, base=10000.0, device="cuda:0"):
+    """cos and sin of position * base^(-2j / rot_dim), for PagedCache.set_rotary."""
+    table = torch.empty((positions, rot_dim // 2, 2), dtype=torch.float32, device=device)
+    rl.rlkv_rotary_table(base ** (-np.arange(0, rot_dim, 2) / rot_dim), positions, table)
+    return table
+
+
+class PromptAttention:
+    """Owns an rlkv_prompt handle: attention over packed prompts, forward and backward."""
+
+    def __init__(self, layers, kv_heads, q_heads, head_dim, max_tokens, head_is_full, sink, window, softcap=0.0, slopes=None,
+                 device="cuda:0"):
+        self.device = torch.device(device)
+        with torch.cuda.device(self.device):
+            self.handle = rl.rlkv_prompt_create(layers, kv_heads, q_heads, head_dim, max_tokens, head_is_full, sink, window, softcap,
+                                                slopes)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            rl.rlkv_prompt_destroy(self.handle)
+            self.handle = None
+
+    __del__ = close
+
+    def forward(self, layer, q, k, v, q_starts, k_starts=None, prefix=None):
+        """Returns out and lse; rows that belong to no document are zero."""
+        out = torch.zeros(q.shape, dtype=torch.bfloat16, device=self.device)
+        lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=self.device)
+        rl.rlkv_prompt_attention(self.handle, layer, q, k, v, q_starts, k_starts, prefix, out, lse)
+        return out, lse
+
+    def backward(self, layer, q, k, v, out, lse, dout, q_starts, k_starts=None, prefix=None):
+        """Returns dq, dk, dv."""
+        dq, dk, dv = (torch.zeros(x.shape, dtype=torch.bfloat16, device=self.device) for x in (q, k, v))
+        rl.rlkv_prompt_attention_backward(self.handle, layer, q, k, v, q_starts, k_starts, prefix, out, lse, dout, dq, dk, dv)
+        return dq, dk, dv
+
+    def status(self) -> int:
+        return rl.rlkv_prompt_kernel_status(self.handle)
 
 
 def paged_seq_seed(w: synth.Workload, i: int) -> int:

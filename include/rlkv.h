@@ -344,7 +344,8 @@ int rlkv_paged_set_output_bf16(rlkv_paged* cache, int on);
 /* The scores of rlkv_paged_decode_attention and rlkv_paged_step from now on, for models that cap them or encode
  * positions in them:
  *     score = softcap * tanh(x / softcap) - slopes[layer][j] * (tokens from the key to the query),
- * x = q.k / sqrt(head_dim), for query head j.  softcap 0: x as it is; else 1e-3 to 1e6.  slopes: HOST float
+ * x = q.k / sqrt(head_dim), for query head j.  softcap 0: x as it is; else 1e-3 to 1000 (the cap is off by up to 2^-22 of
+ * itself: 3e-4 in a score at the largest).  slopes: HOST float
  * [layers][q_heads], magnitudes up to 1e6, copied, or NULL: no distance term.  Distances are those of the tokens,
  * whatever ring slot a compressed head keeps a key in.  Synchronous where slopes are given (it waits for the device);
  * not during a stream capture.  A captured graph keeps the softcap of its capture and reads the slopes set last.

@@ -115,7 +115,7 @@ int rlkv_prompt_create(rlkv_prompt** out, int layers, int kv_heads, int q_heads,
         q_heads % kv_heads != 0 || q_heads / kv_heads > kMaxGroup || (head_dim != 64 && head_dim != 128) || max_tokens < 1 ||
         max_tokens > kMaxPromptTokens || sink < 0 || window < 1 || (long long)sink + window > (1 << 24))
         return RLKV_EINVAL;
-    if (!(softcap >= 0.f) || (softcap != 0.f && (softcap < 1e-3f || softcap > 1e6f))) return RLKV_EINVAL;
+    if (!(softcap >= 0.f) || (softcap != 0.f && (softcap < 1e-3f || softcap > 1e3f))) return RLKV_EINVAL;
     const size_t count = (size_t)layers * q_heads;
     bool biased = false;
     if (slopes)

@@ -333,7 +333,7 @@ def test_refusals(rl, cuda_device):
     dev = cuda_device
     ok = dict(layers=1, kv_heads=2, q_heads=8, head_dim=128, max_tokens=64, head_is_full=[1, 0], sink=4, window=60, softcap=0.0, slopes=None)
     for bad in (dict(layers=0), dict(kv_heads=3), dict(q_heads=18), dict(head_dim=96), dict(max_tokens=0), dict(max_tokens=1 << 25),
-                dict(sink=-1), dict(window=0), dict(softcap=-1.0), dict(softcap=float("nan")), dict(softcap=1e-5),
+                dict(sink=-1), dict(window=0), dict(softcap=-1.0), dict(softcap=float("nan")), dict(softcap=1e-5), dict(softcap=2e3),
                 dict(slopes=np.full(8, np.nan, np.float32)), dict(slopes=np.full(8, 1e7, np.float32))):
         kw = {**ok, **bad}
         if "kv_heads" in bad:

@@ -137,7 +137,7 @@ def test_large_products_stay_capped(rl, hz, cuda_device):
 def test_refusals(rl, hz, cuda_device):
     cache = hz.PagedCache(1, 2, 8, 128, 2, 8, 200, [1, 0], 4, 60, device=cuda_device)
     ok = np.full(8, 0.5, np.float32)
-    for cap, slopes in ((-1.0, None), (float("nan"), None), (float("inf"), None), (1e-4, None), (1e7, None),
+    for cap, slopes in ((-1.0, None), (float("nan"), None), (float("inf"), None), (1e-4, None), (1e7, None), (1001.0, None),
                         (0.0, np.full(8, np.nan, np.float32)), (0.0, np.full(8, np.inf, np.float32)), (0.0, np.full(8, -2e6, np.float32))):
         with pytest.raises(rl.RlkvError) as e:
             rl.rlkv_paged_set_scores(cache.handle, cap, slopes)

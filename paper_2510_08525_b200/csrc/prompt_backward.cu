@@ -195,6 +195,7 @@ prompt_keys_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     using F = Keys<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     float* stats = reinterpret_cast<float*>(smem + F::kStats);  // per stage: -lse of 128 queries, then their -D
+    static_assert(sizeof(KeysShared) <= 1024 && F::kSmem <= kMaxDynamicSmem, "shared memory");
     KeysShared& sh = *reinterpret_cast<KeysShared*>(smem + F::kStats + F::kStages * kTok * 8);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     // `split` CTAs, a cluster, share the query heads of a KV head
@@ -540,6 +541,7 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
 {
     using F = RowsK<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
+    static_assert(sizeof(RowsShared) <= 1024 && F::kSmem <= kMaxDynamicSmem, "shared memory");
     RowsShared& sh = *reinterpret_cast<RowsShared*>(smem + (6 + F::kValues) * F::kTile);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     volatile int* abort_flag = &sh.abort;

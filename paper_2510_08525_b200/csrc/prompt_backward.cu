@@ -97,7 +97,7 @@ __device__ __forceinline__ void finish_scores(const Cap& cap, float sl2, float s
     }
     if constexpr (BIAS) {
 #pragma unroll
-        for (int c = 0; c < N; ++c) s[c] = fmaf(-slope2, fabsf((float)(dist0 + step * c)), CAP ? s[c] : s[c] * sl2);
+        for (int c = 0; c < N; ++c) s[c] = fmaf(-slope2, fabsf((float)dist0 + (float)(step * c)), CAP ? s[c] : s[c] * sl2);
     }
 }
 

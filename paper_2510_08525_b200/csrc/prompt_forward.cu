@@ -185,13 +185,24 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
                     cap.apply(s, mine);
                 }
                 if (BIAS) {
-                    if (causal_past) {  // -slope (pos - start - c): linear in the column
-                        const float t0 = slope2 * (float)(start - pos);
+                    // From the distance itself, a whole number and exact: slope * (start - pos) + slope * c would round at the size
+                    // of its terms and lose the score of the keys next to the query where slopes are steep.
+                    const float far = (float)(pos - start);
+                    if (causal_past) {
+                        float2 d[4];
 #pragma unroll
-                        for (int c = 0; c < kRows; ++c) s[c] = fmaf(slope2, (float)c, CAP ? s[c] + t0 : fmaf(s[c], sl2, t0));
+                        for (int c = 0; c < 8; c += 2) d[c / 2] = make_float2((float)c - far, (float)(c + 1) - far);
+#pragma unroll
+                        for (int c = 0; c < kRows; c += 2) {
+                            const float2 x = CAP ? make_float2(s[c], s[c + 1]) : mul2(make_float2(s[c], s[c + 1]), make_float2(sl2, sl2));
+                            const float2 y = fma2(make_float2(slope2, slope2), d[c / 2 & 3], x);
+                            s[c] = y.x;
+                            s[c + 1] = y.y;
+                            d[c / 2 & 3] = add2(d[c / 2 & 3], make_float2(8.f, 8.f));
+                        }
                     } else {
 #pragma unroll
-                        for (int c = 0; c < kRows; ++c) s[c] = fmaf(-slope2, fabsf((float)(pos - start - c)), CAP ? s[c] : s[c] * sl2);
+                        for (int c = 0; c < kRows; ++c) s[c] = fmaf(-slope2, fabsf(far - (float)c), CAP ? s[c] : s[c] * sl2);
                     }
                 }
                 if (!plain) {

@@ -218,6 +218,20 @@ def test_large_scores(rl, cuda_device):
     assert bool(((lse.double() - want["lse"]).abs() <= 1e-3).all())
 
 
+@pytest.mark.parametrize("D,cap,more", [(64, 0.0, 0), (128, 30.0, 0), (64, 0.0, 127), (128, 0.0, 255), (128, 30.0, 127)])
+def test_steep_slopes(rl, cuda_device, D, cap, more):
+    """Slopes up to the largest: the scores of the keys next to the query keep their digits, whatever the far ones come to.
+    (With 127 keys before the first query its own key is the last of a tile that lies wholly behind the queries.)"""
+    dev, Hkv, Hq, n = cuda_device, 2, 8, 700
+    slopes = np.float32([1e6, 1e3, 37, 3, 1e6, 1e4, 100, 0.7])
+    c = dict(mask=[1, 0], sink=4, window=200, cap=cap, slopes=slopes, prefix=None)
+    p = Prompt(rl, 1, Hkv, Hq, D, n, c["mask"], 4, 200, cap, slopes)
+    q, k, v, dout = inputs(n, n + more, Hq, Hkv, D, 29, dev)
+    got = call(rl, p.h, 0, q, k, v, starts([n], dev), starts([n + more], dev), None, dout)
+    want, tol = reference(c, q, k, v, [n], [n + more], dout)
+    check(got, want, tol, n, n + more)
+
+
 def test_last_row_is_the_decode_step(rl, cuda_device):
     """The last query of a prompt sees what the cache retains: prompt attention, paged decode and the mixed call agree."""
     import paper_2510_08525_b200.harness as hz

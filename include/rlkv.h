@@ -347,8 +347,10 @@ int rlkv_paged_set_output_bf16(rlkv_paged* cache, int on);
  * x = q.k / sqrt(head_dim), for query head j.  softcap 0: x as it is; else 1e-3 to 1000 (the cap is off by up to 2^-22 of
  * itself: 3e-4 in a score at the largest).  slopes: HOST float
  * [layers][q_heads], magnitudes up to 1e6, copied, or NULL: no distance term.  Distances are those of the tokens,
- * whatever ring slot a compressed head keeps a key in.  Synchronous where slopes are given (it waits for the device);
- * not during a stream capture.  A captured graph keeps the softcap of its capture and reads the slopes set last.
+ * whatever ring slot a compressed head keeps a key in.  Synchronous where slopes are or have been given (it waits for the
+ * device); not during a stream capture.  A captured graph keeps its capture's softcap, and its capture's lack of a distance
+ * term; one with a distance term reads the slopes set last (none: zeros).  Scores are fp32: a weight is off by about 2^-23 of
+ * the magnitude of its score.
  * RLKV_EINVAL (nothing changed) for other values. */
 int rlkv_paged_set_scores(rlkv_paged* cache, float softcap, const float* slopes);
 int rlkv_paged_length(const rlkv_paged* cache, int layer, int slot, int* len_out);
@@ -388,6 +390,7 @@ int rlkv_debug_paged_schedule(const int* lens, int n, int n_full, int n_comp, in
  * what a compressed head would retain when token pos is the newest.  Over the visible keys
  *     score = softcap * tanh(x / softcap) - slopes[layer][j] * |pos - position of the key|,  x = q.k / sqrt(head_dim),
  *     out = softmax(score) . V,  lse = log sum exp(score).
+ * Scores, lse and their differences are fp32: a weight is off by about 2^-22 of the magnitude of its score and of lse.
  * A query that sees no key gets out = 0 and lse = -infinity.  Tokens behind the last document belong to none: their
  * rows of out, lse, dq, dk, dv are left as they are, and whatever their rows of q, k, v, dout hold has no effect on
  * others; nor do the rows of one document on another's.  Values of a document's own rows are assumed finite.

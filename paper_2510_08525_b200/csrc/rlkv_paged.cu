@@ -67,6 +67,7 @@ struct rlkv_paged {
     int rotary_rows, rotary_dim, rotary_interleaved;
     float softcap;                // rlkv_paged_set_scores: 0 no cap
     bool biased;                  // and whether scores are lowered by distance (slopes at off_slopes)
+    bool has_slopes;              // whether slopes have ever been written
 };
 
 namespace {
@@ -291,7 +292,7 @@ static int paged_create(rlkv_paged** out, int layers, int kv_heads, int q_heads,
     p->max_seqs = max_seqs; p->n_pages = n_pages; p->sink = sink; p->window = window; p->max_seq_len = max_seq_len;
     p->claims[0] = p->claims[1] = 0; p->launches = 0; p->dev_base = nullptr; p->owns_buffer = false; p->out_bf16 = 0;
     p->step_mode = 0;
-    p->softcap = 0.f; p->biased = false;
+    p->softcap = 0.f; p->biased = p->has_slopes = false;
     p->rotary = nullptr; p->rotary_rows = p->rotary_dim = p->rotary_interleaved = 0;
     p->fp8 = fp8;
     if (fp8) {
@@ -888,9 +889,14 @@ int rlkv_paged_set_scores(rlkv_paged* p, float softcap, const float* slopes)
         }
     DeviceGuard g(p->device);
     if (!g.ok) return RLKV_ECUDA;
-    if (biased) {
+    // (a captured launch with a distance term reads them even after slopes that are all zero, or none, were set)
+    if (biased || p->has_slopes) {
         RLKV_CUDA(cudaDeviceSynchronize());  // launches in flight read the slopes they were given
-        RLKV_CUDA(cudaMemcpy(p->dev_base + p->off_slopes, slopes, count * sizeof(float), cudaMemcpyHostToDevice));
+        void* at = p->dev_base + p->off_slopes;
+        if (biased) RLKV_CUDA(cudaMemcpy(at, slopes, count * sizeof(float), cudaMemcpyHostToDevice));
+        else RLKV_CUDA(cudaMemset(at, 0, count * sizeof(float)));
+        RLKV_CUDA(cudaDeviceSynchronize());  // a copy from pageable memory returns before its last piece has landed
+        p->has_slopes = true;
     }
     p->softcap = softcap;
     p->biased = biased;

@@ -143,3 +143,28 @@ def test_refusals(rl, hz, cuda_device):
             rl.rlkv_paged_set_scores(cache.handle, cap, slopes)
         assert e.value.code == rl.RLKV_EINVAL
     rl.rlkv_paged_set_scores(cache.handle, 1.0, ok)
+
+
+def test_captured_call_reads_the_slopes_set_last(rl, hz, cuda_device):
+    dev = cuda_device
+    cache = hz.PagedCache(1, 2, 8, 128, 1, 8, 300, [1, 0], 4, 60, device=dev)
+    s = cache.open_seq()
+    cache.prefill(0, s, rand_bf16((200, 2, 128), 1).to(dev), rand_bf16((200, 2, 128), 2).to(dev))
+    q, out = rand_bf16((1, 8, 128), 3).to(dev), torch.empty((1, 8, 128), device=dev)
+    zeros, some, other = np.zeros(8, np.float32), np.full(8, 0.25, np.float32), np.linspace(0.1, 2, 8).astype(np.float32)
+    cache.set_scores(20.0, some)
+    cache.decode(0, [s], q, out)
+    want = {}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.decode(0, [s], q, out)
+    for name, slopes in (("some", some), ("other", other), ("zeros", zeros), ("none", None), ("again", some)):
+        cache.set_scores(20.0, slopes)
+        want[name] = cache.decode(0, [s], q).clone()
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        # zeros: the launch without a distance term adds none, the captured one adds 0 * distance
+        assert torch.equal(out, want[name]), name
+    assert torch.equal(want["some"], want["again"]) and torch.equal(want["zeros"], want["none"])
+    assert not torch.equal(want["some"], want["none"]) and not torch.equal(want["some"], want["other"])

@@ -128,14 +128,16 @@ def _ptr(x) -> int:
     return x.data_ptr()
 
 
-def _stream(s) -> int:
+def _stream(s, of=None) -> int:
+    """A stream's handle; None: the current stream, of the GPU that holds the tensor `of` where one is given."""
     if s is None:
         import torch
+        device = torch.cuda.current_device() if of is None or isinstance(of, int) else of.get_device()
         # the raw handle: building the Stream object takes several microseconds, as long as a small call
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is not None:
-            return raw(torch.cuda.current_device())
-        return torch.cuda.current_stream().cuda_stream
+            return raw(device)
+        return torch.cuda.current_stream(device).cuda_stream
     if isinstance(s, int):
         return s
     return s.cuda_stream
@@ -439,18 +441,39 @@ def _on_device(x) -> bool:
     return not isinstance(x, np.ndarray) and x.is_cuda
 
 
-def _rows(x):
-    """(address, elements from token to token) of a [tokens][heads][head_dim] tensor, which may be a slice of a
-    wider projection; an address alone stands for contiguous tokens."""
+def _rows(x, least=1):
+    """(address, elements from token to token) of a bf16 [tokens][heads][head_dim] tensor of at least `least` tokens, which
+    may be a slice of a wider projection; an address alone stands for contiguous tokens."""
     if x is None or isinstance(x, int):
         return x or 0, 0
     if not _on_device(x):
         raise ValueError("a tensor in device memory is wanted")
     n, _, dim = x.shape  # ValueError where it has other than three dimensions
     token, head, one = x.stride()
+    if x.element_size() != 2 or not x.is_floating_point():
+        raise ValueError("rows are bf16")
+    if n < least:
+        raise ValueError(f"{n} tokens where the call names {least}")
     if one != 1 or head != dim:
         raise ValueError("tokens must be [tokens][heads][head_dim] with contiguous heads")
-    return x.data_ptr(), token if n > 1 else 0
+    if n <= 1:
+        return x.data_ptr(), 0
+    if token == 0:  # an expanded tensor; 0 would stand for contiguous tokens
+        raise ValueError("tokens share their memory")
+    return x.data_ptr(), token
+
+
+def _room(x, least, size=2):
+    """Address of a contiguous tensor in device memory of `least` elements or more, `size` bytes each; or the address itself."""
+    if x is None or isinstance(x, int):
+        return x or 0
+    if not _on_device(x) or x.element_size() != size or x.numel() < least:
+        raise RlkvError(RLKV_EINVAL, f"a tensor in device memory of {least} elements of {size} bytes is wanted")
+    return _ptr(x)
+
+
+def _size(x) -> int:
+    return 0 if x is None or isinstance(x, int) else x.numel()
 
 
 def rlkv_paged_set_scores(cache, softcap, slopes=None) -> None:
@@ -461,22 +484,28 @@ def rlkv_paged_set_scores(cache, softcap, slopes=None) -> None:
 
 def rlkv_rotary_table(inv_freq, positions, table, stream=None) -> None:
     f = np.ascontiguousarray(inv_freq, dtype=np.float64)
+    if _size(table) and table.numel() < 2 * f.size * positions:
+        raise ValueError("the table holds fewer rows")
     _check(lib.rlkv_rotary_table(f.ctypes.data, 2 * f.size, positions, _ptr(table), _stream(stream)))
 
 
 def rlkv_paged_set_rotary(cache, table, positions, rot_dim, interleaved=False) -> None:
+    if _size(table) and (table.element_size() != 4 or table.numel() < min(rot_dim, 128) * positions):
+        raise ValueError("the table is fp32 [positions][rot_dim / 2][2]")
     _check(lib.rlkv_paged_set_rotary(cache, _ptr(table), positions, rot_dim, int(bool(interleaved))))
 
 
 def rlkv_paged_append_rotated(cache, layer, slots, q, k, v, q_out, stream=None) -> None:
     s = np.ascontiguousarray(slots, dtype=np.int32)
-    _check(lib.rlkv_paged_append_rotated(cache, layer, s.ctypes.data, s.size, *_rows(q), *_rows(k), *_rows(v), _ptr(q_out),
-                                         _stream(stream)))
+    n = s.size
+    _check(lib.rlkv_paged_append_rotated(cache, layer, s.ctypes.data, n, *_rows(q, n), *_rows(k, n), *_rows(v, n),
+                                         _room(q_out, _size(q)), _stream(stream, k)))
 
 
 def rlkv_paged_prefill_rotated(cache, layer, slot, q, k, v, n_tokens, q_out, k_out=None, stream=None) -> None:
-    _check(lib.rlkv_paged_prefill_rotated(cache, layer, slot, *_rows(q), *_rows(k), *_rows(v), n_tokens, _ptr(q_out),
-                                          _ptr(k_out), _stream(stream)))
+    n = n_tokens
+    _check(lib.rlkv_paged_prefill_rotated(cache, layer, slot, *_rows(q, n), *_rows(k, n), *_rows(v, n), n, _room(q_out, _size(q)),
+                                          _room(k_out, _size(k)), _stream(stream, k)))
 
 
 def rlkv_paged_decode_attention(cache, layer, slots, q, out, stream=None) -> None:
@@ -548,26 +577,31 @@ def rlkv_prompt_destroy(prompt) -> None:
 
 
 def _prompt_args(q, k, v, q_starts, k_starts, prefix):
-    if any(x is not None and not _on_device(x) for x in (q_starts, k_starts, prefix)):
+    ints = [x for x in (q_starts, k_starts, prefix) if x is not None]
+    if not all(map(_on_device, ints)):
         raise ValueError("q_starts, k_starts and prefix are read on the device")
     n_docs = q_starts.numel() - 1
     if k_starts is not None and k_starts.numel() != n_docs + 1 or prefix is not None and prefix.numel() != n_docs:
         raise ValueError("k_starts must have as many entries as q_starts, prefix one less")
-    if any(x is not None and x.element_size() != 4 for x in (q_starts, k_starts, prefix)):
+    if any(x.element_size() != 4 or x.is_floating_point() for x in ints):
         raise ValueError("q_starts, k_starts and prefix are int32")
-    return (*_rows(q), *_rows(k), *_rows(v), q.shape[0], k.shape[0], _ptr(q_starts), _ptr(k_starts), n_docs, _ptr(prefix))
+    if k.shape != v.shape:
+        raise ValueError("k and v must have the same shape")
+    return (*_rows(q, 0), *_rows(k, 0), *_rows(v, 0), q.shape[0], k.shape[0], _ptr(q_starts), _ptr(k_starts), n_docs, _ptr(prefix))
 
 
 def rlkv_prompt_attention(prompt, layer, q, k, v, q_starts, k_starts, prefix, out, lse, stream=None) -> None:
     """q, k, v: [tokens][heads][head_dim], possibly slices of one projection's output; q_starts, k_starts, prefix: int32."""
-    _check(lib.rlkv_prompt_attention(prompt, layer, *_prompt_args(q, k, v, q_starts, k_starts, prefix), _ptr(out), _ptr(lse),
-                                     _stream(stream)))
+    _check(lib.rlkv_prompt_attention(prompt, layer, *_prompt_args(q, k, v, q_starts, k_starts, prefix), _room(out, q.numel()),
+                                     _room(lse, q.shape[0] * q.shape[1], 4), _stream(stream, q)))
 
 
 def rlkv_prompt_attention_backward(prompt, layer, q, k, v, q_starts, k_starts, prefix, out, lse, dout, dq, dk, dv,
                                    stream=None) -> None:
-    _check(lib.rlkv_prompt_attention_backward(prompt, layer, *_prompt_args(q, k, v, q_starts, k_starts, prefix), _ptr(out),
-                                              _ptr(lse), _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv), _stream(stream)))
+    n_q, n_k = q.numel(), k.numel()
+    _check(lib.rlkv_prompt_attention_backward(prompt, layer, *_prompt_args(q, k, v, q_starts, k_starts, prefix), _room(out, n_q),
+                                              _room(lse, q.shape[0] * q.shape[1], 4), _room(dout, n_q), _room(dq, n_q),
+                                              _room(dk, n_k), _room(dv, n_k), _stream(stream, q)))
 
 
 def rlkv_prompt_kernel_status(prompt) -> int:

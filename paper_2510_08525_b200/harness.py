@@ -150,18 +150,22 @@ class PagedCache:
         rl.rlkv_paged_prefill(self.handle, layer, slot, k, v, k.shape[0])
 
     def set_rotary(self, table, rot_dim, interleaved=False):
-        """table: fp32 [positions][rot_dim / 2][2] (rotary_table); it is kept alive with the cache."""
-        rl.rlkv_paged_set_rotary(self.handle, table, table.shape[0], rot_dim, interleaved)
+        """table: fp32 [positions][rot_dim / 2][2] (rotary_table); it is kept alive with the cache.  None: no rotation."""
+        if table is not None and (table.dtype != torch.float32 or tuple(table.shape[1:]) != (rot_dim // 2, 2)):
+            raise ValueError("the table is fp32 [positions][rot_dim / 2][2]")
+        rl.rlkv_paged_set_rotary(self.handle, table, 0 if table is None else table.shape[0], rot_dim, interleaved)
         self._rotary = table
 
     def append_rotated(self, layer, slots, q, k, v):
         """Appends the keys rotated by their position; returns the rotated queries."""
+        _check_rows(self, q, k, v)
         q_out = torch.empty((len(slots), self.q_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
         rl.rlkv_paged_append_rotated(self.handle, layer, slots, q, k, v, q_out)
         return q_out
 
     def prefill_rotated(self, layer, slot, q, k, v):
         """The same for a prompt; returns the rotated queries and keys, for PromptAttention."""
+        _check_rows(self, q, k, v)
         q_out = torch.empty((q.shape[0], self.q_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
         k_out = torch.empty((k.shape[0], self.kv_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
         rl.rlkv_paged_prefill_rotated(self.handle, layer, slot, q, k, v, k.shape[0], q_out, k_out)
@@ -195,6 +199,15 @@ class PagedCache:
         return rl.rlkv_paged_kernel_status(self.handle)
 
 
+def _check_rows(owner, q, k, v):
+    """The handle knows its heads, a call's addresses do not: rows of fewer would be read past their end."""
+    for x, heads in ((q, owner.q_heads), (k, owner.kv_heads), (v, owner.kv_heads)):
+        if x.dtype != torch.bfloat16 or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != owner.head_dim:
+            raise ValueError(f"rows must be bf16 [tokens][{heads}][{owner.head_dim}]")
+        if not x.is_cuda or owner.device.index not in (None, x.get_device()):
+            raise ValueError(f"rows must be on {owner.device}")
+
+
 def rotary_table(positions, rot_dim, base=10000.0, device="cuda:0"):
     """cos and sin of position * base^(-2j / rot_dim), for PagedCache.set_rotary."""
     table = torch.empty((positions, rot_dim // 2, 2), dtype=torch.float32, device=device)
@@ -208,6 +221,7 @@ class PromptAttention:
     def __init__(self, layers, kv_heads, q_heads, head_dim, max_tokens, head_is_full, sink, window, softcap=0.0, slopes=None,
                  device="cuda:0"):
         self.device = torch.device(device)
+        self.kv_heads, self.q_heads, self.head_dim = kv_heads, q_heads, head_dim
         with torch.cuda.device(self.device):
             self.handle = rl.rlkv_prompt_create(layers, kv_heads, q_heads, head_dim, max_tokens, head_is_full, sink, window, softcap,
                                                 slopes)
@@ -221,6 +235,7 @@ class PromptAttention:
 
     def forward(self, layer, q, k, v, q_starts, k_starts=None, prefix=None):
         """Returns out and lse; rows that belong to no document are zero."""
+        _check_rows(self, q, k, v)
         out = torch.zeros(q.shape, dtype=torch.bfloat16, device=self.device)
         lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=self.device)
         rl.rlkv_prompt_attention(self.handle, layer, q, k, v, q_starts, k_starts, prefix, out, lse)
@@ -228,6 +243,7 @@ class PromptAttention:
 
     def backward(self, layer, q, k, v, out, lse, dout, q_starts, k_starts=None, prefix=None):
         """Returns dq, dk, dv."""
+        _check_rows(self, q, k, v)
         dq, dk, dv = (torch.zeros(x.shape, dtype=torch.bfloat16, device=self.device) for x in (q, k, v))
         rl.rlkv_prompt_attention_backward(self.handle, layer, q, k, v, q_starts, k_starts, prefix, out, lse, dout, dq, dk, dv)
         return dq, dk, dv

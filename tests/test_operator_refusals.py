@@ -40,3 +40,72 @@ def test_prompt_calls_refuse_without_a_device(binding):
         b.rlkv_prompt_create(1, 2, 8, 128, 10, m, 4, 60, 0.0, np.ones(7))
     assert lib.rlkv_prompt_attention(0, 0, 16, 0, 16, 0, 16, 0, 1, 1, 16, 0, 1, 0, 16, 16, 0) == b.RLKV_EINVAL
     assert lib.rlkv_prompt_attention_backward(0, 0, 16, 0, 16, 0, 16, 0, 1, 1, 16, 0, 1, 0, 16, 16, 16, 16, 16, 16, 0) == b.RLKV_EINVAL
+
+
+class Rows:
+    """Stands for a bf16 tensor in device memory; its address is never read."""
+
+    def __init__(self, shape, stride=None, size=2, device=0, whole=False):
+        self.shape, self.size, self.device, self.is_cuda, self.whole = shape, size, device, True, whole
+        self.strides = stride or tuple(int(np.prod(shape[i + 1:])) for i in range(len(shape)))
+
+    def stride(self):
+        return self.strides
+
+    def data_ptr(self):
+        return 4096
+
+    def numel(self):
+        return int(np.prod(self.shape))
+
+    def element_size(self):
+        return self.size
+
+    def is_floating_point(self):
+        return not self.whole
+
+    def is_contiguous(self):
+        return True
+
+    def get_device(self):
+        return self.device
+
+
+def test_rows_and_their_strides(binding):
+    b = binding
+    assert b._rows(None) == (0, 0) and b._rows(64) == (64, 0)
+    assert b._rows(Rows((5, 8, 128))) == (4096, 1024)
+    assert b._rows(Rows((5, 8, 128), (2048, 128, 1)), 5) == (4096, 2048)
+    assert b._rows(Rows((1, 8, 128), (0, 128, 1))) == (4096, 0)
+    for bad, least in ((Rows((5, 8, 128), (0, 128, 1)), 1),               # expanded: 0 would stand for contiguous tokens
+                       (Rows((5, 8, 128), (1024, 0, 1)), 1), (Rows((5, 8, 128), (1024, 1, 8)), 1), (Rows((5, 1024)), 1),
+                       (Rows((5, 8, 128), size=4), 1), (Rows((4, 8, 128)), 5), (np.zeros((5, 8, 128), np.float16), 1)):
+        with pytest.raises(ValueError):
+            b._rows(bad, least)
+    assert b._room(None, 9) == 0 and b._room(64, 9) == 64 and b._room(Rows((3, 3)), 9) == 4096
+    for bad in (Rows((2, 4)), Rows((3, 3), size=4), np.zeros(9, np.float16)):
+        with pytest.raises(b.RlkvError) as e:
+            b._room(bad, 9)
+        assert e.value.code == b.RLKV_EINVAL
+
+
+def test_calls_refuse_tensors_too_small_for_them(binding):
+    b = binding
+    q, k, starts = Rows((4, 8, 128)), Rows((4, 2, 128)), Rows((2,), size=4, whole=True)
+    for call in (lambda: b.rlkv_paged_append_rotated(0, 0, [0, 1, 2, 3, 4], q, k, k, q, stream=0),
+                 lambda: b.rlkv_paged_prefill_rotated(0, 0, 0, q, k, k, 5, q, stream=0),
+                 lambda: b.rlkv_rotary_table(np.ones(64), 5, Rows((4, 64, 2), size=4), stream=0),
+                 lambda: b.rlkv_paged_set_rotary(0, Rows((4, 64, 2), size=4), 5, 128),
+                 lambda: b.rlkv_paged_set_rotary(0, Rows((4, 64, 2)), 4, 128),
+                 lambda: b.rlkv_prompt_attention(0, 0, q, k, k, Rows((2,), size=4), None, None, q, None, 0),
+                 lambda: b.rlkv_prompt_attention(0, 0, q, k, Rows((3, 2, 128)), starts, None, None, q, None, 0)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_the_stream_is_that_of_the_tensors_gpu(binding, monkeypatch):
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 100 + device, raising=False)
+    assert binding._stream(None) == 100 and binding._stream(None, Rows((1, 1, 64), device=3)) == 103
+    assert binding._stream(None, 4096) == 100 and binding._stream(7, Rows((1, 1, 64), device=3)) == 7

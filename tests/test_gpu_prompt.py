@@ -232,6 +232,36 @@ def test_steep_slopes(rl, cuda_device, D, cap, more):
     check(got, want, tol, n, n + more)
 
 
+@pytest.mark.parametrize("D,S,W,full,cap", [(128, 0, 5, 0, 50.0), (64, 0, 5, 0, 0.0), (128, 2, 3, 0, 0.0), (64, 4, 60, 1, 0.0)])
+def test_gradients_of_queries_that_see_few_keys(rl, cuda_device, D, S, W, full, cap):
+    """Documents of one tile: the rounding of `out` does not come back in dQ, which is off by little more than its own rounding."""
+    dev, Hkv, Hq, lens = cuda_device, 2, 4, [71, 128, 5, 1, 40]
+    n = sum(lens)
+    p = Prompt(rl, 1, Hkv, Hq, D, n, [full] * 2, S, W, cap)
+    q, k, v, dout = inputs(n, n, Hq, Hkv, D, 37, dev)
+    got = call(rl, p.h, 0, q, k, v, starts(lens, dev), None, None, dout)
+    at = 0
+    for a in lens:
+        rows, i, j = slice(at, at + a), torch.arange(a, device=dev)[:, None], torch.arange(a, device=dev)[None]
+        at += a
+        see = (j <= i) & ((j < S) | (j > i - W) | bool(full))
+        for h in range(Hq):
+            qh, kh, vh, do = (x[rows, y].double() for x, y in ((q, h), (k, h // 2), (v, h // 2), (dout, h)))
+            x, dx = qh @ kh.T * D ** -0.5, 1.0
+            if cap:
+                t = torch.tanh(x / cap)
+                x, dx = cap * t, 1 - t * t
+            pr = torch.softmax(x.masked_fill(~see, -np.inf), 1)
+            ds = pr * (do @ vh.T - (do * (pr @ vh)).sum(1, keepdim=True)) * dx
+            want = ds @ kh * D ** -0.5
+            # dS is 2^-17 off as two bf16 parts and 5e-4 with its P; dP, an fp32 sum of 128 products, and the sum of P dP that
+            # takes its place in D are off by 1e-5 of what they add up, each
+            eds = 6e-4 * ds.abs() + 2e-5 * pr * (do.abs() @ vh.abs().T + (pr * (do.abs() @ vh.abs().T)).sum(1, keepdim=True))
+            tol = E * want.abs() + eds @ kh.abs() * D ** -0.5 + 1e-7
+            err = (got["dq"][rows, h].double() - want).abs()
+            assert bool((err <= tol).all()), (a, h, float((err / tol).max()))
+
+
 def test_last_row_is_the_decode_step(rl, cuda_device):
     """The last query of a prompt sees what the cache retains: prompt attention, paged decode and the mixed call agree."""
     import paper_2510_08525_b200.harness as hz

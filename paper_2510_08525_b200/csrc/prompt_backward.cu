@@ -26,7 +26,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTok = 128;            // tokens of a tile, of queries and of keys
 constexpr int kBlock = kTok * 128;  // bytes of a block of 64 elements of its rows
 constexpr int kThreads = 384;
-constexpr int kFewKeys = 2048;
+constexpr int kFewKeys = 1024;
 
 // ---- D and lse ---------------------------------------------------------------------------------------
 
@@ -589,11 +589,14 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     const int n_tiles = sh.at.n_tiles, a_end = sh.at.a_end, b0 = sh.at.b0, kn = sh.at.kn, prefix = sh.at.prefix;
     const int n_sub = sh.at.n_sub, kv_head = sh.at.kv_head;
     const bool full_head = a.full[kv_head] != 0;
-    // Where a query sees few keys, what the rounding of `out` did to D weighs as much in dQ as the rounding of dS: dS then
-    // goes into its product in two bf16 parts, and dQ is off by 2.3e-3 of its norm instead of 2.8e-3 (documents of a few
-    // hundred tokens; one rounding of the exact gradient to bf16: 1.7e-3).  With thousands of keys D is near enough (2.4e-3
-    // without) and the fourth product would cost a quarter of the kernel's time (8192 tokens: 680 -> 857 us).
-    const bool in_two = (full_head ? kn : min(kn, a.sink + a.window)) <= kFewKeys;
+    // Where queries see few keys, or slopes leave them few that matter, the rounding of dS weighs as much in dQ as that of the
+    // result: dS then goes into its product in two bf16 parts.  The first queries of a long document, whose gradients are the
+    // largest, are such queries, and cheap ones: 8192 tokens 697 -> 700 us, dQ off by 1.9e-3 of its norm instead of 2.4e-3 (one
+    // rounding of the exact gradient: 1.7e-3).  Up to 2048 keys: 712 us, 1.9e-3; for all, the fourth product would cost a quarter
+    // of the kernel's time (857 us).
+    const int seen = full_head ? min(kn, n_tiles * kTok) : min(kn, a.sink + a.window);
+    const float steepest = BIAS ? fmaxf(fabsf(a.slopes[sh.at.head[0]]), fabsf(a.slopes[sh.at.head[1]])) : 0.f;
+    const bool in_two = seen <= kFewKeys || steepest * kFewKeys >= 1.f;
     const uint32_t q_smem = smem_u32(smem), o_smem = q_smem + 2 * F::kTile, k_smem = q_smem + 4 * F::kTile, v_smem = q_smem + 6 * F::kTile;
     auto tile_at = [&](int j) { return j < a_end ? j : b0 + j - a_end; };
     // (launched with 384 x 168 = 64512 registers: 256 x 232 + 128 x 40)

@@ -358,6 +358,26 @@ def test_captured_call_reads_starts_and_inputs_anew(rl, cuda_device):
             assert torch.equal(eager[name], bufs[name]), (name, lens)
 
 
+@pytest.mark.parametrize("Hkv,Hq,D,lens", [(2, 8, 64, [300, 5, 70]), (4, 28, 128, [900]), (1, 1, 128, [2000, 1])])
+def test_calls_one_after_the_other(rl, cuda_device, Hkv, Hq, D, lens):
+    """The backward pass's launches overlap: calls on other inputs right behind one another, without documents between them,
+    give the bits that each gives alone."""
+    dev, n = cuda_device, sum(lens)
+    p = Prompt(rl, 1, Hkv, Hq, D, n, [1] * Hkv, 4, 60)
+    sets = [inputs(n, n, Hq, Hkv, D, 71 + 5 * i, dev) for i in range(3)]
+    of = [starts(lens, dev), starts(lens[::-1], dev), torch.zeros(2, dtype=torch.int32, device=dev)]
+    alone = []
+    for x, s in zip(sets, of):
+        alone.append(call(rl, p.h, 0, *x[:3], s, None, None, x[3]))
+        torch.cuda.synchronize()
+    many = [[call(rl, p.h, 0, *x[:3], s, None, None, x[3]) for x, s in zip(sets, of)] for _ in range(8)]
+    for got in many:
+        for a, b in zip(got, alone):
+            for name in a:
+                assert torch.equal(a[name], b[name]), name
+    assert rl.rlkv_prompt_kernel_status(p.h) == 0
+
+
 def test_starts_outside_the_tensors_stay_inside(rl, cuda_device):
     """Starts that run past the tensors or backwards name clipped or empty documents: no row outside is touched."""
     dev, Hkv, Hq, D, n = cuda_device, 1, 2, 64, 100

@@ -10,7 +10,7 @@
 // in a fixed order: no atomics on dQ, no fp32 copy of it in memory, the same bits on every run.  P and dS are written
 // to tensor memory as bf16 over S and dP and are the A operand of the second products straight from there.
 //
-// Measured (32 / 8 heads of 128, causal, 8192 tokens): stats 26 us (DRAM), rows 690 us, keys 815 us; 0.9 PFLOP/s of the five
+// Measured (32 / 8 heads of 128, causal, 8192 tokens): stats 26 us (DRAM), rows 700 us, keys 810 us; 0.9 PFLOP/s of the five
 // products, 1.25 of the seven that run.  What bounds it: in `keys` the exponential unit (64 scores a thread, eight warps at
 // once: 1024 cycles of the 1180 that P takes) in the chain S - P - dV - S of 2900 cycles beside 2048 of products; in `rows`
 // the same unit and the hand-overs between threads and products.

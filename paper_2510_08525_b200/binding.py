@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 
 import numpy as np
 
@@ -141,6 +142,17 @@ def _stream(s, of=None) -> int:
     if isinstance(s, int):
         return s
     return s.cuda_stream
+
+
+_Byte = ctypes.c_ubyte
+
+
+def _host(a) -> int:
+    """Address of a contiguous numpy array (a.ctypes builds an object first, which takes a microsecond more)."""
+    try:
+        return ctypes.addressof(_Byte.from_buffer(a))
+    except (TypeError, ValueError):  # read-only, or empty
+        return a.ctypes.data
 
 
 def _mask(head_is_full) -> np.ndarray:
@@ -446,15 +458,16 @@ def _rows(x, least=1):
     may be a slice of a wider projection; an address alone stands for contiguous tokens."""
     if x is None or isinstance(x, int):
         return x or 0, 0
-    if not _on_device(x):
+    if not getattr(x, "is_cuda", False):
         raise ValueError("a tensor in device memory is wanted")
-    n, _, dim = x.shape  # ValueError where it has other than three dimensions
-    token, head, one = x.stride()
-    if x.element_size() != 2 or not x.is_floating_point():
+    token, head, one = x.stride()  # ValueError where it has other than three dimensions
+    if x.dtype is not sys.modules["torch"].bfloat16:
         raise ValueError("rows are bf16")
+    shape = x.shape
+    n = shape[0]
     if n < least:
         raise ValueError(f"{n} tokens where the call names {least}")
-    if one != 1 or head != dim:
+    if one != 1 or head != shape[2]:
         raise ValueError("tokens must be [tokens][heads][head_dim] with contiguous heads")
     if n <= 1:
         return x.data_ptr(), 0
@@ -467,9 +480,11 @@ def _room(x, least, size=2):
     """Address of a contiguous tensor in device memory of `least` elements or more, `size` bytes each; or the address itself."""
     if x is None or isinstance(x, int):
         return x or 0
-    if not _on_device(x) or x.element_size() != size or x.numel() < least:
+    if not getattr(x, "is_cuda", False) or x.element_size() != size or x.numel() < least:
         raise RlkvError(RLKV_EINVAL, f"a tensor in device memory of {least} elements of {size} bytes is wanted")
-    return _ptr(x)
+    if not x.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    return x.data_ptr()
 
 
 def _size(x) -> int:
@@ -498,7 +513,7 @@ def rlkv_paged_set_rotary(cache, table, positions, rot_dim, interleaved=False) -
 def rlkv_paged_append_rotated(cache, layer, slots, q, k, v, q_out, stream=None) -> None:
     s = np.ascontiguousarray(slots, dtype=np.int32)
     n = s.size
-    _check(lib.rlkv_paged_append_rotated(cache, layer, s.ctypes.data, n, *_rows(q, n), *_rows(k, n), *_rows(v, n),
+    _check(lib.rlkv_paged_append_rotated(cache, layer, _host(s), n, *_rows(q, n), *_rows(k, n), *_rows(v, n),
                                          _room(q_out, _size(q)), _stream(stream, k)))
 
 
@@ -510,7 +525,7 @@ def rlkv_paged_prefill_rotated(cache, layer, slot, q, k, v, n_tokens, q_out, k_o
 
 def rlkv_paged_decode_attention(cache, layer, slots, q, out, stream=None) -> None:
     s = _slots(slots)
-    _check(lib.rlkv_paged_decode_attention(cache, layer, s.ctypes.data, s.size, _ptr(q), _ptr(out), _stream(stream)))
+    _check(lib.rlkv_paged_decode_attention(cache, layer, _host(s), s.size, _ptr(q), _ptr(out), _stream(stream)))
 
 
 def rlkv_paged_step(cache, slots, k, v, q, out, stream=None) -> None:

@@ -1,6 +1,7 @@
 """Refusals of the rotation, score and prompt calls that need no device."""
 import numpy as np
 import pytest
+import torch
 
 
 @pytest.fixture(scope="module")
@@ -47,6 +48,7 @@ class Rows:
 
     def __init__(self, shape, stride=None, size=2, device=0, whole=False):
         self.shape, self.size, self.device, self.is_cuda, self.whole = shape, size, device, True, whole
+        self.dtype = torch.int32 if whole else torch.bfloat16 if size == 2 else torch.float32
         self.strides = stride or tuple(int(np.prod(shape[i + 1:])) for i in range(len(shape)))
 
     def stride(self):
@@ -103,8 +105,14 @@ def test_calls_refuse_tensors_too_small_for_them(binding):
             call()
 
 
+def test_addresses_of_host_arrays(binding):
+    a = np.arange(5, dtype=np.int32)
+    assert binding._host(a) == a.ctypes.data
+    a.flags.writeable = False
+    assert binding._host(a) == a.ctypes.data and isinstance(binding._host(a[:0]), int)
+
+
 def test_the_stream_is_that_of_the_tensors_gpu(binding, monkeypatch):
-    import torch
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 100 + device, raising=False)
     assert binding._stream(None) == 100 and binding._stream(None, Rows((1, 1, 64), device=3)) == 103

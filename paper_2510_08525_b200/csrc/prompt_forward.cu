@@ -259,9 +259,12 @@ prompt_forward_kernel(const __grid_constant__ PromptArgs a, const __grid_constan
     } else if (warp == 8) {
         // ------------------------------------------------------------------ tile loads
         if (lane == 0 && n_tiles > 0) {
-            mbar_expect_tx(smem_u32(&sh.q_full), n_sub * F::kTileBytes);
-            for (int w = 0; w < n_sub; ++w)
-                for (int b = 0; b < D / 64; ++b)
+            // (no queries for a sub-tile that sees no key beside one that does: its threads wait for no product, and the zeros of its
+            // rows go out through the memory that the queries would be copied to)
+            auto sees = [&](int w) { return sh.at.sub_a[w] > 0 || sh.at.sub_b[w] < sh.at.sub_e[w]; };
+            mbar_expect_tx(smem_u32(&sh.q_full), ((int)sees(0) + (int)sees(1)) * F::kTileBytes);
+            for (int w = 0; w < 2; ++w)
+                for (int b = 0; sees(w) && b < D / 64; ++b)
                     load_box(q_smem + w * F::kTileBytes + b * kBlock, &map_q, b * 64, sh.at.head[w], sh.at.q0[w], smem_u32(&sh.q_full));
             int issued = 0;
             bool ok = true;

@@ -159,6 +159,29 @@ def test_prompt_forward_and_backward(rl, cuda_device, Hkv, Hq, D, S, W, mask, lq
     assert torch.equal(out, got["out"])
 
 
+@pytest.mark.parametrize("Hkv,Hq,D", [(1, 7, 128), (1, 7, 64), (2, 2, 128), (2, 6, 64)])
+@pytest.mark.parametrize("lq,lk", [([300], [100]), ([700], [300]), ([300, 700, 256], [100, 300, 1])])
+def test_queries_before_the_first_key(rl, cuda_device, Hkv, Hq, D, lq, lk):
+    """Documents of many more queries than keys, odd groups: 128 queries that see no key beside 128 that do, in one CTA.  Their
+    rows are zeros whatever their queries hold, in every one of many calls."""
+    dev, nq, nk = cuda_device, sum(lq), sum(lk)
+    mask = [1, 0][:Hkv]
+    for full in (mask, [1 - x for x in mask]):
+        c = dict(mask=full, sink=4, window=60, cap=0.0, slopes=None, prefix=None)
+        p = Prompt(rl, 1, Hkv, Hq, D, nq, full, 4, 60)
+        q, k, v, dout = inputs(nq, nk, Hq, Hkv, D, 43, dev)
+        got = call(rl, p.h, 0, q, k, v, starts(lq, dev), starts(lk, dev), None, dout)
+        want, tol = reference(c, q, k, v, lq, lk, dout)
+        check(got, want, tol, nq, nk)
+        unseen = torch.cat([torch.arange(a, device=dev) < a - b for a, b in zip(lq, lk)])
+        bufs = [torch.full_like(q, 7.0) for _ in range(20)]
+        for out in bufs:
+            rl.rlkv_prompt_attention(p.h, 0, q, k, v, starts(lq, dev), starts(lk, dev), None, out, None)
+        for out in [got["out"], *bufs]:
+            assert bool((out[unseen] == 0).all()) and torch.equal(out, got["out"])
+        assert bool((got["dq"][unseen] == 0).all()) and rl.rlkv_prompt_kernel_status(p.h) == 0
+
+
 def test_documents_do_not_touch_one_another(rl, cuda_device):
     """A document's bits are those it has alone, whatever is packed around it, NaN included."""
     dev, Hkv, Hq, D = cuda_device, 2, 8, 128

@@ -476,12 +476,12 @@ def _rows(x, least=1):
     return x.data_ptr(), token
 
 
-def _room(x, least, size=2):
-    """Address of a contiguous tensor in device memory of `least` elements or more, `size` bytes each; or the address itself."""
+def _room(x, least, dtype="bfloat16"):
+    """Address of a contiguous tensor in device memory of `least` elements or more of that type; or the address itself."""
     if x is None or isinstance(x, int):
         return x or 0
-    if not getattr(x, "is_cuda", False) or x.element_size() != size or x.numel() < least:
-        raise RlkvError(RLKV_EINVAL, f"a tensor in device memory of {least} elements of {size} bytes is wanted")
+    if not getattr(x, "is_cuda", False) or x.dtype is not getattr(sys.modules["torch"], dtype) or x.numel() < least:
+        raise RlkvError(RLKV_EINVAL, f"a tensor in device memory of {least} {dtype} elements is wanted")
     if not x.is_contiguous():
         raise ValueError("tensor must be contiguous")
     return x.data_ptr()
@@ -608,14 +608,14 @@ def _prompt_args(q, k, v, q_starts, k_starts, prefix):
 def rlkv_prompt_attention(prompt, layer, q, k, v, q_starts, k_starts, prefix, out, lse, stream=None) -> None:
     """q, k, v: [tokens][heads][head_dim], possibly slices of one projection's output; q_starts, k_starts, prefix: int32."""
     _check(lib.rlkv_prompt_attention(prompt, layer, *_prompt_args(q, k, v, q_starts, k_starts, prefix), _room(out, q.numel()),
-                                     _room(lse, q.shape[0] * q.shape[1], 4), _stream(stream, q)))
+                                     _room(lse, q.shape[0] * q.shape[1], "float32"), _stream(stream, q)))
 
 
 def rlkv_prompt_attention_backward(prompt, layer, q, k, v, q_starts, k_starts, prefix, out, lse, dout, dq, dk, dv,
                                    stream=None) -> None:
     n_q, n_k = q.numel(), k.numel()
     _check(lib.rlkv_prompt_attention_backward(prompt, layer, *_prompt_args(q, k, v, q_starts, k_starts, prefix), _room(out, n_q),
-                                              _room(lse, q.shape[0] * q.shape[1], 4), _room(dout, n_q), _room(dq, n_q),
+                                              _room(lse, q.shape[0] * q.shape[1], "float32"), _room(dout, n_q), _room(dq, n_q),
                                               _room(dk, n_k), _room(dv, n_k), _stream(stream, q)))
 
 

@@ -117,3 +117,42 @@ def test_the_stream_is_that_of_the_tensors_gpu(binding, monkeypatch):
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 100 + device, raising=False)
     assert binding._stream(None) == 100 and binding._stream(None, Rows((1, 1, 64), device=3)) == 103
     assert binding._stream(None, 4096) == 100 and binding._stream(7, Rows((1, 1, 64), device=3)) == 7
+
+
+def of_type(shape, dtype):
+    x = Rows(shape, size=dtype.itemsize)
+    x.dtype = dtype
+    return x
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.int16, torch.uint16])
+def test_other_types_of_the_same_size_are_refused(binding, dtype):
+    """16-bit tensors that are not bf16, 32-bit ones that are not fp32: their bits would be taken for numbers of those types."""
+    b = binding
+    q, k, starts = Rows((4, 8, 128)), Rows((4, 2, 128)), Rows((2,), size=4, whole=True)
+    lse, other_lse = of_type((4, 8), torch.float32), of_type((4, 8), torch.int32)
+    like = lambda x: of_type(x.shape, dtype)  # noqa: E731
+    grads = dict(out=q, lse=lse, dout=q, dq=q, dk=k, dv=k)
+    calls = [lambda: b.rlkv_paged_append_rotated(16, 0, [0, 1, 2, 3], q, k, k, like(q), stream=0),
+             lambda: b.rlkv_paged_prefill_rotated(16, 0, 0, q, k, k, 4, like(q), None, stream=0),
+             lambda: b.rlkv_paged_prefill_rotated(16, 0, 0, q, k, k, 4, q, like(k), stream=0),
+             lambda: b.rlkv_prompt_attention(16, 0, q, k, k, starts, None, None, like(q), lse, 0),
+             lambda: b.rlkv_prompt_attention(16, 0, q, k, k, starts, None, None, q, other_lse, 0)]
+    for name, x in grads.items():
+        given = {**grads, name: other_lse if name == "lse" else like(x)}
+        calls.append(lambda given=given: b.rlkv_prompt_attention_backward(16, 0, q, k, k, starts, None, None, *given.values(), stream=0))
+
+    class Library:  # the calls are to be refused before the library sees them
+        def __getattr__(self, name):
+            def called(*args):
+                raise AssertionError(f"{name} was called")
+            return called
+
+    lib, b.lib = b.lib, Library()
+    try:
+        for call in calls:
+            with pytest.raises(b.RlkvError) as e:
+                call()
+            assert e.value.code == b.RLKV_EINVAL
+    finally:
+        b.lib = lib

@@ -155,6 +155,17 @@ def _host(a) -> int:
         return a.ctypes.data
 
 
+class Handle(int):
+    """The address of a paged cache or prompt handle, with the shape it was created with: what a call reads and writes goes by
+    it, so it is what the call's arrays are checked against.  (An address alone, like a tensor's, is taken as it is.)"""
+
+
+def _handle(address, layers, kv_heads, q_heads, head_dim) -> Handle:
+    h = Handle(address)
+    h.layers, h.kv_heads, h.q_heads, h.head_dim = layers, kv_heads, q_heads, head_dim
+    return h
+
+
 def _mask(head_is_full) -> np.ndarray:
     return np.ascontiguousarray(np.asarray(head_is_full, dtype=np.uint8).reshape(-1))
 
@@ -398,7 +409,7 @@ def rlkv_paged_create(layers, kv_heads, q_heads, head_dim, max_seqs, n_pages, ma
     handle = _vp(0)
     _check(lib.rlkv_paged_create(ctypes.byref(handle), layers, kv_heads, q_heads, head_dim, max_seqs, n_pages, max_seq_len,
                                  m.ctypes.data, sink, window, _ptr(device_buf), device_buf_bytes))
-    return int(handle.value)
+    return _handle(handle.value, layers, kv_heads, q_heads, head_dim)
 
 
 def rlkv_paged_size_fp8(layers, kv_heads, q_heads, head_dim, max_seqs, n_pages, max_seq_len, head_is_full, sink,
@@ -423,7 +434,7 @@ def rlkv_paged_create_fp8(layers, kv_heads, q_heads, head_dim, max_seqs, n_pages
     _check(lib.rlkv_paged_create_fp8(ctypes.byref(handle), layers, kv_heads, q_heads, head_dim, max_seqs, n_pages,
                                      max_seq_len, m.ctypes.data, sink, window, ks.ctypes.data, vs.ctypes.data,
                                      _ptr(device_buf), device_buf_bytes))
-    return int(handle.value)
+    return _handle(handle.value, layers, kv_heads, q_heads, head_dim)
 
 
 def rlkv_paged_destroy(cache) -> None:
@@ -492,8 +503,10 @@ def _size(x) -> int:
 
 
 def rlkv_paged_set_scores(cache, softcap, slopes=None) -> None:
-    """slopes: host, [layers][q_heads] (the caller's to get right: the handle knows its own shape), or None."""
+    """slopes: host, [layers][q_heads], or None."""
     s = None if slopes is None else np.ascontiguousarray(slopes, dtype=np.float32)
+    if s is not None and isinstance(cache, Handle) and s.size != cache.layers * cache.q_heads:
+        raise ValueError("slopes must have layers*q_heads entries")
     _check(lib.rlkv_paged_set_scores(cache, float(softcap), 0 if s is None else s.ctypes.data))
 
 

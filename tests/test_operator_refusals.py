@@ -119,6 +119,24 @@ def test_the_stream_is_that_of_the_tensors_gpu(binding, monkeypatch):
     assert binding._stream(None, 4096) == 100 and binding._stream(7, Rows((1, 1, 64), device=3)) == 7
 
 
+def without_the_library(b, calls, error):
+    """Every call raises `error` before the library sees it."""
+    class Library:
+        def __getattr__(self, name):
+            def called(*args):
+                raise AssertionError(f"{name} was called")
+            return called
+
+    lib, b.lib = b.lib, Library()
+    try:
+        for call in calls:
+            with pytest.raises(error) as e:
+                call()
+            assert error is not b.RlkvError or e.value.code == b.RLKV_EINVAL
+    finally:
+        b.lib = lib
+
+
 def of_type(shape, dtype):
     x = Rows(shape, size=dtype.itemsize)
     x.dtype = dtype
@@ -142,17 +160,28 @@ def test_other_types_of_the_same_size_are_refused(binding, dtype):
         given = {**grads, name: other_lse if name == "lse" else like(x)}
         calls.append(lambda given=given: b.rlkv_prompt_attention_backward(16, 0, q, k, k, starts, None, None, *given.values(), stream=0))
 
-    class Library:  # the calls are to be refused before the library sees them
-        def __getattr__(self, name):
-            def called(*args):
-                raise AssertionError(f"{name} was called")
-            return called
+    without_the_library(b, calls, b.RlkvError)
 
-    lib, b.lib = b.lib, Library()
-    try:
-        for call in calls:
-            with pytest.raises(b.RlkvError) as e:
-                call()
-            assert e.value.code == b.RLKV_EINVAL
-    finally:
-        b.lib = lib
+
+def test_slopes_of_another_count_are_refused(binding):
+    """The library reads layers * q_heads slopes, whatever the array holds."""
+    b = binding
+    cache = b._handle(16, 3, 2, 8, 128)
+    without_the_library(b, [lambda n=n: b.rlkv_paged_set_scores(cache, 0.0, np.full(n, 0.5, np.float32)) for n in (0, 1, 8, 23, 25)] +
+                        [lambda: b.rlkv_paged_set_scores(cache, 0.0, 0.5)], ValueError)
+
+
+def test_a_created_handle_knows_its_shape(binding, monkeypatch):
+    b = binding
+
+    class Library:
+        def __getattr__(self, name):
+            def create(out, *args):
+                out._obj.value = 4096
+                return 0
+            return create
+
+    monkeypatch.setattr(b, "lib", Library())
+    shape, rest = (2, 4, 28, 128), (2, 8, 100, [1] * 8, 4, 60)
+    for h in (b.rlkv_paged_create(*shape, *rest), b.rlkv_paged_create_fp8(*shape, *rest, [1.0] * 8, [1.0] * 8)):
+        assert h == 4096 and isinstance(h, int) and (h.layers, h.kv_heads, h.q_heads, h.head_dim) == shape

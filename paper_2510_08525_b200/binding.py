@@ -464,9 +464,14 @@ def _on_device(x) -> bool:
     return not isinstance(x, np.ndarray) and x.is_cuda
 
 
-def _rows(x, least=1):
+def _heads(handle):
+    """q_heads, kv_heads and head_dim of a handle, zeros for an address alone."""
+    return (handle.q_heads, handle.kv_heads, handle.head_dim) if isinstance(handle, Handle) else (0, 0, 0)
+
+
+def _rows(x, least=1, heads=0, head_dim=0):
     """(address, elements from token to token) of a bf16 [tokens][heads][head_dim] tensor of at least `least` tokens, which
-    may be a slice of a wider projection; an address alone stands for contiguous tokens."""
+    may be a slice of a wider projection; an address alone stands for contiguous tokens.  `heads`: of the handle (0: unknown)."""
     if x is None or isinstance(x, int):
         return x or 0, 0
     if not getattr(x, "is_cuda", False):
@@ -474,12 +479,13 @@ def _rows(x, least=1):
     token, head, one = x.stride()  # ValueError where it has other than three dimensions
     if x.dtype is not sys.modules["torch"].bfloat16:
         raise ValueError("rows are bf16")
-    shape = x.shape
-    n = shape[0]
+    n, held, dim = x.shape
     if n < least:
         raise ValueError(f"{n} tokens where the call names {least}")
-    if one != 1 or head != shape[2]:
+    if one != 1 or head != dim:
         raise ValueError("tokens must be [tokens][heads][head_dim] with contiguous heads")
+    if heads and (held != heads or dim != head_dim):
+        raise ValueError(f"rows are [tokens][{heads}][{head_dim}]")
     if n <= 1:
         return x.data_ptr(), 0
     if token == 0:  # an expanded tensor; 0 would stand for contiguous tokens
@@ -526,14 +532,16 @@ def rlkv_paged_set_rotary(cache, table, positions, rot_dim, interleaved=False) -
 def rlkv_paged_append_rotated(cache, layer, slots, q, k, v, q_out, stream=None) -> None:
     s = np.ascontiguousarray(slots, dtype=np.int32)
     n = s.size
-    _check(lib.rlkv_paged_append_rotated(cache, layer, _host(s), n, *_rows(q, n), *_rows(k, n), *_rows(v, n),
+    hq, hkv, d = _heads(cache)
+    _check(lib.rlkv_paged_append_rotated(cache, layer, _host(s), n, *_rows(q, n, hq, d), *_rows(k, n, hkv, d), *_rows(v, n, hkv, d),
                                          _room(q_out, _size(q)), _stream(stream, k)))
 
 
 def rlkv_paged_prefill_rotated(cache, layer, slot, q, k, v, n_tokens, q_out, k_out=None, stream=None) -> None:
     n = n_tokens
-    _check(lib.rlkv_paged_prefill_rotated(cache, layer, slot, *_rows(q, n), *_rows(k, n), *_rows(v, n), n, _room(q_out, _size(q)),
-                                          _room(k_out, _size(k)), _stream(stream, k)))
+    hq, hkv, d = _heads(cache)
+    _check(lib.rlkv_paged_prefill_rotated(cache, layer, slot, *_rows(q, n, hq, d), *_rows(k, n, hkv, d), *_rows(v, n, hkv, d), n,
+                                          _room(q_out, _size(q)), _room(k_out, _size(k)), _stream(stream, k)))
 
 
 def rlkv_paged_decode_attention(cache, layer, slots, q, out, stream=None) -> None:
@@ -597,14 +605,14 @@ def rlkv_prompt_create(layers, kv_heads, q_heads, head_dim, max_tokens, head_is_
     handle = _vp(0)
     _check(lib.rlkv_prompt_create(ctypes.byref(handle), layers, kv_heads, q_heads, head_dim, max_tokens, m.ctypes.data, sink,
                                   window, float(softcap), 0 if s is None else s.ctypes.data))
-    return int(handle.value)
+    return _handle(handle.value, layers, kv_heads, q_heads, head_dim)
 
 
 def rlkv_prompt_destroy(prompt) -> None:
     _check(lib.rlkv_prompt_destroy(prompt))
 
 
-def _prompt_args(q, k, v, q_starts, k_starts, prefix):
+def _prompt_args(prompt, q, k, v, q_starts, k_starts, prefix):
     ints = [x for x in (q_starts, k_starts, prefix) if x is not None]
     if not all(map(_on_device, ints)):
         raise ValueError("q_starts, k_starts and prefix are read on the device")
@@ -615,19 +623,20 @@ def _prompt_args(q, k, v, q_starts, k_starts, prefix):
         raise ValueError("q_starts, k_starts and prefix are int32")
     if k.shape != v.shape:
         raise ValueError("k and v must have the same shape")
-    return (*_rows(q, 0), *_rows(k, 0), *_rows(v, 0), q.shape[0], k.shape[0], _ptr(q_starts), _ptr(k_starts), n_docs, _ptr(prefix))
+    hq, hkv, d = _heads(prompt)
+    return (*_rows(q, 0, hq, d), *_rows(k, 0, hkv, d), *_rows(v, 0, hkv, d), q.shape[0], k.shape[0], _ptr(q_starts), _ptr(k_starts), n_docs, _ptr(prefix))
 
 
 def rlkv_prompt_attention(prompt, layer, q, k, v, q_starts, k_starts, prefix, out, lse, stream=None) -> None:
     """q, k, v: [tokens][heads][head_dim], possibly slices of one projection's output; q_starts, k_starts, prefix: int32."""
-    _check(lib.rlkv_prompt_attention(prompt, layer, *_prompt_args(q, k, v, q_starts, k_starts, prefix), _room(out, q.numel()),
+    _check(lib.rlkv_prompt_attention(prompt, layer, *_prompt_args(prompt, q, k, v, q_starts, k_starts, prefix), _room(out, q.numel()),
                                      _room(lse, q.shape[0] * q.shape[1], "float32"), _stream(stream, q)))
 
 
 def rlkv_prompt_attention_backward(prompt, layer, q, k, v, q_starts, k_starts, prefix, out, lse, dout, dq, dk, dv,
                                    stream=None) -> None:
     n_q, n_k = q.numel(), k.numel()
-    _check(lib.rlkv_prompt_attention_backward(prompt, layer, *_prompt_args(q, k, v, q_starts, k_starts, prefix), _room(out, n_q),
+    _check(lib.rlkv_prompt_attention_backward(prompt, layer, *_prompt_args(prompt, q, k, v, q_starts, k_starts, prefix), _room(out, n_q),
                                               _room(lse, q.shape[0] * q.shape[1], "float32"), _room(dout, n_q), _room(dq, n_q),
                                               _room(dk, n_k), _room(dv, n_k), _stream(stream, q)))
 

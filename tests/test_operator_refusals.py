@@ -185,3 +185,37 @@ def test_a_created_handle_knows_its_shape(binding, monkeypatch):
     shape, rest = (2, 4, 28, 128), (2, 8, 100, [1] * 8, 4, 60)
     for h in (b.rlkv_paged_create(*shape, *rest), b.rlkv_paged_create_fp8(*shape, *rest, [1.0] * 8, [1.0] * 8)):
         assert h == 4096 and isinstance(h, int) and (h.layers, h.kv_heads, h.q_heads, h.head_dim) == shape
+
+
+def test_rows_of_other_heads_than_the_handles_are_refused(binding):
+    """The library reads and writes rows of the handle's heads.  One token's rows, and slices of a projection that are wide enough
+    apart for it, would pass the checks of their strides."""
+    b, starts = binding, Rows((2,), size=4, whole=True)
+    h = b._handle(16, 1, 2, 8, 128)
+    wide = lambda n, heads, d=128: Rows((n, heads, d), (12 * 128, d, 1))  # noqa: E731
+    calls = []
+    for n in (1, 4):
+        q, kv, lse = wide(n, 8), wide(n, 2), of_type((n, 8), torch.float32)
+        for bad_q, bad_k, bad_v in ((wide(n, 4), kv, kv), (wide(n, 9), kv, kv), (wide(n, 8, 64), kv, kv), (q, wide(n, 1), kv),
+                                    (q, kv, wide(n, 1)), (q, wide(n, 2, 64), wide(n, 2, 64)), (q, wide(n, 1), wide(n, 1))):
+            out, args = Rows(bad_q.shape), (bad_q, bad_k, bad_v)
+            calls += [lambda n=n, args=args, out=out: b.rlkv_paged_append_rotated(h, 0, range(n), *args, out, stream=0),
+                      lambda n=n, args=args, out=out: b.rlkv_paged_prefill_rotated(h, 0, 0, *args, n, out, None, stream=0),
+                      lambda args=args, out=out, lse=lse: b.rlkv_prompt_attention(h, 0, *args, starts, None, None, out, lse, stream=0),
+                      lambda args=args, out=out, lse=lse: b.rlkv_prompt_attention_backward(
+                          h, 0, *args, starts, None, None, out, lse, out, out, Rows(args[1].shape), Rows(args[2].shape), stream=0)]
+    without_the_library(b, calls, ValueError)
+
+
+def test_a_created_prompt_handle_knows_its_shape(binding, monkeypatch):
+    b, asked = binding, []
+
+    class Library:
+        def rlkv_prompt_create(self, out, *args):
+            out._obj.value = 4096
+            asked.append(args[:4])
+            return 0
+
+    monkeypatch.setattr(b, "lib", Library())
+    h = b.rlkv_prompt_create(2, 4, 28, 128, 100, [1] * 8, 4, 60)
+    assert h == 4096 and (h.layers, h.kv_heads, h.q_heads, h.head_dim) == (2, 4, 28, 128) == asked[0]

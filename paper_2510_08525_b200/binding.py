@@ -516,16 +516,21 @@ def rlkv_paged_set_scores(cache, softcap, slopes=None) -> None:
     _check(lib.rlkv_paged_set_scores(cache, float(softcap), 0 if s is None else s.ctypes.data))
 
 
+def _check_table(table, rot_dim, positions) -> None:
+    if table is None or isinstance(table, int):
+        return
+    if table.dtype is not sys.modules["torch"].float32 or table.numel() < rot_dim * positions:
+        raise ValueError("the table is fp32 [positions][rot_dim / 2][2]")
+
+
 def rlkv_rotary_table(inv_freq, positions, table, stream=None) -> None:
     f = np.ascontiguousarray(inv_freq, dtype=np.float64)
-    if _size(table) and table.numel() < 2 * f.size * positions:
-        raise ValueError("the table holds fewer rows")
+    _check_table(table, 2 * f.size, positions)
     _check(lib.rlkv_rotary_table(f.ctypes.data, 2 * f.size, positions, _ptr(table), _stream(stream)))
 
 
 def rlkv_paged_set_rotary(cache, table, positions, rot_dim, interleaved=False) -> None:
-    if _size(table) and (table.element_size() != 4 or table.numel() < min(rot_dim, 128) * positions):
-        raise ValueError("the table is fp32 [positions][rot_dim / 2][2]")
+    _check_table(table, min(rot_dim, 128), positions)
     _check(lib.rlkv_paged_set_rotary(cache, _ptr(table), positions, rot_dim, int(bool(interleaved))))
 
 

@@ -219,3 +219,14 @@ def test_a_created_prompt_handle_knows_its_shape(binding, monkeypatch):
     monkeypatch.setattr(b, "lib", Library())
     h = b.rlkv_prompt_create(2, 4, 28, 128, 100, [1] * 8, 4, 60)
     assert h == 4096 and (h.layers, h.kv_heads, h.q_heads, h.head_dim) == (2, 4, 28, 128) == asked[0]
+
+
+def test_tables_of_other_types_are_refused(binding):
+    """A 16-bit table has half the bytes that its count of elements says; integers are not angles;
+    an empty one holds none."""
+    b, calls = binding, []
+    tables = [of_type((10, 64, 2), t) for t in (torch.bfloat16, torch.float16, torch.int32, torch.float64)] + [Rows((0, 64, 2), size=4)]
+    for table in tables:
+        calls += [lambda table=table: b.rlkv_rotary_table(np.ones(64), 10, table, stream=0),
+                  lambda table=table: b.rlkv_paged_set_rotary(16, table, 10, 128)]
+    without_the_library(b, calls, ValueError)

@@ -156,13 +156,15 @@ def _host(a) -> int:
 
 
 class Handle(int):
-    """The address of a paged cache or prompt handle, with the shape it was created with: what a call reads and writes goes by
-    it, so it is what the call's arrays are checked against.  (An address alone, like a tensor's, is taken as it is.)"""
+    """The address of a paged cache or prompt handle, with the shape and the GPU it was created with: what a call reads and writes
+    goes by them, so they are what the call's arrays are checked against.  (An address alone, like a tensor's, is taken as it is.)"""
 
 
 def _handle(address, layers, kv_heads, q_heads, head_dim) -> Handle:
     h = Handle(address)
     h.layers, h.kv_heads, h.q_heads, h.head_dim = layers, kv_heads, q_heads, head_dim
+    torch = sys.modules.get("torch")  # (the library creates on the current device)
+    h.device = torch.cuda.current_device() if torch is not None and torch.cuda.is_available() else None
     return h
 
 
@@ -504,6 +506,22 @@ def _room(x, least, dtype="bfloat16"):
     return x.data_ptr()
 
 
+def _stream_of(s, handle, tensors) -> int:
+    """The stream of a call whose tensors have passed their other checks: they have to be on the handle's GPU, which the launch
+    goes to.  (An address alone as handle: all on one GPU.)"""
+    device = getattr(handle, "device", None)
+    of = None
+    for x in tensors:
+        if x is None or isinstance(x, int):
+            continue
+        of, at = x, x.get_device()
+        if device is None:
+            device = at
+        elif at != device:
+            raise ValueError(f"a tensor on GPU {at} in a call on GPU {device}")
+    return _stream(s, of)
+
+
 def _size(x) -> int:
     return 0 if x is None or isinstance(x, int) else x.numel()
 
@@ -539,14 +557,15 @@ def rlkv_paged_append_rotated(cache, layer, slots, q, k, v, q_out, stream=None) 
     n = s.size
     hq, hkv, d = _heads(cache)
     _check(lib.rlkv_paged_append_rotated(cache, layer, _host(s), n, *_rows(q, n, hq, d), *_rows(k, n, hkv, d), *_rows(v, n, hkv, d),
-                                         _room(q_out, _size(q)), _stream(stream, k)))
+                                         _room(q_out, _size(q)), _stream_of(stream, cache, (q, k, v, q_out))))
 
 
 def rlkv_paged_prefill_rotated(cache, layer, slot, q, k, v, n_tokens, q_out, k_out=None, stream=None) -> None:
     n = n_tokens
     hq, hkv, d = _heads(cache)
     _check(lib.rlkv_paged_prefill_rotated(cache, layer, slot, *_rows(q, n, hq, d), *_rows(k, n, hkv, d), *_rows(v, n, hkv, d), n,
-                                          _room(q_out, _size(q)), _room(k_out, _size(k)), _stream(stream, k)))
+                                          _room(q_out, _size(q)), _room(k_out, _size(k)),
+                                          _stream_of(stream, cache, (q, k, v, q_out, k_out))))
 
 
 def rlkv_paged_decode_attention(cache, layer, slots, q, out, stream=None) -> None:
@@ -629,13 +648,15 @@ def _prompt_args(prompt, q, k, v, q_starts, k_starts, prefix):
     if k.shape != v.shape:
         raise ValueError("k and v must have the same shape")
     hq, hkv, d = _heads(prompt)
-    return (*_rows(q, 0, hq, d), *_rows(k, 0, hkv, d), *_rows(v, 0, hkv, d), q.shape[0], k.shape[0], _ptr(q_starts), _ptr(k_starts), n_docs, _ptr(prefix))
+    return (*_rows(q, 0, hq, d), *_rows(k, 0, hkv, d), *_rows(v, 0, hkv, d), q.shape[0], k.shape[0], _ptr(q_starts), _ptr(k_starts),
+            n_docs, _ptr(prefix))
 
 
 def rlkv_prompt_attention(prompt, layer, q, k, v, q_starts, k_starts, prefix, out, lse, stream=None) -> None:
     """q, k, v: [tokens][heads][head_dim], possibly slices of one projection's output; q_starts, k_starts, prefix: int32."""
     _check(lib.rlkv_prompt_attention(prompt, layer, *_prompt_args(prompt, q, k, v, q_starts, k_starts, prefix), _room(out, q.numel()),
-                                     _room(lse, q.shape[0] * q.shape[1], "float32"), _stream(stream, q)))
+                                     _room(lse, q.shape[0] * q.shape[1], "float32"),
+                                     _stream_of(stream, prompt, (q, k, v, q_starts, k_starts, prefix, out, lse))))
 
 
 def rlkv_prompt_attention_backward(prompt, layer, q, k, v, q_starts, k_starts, prefix, out, lse, dout, dq, dk, dv,
@@ -643,7 +664,8 @@ def rlkv_prompt_attention_backward(prompt, layer, q, k, v, q_starts, k_starts, p
     n_q, n_k = q.numel(), k.numel()
     _check(lib.rlkv_prompt_attention_backward(prompt, layer, *_prompt_args(prompt, q, k, v, q_starts, k_starts, prefix), _room(out, n_q),
                                               _room(lse, q.shape[0] * q.shape[1], "float32"), _room(dout, n_q), _room(dq, n_q),
-                                              _room(dk, n_k), _room(dv, n_k), _stream(stream, q)))
+                                              _room(dk, n_k), _room(dv, n_k),
+                                              _stream_of(stream, prompt, (q, k, v, q_starts, k_starts, prefix, out, lse, dout, dq, dk, dv))))
 
 
 def rlkv_prompt_kernel_status(prompt) -> int:

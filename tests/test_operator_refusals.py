@@ -230,3 +230,30 @@ def test_tables_of_other_types_are_refused(binding):
         calls += [lambda table=table: b.rlkv_rotary_table(np.ones(64), 10, table, stream=0),
                   lambda table=table: b.rlkv_paged_set_rotary(16, table, 10, 128)]
     without_the_library(b, calls, ValueError)
+
+
+def test_tensors_of_another_gpu_are_refused(binding, monkeypatch):
+    """Every tensor of a call has to be on the GPU of its handle; where the handle is an address alone, on one GPU."""
+    b, away = binding, 1
+    monkeypatch.setattr(b, "_ptr", lambda x: 0 if x is None else x.data_ptr())
+    on_gpu = b._handle(16, 1, 2, 8, 128)
+    on_gpu.device = 0
+    q, k, starts, lse = Rows((4, 8, 128)), Rows((4, 2, 128)), Rows((2,), size=4, whole=True), of_type((4, 8), torch.float32)
+    prefix = Rows((1,), size=4, whole=True)
+
+    def elsewhere(x):
+        y = Rows(x.shape, size=x.size, device=away, whole=x.whole)
+        y.dtype = x.dtype
+        return y
+
+    kinds = [((q, k, k, q), lambda h, a: b.rlkv_paged_append_rotated(h, 0, [0, 1, 2, 3], *a, stream=0)),
+             ((q, k, k, q, k), lambda h, a: b.rlkv_paged_prefill_rotated(h, 0, 0, *a[:3], 4, *a[3:], stream=0)),
+             ((q, k, k, starts, starts, prefix, q, lse), lambda h, a: b.rlkv_prompt_attention(h, 0, *a, stream=0)),
+             ((q, k, k, starts, starts, prefix, q, lse, q, q, k, k), lambda h, a: b.rlkv_prompt_attention_backward(h, 0, *a, stream=0))]
+    calls = []
+    for args, call in kinds:
+        for i in range(len(args)):
+            given = tuple(elsewhere(x) if i == j else x for j, x in enumerate(args))
+            calls += [lambda call=call, given=given, h=h: call(h, given) for h in (on_gpu, 16)]
+        calls.append(lambda call=call, given=tuple(map(elsewhere, args)): call(on_gpu, given))
+    without_the_library(b, calls, ValueError)

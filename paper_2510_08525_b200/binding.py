@@ -129,11 +129,34 @@ def _ptr(x) -> int:
     return x.data_ptr()
 
 
-def _stream(s, of=None) -> int:
-    """A stream's handle; None: the current stream, of the GPU that holds the tensor `of` where one is given."""
+class Handle(int):
+    """The address of a cache or prompt handle, with the shape and the GPU it was created with: what a call reads and writes
+    goes by them, so they are what the call's arrays are checked against.  (An address alone, like a tensor's, is taken as it is.)"""
+
+
+def _handle(address, layers, kv_heads, q_heads, head_dim) -> Handle:
+    h = Handle(address)
+    h.layers, h.kv_heads, h.q_heads, h.head_dim = layers, kv_heads, q_heads, head_dim
+    torch = sys.modules.get("torch")  # (the library creates on the current device)
+    h.device = torch.cuda.current_device() if torch is not None and torch.cuda.is_available() else None
+    return h
+
+
+def _stream(s, *of) -> int:
+    """A stream's handle.  None: the current stream of the call's GPU -- that of the first of `of` that knows one, a Handle or a
+    tensor in device memory, else the current device -- so that the calls on one cache go to one stream."""
     if s is None:
         import torch
-        device = torch.cuda.current_device() if of is None or isinstance(of, int) else of.get_device()
+        device = None
+        for x in of:
+            if isinstance(x, Handle):
+                device = x.device
+            elif x is not None and not isinstance(x, int) and getattr(x, "is_cuda", False):
+                device = x.get_device()
+            if device is not None:
+                break
+        if device is None:
+            device = torch.cuda.current_device()
         # the raw handle: building the Stream object takes several microseconds, as long as a small call
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is not None:
@@ -153,19 +176,6 @@ def _host(a) -> int:
         return ctypes.addressof(_Byte.from_buffer(a))
     except (TypeError, ValueError):  # read-only, or empty
         return a.ctypes.data
-
-
-class Handle(int):
-    """The address of a paged cache or prompt handle, with the shape and the GPU it was created with: what a call reads and writes
-    goes by them, so they are what the call's arrays are checked against.  (An address alone, like a tensor's, is taken as it is.)"""
-
-
-def _handle(address, layers, kv_heads, q_heads, head_dim) -> Handle:
-    h = Handle(address)
-    h.layers, h.kv_heads, h.q_heads, h.head_dim = layers, kv_heads, q_heads, head_dim
-    torch = sys.modules.get("torch")  # (the library creates on the current device)
-    h.device = torch.cuda.current_device() if torch is not None and torch.cuda.is_available() else None
-    return h
 
 
 def _mask(head_is_full) -> np.ndarray:
@@ -191,7 +201,7 @@ def rlkv_cache_create(layers, kv_heads, q_heads, head_dim, batch, max_len, head_
     handle = _vp(0)
     _check(lib.rlkv_cache_create(ctypes.byref(handle), layers, kv_heads, q_heads, head_dim, batch, max_len,
                                  m.ctypes.data, sink, window, _ptr(device_buf), device_buf_bytes))
-    return int(handle.value)
+    return _handle(handle.value, layers, kv_heads, q_heads, head_dim)
 
 
 def rlkv_cache_size_fp8(layers, kv_heads, q_heads, head_dim, batch, max_len, head_is_full, sink, window) -> int:
@@ -215,7 +225,7 @@ def rlkv_cache_create_fp8(layers, kv_heads, q_heads, head_dim, batch, max_len, h
     _check(lib.rlkv_cache_create_fp8(ctypes.byref(handle), layers, kv_heads, q_heads, head_dim, batch, max_len,
                                      m.ctypes.data, sink, window, ks.ctypes.data, vs.ctypes.data,
                                      _ptr(device_buf), device_buf_bytes))
-    return int(handle.value)
+    return _handle(handle.value, layers, kv_heads, q_heads, head_dim)
 
 
 def rlkv_cache_destroy(cache) -> None:
@@ -223,31 +233,31 @@ def rlkv_cache_destroy(cache) -> None:
 
 
 def rlkv_cache_reset(cache, stream=None) -> None:
-    _check(lib.rlkv_cache_reset(cache, _stream(stream)))
+    _check(lib.rlkv_cache_reset(cache, _stream(stream, cache)))
 
 
 def rlkv_append(cache, layer, k, v, stream=None) -> None:
-    _check(lib.rlkv_append(cache, layer, _ptr(k), _ptr(v), _stream(stream)))
+    _check(lib.rlkv_append(cache, layer, _ptr(k), _ptr(v), _stream(stream, cache, k)))
 
 
 def rlkv_prefill(cache, layer, k, v, n_tokens, stream=None) -> None:
-    _check(lib.rlkv_prefill(cache, layer, _ptr(k), _ptr(v), n_tokens, _stream(stream)))
+    _check(lib.rlkv_prefill(cache, layer, _ptr(k), _ptr(v), n_tokens, _stream(stream, cache, k)))
 
 
 def rlkv_decode_attention(cache, layer, q, out, stream=None) -> None:
-    _check(lib.rlkv_decode_attention(cache, layer, _ptr(q), _ptr(out), _stream(stream)))
+    _check(lib.rlkv_decode_attention(cache, layer, _ptr(q), _ptr(out), _stream(stream, cache, q)))
 
 
 def rlkv_append_overlapped(cache, layer, k, v, stream=None) -> None:
-    _check(lib.rlkv_append_overlapped(cache, layer, _ptr(k), _ptr(v), _stream(stream)))
+    _check(lib.rlkv_append_overlapped(cache, layer, _ptr(k), _ptr(v), _stream(stream, cache, k)))
 
 
 def rlkv_decode_attention_overlapped(cache, layer, q, out, stream=None) -> None:
-    _check(lib.rlkv_decode_attention_overlapped(cache, layer, _ptr(q), _ptr(out), _stream(stream)))
+    _check(lib.rlkv_decode_attention_overlapped(cache, layer, _ptr(q), _ptr(out), _stream(stream, cache, q)))
 
 
 def rlkv_layer_step_overlapped(cache, layer, k, v, q, out, stream=None) -> None:
-    _check(lib.rlkv_layer_step_overlapped(cache, layer, _ptr(k), _ptr(v), _ptr(q), _ptr(out), _stream(stream)))
+    _check(lib.rlkv_layer_step_overlapped(cache, layer, _ptr(k), _ptr(v), _ptr(q), _ptr(out), _stream(stream, cache, k)))
 
 
 def rlkv_debug_standin(dst, src, nbytes, after, produce, produce_src, produce_bytes, overlap, stream=None) -> None:
@@ -258,7 +268,7 @@ def rlkv_debug_standin(dst, src, nbytes, after, produce, produce_src, produce_by
 def rlkv_decode_attention_static_scratch(cache, layer, q, out, stream=None) -> None:
     """rlkv_decode_attention with the kernel's work area in the library's static device array;
     the call allocates nothing (see include/rlkv.h for who needs that and for the limits)."""
-    _check(lib.rlkv_decode_attention_static_scratch(cache, layer, _ptr(q), _ptr(out), _stream(stream)))
+    _check(lib.rlkv_decode_attention_static_scratch(cache, layer, _ptr(q), _ptr(out), _stream(stream, cache, q)))
 
 
 def rlkv_static_scratch_bytes() -> int:
@@ -268,7 +278,7 @@ def rlkv_static_scratch_bytes() -> int:
 def rlkv_decode_mixed_attention(cache, layer, q, alpha, out, stream=None) -> None:
     """Eq. 1: alpha[h] * full attention + (1 - alpha[h]) * sink+window attention over a layer whose
     heads are all full.  alpha: device fp32 [kv_heads]."""
-    _check(lib.rlkv_decode_mixed_attention(cache, layer, _ptr(q), _ptr(alpha), _ptr(out), _stream(stream)))
+    _check(lib.rlkv_decode_mixed_attention(cache, layer, _ptr(q), _ptr(alpha), _ptr(out), _stream(stream, cache, q)))
 
 
 def rlkv_set_output_bf16(cache, on) -> None:
@@ -284,11 +294,11 @@ def rlkv_paged_set_output_bf16(cache, on) -> None:
 
 
 def rlkv_step(cache, k, v, q, out, stream=None) -> None:
-    _check(lib.rlkv_step(cache, _ptr(k), _ptr(v), _ptr(q), _ptr(out), _stream(stream)))
+    _check(lib.rlkv_step(cache, _ptr(k), _ptr(v), _ptr(q), _ptr(out), _stream(stream, cache, k)))
 
 
 def rlkv_step_host(cache, k_host, v_host, q_host, out_host, stream=None) -> None:
-    _check(lib.rlkv_step_host(cache, _ptr(k_host), _ptr(v_host), _ptr(q_host), _ptr(out_host), _stream(stream)))
+    _check(lib.rlkv_step_host(cache, _ptr(k_host), _ptr(v_host), _ptr(q_host), _ptr(out_host), _stream(stream, cache)))
 
 
 def rlkv_length(cache, layer) -> int:
@@ -455,11 +465,11 @@ def rlkv_paged_seq_close(cache, slot) -> None:
 
 def rlkv_paged_append(cache, layer, slots, k, v, stream=None) -> None:
     s = _slots(slots)
-    _check(lib.rlkv_paged_append(cache, layer, s.ctypes.data, s.size, _ptr(k), _ptr(v), _stream(stream)))
+    _check(lib.rlkv_paged_append(cache, layer, s.ctypes.data, s.size, _ptr(k), _ptr(v), _stream(stream, cache, k)))
 
 
 def rlkv_paged_prefill(cache, layer, slot, k, v, n_tokens, stream=None) -> None:
-    _check(lib.rlkv_paged_prefill(cache, layer, slot, _ptr(k), _ptr(v), n_tokens, _stream(stream)))
+    _check(lib.rlkv_paged_prefill(cache, layer, slot, _ptr(k), _ptr(v), n_tokens, _stream(stream, cache, k)))
 
 
 def _on_device(x) -> bool:
@@ -509,8 +519,7 @@ def _room(x, least, dtype="bfloat16"):
 def _stream_of(s, handle, tensors) -> int:
     """The stream of a call whose tensors have passed their other checks: they have to be on the handle's GPU, which the launch
     goes to.  (An address alone as handle: all on one GPU.)"""
-    device = getattr(handle, "device", None)
-    of = None
+    device, of = getattr(handle, "device", None), None
     for x in tensors:
         if x is None or isinstance(x, int):
             continue
@@ -519,7 +528,7 @@ def _stream_of(s, handle, tensors) -> int:
             device = at
         elif at != device:
             raise ValueError(f"a tensor on GPU {at} in a call on GPU {device}")
-    return _stream(s, of)
+    return _stream(s, handle, of)
 
 
 def _size(x) -> int:
@@ -544,7 +553,7 @@ def _check_table(table, rot_dim, positions) -> None:
 def rlkv_rotary_table(inv_freq, positions, table, stream=None) -> None:
     f = np.ascontiguousarray(inv_freq, dtype=np.float64)
     _check_table(table, 2 * f.size, positions)
-    _check(lib.rlkv_rotary_table(f.ctypes.data, 2 * f.size, positions, _ptr(table), _stream(stream)))
+    _check(lib.rlkv_rotary_table(f.ctypes.data, 2 * f.size, positions, _ptr(table), _stream(stream, table)))
 
 
 def rlkv_paged_set_rotary(cache, table, positions, rot_dim, interleaved=False) -> None:
@@ -570,12 +579,12 @@ def rlkv_paged_prefill_rotated(cache, layer, slot, q, k, v, n_tokens, q_out, k_o
 
 def rlkv_paged_decode_attention(cache, layer, slots, q, out, stream=None) -> None:
     s = _slots(slots)
-    _check(lib.rlkv_paged_decode_attention(cache, layer, _host(s), s.size, _ptr(q), _ptr(out), _stream(stream)))
+    _check(lib.rlkv_paged_decode_attention(cache, layer, _host(s), s.size, _ptr(q), _ptr(out), _stream(stream, cache, q)))
 
 
 def rlkv_paged_step(cache, slots, k, v, q, out, stream=None) -> None:
     s = _slots(slots)
-    _check(lib.rlkv_paged_step(cache, s.ctypes.data, s.size, _ptr(k), _ptr(v), _ptr(q), _ptr(out), _stream(stream)))
+    _check(lib.rlkv_paged_step(cache, s.ctypes.data, s.size, _ptr(k), _ptr(v), _ptr(q), _ptr(out), _stream(stream, cache, k)))
 
 
 def rlkv_paged_length(cache, layer, slot) -> int:

@@ -257,3 +257,60 @@ def test_tensors_of_another_gpu_are_refused(binding, monkeypatch):
             calls += [lambda call=call, given=given, h=h: call(h, given) for h in (on_gpu, 16)]
         calls.append(lambda call=call, given=tuple(map(elsewhere, args)): call(on_gpu, given))
     without_the_library(b, calls, ValueError)
+
+
+def test_calls_on_one_handle_share_one_stream(binding, monkeypatch):
+    """Without a stream every call goes to the current stream of the handle's GPU, whatever device is current and whatever
+    kind of call it is: an append and the decode behind it are in order."""
+    b, seen = binding, {}
+
+    class Library:
+        def __getattr__(self, name):
+            def called(*args):
+                if "create" in name:
+                    args[0]._obj.value = 4096
+                else:
+                    seen.setdefault(name, set()).add(args[-1])
+                return 0
+            return called
+
+    current = [3]
+    monkeypatch.setattr(b, "lib", Library())
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 100 + device, raising=False)
+    mask, sizes = [1, 0], (1, 2, 8, 128)
+    locked = [b.rlkv_cache_create(*sizes, 1, 100, mask, 4, 60), b.rlkv_cache_create_fp8(*sizes, 1, 100, mask, 4, 60, [1, 1], [1, 1])]
+    paged = [b.rlkv_paged_create(*sizes, 2, 8, 100, mask, 4, 60), b.rlkv_paged_create_fp8(*sizes, 2, 8, 100, mask, 4, 60, [1, 1], [1, 1])]
+    prompt = b.rlkv_prompt_create(*sizes, 64, mask, 4, 60)
+    current[0] = 0
+    rows = lambda *shape: Rows(shape, device=3)  # noqa: E731
+    q, k, out = rows(1, 8, 128), rows(1, 2, 128), rows(1, 8, 128)
+    starts, lse = Rows((2,), size=4, device=3, whole=True), Rows((1, 8), size=4, device=3)
+    for h in locked:
+        for name in ("rlkv_append", "rlkv_append_overlapped"):
+            getattr(b, name)(h, 0, k, k)
+        for name in ("rlkv_decode_attention", "rlkv_decode_attention_overlapped", "rlkv_decode_attention_static_scratch"):
+            getattr(b, name)(h, 0, q, out)
+        b.rlkv_prefill(h, 0, k, k, 1)
+        b.rlkv_layer_step_overlapped(h, 0, k, k, q, out)
+        b.rlkv_decode_mixed_attention(h, 0, q, lse, out)
+        b.rlkv_step(h, k, k, q, out)
+        b.rlkv_step_host(h, 16, 16, 16, 16)
+        b.rlkv_cache_reset(h)
+    for h in paged:
+        for k_, q_, out_ in ((k, q, out), (16, 32, 64)):         # tensors, and addresses alone
+            b.rlkv_paged_append(h, 0, [0], k_, k_)
+            b.rlkv_paged_prefill(h, 0, 0, k_, k_, 1)
+            b.rlkv_paged_append_rotated(h, 0, [0], q_, k_, k_, out_)
+            b.rlkv_paged_prefill_rotated(h, 0, 0, q_, k_, k_, 1, out_)
+            b.rlkv_paged_decode_attention(h, 0, [0], q_, out_)
+            b.rlkv_paged_step(h, [0], k_, k_, q_, out_)
+    b.rlkv_prompt_attention(prompt, 0, q, k, k, starts, None, None, out, lse)
+    b.rlkv_prompt_attention_backward(prompt, 0, q, k, k, starts, None, None, out, lse, out, out, k, k)
+    b.rlkv_rotary_table(np.ones(64), 1, Rows((1, 64, 2), size=4, device=3))
+    assert len(seen) == 20 and all(streams == {103} for streams in seen.values()), seen
+    b.rlkv_paged_append(16, 0, [0], k, k)                          # an address alone: the tensors' GPU
+    b.rlkv_paged_decode_attention(16, 0, [0], 16, 16)              # nothing but addresses: the current device
+    b.rlkv_paged_append(paged[0], 0, [0], k, k, 7)
+    assert seen["rlkv_paged_append"] == {103, 7} and seen["rlkv_paged_decode_attention"] == {103, 100}

@@ -142,19 +142,17 @@ def _handle(address, layers, kv_heads, q_heads, head_dim) -> Handle:
     return h
 
 
-def _stream(s, *of) -> int:
-    """A stream's handle.  None: the current stream of the call's GPU -- that of the first of `of` that knows one, a Handle or a
-    tensor in device memory, else the current device -- so that the calls on one cache go to one stream."""
+def _stream(s, of=None, x=None) -> int:
+    """A stream's handle.  None: the current stream of the call's GPU, so that the calls on one cache go to one stream -- that of
+    `of`, a Handle or a tensor in device memory, else that of the tensor x, else the current device."""
     if s is None:
+        if isinstance(of, Handle) and of.device is not None:
+            device = of.device
+        else:
+            device = _gpu_of(of)
+            if device is None:
+                device = _gpu_of(x)
         import torch
-        device = None
-        for x in of:
-            if isinstance(x, Handle):
-                device = x.device
-            elif x is not None and not isinstance(x, int) and getattr(x, "is_cuda", False):
-                device = x.get_device()
-            if device is not None:
-                break
         if device is None:
             device = torch.cuda.current_device()
         # the raw handle: building the Stream object takes several microseconds, as long as a small call
@@ -165,6 +163,11 @@ def _stream(s, *of) -> int:
     if isinstance(s, int):
         return s
     return s.cuda_stream
+
+
+def _gpu_of(x):
+    """The GPU of a tensor in device memory, else None."""
+    return None if x is None or isinstance(x, int) or not getattr(x, "is_cuda", False) else x.get_device()
 
 
 _Byte = ctypes.c_ubyte
@@ -476,22 +479,27 @@ def _on_device(x) -> bool:
     return not isinstance(x, np.ndarray) and x.is_cuda
 
 
-def _heads(handle):
-    """q_heads, kv_heads and head_dim of a handle, zeros for an address alone."""
-    return (handle.q_heads, handle.kv_heads, handle.head_dim) if isinstance(handle, Handle) else (0, 0, 0)
+def _shape_of(handle, x):
+    """q_heads, kv_heads, head_dim and GPU that a call's tensors are held to: the handle's; of an address alone no heads are known
+    (0), and the GPU is that of the tensor x (None where x is an address too)."""
+    if isinstance(handle, Handle):
+        return handle.q_heads, handle.kv_heads, handle.head_dim, handle.device
+    return 0, 0, 0, _gpu_of(x)
 
 
-def _rows(x, least=1, heads=0, head_dim=0):
+def _rows(x, least=1, heads=0, head_dim=0, gpu=None):
     """(address, elements from token to token) of a bf16 [tokens][heads][head_dim] tensor of at least `least` tokens, which
-    may be a slice of a wider projection; an address alone stands for contiguous tokens.  `heads`: of the handle (0: unknown)."""
+    may be a slice of a wider projection; an address alone stands for contiguous tokens.  heads 0, gpu None: any."""
     if x is None or isinstance(x, int):
         return x or 0, 0
-    if not getattr(x, "is_cuda", False):
-        raise ValueError("a tensor in device memory is wanted")
-    token, head, one = x.stride()  # ValueError where it has other than three dimensions
+    try:
+        at, (token, head, one), (n, held, dim) = x.get_device(), x.stride(), x.shape  # ValueError: other than three dimensions
+    except (AttributeError, TypeError):
+        raise ValueError("a tensor in device memory is wanted") from None
+    if at < 0 or at != gpu and gpu is not None:
+        raise ValueError(f"a tensor in the memory of GPU {gpu} is wanted")
     if x.dtype is not sys.modules["torch"].bfloat16:
         raise ValueError("rows are bf16")
-    n, held, dim = x.shape
     if n < least:
         raise ValueError(f"{n} tokens where the call names {least}")
     if one != 1 or head != dim:
@@ -505,30 +513,17 @@ def _rows(x, least=1, heads=0, head_dim=0):
     return x.data_ptr(), token
 
 
-def _room(x, least, dtype="bfloat16"):
+def _room(x, least, dtype="bfloat16", gpu=None):
     """Address of a contiguous tensor in device memory of `least` elements or more of that type; or the address itself."""
     if x is None or isinstance(x, int):
         return x or 0
     if not getattr(x, "is_cuda", False) or x.dtype is not getattr(sys.modules["torch"], dtype) or x.numel() < least:
         raise RlkvError(RLKV_EINVAL, f"a tensor in device memory of {least} {dtype} elements is wanted")
+    if gpu is not None and x.get_device() != gpu:
+        raise ValueError(f"a tensor in the memory of GPU {gpu} is wanted")
     if not x.is_contiguous():
         raise ValueError("tensor must be contiguous")
     return x.data_ptr()
-
-
-def _stream_of(s, handle, tensors) -> int:
-    """The stream of a call whose tensors have passed their other checks: they have to be on the handle's GPU, which the launch
-    goes to.  (An address alone as handle: all on one GPU.)"""
-    device, of = getattr(handle, "device", None), None
-    for x in tensors:
-        if x is None or isinstance(x, int):
-            continue
-        of, at = x, x.get_device()
-        if device is None:
-            device = at
-        elif at != device:
-            raise ValueError(f"a tensor on GPU {at} in a call on GPU {device}")
-    return _stream(s, handle, of)
 
 
 def _size(x) -> int:
@@ -564,17 +559,17 @@ def rlkv_paged_set_rotary(cache, table, positions, rot_dim, interleaved=False) -
 def rlkv_paged_append_rotated(cache, layer, slots, q, k, v, q_out, stream=None) -> None:
     s = np.ascontiguousarray(slots, dtype=np.int32)
     n = s.size
-    hq, hkv, d = _heads(cache)
-    _check(lib.rlkv_paged_append_rotated(cache, layer, _host(s), n, *_rows(q, n, hq, d), *_rows(k, n, hkv, d), *_rows(v, n, hkv, d),
-                                         _room(q_out, _size(q)), _stream_of(stream, cache, (q, k, v, q_out))))
+    hq, hkv, d, gpu = _shape_of(cache, k)
+    _check(lib.rlkv_paged_append_rotated(cache, layer, _host(s), n, *_rows(q, n, hq, d, gpu), *_rows(k, n, hkv, d, gpu),
+                                         *_rows(v, n, hkv, d, gpu), _room(q_out, _size(q), gpu=gpu), _stream(stream, cache, k)))
 
 
 def rlkv_paged_prefill_rotated(cache, layer, slot, q, k, v, n_tokens, q_out, k_out=None, stream=None) -> None:
     n = n_tokens
-    hq, hkv, d = _heads(cache)
-    _check(lib.rlkv_paged_prefill_rotated(cache, layer, slot, *_rows(q, n, hq, d), *_rows(k, n, hkv, d), *_rows(v, n, hkv, d), n,
-                                          _room(q_out, _size(q)), _room(k_out, _size(k)),
-                                          _stream_of(stream, cache, (q, k, v, q_out, k_out))))
+    hq, hkv, d, gpu = _shape_of(cache, k)
+    _check(lib.rlkv_paged_prefill_rotated(cache, layer, slot, *_rows(q, n, hq, d, gpu), *_rows(k, n, hkv, d, gpu),
+                                          *_rows(v, n, hkv, d, gpu), n, _room(q_out, _size(q), gpu=gpu),
+                                          _room(k_out, _size(k), gpu=gpu), _stream(stream, cache, k)))
 
 
 def rlkv_paged_decode_attention(cache, layer, slots, q, out, stream=None) -> None:
@@ -645,36 +640,42 @@ def rlkv_prompt_destroy(prompt) -> None:
     _check(lib.rlkv_prompt_destroy(prompt))
 
 
-def _prompt_args(prompt, q, k, v, q_starts, k_starts, prefix):
-    ints = [x for x in (q_starts, k_starts, prefix) if x is not None]
-    if not all(map(_on_device, ints)):
-        raise ValueError("q_starts, k_starts and prefix are read on the device")
+def _prompt_args(prompt, gpu, q, k, v, q_starts, k_starts, prefix):
+    int32 = sys.modules["torch"].int32
+    for x in (q_starts, k_starts, prefix):
+        if x is None:
+            continue
+        if not _on_device(x):
+            raise ValueError("q_starts, k_starts and prefix are read on the device")
+        if x.dtype is not int32:
+            raise ValueError("q_starts, k_starts and prefix are int32")
+        if gpu is not None and x.get_device() != gpu:
+            raise ValueError(f"a tensor in the memory of GPU {gpu} is wanted")
     n_docs = q_starts.numel() - 1
     if k_starts is not None and k_starts.numel() != n_docs + 1 or prefix is not None and prefix.numel() != n_docs:
         raise ValueError("k_starts must have as many entries as q_starts, prefix one less")
-    if any(x.element_size() != 4 or x.is_floating_point() for x in ints):
-        raise ValueError("q_starts, k_starts and prefix are int32")
     if k.shape != v.shape:
         raise ValueError("k and v must have the same shape")
-    hq, hkv, d = _heads(prompt)
-    return (*_rows(q, 0, hq, d), *_rows(k, 0, hkv, d), *_rows(v, 0, hkv, d), q.shape[0], k.shape[0], _ptr(q_starts), _ptr(k_starts),
-            n_docs, _ptr(prefix))
+    hq, hkv, d, _ = _shape_of(prompt, q)
+    return (*_rows(q, 0, hq, d, gpu), *_rows(k, 0, hkv, d, gpu), *_rows(v, 0, hkv, d, gpu), q.shape[0], k.shape[0], _ptr(q_starts),
+            _ptr(k_starts), n_docs, _ptr(prefix))
 
 
 def rlkv_prompt_attention(prompt, layer, q, k, v, q_starts, k_starts, prefix, out, lse, stream=None) -> None:
     """q, k, v: [tokens][heads][head_dim], possibly slices of one projection's output; q_starts, k_starts, prefix: int32."""
-    _check(lib.rlkv_prompt_attention(prompt, layer, *_prompt_args(prompt, q, k, v, q_starts, k_starts, prefix), _room(out, q.numel()),
-                                     _room(lse, q.shape[0] * q.shape[1], "float32"),
-                                     _stream_of(stream, prompt, (q, k, v, q_starts, k_starts, prefix, out, lse))))
+    gpu = _shape_of(prompt, q)[3]
+    _check(lib.rlkv_prompt_attention(prompt, layer, *_prompt_args(prompt, gpu, q, k, v, q_starts, k_starts, prefix),
+                                     _room(out, q.numel(), gpu=gpu), _room(lse, q.shape[0] * q.shape[1], "float32", gpu),
+                                     _stream(stream, prompt, q)))
 
 
 def rlkv_prompt_attention_backward(prompt, layer, q, k, v, q_starts, k_starts, prefix, out, lse, dout, dq, dk, dv,
                                    stream=None) -> None:
-    n_q, n_k = q.numel(), k.numel()
-    _check(lib.rlkv_prompt_attention_backward(prompt, layer, *_prompt_args(prompt, q, k, v, q_starts, k_starts, prefix), _room(out, n_q),
-                                              _room(lse, q.shape[0] * q.shape[1], "float32"), _room(dout, n_q), _room(dq, n_q),
-                                              _room(dk, n_k), _room(dv, n_k),
-                                              _stream_of(stream, prompt, (q, k, v, q_starts, k_starts, prefix, out, lse, dout, dq, dk, dv))))
+    n_q, n_k, gpu = q.numel(), k.numel(), _shape_of(prompt, q)[3]
+    _check(lib.rlkv_prompt_attention_backward(prompt, layer, *_prompt_args(prompt, gpu, q, k, v, q_starts, k_starts, prefix),
+                                              _room(out, n_q, gpu=gpu), _room(lse, q.shape[0] * q.shape[1], "float32", gpu),
+                                              _room(dout, n_q, gpu=gpu), _room(dq, n_q, gpu=gpu), _room(dk, n_k, gpu=gpu),
+                                              _room(dv, n_k, gpu=gpu), _stream(stream, prompt, q)))
 
 
 def rlkv_prompt_kernel_status(prompt) -> int:

@@ -378,6 +378,11 @@ int rlkv_paged_kernel_status(rlkv_paged* cache, int* status_out);
 int rlkv_debug_paged_schedule(const int* lens, int n, int n_full, int n_comp, int cap, int ctas,
                               int item_tiles, int* n_items_out, int* delivered_out,
                               int* expected_out, int* complete_out);
+/* Host-only check of how rlkv_paged_decode_attention (in_step: a layer's launch of rlkv_paged_step) cuts such a launch
+ * on `ctas` CTAs: the tiles of its smallest work items and how many items there are.  fp8: an 8-bit cache; scored: with
+ * capped or biased scores. */
+int rlkv_debug_paged_cut(const int* lens, int n, int n_full, int n_comp, int cap, int ctas, int fp8, int scored, int in_step,
+                         int* item_tiles_out, int* n_items_out);
 
 /* ---- attention over whole prompts -------------------------------------------------------------------
  * What a prompt (or a training sample) needs before its tokens are decoded: every token attends the tokens

@@ -84,6 +84,7 @@ SIGNATURES = {
     "rlkv_prompt_attention_backward": (_ci, [_vp, _ci, _vp, _i64, _vp, _i64, _vp, _i64, _ci, _ci, _vp, _vp, _ci, _vp, _vp, _vp, _vp,
                                              _vp, _vp, _vp, _vp]),
     "rlkv_prompt_kernel_status": (_ci, [_vp, ctypes.POINTER(_ci)]),
+    "rlkv_debug_paged_cut": (_ci, [_vp, _ci, _ci, _ci, _ci, _ci, _ci, _ci, _ci, ctypes.POINTER(_ci), ctypes.POINTER(_ci)]),
     "rlkv_debug_paged_schedule": (_ci, [_vp, _ci, _ci, _ci, _ci, _ci, _ci, ctypes.POINTER(_ci), _vp, _vp, _vp]),
 }
 
@@ -682,6 +683,14 @@ def rlkv_prompt_kernel_status(prompt) -> int:
     out = _ci(0)
     _check(lib.rlkv_prompt_kernel_status(prompt, ctypes.byref(out)))
     return int(out.value)
+
+
+def rlkv_debug_paged_cut(lens, n_full, n_comp, cap, ctas, fp8=False, scored=False, in_step=False):
+    """Returns (tiles of the smallest work items, number of items)."""
+    ln, item_tiles, n_items = _slots(lens), _ci(0), _ci(0)
+    _check(lib.rlkv_debug_paged_cut(ln.ctypes.data, ln.size, n_full, n_comp, cap, ctas, int(fp8), int(scored), int(in_step),
+                                    ctypes.byref(item_tiles), ctypes.byref(n_items)))
+    return int(item_tiles.value), int(n_items.value)
 
 
 def rlkv_debug_paged_schedule(lens, n_full, n_comp, cap, ctas, item_tiles):

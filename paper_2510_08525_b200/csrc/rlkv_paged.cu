@@ -634,6 +634,32 @@ uint64_t rlkv::paged_launch_count(const rlkv_paged* p) { return p ? p->launches 
 
 extern "C" {
 
+// The cut of a launch that serves one layer: `most` the largest "smallest work item", real_tiles the tiles that exist (the
+// schedule also spans those past a shorter sequence's end), scored: with capped or biased scores.
+static Schedule layer_schedule(int full, int tiles_full, int comp, int tiles_comp, long long real_tiles, int grid, int most, bool scored,
+                               bool in_step)
+{
+    int item_tiles = (int)(real_tiles / grid);
+    if (item_tiles > most) item_tiles = most;
+    if (item_tiles < kMinItemTiles) item_tiles = kMinItemTiles;
+    Schedule s = make_schedule(full, tiles_full, comp, tiles_comp, grid, item_tiles);
+    // A launch of few tiles whose items are a few more than CTAs would run a second wave for them: items one tile longer give
+    // every CTA at most one (one sequence of 8192 tokens, 6 of 8 heads full: 20.3 -> 18.0 us on the GPU).  Only where every
+    // tile of the span exists: a ragged batch spans the longest sequence's tiles for all, and one wave over that span would
+    // leave the long sequence to few CTAs (8 heads in 16 bits: one sequence of 4096 tokens beside 79 of 50, all in rings of
+    // 4096: 141 us so, 18 cut as without scores; one of 8000 beside 7 of 700, 4 heads full: 28 and 20).  Only with capped or
+    // biased scores: launches without them keep the cuts, and with them the bits, that they have always had.
+    if (scored && !in_step && s.R == 0 && s.n_items > grid && item_tiles < most && s.T == real_tiles)
+        s = make_schedule(full, tiles_full, comp, tiles_comp, grid, ++item_tiles);
+    // a launch too small for bands: no full unit in more than kPagedMaxFanIn pieces (their merge by one
+    // CTA, not the bytes, would set the time)
+    if (s.R == 0 && full > 0 && tiles_full > kPagedMaxFanIn * item_tiles && (!in_step || s.n_items < grid)) {
+        item_tiles = (tiles_full + kPagedMaxFanIn - 1) / kPagedMaxFanIn;
+        s = make_schedule(full, tiles_full, comp, tiles_comp, grid, item_tiles);
+    }
+    return s;
+}
+
 // One decode launch (arguments checked by the caller).  `half`: which copy of tickets, claim counter
 // and partials; `overlap`, `dep_wait`: as for the lock-step cache (launch_decode, decode_kernel);
 // `in_step`: the launch belongs to rlkv_paged_step (coarser items: its neighbours hide its tail).
@@ -725,25 +751,10 @@ static int paged_decode(rlkv_paged* p, int layer, const int* slots, int n, const
         pa.scales = dev_at<float>(p, p->off_scales) + (size_t)2 * p->layers * p->kv_heads;
         half = 0;
     } else {
-    int item_tiles = (int)(real_tiles / grid);
     // (a tile of 8-bit pages is half the bytes, so the same grain in time is twice the tiles)
     const int most = (in_step ? kPagedItemTilesStep : p->item_tiles) * (p->fp8 ? 2 : 1);
-    if (item_tiles > most) item_tiles = most;
-    if (item_tiles < kMinItemTiles) item_tiles = kMinItemTiles;
-    a.sched = make_schedule(n * a.n_full, tiles_full, n * a.n_comp, tiles_comp, grid, item_tiles);
-    // A launch of few tiles whose items are a few more than CTAs would run a second wave for them: items one tile longer give
-    // every CTA at most one (one sequence of 8192 tokens, 6 of 8 heads full: 20.3 -> 18.0 us).  Only with capped or biased
-    // scores: launches without them keep the cuts, and with them the bits, that they have always had.
-    if ((p->softcap != 0.f || p->biased) && !in_step && a.sched.R == 0 && a.sched.n_items > grid && item_tiles < most) {
-        item_tiles = (a.sched.T + grid - 1) / grid;
-        a.sched = make_schedule(n * a.n_full, tiles_full, n * a.n_comp, tiles_comp, grid, item_tiles);
-    }
-    // a launch too small for bands: no full unit in more than kPagedMaxFanIn pieces (their merge by one
-    // CTA, not the bytes, would set the time)
-    if (a.sched.R == 0 && a.n_full > 0 && tiles_full > kPagedMaxFanIn * item_tiles && (!in_step || a.sched.n_items < grid)) {
-        item_tiles = (tiles_full + kPagedMaxFanIn - 1) / kPagedMaxFanIn;
-        a.sched = make_schedule(n * a.n_full, tiles_full, n * a.n_comp, tiles_comp, grid, item_tiles);
-    }
+    a.sched = layer_schedule(n * a.n_full, tiles_full, n * a.n_comp, tiles_comp, real_tiles, grid, most,
+                             p->softcap != 0.f || p->biased, in_step);
     if (grid > a.sched.n_items) grid = a.sched.n_items;
     if (a.sched.n_slots > p->max_items) return RLKV_ESCRATCH;  // cannot happen: the scratch is sized for it
     a.partials = dev_at<float>(p, p->off_partials) + (size_t)half * p->max_items * partial_floats(p->head_dim, a.group);
@@ -1024,6 +1035,27 @@ int rlkv_paged_debug_export_head(rlkv_paged* p, int layer, int slot, int kv_head
         }
         *rows_out = cap;
     }
+    return RLKV_OK;
+}
+
+int rlkv_debug_paged_cut(const int* lens, int n, int n_full, int n_comp, int cap, int ctas, int fp8, int scored, int in_step,
+                         int* item_tiles_out, int* n_items_out)
+{
+    if (!lens || n < 1 || n > kMaxPagedBatch || n_full < 0 || n_comp < 0 || n_full + n_comp < 1 || cap < 1 || ctas < 1 ||
+        !item_tiles_out || !n_items_out)
+        return RLKV_EINVAL;
+    int longest = 0;
+    long long real_tiles = 0;
+    for (int i = 0; i < n; ++i) {
+        if (lens[i] < 1) return RLKV_EINVAL;
+        if (lens[i] > longest) longest = lens[i];
+        real_tiles += (long long)n_full * ((lens[i] + kTile - 1) / kTile) + (long long)n_comp * (((lens[i] < cap ? lens[i] : cap) + kTile - 1) / kTile);
+    }
+    const int tf = (longest + kTile - 1) / kTile, tc = ((longest < cap ? longest : cap) + kTile - 1) / kTile;
+    const int most = (in_step ? kPagedItemTilesStep : kPagedItemTiles) * (fp8 ? 2 : 1);
+    const Schedule s = layer_schedule(n * n_full, tf, n * n_comp, tc, real_tiles, ctas, most, scored != 0, in_step != 0);
+    *item_tiles_out = s.min_sz;
+    *n_items_out = s.n_items;
     return RLKV_OK;
 }
 

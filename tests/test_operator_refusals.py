@@ -314,3 +314,19 @@ def test_calls_on_one_handle_share_one_stream(binding, monkeypatch):
     b.rlkv_paged_decode_attention(16, 0, [0], 16, 16)              # nothing but addresses: the current device
     b.rlkv_paged_append(paged[0], 0, [0], k, k, 7)
     assert seen["rlkv_paged_append"] == {103, 7} and seen["rlkv_paged_decode_attention"] == {103, 100}
+
+
+def test_a_prompt_of_more_queries_than_keys_is_refused(binding):
+    """The call turns as many queries as there are keys; the rest of the returned queries would be whatever the memory held."""
+    import paper_2510_08525_b200.harness as hz
+
+    class Tensor(Rows):
+        def dim(self):
+            return len(self.shape)
+
+    cache = hz.PagedCache.__new__(hz.PagedCache)
+    cache.handle, cache.q_heads, cache.kv_heads, cache.head_dim, cache.device = None, 8, 2, 128, torch.device("cuda:0")
+    q, k = (lambda n: Tensor((n, 8, 128))), (lambda n: Tensor((n, 2, 128)))
+    for args in ((q(5), k(4), k(4)), (q(3), k(4), k(4)), (q(4), k(4), k(5)), (q(4), k(4), k(3))):
+        with pytest.raises(ValueError, match="same tokens"):
+            cache.prefill_rotated(0, 0, *args)

@@ -555,6 +555,8 @@ def rlkv_rotary_table(inv_freq, positions, table, stream=None) -> None:
 def rlkv_paged_set_rotary(cache, table, positions, rot_dim, interleaved=False) -> None:
     _check_table(table, min(rot_dim, 128), positions)
     _check(lib.rlkv_paged_set_rotary(cache, _ptr(table), positions, rot_dim, int(bool(interleaved))))
+    if isinstance(cache, Handle):
+        cache.rotary = table  # (the launches read it: it lives as long as the handle, or until another is set)
 
 
 def rlkv_paged_append_rotated(cache, layer, slots, q, k, v, q_out, stream=None) -> None:

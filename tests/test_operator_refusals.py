@@ -330,3 +330,33 @@ def test_a_prompt_of_more_queries_than_keys_is_refused(binding):
     for args in ((q(5), k(4), k(4)), (q(3), k(4), k(4)), (q(4), k(4), k(5)), (q(4), k(4), k(3))):
         with pytest.raises(ValueError, match="same tokens"):
             cache.prefill_rotated(0, 0, *args)
+
+
+def test_a_handle_keeps_its_table_of_angles(binding, monkeypatch):
+    """The rotated calls read the table: its memory is not given back while a handle has it."""
+    import gc
+    import weakref
+    b = binding
+
+    class Library:
+        def rlkv_paged_set_rotary(self, cache, table, positions, *args):
+            return 0 if positions >= 0 else b.RLKV_EINVAL
+
+        def rlkv_strerror(self, rc):
+            return b"refused"
+
+    monkeypatch.setattr(b, "lib", Library())
+    monkeypatch.setattr(b, "_ptr", lambda x: 0 if x is None else x.data_ptr())
+    h, table = b._handle(16, 1, 2, 8, 128), Rows((10, 64, 2), size=4)
+    alive = weakref.ref(table)
+    b.rlkv_paged_set_rotary(h, table, 10, 128)
+    del table
+    gc.collect()
+    assert alive() is not None
+    with pytest.raises(b.RlkvError):
+        b.rlkv_paged_set_rotary(h, None, -1, 128)                  # refused: the one before stays set
+    gc.collect()
+    assert alive() is not None
+    b.rlkv_paged_set_rotary(h, None, 0, 128)
+    gc.collect()
+    assert alive() is None

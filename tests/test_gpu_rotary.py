@@ -170,6 +170,40 @@ def check_codes(cache, plain, a, b, want, size, k_scale, S, W):
         assert bool(((x - w).abs() <= tol).all())
 
 
+@pytest.mark.parametrize("Hkv,Hq,S,W,mask,rot,interleaved,sliced,lens", [
+    (4, 28, 16, 112, "0110", 64, False, False, [129, 700, 1]), (3, 24, 4, 60, "010", 128, True, True, [64, 65, 3]),
+    (2, 2, 0, 5, "10", 112, False, True, [60, 127]), (1, 8, 100, 200, "0", 16, True, False, [250])])
+def test_single_tokens_in_8_bits(rl, hz, cuda_device, Hkv, Hq, S, W, mask, rot, interleaved, sliced, lens):
+    """The codes of 140 tokens appended one by one behind prompts: K codes of the fp32 rotation, V codes those of the plain append,
+    across page borders, over ring wraps, on sequences at different places of their pages."""
+    dev, mask, more, D = cuda_device, [int(c) for c in mask], 140, 128
+    max_len, pages = max(lens) + more, sum((n + more + 63) // 64 for n in lens)
+    k_scale, v_scale = [0.01 + 0.003 * h for h in range(Hkv)], [0.02 + 0.001 * h for h in range(Hkv)]
+    make = lambda: hz.PagedCache(1, Hkv, Hq, D, len(lens), pages, max_len, mask, S, W, device=dev, k_scale=k_scale, v_scale=v_scale)  # noqa: E731
+    cache, plain = make(), make()
+    rl.rlkv_paged_set_rotary(cache.handle, make_table(rl, rot, max_len, dev), max_len, rot, interleaved)
+    give = fused if sliced else apart
+    slots, history = [], []
+    for i, n in enumerate(lens):
+        _, k, v = give(n, Hq, Hkv, D, 10 + i, dev)
+        a, b = cache.open_seq(), plain.open_seq()
+        slots.append((a, b))
+        rl.rlkv_paged_prefill_rotated(cache.handle, 0, a, None, k, v, n, None)
+        plain.prefill(0, b, k.contiguous(), v.contiguous())
+        history.append([rotate64(k, np.arange(n), rot, interleaved)])
+    for step in range(more):
+        q, k, v = give(len(lens), Hq, Hkv, D, 1000 + step, dev)
+        out = torch.empty((len(lens), Hq, D), dtype=torch.bfloat16, device=dev)
+        rl.rlkv_paged_append_rotated(cache.handle, 0, [a for a, _ in slots], q, k, v, out)
+        plain.append(0, [b for _, b in slots], k.contiguous(), v.contiguous())
+        want, size = rotate64(k, [n + step for n in lens], rot, interleaved)
+        for i, x in enumerate(history):
+            x.append((want[i:i + 1], size[i:i + 1]))
+    for (a, b), x in zip(slots, history):
+        check_codes(cache, plain, a, b, torch.cat([w for w, _ in x]), torch.cat([s for _, s in x]), k_scale, S, W)
+    assert cache.status() == 0
+
+
 def test_rotated_rows_are_attended(rl, hz, cuda_device):
     """Decode after rotated appends: products of rotated heads depend on the distance alone, so a history shifted by
     any number of tokens gives the same attention up to rounding."""

@@ -319,7 +319,8 @@ int rlkv_paged_prefill_rotated(rlkv_paged* cache, int layer, int slot, const voi
 /* Decode attention for n sequences of one layer, each over its own length, one launch for both
  * head classes and all lengths.  q: device bf16 [n][q_heads][head_dim]; out: device fp32
  * [n][q_heads][head_dim]; entry i belongs to slots[i] (HOST int[n]).  RLKV_EEMPTY if a listed
- * sequence holds no token in this layer. */
+ * sequence holds no token in this layer.  A captured call attends the sequences at the lengths they had at its
+ * capture, as often as it is replayed. */
 int rlkv_paged_decode_attention(rlkv_paged* cache, int layer, const int* slots, int n,
                                 const void* q, void* out, void* stream);
 /* One whole decode step for n sequences: one token appended to every layer of each, then every

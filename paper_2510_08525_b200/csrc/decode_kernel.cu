@@ -1545,8 +1545,11 @@ decode_kernel(const __grid_constant__ DecodeArgs args, const __grid_constant__ C
                     grid_dep_wait();
                     waited = true;
                 }
-                // the counter only ever grows; this launch's claims start at claim_base
-                const int k = sc.P + (int)(atomicAdd(a.claim_counter, 1u) - a.claim_base);
+                // A launch draws exactly n_items times: every item past the first P, and once more for every CTA.  Its last
+                // draw puts the counter back to zero for the next launch, so that a captured launch can be replayed.
+                const unsigned int drawn = atomicAdd(a.claim_counter, 1u);
+                if (drawn == (unsigned int)sc.n_items - 1u) atomicExch(a.claim_counter, 0u);
+                const int k = sc.P + (int)drawn;
                 *claim_slot = k;
                 mbar_arrive(smem_u32(claim_full));
                 if (k >= sc.n_items) break;  // the producer stops asking once it has seen this answer

@@ -11,8 +11,8 @@
 //   tickets   int32 [layers][2*batch*kv_heads] (split bookkeeping, zero between launches; one per unit of a
 //             launch -- a whole-step launch numbers the units of all its layers in one list)
 //   tables    then LayerDesc[layers] (where each layer's regions start; for the step's append launch)
-//   status    int32 kernel status word, then two work-claim counters (they only grow; consecutive
-//             launches of a step alternate between them)
+//   status    int32 kernel status word, then two work-claim counters (zero between launches;
+//             consecutive launches of a step alternate between them)
 //   partials  float [2][max_slots][partial_floats]  (split-KV scratch; the two halves alternate too)
 //   staging   k, v, q (twice: calls alternate) and out of one whole step, for rlkv_step_host
 //   trace     uint64 [max_grid][40]  (debug trace of the decode kernel)
@@ -160,7 +160,6 @@ struct rlkv_cache {
     int out_bf16;            // results are stored as bf16 instead of fp32 (rlkv_set_output_bf16)
     int step_mode;           // rlkv_step: 0 chooses, 1 one decode launch per layer, 2 one for the whole step
     StepArgs step_args;      // the layer tables of a whole-step launch
-    unsigned int claims[2];  // value of each work-claim counter after the launches issued so far
     cudaStream_t in_stream, out_stream;  // rlkv_step_host: copies that run beside the kernels
     cudaEvent_t ev_step[2], ev_done;     // kernels of a call done with staging copy p / results copied out
     cudaEvent_t ev_in[4], ev_out[4];     // per chunk of layers: its inputs have arrived / its results are ready
@@ -330,10 +329,8 @@ int do_decode(rlkv_cache* c, int layer, const void* q, void* out, cudaStream_t s
                  (size_t)half * c->lay.max_items * partial_floats(c->head_dim, a.group);
     a.tickets = dev_at<int>(c, c->lay.off_tickets) + (size_t)layer * 2 * c->batch * c->kv_heads;
     a.claim_counter = dev_at<unsigned int>(c, c->lay.off_status) + 4 + half;
-    a.claim_base = c->claims[half];
     a.dep_wait = dep_wait;
     RLKV_CUDA(launch_decode(a, &c->tmap, c->head_dim, grid, c->stages, c->groups, s, overlap, alpha ? kModeMixed : kModePlain));
-    c->claims[half] += (unsigned int)a.sched.n_items;  // every CTA claims until it is told there is no more
     if (grid_out) *grid_out = grid;
     c->launches++;
     return RLKV_OK;
@@ -403,11 +400,9 @@ int do_decode_step(rlkv_cache* c, int l0, int l1, const void* q, void* out, cuda
     a.partials = dev_at<float>(c, c->lay.off_partials);                // both halves as one
     a.tickets = dev_at<int>(c, c->lay.off_tickets) + (size_t)l0 * 2 * c->batch * c->kv_heads;  // one per unit of the launch
     a.claim_counter = dev_at<unsigned int>(c, c->lay.off_status) + 4;
-    a.claim_base = c->claims[0];
     a.dep_wait = after_append ? 1 : 0;
     RLKV_CUDA(launch_decode(a, &c->tmap, c->head_dim, grid, c->stages, c->groups, s, after_append, kModeStep, nullptr, nullptr,
                             &st));
-    c->claims[0] += (unsigned int)a.sched.n_items;
     c->launches++;
     return RLKV_OK;
 }
@@ -469,7 +464,6 @@ int do_decode_static_scratch(rlkv_cache* c, int layer, const void* q, void* out,
     rc = static_scratch_address(c->device, &base);
     if (rc) return rc;
     a.claim_counter = reinterpret_cast<unsigned int*>(base);
-    a.claim_base = 0;
     a.dep_wait = 0;
     a.tickets = reinterpret_cast<int*>(base) + 2;
     a.partials = reinterpret_cast<float*>(base + head_bytes);
@@ -628,7 +622,6 @@ int rlkv_cache_create(rlkv_cache** out, int layers, int kv_heads, int q_heads, i
     c->step_mode = 0;
     c->fp8 = nullptr;
     c->fp8_staging = nullptr;
-    c->claims[0] = c->claims[1] = 0;
     c->in_stream = c->out_stream = nullptr;
     c->ev_step[0] = c->ev_step[1] = c->ev_done = nullptr;
     c->host_steps = 0;
@@ -861,7 +854,6 @@ int rlkv_cache_reset(rlkv_cache* c, void* stream)
     int rc = zero_state(c, static_cast<cudaStream_t>(stream));
     if (rc) return rc;
     std::fill(c->len.begin(), c->len.end(), 0);
-    c->claims[0] = c->claims[1] = 0;  // zero_state has cleared the counters on the device
     return RLKV_OK;
 }
 

@@ -285,8 +285,7 @@ struct DecodeArgs {
     float* out;                 // [batch][q_heads][head_dim]; bf16 elements instead of fp32 if out_bf16
     float* partials;            // [sched.n_slots][partial_floats]
     int* tickets;               // one per unit of this layer, zero between launches
-    unsigned int* claim_counter;  // items claimed beyond the first P, over all launches so far (never reset)
-    unsigned int claim_base;      // its value when this launch starts: every launch adds exactly sched.n_items
+    unsigned int* claim_counter;  // items claimed beyond the first P, zero between launches
     int dep_wait;               // how the launch is ordered against its predecessor in the stream (see the
                                 // first lines of decode_kernel and step_launch_mode): 0 ordinary, 1 it may run
                                 // beside the step's append launch, 2 it may run beside the decode launch before it

@@ -58,7 +58,6 @@ struct rlkv_paged {
     std::vector<int> free_pages;  // stack of physical pages
     std::vector<uint8_t> open;    // [max_seqs]
     size_t off_pool, off_tables, off_head_table, off_layer_desc, off_slopes, off_page_table, off_tickets, off_status, off_partials, total;
-    unsigned int claims[2];
     uint8_t* dev_base;
     bool owns_buffer;
     CUtensorMap tmap;
@@ -290,7 +289,7 @@ static int paged_create(rlkv_paged** out, int layers, int kv_heads, int q_heads,
     if (!p) return RLKV_ENOMEM;
     p->layers = layers; p->kv_heads = kv_heads; p->q_heads = q_heads; p->head_dim = head_dim;
     p->max_seqs = max_seqs; p->n_pages = n_pages; p->sink = sink; p->window = window; p->max_seq_len = max_seq_len;
-    p->claims[0] = p->claims[1] = 0; p->launches = 0; p->dev_base = nullptr; p->owns_buffer = false; p->out_bf16 = 0;
+    p->launches = 0; p->dev_base = nullptr; p->owns_buffer = false; p->out_bf16 = 0;
     p->step_mode = 0;
     p->softcap = 0.f; p->biased = p->has_slopes = false;
     p->rotary = nullptr; p->rotary_rows = p->rotary_dim = p->rotary_interleaved = 0;
@@ -732,7 +731,6 @@ static int paged_decode(rlkv_paged* p, int layer, const int* slots, int n, const
         a.partials = dev_at<float>(p, p->off_partials);
         a.tickets = dev_at<int>(p, p->off_tickets);
         a.claim_counter = dev_at<unsigned int>(p, p->off_status) + 4;
-        a.claim_base = p->claims[0];
         a.dep_wait = dep_wait;
         StepArgs& st = pa.step;
         st.head_of_slot = dev_at<int>(p, p->off_head_table);
@@ -760,7 +758,6 @@ static int paged_decode(rlkv_paged* p, int layer, const int* slots, int n, const
     a.partials = dev_at<float>(p, p->off_partials) + (size_t)half * p->max_items * partial_floats(p->head_dim, a.group);
     a.tickets = dev_at<int>(p, p->off_tickets) + (size_t)half * kMaxPagedBatch * p->kv_heads;
     a.claim_counter = dev_at<unsigned int>(p, p->off_status) + 4 + half;
-    a.claim_base = p->claims[half];
     a.dep_wait = dep_wait;
     }
     pa.page_table = dev_at<int>(p, p->off_page_table);
@@ -791,7 +788,6 @@ static int paged_decode(rlkv_paged* p, int layer, const int* slots, int n, const
     } else {
         RLKV_CUDA(launch_decode(a, &p->tmap, p->head_dim, grid, p->stages, p->groups, stream, overlap, kModePaged, &pa));
     }
-    p->claims[half] += (unsigned int)a.sched.n_items;
     p->launches++;
     if (grid_out) *grid_out = grid;
     return RLKV_OK;

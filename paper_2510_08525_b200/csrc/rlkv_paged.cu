@@ -642,14 +642,18 @@ static Schedule layer_schedule(int full, int tiles_full, int comp, int tiles_com
     if (item_tiles > most) item_tiles = most;
     if (item_tiles < kMinItemTiles) item_tiles = kMinItemTiles;
     Schedule s = make_schedule(full, tiles_full, comp, tiles_comp, grid, item_tiles);
-    // A launch of few tiles whose items are a few more than CTAs would run a second wave for them: items one tile longer give
-    // every CTA at most one (one sequence of 8192 tokens, 6 of 8 heads full: 20.3 -> 18.0 us on the GPU).  Only where every
-    // tile of the span exists: a ragged batch spans the longest sequence's tiles for all, and one wave over that span would
-    // leave the long sequence to few CTAs (8 heads in 16 bits: one sequence of 4096 tokens beside 79 of 50, all in rings of
-    // 4096: 141 us so, 18 cut as without scores; one of 8000 beside 7 of 700, 4 heads full: 28 and 20).  Only with capped or
-    // biased scores: launches without them keep the cuts, and with them the bits, that they have always had.
-    if (scored && !in_step && s.R == 0 && s.n_items > grid && item_tiles < most && s.T == real_tiles)
-        s = make_schedule(full, tiles_full, comp, tiles_comp, grid, ++item_tiles);
+    // A launch of few tiles whose items are more than CTAs would run a second wave for a few of them: items so long that
+    // every CTA gets at most one are faster, as long as they stay within `most` (passes over 8 heads in 16 bits, 6 full: one
+    // sequence of 8192 tokens 21.1 -> 19.5 us, of 6000 and 3000 21.3 -> 18.5; all full: of 4000 and 64 22.6 -> 16.5, three of
+    // 700 and one of 2000 21.8 -> 18.5; of 17 such batches, in 16 and in 8 bits, one was slower, 18.9 -> 20.3).  Past `most`
+    // the span of a ragged batch -- the longest sequence's tiles for every sequence -- would leave that sequence to few CTAs:
+    // one of 4096 tokens beside 79 of 50, all in rings of 4096, takes 143 us so and 79 cut as without scores.  Only with
+    // capped or biased scores: launches without them keep the cuts, and with them the bits, that they have always had.
+    const int one_wave = (s.T + grid - 1) / grid;
+    if (scored && !in_step && s.R == 0 && s.n_items > grid && one_wave <= most) {
+        item_tiles = one_wave;
+        s = make_schedule(full, tiles_full, comp, tiles_comp, grid, item_tiles);
+    }
     // a launch too small for bands: no full unit in more than kPagedMaxFanIn pieces (their merge by one
     // CTA, not the bytes, would set the time)
     if (s.R == 0 && full > 0 && tiles_full > kPagedMaxFanIn * item_tiles && (!in_step || s.n_items < grid)) {

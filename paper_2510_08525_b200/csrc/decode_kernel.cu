@@ -567,7 +567,8 @@ __device__ __forceinline__ void merge_units(const float* partials, float* out, i
 // where the approximate tanh instruction would be off by 2^-11 of it, too much in an exponent.  Scores are a handful of
 // instructions per 16 tokens and warp beside the K/V stream: a launch over 32 x 16384 tokens (1.07 GB) takes 171 us with
 // cap, slope or both against 168 us without; in 8 bits, where the arithmetic is closer to the stream, 16 ragged sequences
-// (199 MB) take 52 us against 49.
+// (199 MB) take 52 us against 49, and a whole step of 8 layers and 16 x 8192 tokens (1.62 GB) 298 to 306 against 285 (in 16 bits
+// 475 to 482 against 475).
 struct ScoreRule {
     float s, cap2, slope2;  // factor of q.k; cap and slope times log2(e) (slope2 0: no distance term, cap2 0: no cap)
     int last, sink, wrap;   // distance of row r: last - r, but newest - r of a ring row, plus the window where it is negative

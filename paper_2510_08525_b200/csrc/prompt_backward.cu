@@ -10,8 +10,9 @@
 // in a fixed order: no atomics on dQ, no fp32 copy of it in memory, the same bits on every run.  P and dS are written
 // to tensor memory as bf16 over S and dP and are the A operand of the second products straight from there.
 //
-// Measured (32 / 8 heads of 128, causal, 8192 tokens): stats 26 us (DRAM), rows 700 us, keys 810 us; 0.9 PFLOP/s of the five
-// products, 1.25 of the seven that run.  What bounds it: in `keys` the exponential unit (64 scores a thread, eight warps at
+// Measured (32 / 8 heads of 128, causal, 8192 tokens, in bursts): stats 26 us (DRAM), rows 700 us, keys 810 us; 0.9 PFLOP/s of the
+// five products, 1.25 of the seven that run.  With the forward pass 1985 us in bursts and 2220 to 2320 over a run of passes, under
+// the power cap.  What bounds it: in `keys` the exponential unit (64 scores a thread, eight warps at
 // once: 1024 cycles of the 1180 that P takes) in the chain S - P - dV - S of 2900 cycles beside 2048 of products; in `rows`
 // the same unit and the hand-overs between threads and products.
 #include "rlkv_prompt.cuh"
@@ -595,9 +596,10 @@ prompt_rows_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     const bool full_head = a.full[kv_head] != 0;
     // Where queries see few keys, or slopes leave them few that matter, the rounding of dS weighs as much in dQ as that of the
     // result: dS then goes into its product in two bf16 parts.  The first queries of a long document, whose gradients are the
-    // largest, are such queries, and cheap ones: 8192 tokens 697 -> 700 us, dQ off by 1.9e-3 of its norm instead of 2.4e-3 (one
+    // largest, are such queries, and cheap ones: 8192 tokens 697 -> 700 us (in bursts), dQ off by 1.9e-3 of its norm instead of 2.4e-3 (one
     // rounding of the exact gradient: 1.7e-3).  Up to 2048 keys: 712 us, 1.9e-3; for all, the fourth product would cost a quarter
-    // of the kernel's time (857 us).
+    // of the kernel's time (857 us).  The usual slopes, 2^(-8 (j + 1) / heads), are steep in this sense for every head, so a sample
+    // with a distance term pays that at every length.
     const int seen = full_head ? min(kn, n_tiles * kTok) : min(kn, a.sink + a.window);
     const float steepest = BIAS ? fmaxf(fabsf(a.slopes[sh.at.head[0]]), fabsf(a.slopes[sh.at.head[1]])) : 0.f;
     const bool in_two = seen <= kFewKeys || steepest * kFewKeys >= 1.f;

@@ -11,18 +11,20 @@
 //   warp 9           issues every tcgen05.mma (in order, so S of the next tile may overwrite P of this one)
 //
 // Tensor memory: S/P of the sub-tiles at columns 0 and 128, O at 256 and 256 + D.
-// Measured (32 / 8 heads of 128, causal): 8192 tokens 448 us, 1.23 PFLOP/s of visible products, 75 % of what a large
-// library product reaches here; half of a 128 x 128 x 128 score product's time is spent at the full rate of shared memory
-// (both operands come from there), and a sub-tile's chain -- products, softmax, hand-overs -- takes 3200 cycles where the
-// two sub-tiles' products take 2048: the chain bounds it.  24 documents of 333 tokens on average, half of the heads compressed,
-// capped: 118 us, two thirds of it set-up, first loads and results of CTAs that see two or three key tiles.  Tried and dropped: CTAs that
-// stay and claim items, with the next item's loads early (8 % and 19 % slower: results can then not go out as whole
-// rows, and the issuing warp runs out of registers); exponentials against the old maximum while the new one is looked for
-// (5 % slower); two threads per row in four softmax warpgroups, which halves a thread's work but adds an exchange of the
-// maxima to every tile (8192 tokens 481 us, 24 documents the same).
-// The running maximum of a row moves only when it would grow by more than 2^8 (its effect cancels in O / l; P <= 256 and
-// O, l are fp32), so the correction of O in tensor memory is rare after the first tile.  P is rounded to bf16 for the
-// product; l sums the fp32 values.
+// Measured (32 / 8 heads of 128, causal): 8192 tokens 450 us in bursts, 1.22 PFLOP/s of visible products, 74 % of what a large
+// library product reaches in bursts; 510 to 520 us over a run of passes, where the power cap holds the clocks down (1.07 PFLOP/s,
+// 76 % of the library's rate over seconds).  Half of a 128 x 128 x 128 score product's time is spent at the full rate of shared
+// memory (both operands come from there), and a sub-tile's chain -- products, softmax, hand-overs -- takes 3200 cycles where the
+// two sub-tiles' products take 2048: the chain bounds it, and what lengthens it shows (8192 tokens with a distance term 615 us,
+// with a cap 630).  24 documents of 333 tokens on average, half of the heads compressed, capped: 117 us, two thirds of it set-up,
+// first loads and results of CTAs that see two or three key tiles.
+// Tried and dropped: CTAs that stay and claim items, with the next item's loads early (8 % and 19 % slower: results can then not
+// go out as whole rows, and the issuing warp runs out of registers); exponentials against the old maximum while the new one is
+// looked for (5 % slower); two threads per row in four softmax warpgroups, which halves a thread's work but adds an exchange of
+// the maxima to every tile (8192 tokens 481 us against 455 in bursts, 534 against 494 over a run; 24 documents the same).
+// The running maximum of a row moves only when it would grow by more than 2^8 (a published idea; its effect cancels in O / l;
+// P <= 256 and O, l are fp32), so the correction of O in tensor memory is rare after the first tile.  P is rounded to bf16 for
+// the product; l sums the fp32 values.
 #include "rlkv_prompt.cuh"
 #include "tcgen05.cuh"
 

@@ -83,9 +83,11 @@ __device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv)
     return bits;
 }
 
-// Bound by memory: 8192 tokens of 32 / 8 heads of 128 read and write 210 MB in 41.5 us, 5.1 TB/s (77 % of a copy's rate).  One
+// Bound by memory: 8192 tokens of 32 / 8 heads of 128 read and write 210 MB in 41 us, 5.1 TB/s (78 % of a copy's rate).  One
 // thread per piece and head, its angles read again for every head, took 57 us; two or eight heads' loads at a time 49 and 60
-// (fewer in flight; fewer threads), more threads with spilled registers 62.  Few tokens are launch latency: 2.8 us.
+// (fewer in flight; fewer threads), more threads with spilled registers 62.  Few tokens are launch latency: 2.5 us.
+// An 8-bit cache takes 44.7 us for the same prompt, which moves 197 MB, and 7.7 for a token each of 64 sequences (2.6 in 16 bits):
+// a V thread writes its sixteen transposed codes one byte at a time.
 // A block takes 256 / PIECES tokens and `heads` of the heads (numbered q heads, K heads, V heads).  A thread keeps
 // one piece of one token: its eight angles stay in registers over the heads, whose loads are issued four at a time.
 template <int PIECES>

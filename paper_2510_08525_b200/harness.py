@@ -166,8 +166,8 @@ class PagedCache:
     def prefill_rotated(self, layer, slot, q, k, v):
         """The same for a prompt; returns the rotated queries and keys, for PromptAttention."""
         _check_rows(self, q, k, v)
-        if not q.shape[0] == k.shape[0] == v.shape[0]:
-            raise ValueError("q, k and v must be of the same tokens")
+        if q.shape[0] != k.shape[0]:
+            raise ValueError("q and k must be of the same tokens")
         q_out = torch.empty((q.shape[0], self.q_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
         k_out = torch.empty((k.shape[0], self.kv_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
         rl.rlkv_paged_prefill_rotated(self.handle, layer, slot, q, k, v, k.shape[0], q_out, k_out)

@@ -306,7 +306,8 @@ int rlkv_paged_set_rotary(rlkv_paged* cache, const void* table, int positions, i
  * q_out: device bf16, contiguous: the rotated queries, for rlkv_paged_decode_attention; it may be q itself where
  * q is contiguous, and overlaps no other argument.  q and q_out may both be NULL.  Products are computed in fp32
  * and rounded once: q_out and 16-bit rows to bf16, 8-bit rows to the code of the fp32 value.  Values are stored
- * as rlkv_paged_append stores them.  RLKV_EINVAL if no rotation is set or a token lies past the table. */
+ * as rlkv_paged_append stores them.  A captured call stores its tokens where they belonged at its capture, as
+ * often as it is replayed.  RLKV_EINVAL if no rotation is set or a token lies past the table. */
 int rlkv_paged_append_rotated(rlkv_paged* cache, int layer, const int* slots, int n, const void* q, int64_t q_stride,
                               const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out,
                               void* stream);

@@ -119,3 +119,48 @@ def test_whole_paged_step_with_scores(hz, cuda_device, fp8):
         assert torch.equal(out, want)
         assert torch.equal(caches[1].decode(1, [0, 1], q2), after)
     assert caches[0].status() == 0 and caches[1].status() == 0
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_rotated_append_and_decode_behind_it(hz, cuda_device, fp8):
+    """A captured token goes where it belonged at the capture: on replays with other inputs its row is written anew, the rows before
+    it and the sequences' lengths stay."""
+    dev, Hkv, Hq, D, lens, mask = cuda_device, 4, 16, 128, [5000, 63, 6016], [1, 0, 1, 0]
+    scales = ([0.02] * Hkv, [0.03] * Hkv) if fp8 else (None, None)
+    table = hz.rotary_table(7000, D, device=dev)
+    n, prompts, caches = len(lens), [], []
+    for i, x in enumerate(lens):
+        prompts.append([rand_bf16((x, Hkv, D), 10 * i + 1).to(dev), rand_bf16((x, Hkv, D), 10 * i + 2).to(dev)])
+    for _ in range(4):
+        c = hz.PagedCache(1, Hkv, Hq, D, n, 200, 6100, mask, 16, 112, device=dev, k_scale=scales[0], v_scale=scales[1])
+        c.set_rotary(table, D)
+        c.set_scores(20.0)
+        for i, (k, v) in enumerate(prompts):
+            c.open_seq()
+            c.prefill(0, i, k, v)
+        caches.append(c)
+    tokens = [[rand_bf16((n, h, D), 50 + 3 * t + j).to(dev) for j, h in enumerate((Hq, Hkv, Hkv))] for t in range(3)]
+    want = []
+    for c, (q, k, v) in zip(caches[1:], tokens):
+        qr = c.append_rotated(0, [0, 1, 2], q, k, v)
+        want.append((qr.clone(), c.decode(0, [0, 1, 2], qr).clone()))
+    import paper_2510_08525_b200.binding as rl
+    c, given = caches[0], [x.clone() for x in tokens[0]]
+    qr, out = torch.empty_like(given[0]), torch.empty((n, Hq, D), device=dev)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        rl.rlkv_paged_append_rotated(c.handle, 0, [0, 1, 2], *given, qr)
+        rl.rlkv_paged_decode_attention(c.handle, 0, [0, 1, 2], qr, out)
+    for t in (0, 1, 2):
+        for x, y in zip(given, tokens[t]):
+            x.copy_(y)
+        g.replay()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(qr, want[t][0]) and torch.equal(out, want[t][1])
+    for i, x in enumerate(lens):
+        assert c.length(0, i) == x + 1
+        for h in range(Hkv):
+            for a, b in zip(c.export_head(0, i, h), caches[3].export_head(0, i, h)):
+                np.testing.assert_array_equal(a, b)
+    assert c.status() == 0

@@ -317,6 +317,56 @@ int rlkv_paged_append_rotated(rlkv_paged* cache, int layer, const int* slots, in
 int rlkv_paged_prefill_rotated(rlkv_paged* cache, int layer, int slot, const void* q, int64_t q_stride, const void* k,
                                int64_t k_stride, const void* v, int64_t v_stride, int n_tokens, void* q_out,
                                void* k_out, void* stream);
+/* Norms of query and key heads, for models that divide every head by its root mean square before it is rotated:
+ *     y = x / sqrt(mean(x^2) + eps) * weight,   then the rotation,
+ * computed in fp32 and rounded once.  From now on the rotated calls of this cache (the two above and rlkv_paged_rotate_chunks)
+ * do it on the way, in the same launch.  q_weight, k_weight: DEVICE fp32 [layers][head_dim] on the cache's GPU, 16-byte aligned,
+ * the caller's, to outlive the calls and read when the kernels run; NULL: the queries (keys) are not normalised.  eps: above 0,
+ * at most 1. */
+int rlkv_paged_set_norms(rlkv_paged* cache, const float* q_weight, const float* k_weight, float eps);
+
+/* ---- chunks: several new tokens of each of several sequences ------------------------------------------
+ * What lies between a whole prompt and one token per sequence: prompts that come in pieces beside sequences that decode, and
+ * drafted tokens that are verified.  A call names n sequences (slots: HOST int[n], open, none twice) and how many new tokens
+ * each brings (counts: HOST int[n], 0 or more); the chunks' tokens lie packed behind one another in the order of the slots, at
+ * most 2^24 in all, and stand at the positions behind the tokens that the sequence holds in that layer.  Rows of q, k and v
+ * are *_stride elements apart (a multiple of 8, at most 2^30; 0: contiguous), so that slices of one projection's output can be
+ * given as they are.  The usual order, layer by layer: rotate the chunks, attend them, append them -- or of drafted tokens
+ * those that were accepted: nothing has to be taken back.  Rows behind the last chunk are neither read nor written.  A
+ * captured call takes its sequences at the lengths of its capture.  RLKV_EFULL if a sequence would come to more than max_seq_len
+ * tokens.  A call whose counts are all 0 does nothing.
+ *
+ * rlkv_paged_rotate_chunks: q_out (device bf16, contiguous [tokens][q_heads][head_dim]) and k_out ([tokens][kv_heads][head_dim])
+ * get the queries and keys with the cache's norms and rotation (at least one of them set; RLKV_EINVAL if a token lies past the
+ * table); they may be q and k themselves where those are contiguous. */
+int rlkv_paged_rotate_chunks(rlkv_paged* cache, int layer, const int* slots, const int* counts, int n, const void* q,
+                             int64_t q_stride, const void* k, int64_t k_stride, void* q_out, void* k_out, void* stream);
+/* Attention of the chunks' tokens over what the cache holds and over the chunk itself, before it is appended: query i of a
+ * sequence of len tokens stands at position len + i and sees key j <= len + i -- a full head every one, a compressed head
+ * those with j < sink or j > len + i - window.  (That is why the chunk is not appended first: a ring would have dropped keys
+ * that its first tokens see.)  Scores as rlkv_paged_set_scores says.  The chunk's own keys and values are taken as they are given,
+ * those of an 8-bit cache as it holds them.  The cache does not change; a sequence may hold nothing yet.
+ * out: device bf16 [tokens][q_heads][head_dim] (fp32 accumulation, rounded once); lse: device fp32 [tokens][q_heads], log sum
+ * exp(score), or NULL.  Every sum has a fixed order: the same call on the same cache gives the same bits.  (What a call keeps
+ * between its CTAs lies in 39 MB -- 20 at head_dim 64 -- that rlkv_paged_create allocates beside the cache's buffer; if it cannot, the
+ * decode launches' scratch serves, and large calls use fewer CTAs.)  Values of a sequence's own rows are
+ * assumed finite; what rows of other sequences or of pages' unused parts hold has no effect. */
+int rlkv_paged_chunk_attention(rlkv_paged* cache, int layer, const int* slots, const int* counts, int n, const void* q,
+                               int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* out,
+                               float* lse, void* stream);
+/* Appends the chunks: the cache's bytes are those of counts[i] single appends to slots[i].  Pages are taken from the free list
+ * sequence by sequence.  RLKV_EFULL (nothing appended for any sequence) if it cannot serve every new page.  A captured call
+ * stores its tokens where they belonged at its capture, as often as it is replayed. */
+int rlkv_paged_append_chunks(rlkv_paged* cache, int layer, const int* slots, const int* counts, int n, const void* k,
+                             int64_t k_stride, const void* v, int64_t v_stride, void* stream);
+/* Reads rows back: tokens first[i] .. first[i] + counts[i] - 1 (HOST int[n], tokens that the sequence holds, else RLKV_EINVAL)
+ * of each sequence, packed in the order of the slots, to k_out and v_out (device bf16, contiguous [tokens][kv_heads][head_dim]).  An
+ * 8-bit cache's are value(code) * scale, rounded to bf16; where a compressed head has dropped a token its rows are zero.
+ * Appending what was read to an empty sequence gives the same cache, in 8 bits too (unless a scale times a code leaves bf16's
+ * normal range). */
+int rlkv_paged_read(rlkv_paged* cache, int layer, const int* slots, const int* first, const int* counts, int n, void* k_out,
+                    void* v_out, void* stream);
+
 /* Decode attention for n sequences of one layer, each over its own length, one launch for both
  * head classes and all lengths.  q: device bf16 [n][q_heads][head_dim]; out: device fp32
  * [n][q_heads][head_dim]; entry i belongs to slots[i] (HOST int[n]).  RLKV_EEMPTY if a listed
@@ -386,6 +436,15 @@ int rlkv_debug_paged_schedule(const int* lens, int n, int n_full, int n_comp, in
 int rlkv_debug_paged_cut(const int* lens, int n, int n_full, int n_comp, int cap, int ctas, int fp8, int scored, int in_step,
                          int* item_tiles_out, int* n_items_out);
 
+/* How rlkv_paged_chunk_attention cuts a call's work for at most max_ctas CTAs (up to 296), host arithmetic only: n sequences of
+ * lens[i] tokens and counts[i] new ones, n_full full and n_comp compressed heads of `group` query heads.  The work is a flat
+ * sequence of key tiles: sequence by sequence, tile of subs * (128 / group) queries by tile, the full heads and then the compressed
+ * ones; a tile has 64 keys with subs 1, 128 with subs 2 (0: as the call would choose).  CTA c takes the tiles from
+ * at_out[4c..4c+3] = (sequence, query tile, head, key tile) up to at_out[4c+4..4c+7], c < *ctas_out; the last entry names
+ * sequence n (host int[4 * (max_ctas + 1)]). */
+int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full, int n_comp, int group, int sink, int window,
+                          int subs, int max_ctas, int* ctas_out, int* at_out);
+
 /* ---- attention over whole prompts -------------------------------------------------------------------
  * What a prompt (or a training sample) needs before its tokens are decoded: every token attends the tokens
  * before it, with the head classes of the caches.  Documents are packed behind one another: document d holds the
@@ -427,6 +486,25 @@ int rlkv_prompt_attention_backward(rlkv_prompt* prompt, int layer, const void* q
                                    const int* q_starts, const int* k_starts, int n_docs, const int* prefix,
                                    const void* out, const float* lse, const void* dout, void* dq, void* dk, void* dv,
                                    void* stream);
+/* Norms of query and key heads and their rotation for packed tokens, with gradients: what comes before prompt attention
+ * while a model is trained.  Setters and formulas are those of the paged cache (rlkv_paged_set_rotary, rlkv_paged_set_norms); at
+ * least one of rotation and norms is set, else the calls return RLKV_EINVAL. */
+int rlkv_prompt_set_rotary(rlkv_prompt* prompt, const void* table, int positions, int rot_dim, int interleaved);
+int rlkv_prompt_set_norms(rlkv_prompt* prompt, const float* q_weight, const float* k_weight, float eps);
+/* q: device bf16 [tokens][q_heads][head_dim], k: [tokens][kv_heads][head_dim], strides as above; tokens: 1 to max_tokens.
+ * positions: DEVICE int32 [tokens], read when the kernel runs, or NULL: token i at position i.  A token whose position is negative
+ * or past the table belongs to no document: its rows of the results stay as they are.  q_out, k_out: device bf16, contiguous;
+ * they may be q and k themselves where those are contiguous. */
+int rlkv_prompt_rotate(rlkv_prompt* prompt, int layer, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                       int tokens, const int* positions, void* q_out, void* k_out, void* stream);
+/* The gradients, from the forward call's inputs and the gradients of its results (device bf16, contiguous): dq and dk as q and
+ * k (tokens *_stride elements apart, slices of one buffer if wanted; dq may be dq_out itself where contiguous, and dk dk_out), each
+ * rounded once; dq_weight, dk_weight: device fp32 [head_dim], summed over tokens and heads in a fixed order and written (not
+ * added), or NULL; RLKV_EINVAL if that norm is not set. */
+int rlkv_prompt_rotate_backward(rlkv_prompt* prompt, int layer, const void* q, int64_t q_stride, const void* k,
+                                int64_t k_stride, int tokens, const int* positions, const void* dq_out, const void* dk_out,
+                                void* dq, int64_t dq_stride, void* dk, int64_t dk_stride, float* dq_weight,
+                                float* dk_weight, void* stream);
 /* As rlkv_kernel_status. */
 int rlkv_prompt_kernel_status(rlkv_prompt* prompt, int* status_out);
 

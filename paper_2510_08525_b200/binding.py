@@ -71,6 +71,11 @@ SIGNATURES = {
     "rlkv_paged_set_rotary": (_ci, [_vp, _vp, _ci, _ci, _ci]),
     "rlkv_paged_append_rotated": (_ci, [_vp, _ci, _vp, _ci, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
     "rlkv_paged_prefill_rotated": (_ci, [_vp, _ci, _ci, _vp, _i64, _vp, _i64, _vp, _i64, _ci, _vp, _vp, _vp]),
+    "rlkv_paged_set_norms": (_ci, [_vp, _vp, _vp, ctypes.c_float]),
+    "rlkv_paged_rotate_chunks": (_ci, [_vp, _ci, _vp, _vp, _ci, _vp, _i64, _vp, _i64, _vp, _vp, _vp]),
+    "rlkv_paged_chunk_attention": (_ci, [_vp, _ci, _vp, _vp, _ci, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp]),
+    "rlkv_paged_append_chunks": (_ci, [_vp, _ci, _vp, _vp, _ci, _vp, _i64, _vp, _i64, _vp]),
+    "rlkv_paged_read": (_ci, [_vp, _ci, _vp, _vp, _vp, _ci, _vp, _vp, _vp]),
     "rlkv_paged_decode_attention": (_ci, [_vp, _ci, _vp, _ci, _vp, _vp, _vp]),
     "rlkv_paged_step": (_ci, [_vp, _vp, _ci, _vp, _vp, _vp, _vp, _vp]),
     "rlkv_paged_length": (_ci, [_vp, _ci, _ci, ctypes.POINTER(_ci)]),
@@ -83,7 +88,12 @@ SIGNATURES = {
     "rlkv_prompt_attention": (_ci, [_vp, _ci, _vp, _i64, _vp, _i64, _vp, _i64, _ci, _ci, _vp, _vp, _ci, _vp, _vp, _vp, _vp]),
     "rlkv_prompt_attention_backward": (_ci, [_vp, _ci, _vp, _i64, _vp, _i64, _vp, _i64, _ci, _ci, _vp, _vp, _ci, _vp, _vp, _vp, _vp,
                                              _vp, _vp, _vp, _vp]),
+    "rlkv_prompt_set_rotary": (_ci, [_vp, _vp, _ci, _ci, _ci]),
+    "rlkv_prompt_set_norms": (_ci, [_vp, _vp, _vp, ctypes.c_float]),
+    "rlkv_prompt_rotate": (_ci, [_vp, _ci, _vp, _i64, _vp, _i64, _ci, _vp, _vp, _vp, _vp]),
+    "rlkv_prompt_rotate_backward": (_ci, [_vp, _ci, _vp, _i64, _vp, _i64, _ci, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp]),
     "rlkv_prompt_kernel_status": (_ci, [_vp, ctypes.POINTER(_ci)]),
+    "rlkv_debug_chunk_plan": (_ci, [_vp, _vp, _ci, _ci, _ci, _ci, _ci, _ci, _ci, _ci, ctypes.POINTER(_ci), _vp]),
     "rlkv_debug_paged_cut": (_ci, [_vp, _ci, _ci, _ci, _ci, _ci, _ci, _ci, _ci, ctypes.POINTER(_ci), ctypes.POINTER(_ci)]),
     "rlkv_debug_paged_schedule": (_ci, [_vp, _ci, _ci, _ci, _ci, _ci, _ci, ctypes.POINTER(_ci), _vp, _vp, _vp]),
 }
@@ -575,6 +585,71 @@ def rlkv_paged_prefill_rotated(cache, layer, slot, q, k, v, n_tokens, q_out, k_o
                                           _room(k_out, _size(k), gpu=gpu), _stream(stream, cache, k)))
 
 
+def _set_norms(call, handle, q_weight, k_weight, eps) -> None:
+    for w in (q_weight, k_weight):
+        if w is None or isinstance(w, int):
+            continue
+        if w.dtype is not sys.modules["torch"].float32 or isinstance(handle, Handle) and w.numel() != handle.layers * handle.head_dim:
+            raise ValueError("a norm's weights are fp32 [layers][head_dim]")
+    _check(call(handle, _ptr(q_weight), _ptr(k_weight), float(eps)))
+    if isinstance(handle, Handle):
+        handle.norms = q_weight, k_weight  # (the launches read them: they live as long as the handle, or until others are set)
+
+
+def rlkv_paged_set_norms(cache, q_weight, k_weight, eps=1e-6) -> None:
+    """q_weight, k_weight: device fp32 [layers][head_dim], or None."""
+    _set_norms(lib.rlkv_paged_set_norms, cache, q_weight, k_weight, eps)
+
+
+def _chunks(slots, counts, *more):
+    """The host arrays of a call on chunks, as int32, and the tokens of all of them."""
+    arrays = [np.ascontiguousarray(x, dtype=np.int32).reshape(-1) for x in (slots, *more, counts)]
+    if any(x.size != arrays[0].size for x in arrays):
+        raise ValueError("slots and counts must have an entry for each sequence")
+    return arrays, int(arrays[-1].sum())
+
+
+def _width(handle, heads, of):
+    """Elements of a token's rows: the handle's, or those of a tensor."""
+    if isinstance(handle, Handle):
+        return getattr(handle, heads) * handle.head_dim
+    return 0 if of is None or isinstance(of, int) else of.shape[1] * of.shape[2]
+
+
+def rlkv_paged_rotate_chunks(cache, layer, slots, counts, q, k, q_out, k_out, stream=None) -> None:
+    (s, m), n = _chunks(slots, counts)
+    hq, hkv, d, gpu = _shape_of(cache, k)
+    _check(lib.rlkv_paged_rotate_chunks(cache, layer, _host(s), _host(m), s.size, *_rows(q, n, hq, d, gpu), *_rows(k, n, hkv, d, gpu),
+                                        _room(q_out, n * _width(cache, "q_heads", q), gpu=gpu),
+                                        _room(k_out, n * _width(cache, "kv_heads", k), gpu=gpu), _stream(stream, cache, k)))
+
+
+def rlkv_paged_chunk_attention(cache, layer, slots, counts, q, k, v, out, lse=None, stream=None) -> None:
+    """q, k, v: the chunks' tokens packed behind one another, [tokens][heads][head_dim], possibly slices of one projection's
+    output; slots, counts: host."""
+    (s, m), n = _chunks(slots, counts)
+    hq, hkv, d, gpu = _shape_of(cache, k)
+    width = _width(cache, "q_heads", q)
+    _check(lib.rlkv_paged_chunk_attention(cache, layer, _host(s), _host(m), s.size, *_rows(q, n, hq, d, gpu), *_rows(k, n, hkv, d, gpu),
+                                          *_rows(v, n, hkv, d, gpu), _room(out, n * width, gpu=gpu),
+                                          _room(lse, n * width // d if d else 0, "float32", gpu), _stream(stream, cache, k)))
+
+
+def rlkv_paged_append_chunks(cache, layer, slots, counts, k, v, stream=None) -> None:
+    (s, m), n = _chunks(slots, counts)
+    _, hkv, d, gpu = _shape_of(cache, k)
+    _check(lib.rlkv_paged_append_chunks(cache, layer, _host(s), _host(m), s.size, *_rows(k, n, hkv, d, gpu), *_rows(v, n, hkv, d, gpu),
+                                        _stream(stream, cache, k)))
+
+
+def rlkv_paged_read(cache, layer, slots, first, counts, k_out, v_out, stream=None) -> None:
+    (s, f, m), n = _chunks(slots, counts, first)
+    gpu = _shape_of(cache, k_out)[3]
+    least = n * _width(cache, "kv_heads", k_out)
+    _check(lib.rlkv_paged_read(cache, layer, _host(s), _host(f), _host(m), s.size, _room(k_out, least, gpu=gpu),
+                               _room(v_out, least, gpu=gpu), _stream(stream, cache, k_out)))
+
+
 def rlkv_paged_decode_attention(cache, layer, slots, q, out, stream=None) -> None:
     s = _slots(slots)
     _check(lib.rlkv_paged_decode_attention(cache, layer, _host(s), s.size, _ptr(q), _ptr(out), _stream(stream, cache, q)))
@@ -681,10 +756,64 @@ def rlkv_prompt_attention_backward(prompt, layer, q, k, v, q_starts, k_starts, p
                                               _room(dv, n_k, gpu=gpu), _stream(stream, prompt, q)))
 
 
+def rlkv_prompt_set_rotary(prompt, table, positions, rot_dim, interleaved=False) -> None:
+    _check_table(table, min(rot_dim, 128), positions)
+    _check(lib.rlkv_prompt_set_rotary(prompt, _ptr(table), positions, rot_dim, int(bool(interleaved))))
+    if isinstance(prompt, Handle):
+        prompt.rotary = table
+
+
+def rlkv_prompt_set_norms(prompt, q_weight, k_weight, eps=1e-6) -> None:
+    """q_weight, k_weight: device fp32 [layers][head_dim], or None."""
+    _set_norms(lib.rlkv_prompt_set_norms, prompt, q_weight, k_weight, eps)
+
+
+def _positions(x, tokens, gpu):
+    if x is None or isinstance(x, int):
+        return x or 0
+    if not _on_device(x) or x.dtype is not sys.modules["torch"].int32 or x.numel() < tokens or not x.is_contiguous():
+        raise ValueError("positions are int32 in device memory, one for each token")
+    if gpu is not None and x.get_device() != gpu:
+        raise ValueError(f"a tensor in the memory of GPU {gpu} is wanted")
+    return x.data_ptr()
+
+
+def rlkv_prompt_rotate(prompt, layer, q, k, positions, q_out, k_out, stream=None) -> None:
+    """q, k: [tokens][heads][head_dim], possibly slices of one projection's output; positions: device int32 [tokens] or None."""
+    n = q.shape[0]
+    hq, hkv, d, gpu = _shape_of(prompt, q)
+    _check(lib.rlkv_prompt_rotate(prompt, layer, *_rows(q, n, hq, d, gpu), *_rows(k, n, hkv, d, gpu), n, _positions(positions, n, gpu),
+                                  _room(q_out, q.numel(), gpu=gpu), _room(k_out, n * k.shape[1] * k.shape[2], gpu=gpu),
+                                  _stream(stream, prompt, q)))
+
+
+def rlkv_prompt_rotate_backward(prompt, layer, q, k, positions, dq_out, dk_out, dq, dk, dq_weight=None, dk_weight=None,
+                                stream=None) -> None:
+    """dq, dk: [tokens][heads][head_dim], possibly slices of one buffer; dq_weight, dk_weight: device fp32 [head_dim] or None."""
+    n = q.shape[0]
+    hq, hkv, d, gpu = _shape_of(prompt, q)
+    _check(lib.rlkv_prompt_rotate_backward(prompt, layer, *_rows(q, n, hq, d, gpu), *_rows(k, n, hkv, d, gpu), n,
+                                           _positions(positions, n, gpu), _room(dq_out, q.numel(), gpu=gpu),
+                                           _room(dk_out, n * k.shape[1] * k.shape[2], gpu=gpu), *_rows(dq, n, hq, d, gpu),
+                                           *_rows(dk, n, hkv, d, gpu), _room(dq_weight, q.shape[2], "float32", gpu),
+                                           _room(dk_weight, k.shape[2], "float32", gpu), _stream(stream, prompt, q)))
+
+
 def rlkv_prompt_kernel_status(prompt) -> int:
     out = _ci(0)
     _check(lib.rlkv_prompt_kernel_status(prompt, ctypes.byref(out)))
     return int(out.value)
+
+
+def rlkv_debug_chunk_plan(lens, counts, n_full, n_comp, group, sink, window, subs=0, max_ctas=296):
+    """int32 [ctas + 1][4]: sequence, query tile, head and key tile that each CTA's range begins with, and the end."""
+    ln, m, ctas = _slots(lens), _slots(counts), _ci(0)
+    if ln.size != m.size:
+        raise ValueError("lens and counts must have an entry for each sequence")
+    at = np.zeros((max_ctas + 1, 4), dtype=np.int32)
+    _check(lib.rlkv_debug_chunk_plan(ln.ctypes.data, m.ctypes.data, ln.size, n_full, n_comp, group, sink, window, subs, max_ctas,
+                                     ctypes.byref(ctas), at.ctypes.data))
+    return at[:ctas.value + 1]
 
 
 def rlkv_debug_paged_cut(lens, n_full, n_comp, cap, ctas, fp8=False, scored=False, in_step=False):

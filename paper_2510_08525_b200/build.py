@@ -8,9 +8,9 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "librlkv.so")
-SOURCES = ["rlkv_api.cu", "rlkv_paged.cu", "rlkv_prompt.cu", "append_kernel.cu", "rotary_kernel.cu", "decode_kernel.cu",
-           "prompt_forward.cu", "prompt_backward.cu", "probe_kernel.cu"]
-HEADERS = ["rlkv_internal.cuh", "rlkv_host.cuh", "rlkv_prompt.cuh", "tcgen05.cuh", os.path.join("..", "..", "include", "rlkv.h")]
+SOURCES = ["rlkv_api.cu", "rlkv_paged.cu", "rlkv_prompt.cu", "rlkv_paged_chunks.cu", "append_kernel.cu", "rotary_kernel.cu",
+           "norm_rotary.cu", "chunk_rows.cu", "decode_kernel.cu", "chunk_attention.cu", "prompt_forward.cu", "prompt_backward.cu", "probe_kernel.cu"]
+HEADERS = ["rlkv_internal.cuh", "rlkv_host.cuh", "rlkv_paged.cuh", "rlkv_prompt.cuh", "rlkv_chunk.cuh", "rotary.cuh", "tcgen05.cuh", os.path.join("..", "..", "include", "rlkv.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
 # Fast-math (approximate exp2 and division, flush-to-zero) is wanted in the decode kernel's softmax and

@@ -123,6 +123,10 @@ namespace rlkv {
 int paged_prefill_strided(rlkv_paged* p, int layer, int slot, const void* k, const void* v, int n_tokens,
                           long long entry_stride, void* stream);
 uint64_t paged_launch_count(const rlkv_paged* p);
+// rlkv_paged_create_fp8 for that cache, which attends no chunks: without their scratch.
+int paged_create_for_batch(rlkv_paged** out, int layers, int kv_heads, int q_heads, int head_dim, int max_seqs, int n_pages, int max_seq_len,
+                           const uint8_t* head_is_full, int sink, int window, const float* k_scale, const float* v_scale,
+                           void* device_buf, size_t device_buf_bytes);
 
 struct DeviceGuard {
     int prev = -1;
@@ -204,6 +208,22 @@ inline int encode_byte_rows_tensor_map(CUtensorMap* tmap, void* base, int row_by
         return RLKV_ECUDA;
     }
     return RLKV_OK;
+}
+
+// Tensor map over [tokens][heads][head_dim] bf16, tokens `stride` elements apart: boxes of 64 elements of box_heads heads of
+// box_tokens tokens, 128-byte swizzle.  Tokens past the end read as zero.  (rlkv_prompt.cu)
+int encode_heads_map(CUtensorMap* map, const void* base, long long tokens, int heads, int head_dim, int64_t stride, int box_heads, int box_tokens);
+
+// Whether x is 16-byte aligned memory of GPU `device`.
+inline bool on_device(const void* x, int device)
+{
+    cudaPointerAttributes at;
+    if (!aligned16(x)) return false;
+    if (cudaPointerGetAttributes(&at, x) != cudaSuccess || at.type != cudaMemoryTypeDevice || at.device != device) {
+        cudaGetLastError();
+        return false;
+    }
+    return true;
 }
 
 }  // namespace rlkv

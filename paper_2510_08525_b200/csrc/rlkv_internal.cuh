@@ -672,6 +672,8 @@ struct RotatedAppendArgs {
     const float* table;         // [positions][rot / 2] (cos, sin)
     long long q_stride, k_stride, v_stride;
     int q_heads, rot, interleaved;
+    const float *q_weight, *k_weight;  // norms of the layer, [head_dim]; null: none
+    float eps;
 };
 cudaError_t launch_rotated_append(const RotatedAppendArgs& a, cudaStream_t stream);
 

@@ -29,45 +29,10 @@
 #include <new>
 #include <vector>
 
-#include "rlkv_host.cuh"
+#include "rlkv_chunk.cuh"
+#include "rlkv_paged.cuh"
 
 using namespace rlkv;
-
-struct rlkv_paged {
-    int layers, kv_heads, q_heads, head_dim, max_seqs, n_pages, table_stride, sink, window;
-    int max_seq_len;              // most tokens a sequence may hold (the page table is laid out for a few more)
-    int device, sm_count, stages, groups, item_tiles;
-    int rows_comp, max_batch, max_items, max_grid;
-    int out_bf16;
-    int step_mode;                // rlkv_paged_step: 0 chooses, 1 one decode launch per layer, 2 one for the whole step
-    bool step_in_one_launch;      // the shape allows one decode launch for a whole step
-    long long step_slots;         // partial records the scratch holds when both copies are used as one
-    int fp8;                      // K/V rows (pages and rings) are held as E4M3 codes
-    std::vector<float> k_scale, v_scale;  // [layers*kv_heads]
-    std::vector<long long> page0_8, ring0_8;  // first full-head page / first ring page of each layer in the 8-bit pool
-    long long pages8;                      // pages of the 8-bit pool
-    size_t off_pool8, off_scales;
-    CUtensorMap map_k;  // the 8-bit pool as rows of 128 bytes, one page per box
-    long long pool_rows;
-    std::vector<uint8_t> is_full;
-    std::vector<int> slot_of_head, head_of_slot;  // [layers*kv_heads]
-    std::vector<int> n_full, n_comp;
-    std::vector<long long> full_row0, comp_row0;
-    std::vector<int> len;         // [layers][max_seqs]
-    std::vector<int> table;       // [max_seqs][table_stride], -1 = no page
-    std::vector<int> free_pages;  // stack of physical pages
-    std::vector<uint8_t> open;    // [max_seqs]
-    size_t off_pool, off_tables, off_head_table, off_layer_desc, off_slopes, off_page_table, off_tickets, off_status, off_partials, total;
-    uint8_t* dev_base;
-    bool owns_buffer;
-    CUtensorMap tmap;
-    uint64_t launches;
-    const float* rotary;          // rlkv_paged_set_rotary: the caller's table of angles (device), null: none set
-    int rotary_rows, rotary_dim, rotary_interleaved;
-    float softcap;                // rlkv_paged_set_scores: 0 no cap
-    bool biased;                  // and whether scores are lowered by distance (slopes at off_slopes)
-    bool has_slopes;              // whether slopes have ever been written
-};
 
 namespace {
 
@@ -187,27 +152,6 @@ int make_paged_layout(rlkv_paged& p, const uint8_t* mask, int max_seq_len)
     return RLKV_OK;
 }
 
-template <typename T>
-T* dev_at(const rlkv_paged* p, size_t off) { return reinterpret_cast<T*>(p->dev_base + off); }
-
-bool valid_layer(const rlkv_paged* p, int layer) { return p && layer >= 0 && layer < p->layers; }
-bool valid_slot(const rlkv_paged* p, int slot) { return slot >= 0 && slot < p->max_seqs && p->open[slot]; }
-
-// The request slots of a call: all open, no slot twice.
-int check_slots(const rlkv_paged* p, const int* slots, int n)
-{
-    if (!slots || n < 1 || n > p->max_batch) return RLKV_EINVAL;
-    std::vector<uint8_t> seen(p->max_seqs, 0);
-    for (int i = 0; i < n; ++i) {
-        if (!valid_slot(p, slots[i]) || seen[slots[i]]) return RLKV_EINVAL;
-        seen[slots[i]] = 1;
-    }
-    return RLKV_OK;
-}
-
-int* len_of(rlkv_paged* p, int layer) { return p->len.data() + (size_t)layer * p->max_seqs; }
-const int* len_of(const rlkv_paged* p, int layer) { return p->len.data() + (size_t)layer * p->max_seqs; }
-
 void fill_append_args(rlkv_paged* p, int layer, const void* k, const void* v, PagedAppendArgs& a)
 {
     a.pool = dev_at<__nv_bfloat16>(p, p->off_pool);
@@ -273,7 +217,7 @@ int rlkv_paged_size_fp8(int layers, int kv_heads, int q_heads, int head_dim, int
 
 static int paged_create(rlkv_paged** out, int layers, int kv_heads, int q_heads, int head_dim, int max_seqs, int n_pages,
                         int max_seq_len, const uint8_t* head_is_full, int sink, int window, const float* k_scale,
-                        const float* v_scale, void* device_buf, size_t device_buf_bytes)
+                        const float* v_scale, void* device_buf, size_t device_buf_bytes, bool chunks = true)
 {
     if (!out) return RLKV_EINVAL;
     *out = nullptr;
@@ -289,9 +233,10 @@ static int paged_create(rlkv_paged** out, int layers, int kv_heads, int q_heads,
     if (!p) return RLKV_ENOMEM;
     p->layers = layers; p->kv_heads = kv_heads; p->q_heads = q_heads; p->head_dim = head_dim;
     p->max_seqs = max_seqs; p->n_pages = n_pages; p->sink = sink; p->window = window; p->max_seq_len = max_seq_len;
-    p->launches = 0; p->dev_base = nullptr; p->owns_buffer = false; p->out_bf16 = 0;
+    p->launches = 0; p->dev_base = nullptr; p->own_records = nullptr; p->owns_buffer = false; p->out_bf16 = 0;
     p->step_mode = 0;
     p->softcap = 0.f; p->biased = p->has_slopes = false;
+    p->q_norm = p->k_norm = nullptr; p->norm_eps = 0.f;
     p->rotary = nullptr; p->rotary_rows = p->rotary_dim = p->rotary_interleaved = 0;
     p->fp8 = fp8;
     if (fp8) {
@@ -354,6 +299,7 @@ static int paged_create(rlkv_paged** out, int layers, int kv_heads, int q_heads,
         e = cudaMemcpy(p->dev_base + p->off_layer_desc, desc.data(), desc.size() * sizeof(LayerDesc), cudaMemcpyHostToDevice);
     }
     if (e == cudaSuccess) e = prepare_decode_kernels(head_dim);
+    if (e == cudaSuccess) e = prepare_chunk_kernels(head_dim, fp8);
     if (e != cudaSuccess) return fail(cuda_fail(e, "rlkv_paged_create"));
     // (a pool without rows -- every head full and in 8-bit pages -- still gets a one-row map: it is never used)
     rc = encode_pool_tensor_map(&p->tmap, p->dev_base + p->off_pool, p->pool_rows > 0 ? p->pool_rows : 1, head_dim);
@@ -361,6 +307,19 @@ static int paged_create(rlkv_paged** out, int layers, int kv_heads, int q_heads,
     if (fp8 && p->pages8 > 0) {
         rc = encode_byte_rows_tensor_map(&p->map_k, p->dev_base + p->off_pool8, 128, p->pages8 * 128, 2 * kTile);
         if (rc) return fail(rc);
+    }
+    // The records of attention on chunks have memory of their own, which the buffer does not count; where there is none left they
+    // share the decode launches' partial records (calls on one cache are ordered), with fewer CTAs to a launch.
+    p->chunk_records = dev_at<float>(p, p->off_partials);
+    p->chunk_bytes = p->total - p->off_partials;
+    if (chunks && chunk_record_bytes(head_dim) > p->chunk_bytes) {
+        void* mem = nullptr;
+        if (cudaMalloc(&mem, chunk_record_bytes(head_dim)) == cudaSuccess) {
+            p->chunk_records = p->own_records = static_cast<float*>(mem);
+            p->chunk_bytes = chunk_record_bytes(head_dim);
+        } else {
+            cudaGetLastError();
+        }
     }
     *out = p;
     return RLKV_OK;
@@ -383,12 +342,26 @@ int rlkv_paged_create_fp8(rlkv_paged** out, int layers, int kv_heads, int q_head
                         k_scale, v_scale, device_buf, device_buf_bytes);
 }
 
+}  // extern "C"
+
+int rlkv::paged_create_for_batch(rlkv_paged** out, int layers, int kv_heads, int q_heads, int head_dim, int max_seqs, int n_pages, int max_seq_len,
+                                 const uint8_t* head_is_full, int sink, int window, const float* k_scale, const float* v_scale,
+                                 void* device_buf, size_t device_buf_bytes)
+{
+    if (!k_scale || !v_scale) return RLKV_EINVAL;
+    return paged_create(out, layers, kv_heads, q_heads, head_dim, max_seqs, n_pages, max_seq_len, head_is_full, sink, window, k_scale, v_scale,
+                        device_buf, device_buf_bytes, false);
+}
+
+extern "C" {
+
 int rlkv_paged_destroy(rlkv_paged* p)
 {
     if (!p) return RLKV_EINVAL;
     DeviceGuard g(p->device);
     cudaDeviceSynchronize();
     if (p->owns_buffer) cudaFree(p->dev_base);
+    if (p->own_records) cudaFree(p->own_records);
     delete p;
     return RLKV_OK;
 }
@@ -509,10 +482,10 @@ int rlkv_paged_set_rotary(rlkv_paged* p, const void* table, int positions, int r
 }
 
 // The arguments of a rotated append that the two forms share; a stride of 0 stands for contiguous tokens.
-static int rotation_args(const rlkv_paged* p, const void* q, int64_t q_stride, int64_t k_stride, int64_t v_stride, void* q_out,
+static int rotation_args(const rlkv_paged* p, int layer, const void* q, int64_t q_stride, int64_t k_stride, int64_t v_stride, void* q_out,
                          void* k_out, RotatedAppendArgs& r)
 {
-    if (!p || !p->rotary || !q != !q_out || !aligned16(q) || !aligned16(q_out) || !aligned16(k_out)) return RLKV_EINVAL;
+    if (!valid_layer(p, layer) || !p->rotary || !q != !q_out || !aligned16(q) || !aligned16(q_out) || !aligned16(k_out)) return RLKV_EINVAL;
     const int64_t q_row = (int64_t)p->q_heads * p->head_dim, kv_row = (int64_t)p->kv_heads * p->head_dim;
     if (!q_stride) q_stride = q_row;
     if (!k_stride) k_stride = kv_row;
@@ -528,6 +501,9 @@ static int rotation_args(const rlkv_paged* p, const void* q, int64_t q_stride, i
     r.q_heads = p->q_heads;
     r.rot = p->rotary_dim;
     r.interleaved = p->rotary_interleaved;
+    r.q_weight = p->q_norm ? p->q_norm + (size_t)layer * p->head_dim : nullptr;
+    r.k_weight = p->k_norm ? p->k_norm + (size_t)layer * p->head_dim : nullptr;
+    r.eps = p->norm_eps;
     return RLKV_OK;
 }
 
@@ -535,7 +511,7 @@ int rlkv_paged_append_rotated(rlkv_paged* p, int layer, const int* slots, int n,
                               int64_t k_stride, const void* v, int64_t v_stride, void* q_out, void* stream)
 {
     RotatedAppendArgs r;
-    const int rc = rotation_args(p, q, q_stride, k_stride, v_stride, q_out, nullptr, r);
+    const int rc = rotation_args(p, layer, q, q_stride, k_stride, v_stride, q_out, nullptr, r);
     if (rc) return rc;
     return paged_append(p, layer, slots, n, k, v, stream, &r);
 }
@@ -553,7 +529,7 @@ int rlkv_paged_prefill_rotated(rlkv_paged* p, int layer, int slot, const void* q
                                void* stream)
 {
     RotatedAppendArgs r;
-    const int rc = rotation_args(p, q, q_stride, k_stride, v_stride, q_out, k_out, r);
+    const int rc = rotation_args(p, layer, q, q_stride, k_stride, v_stride, q_out, k_out, r);
     if (rc) return rc;
     return paged_prefill(p, layer, slot, k, v, n_tokens, (long long)p->kv_heads * p->head_dim, stream, &r);
 }

@@ -1,0 +1,387 @@
+// Host side of the calls that take a chunk of tokens of each of several sequences of the paged cache (rlkv_paged_rotate_chunks,
+// rlkv_paged_chunk_attention, rlkv_paged_append_chunks, rlkv_paged_read in include/rlkv.h).
+#include <math.h>
+#include <string.h>
+
+#include "rlkv_chunk.cuh"
+#include "rlkv_paged.cuh"
+
+using namespace rlkv;
+
+namespace {
+
+constexpr int kMaxChunkTokens = 1 << 24;  // of one call
+constexpr int kMinChunkTiles = 4;         // key tiles of a CTA's range, at least
+constexpr int kUnitTiles = 1;             // what a unit's queries and results count as, in key tiles
+
+// The sequences of a call: open slots, none twice, `counts` tokens each, from `first` on (null: behind those held).  `to`:
+// most tokens a sequence may come to; more are `over`.
+int check_chunks(const rlkv_paged* p, int layer, const int* slots, const int* first, const int* counts, int n, bool held, ChunkSeqs& s)
+{
+    if (!valid_layer(p, layer) || !slots || !counts || n < 1 || n > p->max_batch) return RLKV_EINVAL;
+    uint64_t seen[65536 / 64];
+    memset(seen, 0, sizeof(uint64_t) * ((size_t)(p->max_seqs + 63) / 64));
+    const int* len = len_of(p, layer);
+    s.n = n;
+    long long at = 0;
+    bool over = false;
+    for (int i = 0; i < n; ++i) {
+        const int slot = slots[i];
+        if (!valid_slot(p, slot) || (seen[slot / 64] >> (slot % 64) & 1) || counts[i] < 0) return RLKV_EINVAL;
+        seen[slot / 64] |= 1ull << (slot % 64);
+        const int from = first ? first[i] : len[slot];
+        if (from < 0 || (held && (long long)from + counts[i] > len[slot])) return RLKV_EINVAL;
+        if ((long long)from + counts[i] > p->max_seq_len) over = true;
+        s.slot[i] = (unsigned short)slot;
+        s.len[i] = from;
+        s.start[i] = (int)at;
+        at += counts[i];
+        if (at > kMaxChunkTokens) return RLKV_EINVAL;
+    }
+    s.start[n] = (int)at;
+    return over ? RLKV_EFULL : RLKV_OK;
+}
+
+// Strides of rows of `heads` heads: 0 stands for contiguous tokens.
+bool check_stride(const rlkv_paged* p, int heads, int64_t& stride)
+{
+    const int64_t row = (int64_t)heads * p->head_dim;
+    if (!stride) stride = row;
+    return stride >= row && stride % 8 == 0 && stride <= (int64_t)1 << 30;
+}
+
+void fill_rows_args(rlkv_paged* p, int layer, ChunkRowsArgs& a)
+{
+    a.page_table = dev_at<int>(p, p->off_page_table);
+    a.table_stride = p->table_stride;
+    a.n_pages = p->n_pages;
+    a.pool = dev_at<__nv_bfloat16>(p, p->off_pool);
+    a.full_row0 = p->full_row0[layer];
+    a.comp_row0 = p->comp_row0[layer];
+    a.rows_comp = p->rows_comp;
+    a.pool8 = p->fp8 ? p->dev_base + p->off_pool8 : nullptr;
+    a.page0_8 = p->page0_8[layer];
+    a.ring0_8 = p->ring0_8[layer];
+    a.ring_tiles = p->rows_comp / kTile;
+    a.n_full = p->n_full[layer];
+    a.n_comp = p->n_comp[layer];
+    a.kv_heads = p->kv_heads;
+    a.head_dim = p->head_dim;
+    a.sink = p->sink;
+    a.window = p->window;
+    a.slot_of_head = dev_at<int>(p, p->off_tables) + (size_t)layer * p->kv_heads;
+    const float* scales = dev_at<float>(p, p->off_scales) + (size_t)layer * p->kv_heads;
+    const size_t all = (size_t)p->layers * p->kv_heads;
+    a.k_inv = scales;
+    a.v_inv = scales + all;
+    a.k_scale = scales + 2 * all;
+    a.v_scale = scales + 3 * all;
+    for (int h = 0; h < p->kv_heads; ++h) a.head_of_slot[h] = (unsigned char)p->head_of_slot[(size_t)layer * p->kv_heads + h];
+}
+
+// Cuts the flat sequence of the units' key tiles for at most max_ctas CTAs of at least min_tiles tiles; a unit counts `extra`
+// tiles more than it has (its queries' load and its results cost about as much).  split: whether a unit lies in two ranges.
+void plan_chunks(ChunkArgs& a, int subs, int max_ctas, int min_tiles, int extra, bool& split)
+{
+    const int keys = subs == 2 ? 128 : 64, tokens = subs * (128 / a.group);
+    const ChunkSeqs& s = a.seqs;
+    auto unit = [&](int i, int j, bool full) {
+        return chunk_unit(s.len[i], s.start[i + 1] - s.start[i], j, tokens, keys, full, a.sink, a.window).tiles + extra;
+    };
+    auto row_tiles = [&](int i) { return (s.start[i + 1] - s.start[i] + tokens - 1) / tokens; };
+    long long all = 0;
+    for (int i = 0; i < s.n; ++i)
+        for (int j = 0; j < row_tiles(i); ++j) {
+            if (a.n_full) all += (long long)a.n_full * unit(i, j, true);
+            if (a.n_comp) all += (long long)a.n_comp * unit(i, j, false);
+        }
+    long long ctas = all / (min_tiles + extra);
+    if (ctas > max_ctas) ctas = max_ctas;
+    if (ctas < 1) ctas = 1;
+    a.ctas = (int)ctas;
+    split = false;
+    int c = 0;
+    long long x = 0;  // flat tiles before the units at hand
+    auto boundary = [&](int k) { return all * k / ctas; };
+    for (int i = 0; i < s.n; ++i)
+        for (int j = 0; j < row_tiles(i); ++j)
+            for (int comp = 0; comp < 2; ++comp) {
+                const int heads = comp ? a.n_comp : a.n_full;
+                if (!heads) continue;
+                const int each = unit(i, j, !comp);
+                while (c < ctas && boundary(c) < x + (long long)heads * each) {
+                    const long long y = boundary(c) - x;
+                    ChunkPos& at = a.at[c++];
+                    at.seq = (unsigned short)i;
+                    at.head = (unsigned short)((comp ? a.n_full : 0) + (int)(y / each));
+                    at.row_tile = j;
+                    at.tile = (int)(y % each) - extra;
+                    if (at.tile <= 0) at.tile = 0;
+                    else split = true;
+                }
+                x += (long long)heads * each;
+            }
+    for (; c <= ctas; ++c) a.at[c] = ChunkPos{(unsigned short)s.n, 0, 0, 0};
+}
+
+// Whether a launch takes two sub-tiles of 128 rows on one CTA of an SM (one-tile CTAs, two on an SM, otherwise): where most key
+// tiles belong to chunks that fill both.
+int choose_subs(const ChunkArgs& a)
+{
+    long long small = 0, large = 0;
+    for (int i = 0; i < a.seqs.n; ++i) {
+        const int m = a.seqs.start[i + 1] - a.seqs.start[i];
+        const long long rows = (long long)a.n_full * (a.seqs.len[i] + m) + (long long)a.n_comp * (a.sink + a.window + 128);
+        const int tiles = (int)(((long long)m * a.group + 127) / 128);
+        if (tiles > 1) large += rows * tiles;
+        else if (tiles == 1) small += rows;
+    }
+    return large > small ? 2 : 1;
+}
+
+}  // namespace
+
+extern "C" {
+
+int rlkv_paged_set_norms(rlkv_paged* p, const float* q_weight, const float* k_weight, float eps)
+{
+    if (!p) return RLKV_EINVAL;
+    if (q_weight || k_weight) {
+        if (!(eps > 0.f) || !(eps <= 1.f)) return RLKV_EINVAL;
+        for (const float* w : {q_weight, k_weight})
+            if (w && !on_device(w, p->device)) return RLKV_EINVAL;
+    }
+    p->q_norm = q_weight;
+    p->k_norm = k_weight;
+    p->norm_eps = eps;
+    return RLKV_OK;
+}
+
+int rlkv_paged_rotate_chunks(rlkv_paged* p, int layer, const int* slots, const int* counts, int n, const void* q, int64_t q_stride,
+                             const void* k, int64_t k_stride, void* q_out, void* k_out, void* stream)
+{
+    ChunkSeqs s;
+    const int rc = check_chunks(p, layer, slots, nullptr, counts, n, false, s);
+    if (rc) return rc;
+    if (!p->rotary && !p->q_norm && !p->k_norm) return RLKV_EINVAL;
+    if (!check_stride(p, p->q_heads, q_stride) || !check_stride(p, p->kv_heads, k_stride)) return RLKV_EINVAL;
+    for (int i = 0; i < n; ++i)
+        if (p->rotary && counts[i] > 0 && (long long)s.len[i] + counts[i] > p->rotary_rows) return RLKV_EINVAL;
+    if (s.start[n] == 0) return RLKV_OK;
+    if (!q || !k || !q_out || !k_out || !aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out)) return RLKV_EINVAL;
+    DeviceGuard g(p->device);
+    if (!g.ok) return RLKV_ECUDA;
+    NormRotaryArgs a;
+    memset(&a, 0, sizeof a);
+    a.q = static_cast<const __nv_bfloat16*>(q);
+    a.k = static_cast<const __nv_bfloat16*>(k);
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.q_out = static_cast<__nv_bfloat16*>(q_out);
+    a.k_out = static_cast<__nv_bfloat16*>(k_out);
+    a.table = p->rotary;
+    a.positions = p->rotary ? p->rotary_rows : kMaxSeqPages * kTile;
+    a.rot = p->rotary_dim;
+    a.interleaved = p->rotary_interleaved;
+    a.q_weight = p->q_norm ? p->q_norm + (size_t)layer * p->head_dim : nullptr;
+    a.k_weight = p->k_norm ? p->k_norm + (size_t)layer * p->head_dim : nullptr;
+    a.eps = p->norm_eps;
+    a.n = s.start[n];
+    a.q_heads = p->q_heads;
+    a.kv_heads = p->kv_heads;
+    a.head_dim = p->head_dim;
+    RLKV_CUDA(launch_norm_rotary_chunks(a, s, static_cast<cudaStream_t>(stream)));
+    p->launches++;
+    return RLKV_OK;
+}
+
+int rlkv_paged_chunk_attention(rlkv_paged* p, int layer, const int* slots, const int* counts, int n, const void* q, int64_t q_stride,
+                               const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* out, float* lse, void* stream)
+{
+    ChunkArgs a;
+    const int rc = check_chunks(p, layer, slots, nullptr, counts, n, false, a.seqs);
+    if (rc) return rc;
+    if (!check_stride(p, p->q_heads, q_stride) || !check_stride(p, p->kv_heads, k_stride) || !check_stride(p, p->kv_heads, v_stride))
+        return RLKV_EINVAL;
+    const int total = a.seqs.start[n];
+    if (total == 0) return RLKV_OK;
+    if (!q || !k || !v || !out || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3))
+        return RLKV_EINVAL;
+    DeviceGuard g(p->device);
+    if (!g.ok) return RLKV_ECUDA;
+    a.page_table = dev_at<int>(p, p->off_page_table);
+    a.table_stride = p->table_stride;
+    a.n_pages = p->n_pages;
+    a.full_row0 = p->full_row0[layer];
+    a.comp_row0 = p->comp_row0[layer];
+    a.rows_comp = p->rows_comp;
+    a.pool8 = p->fp8 ? p->dev_base + p->off_pool8 : nullptr;
+    a.page0_8 = p->page0_8[layer];
+    a.ring0_8 = p->ring0_8[layer];
+    a.ring_tiles = p->rows_comp / kTile;
+    a.n_full = p->n_full[layer];
+    a.n_comp = p->n_comp[layer];
+    a.group = p->q_heads / p->kv_heads;
+    a.q_heads = p->q_heads;
+    a.sink = p->sink;
+    a.window = p->window;
+    a.scale = 1.f / sqrtf((float)p->head_dim);
+    a.softcap = p->softcap;
+    a.slopes = p->biased ? dev_at<float>(p, p->off_slopes) + (size_t)layer * p->q_heads : nullptr;
+    a.out = static_cast<__nv_bfloat16*>(out);
+    a.lse = lse;
+    a.records = p->chunk_records;
+    a.status = dev_at<int>(p, p->off_status);
+    for (int h = 0; h < p->kv_heads; ++h) {
+        a.head_of_slot[h] = (unsigned char)p->head_of_slot[(size_t)layer * p->kv_heads + h];
+        a.k_scale[h] = p->fp8 ? p->k_scale[(size_t)layer * p->kv_heads + h] : 1.f;
+        a.v_scale[h] = p->fp8 ? p->v_scale[(size_t)layer * p->kv_heads + h] : 1.f;
+    }
+    const int subs = choose_subs(a);
+    const int sms = p->sm_count < kMaxChunkCtas / 2 ? p->sm_count : kMaxChunkCtas / 2;
+    const long long room = (long long)(p->chunk_bytes / (2 * sizeof(float) * chunk_record_floats(p->head_dim, subs)));  // CTAs it has records for
+    int ctas = subs == 2 ? sms : 2 * sms;
+    if (ctas > room) ctas = room < 1 ? 1 : (int)room;
+    bool split;
+    plan_chunks(a, subs, ctas, kMinChunkTiles, kUnitTiles, split);
+    const int keys = subs == 2 ? 128 : 64;
+    ChunkMaps m;
+    int e = encode_heads_map(&m.q, q, total, p->q_heads, p->head_dim, q_stride, a.group, 128 / a.group);
+    if (!e) e = encode_heads_map(&m.k, k, total, p->kv_heads, p->head_dim, k_stride, 1, keys);
+    if (!e) e = encode_heads_map(&m.v, v, total, p->kv_heads, p->head_dim, v_stride, 1, keys);
+    if (!e && !p->fp8) e = encode_heads_map(&m.pool, dev_at<__nv_bfloat16>(p, p->off_pool), p->pool_rows, 1, p->head_dim, p->head_dim, 1, kTile);
+    else if (!e) m.pool = m.k;  // (not used: the 8-bit pool is copied as it lies)
+    if (e) return e;
+    RLKV_CUDA(launch_chunk_attention(a, m, p->head_dim, subs, split, static_cast<cudaStream_t>(stream)));
+    p->launches += split ? 2 : 1;
+    return RLKV_OK;
+}
+
+int rlkv_paged_append_chunks(rlkv_paged* p, int layer, const int* slots, const int* counts, int n, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, void* stream)
+{
+    ChunkSeqs s;
+    int rc = check_chunks(p, layer, slots, nullptr, counts, n, false, s);
+    if (rc) return rc;
+    if (!check_stride(p, p->kv_heads, k_stride) || !check_stride(p, p->kv_heads, v_stride)) return RLKV_EINVAL;
+    if (s.start[n] == 0) return RLKV_OK;
+    if (!k || !v || !aligned16(k) || !aligned16(v)) return RLKV_EINVAL;
+    auto first_page = [&](int i) { return s.len[i] / kTile; };
+    auto end_page = [&](int i) { return counts[i] ? (s.len[i] + counts[i] - 1) / kTile + 1 : first_page(i); };
+    // every page there is room for, before anything changes
+    long long need = 0;
+    for (int i = 0; i < n; ++i)
+        for (int j = first_page(i); j < end_page(i); ++j)
+            if (p->table[(size_t)slots[i] * p->table_stride + j] < 0) ++need;
+    if (need > (long long)p->free_pages.size()) return RLKV_EFULL;
+    DeviceGuard g(p->device);
+    if (!g.ok) return RLKV_ECUDA;
+    for (int i = 0; i < n; ++i)
+        for (int j = first_page(i); j < end_page(i); ++j) {
+            int& entry = p->table[(size_t)slots[i] * p->table_stride + j];
+            if (entry < 0) {
+                entry = p->free_pages.back();
+                p->free_pages.pop_back();
+            }
+        }
+    // launches of as many sequences as the arguments can name pages for (one sequence's always fit)
+    for (int i0 = 0; i0 < n;) {
+        ChunkRowsArgs a;
+        ChunkPages pages;
+        fill_rows_args(p, layer, a);
+        a.k = static_cast<const __nv_bfloat16*>(k);
+        a.v = static_cast<const __nv_bfloat16*>(v);
+        a.k_stride = k_stride;
+        a.v_stride = v_stride;
+        int named = 0, tasks = 0, i = i0;
+        for (; i < n && named + end_page(i) - first_page(i) <= kMaxChunkPages; ++i) {
+            const int x = i - i0, count = end_page(i) - first_page(i);
+            a.seqs.slot[x] = s.slot[i];
+            a.seqs.len[x] = s.len[i];
+            a.seqs.start[x] = s.start[i];
+            pages.first_task[x] = tasks;
+            pages.page0[x] = named;
+            for (int j = 0; j < count; ++j) pages.page[named + j] = p->table[(size_t)slots[i] * p->table_stride + first_page(i) + j];
+            named += count;
+            if (counts[i]) tasks += count * a.n_full + a.ring_tiles * a.n_comp;
+        }
+        a.seqs.n = i - i0;
+        a.seqs.start[i - i0] = s.start[i];
+        pages.first_task[i - i0] = tasks;
+        if (tasks) {
+            RLKV_CUDA(launch_write_chunks(a, pages, static_cast<cudaStream_t>(stream)));
+            p->launches++;
+        }
+        i0 = i;
+    }
+    int* len = len_of(p, layer);
+    for (int i = 0; i < n; ++i) len[slots[i]] += counts[i];
+    return RLKV_OK;
+}
+
+int rlkv_paged_read(rlkv_paged* p, int layer, const int* slots, const int* first, const int* counts, int n, void* k_out, void* v_out,
+                    void* stream)
+{
+    ChunkRowsArgs a;
+    if (!first) return RLKV_EINVAL;
+    const int rc = check_chunks(p, layer, slots, first, counts, n, true, a.seqs);
+    if (rc) return rc;
+    if (a.seqs.start[n] == 0) return RLKV_OK;
+    if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return RLKV_EINVAL;
+    DeviceGuard g(p->device);
+    if (!g.ok) return RLKV_ECUDA;
+    fill_rows_args(p, layer, a);
+    a.k_out = static_cast<__nv_bfloat16*>(k_out);
+    a.v_out = static_cast<__nv_bfloat16*>(v_out);
+    ChunkPages pages;
+    long long tasks = 0;
+    for (int i = 0; i < n; ++i) {
+        a.length[i] = len_of(p, layer)[slots[i]];
+        pages.first_task[i] = (int)tasks;
+        if (counts[i]) tasks += (long long)((first[i] + counts[i] - 1) / kTile - first[i] / kTile + 1) * p->kv_heads;
+        if (tasks >= 1ll << 31) return RLKV_EINVAL;
+    }
+    pages.first_task[n] = (int)tasks;
+    RLKV_CUDA(launch_read_rows(a, pages, static_cast<cudaStream_t>(stream)));
+    p->launches++;
+    return RLKV_OK;
+}
+
+int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full, int n_comp, int group, int sink, int window, int subs,
+                          int max_ctas, int* ctas_out, int* at_out)
+{
+    if (!lens || !counts || n < 1 || n > kMaxPagedBatch || n_full < 0 || n_comp < 0 || n_full + n_comp < 1 || group < 1 || group > kMaxGroup ||
+        sink < 0 || window < 1 || max_ctas < 1 || max_ctas > kMaxChunkCtas || !ctas_out || !at_out)
+        return RLKV_EINVAL;
+    ChunkArgs a;
+    a.seqs.n = n;
+    long long total = 0;
+    for (int i = 0; i < n; ++i) {
+        if (lens[i] < 0 || counts[i] < 0) return RLKV_EINVAL;
+        a.seqs.len[i] = lens[i];
+        a.seqs.start[i] = (int)total;
+        total += counts[i];
+        if (total > kMaxChunkTokens) return RLKV_EINVAL;
+    }
+    if (total < 1) return RLKV_EINVAL;
+    a.seqs.start[n] = (int)total;
+    a.n_full = n_full;
+    a.n_comp = n_comp;
+    a.group = group;
+    a.sink = sink;
+    a.window = window;
+    if (subs == 0) subs = choose_subs(a);
+    if (subs != 1 && subs != 2) return RLKV_EINVAL;
+    bool split;
+    plan_chunks(a, subs, max_ctas, kMinChunkTiles, kUnitTiles, split);
+    for (int c = 0; c <= a.ctas; ++c) {
+        at_out[4 * c] = a.at[c].seq;
+        at_out[4 * c + 1] = a.at[c].row_tile;
+        at_out[4 * c + 2] = a.at[c].head;
+        at_out[4 * c + 3] = a.at[c].tile;
+    }
+    *ctas_out = a.ctas;
+    return RLKV_OK;
+}
+
+}  // extern "C"

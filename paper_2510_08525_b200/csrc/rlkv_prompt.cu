@@ -6,6 +6,7 @@
 #include <new>
 #include <vector>
 
+#include "rlkv_chunk.cuh"
 #include "rlkv_host.cuh"
 #include "rlkv_prompt.cuh"
 
@@ -16,8 +17,12 @@ struct rlkv_prompt {
     float softcap;
     bool biased;
     std::vector<uint8_t> is_full;  // [layers*kv_heads]
-    uint8_t* dev_base;             // status, then slopes [layers][q_heads], then stats (float2) [q_heads][max_tokens]
-    size_t off_slopes, off_stats;
+    uint8_t* dev_base;             // status, then slopes [layers][q_heads], then stats (float2) [q_heads][max_tokens], then the norms' sums
+    size_t off_slopes, off_stats, off_norms;
+    const float* rotary;           // rlkv_prompt_set_rotary: the caller's table of angles (device), null: none set
+    int rotary_rows, rotary_dim, rotary_interleaved;
+    const float *q_norm, *k_norm;  // rlkv_prompt_set_norms: the caller's weights (device), null: none set
+    float norm_eps;
 };
 
 namespace {
@@ -73,9 +78,10 @@ int fill_prompt_args(const rlkv_prompt* p, int layer, const void* q, int64_t q_s
     return RLKV_OK;
 }
 
-// Tensor map over [tokens][heads][head_dim], tokens `stride` elements apart: boxes of 64 elements of one head of
-// `box_tokens` tokens, 128-byte swizzle.  Tokens past the end read as zero.
-int encode_heads_map(CUtensorMap* map, const void* base, int tokens, int heads, int head_dim, int64_t stride, int box_tokens)
+}  // namespace
+
+int rlkv::encode_heads_map(CUtensorMap* map, const void* base, long long tokens, int heads, int head_dim, int64_t stride, int box_heads,
+                           int box_tokens)
 {
     typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                       const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -90,19 +96,17 @@ int encode_heads_map(CUtensorMap* map, const void* base, int tokens, int heads, 
     }
     const cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)tokens};
     const cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)stride * 2};
-    const cuuint32_t box[3] = {64, 1, (cuuint32_t)box_tokens};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens};
     const cuuint32_t one[3] = {1, 1, 1};
     const CUresult r = reinterpret_cast<EncodeTiledFn>(fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides,
                                                            box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
-        snprintf(g_cuda_text, sizeof g_cuda_text, "cuTensorMapEncodeTiled (prompt) failed with CUresult %d", (int)r);
+        snprintf(g_cuda_text, sizeof g_cuda_text, "cuTensorMapEncodeTiled (heads) failed with CUresult %d", (int)r);
         return RLKV_ECUDA;
     }
     return RLKV_OK;
 }
-
-}  // namespace
 
 extern "C" {
 
@@ -127,6 +131,7 @@ int rlkv_prompt_create(rlkv_prompt** out, int layers, int kv_heads, int q_heads,
     if (!p) return RLKV_ENOMEM;
     p->layers = layers; p->kv_heads = kv_heads; p->q_heads = q_heads; p->head_dim = head_dim; p->max_tokens = max_tokens;
     p->sink = sink; p->window = window; p->softcap = softcap; p->biased = biased; p->dev_base = nullptr;
+    p->rotary = p->q_norm = p->k_norm = nullptr; p->rotary_rows = p->rotary_dim = p->rotary_interleaved = 0; p->norm_eps = 0.f;
     try {
         p->is_full.assign(head_is_full, head_is_full + (size_t)layers * kv_heads);
     } catch (const std::bad_alloc&) {
@@ -135,7 +140,8 @@ int rlkv_prompt_create(rlkv_prompt** out, int layers, int kv_heads, int q_heads,
     }
     p->off_slopes = 1024;
     p->off_stats = align_up(p->off_slopes + count * sizeof(float), 1024);
-    const size_t total = p->off_stats + (size_t)max_tokens * q_heads * sizeof(float2);
+    p->off_norms = align_up(p->off_stats + (size_t)max_tokens * q_heads * sizeof(float2), 1024);
+    const size_t total = p->off_norms + (size_t)kMaxNormBlocks * head_dim * sizeof(float);
     cudaError_t e = cudaGetDevice(&p->device);
     if (e != cudaSuccess) { delete p; return cuda_fail(e, "device query"); }
     void* mem = nullptr;
@@ -177,9 +183,9 @@ int rlkv_prompt_attention(rlkv_prompt* p, int layer, const void* q, int64_t q_st
     DeviceGuard g(p->device);
     if (!g.ok) return RLKV_ECUDA;
     CUtensorMap map_q, map_k, map_v;
-    int e = encode_heads_map(&map_q, q, q_tokens, p->q_heads, p->head_dim, a.q_stride, 128);
-    if (!e) e = encode_heads_map(&map_k, k, k_tokens, p->kv_heads, p->head_dim, a.k_stride, 128);
-    if (!e) e = encode_heads_map(&map_v, v, k_tokens, p->kv_heads, p->head_dim, a.v_stride, 128);
+    int e = encode_heads_map(&map_q, q, q_tokens, p->q_heads, p->head_dim, a.q_stride, 1, 128);
+    if (!e) e = encode_heads_map(&map_k, k, k_tokens, p->kv_heads, p->head_dim, a.k_stride, 1, 128);
+    if (!e) e = encode_heads_map(&map_v, v, k_tokens, p->kv_heads, p->head_dim, a.v_stride, 1, 128);
     if (e) return e;
     RLKV_CUDA(launch_prompt_forward(a, map_q, map_k, map_v, p->head_dim, static_cast<cudaStream_t>(stream)));
     return RLKV_OK;
@@ -202,12 +208,113 @@ int rlkv_prompt_attention_backward(rlkv_prompt* p, int layer, const void* q, int
     DeviceGuard g(p->device);
     if (!g.ok) return RLKV_ECUDA;
     CUtensorMap map_q, map_k, map_v, map_do;
-    int e = encode_heads_map(&map_q, q, q_tokens, p->q_heads, p->head_dim, a.q_stride, 128);
-    if (!e) e = encode_heads_map(&map_k, k, k_tokens, p->kv_heads, p->head_dim, a.k_stride, 128);
-    if (!e) e = encode_heads_map(&map_v, v, k_tokens, p->kv_heads, p->head_dim, a.v_stride, 128);
-    if (!e) e = encode_heads_map(&map_do, dout, q_tokens, p->q_heads, p->head_dim, (int64_t)p->q_heads * p->head_dim, 128);
+    int e = encode_heads_map(&map_q, q, q_tokens, p->q_heads, p->head_dim, a.q_stride, 1, 128);
+    if (!e) e = encode_heads_map(&map_k, k, k_tokens, p->kv_heads, p->head_dim, a.k_stride, 1, 128);
+    if (!e) e = encode_heads_map(&map_v, v, k_tokens, p->kv_heads, p->head_dim, a.v_stride, 1, 128);
+    if (!e) e = encode_heads_map(&map_do, dout, q_tokens, p->q_heads, p->head_dim, (int64_t)p->q_heads * p->head_dim, 1, 128);
     if (e) return e;
     RLKV_CUDA(launch_prompt_backward(a, map_q, map_k, map_v, map_do, p->head_dim, static_cast<cudaStream_t>(stream)));
+    return RLKV_OK;
+}
+
+int rlkv_prompt_set_rotary(rlkv_prompt* p, const void* table, int positions, int rot_dim, int interleaved)
+{
+    if (!p) return RLKV_EINVAL;
+    if (table && (positions < 1 || rot_dim < 16 || rot_dim % 16 || rot_dim > p->head_dim || !on_device(table, p->device))) return RLKV_EINVAL;
+    p->rotary = static_cast<const float*>(table);
+    p->rotary_rows = table ? positions : 0;
+    p->rotary_dim = rot_dim;
+    p->rotary_interleaved = interleaved ? 1 : 0;
+    return RLKV_OK;
+}
+
+int rlkv_prompt_set_norms(rlkv_prompt* p, const float* q_weight, const float* k_weight, float eps)
+{
+    if (!p) return RLKV_EINVAL;
+    if (q_weight || k_weight) {
+        if (!(eps > 0.f) || !(eps <= 1.f)) return RLKV_EINVAL;
+        for (const float* w : {q_weight, k_weight})
+            if (w && !on_device(w, p->device)) return RLKV_EINVAL;
+    }
+    p->q_norm = q_weight;
+    p->k_norm = k_weight;
+    p->norm_eps = eps;
+    return RLKV_OK;
+}
+
+// What the two directions share.
+static int norm_rotary_args(const rlkv_prompt* p, int layer, const void* q, int64_t q_stride, const void* k, int64_t k_stride, int tokens,
+                            const int* positions, NormRotaryArgs& a)
+{
+    if (!p || layer < 0 || layer >= p->layers || !q || !k || !aligned16(q) || !aligned16(k) || tokens < 1 || tokens > p->max_tokens ||
+        (reinterpret_cast<uintptr_t>(positions) & 3))
+        return RLKV_EINVAL;
+    if (!p->rotary && !p->q_norm && !p->k_norm) return RLKV_EINVAL;
+    const int64_t q_row = (int64_t)p->q_heads * p->head_dim, kv_row = (int64_t)p->kv_heads * p->head_dim;
+    if (!q_stride) q_stride = q_row;
+    if (!k_stride) k_stride = kv_row;
+    if (q_stride < q_row || k_stride < kv_row || q_stride % 8 || k_stride % 8) return RLKV_EINVAL;
+    memset(&a, 0, sizeof a);
+    a.q = static_cast<const __nv_bfloat16*>(q);
+    a.k = static_cast<const __nv_bfloat16*>(k);
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.table = p->rotary;
+    a.positions = p->rotary ? p->rotary_rows : INT_MAX;
+    a.rot = p->rotary_dim;
+    a.interleaved = p->rotary_interleaved;
+    a.q_weight = p->q_norm ? p->q_norm + (size_t)layer * p->head_dim : nullptr;
+    a.k_weight = p->k_norm ? p->k_norm + (size_t)layer * p->head_dim : nullptr;
+    a.eps = p->norm_eps;
+    a.position = positions;
+    a.n = tokens;
+    a.q_heads = p->q_heads;
+    a.kv_heads = p->kv_heads;
+    a.head_dim = p->head_dim;
+    return RLKV_OK;
+}
+
+int rlkv_prompt_rotate(rlkv_prompt* p, int layer, const void* q, int64_t q_stride, const void* k, int64_t k_stride, int tokens,
+                       const int* positions, void* q_out, void* k_out, void* stream)
+{
+    NormRotaryArgs a;
+    const int rc = norm_rotary_args(p, layer, q, q_stride, k, k_stride, tokens, positions, a);
+    if (rc) return rc;
+    if (!q_out || !k_out || !aligned16(q_out) || !aligned16(k_out)) return RLKV_EINVAL;
+    a.q_out = static_cast<__nv_bfloat16*>(q_out);
+    a.k_out = static_cast<__nv_bfloat16*>(k_out);
+    DeviceGuard g(p->device);
+    if (!g.ok) return RLKV_ECUDA;
+    RLKV_CUDA(launch_norm_rotary(a, static_cast<cudaStream_t>(stream)));
+    return RLKV_OK;
+}
+
+int rlkv_prompt_rotate_backward(rlkv_prompt* p, int layer, const void* q, int64_t q_stride, const void* k, int64_t k_stride, int tokens,
+                                const int* positions, const void* dq_out, const void* dk_out, void* dq, int64_t dq_stride, void* dk,
+                                int64_t dk_stride, float* dq_weight, float* dk_weight, void* stream)
+{
+    NormRotaryArgs a;
+    const int rc = norm_rotary_args(p, layer, q, q_stride, k, k_stride, tokens, positions, a);
+    if (rc) return rc;
+    if (!dq_out || !dk_out || !dq || !dk || !aligned16(dq_out) || !aligned16(dk_out) || !aligned16(dq) || !aligned16(dk)) return RLKV_EINVAL;
+    if ((reinterpret_cast<uintptr_t>(dq_weight) | reinterpret_cast<uintptr_t>(dk_weight)) & 3) return RLKV_EINVAL;
+    if ((dq_weight && !p->q_norm) || (dk_weight && !p->k_norm)) return RLKV_EINVAL;
+    const int64_t q_row = (int64_t)p->q_heads * p->head_dim, kv_row = (int64_t)p->kv_heads * p->head_dim;
+    if (!dq_stride) dq_stride = q_row;
+    if (!dk_stride) dk_stride = kv_row;
+    if (dq_stride < q_row || dk_stride < kv_row || dq_stride % 8 || dk_stride % 8) return RLKV_EINVAL;
+    a.dq_out = static_cast<const __nv_bfloat16*>(dq_out);
+    a.dk_out = static_cast<const __nv_bfloat16*>(dk_out);
+    a.dq = static_cast<__nv_bfloat16*>(dq);
+    a.dk = static_cast<__nv_bfloat16*>(dk);
+    a.dq_stride = dq_stride;
+    a.dk_stride = dk_stride;
+    a.dq_weight = dq_weight;
+    a.dk_weight = dk_weight;
+    a.partials = reinterpret_cast<float*>(p->dev_base + p->off_norms);
+    DeviceGuard g(p->device);
+    if (!g.ok) return RLKV_ECUDA;
+    RLKV_CUDA(launch_norm_rotary_backward(a, static_cast<cudaStream_t>(stream)));
     return RLKV_OK;
 }
 

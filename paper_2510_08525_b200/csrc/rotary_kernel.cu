@@ -5,15 +5,12 @@
 // angle t * inv_freq[j] of pair j (pairs (j, j + rot/2) or, interleaved, (2j, 2j + 1)); elements past
 // `rot` pass through.  The products are computed in fp32 on the bf16 inputs and rounded ONCE: to bf16 for
 // the rotated queries, the prompt's rotated keys and 16-bit rows, to the E4M3 code for 8-bit pages (from
-// the fp32 value, not from its bf16 rounding).  Where a row goes is the rule of append_kernel.cu.
-#include <cuda_fp8.h>
-
-#include "rlkv_internal.cuh"
+// the fp32 value, not from its bf16 rounding).  With norms set, a query or key head is first divided by the root of its mean
+// square and multiplied by the norm's weight, in fp32 as well: the lanes that hold a row's pieces add up its squares.  Where a row goes is the rule of append_kernel.cu.
+#include "rotary.cuh"
 
 namespace rlkv {
 namespace {
-
-constexpr int kPiece = 16;  // elements one thread turns: eight pairs, so two 16-byte loads and one 64-byte table read
 
 // Where the K (kv = 0) or V (kv = 1) row of a token lands; `slot`: the head's place among the heads of its class.
 struct RowPlace {
@@ -47,42 +44,6 @@ __device__ __forceinline__ RowPlace place_of(const PagedAppendArgs& a, int slot,
     return p;
 }
 
-__device__ __forceinline__ void rotate(float& u, float& v, float2 cs)
-{
-    const float x = u, y = v;
-    u = fmaf(x, cs.x, -__fmul_rn(y, cs.y));
-    v = fmaf(y, cs.x, __fmul_rn(x, cs.y));
-}
-
-__device__ __forceinline__ void unpack8(const uint4& bits, float (&x)[8])
-{
-    const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&bits);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float2 f = __bfloat1622float2(p[j]);
-        x[2 * j] = f.x;
-        x[2 * j + 1] = f.y;
-    }
-}
-
-__device__ __forceinline__ uint4 pack8(const float (&x)[8])
-{
-    uint4 bits;
-    __nv_bfloat162* p = reinterpret_cast<__nv_bfloat162*>(&bits);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) p[j] = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
-    return bits;
-}
-
-__device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv)
-{
-    uint2 bits;
-    unsigned char* c = reinterpret_cast<unsigned char*>(&bits);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) c[j] = (unsigned char)__nv_cvt_float_to_fp8(x[j] * inv, __NV_SATFINITE, __NV_E4M3);
-    return bits;
-}
-
 // Bound by memory: 8192 tokens of 32 / 8 heads of 128 read and write 210 MB in 41 us, 5.1 TB/s (78 % of a copy's rate).  One
 // thread per piece and head, its angles read again for every head, took 57 us; two or eight heads' loads at a time 49 and 60
 // (fewer in flight; fewer threads), more threads with spilled registers 62.  Few tokens are launch latency: 2.5 us.
@@ -90,7 +51,7 @@ __device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv)
 // a V thread writes its sixteen transposed codes one byte at a time.
 // A block takes 256 / PIECES tokens and `heads` of the heads (numbered q heads, K heads, V heads).  A thread keeps
 // one piece of one token: its eight angles stay in registers over the heads, whose loads are issued four at a time.
-template <int PIECES>
+template <int PIECES, bool NORM>
 __global__ void __launch_bounds__(256) rotated_append_kernel(const __grid_constant__ RotatedAppendArgs r, const int heads)
 {
     constexpr int kTokens = 256 / PIECES, kBatch = 4;
@@ -114,13 +75,7 @@ __global__ void __launch_bounds__(256) rotated_append_kernel(const __grid_consta
         const bool turned = piece * kPiece < r.rot;
         float2 f[8];
         if (turned && from < q_heads + a.kv_heads) {
-            const float4* cs = reinterpret_cast<const float4*>(r.table + (long long)t * r.rot + piece * kPiece);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 v = __ldg(cs + j);
-                f[2 * j] = make_float2(v.x, v.y);
-                f[2 * j + 1] = make_float2(v.z, v.w);
-            }
+            load_angles(r.table, t, r.rot, piece, f);
         }
         for (int base = from; base < to; base += kBatch) {
             uint4 b[kBatch][2];
@@ -148,17 +103,22 @@ __global__ void __launch_bounds__(256) rotated_append_kernel(const __grid_consta
                 float x0[8], x1[8];
                 unpack8(b[x][0], x0);
                 unpack8(b[x][1], x1);
-                if (turn) {
-                    if (r.interleaved) {
+                if (NORM && !is_v) {
+                    const float* weight = is_q ? r.q_weight : r.k_weight;
+                    if (weight) {
+                        const float rms = row_rsqrt<PIECES>(x0, x1, r.eps);
+                        float w0[8], w1[8];
+                        load8(weight + c0, w0);
+                        load8(weight + c1, w1);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            rotate(x0[2 * j], x0[2 * j + 1], f[j]);
-                            rotate(x1[2 * j], x1[2 * j + 1], f[4 + j]);
+                        for (int j = 0; j < 8; ++j) {
+                            x0[j] = x0[j] * rms * w0[j];
+                            x1[j] = x1[j] * rms * w1[j];
                         }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) rotate(x0[j], x1[j], f[j]);
                     }
+                }
+                if (turn) rotate_piece(x0, x1, f, r.interleaved);
+                if (turn || (NORM && !is_v)) {
                     b[x][0] = pack8(x0);
                     b[x][1] = pack8(x1);
                 }
@@ -228,8 +188,13 @@ cudaError_t launch_rotated_append(const RotatedAppendArgs& a, cudaStream_t strea
     int heads = 1;
     while (heads < 8 && (long long)tiles * ((rows + 2 * heads - 1) / (2 * heads)) >= 148 * 8) heads *= 2;
     const dim3 grid(tiles, (rows + heads - 1) / heads);
-    if (pieces == 8) rotated_append_kernel<8><<<grid, 256, 0, stream>>>(a, heads);
-    else rotated_append_kernel<4><<<grid, 256, 0, stream>>>(a, heads);
+    if (a.q_weight || a.k_weight) {
+        if (pieces == 8) rotated_append_kernel<8, true><<<grid, 256, 0, stream>>>(a, heads);
+        else rotated_append_kernel<4, true><<<grid, 256, 0, stream>>>(a, heads);
+    } else {
+        if (pieces == 8) rotated_append_kernel<8, false><<<grid, 256, 0, stream>>>(a, heads);
+        else rotated_append_kernel<4, false><<<grid, 256, 0, stream>>>(a, heads);
+    }
     return cudaGetLastError();
 }
 

@@ -173,6 +173,34 @@ class PagedCache:
         rl.rlkv_paged_prefill_rotated(self.handle, layer, slot, q, k, v, k.shape[0], q_out, k_out)
         return q_out, k_out
 
+    def set_norms(self, q_weight, k_weight, eps=1e-6):
+        """Norms of the rotated calls: fp32 [layers][head_dim] on the cache's device, or None; kept alive with the cache."""
+        rl.rlkv_paged_set_norms(self.handle, q_weight, k_weight, eps)
+
+    def rotate_chunks(self, layer, slots, counts, q, k):
+        """New tokens of several sequences, packed: returns the queries and keys with the cache's norms and rotation."""
+        _check_rows(self, q, k, k)
+        q_out, k_out = (torch.empty(x.shape, dtype=torch.bfloat16, device=self.device) for x in (q, k))
+        rl.rlkv_paged_rotate_chunks(self.handle, layer, slots, counts, q, k, q_out, k_out)
+        return q_out, k_out
+
+    def attend_chunks(self, layer, slots, counts, q, k, v):
+        """Attention of new tokens over the cache and themselves, before they are appended; returns out and lse."""
+        _check_rows(self, q, k, v)
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device)
+        rl.rlkv_paged_chunk_attention(self.handle, layer, slots, counts, q, k, v, out, lse)
+        return out, lse
+
+    def append_chunks(self, layer, slots, counts, k, v):
+        rl.rlkv_paged_append_chunks(self.handle, layer, slots, counts, k, v)
+
+    def read(self, layer, slots, first, counts):
+        """K and V rows of tokens first[i] .. first[i] + counts[i] - 1 of each sequence, packed."""
+        k, v = (torch.empty((int(np.sum(counts)), self.kv_heads, self.head_dim), dtype=torch.bfloat16, device=self.device) for _ in range(2))
+        rl.rlkv_paged_read(self.handle, layer, slots, first, counts, k, v)
+        return k, v
+
     def set_scores(self, softcap=0.0, slopes=None):
         if slopes is not None and np.size(slopes) != self.layers * self.q_heads:
             raise ValueError("slopes must have layers*q_heads entries")
@@ -249,6 +277,31 @@ class PromptAttention:
         dq, dk, dv = (torch.zeros(x.shape, dtype=torch.bfloat16, device=self.device) for x in (q, k, v))
         rl.rlkv_prompt_attention_backward(self.handle, layer, q, k, v, q_starts, k_starts, prefix, out, lse, dout, dq, dk, dv)
         return dq, dk, dv
+
+    def set_rotary(self, table, rot_dim, interleaved=False):
+        """As PagedCache.set_rotary."""
+        if table is not None and (table.dtype != torch.float32 or tuple(table.shape[1:]) != (rot_dim // 2, 2)):
+            raise ValueError("the table is fp32 [positions][rot_dim / 2][2]")
+        rl.rlkv_prompt_set_rotary(self.handle, table, 0 if table is None else table.shape[0], rot_dim, interleaved)
+
+    def set_norms(self, q_weight, k_weight, eps=1e-6):
+        """As PagedCache.set_norms."""
+        rl.rlkv_prompt_set_norms(self.handle, q_weight, k_weight, eps)
+
+    def rotate(self, layer, q, k, positions=None):
+        """q and k normalised and rotated by their positions (int32; rows of tokens at negative ones are zero)."""
+        _check_rows(self, q, k, k)
+        q_out, k_out = (torch.zeros(x.shape, dtype=torch.bfloat16, device=self.device) for x in (q, k))
+        rl.rlkv_prompt_rotate(self.handle, layer, q, k, positions, q_out, k_out)
+        return q_out, k_out
+
+    def rotate_backward(self, layer, q, k, dq_out, dk_out, positions=None, weights=True):
+        """Returns dq, dk and, with `weights`, the gradients of the norms' weights."""
+        _check_rows(self, q, k, k)
+        dq, dk = (torch.zeros(x.shape, dtype=torch.bfloat16, device=self.device) for x in (q, k))
+        dw = [torch.empty(self.head_dim, dtype=torch.float32, device=self.device) for _ in range(2)] if weights else [None, None]
+        rl.rlkv_prompt_rotate_backward(self.handle, layer, q, k, positions, dq_out, dk_out, dq, dk, *dw)
+        return (dq, dk, *dw) if weights else (dq, dk)
 
     def status(self) -> int:
         return rl.rlkv_prompt_kernel_status(self.handle)

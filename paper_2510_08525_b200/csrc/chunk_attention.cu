@@ -25,6 +25,8 @@
 // are fp32).  P is rounded to bf16 for the product, half a step 2^-8 of each weight; l sums the fp32 values.  Scales of an 8-bit
 // cache never touch the codes: K's goes into the score's factor; O is kept in units of V's and multiplied by it once, before
 // the chunk's first tile or at the end.
+#include <cuda_fp16.h>
+
 #include "rlkv_chunk.cuh"
 #include "rlkv_prompt.cuh"
 #include "tcgen05.cuh"
@@ -46,15 +48,15 @@ struct Chunk {
     static constexpr int kPages = kKeys / kTile;
     static constexpr int kQBytes = kRows * D * 2, kTileBytes = kKeys * D * 2;
     static constexpr int kBlock = kKeys * 128;  // bytes of a [kKeys][64 elements] block
-    static constexpr int kStages = FP8 ? (SUBS == 2 ? 4 : 3) : D == 128 ? 5 : 10;
-    static constexpr int kRaw = FP8 ? 2 : 0;  // pages
-    static constexpr int kState = SUBS * kQBytes + kStages * kTileBytes + kRaw * kPageBytes;
+    static constexpr int kStages = FP8 ? 3 : D == 128 ? 5 : 10;  // K or V tiles in the ring; of an 8-bit cache, the codes of both
+    static constexpr int kDecoded = FP8 ? 2 : 0;                 // decoded V tiles
+    static constexpr int kState = SUBS * kQBytes + (kStages + kDecoded) * kTileBytes;
     static constexpr int kSmem = kState + 1024 * SUBS;
     static constexpr int kSoftmaxWarps = 4 * SUBS;
     static constexpr int kThreads = 32 * (kSoftmaxWarps + 4 + (FP8 ? 4 : 0));
     static constexpr int kPerSm = SUBS == 2 ? 1 : 2;
     static constexpr int kColumns = SUBS == 2 ? 512 : 256;  // of tensor memory: two S/P places, then O
-    static constexpr int kFills = FP8 ? 4 : 1;  // arrivals that fill a stage: the decoding warps', or one copy's
+    static constexpr int kReleases = FP8 ? 5 : 1;           // arrivals that free a stage: the products' end, and the decoding warps
 };
 
 // The part of a CTA's range that lies in one unit.
@@ -64,6 +66,7 @@ struct Segment {
     int head;                 // KV head
     bool full;
     int index;                // among the heads of its class
+    int fresh;                // the chunk's own key tiles; the cached ones come behind them
     int t0, t1, subs;         // key tiles, sub-tiles that hold rows
     int record;               // -1: the whole unit, whose rows are final
 };
@@ -75,7 +78,8 @@ struct SoftmaxPlace {
 };
 
 struct ChunkShared {
-    uint64_t q_full, q_empty[2], full[10], empty[10], dirty[10], clean[10], raw_full[2], raw_empty[2], s_full[2], p_full[2][2], pv_done[2], drain;
+    uint64_t q_full[2], q_split[2], q_empty[2], full[10], empty[10], dirty[10], clean[10], decoded[2], decoded_empty[2];
+    uint64_t s_full[2], p_full[2][2], pv_done[2], drain;
     uint32_t tmem;
     int abort;
     SoftmaxPlace place[1];  // (one of each softmax warp)
@@ -94,11 +98,142 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
     return ok != 0;
 }
 
-// `bytes` (a multiple of 16) from 16-byte aligned global to shared memory.
-__device__ __forceinline__ void load_bytes(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
+// An 8-bit page: 128 rows of 128 bytes from row `row` on, 128-byte swizzle.
+__device__ __forceinline__ void load_page(uint32_t dst, const CUtensorMap* map, int row, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(0),
+                 "r"(row), "r"(bar)
                  : "memory");
+}
+
+// E4M3 x E4M3 -> fp32, 32 elements of the contraction; both operands in shared memory, rows of 128 bytes.
+__host__ __device__ constexpr uint32_t instr_desc8(int m, int n) { return 1u << 4 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24; }
+__device__ __forceinline__ void mma_ss8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+
+// Four numbers to E4M3 (nearest, saturating) and back.
+__device__ __forceinline__ uint32_t codes4(float2 f, float2 g)
+{
+    uint32_t d;
+    asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\n\tmov.b32 %0, {a, b};\n\t}"
+        : "=r"(d)
+        : "f"(f.x), "f"(f.y), "f"(g.x), "f"(g.y));
+    return d;
+}
+__device__ __forceinline__ void values4(uint32_t codes, float2& f, float2& g)
+{
+    uint32_t a, b;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+        : "=&r"(a), "=&r"(b)
+        : "r"(codes));
+    f = __half22float2(*reinterpret_cast<const __half2*>(&a));
+    g = __half22float2(*reinterpret_cast<const __half2*>(&b));
+}
+
+// A query row of 128 bf16 elements in shared memory (two runs of 128 bytes, swizzled by the row) becomes, in place, two rows of
+// E4M3: x 2^e = a + b, a rounded to four bits, b what is left.  2^e brings the largest element to 128 .. 256; a bf16 number has
+// eight bits, so a + b is exact down to 2^-10 of the largest element and off by at most 2^-18 of it below -- less than what
+// bf16 itself leaves of such an element next to it.  Returns 2^-e.
+__device__ __forceinline__ float split_row(uint8_t* q, int row)
+{
+    uint4* at[2] = {reinterpret_cast<uint4*>(q + row * 128), reinterpret_cast<uint4*>(q + kQBlock + row * 128)};
+    uint4 x[16];
+#pragma unroll
+    for (int c = 0; c < 16; ++c) x[c] = at[c / 8][(c & 7) ^ (row & 7)];
+    __nv_bfloat162 top = __float2bfloat162_rn(0.f);
+    const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(x);
+#pragma unroll
+    for (int i = 0; i < 64; ++i) top = __hmax2(top, __habs2(p[i]));
+    const float big = fmaxf(__low2float(top), __high2float(top));
+    const int exponent = min(max((__float_as_int(big) >> 23 & 255) - 134, -126), 120);  // of the largest element's distance from 2^7
+    const float up = __int_as_float((127 - exponent) << 23), down = __int_as_float((127 + exponent) << 23);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {  // sixteen elements: sixteen bytes of a and of b
+        uint32_t a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float2 f = __bfloat1622float2(p[c * 8 + 2 * i]), g = __bfloat1622float2(p[c * 8 + 2 * i + 1]), r, t;
+            f = mul2(f, make_float2(up, up));
+            g = mul2(g, make_float2(up, up));
+            a[i] = codes4(f, g);
+            values4(a[i], r, t);
+            b[i] = codes4(make_float2(f.x - r.x, f.y - r.y), make_float2(g.x - t.x, g.y - t.y));
+        }
+        at[0][c ^ (row & 7)] = make_uint4(a[0], a[1], a[2], a[3]);
+        at[1][c ^ (row & 7)] = make_uint4(b[0], b[1], b[2], b[3]);
+    }
+    return down;
+}
+
+// A row's columns, waited for in the same statement: none of them can be spilled before it has arrived.
+__device__ __forceinline__ void read_columns(uint32_t addr, float (&s)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(s[0]), "=f"(s[1]), "=f"(s[2]), "=f"(s[3]), "=f"(s[4]), "=f"(s[5]), "=f"(s[6]), "=f"(s[7]), "=f"(s[8]), "=f"(s[9]),
+          "=f"(s[10]), "=f"(s[11]), "=f"(s[12]), "=f"(s[13]), "=f"(s[14]), "=f"(s[15]), "=f"(s[16]), "=f"(s[17]), "=f"(s[18]),
+          "=f"(s[19]), "=f"(s[20]), "=f"(s[21]), "=f"(s[22]), "=f"(s[23]), "=f"(s[24]), "=f"(s[25]), "=f"(s[26]), "=f"(s[27]),
+          "=f"(s[28]), "=f"(s[29]), "=f"(s[30]), "=f"(s[31])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void read_columns(uint32_t addr, float (&s)[64])
+{
+    asm volatile(
+        "{\n\t.reg .b32 at;\n\tmov.b32 at, %64;\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [at];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+        "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [at+32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;\n\t}"
+        : "=f"(s[0]), "=f"(s[1]), "=f"(s[2]), "=f"(s[3]), "=f"(s[4]), "=f"(s[5]), "=f"(s[6]), "=f"(s[7]), "=f"(s[8]), "=f"(s[9]),
+          "=f"(s[10]), "=f"(s[11]), "=f"(s[12]), "=f"(s[13]), "=f"(s[14]), "=f"(s[15]), "=f"(s[16]), "=f"(s[17]), "=f"(s[18]),
+          "=f"(s[19]), "=f"(s[20]), "=f"(s[21]), "=f"(s[22]), "=f"(s[23]), "=f"(s[24]), "=f"(s[25]), "=f"(s[26]), "=f"(s[27]),
+          "=f"(s[28]), "=f"(s[29]), "=f"(s[30]), "=f"(s[31]), "=f"(s[32]), "=f"(s[33]), "=f"(s[34]), "=f"(s[35]), "=f"(s[36]),
+          "=f"(s[37]), "=f"(s[38]), "=f"(s[39]), "=f"(s[40]), "=f"(s[41]), "=f"(s[42]), "=f"(s[43]), "=f"(s[44]), "=f"(s[45]),
+          "=f"(s[46]), "=f"(s[47]), "=f"(s[48]), "=f"(s[49]), "=f"(s[50]), "=f"(s[51]), "=f"(s[52]), "=f"(s[53]), "=f"(s[54]),
+          "=f"(s[55]), "=f"(s[56]), "=f"(s[57]), "=f"(s[58]), "=f"(s[59]), "=f"(s[60]), "=f"(s[61]), "=f"(s[62]), "=f"(s[63])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void read_columns(uint32_t addr, float (&s)[128])
+{
+    asm volatile(
+        "{\n\t.reg .b32 at;\n\tmov.b32 at, %128;\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [at];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+        "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [at+32];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%64,%65,%66,%67,%68,%69,%70,%71,%72,%73,%74,%75,%76,%77,%78,%79,"
+        "%80,%81,%82,%83,%84,%85,%86,%87,%88,%89,%90,%91,%92,%93,%94,%95}, [at+64];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%96,%97,%98,%99,%100,%101,%102,%103,%104,%105,%106,%107,%108,%109,%110,%111,"
+        "%112,%113,%114,%115,%116,%117,%118,%119,%120,%121,%122,%123,%124,%125,%126,%127}, [at+96];\n\t"
+        "tcgen05.wait::ld.sync.aligned;\n\t}"
+        : "=f"(s[0]), "=f"(s[1]), "=f"(s[2]), "=f"(s[3]), "=f"(s[4]), "=f"(s[5]), "=f"(s[6]), "=f"(s[7]), "=f"(s[8]), "=f"(s[9]),
+          "=f"(s[10]), "=f"(s[11]), "=f"(s[12]), "=f"(s[13]), "=f"(s[14]), "=f"(s[15]), "=f"(s[16]), "=f"(s[17]), "=f"(s[18]),
+          "=f"(s[19]), "=f"(s[20]), "=f"(s[21]), "=f"(s[22]), "=f"(s[23]), "=f"(s[24]), "=f"(s[25]), "=f"(s[26]), "=f"(s[27]),
+          "=f"(s[28]), "=f"(s[29]), "=f"(s[30]), "=f"(s[31]), "=f"(s[32]), "=f"(s[33]), "=f"(s[34]), "=f"(s[35]), "=f"(s[36]),
+          "=f"(s[37]), "=f"(s[38]), "=f"(s[39]), "=f"(s[40]), "=f"(s[41]), "=f"(s[42]), "=f"(s[43]), "=f"(s[44]), "=f"(s[45]),
+          "=f"(s[46]), "=f"(s[47]), "=f"(s[48]), "=f"(s[49]), "=f"(s[50]), "=f"(s[51]), "=f"(s[52]), "=f"(s[53]), "=f"(s[54]),
+          "=f"(s[55]), "=f"(s[56]), "=f"(s[57]), "=f"(s[58]), "=f"(s[59]), "=f"(s[60]), "=f"(s[61]), "=f"(s[62]), "=f"(s[63]),
+          "=f"(s[64]), "=f"(s[65]), "=f"(s[66]), "=f"(s[67]), "=f"(s[68]), "=f"(s[69]), "=f"(s[70]), "=f"(s[71]), "=f"(s[72]),
+          "=f"(s[73]), "=f"(s[74]), "=f"(s[75]), "=f"(s[76]), "=f"(s[77]), "=f"(s[78]), "=f"(s[79]), "=f"(s[80]), "=f"(s[81]),
+          "=f"(s[82]), "=f"(s[83]), "=f"(s[84]), "=f"(s[85]), "=f"(s[86]), "=f"(s[87]), "=f"(s[88]), "=f"(s[89]), "=f"(s[90]),
+          "=f"(s[91]), "=f"(s[92]), "=f"(s[93]), "=f"(s[94]), "=f"(s[95]), "=f"(s[96]), "=f"(s[97]), "=f"(s[98]), "=f"(s[99]),
+          "=f"(s[100]), "=f"(s[101]), "=f"(s[102]), "=f"(s[103]), "=f"(s[104]), "=f"(s[105]), "=f"(s[106]), "=f"(s[107]),
+          "=f"(s[108]), "=f"(s[109]), "=f"(s[110]), "=f"(s[111]), "=f"(s[112]), "=f"(s[113]), "=f"(s[114]), "=f"(s[115]),
+          "=f"(s[116]), "=f"(s[117]), "=f"(s[118]), "=f"(s[119]), "=f"(s[120]), "=f"(s[121]), "=f"(s[122]), "=f"(s[123]),
+          "=f"(s[124]), "=f"(s[125]), "=f"(s[126]), "=f"(s[127])
+        : "r"(addr)
+        : "memory");
 }
 
 // P = 2^(s factor - base) of a row's scores, as bf16 to tensor memory, and their sums; 64 keys at a time, so that the
@@ -169,6 +304,7 @@ struct Walk {
         s.head = a.head_of_slot[at.head];
         s.u = chunk_unit(s.len, s.m, at.row_tile, SUBS * tokens, KEYS, s.full, a.sink, a.window);
         s.subs = SUBS == 2 && s.m - s.u.tok0 > tokens ? 2 : 1;
+        s.fresh = s.u.tiles - s.u.cached;
         s.t0 = at.tile;
         const bool last = same_unit(at, end);
         s.t1 = last ? end.tile : s.u.tiles;
@@ -189,24 +325,17 @@ struct Walk {
         }
         return true;
     }
-    // First chunk token of key tile t >= cached.
-    static __device__ __forceinline__ int chunk_tile(const volatile ChunkUnit& u, int t)
-    {
-        const int x = t - u.cached;
-        return (x < u.a_end ? x : u.b0 + x - u.a_end) * KEYS;
-    }
-    // Whether the K (v 0) or V rows of key tile t are to be cleared where they hold no token: V always (0 * NaN), K where what it
-    // holds has a say in how a warp computes the cap; decoded rows are finite, and cleared as they are written.
-    template <bool FP8, bool CAP>
-    static __device__ __forceinline__ bool unclean(const Segment& s, int t, int v)
-    {
-        return (v || CAP) && (!FP8 || t >= s.u.cached) && valid_rows(s, t) < KEYS;
-    }
+    // First chunk token of key tile t < fresh.
+    static __device__ __forceinline__ int chunk_tile(const volatile ChunkUnit& u, int t) { return (t < u.a_end ? t : u.b0 + t - u.a_end) * KEYS; }
     // Rows of key tile t that hold a token (KEYS or more: all of them).
     static __device__ __forceinline__ int valid_rows(const Segment& s, int t)
     {
-        return t < s.u.cached ? s.u.rows - t * KEYS : s.m - chunk_tile(s.u, t);
+        return t < s.fresh ? s.m - chunk_tile(s.u, t) : s.u.rows - (t - s.fresh) * KEYS;
     }
+    // Whether the V rows of key tile t are to be cleared where they hold no token: 0 * NaN of what lies there would be NaN.
+    // (Decoded codes are finite.)
+    template <bool FP8>
+    static __device__ __forceinline__ bool unclean(const Segment& s, int t) { return (!FP8 || t < s.fresh) && valid_rows(s, t) < KEYS; }
 };
 
 template <int D, int SUBS, bool FP8, bool CAP, bool BIAS>
@@ -234,19 +363,20 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
             prefetch_map(&maps.q);
             prefetch_map(&maps.k);
             prefetch_map(&maps.v);
-            if (!FP8) prefetch_map(&maps.pool);
+            prefetch_map(&maps.pool);
             sh.abort = 0;
-            mbar_init(smem_u32(&sh.q_full), 1);
             for (int i = 0; i < C::kStages; ++i) {
-                mbar_init(smem_u32(&sh.full[i]), C::kFills);
-                mbar_init(smem_u32(&sh.empty[i]), 1);
+                mbar_init(smem_u32(&sh.full[i]), 1);
+                mbar_init(smem_u32(&sh.empty[i]), C::kReleases);
                 mbar_init(smem_u32(&sh.dirty[i]), 1);
                 mbar_init(smem_u32(&sh.clean[i]), 1);
             }
             for (int w = 0; w < 2; ++w) {
+                mbar_init(smem_u32(&sh.q_full[w]), 1);
                 mbar_init(smem_u32(&sh.q_empty[w]), 4);
-                mbar_init(smem_u32(&sh.raw_full[w]), 1);
-                mbar_init(smem_u32(&sh.raw_empty[w]), 4);
+                mbar_init(smem_u32(&sh.q_split[w]), 4);
+                mbar_init(smem_u32(&sh.decoded[w]), 4);
+                mbar_init(smem_u32(&sh.decoded_empty[w]), 1);
                 mbar_init(smem_u32(&sh.s_full[w]), 1);
                 mbar_init(smem_u32(&sh.p_full[w][0]), 4);
                 mbar_init(smem_u32(&sh.p_full[w][1]), 4);
@@ -263,12 +393,13 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
     __syncthreads();
     fence_after();
     const uint32_t tmem = sh.tmem;
-    const uint32_t q_smem = smem_u32(smem), ring = q_smem + SUBS * C::kQBytes, raw = ring + C::kStages * C::kTileBytes;
+    const uint32_t q_smem = smem_u32(smem), ring = q_smem + SUBS * C::kQBytes, decoded = ring + C::kStages * C::kTileBytes;
     const uint32_t o_column = SUBS == 2 ? 256 : 128;
-    // Registers: 384 x 168 = 64512 = 256 x 224 + 128 x 56; 512 x 128 = 65536 = 256 x 200 + 256 x 56;
-    // 256 x 128 = 32768 = 128 x 184 + 128 x 72; 384 x 80 = 30720 = 128 x 128 + 256 x 56
+    // Registers of the warpgroups, which together have what the block was launched with.  16 bits: 384 x 168 = 256 x 224 + 128 x 56,
+    // 256 x 128 = 128 x 184 + 128 x 72; 8 bits: 512 x 128 = 256 x 200 + 128 x 72 + 128 x 40, 384 x 80 = 128 x (128 + 72 + 40)
     if (warp < C::kSoftmaxWarps) more_registers<SUBS == 2 ? (FP8 ? 200 : 224) : FP8 ? 128 : 184>();
-    else fewer_registers<SUBS == 1 && !FP8 ? 72 : 56>();
+    else if (warp >= kDecode) fewer_registers<40>();
+    else fewer_registers<SUBS == 2 && !FP8 ? 56 : 72>();
     if (warp < C::kSoftmaxWarps) {
         // ------------------------------------------------------------------ softmax
         const int w = warp >> 2, row = (warp & 3) * 32 + lane;
@@ -276,7 +407,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
         const uint32_t O = tmem + lanes + o_column + w * D;
         const int in_tile = row / a.group, member = row - in_tile * a.group;
         const int tokens = kRows / a.group;
-        int total = 0;  // tiles of this sub-tile so far
+        int total = 0, seg = 0;  // tiles of this sub-tile and segments so far
         bool ok = true;
         // SUBS 1: the score product of tile n goes out before the value product of tile n - 1, so that two of the latter may be
         // outstanding: they take turns at two barriers, or a wait could take the end of the one before for its own
@@ -315,30 +446,73 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
             // window older
             const int w1 = g.len > a.sink ? a.sink + (g.len - 1 - a.sink) % a.window + 1 : g.len;
             const float k_scale = FP8 ? a.k_scale[g.head] : 1.f, v_scale = FP8 ? a.v_scale[g.head] : 1.f;
-            float scale = a.scale * (FP8 && g.t0 < g.u.cached ? k_scale : 1.f);
+            const bool busy = __any_sync(0xffffffffu, mine);  // (a warp none of whose rows is a query only keeps step)
+            float scale = a.scale;
             Cap cap(CAP ? a.softcap : 1.f, scale);
             float m = -INFINITY, l = 0.f;
             for (int t = g.t0; t < g.t1; ++t) {
                 const int place = SUBS == 2 ? w : total & 1;
                 const uint32_t S = tmem + lanes + place * KEYS;
+                const bool cached = t >= g.fresh;
+                float corr = 1.f;  // of O
+                if (FP8 && cached && t == max(g.t0, g.fresh)) {  // from the chunk's rows to the cache's codes
+                    // (the score products of the rows have ended: this warp has seen the last one's result)
+                    ok = wait(smem_u32(&sh.q_full[w]), seg & 1, abort_flag, a.status, kChunkWaitQueries);
+                    if (!ok) break;
+                    if (busy) scale = a.scale * k_scale * split_row(smem + w * C::kQBytes, row);
+                    if (CAP) cap = Cap(a.softcap, scale);
+                    if (t > g.t0) corr = 1.f / v_scale;
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&sh.q_split[w]));
+                }
                 ok = wait(smem_u32(&sh.s_full[place]), (SUBS == 2 ? total : total >> 1) & 1, abort_flag, a.status, kChunkWaitProduct);
                 if (!ok) break;
-                fence_after();
-                float s[KEYS];
-#pragma unroll
-                for (int c = 0; c < KEYS; c += 32) tmem_ld32(S + c, s + c);
-                wait_ld();
-#pragma unroll
-                for (int c = 0; c < KEYS; ++c) asm volatile("" : "+f"(s[c]));  // nothing of the above is used before the wait
-                const bool cached = t < g.u.cached;
-                float corr = 1.f;  // of O
-                if (FP8 && t == g.u.cached && t > g.t0) {  // from the cache's codes to the chunk's rows
-                    corr = v_scale;
-                    scale = a.scale;
-                    if (CAP) cap = Cap(a.softcap, scale);
+                ++total;
+                if (!busy) {
+                    __syncwarp();
+                    if (lane < kHalves) mbar_arrive(smem_u32(&sh.p_full[place][lane]));
+                    continue;
                 }
-                const int start = cached ? t * KEYS : W::chunk_tile(g.u, t);
-                if (CAP) cap.apply(s, mine);
+                fence_after();
+                // what this row sees of the tile: up to three ranges of columns, [lo1, hi1), [lo2, hi2), [0, hi3)
+                const int start = cached ? (t - g.fresh) * KEYS : W::chunk_tile(g.u, t);
+                bool plain;
+                int lo1 = 0, hi1, lo2 = 0, hi2 = 0, hi3 = 0;
+                if (cached) {
+                    if (g.full) {
+                        hi1 = g.len - start;
+                        plain = hi1 >= KEYS;
+                    } else {
+                        hi3 = min(a.sink, g.u.rows) - start;
+                        lo1 = max(a.sink, w1 + i + 1 - a.window) - start;
+                        hi1 = w1 - start;
+                        lo2 = w1 + i + 1 - start;
+                        hi2 = g.u.rows - start;
+                        plain = false;
+                    }
+                } else {
+                    hi1 = i + 1 - start;
+                    plain = start + KEYS <= from + 1;
+                    if (!g.full) {
+                        lo1 = i - a.window + 1 - start;
+                        hi3 = min(a.sink - g.len, i + 1) - start;
+                        plain = plain && (start > upto - a.window || start + KEYS <= a.sink - g.len);
+                    }
+                }
+                uint32_t see[KEYS / 32];
+#pragma unroll
+                for (int x = 0; x < KEYS; x += 32)
+                    see[x / 32] = mine ? range_bits(lo1 - x, hi1 - x) | range_bits(lo2 - x, hi2 - x) | range_bits(0, hi3 - x) : 0u;
+                float s[KEYS];
+                read_columns(S, s);
+                if (CAP) {
+                    if (!plain) {  // (what lies in rows without a token has no say in how a warp computes the cap)
+#pragma unroll
+                        for (int c = 0; c < KEYS; ++c) s[c] = see[c / 32] >> (c & 31) & 1 ? s[c] : 0.f;
+                    }
+                    cap.apply(s, mine);
+                }
                 if (BIAS) {
                     // from the distance itself, a whole number and exact: a sum of terms would round at their size and lose the
                     // scores next to the query where slopes are steep
@@ -366,37 +540,9 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                         }
                     }
                 }
-                // what this row sees of the tile: up to three ranges of columns
-                bool plain;
-                int lo1 = 0, hi1, lo2 = 0, hi2 = 0, hi3 = 0;  // [lo1, hi1), [lo2, hi2), [0, hi3)
-                if (cached) {
-                    if (g.full) {
-                        hi1 = g.len - start;
-                        plain = hi1 >= KEYS;
-                    } else {
-                        hi3 = min(a.sink, g.u.rows) - start;
-                        lo1 = max(a.sink, w1 + i + 1 - a.window) - start;
-                        hi1 = w1 - start;
-                        lo2 = w1 + i + 1 - start;
-                        hi2 = g.u.rows - start;
-                        plain = false;
-                    }
-                } else {
-                    hi1 = i + 1 - start;
-                    plain = start + KEYS <= from + 1;
-                    if (!g.full) {
-                        lo1 = i - a.window + 1 - start;
-                        hi3 = min(a.sink - g.len, i + 1) - start;
-                        plain = plain && (start > upto - a.window || start + KEYS <= a.sink - g.len);
-                    }
-                }
                 if (!plain) {
 #pragma unroll
-                    for (int x = 0; x < KEYS; x += 32) {
-                        const uint32_t see = mine ? range_bits(lo1 - x, hi1 - x) | range_bits(lo2 - x, hi2 - x) | range_bits(0, hi3 - x) : 0u;
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) s[x + c] = see >> c & 1 ? s[x + c] : -INFINITY;
-                    }
+                    for (int c = 0; c < KEYS; ++c) s[c] = see[c / 32] >> (c & 31) & 1 ? s[c] : -INFINITY;
                 }
                 const float factor = CAP || BIAS ? 1.f : scale * kLog2e;
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -410,13 +556,13 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                     corr *= x;
                 }
                 if (t > g.t0 && __any_sync(0xffffffffu, corr != 1.f)) {
-                    ok = product_done(total - 1);
+                    ok = product_done(total - 2);
                     if (!ok) break;
                     fence_after();
 #pragma unroll
                     for (int c = 0; c < D; c += 32) {
                         float o[32];
-                        tmem_read32(O + c, o);
+                        read_columns(O + c, o);
 #pragma unroll
                         for (int x = 0; x < 32; ++x) o[x] *= corr;
                         tmem_st32(O + c, o);
@@ -426,15 +572,18 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                 exponentials(s, factor, base, sum, S, sh.p_full[place], lane);
                 l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-                ++total;
             }
             if (!ok) break;
-            ok = product_done(total - 1);
-            if (!ok) break;
-            fence_after();
-            const float unit = FP8 && g.t1 <= g.u.cached ? v_scale : 1.f;
+            ++seg;
+            if (busy) {
+                ok = product_done(total - 1);
+                if (!ok) break;
+                fence_after();
+            }
+            const float unit = FP8 && g.t1 > g.fresh ? v_scale : 1.f;
             const long long at_head = ((long long)(g.start + i) * a.q_heads + head);
-            if (g.record < 0) {
+            if (!busy) {
+            } else if (g.record < 0) {
                 const float inv = l > 0.f ? unit / l : 0.f;
                 if (mine && a.lse) a.lse[at_head] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
                 // through shared memory (the sub-tile's queries are not needed any more), so that whole rows go out
@@ -443,7 +592,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
                     float o[32];
-                    tmem_read32(O + c, o);
+                    read_columns(O + c, o);
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
                         *reinterpret_cast<uint4*>(stage + lane * D * 2 + (((c / 8 + x) ^ (lane & 7)) << 4)) =
@@ -465,7 +614,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
                     float o[32];
-                    tmem_read32(O + c, o);
+                    read_columns(O + c, o);
                     if (mine)
 #pragma unroll
                         for (int x = 0; x < 8; ++x)
@@ -484,9 +633,8 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
         // ------------------------------------------------------------------ tile loads
         W walk(a);
         Segment g;
-        int issued = 0, pages = 0, segs[2] = {0, 0};  // stages and raw pages so far; segments of each sub-tile
-        uint32_t copied = 0;  // stages whose last fill was a copy of this warp's
-        bool ok = true, q_out = false;
+        int issued = 0, segs[2] = {0, 0}, loaded[2] = {0, 0};  // stages so far; segments of each sub-tile, those whose queries are on the way
+        bool ok = true;
         while (ok && walk.next(g)) {
             const int row0 = g.start + g.u.tok0;
             bool q_waits = true;
@@ -496,68 +644,73 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                     ++segs[w];
                 }
                 if (!ok) return;
-                if (lane == 0) {
-                    mbar_expect_tx(smem_u32(&sh.q_full), g.subs * (D / 64) * walk.tokens * a.group * 128);
-                    for (int w = 0; w < g.subs; ++w)
+                if (lane == 0)
+                    for (int w = 0; w < g.subs; ++w) {
+                        mbar_expect_tx(smem_u32(&sh.q_full[w]), (D / 64) * walk.tokens * a.group * 128);
                         for (int b = 0; b < D / 64; ++b)
                             load_box(q_smem + w * C::kQBytes + b * kQBlock, &maps.q, b * 64, g.head * a.group, row0 + w * walk.tokens,
-                                     smem_u32(&sh.q_full));
-                }
+                                     smem_u32(&sh.q_full[w]));
+                    }
                 q_waits = false;
-                q_out = true;
+                for (int w = 0; w < g.subs; ++w) ++loaded[w];
             };
             auto free_queries = [&]() {
                 bool yes = true;
                 for (int w = 0; w < g.subs; ++w) yes = yes && mbar_test(smem_u32(&sh.q_empty[w]), (segs[w] & 1) ^ 1);
                 return __all_sync(0xffffffffu, yes);
             };
-            // waits for a stage (or raw page) to be free; K and V tiles of a segment come in ahead of its queries while those
-            // of the segment before are still in use, but never wait for a stage that only their product would free
-            auto free_stage = [&](uint64_t* bar, uint32_t parity) {
-                if (q_waits && (free_queries() || !__all_sync(0xffffffffu, mbar_test(smem_u32(bar), parity)))) queries();
-                ok = ok && wait_warp(smem_u32(bar), parity, abort_flag, a.status, kChunkWaitStage);
+            // waits for a stage to be free; K and V tiles of a segment come in ahead of its queries while those of the segment
+            // before are still in use, but never wait for a stage that only their product would free
+            auto free_stage = [&](int slot) {
+                const uint32_t bar = smem_u32(&sh.empty[slot]), parity = (issued / C::kStages & 1) ^ 1;
+                if (q_waits && (free_queries() || !__all_sync(0xffffffffu, mbar_test(bar, parity)))) queries();
+                ok = ok && wait_warp(bar, parity, abort_flag, a.status, kChunkWaitStage);
                 return ok;
             };
             const int* table = a.page_table + (long long)g.slot * a.table_stride;
             const int n_pages = (g.u.rows + kTile - 1) / kTile;
-            int batch = g.t0 * C::kPages, entry = 0;  // page-table entries batch .. batch+31, one per lane
+            int batch = max(g.t0 - g.fresh, 0) * C::kPages, entry = 0;  // page-table entries batch .. batch+31, one per lane
             auto fetch = [&](int first) {
                 batch = first;
                 entry = g.full && first + lane < n_pages ? min(max(table[first + lane], 0), a.n_pages - 1) : 0;
             };
-            if (g.t0 < g.u.cached) fetch(batch);
+            if (g.t1 > g.fresh) fetch(batch);
             for (int t = g.t0; ok && t < g.t1; ++t) {
-                if (t < g.u.cached) {
-                    const int page = t * C::kPages;
-                    if (page >= batch + 32) fetch(page);
-                    const int have = min(C::kPages, n_pages - page);  // pages of this tile
-                    if constexpr (FP8) {
-                        for (int p = 0; p < have; ++p) {
-                            const int phys = __shfl_sync(0xffffffffu, entry, (page + p - batch) & 31);
-                            const long long index = g.full ? a.page0_8 + (long long)g.index * a.n_pages + phys
-                                                           : a.ring0_8 + ((long long)g.slot * a.n_comp + g.index) * a.ring_tiles + page + p;
-                            const int rs = pages & 1;
-                            if (!free_stage(&sh.raw_empty[rs], (pages >> 1 & 1) ^ 1)) break;
-                            if (lane == 0) {
-                                mbar_expect_tx(smem_u32(&sh.raw_full[rs]), kPageBytes);
-                                load_bytes(raw + rs * kPageBytes, a.pool8 + index * kPageBytes, kPageBytes, smem_u32(&sh.raw_full[rs]));
-                            }
-                            ++pages;
-                        }
-                        copied &= ~(1u << issued % C::kStages | 1u << (issued + 1) % C::kStages);
-                        issued += 2;
-                    } else {
-                    int phys[C::kPages];
-#pragma unroll
-                    for (int p = 0; p < C::kPages; ++p) phys[p] = __shfl_sync(0xffffffffu, entry, (page + p - batch) & 31);
+                if (t < g.fresh) {
+                    const int token = g.start + W::chunk_tile(g.u, t);
                     for (int kv = 0; kv < 2; ++kv) {
                         const int slot = issued % C::kStages;
-                        if (!free_stage(&sh.empty[slot], (issued / C::kStages & 1) ^ 1)) break;
+                        if (!free_stage(slot)) break;
                         if (lane == 0) {
-                            mbar_expect_tx(smem_u32(&sh.full[slot]), have * kTile * D * 2);
+                            mbar_expect_tx(smem_u32(&sh.full[slot]), C::kTileBytes);
+                            for (int b = 0; b < D / 64; ++b)
+                                load_box(ring + slot * C::kTileBytes + b * C::kBlock, kv ? &maps.v : &maps.k, b * 64, g.head, token,
+                                         smem_u32(&sh.full[slot]));
+                            if (kv && W::template unclean<FP8>(g, t)) mbar_arrive(smem_u32(&sh.dirty[slot]));
+                        }
+                        ++issued;
+                    }
+                    continue;
+                }
+                const int page = (t - g.fresh) * C::kPages;
+                if (page >= batch + 32) fetch(page);
+                const int have = min(C::kPages, n_pages - page);  // pages of this tile
+                int phys[C::kPages];
 #pragma unroll
-                            for (int p = 0; p < C::kPages; ++p) {
-                                if (p >= have) break;
+                for (int p = 0; p < C::kPages; ++p) phys[p] = __shfl_sync(0xffffffffu, entry, (page + p - batch) & 31);
+                for (int kv = 0; kv < (FP8 ? 1 : 2); ++kv) {
+                    const int slot = issued % C::kStages;
+                    if (!free_stage(slot)) break;
+                    if (lane == 0) {
+                        mbar_expect_tx(smem_u32(&sh.full[slot]), have * (FP8 ? kPageBytes : kTile * D * 2));
+#pragma unroll
+                        for (int p = 0; p < C::kPages; ++p) {
+                            if (p >= have) break;
+                            if constexpr (FP8) {
+                                const long long index = g.full ? a.page0_8 + (long long)g.index * a.n_pages + phys[p]
+                                                               : a.ring0_8 + ((long long)g.slot * a.n_comp + g.index) * a.ring_tiles + page + p;
+                                load_page(ring + slot * C::kTileBytes + p * kPageBytes, &maps.pool, (int)(index * 128), smem_u32(&sh.full[slot]));
+                            } else {
                                 const long long r = g.full ? a.full_row0 + (((long long)g.index * a.n_pages + phys[p]) * 2 + kv) * kTile
                                                            : a.comp_row0 + (((long long)g.slot * a.n_comp + g.index) * 2 + kv) * a.rows_comp +
                                                                  (page + p) * kTile;
@@ -565,62 +718,47 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                                     load_box(ring + slot * C::kTileBytes + b * C::kBlock + p * kTile * 128, &maps.pool, b * 64, 0, (int)r,
                                              smem_u32(&sh.full[slot]));
                             }
-                            if (W::template unclean<FP8, CAP>(g, t, kv)) mbar_arrive(smem_u32(&sh.dirty[slot]));
                         }
-                        copied |= 1u << slot;
-                        ++issued;
+                        if (kv && W::template unclean<FP8>(g, t)) mbar_arrive(smem_u32(&sh.dirty[slot]));
                     }
-                    }
-                } else {
-                    // (a stage's earlier contents may be the decoding warps': those have all been written once the last raw
-                    // page has been read, so that the wait below cannot take an earlier use of the stage for its last)
-                    if (FP8 && pages > 0) {
-                        if (q_waits) queries();
-                        ok = ok && wait_warp(smem_u32(&sh.raw_empty[(pages - 1) & 1]), (pages - 1) >> 1 & 1, abort_flag, a.status, kChunkWaitRaw);
-                    }
-                    const int token = g.start + W::chunk_tile(g.u, t);
-                    for (int kv = 0; ok && kv < 2; ++kv) {
-                        const int slot = issued % C::kStages;
-                        if (!free_stage(&sh.empty[slot], (issued / C::kStages & 1) ^ 1)) break;
-                        if (lane == 0) {
-                            mbar_expect_tx(smem_u32(&sh.full[slot]), C::kTileBytes);
-                            for (int x = 1; x < C::kFills; ++x) mbar_arrive(smem_u32(&sh.full[slot]));
-                            for (int b = 0; b < D / 64; ++b)
-                                load_box(ring + slot * C::kTileBytes + b * C::kBlock, kv ? &maps.v : &maps.k, b * 64, g.head, token,
-                                         smem_u32(&sh.full[slot]));
-                            if (W::template unclean<FP8, CAP>(g, t, kv)) mbar_arrive(smem_u32(&sh.dirty[slot]));
-                        }
-                        copied |= 1u << slot;
-                        ++issued;
-                    }
+                    ++issued;
                 }
             }
             if (ok && q_waits) queries();
         }
         if (!ok || *abort_flag) {  // nothing of this CTA's copies may be in flight when it ends
-            if (q_out) wait_warp(smem_u32(&sh.q_full), (max(segs[0], 1) - 1) & 1, nullptr, a.status, kChunkWaitDrain);
+            for (int w = 0; w < SUBS; ++w)
+                if (loaded[w] > 0) wait_warp(smem_u32(&sh.q_full[w]), (loaded[w] - 1) & 1, nullptr, a.status, kChunkWaitDrain);
             for (int i = max(0, issued - C::kStages); i < issued; ++i)
-                if (copied >> i % C::kStages & 1) wait_warp(smem_u32(&sh.full[i % C::kStages]), i / C::kStages & 1, nullptr, a.status, kChunkWaitDrain);
-            for (int i = max(0, pages - 2); i < pages; ++i)
-                wait_warp(smem_u32(&sh.raw_full[i & 1]), i >> 1 & 1, nullptr, a.status, kChunkWaitDrain);
+                wait_warp(smem_u32(&sh.full[i % C::kStages]), i / C::kStages & 1, nullptr, a.status, kChunkWaitDrain);
         }
     } else if (warp == kMma) {
         // ------------------------------------------------------------------ matrix products
         W walk(a);
         Segment g;
         constexpr uint32_t kQK = instr_desc(kRows, KEYS, false), kPV = instr_desc(kRows, D, true), kPVt = instr_desc(kRows, D, false);
-        int used[2] = {0, 0};    // P tiles multiplied so far (SUBS 1: used[0])
-        int base = 0, seg = 0;   // stages and segments so far
-        uint32_t cleaned = 0;    // phase of each stage's `clean`
+        constexpr uint32_t kQK8 = instr_desc8(kRows, kTile);
+        int used[2] = {0, 0};               // P tiles multiplied so far (SUBS 1: used[0])
+        int base = 0, dbase = 0;            // stages and decoded tiles so far
+        int segs[2] = {0, 0}, split[2] = {0, 0};  // segments of each sub-tile, those whose queries were split
+        uint32_t cleaned = 0;               // phase of each stage's `clean`
         bool ok = true;
         while (ok && walk.next(g)) {
-            const int n = g.t1 - g.t0;
-            auto stage = [&](int i) { return ring + (base + i) % C::kStages * C::kTileBytes; };
-            // K (even) and V tiles in turn
-            auto loaded = [&](int i) {
-                const int slot = (base + i) % C::kStages, t = g.t0 + (i >> 1);
-                if (!wait_warp(smem_u32(&sh.full[slot]), (base + i) / C::kStages & 1, abort_flag, a.status, kChunkWaitLoad)) return false;
-                if (W::template unclean<FP8, CAP>(g, t, i & 1)) {
+            const int n = g.t1 - g.t0, c = FP8 ? max(0, min(g.t1, g.fresh) - g.t0) : n;  // tiles, and those that take two stages
+            // the stage of tile j's K rows (of an 8-bit cache, of its codes) and, of the chunk or a 16-bit cache, of its V rows
+            auto k_stage = [&](int j) { return base + (j < c ? 2 * j : c + j); };
+            auto k_loaded = [&](int j) {
+                const int i = k_stage(j);
+                return wait_warp(smem_u32(&sh.full[i % C::kStages]), i / C::kStages & 1, abort_flag, a.status, kChunkWaitLoad);
+            };
+            auto v_loaded = [&](int j) {
+                if (FP8 && j >= c) {
+                    const int i = dbase + j - c;
+                    return wait_warp(smem_u32(&sh.decoded[i & 1]), i >> 1 & 1, abort_flag, a.status, kChunkWaitDecoded);
+                }
+                const int i = k_stage(j) + 1, slot = i % C::kStages;
+                if (!wait_warp(smem_u32(&sh.full[slot]), i / C::kStages & 1, abort_flag, a.status, kChunkWaitLoad)) return false;
+                if (W::template unclean<FP8>(g, g.t0 + j)) {
                     if (!wait_warp(smem_u32(&sh.clean[slot]), cleaned >> slot & 1, abort_flag, a.status, kChunkWaitLoad)) return false;
                     cleaned ^= 1u << slot;
                 }
@@ -629,60 +767,79 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
             auto signal = [&](uint64_t* bar) {
                 if (elect_one()) commit(smem_u32(bar));
             };
+            auto k_done = [&](int j) { signal(&sh.empty[k_stage(j) % C::kStages]); };
+            auto v_done = [&](int j) { signal(FP8 && j >= c ? &sh.decoded_empty[(dbase + j - c) & 1] : &sh.empty[(k_stage(j) + 1) % C::kStages]); };
+            // S of tile j; the first cached tile of an 8-bit cache waits for the queries' split
             auto scores = [&](int w, int place, int j) {
-                const uint64_t q = smem_desc(q_smem + w * C::kQBytes), k = smem_desc(stage(2 * j));
+                if (FP8 && j == c) {
+                    if (!wait_warp(smem_u32(&sh.q_split[w]), split[w] & 1, abort_flag, a.status, kChunkWaitQueries)) return false;
+                    ++split[w];
+                }
+                const uint32_t to = tmem + place * KEYS, at = ring + k_stage(j) % C::kStages * C::kTileBytes;
+                const uint64_t q = smem_desc(q_smem + w * C::kQBytes), k = smem_desc(at);
                 fence_after();
-                if (elect_one()) {
+                if (FP8 && j >= c) {
+                    if (elect_one()) {
+#pragma unroll
+                        for (int p = 0; p < C::kPages; ++p)
+#pragma unroll
+                            for (int x = 0; x < 8; ++x)  // the queries' first and second parts
+                                mma_ss8(to + p * kTile, q + ((x / 4 * kQBlock + x % 4 * 32) >> 4), k + ((p * kPageBytes + x % 4 * 32) >> 4), kQK8, x > 0);
+                        commit(smem_u32(&sh.s_full[place]));
+                    }
+                } else if (elect_one()) {
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x)
-                        mma_ss(tmem + place * KEYS, q + ((x / 4 * kQBlock + x % 4 * 32) >> 4), k + ((x / 4 * C::kBlock + x % 4 * 32) >> 4), kQK, x > 0);
+                        mma_ss(to, q + ((x / 4 * kQBlock + x % 4 * 32) >> 4), k + ((x / 4 * C::kBlock + x % 4 * 32) >> 4), kQK, x > 0);
                     commit(smem_u32(&sh.s_full[place]));
                 }
+                return true;
             };
             // the products of one half (64 keys) of tile j's P
             auto values = [&](int w, int place, int j, int half) {
                 fence_after();
                 const uint32_t d = tmem + o_column + w * D, p = tmem + place * KEYS + half * 32;
-                if (FP8 && g.t0 + j < g.u.cached) {  // V^T: rows of 64 tokens
-                    const uint64_t v = smem_desc(stage(2 * j + 1) + half * (D * 128));
+                if (FP8 && j >= c) {  // V^T: rows of 64 tokens
+                    const uint64_t v = smem_desc(decoded + ((dbase + j - c) & 1) * C::kTileBytes + half * (D * 128));
                     if (elect_one()) {
 #pragma unroll
                         for (int x = 0; x < 4; ++x) mma_ts(d, p + x * 8, v + (x * 32 >> 4), kPVt, j > 0 || half > 0 || x > 0);
                     }
                 } else {
-                    const uint64_t v = smem_desc(stage(2 * j + 1) + half * (64 * 128), C::kBlock);
+                    const uint64_t v = smem_desc(ring + (k_stage(j) + 1) % C::kStages * C::kTileBytes + half * (64 * 128), C::kBlock);
                     if (elect_one()) {
 #pragma unroll
                         for (int x = 0; x < 4; ++x) mma_ts(d, p + x * 8, v + (x * 2048 >> 4), kPV, j > 0 || half > 0 || x > 0);
                     }
                 }
             };
-            ok = wait_warp(smem_u32(&sh.q_full), seg & 1, abort_flag, a.status, kChunkWaitQueries) && loaded(0);
+            for (int w = 0; ok && w < g.subs; ++w)
+                ok = wait_warp(smem_u32(&sh.q_full[w]), segs[w]++ & 1, abort_flag, a.status, kChunkWaitQueries);
+            ok = ok && k_loaded(0);
             if (!ok) break;
             if (SUBS == 1) {
-                scores(0, used[0] & 1, 0);
-                signal(&sh.empty[base % C::kStages]);
+                ok = scores(0, used[0] & 1, 0);
+                if (ok) k_done(0);
                 for (int j = 0; ok && j < n; ++j) {
                     const int place = used[0] & 1;
                     if (j + 1 < n) {
-                        ok = loaded(2 * j + 2);
+                        ok = k_loaded(j + 1) && scores(0, place ^ 1, j + 1);
                         if (!ok) break;
-                        scores(0, place ^ 1, j + 1);
-                        signal(&sh.empty[(base + 2 * j + 2) % C::kStages]);
+                        k_done(j + 1);
                     }
-                    ok = wait_warp(smem_u32(&sh.p_full[place][0]), used[0] >> 1 & 1, abort_flag, a.status, kChunkWaitSoftmax) && loaded(2 * j + 1);
+                    ok = wait_warp(smem_u32(&sh.p_full[place][0]), used[0] >> 1 & 1, abort_flag, a.status, kChunkWaitSoftmax) && v_loaded(j);
                     if (!ok) break;
                     values(0, place, j, 0);
                     signal(&sh.pv_done[place]);
-                    signal(&sh.empty[(base + 2 * j + 1) % C::kStages]);
+                    v_done(j);
                     ++used[0];
                 }
             } else {
-                for (int w = 0; w < g.subs; ++w) scores(w, w, 0);
-                signal(&sh.empty[base % C::kStages]);
+                for (int w = 0; ok && w < g.subs; ++w) ok = scores(w, w, 0);
+                if (ok) k_done(0);
                 for (int j = 0; ok && j < n; ++j) {
-                    ok = loaded(2 * j + 1);
-                    if (ok && j + 1 < n) ok = loaded(2 * j + 2);
+                    ok = v_loaded(j);
+                    if (ok && j + 1 < n) ok = k_loaded(j + 1);
 #pragma unroll
                     for (int w = 0; w < SUBS; ++w) {
                         if (!ok) break;
@@ -696,14 +853,14 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                             signal(&sh.pv_done[w]);
                             ++used[w];
                         }
-                        if (w == SUBS - 1) signal(&sh.empty[(base + 2 * j + 1) % C::kStages]);
-                        if (j + 1 < n && w < g.subs) scores(w, w, j + 1);
+                        if (w == SUBS - 1) v_done(j);
+                        if (j + 1 < n && w < g.subs) ok = scores(w, w, j + 1);
                     }
-                    if (ok && j + 1 < n) signal(&sh.empty[(base + 2 * j + 2) % C::kStages]);
+                    if (ok && j + 1 < n) k_done(j + 1);
                 }
             }
-            base += 2 * n;
-            ++seg;
+            base += c + n;
+            dbase += n - c;
         }
         // every product is done before tensor memory is given back
         if (elect_one()) commit(smem_u32(&sh.drain));
@@ -717,85 +874,68 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
         uint32_t told = 0;  // phase of each stage's `dirty`
         bool ok = true;
         while (ok && walk.next(g)) {
-            for (int t = g.t0; ok && t < g.t1; ++t)
-                for (int v = 0; ok && v < 2; ++v) {
-                    if (!W::template unclean<FP8, CAP>(g, t, v)) continue;
-                    const int i = base + 2 * (t - g.t0) + v, slot = i % C::kStages;
-                    ok = wait_warp(smem_u32(&sh.dirty[slot]), told >> slot & 1, abort_flag, a.status, kChunkWaitLoad) &&
-                         wait_warp(smem_u32(&sh.full[slot]), i / C::kStages & 1, abort_flag, a.status, kChunkWaitLoad);
-                    if (!ok) break;
-                    told ^= 1u << slot;
-                    uint8_t* x = smem + SUBS * C::kQBytes + slot * C::kTileBytes;
-                    for (int y = W::valid_rows(g, t) * 8 + lane; y < KEYS * 8; y += 32)
-                        for (int b = 0; b < D / 64; ++b) *reinterpret_cast<uint4*>(x + b * C::kBlock + y * 16) = make_uint4(0, 0, 0, 0);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&sh.clean[slot]));
-                }
-            base += 2 * (g.t1 - g.t0);
+            const int n = g.t1 - g.t0, c = FP8 ? max(0, min(g.t1, g.fresh) - g.t0) : n;
+            for (int j = 0; ok && j < c; ++j) {
+                if (!W::template unclean<FP8>(g, g.t0 + j)) continue;
+                const int i = base + 2 * j + 1, slot = i % C::kStages;
+                ok = wait_warp(smem_u32(&sh.dirty[slot]), told >> slot & 1, abort_flag, a.status, kChunkWaitLoad) &&
+                     wait_warp(smem_u32(&sh.full[slot]), i / C::kStages & 1, abort_flag, a.status, kChunkWaitLoad);
+                if (!ok) break;
+                told ^= 1u << slot;
+                uint8_t* x = smem + SUBS * C::kQBytes + slot * C::kTileBytes;
+                for (int y = W::valid_rows(g, g.t0 + j) * 8 + lane; y < KEYS * 8; y += 32)
+                    for (int b = 0; b < D / 64; ++b) *reinterpret_cast<uint4*>(x + b * C::kBlock + y * 16) = make_uint4(0, 0, 0, 0);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.clean[slot]));
+            }
+            base += c + n;
         }
     } else if (FP8 && warp >= kDecode) {
-        // ------------------------------------------------------------------ codes to bf16 operands
+        // ------------------------------------------------------------------ V codes to bf16
         W walk(a);
         Segment g;
         const int ct = (warp - kDecode) * 32 + lane;
-        int base = 0, pages = 0;
+        int i = 0, d = 0;  // stages and decoded tiles so far
         bool ok = true;
         while (ok && walk.next(g)) {
             const int n_pages = (g.u.rows + kTile - 1) / kTile;
-            for (int t = g.t0; ok && t < min(g.t1, g.u.cached); ++t) {
-                const int i = base + 2 * (t - g.t0);
-                const int ks = i % C::kStages, vs = (i + 1) % C::kStages;
-                // the raw page first: by then the copies before it have been issued, so that the stages' last uses are known
-                ok = wait_warp(smem_u32(&sh.raw_full[pages & 1]), pages >> 1 & 1, abort_flag, a.status, kChunkWaitRaw) &&
-                     wait_warp(smem_u32(&sh.empty[ks]), (i / C::kStages & 1) ^ 1, abort_flag, a.status, kChunkWaitStage) &&
-                     wait_warp(smem_u32(&sh.empty[vs]), ((i + 1) / C::kStages & 1) ^ 1, abort_flag, a.status, kChunkWaitStage);
+            for (int t = g.t0; ok && t < g.t1; ++t) {
+                if (t < g.fresh) {  // rows of the chunk: nothing to decode (a stage is free when these warps have let it go, too)
+                    for (int kv = 0; ok && kv < 2; ++kv, ++i) {
+                        ok = wait_warp(smem_u32(&sh.full[i % C::kStages]), i / C::kStages & 1, abort_flag, a.status, kChunkWaitLoad);
+                        if (ok && lane == 0) mbar_arrive(smem_u32(&sh.empty[i % C::kStages]));
+                    }
+                    continue;
+                }
+                const int slot = i % C::kStages;
+                ok = wait_warp(smem_u32(&sh.full[slot]), i / C::kStages & 1, abort_flag, a.status, kChunkWaitLoad) &&
+                     wait_warp(smem_u32(&sh.decoded_empty[d & 1]), (d >> 1 & 1) ^ 1, abort_flag, a.status, kChunkWaitDecoded);
                 if (!ok) break;
-                uint8_t *kt = smem + SUBS * C::kQBytes + ks * C::kTileBytes, *vt = smem + SUBS * C::kQBytes + vs * C::kTileBytes;
+                const uint8_t* from = smem + SUBS * C::kQBytes + slot * C::kTileBytes + kTile * 128;
+                uint8_t* to = smem + SUBS * C::kQBytes + (C::kStages + (d & 1)) * C::kTileBytes;
 #pragma unroll 1
                 for (int p = 0; p < C::kPages; ++p) {
-                    const bool have = t * C::kPages + p < n_pages;
-                    const int rs = pages & 1;
-                    if (have) {
-                        ok = wait_warp(smem_u32(&sh.raw_full[rs]), pages >> 1 & 1, abort_flag, a.status, kChunkWaitRaw);
-                        if (!ok) break;
-                    }
-                    const uint4* src = reinterpret_cast<const uint4*>(smem + SUBS * C::kQBytes + C::kStages * C::kTileBytes + rs * kPageBytes);
-                    const int valid = g.u.rows - (t * KEYS + p * kTile);  // rows of the page that hold a token
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {  // K: 16 elements of a row
-                        const int piece = x * 128 + ct, r = piece >> 3, c = piece & 7;
+                    const bool have = (t - g.fresh) * C::kPages + p < n_pages;
+#pragma unroll 2
+                    for (int x = 0; x < 4; ++x) {  // sixteen tokens of an element; a row of 128 bytes holds two elements
+                        const int piece = x * 128 + ct, r = piece >> 3, c = piece & 7, e = r * 2 + (c >> 2), ch = (c & 3) * 2;
                         uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-                        if (r < valid) decode16(src[piece], lo, hi);
-                        const int y = p * kTile + r, ch = (c & 3) * 2, odd = c >> 2;  // (the two blocks' first stores go to different banks)
-                        uint8_t* to = kt + (c >> 2) * C::kBlock + y * 128;
-                        *reinterpret_cast<uint4*>(to + (((ch + odd) ^ (y & 7)) << 4)) = odd ? hi : lo;
-                        *reinterpret_cast<uint4*>(to + (((ch + 1 - odd) ^ (y & 7)) << 4)) = odd ? lo : hi;
-                    }
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {  // V^T: 16 tokens of an element
-                        const int piece = x * 128 + ct, d = piece >> 2, ch = (piece & 3) * 2;
-                        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-                        if (have) decode16(src[512 + piece], lo, hi);
-                        uint8_t* to = vt + p * (128 * 128) + d * 128;
-                        *reinterpret_cast<uint4*>(to + ((ch ^ (d & 7)) << 4)) = lo;
-                        *reinterpret_cast<uint4*>(to + (((ch + 1) ^ (d & 7)) << 4)) = hi;
-                    }
-                    if (have) {
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&sh.raw_empty[rs]));
-                        ++pages;
+                        if (have) decode16(*reinterpret_cast<const uint4*>(from + p * kPageBytes + r * 128 + ((c ^ (r & 7)) << 4)), lo, hi);
+                        uint8_t* row = to + p * (128 * 128) + e * 128;
+                        *reinterpret_cast<uint4*>(row + ((ch ^ (e & 7)) << 4)) = lo;
+                        *reinterpret_cast<uint4*>(row + (((ch + 1) ^ (e & 7)) << 4)) = hi;
                     }
                 }
-                if (!ok) break;
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(smem_u32(&sh.full[ks]));
-                    mbar_arrive(smem_u32(&sh.full[vs]));
+                    mbar_arrive(smem_u32(&sh.decoded[d & 1]));
+                    mbar_arrive(smem_u32(&sh.empty[slot]));
                 }
+                ++i;
+                ++d;
             }
-            base += 2 * (g.t1 - g.t0);
         }
     }
     fence_before();
@@ -807,12 +947,15 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
     }
 }
 
-// Adds up the pieces of the units that a boundary cuts.  Block (c - 1, rows, columns): the unit that CTA c's range begins
-// inside of, if it is the first to; 32 rows and 32 columns of it.  A lane holds a row's columns of every eighth piece, the
-// eight warps' sums meet in shared memory.  The pieces' order is that of the keys, whatever CTA ran first.
-template <int D, int SUBS>
+// Adds up the pieces of the units that a boundary cuts.  Block (c - 1, 32 rows, columns): the unit that CTA c's range begins
+// inside of, if it is the first to.  A warp's lanes hold 32 rows' columns, 32 of them; its warps take COLUMNS such runs of
+// columns and of each run every 8 / COLUMNS-th piece, and meet in shared memory: all columns and few pieces at a time where units
+// are cut once or twice, one run and eight pieces where few units are cut into many.  The pieces' order is that of the keys,
+// whatever CTA ran first.
+template <int D, int SUBS, int COLUMNS>
 __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constant__ ChunkArgs a)
 {
+    constexpr int kPieces = 8 / COLUMNS;
     __shared__ float part[8][32][33], top[8][32], sum[8][32];
     const int c = blockIdx.x + 1;
     const ChunkPos b = a.at[c], before = a.at[c - 1];
@@ -828,13 +971,14 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
     float o[32], mx = -INFINITY, l = 0.f;
 #pragma unroll
     for (int x = 0; x < 32; ++x) o[x] = 0.f;
-    for (int k = c - 1 + warp; k <= last; k += 8) {
-        const int slot = k > c - 1 || (same_unit(before, b)) ? 2 * k : 2 * k + 1;
+    for (int k = c - 1 + warp / COLUMNS; k <= last; k += kPieces) {
+        const int slot = k > c - 1 || same_unit(before, b) ? 2 * k : 2 * k + 1;
         const float* rec = a.records + (long long)slot * chunk_record_floats(D, SUBS) + (long long)w * kRows * (D + 2);
         const float pm = rec[D * kRows + row0 + lane], pl = rec[(D + 1) * kRows + row0 + lane];
         float4 y[8];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) y[x] = reinterpret_cast<const float4*>(rec)[(blockIdx.z * 8 + x) * kRows + row0 + lane];
+        for (int x = 0; x < 8; ++x)
+            y[x] = reinterpret_cast<const float4*>(rec)[((blockIdx.z * COLUMNS + warp % COLUMNS) * 8 + x) * kRows + row0 + lane];
         if (pm == -INFINITY) continue;  // the row sees none of the piece's keys
         const float to = fmaxf(mx, pm), old = mx == -INFINITY ? 0.f : ex2(mx - to), f = ex2(pm - to);
         mx = to;
@@ -852,39 +996,46 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
 #pragma unroll
     for (int x = 0; x < 32; ++x) part[warp][lane][x] = o[x];
     __syncthreads();
-    // eight threads a row, four columns each
+    // eight threads a row, four columns of each run
     const int r = threadIdx.x >> 3, x0 = (threadIdx.x & 7) * 4, in_tile = (row0 + r) / a.group, i = from + in_tile;
     if (in_tile >= tokens || i >= m) return;
-    float all = -INFINITY;
+    float all = -INFINITY, total = 0.f, f[kPieces];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) all = fmaxf(all, top[k][r]);
-    float total = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < kPieces; ++k) all = fmaxf(all, top[k * COLUMNS][r]);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        if (top[k][r] == -INFINITY) continue;
-        const float f = ex2(top[k][r] - all);
-        total += sum[k][r] * f;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) y[x] += part[k][r][x0 + x] * f;
+    for (int k = 0; k < kPieces; ++k) {
+        const float t = top[k * COLUMNS][r];
+        f[k] = t == -INFINITY ? 0.f : ex2(t - all);
+        total += sum[k * COLUMNS][r] * f[k];
     }
     const float inv = total > 0.f ? 1.f / total : 0.f;
     const int head = a.head_of_slot[b.head] * a.group + (row0 + r) % a.group;
     const long long at_head = (long long)(start + i) * a.q_heads + head;
-    *reinterpret_cast<uint2*>(a.out + at_head * D + blockIdx.z * 32 + x0) = make_uint2(bf16x2(y[0] * inv, y[1] * inv), bf16x2(y[2] * inv, y[3] * inv));
+#pragma unroll
+    for (int run = 0; run < COLUMNS; ++run) {
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) y[x] += part[k * COLUMNS + run][r][x0 + x] * f[k];
+        *reinterpret_cast<uint2*>(a.out + at_head * D + (blockIdx.z * COLUMNS + run) * 32 + x0) =
+            make_uint2(bf16x2(y[0] * inv, y[1] * inv), bf16x2(y[2] * inv, y[3] * inv));
+    }
     if (a.lse && blockIdx.z == 0 && x0 == 0) a.lse[at_head] = total > 0.f ? (all + log2f(total)) * kLn2 : -INFINITY;
 }
 
 template <int D, int SUBS, bool FP8>
-cudaError_t launch_shape(const ChunkArgs& a, const ChunkMaps& m, bool split, cudaStream_t stream)
+cudaError_t launch_shape(const ChunkArgs& a, const ChunkMaps& m, int pieces, cudaStream_t stream)
 {
     using C = Chunk<D, SUBS, FP8>;
     auto kernel = a.softcap != 0.f ? (a.slopes ? chunk_attention_kernel<D, SUBS, FP8, true, true> : chunk_attention_kernel<D, SUBS, FP8, true, false>)
                                    : (a.slopes ? chunk_attention_kernel<D, SUBS, FP8, false, true> : chunk_attention_kernel<D, SUBS, FP8, false, false>);
     kernel<<<a.ctas, C::kThreads, C::kSmem, stream>>>(a, m);
     cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess || !split) return e;
+    if (e != cudaSuccess || pieces < 2) return e;
+    const bool few = pieces <= 4;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.ctas - 1, SUBS * 4, D / 32);
+    cfg.gridDim = dim3(a.ctas - 1, SUBS * 4, few ? 1 : D / 32);
     cfg.blockDim = dim3(256);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -892,7 +1043,7 @@ cudaError_t launch_shape(const ChunkArgs& a, const ChunkMaps& m, bool split, cud
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, chunk_combine_kernel<D, SUBS>, a);
+    return few ? cudaLaunchKernelEx(&cfg, chunk_combine_kernel<D, SUBS, D / 32>, a) : cudaLaunchKernelEx(&cfg, chunk_combine_kernel<D, SUBS, 1>, a);
 }
 
 template <int D, int SUBS, bool FP8>
@@ -909,11 +1060,11 @@ cudaError_t prepare_shape()
 
 }  // namespace
 
-cudaError_t launch_chunk_attention(const ChunkArgs& a, const ChunkMaps& m, int head_dim, int subs, bool split, cudaStream_t stream)
+cudaError_t launch_chunk_attention(const ChunkArgs& a, const ChunkMaps& m, int head_dim, int subs, int pieces, cudaStream_t stream)
 {
-    if (a.pool8) return subs == 2 ? launch_shape<128, 2, true>(a, m, split, stream) : launch_shape<128, 1, true>(a, m, split, stream);
-    if (head_dim == 128) return subs == 2 ? launch_shape<128, 2, false>(a, m, split, stream) : launch_shape<128, 1, false>(a, m, split, stream);
-    return subs == 2 ? launch_shape<64, 2, false>(a, m, split, stream) : launch_shape<64, 1, false>(a, m, split, stream);
+    if (a.pool8) return subs == 2 ? launch_shape<128, 2, true>(a, m, pieces, stream) : launch_shape<128, 1, true>(a, m, pieces, stream);
+    if (head_dim == 128) return subs == 2 ? launch_shape<128, 2, false>(a, m, pieces, stream) : launch_shape<128, 1, false>(a, m, pieces, stream);
+    return subs == 2 ? launch_shape<64, 2, false>(a, m, pieces, stream) : launch_shape<64, 1, false>(a, m, pieces, stream);
 }
 
 cudaError_t prepare_chunk_kernels(int head_dim, bool fp8)

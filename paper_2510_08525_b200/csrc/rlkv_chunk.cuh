@@ -28,13 +28,13 @@ __device__ __forceinline__ int entry_of_token(const ChunkSeqs& s, int t)
 
 // ---- attention ----------------------------------------------------------------------------------------
 // A UNIT is one KV head of one sequence and a row tile of its chunk: the queries of `tokens` consecutive tokens, all the
-// query heads of the KV head packed into one tile of rows (token-major).  Its keys come in tiles of `kt`: first the rows the
-// cache holds (pages of a full head, the ring of a compressed one), then the chunk's own tokens.
+// query heads of the KV head packed into one tile of rows (token-major).  Its keys come in tiles of `kt`: first the chunk's own
+// tokens, then the rows the cache holds (pages of a full head, the ring of a compressed one).
 struct ChunkUnit {
     int tok0;        // first token of the row tile, inside the chunk
     int rows;        // cached rows that any of its queries may see
     int cached;      // tiles of them
-    int a_end, b0;   // key tiles of the chunk: 0 .. a_end-1, then from b0 on
+    int a_end, b0;   // key tiles of the chunk: 0 .. a_end-1, then from b0 on (they come first)
     int tiles;       // in all
 };
 __host__ __device__ inline ChunkUnit chunk_unit(int len, int m, int row_tile, int tokens, int kt, bool full, int sink, int window)
@@ -102,12 +102,13 @@ inline size_t chunk_record_bytes(int head_dim) { return (size_t)2 * kMaxChunkCta
 
 // Status codes (device error word of the cache): which wait of the chunk kernel ran out.
 enum : int { kChunkWaitLoad = 201, kChunkWaitProduct = 202, kChunkWaitSoftmax = 203, kChunkWaitStage = 204, kChunkWaitDrain = 205,
-             kChunkWaitRaw = 206, kChunkWaitQueries = 207, kChunkSmemMisaligned = 208 };
+             kChunkWaitDecoded = 206, kChunkWaitQueries = 207, kChunkSmemMisaligned = 208 };
 
 struct ChunkMaps {
-    CUtensorMap q, k, v, pool;  // pool: 64 elements x 64 rows of the 16-bit pool
+    CUtensorMap q, k, v, pool;  // pool: 64 elements x 64 rows of the 16-bit pool, or whole pages of the 8-bit one
 };
-cudaError_t launch_chunk_attention(const ChunkArgs& a, const ChunkMaps& m, int head_dim, int subs, bool split, cudaStream_t stream);
+// pieces: most ranges that a unit lies in (1: none is cut)
+cudaError_t launch_chunk_attention(const ChunkArgs& a, const ChunkMaps& m, int head_dim, int subs, int pieces, cudaStream_t stream);
 cudaError_t prepare_chunk_kernels(int head_dim, bool fp8);
 
 // ---- rows in and out of the cache -----------------------------------------------------------------------

@@ -80,8 +80,8 @@ void fill_rows_args(rlkv_paged* p, int layer, ChunkRowsArgs& a)
 }
 
 // Cuts the flat sequence of the units' key tiles for at most max_ctas CTAs of at least min_tiles tiles; a unit counts `extra`
-// tiles more than it has (its queries' load and its results cost about as much).  split: whether a unit lies in two ranges.
-void plan_chunks(ChunkArgs& a, int subs, int max_ctas, int min_tiles, int extra, bool& split)
+// tiles more than it has (its queries' load and its results cost about as much).  Returns the most ranges that one unit lies in.
+int plan_chunks(ChunkArgs& a, int subs, int max_ctas, int min_tiles, int extra)
 {
     const int keys = subs == 2 ? 128 : 64, tokens = subs * (128 / a.group);
     const ChunkSeqs& s = a.seqs;
@@ -99,8 +99,7 @@ void plan_chunks(ChunkArgs& a, int subs, int max_ctas, int min_tiles, int extra,
     if (ctas > max_ctas) ctas = max_ctas;
     if (ctas < 1) ctas = 1;
     a.ctas = (int)ctas;
-    split = false;
-    int c = 0;
+    int c = 0, pieces = 1, most = 1;
     long long x = 0;  // flat tiles before the units at hand
     auto boundary = [&](int k) { return all * k / ctas; };
     for (int i = 0; i < s.n; ++i)
@@ -116,12 +115,14 @@ void plan_chunks(ChunkArgs& a, int subs, int max_ctas, int min_tiles, int extra,
                     at.head = (unsigned short)((comp ? a.n_full : 0) + (int)(y / each));
                     at.row_tile = j;
                     at.tile = (int)(y % each) - extra;
-                    if (at.tile <= 0) at.tile = 0;
-                    else split = true;
+                    if (at.tile < 0) at.tile = 0;
+                    pieces = at.tile == 0 ? 1 : c > 1 && same_unit(a.at[c - 2], at) ? pieces + 1 : 2;
+                    if (pieces > most) most = pieces;
                 }
                 x += (long long)heads * each;
             }
     for (; c <= ctas; ++c) a.at[c] = ChunkPos{(unsigned short)s.n, 0, 0, 0};
+    return most;
 }
 
 // Whether a launch takes two sub-tiles of 128 rows on one CTA of an SM (one-tile CTAs, two on an SM, otherwise): where most key
@@ -242,18 +243,17 @@ int rlkv_paged_chunk_attention(rlkv_paged* p, int layer, const int* slots, const
     const long long room = (long long)(p->chunk_bytes / (2 * sizeof(float) * chunk_record_floats(p->head_dim, subs)));  // CTAs it has records for
     int ctas = subs == 2 ? sms : 2 * sms;
     if (ctas > room) ctas = room < 1 ? 1 : (int)room;
-    bool split;
-    plan_chunks(a, subs, ctas, kMinChunkTiles, kUnitTiles, split);
+    const int pieces = plan_chunks(a, subs, ctas, kMinChunkTiles, kUnitTiles);
     const int keys = subs == 2 ? 128 : 64;
     ChunkMaps m;
     int e = encode_heads_map(&m.q, q, total, p->q_heads, p->head_dim, q_stride, a.group, 128 / a.group);
     if (!e) e = encode_heads_map(&m.k, k, total, p->kv_heads, p->head_dim, k_stride, 1, keys);
     if (!e) e = encode_heads_map(&m.v, v, total, p->kv_heads, p->head_dim, v_stride, 1, keys);
     if (!e && !p->fp8) e = encode_heads_map(&m.pool, dev_at<__nv_bfloat16>(p, p->off_pool), p->pool_rows, 1, p->head_dim, p->head_dim, 1, kTile);
-    else if (!e) m.pool = m.k;  // (not used: the 8-bit pool is copied as it lies)
+    else if (!e) m.pool = p->map_k;
     if (e) return e;
-    RLKV_CUDA(launch_chunk_attention(a, m, p->head_dim, subs, split, static_cast<cudaStream_t>(stream)));
-    p->launches += split ? 2 : 1;
+    RLKV_CUDA(launch_chunk_attention(a, m, p->head_dim, subs, pieces, static_cast<cudaStream_t>(stream)));
+    p->launches += pieces > 1 ? 2 : 1;
     return RLKV_OK;
 }
 
@@ -372,8 +372,7 @@ int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full,
     a.window = window;
     if (subs == 0) subs = choose_subs(a);
     if (subs != 1 && subs != 2) return RLKV_EINVAL;
-    bool split;
-    plan_chunks(a, subs, max_ctas, kMinChunkTiles, kUnitTiles, split);
+    plan_chunks(a, subs, max_ctas, kMinChunkTiles, kUnitTiles);
     for (int c = 0; c <= a.ctas; ++c) {
         at_out[4 * c] = a.at[c].seq;
         at_out[4 * c + 1] = a.at[c].row_tile;

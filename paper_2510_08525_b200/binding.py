@@ -805,13 +805,13 @@ def rlkv_prompt_kernel_status(prompt) -> int:
     return int(out.value)
 
 
-def rlkv_debug_chunk_plan(lens, counts, n_full, n_comp, group, sink, window, subs=0, max_ctas=296):
+def rlkv_debug_chunk_plan(lens, counts, n_full, n_comp, group, sink, window, shape=-1, max_ctas=296):
     """int32 [ctas + 1][4]: sequence, query tile, head and key tile that each CTA's range begins with, and the end."""
     ln, m, ctas = _slots(lens), _slots(counts), _ci(0)
     if ln.size != m.size:
         raise ValueError("lens and counts must have an entry for each sequence")
     at = np.zeros((max_ctas + 1, 4), dtype=np.int32)
-    _check(lib.rlkv_debug_chunk_plan(ln.ctypes.data, m.ctypes.data, ln.size, n_full, n_comp, group, sink, window, subs, max_ctas,
+    _check(lib.rlkv_debug_chunk_plan(ln.ctypes.data, m.ctypes.data, ln.size, n_full, n_comp, group, sink, window, shape, max_ctas,
                                      ctypes.byref(ctas), at.ctypes.data))
     return at[:ctas.value + 1]
 

@@ -42,8 +42,10 @@ constexpr int kRows = 128;           // query rows of a sub-tile
 constexpr int kQBlock = kRows * 128; // bytes of a [128 rows][64 elements] block
 constexpr int kPageBytes = 2 * kTile * 128;  // of an 8-bit page
 
-template <int D, int SUBS, bool FP8>
+template <int D, int SHAPE, bool FP8>
 struct Chunk {
+    static constexpr int SUBS = SHAPE == 2 ? 2 : 1;
+    static constexpr bool QUAD = SHAPE == 0;
     static constexpr int kKeys = SUBS == 2 ? 128 : 64;  // of a tile
     static constexpr int kPages = kKeys / kTile;
     static constexpr int kQBytes = kRows * D * 2, kTileBytes = kKeys * D * 2;
@@ -79,7 +81,7 @@ struct SoftmaxPlace {
 
 struct ChunkShared {
     uint64_t q_full[2], q_split[2], q_empty[2], full[10], empty[10], dirty[10], clean[10], decoded[2], decoded_empty[2];
-    uint64_t s_full[2], p_full[2][2], pv_done[2], drain;
+    uint64_t s_full[2], p_full[2][2], pv_done[2], meet, drain;
     uint32_t tmem;
     int abort;
     SoftmaxPlace place[1];  // (one of each softmax warp)
@@ -172,6 +174,16 @@ __device__ __forceinline__ float split_row(uint8_t* q, int row)
 }
 
 // A row's columns, waited for in the same statement: none of them can be spilled before it has arrived.
+__device__ __forceinline__ void read_columns(uint32_t addr, float (&s)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(s[0]), "=f"(s[1]), "=f"(s[2]), "=f"(s[3]), "=f"(s[4]), "=f"(s[5]), "=f"(s[6]), "=f"(s[7]), "=f"(s[8]),
+          "=f"(s[9]), "=f"(s[10]), "=f"(s[11]), "=f"(s[12]), "=f"(s[13]), "=f"(s[14]), "=f"(s[15])
+        : "r"(addr)
+        : "memory");
+}
 __device__ __forceinline__ void read_columns(uint32_t addr, float (&s)[32])
 {
     asm volatile(
@@ -239,7 +251,7 @@ __device__ __forceinline__ void read_columns(uint32_t addr, float (&s)[128])
 // P = 2^(s factor - base) of a row's scores, as bf16 to tensor memory, and their sums; 64 keys at a time, so that the
 // product starts on the first.
 template <int N>
-__device__ __forceinline__ void exponentials(float (&s)[N], float factor, float base, float2 (&sum)[2], uint32_t P, uint64_t* done, int lane)
+__device__ __forceinline__ void exponentials(float (&s)[N], float factor, float base, float2 (&sum)[2], uint32_t P, uint64_t* done, int lane, int)
 {
     const float2 factor2 = make_float2(factor, factor), base2 = make_float2(-base, -base);
 #pragma unroll
@@ -264,6 +276,32 @@ __device__ __forceinline__ void exponentials(float (&s)[N], float factor, float 
     for (int c = 0; c < N; c += 2) sum[c / 2 & 1] = add2(sum[c / 2 & 1], make_float2(s[c], s[c + 1]));
 }
 
+// The same for a quarter of 64 keys, those of warp `quarter`: P of the other keys is zero in this warp's rows.
+__device__ __forceinline__ void exponentials(float (&s)[16], float factor, float base, float2 (&sum)[2], uint32_t P, uint64_t* done, int lane, int quarter)
+{
+    const float2 factor2 = make_float2(factor, factor), base2 = make_float2(-base, -base);
+    uint32_t packed[8];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+        const float2 x = fma2(make_float2(s[i], s[i + 1]), factor2, base2);
+        s[i] = ex2(x.x);
+        s[i + 1] = ex2(x.y);
+        packed[i / 2] = bf16x2(s[i], s[i + 1]);
+    }
+#pragma unroll
+    for (int x = 1; x < 4; ++x)
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%1,%1,%1,%1,%1,%1,%1};" ::"r"(P + ((quarter + x) & 3) * 8), "r"(0) : "memory");
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(P + quarter * 8), "r"(packed[0]), "r"(packed[1]),
+                 "r"(packed[2]), "r"(packed[3]), "r"(packed[4]), "r"(packed[5]), "r"(packed[6]), "r"(packed[7])
+                 : "memory");
+    wait_st();
+    fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(done));
+#pragma unroll
+    for (int c = 0; c < 16; c += 2) sum[c / 2 & 1] = add2(sum[c / 2 & 1], make_float2(s[c], s[c + 1]));
+}
+
 // Two E4M3 codes in the high bytes of a word's halves, as bf16: the exponent and mantissa bits moved to their places read
 // as a bf16 number 2^-120 times the value (subnormals too); the product is exact.
 __device__ __forceinline__ uint32_t decode2(uint32_t x)
@@ -285,13 +323,13 @@ __device__ __forceinline__ void decode16(const uint4& codes, uint4& lo, uint4& h
 }
 
 // Walks the segments of CTA `cta` in order.
-template <int KEYS, int SUBS>
+template <int KEYS, int SUBS, int ROWS>
 struct Walk {
     const ChunkArgs& a;
     ChunkPos at, end;
     int tokens, cta;  // tokens of a sub-tile
     bool first = true;
-    __device__ __forceinline__ Walk(const ChunkArgs& args) : a(args), at(args.at[blockIdx.x]), end(args.at[blockIdx.x + 1]), tokens(kRows / args.group), cta(blockIdx.x) {}
+    __device__ __forceinline__ Walk(const ChunkArgs& args) : a(args), at(args.at[blockIdx.x]), end(args.at[blockIdx.x + 1]), tokens(ROWS / args.group), cta(blockIdx.x) {}
     __device__ __forceinline__ bool next(Segment& s)
     {
         if (same_unit(at, end) && at.tile >= end.tile) return false;
@@ -338,13 +376,16 @@ struct Walk {
     static __device__ __forceinline__ bool unclean(const Segment& s, int t) { return (!FP8 || t < s.fresh) && valid_rows(s, t) < KEYS; }
 };
 
-template <int D, int SUBS, bool FP8, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(Chunk<D, SUBS, FP8>::kThreads, Chunk<D, SUBS, FP8>::kPerSm)
+template <int D, int SHAPE, bool FP8, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(Chunk<D, SHAPE, FP8>::kThreads, Chunk<D, SHAPE, FP8>::kPerSm)
 chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkMaps maps)
 {
-    using C = Chunk<D, SUBS, FP8>;
-    using W = Walk<C::kKeys, SUBS>;
-    constexpr int KEYS = C::kKeys, kHalves = KEYS / 64;
+    using C = Chunk<D, SHAPE, FP8>;
+    constexpr int SUBS = C::SUBS, KEYS = C::kKeys, kHalves = KEYS / 64;
+    constexpr bool QUAD = C::QUAD;
+    constexpr int kTileRows = QUAD ? 32 : kRows;      // query rows of a sub-tile
+    constexpr int kColumnsOf = QUAD ? KEYS / 4 : KEYS;  // scores of a thread
+    using W = Walk<KEYS, SUBS, kTileRows>;
     extern __shared__ __align__(1024) uint8_t smem[];
     static_assert(sizeof(ChunkShared) + (C::kSoftmaxWarps - 1) * sizeof(SoftmaxPlace) <= C::kSmem - C::kState && C::kSmem <= kMaxDynamicSmem, "shared memory");
     static_assert(C::kPerSm * (C::kSmem + 1024) <= 228 * 1024, "shared memory of an SM");
@@ -382,6 +423,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 mbar_init(smem_u32(&sh.p_full[w][1]), 4);
                 mbar_init(smem_u32(&sh.pv_done[w]), 1);
             }
+            mbar_init(smem_u32(&sh.meet), 4);
             mbar_init(smem_u32(&sh.drain), 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
@@ -405,8 +447,9 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
         const int w = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t O = tmem + lanes + o_column + w * D;
-        const int in_tile = row / a.group, member = row - in_tile * a.group;
-        const int tokens = kRows / a.group;
+        const int tile_row = QUAD ? lane : row, in_tile = tile_row / a.group, member = tile_row - in_tile * a.group;
+        const int tokens = kTileRows / a.group;
+        const int column0 = QUAD ? warp * kColumnsOf : 0;  // the warp's part of a tile's keys
         int total = 0, seg = 0;  // tiles of this sub-tile and segments so far
         bool ok = true;
         // SUBS 1: the score product of tile n goes out before the value product of tile n - 1, so that two of the latter may be
@@ -414,6 +457,12 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
         auto product_done = [&](int n) {
             return SUBS == 2 ? wait(smem_u32(&sh.pv_done[w]), n & 1, abort_flag, a.status, kChunkWaitProduct)
                              : wait(smem_u32(&sh.pv_done[n & 1]), n >> 1 & 1, abort_flag, a.status, kChunkWaitProduct);
+        };
+        int met = 0;
+        auto meet = [&]() {  // the four softmax warps of a CTA wait for one another
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.meet));
+            return wait(smem_u32(&sh.meet), met++ & 1, abort_flag, a.status, kChunkWaitSoftmax);
         };
         SoftmaxPlace* place_of = sh.place + warp;
         const volatile Segment& g = place_of->g;
@@ -476,13 +525,13 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 }
                 fence_after();
                 // what this row sees of the tile: up to three ranges of columns, [lo1, hi1), [lo2, hi2), [0, hi3)
-                const int start = cached ? (t - g.fresh) * KEYS : W::chunk_tile(g.u, t);
+                const int start = (cached ? (t - g.fresh) * KEYS : W::chunk_tile(g.u, t)) + column0;
                 bool plain;
                 int lo1 = 0, hi1, lo2 = 0, hi2 = 0, hi3 = 0;
                 if (cached) {
                     if (g.full) {
                         hi1 = g.len - start;
-                        plain = hi1 >= KEYS;
+                        plain = hi1 >= kColumnsOf;
                     } else {
                         hi3 = min(a.sink, g.u.rows) - start;
                         lo1 = max(a.sink, w1 + i + 1 - a.window) - start;
@@ -493,23 +542,23 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                     }
                 } else {
                     hi1 = i + 1 - start;
-                    plain = start + KEYS <= from + 1;
+                    plain = start + kColumnsOf <= from + 1;
                     if (!g.full) {
                         lo1 = i - a.window + 1 - start;
                         hi3 = min(a.sink - g.len, i + 1) - start;
-                        plain = plain && (start > upto - a.window || start + KEYS <= a.sink - g.len);
+                        plain = plain && (start > upto - a.window || start + kColumnsOf <= a.sink - g.len);
                     }
                 }
-                uint32_t see[KEYS / 32];
+                uint32_t see[(kColumnsOf + 31) / 32];
 #pragma unroll
-                for (int x = 0; x < KEYS; x += 32)
+                for (int x = 0; x < kColumnsOf; x += 32)
                     see[x / 32] = mine ? range_bits(lo1 - x, hi1 - x) | range_bits(lo2 - x, hi2 - x) | range_bits(0, hi3 - x) : 0u;
-                float s[KEYS];
-                read_columns(S, s);
+                float s[kColumnsOf];
+                read_columns(S + column0, s);
                 if (CAP) {
                     if (!plain) {  // (what lies in rows without a token has no say in how a warp computes the cap)
 #pragma unroll
-                        for (int c = 0; c < KEYS; ++c) s[c] = see[c / 32] >> (c & 31) & 1 ? s[c] : 0.f;
+                        for (int c = 0; c < kColumnsOf; ++c) s[c] = see[c / 32] >> (c & 31) & 1 ? s[c] : 0.f;
                     }
                     cap.apply(s, mine);
                 }
@@ -523,7 +572,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
 #pragma unroll
                         for (int c = 0; c < 8; c += 2) d[c / 2] = make_float2((float)c - far, (float)(c + 1) - far);
 #pragma unroll
-                        for (int c = 0; c < KEYS; c += 2) {
+                        for (int c = 0; c < kColumnsOf; c += 2) {
                             const float2 x = CAP ? make_float2(s[c], s[c + 1]) : mul2(make_float2(s[c], s[c + 1]), make_float2(sl2, sl2));
                             const float2 y = fma2(make_float2(slope2, slope2), d[c / 2 & 3], x);
                             s[c] = y.x;
@@ -534,7 +583,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                         const float near = (float)(i + w1 - start), older = (float)(i + w1 + a.window - start);
                         const int b1 = a.sink - start, b2 = w1 - start;
 #pragma unroll
-                        for (int c = 0; c < KEYS; ++c) {
+                        for (int c = 0; c < kColumnsOf; ++c) {
                             const float from_row = c < b1 ? far : c < b2 ? near : older;
                             s[c] = fmaf(-slope2, from_row - (float)c, CAP ? s[c] : s[c] * sl2);
                         }
@@ -542,12 +591,12 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 }
                 if (!plain) {
 #pragma unroll
-                    for (int c = 0; c < KEYS; ++c) s[c] = see[c / 32] >> (c & 31) & 1 ? s[c] : -INFINITY;
+                    for (int c = 0; c < kColumnsOf; ++c) s[c] = see[c / 32] >> (c & 31) & 1 ? s[c] : -INFINITY;
                 }
                 const float factor = CAP || BIAS ? 1.f : scale * kLog2e;
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int c = 0; c < KEYS; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);
+                for (int c = 0; c < kColumnsOf; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);
                 const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * factor;
                 if (top > m + 8.f) {  // (m may still be -infinity: then there is nothing to correct)
                     const float x = m == -INFINITY ? 1.f : ex2(m - top);
@@ -570,7 +619,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 }
                 const float base = m == -INFINITY ? 0.f : m;
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                exponentials(s, factor, base, sum, S, sh.p_full[place], lane);
+                exponentials(s, factor, base, sum, S, sh.p_full[place], lane, warp);
                 l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             }
             if (!ok) break;
@@ -582,7 +631,62 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
             }
             const float unit = FP8 && g.t1 > g.fresh ? v_scale : 1.f;
             const long long at_head = ((long long)(g.start + i) * a.q_heads + head);
-            if (!busy) {
+            if (QUAD) {
+                // the warps' parts of the keys meet, in the memory of the queries (which are not needed any more): maxima and sums,
+                // then half of the output's columns at a time, of which each warp adds up a quarter
+                float* at = reinterpret_cast<float*>(smem);
+                at[warp * 32 + lane] = m;
+                at[128 + warp * 32 + lane] = l;
+                ok = meet();
+                float all = -INFINITY, total_l = 0.f;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) all = fmaxf(all, at[x * 32 + lane]);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) total_l += at[x * 32 + lane] == -INFINITY ? 0.f : at[128 + x * 32 + lane] * ex2(at[x * 32 + lane] - all);
+                const bool whole = g.record < 0;
+                const float f = m == -INFINITY ? 0.f : ex2(m - all) * unit, inv = whole ? (total_l > 0.f ? 1.f / total_l : 0.f) : 1.f;
+                float* rec = a.records + (long long)max(g.record, 0) * chunk_record_floats(D, SHAPE);
+                if (warp == 0) {
+                    if (!whole) {
+                        rec[D * 32 + lane] = all;
+                        rec[(D + 1) * 32 + lane] = total_l;
+                    } else if (mine && a.lse) {
+                        a.lse[at_head] = total_l > 0.f ? (all + log2f(total_l)) * kLn2 : -INFINITY;
+                    }
+                }
+                constexpr int kHalf = D / 8, kMine = D / 32;  // groups of four columns in a half, and a warp's of them
+                float4* part = reinterpret_cast<float4*>(smem);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    ok = ok && meet();
+#pragma unroll
+                    for (int c = 0; c < D / 2; c += 32) {
+                        float o[32];
+                        read_columns(O + half * (D / 2) + c, o);
+#pragma unroll
+                        for (int x = 0; x < 8; ++x)
+                            part[(warp * kHalf + c / 4 + x) * 32 + lane] = make_float4(o[4 * x] * f, o[4 * x + 1] * f, o[4 * x + 2] * f, o[4 * x + 3] * f);
+                    }
+                    ok = ok && meet();
+                    float4 y[kMine];
+#pragma unroll
+                    for (int c = 0; c < kMine; ++c) {
+                        y[c] = part[(warp * kMine + c) * 32 + lane];
+#pragma unroll
+                        for (int x = 1; x < 4; ++x) {
+                            const float4 z = part[(x * kHalf + warp * kMine + c) * 32 + lane];
+                            y[c] = make_float4(y[c].x + z.x, y[c].y + z.y, y[c].z + z.z, y[c].w + z.w);
+                        }
+                        if (!whole) reinterpret_cast<float4*>(rec)[(half * kHalf + warp * kMine + c) * 32 + lane] = y[c];
+                    }
+                    if (whole && mine)
+#pragma unroll
+                        for (int c = 0; c < kMine; c += 2)
+                            *reinterpret_cast<uint4*>(a.out + at_head * D + half * (D / 2) + (warp * kMine + c) * 4) =
+                                make_uint4(bf16x2(y[c].x * inv, y[c].y * inv), bf16x2(y[c].z * inv, y[c].w * inv),
+                                           bf16x2(y[c + 1].x * inv, y[c + 1].y * inv), bf16x2(y[c + 1].z * inv, y[c + 1].w * inv));
+                }
+            } else if (!busy) {
             } else if (g.record < 0) {
                 const float inv = l > 0.f ? unit / l : 0.f;
                 if (mine && a.lse) a.lse[at_head] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
@@ -610,7 +714,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                             *reinterpret_cast<const uint4*>(stage + r * D * 2 + (((lane % kChunks) ^ (r & 7)) << 4));
                 }
             } else {
-                float* rec = a.records + (long long)g.record * chunk_record_floats(D, SUBS) + (long long)w * kRows * (D + 2);
+                float* rec = a.records + (long long)g.record * chunk_record_floats(D, SHAPE) + (long long)w * kRows * (D + 2);
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
                     float o[32];
@@ -624,6 +728,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 rec[D * kRows + row] = m;
                 rec[(D + 1) * kRows + row] = l;
             }
+            if (!ok) break;
             fence_before();
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -646,10 +751,11 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 if (!ok) return;
                 if (lane == 0)
                     for (int w = 0; w < g.subs; ++w) {
-                        mbar_expect_tx(smem_u32(&sh.q_full[w]), (D / 64) * walk.tokens * a.group * 128);
-                        for (int b = 0; b < D / 64; ++b)
-                            load_box(q_smem + w * C::kQBytes + b * kQBlock, &maps.q, b * 64, g.head * a.group, row0 + w * walk.tokens,
-                                     smem_u32(&sh.q_full[w]));
+                        constexpr int kCopies = QUAD ? 4 : 1;  // (the quarters' warps each have rows of their own)
+                        mbar_expect_tx(smem_u32(&sh.q_full[w]), kCopies * (D / 64) * walk.tokens * a.group * 128);
+                        for (int b = 0; b < kCopies * (D / 64); ++b)
+                            load_box(q_smem + w * C::kQBytes + b / kCopies * kQBlock + b % kCopies * (32 * 128), &maps.q, b / kCopies * 64,
+                                     g.head * a.group, row0 + w * walk.tokens, smem_u32(&sh.q_full[w]));
                     }
                 q_waits = false;
                 for (int w = 0; w < g.subs; ++w) ++loaded[w];
@@ -952,17 +1058,17 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
 // columns and of each run every 8 / COLUMNS-th piece, and meet in shared memory: all columns and few pieces at a time where units
 // are cut once or twice, one run and eight pieces where few units are cut into many.  The pieces' order is that of the keys,
 // whatever CTA ran first.
-template <int D, int SUBS, int COLUMNS>
+template <int D, int SHAPE, int COLUMNS>
 __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constant__ ChunkArgs a)
 {
-    constexpr int kPieces = 8 / COLUMNS;
+    constexpr int kPieces = 8 / COLUMNS, kRecordRows = SHAPE == 0 ? 32 : kRows;
     __shared__ float part[8][32][33], top[8][32], sum[8][32];
     const int c = blockIdx.x + 1;
     const ChunkPos b = a.at[c], before = a.at[c - 1];
     if (b.tile == 0 || b.seq >= a.seqs.n || (same_unit(before, b) && before.tile > 0)) return;
-    const int tokens = kRows / a.group, w = blockIdx.y / 4, row0 = blockIdx.y % 4 * 32;
+    const int tokens = kRecordRows / a.group, w = blockIdx.y / 4, row0 = blockIdx.y % 4 * 32;
     const int start = a.seqs.start[b.seq], m = a.seqs.start[b.seq + 1] - start;
-    const int from = b.row_tile * SUBS * tokens + w * tokens;
+    const int from = (b.row_tile * (SHAPE == 2 ? 2 : 1) + w) * tokens;
     if (row0 / a.group >= tokens || from + row0 / a.group >= m) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int last = c;  // the pieces are those of CTAs c - 1 .. last
@@ -973,12 +1079,12 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
     for (int x = 0; x < 32; ++x) o[x] = 0.f;
     for (int k = c - 1 + warp / COLUMNS; k <= last; k += kPieces) {
         const int slot = k > c - 1 || same_unit(before, b) ? 2 * k : 2 * k + 1;
-        const float* rec = a.records + (long long)slot * chunk_record_floats(D, SUBS) + (long long)w * kRows * (D + 2);
-        const float pm = rec[D * kRows + row0 + lane], pl = rec[(D + 1) * kRows + row0 + lane];
+        const float* rec = a.records + (long long)slot * chunk_record_floats(D, SHAPE) + (long long)w * kRows * (D + 2);
+        const float pm = rec[D * kRecordRows + row0 + lane], pl = rec[(D + 1) * kRecordRows + row0 + lane];
         float4 y[8];
 #pragma unroll
         for (int x = 0; x < 8; ++x)
-            y[x] = reinterpret_cast<const float4*>(rec)[((blockIdx.z * COLUMNS + warp % COLUMNS) * 8 + x) * kRows + row0 + lane];
+            y[x] = reinterpret_cast<const float4*>(rec)[((blockIdx.z * COLUMNS + warp % COLUMNS) * 8 + x) * kRecordRows + row0 + lane];
         if (pm == -INFINITY) continue;  // the row sees none of the piece's keys
         const float to = fmaxf(mx, pm), old = mx == -INFINITY ? 0.f : ex2(mx - to), f = ex2(pm - to);
         mx = to;
@@ -1024,18 +1130,18 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
     if (a.lse && blockIdx.z == 0 && x0 == 0) a.lse[at_head] = total > 0.f ? (all + log2f(total)) * kLn2 : -INFINITY;
 }
 
-template <int D, int SUBS, bool FP8>
+template <int D, int SHAPE, bool FP8>
 cudaError_t launch_shape(const ChunkArgs& a, const ChunkMaps& m, int pieces, cudaStream_t stream)
 {
-    using C = Chunk<D, SUBS, FP8>;
-    auto kernel = a.softcap != 0.f ? (a.slopes ? chunk_attention_kernel<D, SUBS, FP8, true, true> : chunk_attention_kernel<D, SUBS, FP8, true, false>)
-                                   : (a.slopes ? chunk_attention_kernel<D, SUBS, FP8, false, true> : chunk_attention_kernel<D, SUBS, FP8, false, false>);
+    using C = Chunk<D, SHAPE, FP8>;
+    auto kernel = a.softcap != 0.f ? (a.slopes ? chunk_attention_kernel<D, SHAPE, FP8, true, true> : chunk_attention_kernel<D, SHAPE, FP8, true, false>)
+                                   : (a.slopes ? chunk_attention_kernel<D, SHAPE, FP8, false, true> : chunk_attention_kernel<D, SHAPE, FP8, false, false>);
     kernel<<<a.ctas, C::kThreads, C::kSmem, stream>>>(a, m);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || pieces < 2) return e;
     const bool few = pieces <= 4;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.ctas - 1, SUBS * 4, few ? 1 : D / 32);
+    cfg.gridDim = dim3(a.ctas - 1, SHAPE == 0 ? 1 : SHAPE * 4, few ? 1 : D / 32);
     cfg.blockDim = dim3(256);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -1043,39 +1149,47 @@ cudaError_t launch_shape(const ChunkArgs& a, const ChunkMaps& m, int pieces, cud
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return few ? cudaLaunchKernelEx(&cfg, chunk_combine_kernel<D, SUBS, D / 32>, a) : cudaLaunchKernelEx(&cfg, chunk_combine_kernel<D, SUBS, 1>, a);
+    return few ? cudaLaunchKernelEx(&cfg, chunk_combine_kernel<D, SHAPE, D / 32>, a) : cudaLaunchKernelEx(&cfg, chunk_combine_kernel<D, SHAPE, 1>, a);
 }
 
-template <int D, int SUBS, bool FP8>
+template <int D, int SHAPE, bool FP8>
 cudaError_t prepare_shape()
 {
-    const void* kernels[] = {(const void*)chunk_attention_kernel<D, SUBS, FP8, false, false>, (const void*)chunk_attention_kernel<D, SUBS, FP8, false, true>,
-                             (const void*)chunk_attention_kernel<D, SUBS, FP8, true, false>, (const void*)chunk_attention_kernel<D, SUBS, FP8, true, true>};
+    const void* kernels[] = {(const void*)chunk_attention_kernel<D, SHAPE, FP8, false, false>, (const void*)chunk_attention_kernel<D, SHAPE, FP8, false, true>,
+                             (const void*)chunk_attention_kernel<D, SHAPE, FP8, true, false>, (const void*)chunk_attention_kernel<D, SHAPE, FP8, true, true>};
     for (const void* k : kernels) {
-        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Chunk<D, SUBS, FP8>::kSmem);
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Chunk<D, SHAPE, FP8>::kSmem);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
 
+template <int D, bool FP8>
+cudaError_t launch_dim(const ChunkArgs& a, const ChunkMaps& m, int shape, int pieces, cudaStream_t stream)
+{
+    return shape == 2 ? launch_shape<D, 2, FP8>(a, m, pieces, stream)
+                      : shape == 1 ? launch_shape<D, 1, FP8>(a, m, pieces, stream) : launch_shape<D, 0, FP8>(a, m, pieces, stream);
+}
+
+template <int D, bool FP8>
+cudaError_t prepare_dim()
+{
+    cudaError_t e = prepare_shape<D, 0, FP8>();
+    if (e == cudaSuccess) e = prepare_shape<D, 1, FP8>();
+    return e == cudaSuccess ? prepare_shape<D, 2, FP8>() : e;
+}
+
 }  // namespace
 
-cudaError_t launch_chunk_attention(const ChunkArgs& a, const ChunkMaps& m, int head_dim, int subs, int pieces, cudaStream_t stream)
+cudaError_t launch_chunk_attention(const ChunkArgs& a, const ChunkMaps& m, int head_dim, int shape, int pieces, cudaStream_t stream)
 {
-    if (a.pool8) return subs == 2 ? launch_shape<128, 2, true>(a, m, pieces, stream) : launch_shape<128, 1, true>(a, m, pieces, stream);
-    if (head_dim == 128) return subs == 2 ? launch_shape<128, 2, false>(a, m, pieces, stream) : launch_shape<128, 1, false>(a, m, pieces, stream);
-    return subs == 2 ? launch_shape<64, 2, false>(a, m, pieces, stream) : launch_shape<64, 1, false>(a, m, pieces, stream);
+    return a.pool8 ? launch_dim<128, true>(a, m, shape, pieces, stream)
+                   : head_dim == 128 ? launch_dim<128, false>(a, m, shape, pieces, stream) : launch_dim<64, false>(a, m, shape, pieces, stream);
 }
 
 cudaError_t prepare_chunk_kernels(int head_dim, bool fp8)
 {
-    cudaError_t e;
-    if (fp8) {
-        e = prepare_shape<128, 2, true>();
-        return e != cudaSuccess ? e : prepare_shape<128, 1, true>();
-    }
-    e = head_dim == 128 ? prepare_shape<128, 2, false>() : prepare_shape<64, 2, false>();
-    return e != cudaSuccess ? e : head_dim == 128 ? prepare_shape<128, 1, false>() : prepare_shape<64, 1, false>();
+    return fp8 ? prepare_dim<128, true>() : head_dim == 128 ? prepare_dim<128, false>() : prepare_dim<64, false>();
 }
 
 }  // namespace rlkv

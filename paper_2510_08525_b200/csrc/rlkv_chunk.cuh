@@ -95,9 +95,12 @@ struct ChunkArgs {
     unsigned char head_of_slot[kMaxKvHeads];
     float k_scale[kMaxKvHeads], v_scale[kMaxKvHeads];  // by head
 };
-// Floats of one record: `subs` sub-tiles of 128 rows, each [head_dim / 4][128] float4, then [2][128] maximum and sum.
-__host__ __device__ constexpr long long chunk_record_floats(int head_dim, int subs) { return (long long)subs * 128 * (head_dim + 2); }
-// (one sub-tile on two CTAs of an SM, or two on one: the same bytes)
+// The kernel's shapes: query rows of a unit's row tile, keys of a tile.  0: 32 rows, 64 keys; 1: 128 rows, 64 keys (both two
+// CTAs on an SM); 2: two times 128 rows, 128 keys.
+__host__ __device__ constexpr int chunk_keys(int shape) { return shape == 2 ? 128 : 64; }
+__host__ __device__ constexpr int chunk_tokens(int shape, int group) { return shape == 2 ? 2 * (128 / group) : (shape == 1 ? 128 : 32) / group; }
+// Floats of one record: of each sub-tile of R rows (32 or 128) [head_dim / 4][R] float4, then [2][R] maximum and sum.
+__host__ __device__ constexpr long long chunk_record_floats(int head_dim, int shape) { return (shape == 2 ? 256ll : shape == 1 ? 128 : 32) * (head_dim + 2); }
 inline size_t chunk_record_bytes(int head_dim) { return (size_t)2 * kMaxChunkCtas * chunk_record_floats(head_dim, 1) * sizeof(float); }
 
 // Status codes (device error word of the cache): which wait of the chunk kernel ran out.
@@ -108,7 +111,7 @@ struct ChunkMaps {
     CUtensorMap q, k, v, pool;  // pool: 64 elements x 64 rows of the 16-bit pool, or whole pages of the 8-bit one
 };
 // pieces: most ranges that a unit lies in (1: none is cut)
-cudaError_t launch_chunk_attention(const ChunkArgs& a, const ChunkMaps& m, int head_dim, int subs, int pieces, cudaStream_t stream);
+cudaError_t launch_chunk_attention(const ChunkArgs& a, const ChunkMaps& m, int head_dim, int shape, int pieces, cudaStream_t stream);
 cudaError_t prepare_chunk_kernels(int head_dim, bool fp8);
 
 // ---- rows in and out of the cache -----------------------------------------------------------------------

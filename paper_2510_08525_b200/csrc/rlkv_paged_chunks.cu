@@ -81,9 +81,9 @@ void fill_rows_args(rlkv_paged* p, int layer, ChunkRowsArgs& a)
 
 // Cuts the flat sequence of the units' key tiles for at most max_ctas CTAs of at least min_tiles tiles; a unit counts `extra`
 // tiles more than it has (its queries' load and its results cost about as much).  Returns the most ranges that one unit lies in.
-int plan_chunks(ChunkArgs& a, int subs, int max_ctas, int min_tiles, int extra)
+int plan_chunks(ChunkArgs& a, int shape, int max_ctas, int min_tiles, int extra)
 {
-    const int keys = subs == 2 ? 128 : 64, tokens = subs * (128 / a.group);
+    const int keys = chunk_keys(shape), tokens = chunk_tokens(shape, a.group);
     const ChunkSeqs& s = a.seqs;
     auto unit = [&](int i, int j, bool full) {
         return chunk_unit(s.len[i], s.start[i + 1] - s.start[i], j, tokens, keys, full, a.sink, a.window).tiles + extra;
@@ -125,19 +125,21 @@ int plan_chunks(ChunkArgs& a, int subs, int max_ctas, int min_tiles, int extra)
     return most;
 }
 
-// Whether a launch takes two sub-tiles of 128 rows on one CTA of an SM (one-tile CTAs, two on an SM, otherwise): where most key
-// tiles belong to chunks that fill both.
-int choose_subs(const ChunkArgs& a)
+// The shape of a launch: 32 rows where every chunk's queries of a KV head fit them, two sub-tiles of 128 where most key tiles
+// belong to chunks that fill both, else one.
+int choose_shape(const ChunkArgs& a)
 {
     long long small = 0, large = 0;
+    bool few = true;
     for (int i = 0; i < a.seqs.n; ++i) {
         const int m = a.seqs.start[i + 1] - a.seqs.start[i];
+        if (m > chunk_tokens(0, a.group)) few = false;
         const long long rows = (long long)a.n_full * (a.seqs.len[i] + m) + (long long)a.n_comp * (a.sink + a.window + 128);
         const int tiles = (int)(((long long)m * a.group + 127) / 128);
         if (tiles > 1) large += rows * tiles;
         else if (tiles == 1) small += rows;
     }
-    return large > small ? 2 : 1;
+    return few ? 0 : large > small ? 2 : 1;
 }
 
 }  // namespace
@@ -238,21 +240,21 @@ int rlkv_paged_chunk_attention(rlkv_paged* p, int layer, const int* slots, const
         a.k_scale[h] = p->fp8 ? p->k_scale[(size_t)layer * p->kv_heads + h] : 1.f;
         a.v_scale[h] = p->fp8 ? p->v_scale[(size_t)layer * p->kv_heads + h] : 1.f;
     }
-    const int subs = choose_subs(a);
+    const int shape = choose_shape(a);
     const int sms = p->sm_count < kMaxChunkCtas / 2 ? p->sm_count : kMaxChunkCtas / 2;
-    const long long room = (long long)(p->chunk_bytes / (2 * sizeof(float) * chunk_record_floats(p->head_dim, subs)));  // CTAs it has records for
-    int ctas = subs == 2 ? sms : 2 * sms;
+    const long long room = (long long)(p->chunk_bytes / (2 * sizeof(float) * chunk_record_floats(p->head_dim, shape)));  // CTAs it has records for
+    int ctas = shape == 2 ? sms : 2 * sms;
     if (ctas > room) ctas = room < 1 ? 1 : (int)room;
-    const int pieces = plan_chunks(a, subs, ctas, kMinChunkTiles, kUnitTiles);
-    const int keys = subs == 2 ? 128 : 64;
+    const int pieces = plan_chunks(a, shape, ctas, kMinChunkTiles, kUnitTiles);
+    const int keys = chunk_keys(shape);
     ChunkMaps m;
-    int e = encode_heads_map(&m.q, q, total, p->q_heads, p->head_dim, q_stride, a.group, 128 / a.group);
+    int e = encode_heads_map(&m.q, q, total, p->q_heads, p->head_dim, q_stride, a.group, (shape == 0 ? 32 : 128) / a.group);
     if (!e) e = encode_heads_map(&m.k, k, total, p->kv_heads, p->head_dim, k_stride, 1, keys);
     if (!e) e = encode_heads_map(&m.v, v, total, p->kv_heads, p->head_dim, v_stride, 1, keys);
     if (!e && !p->fp8) e = encode_heads_map(&m.pool, dev_at<__nv_bfloat16>(p, p->off_pool), p->pool_rows, 1, p->head_dim, p->head_dim, 1, kTile);
     else if (!e) m.pool = p->map_k;
     if (e) return e;
-    RLKV_CUDA(launch_chunk_attention(a, m, p->head_dim, subs, pieces, static_cast<cudaStream_t>(stream)));
+    RLKV_CUDA(launch_chunk_attention(a, m, p->head_dim, shape, pieces, static_cast<cudaStream_t>(stream)));
     p->launches += pieces > 1 ? 2 : 1;
     return RLKV_OK;
 }
@@ -347,7 +349,7 @@ int rlkv_paged_read(rlkv_paged* p, int layer, const int* slots, const int* first
     return RLKV_OK;
 }
 
-int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full, int n_comp, int group, int sink, int window, int subs,
+int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full, int n_comp, int group, int sink, int window, int shape,
                           int max_ctas, int* ctas_out, int* at_out)
 {
     if (!lens || !counts || n < 1 || n > kMaxPagedBatch || n_full < 0 || n_comp < 0 || n_full + n_comp < 1 || group < 1 || group > kMaxGroup ||
@@ -370,9 +372,9 @@ int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full,
     a.group = group;
     a.sink = sink;
     a.window = window;
-    if (subs == 0) subs = choose_subs(a);
-    if (subs != 1 && subs != 2) return RLKV_EINVAL;
-    plan_chunks(a, subs, max_ctas, kMinChunkTiles, kUnitTiles);
+    if (shape < 0) shape = choose_shape(a);
+    if (shape > 2) return RLKV_EINVAL;
+    plan_chunks(a, shape, max_ctas, kMinChunkTiles, kUnitTiles);
     for (int c = 0; c <= a.ctas; ++c) {
         at_out[4 * c] = a.at[c].seq;
         at_out[4 * c + 1] = a.at[c].row_tile;

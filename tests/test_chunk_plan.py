@@ -31,10 +31,10 @@ def unit_tiles(n, m, tok0, tokens, keys, full, sink, window):
     return -(-rows // keys) + len(tiles)
 
 
-def check(binding, lens, counts, n_full, n_comp, group, sink, window, subs, ctas):
-    at = binding.rlkv_debug_chunk_plan(lens, counts, n_full, n_comp, group, sink, window, subs, ctas)
+def check(binding, lens, counts, n_full, n_comp, group, sink, window, shape, ctas):
+    at = binding.rlkv_debug_chunk_plan(lens, counts, n_full, n_comp, group, sink, window, shape, ctas)
     assert 1 <= len(at) - 1 <= ctas
-    keys, tokens = (128, 2 * (128 // group)) if subs == 2 else (64, 128 // group)
+    keys, tokens = ((64, 32 // group), (64, 128 // group), (128, 2 * (128 // group)))[shape]
     order, sizes = [], {}
     for i, (n, m) in enumerate(zip(lens, counts)):
         for j in range(-(-m // tokens)):
@@ -56,13 +56,13 @@ def check(binding, lens, counts, n_full, n_comp, group, sink, window, subs, ctas
     assert lengths.max() <= share + 2
 
 
-@pytest.mark.parametrize("subs", [1, 2])
+@pytest.mark.parametrize("shape", [0, 1, 2])
 @pytest.mark.parametrize("lens,counts,n_full,n_comp,group,sink,window,ctas", [
     ([8192], [5], 6, 2, 4, 16, 112, 296), ([8192], [700], 8, 0, 4, 16, 112, 148), ([0], [1], 1, 0, 1, 0, 5, 296),
     ([0, 3, 64, 65, 63, 200, 127, 128], [3, 0, 1, 65, 64, 1, 0, 130], 1, 3, 7, 16, 112, 296),
     ([10, 0, 0], [0, 300, 0], 0, 2, 8, 40, 25, 17), ([5, 500, 129], [70, 200, 1], 0, 1, 3, 100, 60, 296), ([1000], [1], 0, 1, 1, 0, 1, 1)])
-def test_ranges(binding, lens, counts, n_full, n_comp, group, sink, window, subs, ctas):
-    check(binding, lens, counts, n_full, n_comp, group, sink, window, subs, ctas)
+def test_ranges(binding, lens, counts, n_full, n_comp, group, sink, window, shape, ctas):
+    check(binding, lens, counts, n_full, n_comp, group, sink, window, shape, ctas)
 
 
 def test_random_batches(binding):
@@ -75,7 +75,7 @@ def test_random_batches(binding):
             counts[0] = 1
         n_full = rng.randint(0, 3)
         check(binding, lens, counts, n_full, rng.randint(0 if n_full else 1, 3), rng.randint(1, 8), rng.choice([0, 4, 16, 130]),
-              rng.choice([1, 5, 60, 112, 300]), rng.choice([1, 2]), rng.choice([1, 7, 148, 296]))
+              rng.choice([1, 5, 60, 112, 300]), rng.choice([0, 1, 2]), rng.choice([1, 7, 148, 296]))
 
 
 def test_refusals(binding):

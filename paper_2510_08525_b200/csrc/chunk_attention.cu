@@ -79,6 +79,19 @@ struct SoftmaxPlace {
     Segment g;
 };
 
+template <bool REFER, class A, class B>
+struct Choose;
+template <class A, class B>
+struct Choose<true, A, B> {
+    typedef A type;
+    static __device__ __forceinline__ A of(const Segment& s) { return s; }
+};
+template <class A, class B>
+struct Choose<false, A, B> {
+    typedef B type;
+    static __device__ __forceinline__ B of(const Segment& s) { return s; }
+};
+
 struct ChunkShared {
     uint64_t q_full[2], q_split[2], q_empty[2], full[10], empty[10], dirty[10], clean[10], decoded[2], decoded_empty[2];
     uint64_t s_full[2], p_full[2][2], pv_done[2], meet, drain;
@@ -363,13 +376,15 @@ struct Walk {
         }
         return true;
     }
-    // First chunk token of key tile t < fresh.
-    static __device__ __forceinline__ int chunk_tile(const volatile ChunkUnit& u, int t) { return (t < u.a_end ? t : u.b0 + t - u.a_end) * KEYS; }
-    // Rows of key tile t that hold a token (KEYS or more: all of them).
-    static __device__ __forceinline__ int valid_rows(const Segment& s, int t)
+    // First key of key tile t: a token of the chunk (t < fresh), or a row of what the cache holds -- from the newest back, so
+    // that distance terms are at their largest first and the running maximum stays.
+    template <class S>
+    static __device__ __forceinline__ int key_tile(const S& s, int t)
     {
-        return t < s.fresh ? s.m - chunk_tile(s.u, t) : s.u.rows - (t - s.fresh) * KEYS;
+        return (t >= s.fresh ? s.u.tiles - 1 - t : t < s.u.a_end ? t : s.u.b0 + t - s.u.a_end) * KEYS;
     }
+    // Rows of key tile t that hold a token (KEYS or more: all of them).
+    static __device__ __forceinline__ int valid_rows(const Segment& s, int t) { return (t < s.fresh ? s.m : s.u.rows) - key_tile(s, t); }
     // Whether the V rows of key tile t are to be cleared where they hold no token: 0 * NaN of what lies there would be NaN.
     // (Decoded codes are finite.)
     template <bool FP8>
@@ -465,7 +480,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
             return wait(smem_u32(&sh.meet), met++ & 1, abort_flag, a.status, kChunkWaitSoftmax);
         };
         SoftmaxPlace* place_of = sh.place + warp;
-        const volatile Segment& g = place_of->g;
+        const volatile Segment& kept = place_of->g;
         if (lane == 0) {
             place_of->at = a.at[blockIdx.x];
             place_of->first = 1;
@@ -485,7 +500,10 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
             }
             if (!__shfl_sync(0xffffffffu, more, 0)) break;
             __syncwarp();
-            if (w >= g.subs) continue;
+            if (w >= kept.subs) continue;
+            // (where scores take all registers, the segment is read where it is needed)
+            typedef Choose<SUBS == 2 || (FP8 && !QUAD), const volatile Segment&, const Segment> Kept;
+            typename Kept::type g = Kept::of(place_of->g);
             const int from = g.u.tok0 + w * tokens;     // the sub-tile's first token
             const int i = from + in_tile, head = g.head * a.group + member;
             const bool mine = in_tile < tokens && i < g.m;
@@ -524,35 +542,33 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                     continue;
                 }
                 fence_after();
-                // what this row sees of the tile: up to three ranges of columns, [lo1, hi1), [lo2, hi2), [0, hi3)
-                const int start = (cached ? (t - g.fresh) * KEYS : W::chunk_tile(g.u, t)) + column0;
-                bool plain;
-                int lo1 = 0, hi1, lo2 = 0, hi2 = 0, hi3 = 0;
-                if (cached) {
-                    if (g.full) {
-                        hi1 = g.len - start;
-                        plain = hi1 >= kColumnsOf;
-                    } else {
-                        hi3 = min(a.sink, g.u.rows) - start;
-                        lo1 = max(a.sink, w1 + i + 1 - a.window) - start;
-                        hi1 = w1 - start;
-                        lo2 = w1 + i + 1 - start;
-                        hi2 = g.u.rows - start;
-                        plain = false;
-                    }
-                } else {
-                    hi1 = i + 1 - start;
-                    plain = start + kColumnsOf <= from + 1;
-                    if (!g.full) {
-                        lo1 = i - a.window + 1 - start;
-                        hi3 = min(a.sink - g.len, i + 1) - start;
-                        plain = plain && (start > upto - a.window || start + kColumnsOf <= a.sink - g.len);
-                    }
-                }
+                const int start = W::key_tile(g, t) + column0;
+                const bool plain = cached ? g.full && start + kColumnsOf <= g.len
+                                          : start + kColumnsOf <= from + 1 && (g.full || start > upto - a.window || start + kColumnsOf <= a.sink - g.len);
                 uint32_t see[(kColumnsOf + 31) / 32];
+                if (!plain) {
+                    // what this row sees of the tile: up to three ranges of columns, [lo1, hi1), [lo2, hi2), [0, hi3)
+                    int lo1 = 0, hi1, lo2 = 0, hi2 = 0, hi3 = 0;
+                    if (cached) {
+                        hi1 = g.len - start;
+                        if (!g.full) {
+                            hi3 = min(a.sink, g.u.rows) - start;
+                            lo1 = max(a.sink, w1 + i + 1 - a.window) - start;
+                            hi1 = w1 - start;
+                            lo2 = w1 + i + 1 - start;
+                            hi2 = g.u.rows - start;
+                        }
+                    } else {
+                        hi1 = i + 1 - start;
+                        if (!g.full) {
+                            lo1 = i - a.window + 1 - start;
+                            hi3 = min(a.sink - g.len, i + 1) - start;
+                        }
+                    }
 #pragma unroll
-                for (int x = 0; x < kColumnsOf; x += 32)
-                    see[x / 32] = mine ? range_bits(lo1 - x, hi1 - x) | range_bits(lo2 - x, hi2 - x) | range_bits(0, hi3 - x) : 0u;
+                    for (int x = 0; x < kColumnsOf; x += 32)
+                        see[x / 32] = mine ? range_bits(lo1 - x, hi1 - x) | range_bits(lo2 - x, hi2 - x) | range_bits(0, hi3 - x) : 0u;
+                }
                 float s[kColumnsOf];
                 read_columns(S + column0, s);
                 if (CAP) {
@@ -775,15 +791,15 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
             };
             const int* table = a.page_table + (long long)g.slot * a.table_stride;
             const int n_pages = (g.u.rows + kTile - 1) / kTile;
-            int batch = max(g.t0 - g.fresh, 0) * C::kPages, entry = 0;  // page-table entries batch .. batch+31, one per lane
-            auto fetch = [&](int first) {
-                batch = first;
-                entry = g.full && first + lane < n_pages ? min(max(table[first + lane], 0), a.n_pages - 1) : 0;
+            int batch = 0, entry = 0;  // page-table entries batch .. batch+31, one per lane; tiles come from the last one back
+            auto fetch = [&](int last) {
+                batch = max(last - 31, 0);
+                entry = g.full && batch + lane < n_pages ? min(max(table[batch + lane], 0), a.n_pages - 1) : 0;
             };
-            if (g.t1 > g.fresh) fetch(batch);
+            if (g.t1 > g.fresh) fetch(W::key_tile(g, max(g.t0, g.fresh)) / kTile + C::kPages - 1);
             for (int t = g.t0; ok && t < g.t1; ++t) {
                 if (t < g.fresh) {
-                    const int token = g.start + W::chunk_tile(g.u, t);
+                    const int token = g.start + W::key_tile(g, t);
                     for (int kv = 0; kv < 2; ++kv) {
                         const int slot = issued % C::kStages;
                         if (!free_stage(slot)) break;
@@ -798,8 +814,8 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                     }
                     continue;
                 }
-                const int page = (t - g.fresh) * C::kPages;
-                if (page >= batch + 32) fetch(page);
+                const int page = W::key_tile(g, t) / kTile;
+                if (page < batch) fetch(page + C::kPages - 1);
                 const int have = min(C::kPages, n_pages - page);  // pages of this tile
                 int phys[C::kPages];
 #pragma unroll
@@ -1022,7 +1038,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 uint8_t* to = smem + SUBS * C::kQBytes + (C::kStages + (d & 1)) * C::kTileBytes;
 #pragma unroll 1
                 for (int p = 0; p < C::kPages; ++p) {
-                    const bool have = (t - g.fresh) * C::kPages + p < n_pages;
+                    const bool have = W::key_tile(g, t) / kTile + p < n_pages;
 #pragma unroll 2
                     for (int x = 0; x < 4; ++x) {  // sixteen tokens of an element; a row of 128 bytes holds two elements
                         const int piece = x * 128 + ct, r = piece >> 3, c = piece & 7, e = r * 2 + (c >> 2), ch = (c & 3) * 2;

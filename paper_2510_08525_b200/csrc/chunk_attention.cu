@@ -132,6 +132,22 @@ __device__ __forceinline__ void mma_ss8(uint32_t d, uint64_t a, uint64_t b, uint
         : "memory");
 }
 
+// Sixteen E4M3 codes as fp16.
+__device__ __forceinline__ void decode4(uint32_t codes, uint32_t& lo, uint32_t& hi)
+{
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=&r"(lo), "=&r"(hi) : "r"(codes));
+}
+__device__ __forceinline__ void decode16(const uint4& codes, uint4& lo, uint4& hi)
+{
+    decode4(codes.x, lo.x, lo.y);
+    decode4(codes.y, lo.z, lo.w);
+    decode4(codes.z, hi.x, hi.y);
+    decode4(codes.w, hi.z, hi.w);
+}
+
+// The first n bytes of a word (n below 0: none, above 4: all).
+__device__ __forceinline__ uint32_t first_bytes(int n) { return n <= 0 ? 0u : n >= 4 ? ~0u : (1u << 8 * n) - 1u; }
+
 // Four numbers to E4M3 (nearest, saturating) and back.
 __device__ __forceinline__ uint32_t codes4(float2 f, float2 g)
 {
@@ -144,9 +160,7 @@ __device__ __forceinline__ uint32_t codes4(float2 f, float2 g)
 __device__ __forceinline__ void values4(uint32_t codes, float2& f, float2& g)
 {
     uint32_t a, b;
-    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
-        : "=&r"(a), "=&r"(b)
-        : "r"(codes));
+    decode4(codes, a, b);
     f = __half22float2(*reinterpret_cast<const __half2*>(&a));
     g = __half22float2(*reinterpret_cast<const __half2*>(&b));
 }
@@ -261,10 +275,17 @@ __device__ __forceinline__ void read_columns(uint32_t addr, float (&s)[128])
         : "memory");
 }
 
-// P = 2^(s factor - base) of a row's scores, as bf16 to tensor memory, and their sums; 64 keys at a time, so that the
-// product starts on the first.
-template <int N>
-__device__ __forceinline__ void exponentials(float (&s)[N], float factor, float base, float2 (&sum)[2], uint32_t P, uint64_t* done, int lane, int)
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// P = 2^(s factor - base) of a row's scores, as bf16 (F16 and `half`: as fp16) to tensor memory, and their sums; 64 keys at a
+// time, so that the product starts on the first.
+template <bool F16, int N>
+__device__ __forceinline__ void exponentials(float (&s)[N], float factor, float base, bool half, float2 (&sum)[2], uint32_t P, uint64_t* done, int lane, int)
 {
     const float2 factor2 = make_float2(factor, factor), base2 = make_float2(-base, -base);
 #pragma unroll
@@ -275,7 +296,16 @@ __device__ __forceinline__ void exponentials(float (&s)[N], float factor, float 
             const float2 x = fma2(make_float2(s[c + i], s[c + i + 1]), factor2, base2);
             s[c + i] = ex2(x.x);
             s[c + i + 1] = ex2(x.y);
-            packed[i / 2] = bf16x2(s[c + i], s[c + i + 1]);
+            if (!F16) packed[i / 2] = bf16x2(s[c + i], s[c + i + 1]);
+        }
+        if (F16) {
+            if (half) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) packed[i] = f16x2(s[c + 2 * i], s[c + 2 * i + 1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) packed[i] = bf16x2(s[c + 2 * i], s[c + 2 * i + 1]);
+            }
         }
         tmem_st16(P + c / 2, packed);
         if (c % 64 == 32) {
@@ -288,22 +318,31 @@ __device__ __forceinline__ void exponentials(float (&s)[N], float factor, float 
 #pragma unroll
     for (int c = 0; c < N; c += 2) sum[c / 2 & 1] = add2(sum[c / 2 & 1], make_float2(s[c], s[c + 1]));
 }
-
 // The same for a quarter of 64 keys, those of warp `quarter`: P of the other keys is zero in this warp's rows.
-__device__ __forceinline__ void exponentials(float (&s)[16], float factor, float base, float2 (&sum)[2], uint32_t P, uint64_t* done, int lane, int quarter)
+template <bool F16>
+__device__ __forceinline__ void exponentials(float (&s)[16], float factor, float base, bool half, float2 (&sum)[2], uint32_t P, uint64_t* done, int lane, int quarter)
 {
     const float2 factor2 = make_float2(factor, factor), base2 = make_float2(-base, -base);
+#pragma unroll
+    for (int x = 1; x < 4; ++x)
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%1,%1,%1,%1,%1,%1,%1};" ::"r"(P + ((quarter + x) & 3) * 8), "r"(0) : "memory");
     uint32_t packed[8];
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
         const float2 x = fma2(make_float2(s[i], s[i + 1]), factor2, base2);
         s[i] = ex2(x.x);
         s[i + 1] = ex2(x.y);
-        packed[i / 2] = bf16x2(s[i], s[i + 1]);
+        if (!F16) packed[i / 2] = bf16x2(s[i], s[i + 1]);
     }
+    if (F16) {
+        if (half) {
 #pragma unroll
-    for (int x = 1; x < 4; ++x)
-        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%1,%1,%1,%1,%1,%1,%1};" ::"r"(P + ((quarter + x) & 3) * 8), "r"(0) : "memory");
+            for (int i = 0; i < 8; ++i) packed[i] = f16x2(s[2 * i], s[2 * i + 1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) packed[i] = bf16x2(s[2 * i], s[2 * i + 1]);
+        }
+    }
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(P + quarter * 8), "r"(packed[0]), "r"(packed[1]),
                  "r"(packed[2]), "r"(packed[3]), "r"(packed[4]), "r"(packed[5]), "r"(packed[6]), "r"(packed[7])
                  : "memory");
@@ -313,26 +352,6 @@ __device__ __forceinline__ void exponentials(float (&s)[16], float factor, float
     if (lane == 0) mbar_arrive(smem_u32(done));
 #pragma unroll
     for (int c = 0; c < 16; c += 2) sum[c / 2 & 1] = add2(sum[c / 2 & 1], make_float2(s[c], s[c + 1]));
-}
-
-// Two E4M3 codes in the high bytes of a word's halves, as bf16: the exponent and mantissa bits moved to their places read
-// as a bf16 number 2^-120 times the value (subnormals too); the product is exact.
-__device__ __forceinline__ uint32_t decode2(uint32_t x)
-{
-    const uint32_t y = (x & 0x80008000u) | ((x >> 4) & 0x07f007f0u), two120 = 0x7b807b80u;
-    const __nv_bfloat162 z = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&y), *reinterpret_cast<const __nv_bfloat162*>(&two120));
-    return *reinterpret_cast<const uint32_t*>(&z);
-}
-__device__ __forceinline__ void decode16(const uint4& codes, uint4& lo, uint4& hi)
-{
-    lo.x = decode2(__byte_perm(codes.x, 0, 0x1404));
-    lo.y = decode2(__byte_perm(codes.x, 0, 0x3424));
-    lo.z = decode2(__byte_perm(codes.y, 0, 0x1404));
-    lo.w = decode2(__byte_perm(codes.y, 0, 0x3424));
-    hi.x = decode2(__byte_perm(codes.z, 0, 0x1404));
-    hi.y = decode2(__byte_perm(codes.z, 0, 0x3424));
-    hi.z = decode2(__byte_perm(codes.w, 0, 0x1404));
-    hi.w = decode2(__byte_perm(codes.w, 0, 0x3424));
 }
 
 // Walks the segments of CTA `cta` in order.
@@ -398,6 +417,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
     using C = Chunk<D, SHAPE, FP8>;
     constexpr int SUBS = C::SUBS, KEYS = C::kKeys, kHalves = KEYS / 64;
     constexpr bool QUAD = C::QUAD;
+    constexpr float kLift = FP8 ? 7.f : 0.f;  // what the running maximum lies below a row's largest score: fp16 P of 2^7, 2^15 at most
     constexpr int kTileRows = QUAD ? 32 : kRows;      // query rows of a sub-tile
     constexpr int kColumnsOf = QUAD ? KEYS / 4 : KEYS;  // scores of a thread
     using W = Walk<KEYS, SUBS, kTileRows>;
@@ -614,9 +634,9 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
 #pragma unroll
                 for (int c = 0; c < kColumnsOf; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);
                 const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * factor;
-                if (top > m + 8.f) {  // (m may still be -infinity: then there is nothing to correct)
-                    const float x = m == -INFINITY ? 1.f : ex2(m - top);
-                    m = top;
+                if (top > m + 8.f + kLift) {  // (m may still be -infinity: then there is nothing to correct)
+                    const float x = m == -INFINITY ? 1.f : ex2(m + kLift - top);
+                    m = top - kLift;
                     l *= x;
                     corr *= x;
                 }
@@ -635,7 +655,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 }
                 const float base = m == -INFINITY ? 0.f : m;
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                exponentials(s, factor, base, sum, S, sh.p_full[place], lane, warp);
+                exponentials<FP8>(s, factor, base, cached, sum, S, sh.p_full[place], lane, warp);
                 l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             }
             if (!ok) break;
@@ -858,7 +878,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
         // ------------------------------------------------------------------ matrix products
         W walk(a);
         Segment g;
-        constexpr uint32_t kQK = instr_desc(kRows, KEYS, false), kPV = instr_desc(kRows, D, true), kPVt = instr_desc(kRows, D, false);
+        constexpr uint32_t kQK = instr_desc(kRows, KEYS, false), kPV = instr_desc(kRows, D, true), kPVt = instr_desc(kRows, D, false) & ~(1u << 7 | 1u << 10);  // (fp16)
         constexpr uint32_t kQK8 = instr_desc8(kRows, kTile);
         int used[2] = {0, 0};               // P tiles multiplied so far (SUBS 1: used[0])
         int base = 0, dbase = 0;            // stages and decoded tiles so far
@@ -1014,14 +1034,17 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
             base += c + n;
         }
     } else if (FP8 && warp >= kDecode) {
-        // ------------------------------------------------------------------ V codes to bf16
+        // ------------------------------------------------------------------ V codes to fp16
         W walk(a);
         Segment g;
         const int ct = (warp - kDecode) * 32 + lane;
+        // a thread's pieces, sixteen tokens of an element, lie 16 rows of 128 bytes apart, which hold two elements each; decoded, an
+        // element's 64 tokens are a row
+        const int r = ct >> 3, c = ct & 7, e = r * 2 + (c >> 2), ch = (c & 3) * 2;
+        const int piece = r * 128 + ((c ^ (r & 7)) << 4), to_lo = e * 128 + ((ch ^ (e & 7)) << 4), to_hi = e * 128 + (((ch + 1) ^ (e & 7)) << 4);
         int i = 0, d = 0;  // stages and decoded tiles so far
         bool ok = true;
         while (ok && walk.next(g)) {
-            const int n_pages = (g.u.rows + kTile - 1) / kTile;
             for (int t = g.t0; ok && t < g.t1; ++t) {
                 if (t < g.fresh) {  // rows of the chunk: nothing to decode (a stage is free when these warps have let it go, too)
                     for (int kv = 0; ok && kv < 2; ++kv, ++i) {
@@ -1038,15 +1061,22 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 uint8_t* to = smem + SUBS * C::kQBytes + (C::kStages + (d & 1)) * C::kTileBytes;
 #pragma unroll 1
                 for (int p = 0; p < C::kPages; ++p) {
-                    const bool have = W::key_tile(g, t) / kTile + p < n_pages;
-#pragma unroll 2
-                    for (int x = 0; x < 4; ++x) {  // sixteen tokens of an element; a row of 128 bytes holds two elements
-                        const int piece = x * 128 + ct, r = piece >> 3, c = piece & 7, e = r * 2 + (c >> 2), ch = (c & 3) * 2;
-                        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-                        if (have) decode16(*reinterpret_cast<const uint4*>(from + p * kPageBytes + r * 128 + ((c ^ (r & 7)) << 4)), lo, hi);
-                        uint8_t* row = to + p * (128 * 128) + e * 128;
-                        *reinterpret_cast<uint4*>(row + ((ch ^ (e & 7)) << 4)) = lo;
-                        *reinterpret_cast<uint4*>(row + (((ch + 1) ^ (e & 7)) << 4)) = hi;
+                    const int left = W::valid_rows(g, t) - p * kTile;  // tokens from here on (64 or more: the page is full)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        uint4 lo, hi, codes = make_uint4(0, 0, 0, 0);
+                        if (left > 0) codes = *reinterpret_cast<const uint4*>(from + p * kPageBytes + x * (16 * 128) + piece);
+                        if (left < kTile) {  // (0 * NaN of what lies behind the last token would be NaN)
+                            const int n = left - (c & 3) * 16;
+                            codes.x &= first_bytes(n);
+                            codes.y &= first_bytes(n - 4);
+                            codes.z &= first_bytes(n - 8);
+                            codes.w &= first_bytes(n - 12);
+                        }
+                        decode16(codes, lo, hi);
+                        uint8_t* row = to + p * (128 * 128) + x * (32 * 128);
+                        *reinterpret_cast<uint4*>(row + to_lo) = lo;
+                        *reinterpret_cast<uint4*>(row + to_hi) = hi;
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

@@ -490,14 +490,14 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
         // SUBS 1: the score product of tile n goes out before the value product of tile n - 1, so that two of the latter may be
         // outstanding: they take turns at two barriers, or a wait could take the end of the one before for its own
         auto product_done = [&](int n) {
-            return SUBS == 2 ? wait(smem_u32(&sh.pv_done[w]), n & 1, abort_flag, a.status, kChunkWaitProduct)
-                             : wait(smem_u32(&sh.pv_done[n & 1]), n >> 1 & 1, abort_flag, a.status, kChunkWaitProduct);
+            return SUBS == 2 ? wait_warp(smem_u32(&sh.pv_done[w]), n & 1, abort_flag, a.status, kChunkWaitProduct)
+                             : wait_warp(smem_u32(&sh.pv_done[n & 1]), n >> 1 & 1, abort_flag, a.status, kChunkWaitProduct);
         };
         int met = 0;
         auto meet = [&]() {  // the four softmax warps of a CTA wait for one another
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.meet));
-            return wait(smem_u32(&sh.meet), met++ & 1, abort_flag, a.status, kChunkWaitSoftmax);
+            return wait_warp(smem_u32(&sh.meet), met++ & 1, abort_flag, a.status, kChunkWaitSoftmax);
         };
         SoftmaxPlace* place_of = sh.place + warp;
         const volatile Segment& kept = place_of->g;
@@ -544,7 +544,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 float corr = 1.f;  // of O
                 if (FP8 && cached && t == max(g.t0, g.fresh)) {  // from the chunk's rows to the cache's codes
                     // (the score products of the rows have ended: this warp has seen the last one's result)
-                    ok = wait(smem_u32(&sh.q_full[w]), seg & 1, abort_flag, a.status, kChunkWaitQueries);
+                    ok = wait_warp(smem_u32(&sh.q_full[w]), seg & 1, abort_flag, a.status, kChunkWaitQueries);
                     if (!ok) break;
                     if (busy) scale = a.scale * k_scale * split_row(smem + w * C::kQBytes, row);
                     if (CAP) cap = Cap(a.softcap, scale);
@@ -553,7 +553,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&sh.q_split[w]));
                 }
-                ok = wait(smem_u32(&sh.s_full[place]), (SUBS == 2 ? total : total >> 1) & 1, abort_flag, a.status, kChunkWaitProduct);
+                ok = wait_warp(smem_u32(&sh.s_full[place]), (SUBS == 2 ? total : total >> 1) & 1, abort_flag, a.status, kChunkWaitProduct);
                 if (!ok) break;
                 ++total;
                 if (!busy) {
@@ -1100,15 +1100,15 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
 }
 
 // Adds up the pieces of the units that a boundary cuts.  Block (c - 1, 32 rows, columns): the unit that CTA c's range begins
-// inside of, if it is the first to.  A warp's lanes hold 32 rows' columns, 32 of them; its warps take COLUMNS such runs of
-// columns and of each run every 8 / COLUMNS-th piece, and meet in shared memory: all columns and few pieces at a time where units
-// are cut once or twice, one run and eight pieces where few units are cut into many.  The pieces' order is that of the keys,
-// whatever CTA ran first.
-template <int D, int SHAPE, int COLUMNS>
+// inside of, if it is the first to.  A warp's lanes hold 32 rows' columns, a run of RUN; a block's eight warps take RUNS such runs,
+// and of each run every 8 / RUNS-th piece, and meet in shared memory: all columns where units are cut once or twice, eight columns
+// and 32 pieces at a time where few units are cut into many (five drafted tokens on 8192: 49 pieces of 8 units).  The pieces'
+// order is that of the keys, whatever CTA ran first.
+template <int D, int SHAPE, int RUN, int RUNS>
 __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constant__ ChunkArgs a)
 {
-    constexpr int kPieces = 8 / COLUMNS, kRecordRows = SHAPE == 0 ? 32 : kRows;
-    __shared__ float part[8][32][33], top[8][32], sum[8][32];
+    constexpr int kPieces = 8 / RUNS, kAtOnce = 32 / RUN, kRecordRows = SHAPE == 0 ? 32 : kRows;
+    __shared__ float part[8][32][RUN + 1], top[8][32], sum[8][32];
     const int c = blockIdx.x + 1;
     const ChunkPos b = a.at[c], before = a.at[c - 1];
     if (b.tile == 0 || b.seq >= a.seqs.n || (same_unit(before, b) && before.tile > 0)) return;
@@ -1120,57 +1120,68 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
     int last = c;  // the pieces are those of CTAs c - 1 .. last
     while (last + 1 < a.ctas && same_unit(a.at[last + 1], b)) ++last;
     grid_dep_wait();
-    float o[32], mx = -INFINITY, l = 0.f;
+    float o[RUN], mx = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int x = 0; x < 32; ++x) o[x] = 0.f;
-    for (int k = c - 1 + warp / COLUMNS; k <= last; k += kPieces) {
-        const int slot = k > c - 1 || same_unit(before, b) ? 2 * k : 2 * k + 1;
-        const float* rec = a.records + (long long)slot * chunk_record_floats(D, SHAPE) + (long long)w * kRows * (D + 2);
-        const float pm = rec[D * kRecordRows + row0 + lane], pl = rec[(D + 1) * kRecordRows + row0 + lane];
-        float4 y[8];
+    for (int x = 0; x < RUN; ++x) o[x] = 0.f;
+    for (int k0 = c - 1 + warp / RUNS; k0 <= last; k0 += kPieces * kAtOnce) {
+        float pm[kAtOnce], pl[kAtOnce];
+        float4 y[kAtOnce][RUN / 4];
 #pragma unroll
-        for (int x = 0; x < 8; ++x)
-            y[x] = reinterpret_cast<const float4*>(rec)[((blockIdx.z * COLUMNS + warp % COLUMNS) * 8 + x) * kRecordRows + row0 + lane];
-        if (pm == -INFINITY) continue;  // the row sees none of the piece's keys
-        const float to = fmaxf(mx, pm), old = mx == -INFINITY ? 0.f : ex2(mx - to), f = ex2(pm - to);
-        mx = to;
-        l = l * old + pl * f;
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int k = k0 + u * kPieces;
+            pm[u] = -INFINITY;
+            if (k > last) continue;
+            const int slot = k > c - 1 || same_unit(before, b) ? 2 * k : 2 * k + 1;
+            const float* rec = a.records + (long long)slot * chunk_record_floats(D, SHAPE) + (long long)w * kRows * (D + 2);
+            pm[u] = rec[D * kRecordRows + row0 + lane];
+            pl[u] = rec[(D + 1) * kRecordRows + row0 + lane];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            o[4 * x] = o[4 * x] * old + y[x].x * f;
-            o[4 * x + 1] = o[4 * x + 1] * old + y[x].y * f;
-            o[4 * x + 2] = o[4 * x + 2] * old + y[x].z * f;
-            o[4 * x + 3] = o[4 * x + 3] * old + y[x].w * f;
+            for (int x = 0; x < RUN / 4; ++x)
+                y[u][x] = reinterpret_cast<const float4*>(rec)[((blockIdx.z * RUNS + warp % RUNS) * (RUN / 4) + x) * kRecordRows + row0 + lane];
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            if (pm[u] == -INFINITY) continue;  // the row sees none of the piece's keys
+            const float to = fmaxf(mx, pm[u]), old = mx == -INFINITY ? 0.f : ex2(mx - to), f = ex2(pm[u] - to);
+            mx = to;
+            l = l * old + pl[u] * f;
+#pragma unroll
+            for (int x = 0; x < RUN / 4; ++x) {
+                o[4 * x] = o[4 * x] * old + y[u][x].x * f;
+                o[4 * x + 1] = o[4 * x + 1] * old + y[u][x].y * f;
+                o[4 * x + 2] = o[4 * x + 2] * old + y[u][x].z * f;
+                o[4 * x + 3] = o[4 * x + 3] * old + y[u][x].w * f;
+            }
         }
     }
     top[warp][lane] = mx;
     sum[warp][lane] = l;
 #pragma unroll
-    for (int x = 0; x < 32; ++x) part[warp][lane][x] = o[x];
+    for (int x = 0; x < RUN; ++x) part[warp][lane][x] = o[x];
     __syncthreads();
-    // eight threads a row, four columns of each run
-    const int r = threadIdx.x >> 3, x0 = (threadIdx.x & 7) * 4, in_tile = (row0 + r) / a.group, i = from + in_tile;
-    if (in_tile >= tokens || i >= m) return;
+    // RUN / 4 threads a row, four columns of each run
+    const int r = threadIdx.x / (RUN / 4), x0 = threadIdx.x % (RUN / 4) * 4, in_tile = (row0 + r) / a.group, i = from + in_tile;
+    if (r >= 32 || in_tile >= tokens || i >= m) return;
     float all = -INFINITY, total = 0.f, f[kPieces];
 #pragma unroll
-    for (int k = 0; k < kPieces; ++k) all = fmaxf(all, top[k * COLUMNS][r]);
+    for (int k = 0; k < kPieces; ++k) all = fmaxf(all, top[k * RUNS][r]);
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
-        const float t = top[k * COLUMNS][r];
+        const float t = top[k * RUNS][r];
         f[k] = t == -INFINITY ? 0.f : ex2(t - all);
-        total += sum[k * COLUMNS][r] * f[k];
+        total += sum[k * RUNS][r] * f[k];
     }
     const float inv = total > 0.f ? 1.f / total : 0.f;
     const int head = a.head_of_slot[b.head] * a.group + (row0 + r) % a.group;
     const long long at_head = (long long)(start + i) * a.q_heads + head;
 #pragma unroll
-    for (int run = 0; run < COLUMNS; ++run) {
+    for (int run = 0; run < RUNS; ++run) {
         float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < kPieces; ++k)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) y[x] += part[k * COLUMNS + run][r][x0 + x] * f[k];
-        *reinterpret_cast<uint2*>(a.out + at_head * D + (blockIdx.z * COLUMNS + run) * 32 + x0) =
+            for (int x = 0; x < 4; ++x) y[x] += part[k * RUNS + run][r][x0 + x] * f[k];
+        *reinterpret_cast<uint2*>(a.out + at_head * D + (blockIdx.z * RUNS + run) * RUN + x0) =
             make_uint2(bf16x2(y[0] * inv, y[1] * inv), bf16x2(y[2] * inv, y[3] * inv));
     }
     if (a.lse && blockIdx.z == 0 && x0 == 0) a.lse[at_head] = total > 0.f ? (all + log2f(total)) * kLn2 : -INFINITY;
@@ -1187,7 +1198,7 @@ cudaError_t launch_shape(const ChunkArgs& a, const ChunkMaps& m, int pieces, cud
     if (e != cudaSuccess || pieces < 2) return e;
     const bool few = pieces <= 4;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.ctas - 1, SHAPE == 0 ? 1 : SHAPE * 4, few ? 1 : D / 32);
+    cfg.gridDim = dim3(a.ctas - 1, SHAPE == 0 ? 1 : SHAPE * 4, few ? 1 : D / 8);
     cfg.blockDim = dim3(256);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -1195,7 +1206,8 @@ cudaError_t launch_shape(const ChunkArgs& a, const ChunkMaps& m, int pieces, cud
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return few ? cudaLaunchKernelEx(&cfg, chunk_combine_kernel<D, SHAPE, D / 32>, a) : cudaLaunchKernelEx(&cfg, chunk_combine_kernel<D, SHAPE, 1>, a);
+    return few ? cudaLaunchKernelEx(&cfg, chunk_combine_kernel<D, SHAPE, 32, D / 32>, a)
+               : cudaLaunchKernelEx(&cfg, chunk_combine_kernel<D, SHAPE, 8, 1>, a);
 }
 
 template <int D, int SHAPE, bool FP8>

@@ -25,184 +25,268 @@ struct ChunkPositions {
     }
 };
 
-// The columns of a piece's two runs.
-__device__ __forceinline__ void piece_columns(const NormRotaryArgs& a, int piece, int& c0, int& c1, bool& turned)
+// A lane holds eight neighbouring elements of a row, D / 8 lanes a row; where pairs are the halves of the rotated part, the other
+// element of each pair is another lane's, and comes by a shuffle.  What a lane multiplies with -- cos, sin, the weights -- stays in
+// registers over a token's heads, whose loads are issued several at a time.  Bound by memory (8192 tokens of 32 / 8 heads of 128):
+// see the kernels.  (Sixteen elements a thread, pairs in one thread, took 117 and 151 registers and had too few loads in flight:
+// 43 us forward and 79 backward.)
+template <int D>
+struct Lane {
+    static constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // of a row, rows of a warp
+    int row, column, partner;  // row of the warp, first element, lane with the pairs' other elements
+    bool turned, inside;       // rotated at all; pairs lie inside a lane
+    float sign;                // of the other element's term in this one's
+    __device__ __forceinline__ Lane(const NormRotaryArgs& a)
+    {
+        const int lane = threadIdx.x & 31, piece = lane % kLanes, half = a.rot / 16;  // lanes of half the rotated part
+        row = lane / kLanes;
+        column = piece * 8;
+        turned = a.table && column < a.rot;
+        inside = a.interleaved;  // (the same for the whole warp, whose lanes all take part in the shuffles otherwise)
+        const bool low = piece < half;
+        partner = turned && !inside ? lane + (low ? half : -half) : lane;
+        sign = !turned ? 0.f : low ? -1.f : 1.f;
+    }
+    // cos and sin of the lane's elements, sin with the sign of the other element's term
+    __device__ __forceinline__ void angles(const NormRotaryArgs& a, int t, float (&c)[8], float (&s)[8]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            c[j] = 1.f;
+            s[j] = 0.f;
+        }
+        if (!turned) return;
+        const float* row_of = a.table + (long long)t * a.rot;
+        if (inside) {  // four pairs
+            const float4* p = reinterpret_cast<const float4*>(row_of + column);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float4 v = __ldg(p + j);
+                c[4 * j] = c[4 * j + 1] = v.x;
+                c[4 * j + 2] = c[4 * j + 3] = v.z;
+                s[4 * j] = -v.y;
+                s[4 * j + 1] = v.y;
+                s[4 * j + 2] = -v.w;
+                s[4 * j + 3] = v.w;
+            }
+        } else {  // eight
+            const float4* p = reinterpret_cast<const float4*>(row_of + (sign < 0.f ? column : column - a.rot / 2) * 2);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 v = __ldg(p + j);
+                c[2 * j] = v.x;
+                c[2 * j + 1] = v.z;
+                s[2 * j] = sign * v.y;
+                s[2 * j + 1] = sign * v.w;
+            }
+        }
+    }
+    // the other elements of the pairs of the lane's eight
+    __device__ __forceinline__ void others(const uint4& own, float (&x)[8]) const
+    {
+        if (inside) {
+            float y[8];
+            unpack8(own, y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = y[j ^ 1];
+            return;
+        }
+        uint4 p;
+        p.x = __shfl_sync(0xffffffffu, own.x, partner);
+        p.y = __shfl_sync(0xffffffffu, own.y, partner);
+        p.z = __shfl_sync(0xffffffffu, own.z, partner);
+        p.w = __shfl_sync(0xffffffffu, own.w, partner);
+        unpack8(p, x);
+    }
+};
+
+__device__ __forceinline__ float lanes_sum(float x, int lanes)
 {
-    turned = a.table && piece * kPiece < a.rot;
-    const bool halves = turned && !a.interleaved;
-    c0 = halves ? piece * 8 : piece * kPiece;
-    c1 = halves ? c0 + a.rot / 2 : c0 + 8;
+    for (int o = 1; o < lanes; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
 }
 
-// A block takes 256 / PIECES tokens and `heads` of the heads (q heads, then K heads).  A thread keeps one piece of one token:
-// its angles stay in registers over the heads, whose loads are issued four at a time.
-template <int PIECES, class Positions>
-__global__ void __launch_bounds__(256) norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, const __grid_constant__ Positions positions, const int heads)
+// A lane's way to its rows: copies to shared memory that run kAhead steps before it reads them (its own pieces only: nothing to
+// wait for but its own copies).  A step is kRows heads of a token; steps go through a warp's heads and then to its next token.
+__device__ __forceinline__ void copy16(void* dst, const void* src, bool take)
 {
-    constexpr int kTokens = 256 / PIECES, kBatch = 4, D = PIECES * kPiece;
-    const int piece = threadIdx.x % PIECES, e = blockIdx.x * kTokens + threadIdx.x / PIECES;
-    const int head0 = blockIdx.y * heads, head1 = min(a.q_heads + a.kv_heads, head0 + heads);
-    if (e >= a.n) return;
-    const int t = positions(e);
-    if (t < 0 || t >= a.positions) return;  // of no document: the token's rows stay as they are
-    int c0, c1;
-    bool turned;
-    piece_columns(a, piece, c0, c1, turned);
-    float2 f[8];
-    if (turned) load_angles(a.table, t, a.rot, piece, f);
-    for (int base = head0; base < head1; base += kBatch) {
-        uint4 b[kBatch][2];
-#pragma unroll
-        for (int x = 0; x < kBatch; ++x) {
-            const int hh = base + x;
-            if (hh < head1) {
-                const bool is_q = hh < a.q_heads;
-                const __nv_bfloat16* src = is_q ? a.q + e * a.q_stride + hh * D : a.k + e * a.k_stride + (hh - a.q_heads) * D;
-                b[x][0] = *reinterpret_cast<const uint4*>(src + c0);
-                b[x][1] = *reinterpret_cast<const uint4*>(src + c1);
-            }
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(dst))), "l"(src), "r"(take ? 16 : 0)
+                 : "memory");
+}
+__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+struct Steps {
+    int e, h;  // token and first head of the next step
+    __device__ __forceinline__ void next(int rows, int head0, int head1, int stride)
+    {
+        h += rows;
+        if (h >= head1) {
+            h = head0;
+            e += stride;
         }
+    }
+};
+
+// blockIdx.y: `heads` query heads, or KV heads; the block's warps take tokens blockIdx.x * 8 + warp and so on.
+template <int D, class Positions>
+__global__ void __launch_bounds__(256, 4) norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, const __grid_constant__ Positions positions, const int heads,
+                                                             const int q_groups)
+{
+    constexpr int kAhead = 4, kRows = Lane<D>::kRows;
+    __shared__ uint4 ring[kAhead][256];
+    const bool is_q = (int)blockIdx.y < q_groups;
+    const int of = is_q ? a.q_heads : a.kv_heads;
+    const int head0 = ((int)blockIdx.y - (is_q ? 0 : q_groups)) * heads, head1 = min(of, head0 + heads);
+    const __nv_bfloat16* rows = is_q ? a.q : a.k;
+    const long long row_stride = is_q ? a.q_stride : a.k_stride;
+    __nv_bfloat16* out = is_q ? a.q_out : a.k_out;
+    const float* weight = is_q ? a.q_weight : a.k_weight;
+    const Lane<D> lane(a);
+    const int stride = gridDim.x * 8;
+    Steps ahead{(int)(blockIdx.x * 8 + (threadIdx.x >> 5)), head0}, at = ahead;
+    auto issue = [&](int slot) {
+        const int h = ahead.h + lane.row;
+        if (ahead.e < a.n) copy16(&ring[slot][threadIdx.x], rows + ahead.e * row_stride + min(h, head1 - 1) * D + lane.column, h < head1);
+        copies_issued();
+        ahead.next(kRows, head0, head1, stride);
+    };
 #pragma unroll
-        for (int x = 0; x < kBatch; ++x) {
-            const int hh = base + x;
-            if (hh >= head1) break;
-            const bool is_q = hh < a.q_heads;
-            float x0[8], x1[8];
-            unpack8(b[x][0], x0);
-            unpack8(b[x][1], x1);
-            const float* weight = is_q ? a.q_weight : a.k_weight;
-            if (weight) {
-                const float rms = row_rsqrt<PIECES>(x0, x1, a.eps);
-                float w0[8], w1[8];
-                load8(weight + c0, w0);
-                load8(weight + c1, w1);
+    for (int i = 0; i < kAhead; ++i) issue(i);
+    float w[8], wo[8], c[8], s[8];
+    if (weight) {
+        load8(weight + lane.column, w);
+        load8(weight + (lane.partner % Lane<D>::kLanes) * 8, wo);
+    }
+    int t = -1;
+    for (int slot = 0; at.e < a.n; slot = slot + 1 == kAhead ? 0 : slot + 1) {
+        const int h = at.h + lane.row;
+        if (at.h == head0) {
+            t = positions(at.e);
+            if (t >= a.positions) t = -1;  // of no document: the token's rows stay as they are
+            if (t >= 0) {
+                lane.angles(a, t, c, s);
+                if (weight) {  // y = r (x c w + x' s w')
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    x0[j] = x0[j] * rms * w0[j];
-                    x1[j] = x1[j] * rms * w1[j];
+                    for (int j = 0; j < 8; ++j) {
+                        c[j] *= w[j];
+                        s[j] *= lane.inside ? wo[j ^ 1] : wo[j];
+                    }
                 }
             }
-            if (turned) rotate_piece(x0, x1, f, a.interleaved);
-            __nv_bfloat16* dst = is_q ? a.q_out + ((long long)e * a.q_heads + hh) * D : a.k_out + ((long long)e * a.kv_heads + hh - a.q_heads) * D;
-            *reinterpret_cast<uint4*>(dst + c0) = pack8(x0);
-            *reinterpret_cast<uint4*>(dst + c1) = pack8(x1);
         }
+        copies_landed<kAhead - 1>();
+        const uint4 x = ring[slot][threadIdx.x];
+        issue(slot);
+        if (t >= 0) {
+            float y[8], z[8], sum = 0.f;
+            unpack8(x, y);
+            lane.others(x, z);
+            float r = 1.f;
+            if (weight) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum = fmaf(y[j], y[j], sum);
+                r = rsqrtf(lanes_sum(sum, Lane<D>::kLanes) * (1.f / D) + a.eps);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = r * fmaf(z[j], s[j], y[j] * c[j]);
+            if (h < head1) *reinterpret_cast<uint4*>(out + ((long long)at.e * of + h) * D + lane.column) = pack8(y);
+        }
+        at.next(kRows, head0, head1, stride);
     }
 }
 
-// A block takes `heads` heads of one kind and every gridDim.x-th tile of tokens; a thread adds up its sixteen columns of dw
-// over all of them, and the block's sums go to `partials`, whose order the launch fixes.
-template <int PIECES>
-__global__ void __launch_bounds__(256) norm_rotary_backward_kernel(const __grid_constant__ NormRotaryArgs a, const int heads, const int q_groups)
+// The same walk.  A lane adds up its eight columns of dw over all steps, and the block's sums go to `partials`, whose order the
+// launch fixes.
+template <int D>
+__global__ void __launch_bounds__(256, 3) norm_rotary_backward_kernel(const __grid_constant__ NormRotaryArgs a, const int heads, const int q_groups)
 {
-    constexpr int kTokens = 256 / PIECES, kBatch = 2, D = PIECES * kPiece;
-    __shared__ float sums[8][D];
-    const int piece = threadIdx.x % PIECES;
+    constexpr int kAhead = 5, kRows = Lane<D>::kRows, kLanes = Lane<D>::kLanes;
+    __shared__ uint4 ring[kAhead][2][256];
     const bool is_q = (int)blockIdx.y < q_groups;
     const int of = is_q ? a.q_heads : a.kv_heads;
     const int head0 = ((int)blockIdx.y - (is_q ? 0 : q_groups)) * heads, head1 = min(of, head0 + heads);
     const __nv_bfloat16 *rows = is_q ? a.q : a.k, *grads = is_q ? a.dq_out : a.dk_out;
-    const long long stride = is_q ? a.q_stride : a.k_stride, to_stride = is_q ? a.dq_stride : a.dk_stride;
+    const long long row_stride = is_q ? a.q_stride : a.k_stride, to_stride = is_q ? a.dq_stride : a.dk_stride;
     __nv_bfloat16* to = is_q ? a.dq : a.dk;
     const float* weight = is_q ? a.q_weight : a.k_weight;
-    int c0, c1;
-    bool turned;
-    piece_columns(a, piece, c0, c1, turned);
-    float w0[8], w1[8], d0[8], d1[8];
+    const Lane<D> lane(a);
+    const int stride = gridDim.x * 8;
+    Steps ahead{(int)(blockIdx.x * 8 + (threadIdx.x >> 5)), head0}, at = ahead;
+    auto issue = [&](int slot) {
+        const int h = ahead.h + lane.row, hc = min(h, head1 - 1);
+        if (ahead.e < a.n) {
+            copy16(&ring[slot][0][threadIdx.x], grads + ((long long)ahead.e * of + hc) * D + lane.column, h < head1);
+            if (weight) copy16(&ring[slot][1][threadIdx.x], rows + ahead.e * row_stride + hc * D + lane.column, h < head1);
+        }
+        copies_issued();
+        ahead.next(kRows, head0, head1, stride);
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) issue(i);
+    float w[8], d[8], c[8], s[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        w0[j] = w1[j] = 1.f;
-        d0[j] = d1[j] = 0.f;
+        w[j] = 1.f;
+        d[j] = 0.f;
     }
-    if (weight) {
-        load8(weight + c0, w0);
-        load8(weight + c1, w1);
-    }
-    for (int tile = blockIdx.x; tile * kTokens < a.n; tile += gridDim.x) {
-        const int e = tile * kTokens + threadIdx.x / PIECES;
-        if (e >= a.n) break;
-        const int t = a.position ? __ldg(a.position + e) : e;
-        if (t < 0 || t >= a.positions) continue;
-        float2 f[8];
-        if (turned) {
-            load_angles(a.table, t, a.rot, piece, f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[j].y = -f[j].y;  // turned back
+    if (weight) load8(weight + lane.column, w);
+    int t = -1;
+    for (int slot = 0; at.e < a.n; slot = slot + 1 == kAhead ? 0 : slot + 1) {
+        const int h = at.h + lane.row;
+        if (at.h == head0) {
+            t = a.position ? __ldg(a.position + at.e) : at.e;
+            if (t >= a.positions) t = -1;
+            if (t >= 0) lane.angles(a, t, c, s);  // (turned back: sin with the other sign)
         }
-        for (int base = head0; base < head1; base += kBatch) {
-            uint4 b[kBatch][2], g[kBatch][2];
+        copies_landed<kAhead - 1>();
+        const uint4 g = ring[slot][0][threadIdx.x], x = ring[slot][1][threadIdx.x];
+        issue(slot);
+        if (t >= 0) {
+            float y[8], z[8];
+            unpack8(g, y);
+            lane.others(g, z);
 #pragma unroll
-            for (int x = 0; x < kBatch; ++x) {
-                const int h = base + x;
-                if (h < head1) {
-                    const __nv_bfloat16 *src = rows + e * stride + h * D, *grad = grads + ((long long)e * of + h) * D;
-                    g[x][0] = *reinterpret_cast<const uint4*>(grad + c0);
-                    g[x][1] = *reinterpret_cast<const uint4*>(grad + c1);
-                    if (weight) {
-                        b[x][0] = *reinterpret_cast<const uint4*>(src + c0);
-                        b[x][1] = *reinterpret_cast<const uint4*>(src + c1);
-                    }
+            for (int j = 0; j < 8; ++j) y[j] = fmaf(-s[j], z[j], y[j] * c[j]);  // h
+            if (weight) {
+                unpack8(x, z);
+                float square = 0.f, dot = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    square = fmaf(z[j], z[j], square);
+                    dot = fmaf(y[j] * w[j], z[j], dot);
+                }
+                square = lanes_sum(square, kLanes);
+                dot = lanes_sum(dot, kLanes);
+                const float r = rsqrtf(square * (1.f / D) + a.eps), back = dot * r * r * (1.f / D);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    d[j] = fmaf(y[j] * r, z[j], d[j]);
+                    y[j] = r * fmaf(-z[j], back, y[j] * w[j]);
                 }
             }
-#pragma unroll
-            for (int x = 0; x < kBatch; ++x) {
-                const int h = base + x;
-                if (h >= head1) break;
-                float h0[8], h1[8];
-                unpack8(g[x][0], h0);
-                unpack8(g[x][1], h1);
-                if (turned) rotate_piece(h0, h1, f, a.interleaved);
-                if (weight) {
-                    float x0[8], x1[8];
-                    unpack8(b[x][0], x0);
-                    unpack8(b[x][1], x1);
-                    const float rms = row_rsqrt<PIECES>(x0, x1, a.eps);
-                    float dot = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        x0[j] *= rms;
-                        x1[j] *= rms;
-                        d0[j] = fmaf(h0[j], x0[j], d0[j]);
-                        d1[j] = fmaf(h1[j], x1[j], d1[j]);
-                        h0[j] *= w0[j];
-                        h1[j] *= w1[j];
-                        dot = fmaf(h0[j], x0[j], fmaf(h1[j], x1[j], dot));
-                    }
-                    const float mean = row_sum<PIECES>(dot) * (1.f / D);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        h0[j] = rms * fmaf(-x0[j], mean, h0[j]);
-                        h1[j] = rms * fmaf(-x1[j], mean, h1[j]);
-                    }
-                }
-                __nv_bfloat16* dst = to + e * to_stride + h * D;
-                *reinterpret_cast<uint4*>(dst + c0) = pack8(h0);
-                *reinterpret_cast<uint4*>(dst + c1) = pack8(h1);
-            }
+            if (h < head1) *reinterpret_cast<uint4*>(to + at.e * to_stride + h * D + lane.column) = pack8(y);
         }
+        at.next(kRows, head0, head1, stride);
     }
     if (!a.partials) return;
-    __syncwarp();
+    grid_dep_launch();
+    float(*sums)[D] = reinterpret_cast<float(*)[D]>(ring);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int o = PIECES; o < 32; o <<= 1) {
-            d0[j] += __shfl_xor_sync(0xffffffffu, d0[j], o);
-            d1[j] += __shfl_xor_sync(0xffffffffu, d1[j], o);
-        }
-    if ((threadIdx.x & 31) < PIECES)
+        for (int o = kLanes; o < 32; o <<= 1) d[j] += __shfl_xor_sync(0xffffffffu, d[j], o);
+    __syncthreads();  // (no copy is on its way any more: each wait above leaves only those behind the last step, which copy nothing)
+    if (lane.row == 0)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            sums[threadIdx.x >> 5][c0 + j] = d0[j];
-            sums[threadIdx.x >> 5][c1 + j] = d1[j];
-        }
+        for (int j = 0; j < 8; ++j) sums[threadIdx.x >> 5][lane.column + j] = d[j];
     __syncthreads();
-    grid_dep_launch();
     if (threadIdx.x < D) {
-        float s = 0.f;
+        float all = 0.f;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) s += sums[w][threadIdx.x];
-        a.partials[((long long)blockIdx.y * gridDim.x + blockIdx.x) * D + threadIdx.x] = s;
+        for (int x = 0; x < 8; ++x) all += sums[x][threadIdx.x];
+        a.partials[((long long)blockIdx.y * gridDim.x + blockIdx.x) * D + threadIdx.x] = all;
     }
 }
 
@@ -229,16 +313,30 @@ __global__ void __launch_bounds__(256) norm_weights_kernel(const float* partials
     }
 }
 
+// How a launch is cut: as many heads to a block's walk as leave the GPU filled (they share the angles), at most `most` blocks.
+struct Cut {
+    int heads, q_groups, groups, columns;
+};
+Cut cut_heads(const NormRotaryArgs& a, int most)
+{
+    const int rows = a.head_dim == 128 ? 2 : 4, tiles = (a.n + 7) / 8;
+    Cut c;
+    auto groups = [&](int h) { return (a.q_heads + h - 1) / h + (a.kv_heads + h - 1) / h; };
+    c.heads = rows;
+    while (c.heads < 16 && ((long long)tiles * groups(2 * c.heads) >= most || groups(c.heads) > most)) c.heads *= 2;
+    c.q_groups = (a.q_heads + c.heads - 1) / c.heads;
+    c.groups = groups(c.heads);
+    c.columns = most / c.groups < tiles ? most / c.groups : tiles;
+    return c;
+}
+
 template <class Positions>
 cudaError_t launch_forward(const NormRotaryArgs& a, const Positions& positions, cudaStream_t stream)
 {
-    const int pieces = a.head_dim / kPiece, tokens = 256 / pieces, tiles = (a.n + tokens - 1) / tokens, rows = a.q_heads + a.kv_heads;
-    // as for the rotated append: enough blocks to fill the GPU first, then as many heads as share one load of the angles
-    int heads = 1;
-    while (heads < 8 && (long long)tiles * ((rows + 2 * heads - 1) / (2 * heads)) >= 148 * 8) heads *= 2;
-    const dim3 grid(tiles, (rows + heads - 1) / heads);
-    if (pieces == 8) norm_rotary_kernel<8, Positions><<<grid, 256, 0, stream>>>(a, positions, heads);
-    else norm_rotary_kernel<4, Positions><<<grid, 256, 0, stream>>>(a, positions, heads);
+    const Cut c = cut_heads(a, kMaxNormBlocks);
+    const dim3 grid(c.columns, c.groups);
+    if (a.head_dim == 128) norm_rotary_kernel<128, Positions><<<grid, 256, 0, stream>>>(a, positions, c.heads, c.q_groups);
+    else norm_rotary_kernel<64, Positions><<<grid, 256, 0, stream>>>(a, positions, c.heads, c.q_groups);
     return cudaGetLastError();
 }
 
@@ -254,16 +352,11 @@ cudaError_t launch_norm_rotary_chunks(const NormRotaryArgs& a, const ChunkSeqs& 
 cudaError_t launch_norm_rotary_backward(const NormRotaryArgs& args, cudaStream_t stream)
 {
     NormRotaryArgs a = args;
-    const int pieces = a.head_dim / kPiece, tokens = 256 / pieces, tiles = (a.n + tokens - 1) / tokens;
-    int heads = 1;
-    auto groups = [&](int h) { return (a.q_heads + h - 1) / h + (a.kv_heads + h - 1) / h; };
-    while (heads < 8 && ((long long)tiles * groups(2 * heads) >= kMaxNormBlocks || groups(heads) > kMaxNormBlocks)) heads *= 2;
-    const int q_groups = (a.q_heads + heads - 1) / heads, all = groups(heads);
-    int columns = kMaxNormBlocks / all;
-    if (columns > tiles) columns = tiles;
+    const Cut c = cut_heads(a, 148 * 3);
     if (!a.dq_weight && !a.dk_weight) a.partials = nullptr;
-    if (pieces == 8) norm_rotary_backward_kernel<8><<<dim3(columns, all), 256, 0, stream>>>(a, heads, q_groups);
-    else norm_rotary_backward_kernel<4><<<dim3(columns, all), 256, 0, stream>>>(a, heads, q_groups);
+    const dim3 grid(c.columns, c.groups);
+    if (a.head_dim == 128) norm_rotary_backward_kernel<128><<<grid, 256, 0, stream>>>(a, c.heads, c.q_groups);
+    else norm_rotary_backward_kernel<64><<<grid, 256, 0, stream>>>(a, c.heads, c.q_groups);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || !a.partials) return e;
     cudaLaunchConfig_t cfg = {};
@@ -275,7 +368,7 @@ cudaError_t launch_norm_rotary_backward(const NormRotaryArgs& args, cudaStream_t
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, norm_weights_kernel, (const float*)a.partials, columns * q_groups, columns * (all - q_groups), a.head_dim, a.dq_weight, a.dk_weight);
+    return cudaLaunchKernelEx(&cfg, norm_weights_kernel, (const float*)a.partials, c.columns * c.q_groups, c.columns * (c.groups - c.q_groups), a.head_dim, a.dq_weight, a.dk_weight);
 }
 
 }  // namespace rlkv

@@ -12,7 +12,12 @@ namespace {
 
 constexpr int kMaxChunkTokens = 1 << 24;  // of one call
 constexpr int kMinChunkTiles = 4;         // key tiles of a CTA's range, at least
-constexpr int kUnitTiles = 1;             // what a unit's queries and results count as, in key tiles
+
+// What a unit's start and end -- its queries' way to shared memory, the first product, its results -- count as in key tiles.  Measured
+// over counts from 1 to 14: 32 rows a unit, 16 bits: 48 single tokens on 3400 each 58 us with 3, 52 with 6, 54 with 10, four drafted
+// tokens of 32 sequences 130, 131 and 135; 8 bits, whose tiles take half as long: 75, 65 and 59 us, 122, 114 and 108; 128 rows: 512
+// tokens beside 47 single ones 105 us with 1, 97 with 4; two times 128 rows: a prompt of 8192 tokens 668 us with 1, 483 with 3.
+int unit_tiles(int shape, bool fp8) { return shape == 2 ? 3 : shape == 1 ? 4 : fp8 ? 10 : 5; }
 
 // The sequences of a call: open slots, none twice, `counts` tokens each, from `first` on (null: behind those held).  `to`:
 // most tokens a sequence may come to; more are `over`.
@@ -125,21 +130,23 @@ int plan_chunks(ChunkArgs& a, int shape, int max_ctas, int min_tiles, int extra)
     return most;
 }
 
-// The shape of a launch: 32 rows where every chunk's queries of a KV head fit them, two sub-tiles of 128 where most key tiles
-// belong to chunks that fill both, else one.
-int choose_shape(const ChunkArgs& a)
+// The shape of a launch.  32 rows where every chunk's queries of a KV head fit them.  Two sub-tiles of 128 where most key tiles
+// belong to chunks that fill more than one, and the launch gives every SM 16 such tiles of 128 keys and more: 64 tokens of each of
+// 32 sequences on 8064 take 303 us so and 360 with one sub-tile, a prompt of 8192 tokens 483 and 550; 300 tokens alone 30 and 21,
+// three times 100 on 500 32 and 25, 512 beside 47 single tokens 140 and 97.
+int choose_shape(const ChunkArgs& a, int sms)
 {
-    long long small = 0, large = 0;
+    const long long ring = a.sink + a.window;
+    long long small = 0, large = 0;  // key rows times row tiles of 128
     bool few = true;
     for (int i = 0; i < a.seqs.n; ++i) {
         const int m = a.seqs.start[i + 1] - a.seqs.start[i];
         if (m > chunk_tokens(0, a.group)) few = false;
-        const long long rows = (long long)a.n_full * (a.seqs.len[i] + m) + (long long)a.n_comp * (a.sink + a.window + 128);
+        const long long rows = (long long)a.n_full * (a.seqs.len[i] + m / 2) + (long long)a.n_comp * ring;
         const int tiles = (int)(((long long)m * a.group + 127) / 128);
-        if (tiles > 1) large += rows * tiles;
-        else if (tiles == 1) small += rows;
+        (tiles > 1 ? large : small) += rows * tiles;
     }
-    return few ? 0 : large > small ? 2 : 1;
+    return few ? 0 : large > small && large / 256 >= 16ll * sms ? 2 : 1;
 }
 
 }  // namespace
@@ -240,12 +247,12 @@ int rlkv_paged_chunk_attention(rlkv_paged* p, int layer, const int* slots, const
         a.k_scale[h] = p->fp8 ? p->k_scale[(size_t)layer * p->kv_heads + h] : 1.f;
         a.v_scale[h] = p->fp8 ? p->v_scale[(size_t)layer * p->kv_heads + h] : 1.f;
     }
-    const int shape = choose_shape(a);
     const int sms = p->sm_count < kMaxChunkCtas / 2 ? p->sm_count : kMaxChunkCtas / 2;
+    const int shape = choose_shape(a, sms);
     const long long room = (long long)(p->chunk_bytes / (2 * sizeof(float) * chunk_record_floats(p->head_dim, shape)));  // CTAs it has records for
     int ctas = shape == 2 ? sms : 2 * sms;
     if (ctas > room) ctas = room < 1 ? 1 : (int)room;
-    const int pieces = plan_chunks(a, shape, ctas, kMinChunkTiles, kUnitTiles);
+    const int pieces = plan_chunks(a, shape, ctas, kMinChunkTiles, unit_tiles(shape, p->fp8));
     const int keys = chunk_keys(shape);
     ChunkMaps m;
     int e = encode_heads_map(&m.q, q, total, p->q_heads, p->head_dim, q_stride, a.group, (shape == 0 ? 32 : 128) / a.group);
@@ -372,9 +379,9 @@ int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full,
     a.group = group;
     a.sink = sink;
     a.window = window;
-    if (shape < 0) shape = choose_shape(a);
+    if (shape < 0) shape = choose_shape(a, kMaxChunkCtas / 2);
     if (shape > 2) return RLKV_EINVAL;
-    plan_chunks(a, shape, max_ctas, kMinChunkTiles, kUnitTiles);
+    plan_chunks(a, shape, max_ctas, kMinChunkTiles, unit_tiles(shape, false));
     for (int c = 0; c <= a.ctas; ++c) {
         at_out[4 * c] = a.at[c].seq;
         at_out[4 * c + 1] = a.at[c].row_tile;

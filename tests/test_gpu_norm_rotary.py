@@ -194,8 +194,8 @@ def test_in_place_and_captured(hz, rl, cuda_device):
     (2, 8, 64, "10", 4, 60, 64, False, False, "qk"), (4, 28, 128, "1001", 16, 112, 128, False, False, "qk"),
     (4, 28, 128, "0110", 16, 112, 64, False, True, "qk"), (3, 24, 128, "010", 4, 60, 128, True, True, "k"), (1, 1, 128, "0", 0, 5, 128, True, False, "q")])
 def test_normed_prefill_and_append(hz, rl, cuda_device, Hkv, Hq, D, mask, S, W, rot, interleaved, fp8, norms):
-    """The rotated calls with norms set: q_out and k_out against the formula, cache bytes against the plain append of k_out (16 bits),
-    or as codes of the exact rows within half a step (8 bits)."""
+    """The rotated calls with norms set: q_out and k_out against the formula; a prompt's cache bytes against the plain append of k_out
+    (16 bits), and every row read back against the formula, rounded to bf16, or to a code."""
     dev, lens = cuda_device, [70, 1, 300]
     scale = ([0.01 + 0.003 * h for h in range(Hkv)], [0.02 + 0.001 * h for h in range(Hkv)]) if fp8 else (None, None)
     cache, plain = (hz.PagedCache(1, Hkv, Hq, D, 3, 12, 400, [int(c) for c in mask], S, W, device=dev, k_scale=scale[0], v_scale=scale[1])
@@ -206,39 +206,44 @@ def test_normed_prefill_and_append(hz, rl, cuda_device, Hkv, Hq, D, mask, S, W, 
     cache.set_norms(qw, kw, EPS)
     w = [None if x is None else x[0] for x in (qw, kw)]
     a, b = [cache.open_seq() for _ in lens], [plain.open_seq() for _ in lens]
-    exact = []
+    exact, size = [], []
     for s, t, n in zip(a, b, lens):
         x = rand_bf16((n, Hq + 2 * Hkv, D), n).to(dev)
         q, k, v = x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
         q_out, k_out = cache.prefill_rotated(0, s, q, k, v)
         check_forward(q_out, q, w[0], np.arange(n), rot, interleaved)
         check_forward(k_out, k, w[1], np.arange(n), rot, interleaved)
-        exact.append(forward64(k, w[1], np.arange(n), rot, interleaved)[0])
+        want = forward64(k, w[1], np.arange(n), rot, interleaved)
+        exact.append(want[0])
+        size.append(want[1])
         plain.prefill(0, t, k_out, v.contiguous())
+    if not fp8:
+        for s, t in zip(a, b):
+            same_state(cache, plain, s, t)
     for step in range(3):
         x = rand_bf16((3, Hq + 2 * Hkv, D), 1000 + step).to(dev)
         q, k, v = x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
         pos = np.array(lens) + step
         other_q, other_k = cache.rotate_chunks(0, a, [1, 1, 1], q, k)     # the same rotation, before it is appended
-        q_out = cache.append_rotated(0, a, q, k, v)
-        assert torch.equal(q_out, other_q)
-        check_forward(q_out, q, w[0], pos, rot, interleaved)
-        want = forward64(k, w[1], pos, rot, interleaved)[0]
-        exact = [torch.cat([old, want[i:i + 1]]) for i, old in enumerate(exact)]
-        plain.append(0, b, other_k, v.contiguous())
-    if not fp8:
-        for s, t in zip(a, b):
-            same_state(cache, plain, s, t)
-        return
+        check_forward(other_q, q, w[0], pos, rot, interleaved)
+        check_forward(other_k, k, w[1], pos, rot, interleaved)
+        check_forward(cache.append_rotated(0, a, q, k, v), q, w[0], pos, rot, interleaved)
+        want = forward64(k, w[1], pos, rot, interleaved)
+        exact, size = ([torch.cat([old, y[i:i + 1]]) for i, old in enumerate(kept)] for kept, y in ((exact, want[0]), (size, want[1])))
     k, _ = cache.read(0, a, [0, 0, 0], [n + 3 for n in lens])
-    for got, want, n in zip(k.cpu().split([n + 3 for n in lens]), exact, lens):
+    for got, want, pairs, n in zip(k.cpu().split([n + 3 for n in lens]), exact, size, lens):
         t = torch.arange(n + 3)
         for h in range(Hkv):
             held = (t < S) | (t >= n + 3 - W) if mask[h] == "0" else t >= 0
-            s = scale[0][h]
-            x = want[held, h].clamp(-448 * s, 448 * s)  # (codes saturate there)
-            # half a step of E4M3 (2^-4 of the value, 2^-10 below its normal range), what fp32 is off by, and bf16 when read back
-            assert bool(((got[held, h].double() - x).abs() <= (2.0 ** -4 + 2.0 ** -7) * x.abs() + 2.0 ** -10 * s).all())
+            x = want[held, h]
+            if fp8:
+                s = scale[0][h]
+                x = x.clamp(-448 * s, 448 * s)  # (codes saturate there)
+                # half a step of E4M3 (2^-4 of the value, 2^-10 below its normal range), what fp32 is off by, and bf16 when read back
+                bound = (2.0 ** -4 + 2.0 ** -7) * x.abs() + 2.0 ** -10 * s
+            else:
+                bound = 2.0 ** -8 * x.abs() + 2.0 ** -20 * (pairs[held, h] + x.abs()) + 2.0 ** -133
+            assert bool(((got[held, h].double() - x).abs() <= bound).all())
 
 
 def test_norms_with_attention_and_its_gradients(hz, cuda_device):

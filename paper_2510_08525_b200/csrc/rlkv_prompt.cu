@@ -152,6 +152,7 @@ int rlkv_prompt_create(rlkv_prompt** out, int layers, int kv_heads, int q_heads,
     if (e == cudaSuccess && biased) e = cudaMemcpy(p->dev_base + p->off_slopes, slopes, count * sizeof(float), cudaMemcpyHostToDevice);
     if (e == cudaSuccess) e = prepare_prompt_kernels(head_dim);
     if (e == cudaSuccess) e = prepare_prompt_backward(head_dim);
+    if (e == cudaSuccess) e = prepare_norm_backward();
     if (e == cudaSuccess) e = cudaDeviceSynchronize();  // the memset is done before a call on any stream
     if (e != cudaSuccess) {
         cudaFree(mem);

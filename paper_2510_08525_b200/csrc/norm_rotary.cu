@@ -30,93 +30,96 @@ using tc::add2;
 using tc::fma2;
 using tc::mul2;
 
-// Eight elements as four pairs, for the instructions that take two fp32 numbers at a time.
+// Eight numbers as four pairs, for the instructions that take two fp32 numbers at a time.
 struct Eight {
     float2 p[4];
 };
-__device__ __forceinline__ Eight unpack(const uint4& x)
-{
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    Eight e;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) e.p[j] = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
-    return e;
-}
-__device__ __forceinline__ uint4 pack(const Eight& e)
-{
-    return make_uint4(tc::bf16x2(e.p[0].x, e.p[0].y), tc::bf16x2(e.p[1].x, e.p[1].y), tc::bf16x2(e.p[2].x, e.p[2].y), tc::bf16x2(e.p[3].x, e.p[3].y));
-}
 
-// A lane holds eight neighbouring elements of a row, D / 8 lanes a row; where pairs are the halves of the rotated part, the other
-// element of each pair is another lane's, and comes by a shuffle.  What a lane multiplies with -- cos, sin, the weights -- stays in
-// registers over a token's heads.
+// A lane holds sixteen elements of a row, the eight pairs that it turns: u the first elements of the pairs, v the second; D / 16 lanes
+// a row.  Two runs of eight in memory, which are u and v where pairs are the halves of the rotated part, and whose even and odd
+// elements are u and v where pairs are neighbours (or where nothing is rotated).
 //
 // Bound by memory at large sizes, and next to it by the instructions a row takes, so that both kernels count them: pairs of fp32
-// operations, running pointers, and copies to shared memory that go out several steps ahead in place of loads whose registers
-// wait.  8192 tokens of 32 / 8 heads of 128: sixteen elements a thread, loads four heads at a time, took 43 us forward and 79
-// backward (117 and 151 registers: too few loads in flight); this form with single operations and addresses computed for every row 42
-// and 68 (72 % of the issue slots).
+// operations, both elements of a pair in one lane, running pointers, and copies to shared memory that go out while the token before
+// is worked on in place of loads whose registers wait.  8192 tokens of 32 / 8 heads of 128: loads of four heads at a time took 43 us
+// forward and 79 backward (117 and 151 registers: too few loads in flight); eight elements a lane, the pairs' others by shuffles, 36
+// and 65 (250 and then 190 instructions for 512 bytes; half of the issue slots).
 template <int D>
 struct Lane {
-    static constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // of a row, rows of a warp
-    int row, column, partner;  // row of the warp, first element, lane with the pairs' other elements
-    bool turned, inside;       // rotated at all; pairs lie inside a lane
-    float sign;                // of the other element's term in this one's
+    static constexpr int kLanes = D / 16, kRows = 32 / kLanes;  // of a row, rows of a warp
+    int row, piece, first, second;  // row of the warp, piece of the row, where its runs begin
+    bool turned, halves;
     __device__ __forceinline__ Lane(const NormRotaryArgs& a)
     {
-        const int lane = threadIdx.x & 31, piece = lane % kLanes, half = a.rot / 16;  // lanes of half the rotated part
+        const int lane = threadIdx.x & 31;
         row = lane / kLanes;
-        column = piece * 8;
-        turned = a.table && column < a.rot;
-        inside = a.interleaved;  // (the same for the whole warp, whose lanes all take part in the shuffles otherwise)
-        const bool low = piece < half;
-        partner = turned && !inside ? lane + (low ? half : -half) : lane;
-        sign = !turned ? 0.f : low ? -1.f : 1.f;
+        piece = lane % kLanes;
+        turned = a.table && piece * kPiece < a.rot;
+        halves = turned && !a.interleaved;
+        first = halves ? piece * 8 : piece * kPiece;
+        second = halves ? first + a.rot / 2 : first + 8;
     }
-    // cos and sin of the lane's elements, sin with the sign of the other element's term, from the token's row of the table
-    __device__ __forceinline__ void angles(const float* row_of, int rot, Eight& c, Eight& s) const
+    __device__ __forceinline__ void unpack(const uint4& x, const uint4& y, Eight& u, Eight& v) const
     {
+        const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        auto lo = [&](int i) { return __uint_as_float(w[i] << 16); };
+        auto hi = [&](int i) { return __uint_as_float(w[i] & 0xffff0000u); };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u.p[i] = halves ? make_float2(lo(i), hi(i)) : make_float2(lo(2 * i), lo(2 * i + 1));
+            v.p[i] = halves ? make_float2(lo(4 + i), hi(4 + i)) : make_float2(hi(2 * i), hi(2 * i + 1));
+        }
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16* row_at, const Eight& u, const Eight& v) const
+    {
+        uint32_t w[8];
+        if (halves) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = tc::bf16x2(u.p[i].x, u.p[i].y);
+                w[4 + i] = tc::bf16x2(v.p[i].x, v.p[i].y);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[2 * i] = tc::bf16x2(u.p[i].x, v.p[i].x);
+                w[2 * i + 1] = tc::bf16x2(u.p[i].y, v.p[i].y);
+            }
+        }
+        *reinterpret_cast<uint4*>(row_at + first) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(row_at + second) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+    // A row of fp32 numbers (a norm's weights) in the lane's order, and back.
+    __device__ __forceinline__ void load(const float* from, Eight& u, Eight& v) const
+    {
+        float x[8], y[8];
+        load8(from + first, x);
+        load8(from + second, y);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u.p[i] = halves ? make_float2(x[2 * i], x[2 * i + 1]) : i < 2 ? make_float2(x[4 * i], x[4 * i + 2]) : make_float2(y[4 * i - 8], y[4 * i - 6]);
+            v.p[i] = halves ? make_float2(y[2 * i], y[2 * i + 1]) : i < 2 ? make_float2(x[4 * i + 1], x[4 * i + 3]) : make_float2(y[4 * i - 7], y[4 * i - 5]);
+        }
+    }
+    __device__ __forceinline__ void store(float* to, const Eight& u, const Eight& v) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float* at = to + (i < 2 ? first + 4 * i : second + 4 * i - 8);  // (neighbours)
+            *reinterpret_cast<float2*>(halves ? to + first + 2 * i : at) = halves ? u.p[i] : make_float2(u.p[i].x, v.p[i].x);
+            *reinterpret_cast<float2*>(halves ? to + second + 2 * i : at + 2) = halves ? v.p[i] : make_float2(u.p[i].y, v.p[i].y);
+        }
+    }
+    // cos and sin of the lane's pairs, from the token's row of the table
+    __device__ __forceinline__ void angles(const float* row_of, Eight& c, Eight& s) const
+    {
+        const float4* p = reinterpret_cast<const float4*>(row_of + piece * kPiece);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            c.p[j] = make_float2(1.f, 1.f);
-            s.p[j] = make_float2(0.f, 0.f);
+            const float4 x = turned ? p[j] : make_float4(1.f, 0.f, 1.f, 0.f);
+            c.p[j] = make_float2(x.x, x.z);
+            s.p[j] = make_float2(x.y, x.w);
         }
-        if (!turned) return;
-        if (inside) {  // four pairs
-            const float4* p = reinterpret_cast<const float4*>(row_of + column);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float4 v = p[j];
-                c.p[2 * j] = make_float2(v.x, v.x);
-                c.p[2 * j + 1] = make_float2(v.z, v.z);
-                s.p[2 * j] = make_float2(-v.y, v.y);
-                s.p[2 * j + 1] = make_float2(-v.w, v.w);
-            }
-        } else {  // eight
-            const float4* p = reinterpret_cast<const float4*>(row_of + (sign < 0.f ? column : column - rot / 2) * 2);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 v = p[j];
-                c.p[j] = make_float2(v.x, v.z);
-                s.p[j] = make_float2(sign * v.y, sign * v.w);
-            }
-        }
-    }
-    // the other elements of the pairs of the lane's eight
-    __device__ __forceinline__ Eight others(const uint4& own, const Eight& mine) const
-    {
-        if (inside) {
-            Eight e;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) e.p[j] = make_float2(mine.p[j].y, mine.p[j].x);
-            return e;
-        }
-        uint4 p;
-        p.x = __shfl_sync(0xffffffffu, own.x, partner);
-        p.y = __shfl_sync(0xffffffffu, own.y, partner);
-        p.z = __shfl_sync(0xffffffffu, own.z, partner);
-        p.w = __shfl_sync(0xffffffffu, own.w, partner);
-        return unpack(p);
     }
 };
 
@@ -140,18 +143,18 @@ __device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_
 template <int LEFT>
 __device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// What a warp keeps of the two tokens it has copies on the way for: STEPS times kRows heads of ROWS tensors, a piece to each lane,
+// What a warp keeps of the two tokens it has copies on the way for: STEPS times kRows heads of ROWS tensors, a piece of two runs to each lane,
 // and the token's row of the table.
 template <int STEPS, int ROWS>
 struct Ring {
-    uint4 piece[2][STEPS][ROWS][256];
+    uint4 piece[2][STEPS][ROWS][2][256];
     float angles[2][8][128];
 };
 
 // blockIdx.y: STEPS * kRows query heads, or KV heads; the block's warps take tokens blockIdx.x * 8 + warp and so on.  A token's rows
 // and angles are copied while those of the token before are worked on.
 template <int D, int STEPS, class Positions>
-__global__ void __launch_bounds__(256, 3) norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, const __grid_constant__ Positions positions, const int q_groups)
+__global__ void __launch_bounds__(256, 2) norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, const __grid_constant__ Positions positions, const int q_groups)
 {
     constexpr int kRows = Lane<D>::kRows;
     extern __shared__ __align__(16) unsigned char memory[];
@@ -163,8 +166,8 @@ __global__ void __launch_bounds__(256, 3) norm_rotary_kernel(const __grid_consta
     const float* weight = is_q ? a.q_weight : a.k_weight;
     const long long row_stride = is_q ? a.q_stride : a.k_stride;
     int e = blockIdx.x * 8 + warp;
-    const __nv_bfloat16* src = (is_q ? a.q : a.k) + e * row_stride + lane.column;
-    __nv_bfloat16* dst = (is_q ? a.q_out : a.k_out) + ((long long)e * of + head0) * D + lane.column;
+    const __nv_bfloat16* src = (is_q ? a.q : a.k) + e * row_stride;
+    __nv_bfloat16* dst = (is_q ? a.q_out : a.k_out) + ((long long)e * of + head0) * D;
     auto place = [&](int token) {  // (-1: of no document, the token's rows stay as they are)
         const int t = token < a.n ? positions(token) : -1;
         return t < a.positions ? t : -1;
@@ -174,7 +177,9 @@ __global__ void __launch_bounds__(256, 3) norm_rotary_kernel(const __grid_consta
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
                 const int h = head0 + i * kRows;
-                copy16(&ring.piece[buffer][i][0][threadIdx.x], src + (h < of ? h : 0) * D, h < of);
+                const __nv_bfloat16* at = src + (h < of ? h : 0) * D;
+                copy16(&ring.piece[buffer][i][0][0][threadIdx.x], at + lane.first, h < of);
+                copy16(&ring.piece[buffer][i][0][1][threadIdx.x], at + lane.second, h < of);
             }
             if (a.table && t >= 0 && (threadIdx.x & 31) * 4 < a.rot)
                 copy16(&ring.angles[buffer][warp][(threadIdx.x & 31) * 4], a.table + (long long)t * a.rot + (threadIdx.x & 31) * 4, true);
@@ -185,40 +190,38 @@ __global__ void __launch_bounds__(256, 3) norm_rotary_kernel(const __grid_consta
     int t = place(e), after = place(e + stride), then = place(e + 2 * stride);
     issue(0, e, t);
     issue(1, e + stride, after);
-    float w[8], wo[8];
-    if (weight) {
-        load8(weight + lane.column, w);
-        load8(weight + (lane.partner % Lane<D>::kLanes) * 8, wo);
-    }
+    Eight wu, wv;
+    if (weight) lane.load(weight, wu, wv);
     for (int buffer = 0; e < a.n; e += stride, buffer ^= 1) {
         copies_landed<1>();
         __syncwarp();
         const int further = place(e + 3 * stride);
         if (t >= 0) {
             Eight c, s;
-            lane.angles(ring.angles[buffer][warp], a.rot, c, s);
-            if (weight) {  // y = r (x c w + x' s w')
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    c.p[j] = mul2(c.p[j], make_float2(w[2 * j], w[2 * j + 1]));
-                    s.p[j] = mul2(s.p[j], lane.inside ? make_float2(wo[2 * j + 1], wo[2 * j]) : make_float2(wo[2 * j], wo[2 * j + 1]));
-                }
-            }
+            lane.angles(ring.angles[buffer][warp], c, s);
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
-                const uint4 x = ring.piece[buffer][i][0][threadIdx.x];
-                Eight y = unpack(x);
-                const Eight z = lane.others(x, y);
-                float2 r = make_float2(1.f, 1.f);
+                Eight u, v;
+                lane.unpack(ring.piece[buffer][i][0][0][threadIdx.x], ring.piece[buffer][i][0][1][threadIdx.x], u, v);
                 if (weight) {
-                    float2 sum = mul2(y.p[0], y.p[0]);
+                    float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-                    for (int j = 1; j < 4; ++j) sum = fma2(y.p[j], y.p[j], sum);
-                    r.x = r.y = rsqrtf(lanes_sum<Lane<D>::kLanes>(sum) * (1.f / D) + a.eps);
+                    for (int j = 0; j < 4; ++j) sum = fma2(v.p[j], v.p[j], fma2(u.p[j], u.p[j], sum));
+                    const float x = rsqrtf(lanes_sum<Lane<D>::kLanes>(sum) * (1.f / D) + a.eps);
+                    const float2 r = make_float2(x, x);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        u.p[j] = mul2(mul2(u.p[j], r), wu.p[j]);
+                        v.p[j] = mul2(mul2(v.p[j], r), wv.p[j]);
+                    }
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y.p[j] = mul2(r, fma2(z.p[j], s.p[j], mul2(y.p[j], c.p[j])));
-                if (head0 + i * kRows < of) *reinterpret_cast<uint4*>(dst + i * kRows * D) = pack(y);
+                for (int j = 0; j < 4; ++j) {
+                    const float2 x = u.p[j], minus = make_float2(-v.p[j].x, -v.p[j].y);
+                    u.p[j] = fma2(x, c.p[j], mul2(minus, s.p[j]));
+                    v.p[j] = fma2(v.p[j], c.p[j], mul2(x, s.p[j]));
+                }
+                if (head0 + i * kRows < of) lane.store(dst + i * kRows * D, u, v);
             }
         }
         __syncwarp();  // every lane has read the angles
@@ -233,7 +236,7 @@ __global__ void __launch_bounds__(256, 3) norm_rotary_kernel(const __grid_consta
 // The same walk.  A lane adds up its eight columns of dw over all steps, and the block's sums go to `partials`, whose order the
 // launch fixes.
 template <int D, int STEPS>
-__global__ void __launch_bounds__(256, 3) norm_rotary_backward_kernel(const __grid_constant__ NormRotaryArgs a, const int q_groups)
+__global__ void __launch_bounds__(256, 2) norm_rotary_backward_kernel(const __grid_constant__ NormRotaryArgs a, const int q_groups)
 {
     constexpr int kRows = Lane<D>::kRows, kLanes = Lane<D>::kLanes;
     extern __shared__ __align__(16) unsigned char memory[];
@@ -245,9 +248,9 @@ __global__ void __launch_bounds__(256, 3) norm_rotary_backward_kernel(const __gr
     const float* weight = is_q ? a.q_weight : a.k_weight;
     const long long row_stride = is_q ? a.q_stride : a.k_stride, to_stride = is_q ? a.dq_stride : a.dk_stride;
     int e = blockIdx.x * 8 + warp;
-    const __nv_bfloat16* src = (is_q ? a.q : a.k) + e * row_stride + lane.column;
-    const __nv_bfloat16* grad = (is_q ? a.dq_out : a.dk_out) + (long long)e * of * D + lane.column;
-    __nv_bfloat16* dst = (is_q ? a.dq : a.dk) + e * to_stride + head0 * D + lane.column;
+    const __nv_bfloat16* src = (is_q ? a.q : a.k) + e * row_stride;
+    const __nv_bfloat16* grad = (is_q ? a.dq_out : a.dk_out) + (long long)e * of * D;
+    __nv_bfloat16* dst = (is_q ? a.dq : a.dk) + e * to_stride + head0 * D;
     auto place = [&](int token) {
         const int t = token >= a.n ? -1 : a.position ? __ldg(a.position + token) : token;
         return t < a.positions ? t : -1;
@@ -257,8 +260,12 @@ __global__ void __launch_bounds__(256, 3) norm_rotary_backward_kernel(const __gr
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
                 const int h = head0 + i * kRows, at = (h < of ? h : 0) * D;
-                copy16(&ring.piece[buffer][i][0][threadIdx.x], grad + at, h < of);
-                if (weight) copy16(&ring.piece[buffer][i][1][threadIdx.x], src + at, h < of);
+                copy16(&ring.piece[buffer][i][0][0][threadIdx.x], grad + at + lane.first, h < of);
+                copy16(&ring.piece[buffer][i][0][1][threadIdx.x], grad + at + lane.second, h < of);
+                if (weight) {
+                    copy16(&ring.piece[buffer][i][1][0][threadIdx.x], src + at + lane.first, h < of);
+                    copy16(&ring.piece[buffer][i][1][1][threadIdx.x], src + at + lane.second, h < of);
+                }
             }
             if (a.table && t >= 0 && (threadIdx.x & 31) * 4 < a.rot)
                 copy16(&ring.angles[buffer][warp][(threadIdx.x & 31) * 4], a.table + (long long)t * a.rot + (threadIdx.x & 31) * 4, true);
@@ -270,54 +277,49 @@ __global__ void __launch_bounds__(256, 3) norm_rotary_backward_kernel(const __gr
     int t = place(e), after = place(e + stride), then = place(e + 2 * stride);
     issue(0, e, t);
     issue(1, e + stride, after);
-    Eight w, d;
+    Eight wu, wv, du, dv;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        w.p[j] = make_float2(1.f, 1.f);
-        d.p[j] = make_float2(0.f, 0.f);
-    }
-    if (weight) {
-        float x[8];
-        load8(weight + lane.column, x);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w.p[j] = make_float2(x[2 * j], x[2 * j + 1]);
-    }
+    for (int j = 0; j < 4; ++j) du.p[j] = dv.p[j] = make_float2(0.f, 0.f);
+    if (weight) lane.load(weight, wu, wv);
     for (int buffer = 0; e < a.n; e += stride, buffer ^= 1) {
         copies_landed<1>();
         __syncwarp();
         const int further = place(e + 3 * stride);
         if (t >= 0) {
             Eight c, s;
-            lane.angles(ring.angles[buffer][warp], a.rot, c, s);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s.p[j] = make_float2(-s.p[j].x, -s.p[j].y);  // turned back
+            lane.angles(ring.angles[buffer][warp], c, s);
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
-                const uint4 g = ring.piece[buffer][i][0][threadIdx.x], x = ring.piece[buffer][i][1][threadIdx.x];
-                Eight h = unpack(g);
-                {
-                    const Eight o = lane.others(g, h);
+                Eight u, v;  // h, the gradient turned back
+                lane.unpack(ring.piece[buffer][i][0][0][threadIdx.x], ring.piece[buffer][i][0][1][threadIdx.x], u, v);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) h.p[j] = fma2(s.p[j], o.p[j], mul2(h.p[j], c.p[j]));
+                for (int j = 0; j < 4; ++j) {
+                    const float2 x = u.p[j], minus = make_float2(-x.x, -x.y);
+                    u.p[j] = fma2(x, c.p[j], mul2(v.p[j], s.p[j]));
+                    v.p[j] = fma2(v.p[j], c.p[j], mul2(minus, s.p[j]));
                 }
                 if (weight) {
-                    const Eight z = unpack(x);
-                    Eight hw;
+                    Eight xu, xv;
+                    lane.unpack(ring.piece[buffer][i][1][0][threadIdx.x], ring.piece[buffer][i][1][1][threadIdx.x], xu, xv);
                     float2 square = make_float2(0.f, 0.f), dot = square;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        hw.p[j] = mul2(h.p[j], w.p[j]);
-                        square = fma2(z.p[j], z.p[j], square);
-                        dot = fma2(hw.p[j], z.p[j], dot);
+                        square = fma2(xv.p[j], xv.p[j], fma2(xu.p[j], xu.p[j], square));
+                        dot = fma2(mul2(v.p[j], wv.p[j]), xv.p[j], fma2(mul2(u.p[j], wu.p[j]), xu.p[j], dot));
                     }
-                    const float r = rsqrtf(lanes_sum<kLanes>(square) * (1.f / D) + a.eps), back = -lanes_sum<kLanes>(dot) * r * r * (1.f / D);
+                    const float x = rsqrtf(lanes_sum<kLanes>(square) * (1.f / D) + a.eps), y = -lanes_sum<kLanes>(dot) * x * x * (1.f / D);
+                    const float2 r = make_float2(x, x), back = make_float2(y, y);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        d.p[j] = fma2(mul2(h.p[j], make_float2(r, r)), z.p[j], d.p[j]);
-                        h.p[j] = mul2(make_float2(r, r), fma2(z.p[j], make_float2(back, back), hw.p[j]));
+                        u.p[j] = mul2(u.p[j], r);
+                        v.p[j] = mul2(v.p[j], r);
+                        du.p[j] = fma2(u.p[j], xu.p[j], du.p[j]);
+                        dv.p[j] = fma2(v.p[j], xv.p[j], dv.p[j]);
+                        u.p[j] = fma2(mul2(xu.p[j], back), r, mul2(u.p[j], wu.p[j]));
+                        v.p[j] = fma2(mul2(xv.p[j], back), r, mul2(v.p[j], wv.p[j]));
                     }
                 }
-                if (head0 + i * kRows < of) *reinterpret_cast<uint4*>(dst + i * kRows * D) = pack(h);
+                if (head0 + i * kRows < of) lane.store(dst + i * kRows * D, u, v);
             }
         }
         __syncwarp();
@@ -333,12 +335,12 @@ __global__ void __launch_bounds__(256, 3) norm_rotary_backward_kernel(const __gr
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int o = kLanes; o < 32; o <<= 1)
-            d.p[j] = add2(d.p[j], make_float2(__shfl_xor_sync(0xffffffffu, d.p[j].x, o), __shfl_xor_sync(0xffffffffu, d.p[j].y, o)));
+        for (int o = kLanes; o < 32; o <<= 1) {
+            du.p[j] = add2(du.p[j], make_float2(__shfl_xor_sync(0xffffffffu, du.p[j].x, o), __shfl_xor_sync(0xffffffffu, du.p[j].y, o)));
+            dv.p[j] = add2(dv.p[j], make_float2(__shfl_xor_sync(0xffffffffu, dv.p[j].x, o), __shfl_xor_sync(0xffffffffu, dv.p[j].y, o)));
+        }
     __syncthreads();  // (no copy is on its way any more: those behind the last token copy nothing)
-    if (lane.row == 0)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) *reinterpret_cast<float2*>(&sums[warp][lane.column + 2 * j]) = d.p[j];
+    if (lane.row == 0) lane.store(sums[warp], du, dv);
     __syncthreads();
     if (threadIdx.x < D) {
         float all = 0.f;
@@ -371,17 +373,17 @@ __global__ void __launch_bounds__(256) norm_weights_kernel(const float* partials
     }
 }
 
-// How a launch is cut: four steps of heads to a token where that leaves the GPU filled (they share the angles and what a token
-// costs beside its rows), else one; at most three blocks on every SM.
+// How a launch is cut: two steps of heads to a token where that leaves the GPU filled (they share the angles and what a token
+// costs beside its rows), else one; at most two blocks on every SM.
 struct Cut {
     int steps, q_groups, groups, columns;
 };
 Cut cut_heads(const NormRotaryArgs& a)
 {
-    const int rows = a.head_dim == 128 ? 2 : 4, tiles = (a.n + 7) / 8, most = 148 * 3;
+    const int rows = a.head_dim == 128 ? 4 : 8, tiles = (a.n + 7) / 8, most = 148 * 2;
     Cut c;
     auto groups = [&](int heads) { return (a.q_heads + heads - 1) / heads + (a.kv_heads + heads - 1) / heads; };
-    c.steps = (long long)tiles * groups(4 * rows) >= most || groups(rows) > most ? 4 : 1;
+    c.steps = (long long)tiles * groups(2 * rows) >= most || groups(rows) > most ? 2 : 1;
     c.q_groups = (a.q_heads + c.steps * rows - 1) / (c.steps * rows);
     c.groups = groups(c.steps * rows);
     c.columns = most / c.groups < tiles ? most / c.groups : tiles;
@@ -399,8 +401,8 @@ template <class Positions>
 cudaError_t launch_forward(const NormRotaryArgs& a, const Positions& positions, cudaStream_t stream)
 {
     const Cut c = cut_heads(a);
-    if (a.head_dim == 128) return c.steps == 4 ? launch_forward_steps<128, 4>(a, positions, c, stream) : launch_forward_steps<128, 1>(a, positions, c, stream);
-    return c.steps == 4 ? launch_forward_steps<64, 4>(a, positions, c, stream) : launch_forward_steps<64, 1>(a, positions, c, stream);
+    if (a.head_dim == 128) return c.steps == 2 ? launch_forward_steps<128, 2>(a, positions, c, stream) : launch_forward_steps<128, 1>(a, positions, c, stream);
+    return c.steps == 2 ? launch_forward_steps<64, 2>(a, positions, c, stream) : launch_forward_steps<64, 1>(a, positions, c, stream);
 }
 
 template <int D, int STEPS>
@@ -424,8 +426,8 @@ cudaError_t launch_norm_rotary_backward(const NormRotaryArgs& args, cudaStream_t
     NormRotaryArgs a = args;
     const Cut c = cut_heads(a);
     if (!a.dq_weight && !a.dk_weight) a.partials = nullptr;
-    cudaError_t e = a.head_dim == 128 ? (c.steps == 4 ? launch_backward_steps<128, 4>(a, c, stream) : launch_backward_steps<128, 1>(a, c, stream))
-                                      : (c.steps == 4 ? launch_backward_steps<64, 4>(a, c, stream) : launch_backward_steps<64, 1>(a, c, stream));
+    cudaError_t e = a.head_dim == 128 ? (c.steps == 2 ? launch_backward_steps<128, 2>(a, c, stream) : launch_backward_steps<128, 1>(a, c, stream))
+                                      : (c.steps == 2 ? launch_backward_steps<64, 2>(a, c, stream) : launch_backward_steps<64, 1>(a, c, stream));
     if (e != cudaSuccess || !a.partials) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(a.head_dim / 8, 2);
@@ -441,8 +443,8 @@ cudaError_t launch_norm_rotary_backward(const NormRotaryArgs& args, cudaStream_t
 
 cudaError_t prepare_norm_backward()
 {
-    cudaError_t e = cudaFuncSetAttribute(norm_rotary_backward_kernel<128, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Ring<4, 2>));
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_rotary_backward_kernel<64, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Ring<4, 2>));
+    cudaError_t e = cudaFuncSetAttribute(norm_rotary_backward_kernel<128, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Ring<2, 2>));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_rotary_backward_kernel<64, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Ring<2, 2>));
     return e;
 }
 

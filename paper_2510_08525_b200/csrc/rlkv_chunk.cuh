@@ -165,7 +165,7 @@ struct NormRotaryArgs {
     float* partials;                     // [kMaxNormBlocks][head_dim]
     float *dq_weight, *dk_weight;
 };
-constexpr int kMaxNormBlocks = 148 * 3;
+constexpr int kMaxNormBlocks = 148 * 2;
 cudaError_t launch_norm_rotary(const NormRotaryArgs& a, cudaStream_t stream);
 cudaError_t launch_norm_rotary_chunks(const NormRotaryArgs& a, const ChunkSeqs& seqs, cudaStream_t stream);
 cudaError_t launch_norm_rotary_backward(const NormRotaryArgs& a, cudaStream_t stream);

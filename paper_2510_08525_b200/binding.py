@@ -467,14 +467,21 @@ def rlkv_paged_destroy(cache) -> None:
     _check(lib.rlkv_paged_destroy(cache))
 
 
+_seq_open, _seq_close, _byref = lib.rlkv_paged_seq_open, lib.rlkv_paged_seq_close, ctypes.byref
+
+
 def rlkv_paged_seq_open(cache) -> int:
     slot = _ci(-1)
-    _check(lib.rlkv_paged_seq_open(cache, ctypes.byref(slot)))
-    return int(slot.value)
+    rc = _seq_open(cache, _byref(slot))
+    if rc:
+        _check(rc)
+    return slot.value
 
 
 def rlkv_paged_seq_close(cache, slot) -> None:
-    _check(lib.rlkv_paged_seq_close(cache, slot))
+    rc = _seq_close(cache, slot)
+    if rc:
+        _check(rc)
 
 
 def rlkv_paged_append(cache, layer, slots, k, v, stream=None) -> None:

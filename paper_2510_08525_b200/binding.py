@@ -610,10 +610,13 @@ def rlkv_paged_set_norms(cache, q_weight, k_weight, eps=1e-6) -> None:
 
 def _chunks(slots, counts, *more):
     """The host arrays of a call on chunks, as int32, and the tokens of all of them."""
-    arrays = [np.ascontiguousarray(x, dtype=np.int32).reshape(-1) for x in (slots, *more, counts)]
-    if any(x.size != arrays[0].size for x in arrays):
-        raise ValueError("slots and counts must have an entry for each sequence")
-    return arrays, int(arrays[-1].sum())
+    arrays = []
+    for x in (slots, *more, counts):
+        x = np.ascontiguousarray(x, dtype=np.int32)
+        arrays.append(x if x.ndim == 1 else x.reshape(-1))
+        if x.size != arrays[0].size:
+            raise ValueError("slots and counts must have an entry for each sequence")
+    return arrays, sum(arrays[-1].tolist())
 
 
 def _width(handle, heads, of):

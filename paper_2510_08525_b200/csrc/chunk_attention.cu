@@ -473,10 +473,10 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
     const uint32_t q_smem = smem_u32(smem), ring = q_smem + SUBS * C::kQBytes, decoded = ring + C::kStages * C::kTileBytes;
     const uint32_t o_column = SUBS == 2 ? 256 : 128;
     // Registers of the warpgroups, which together have what the block was launched with.  16 bits: 384 x 168 = 256 x 224 + 128 x 56,
-    // 256 x 128 = 128 x 184 + 128 x 72; 8 bits: 512 x 128 = 256 x 200 + 128 x 72 + 128 x 40, 384 x 80 = 128 x (128 + 72 + 40)
-    if (warp < C::kSoftmaxWarps) more_registers<SUBS == 2 ? (FP8 ? 200 : 224) : FP8 ? 128 : 184>();
+    // 256 x 128 = 128 x 184 + 128 x 72; 8 bits: 512 x 128 = 256 x 208 + 128 x 56 + 128 x 40, 384 x 80 = 128 x (128 + 72 + 40)
+    if (warp < C::kSoftmaxWarps) more_registers<SUBS == 2 ? (FP8 ? 208 : 224) : FP8 ? 128 : 184>();
     else if (warp >= kDecode) fewer_registers<40>();
-    else fewer_registers<SUBS == 2 && !FP8 ? 56 : 72>();
+    else fewer_registers<SUBS == 2 ? 56 : 72>();
     if (warp < C::kSoftmaxWarps) {
         // ------------------------------------------------------------------ softmax
         const int w = warp >> 2, row = (warp & 3) * 32 + lane;

@@ -1196,7 +1196,7 @@ cudaError_t launch_shape(const ChunkArgs& a, const ChunkMaps& m, int pieces, cud
     kernel<<<a.ctas, C::kThreads, C::kSmem, stream>>>(a, m);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || pieces < 2) return e;
-    const bool few = pieces <= 4;
+    const bool few = pieces <= (SHAPE == 0 ? 4 : 16);  // (128 rows of a unit are four times the blocks: 512 tokens on 3400, five pieces, 54 -> 36 us)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(a.ctas - 1, SHAPE == 0 ? 1 : SHAPE * 4, few ? 1 : D / 8);
     cfg.blockDim = dim3(256);

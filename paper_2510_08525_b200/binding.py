@@ -157,13 +157,14 @@ def _stream(s, of=None, x=None) -> int:
     """A stream's handle.  None: the current stream of the call's GPU, so that the calls on one cache go to one stream -- that of
     `of`, a Handle or a tensor in device memory, else that of the tensor x, else the current device."""
     if s is None:
-        if isinstance(of, Handle) and of.device is not None:
-            device = of.device
-        else:
+        device = of.device if type(of) is Handle else None
+        if device is None:
             device = _gpu_of(of)
             if device is None:
                 device = _gpu_of(x)
-        import torch
+        torch = sys.modules.get("torch")
+        if torch is None:
+            import torch
         if device is None:
             device = torch.cuda.current_device()
         # the raw handle: building the Stream object takes several microseconds, as long as a small call
@@ -500,7 +501,7 @@ def _on_device(x) -> bool:
 def _shape_of(handle, x):
     """q_heads, kv_heads, head_dim and GPU that a call's tensors are held to: the handle's; of an address alone no heads are known
     (0), and the GPU is that of the tensor x (None where x is an address too)."""
-    if isinstance(handle, Handle):
+    if type(handle) is Handle:
         return handle.q_heads, handle.kv_heads, handle.head_dim, handle.device
     return 0, 0, 0, _gpu_of(x)
 
@@ -531,11 +532,17 @@ def _rows(x, least=1, heads=0, head_dim=0, gpu=None):
     return x.data_ptr(), token
 
 
+_dtypes = {}  # torch's, by name (the library is loaded before torch is, if ever)
+
+
 def _room(x, least, dtype="bfloat16", gpu=None):
     """Address of a contiguous tensor in device memory of `least` elements or more of that type; or the address itself."""
     if x is None or isinstance(x, int):
         return x or 0
-    if not getattr(x, "is_cuda", False) or x.dtype is not getattr(sys.modules["torch"], dtype) or x.numel() < least:
+    wanted = _dtypes.get(dtype)
+    if wanted is None:
+        wanted = _dtypes[dtype] = getattr(sys.modules["torch"], dtype)
+    if not getattr(x, "is_cuda", False) or x.dtype is not wanted or x.numel() < least:
         raise RlkvError(RLKV_EINVAL, f"a tensor in device memory of {least} {dtype} elements is wanted")
     if gpu is not None and x.get_device() != gpu:
         raise ValueError(f"a tensor in the memory of GPU {gpu} is wanted")
@@ -621,7 +628,7 @@ def _chunks(slots, counts, *more):
 
 def _width(handle, heads, of):
     """Elements of a token's rows: the handle's, or those of a tensor."""
-    if isinstance(handle, Handle):
+    if type(handle) is Handle:
         return getattr(handle, heads) * handle.head_dim
     return 0 if of is None or isinstance(of, int) else of.shape[1] * of.shape[2]
 

@@ -38,7 +38,7 @@
 // Measured on one B200 (us on the GPU; 32 / 8 heads of 128, 6 of 8 full, unless said otherwise): five drafted tokens on 8192 14.5
 // (latency of one wave and of the join); four of each of 32 sequences of 8064 on average, 16 bits 129 (819 MB: 6.3 TB/s), 8 bits 106
 // (410 MB: the products, the decoding and the softmax of a tile share an SM's shared memory and issue slots); 2048 on 8192, all
-// full, 265 in bursts (1.17 PFLOP/s, 69 % of a large library product's burst rate), 8 bits 395.
+// full, 265 in bursts (1.17 PFLOP/s, 69 % of a large library product's burst rate), 8 bits 383 (one product per 128 keys; 395 with one per page).
 #include <cuda_fp16.h>
 
 #include "rlkv_chunk.cuh"
@@ -127,7 +127,7 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
     return ok != 0;
 }
 
-// An 8-bit page: 128 rows of 128 bytes from row `row` on, 128-byte swizzle.
+// An 8-bit page, or its K or its V codes: rows of 128 bytes from row `row` on, as many as the map's box has, 128-byte swizzle.
 __device__ __forceinline__ void load_page(uint32_t dst, const CUtensorMap* map, int row, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(0),
@@ -862,7 +862,13 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
 #pragma unroll
                         for (int p = 0; p < C::kPages; ++p) {
                             if (p >= have) break;
-                            if constexpr (FP8) {
+                            if constexpr (FP8 && SUBS == 2) {  // the pages' K codes behind one another, then their V codes
+                                const long long index = g.full ? a.page0_8 + (long long)g.index * a.n_pages + phys[p]
+                                                               : a.ring0_8 + ((long long)g.slot * a.n_comp + g.index) * a.ring_tiles + page + p;
+                                for (int v = 0; v < 2; ++v)
+                                    load_page(ring + slot * C::kTileBytes + (2 * v + p) * (kPageBytes / 2), &maps.pool, (int)(index * 128) + v * 64,
+                                              smem_u32(&sh.full[slot]));
+                            } else if constexpr (FP8) {
                                 const long long index = g.full ? a.page0_8 + (long long)g.index * a.n_pages + phys[p]
                                                                : a.ring0_8 + ((long long)g.slot * a.n_comp + g.index) * a.ring_tiles + page + p;
                                 load_page(ring + slot * C::kTileBytes + p * kPageBytes, &maps.pool, (int)(index * 128), smem_u32(&sh.full[slot]));
@@ -893,7 +899,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
         W walk(a);
         Segment g;
         constexpr uint32_t kQK = instr_desc(kRows, KEYS, false), kPV = instr_desc(kRows, D, true), kPVt = instr_desc(kRows, D, false) & ~(1u << 7 | 1u << 10);  // (fp16)
-        constexpr uint32_t kQK8 = instr_desc8(kRows, kTile);
+        constexpr uint32_t kQK8 = instr_desc8(kRows, KEYS);
         int used[2] = {0, 0};               // P tiles multiplied so far (SUBS 1: used[0])
         int base = 0, dbase = 0;            // stages and decoded tiles so far
         int segs[2] = {0, 0}, split[2] = {0, 0};  // segments of each sub-tile, those whose queries were split
@@ -937,10 +943,8 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 if (FP8 && j >= c) {
                     if (elect_one()) {
 #pragma unroll
-                        for (int p = 0; p < C::kPages; ++p)
-#pragma unroll
-                            for (int x = 0; x < 8; ++x)  // the queries' first and second parts
-                                mma_ss8(to + p * kTile, q + ((x / 4 * kQBlock + x % 4 * 32) >> 4), k + ((p * kPageBytes + x % 4 * 32) >> 4), kQK8, x > 0);
+                        for (int x = 0; x < 8; ++x)  // the queries' first and second parts
+                            mma_ss8(to, q + ((x / 4 * kQBlock + x % 4 * 32) >> 4), k + (x % 4 * 32 >> 4), kQK8, x > 0);
                         commit(smem_u32(&sh.s_full[place]));
                     }
                 } else if (elect_one()) {
@@ -1071,7 +1075,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 ok = wait_warp(smem_u32(&sh.full[slot]), i / C::kStages & 1, abort_flag, a.status, kChunkWaitLoad) &&
                      wait_warp(smem_u32(&sh.decoded_empty[d & 1]), (d >> 1 & 1) ^ 1, abort_flag, a.status, kChunkWaitDecoded);
                 if (!ok) break;
-                const uint8_t* from = smem + SUBS * C::kQBytes + slot * C::kTileBytes + kTile * 128;
+                const uint8_t* from = smem + SUBS * C::kQBytes + slot * C::kTileBytes + C::kPages * (kPageBytes / 2);
                 uint8_t* to = smem + SUBS * C::kQBytes + (C::kStages + (d & 1)) * C::kTileBytes;
 #pragma unroll 1
                 for (int p = 0; p < C::kPages; ++p) {
@@ -1079,7 +1083,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         uint4 lo, hi, codes = make_uint4(0, 0, 0, 0);
-                        if (left > 0) codes = *reinterpret_cast<const uint4*>(from + p * kPageBytes + x * (16 * 128) + piece);
+                        if (left > 0) codes = *reinterpret_cast<const uint4*>(from + p * (kPageBytes / 2) + x * (16 * 128) + piece);
                         if (left < kTile) {  // (0 * NaN of what lies behind the last token would be NaN)
                             const int n = left - (c & 3) * 16;
                             codes.x &= first_bytes(n);

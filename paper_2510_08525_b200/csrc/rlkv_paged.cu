@@ -306,6 +306,7 @@ static int paged_create(rlkv_paged** out, int layers, int kv_heads, int q_heads,
     if (rc) return fail(rc);
     if (fp8 && p->pages8 > 0) {
         rc = encode_byte_rows_tensor_map(&p->map_k, p->dev_base + p->off_pool8, 128, p->pages8 * 128, 2 * kTile);
+        if (!rc) rc = encode_byte_rows_tensor_map(&p->map_codes, p->dev_base + p->off_pool8, 128, p->pages8 * 128, kTile);
         if (rc) return fail(rc);
     }
     // The records of attention on chunks have memory of their own, which the buffer does not count; where there is none left they

@@ -20,6 +20,7 @@ struct rlkv_paged {
     long long pages8;                      // pages of the 8-bit pool
     size_t off_pool8, off_scales;
     CUtensorMap map_k;  // the 8-bit pool as rows of 128 bytes, one page per box
+    CUtensorMap map_codes;  // and the K or the V codes of a page per box
     long long pool_rows;
     std::vector<uint8_t> is_full;
     std::vector<int> slot_of_head, head_of_slot;  // [layers*kv_heads]

@@ -259,7 +259,7 @@ int rlkv_paged_chunk_attention(rlkv_paged* p, int layer, const int* slots, const
     if (!e) e = encode_heads_map(&m.k, k, total, p->kv_heads, p->head_dim, k_stride, 1, keys);
     if (!e) e = encode_heads_map(&m.v, v, total, p->kv_heads, p->head_dim, v_stride, 1, keys);
     if (!e && !p->fp8) e = encode_heads_map(&m.pool, dev_at<__nv_bfloat16>(p, p->off_pool), p->pool_rows, 1, p->head_dim, p->head_dim, 1, kTile);
-    else if (!e) m.pool = p->map_k;
+    else if (!e) m.pool = shape == 2 ? p->map_codes : p->map_k;
     if (e) return e;
     RLKV_CUDA(launch_chunk_attention(a, m, p->head_dim, shape, pieces, static_cast<cudaStream_t>(stream)));
     p->launches += pieces > 1 ? 2 : 1;

@@ -150,6 +150,39 @@ def test_attention(hz, cuda_device, Hkv, Hq, D, mask, S, W, lens, counts, cap, b
     assert [cache.length(0, s) for s in slots] == lens
 
 
+LARGE = [
+    # two tiles of rows at a time (see the plan), the last of them alone, one page in the last tile, rows that end inside a tile
+    (2, 8, 32, 128, "11111111", 16, 112, [2500], [1500], 0, False, False),
+    (2, 8, 32, 128, "11011011", 16, 112, [3000, 17, 640], [900, 4, 333], 50.0, True, False),
+    (2, 8, 32, 128, "11011011", 16, 112, [3000, 17, 640], [900, 4, 333], 0, True, True),
+    (2, 4, 28, 128, "1101", 16, 112, [4000, 100, 0], [700, 129, 1500], 0, False, False),
+    (2, 4, 28, 128, "1101", 16, 112, [4033, 64, 0], [700, 129, 1500], 20.0, False, True),
+    (2, 4, 16, 64, "1111", 4, 60, [5000, 63], [1031, 800], 20.0, True, False),
+    (2, 8, 32, 128, "00000000", 16, 1000, [2000], [2999], 0, False, True),
+    (2, 8, 32, 128, "01000010", 40, 2000, [1990, 0], [1500, 700], 0, True, False),
+    # many ranges in one unit, for each way of joining them
+    (1, 1, 8, 128, "1", 16, 112, [30000], [17], 0, False, False),
+    (1, 1, 8, 128, "1", 16, 112, [30001], [33], 50.0, False, True),
+    (1, 2, 14, 64, "11", 16, 112, [12000], [40], 0, False, False),
+    (0, 1, 8, 128, "1", 16, 112, [30000], [4], 0, False, False),
+    (0, 1, 7, 128, "1", 16, 112, [29999], [3], 0, False, True),
+]
+
+
+@pytest.mark.parametrize("shape,Hkv,Hq,D,mask,S,W,lens,counts,cap,biased,fp8", LARGE)
+def test_attention_of_large_calls(hz, rl, cuda_device, shape, Hkv, Hq, D, mask, S, W, lens, counts, cap, biased, fp8):
+    plan = lambda shape: rl.rlkv_debug_chunk_plan(lens, counts, mask.count("1"), mask.count("0"), Hq // Hkv, S, W, shape)  # noqa: E731
+    np.testing.assert_array_equal(plan(-1), plan(shape))
+    cache, slots, rows, slopes, q, k, v = build(hz, cuda_device, Hkv, Hq, D, mask, S, W, lens, counts, cap, biased, fp8)
+    out, lse = cache.attend_chunks(0, slots, counts, q, k, v)
+    assert cache.status() == 0
+    starts = np.cumsum([0] + counts)
+    for i, (a, b) in enumerate(zip(starts, starts[1:])):
+        compare(out[a:b], lse[a:b], reference(q[a:b], rows[i:i + 1], (k[a:b], v[a:b]), lens[i:i + 1], counts[i:i + 1], mask, S, W, cap, slopes, fp8))
+    again, lse2 = cache.attend_chunks(0, slots, counts, q.contiguous(), k.contiguous(), v.contiguous())
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
 def test_many_sequences(hz, cuda_device):
     lens = [(i * 37) % 400 for i in range(200)]
     counts = [1 + (i * 7) % 5 if i % 9 else 0 for i in range(200)]

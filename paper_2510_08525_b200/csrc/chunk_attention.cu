@@ -40,6 +40,7 @@
 // (410 MB: the products, the decoding and the softmax of a tile share an SM's shared memory and issue slots); 2048 on 8192, all
 // full, 265 in bursts (1.17 PFLOP/s, 69 % of a large library product's burst rate), 8 bits 383 (one product per 128 keys; 395 with one per page).
 #include <cuda_fp16.h>
+#include <float.h>
 
 #include "rlkv_chunk.cuh"
 #include "rlkv_prompt.cuh"
@@ -643,7 +644,8 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
 #pragma unroll
                     for (int c = 0; c < kColumnsOf; ++c) s[c] = see[c / 32] >> (c & 31) & 1 ? s[c] : -INFINITY;
                 }
-                const float factor = CAP || BIAS ? 1.f : scale * kLog2e;
+                // (a row of zeros on an 8-bit cache has next to no scale; times -infinity it must not be 0)
+                const float factor = CAP || BIAS ? 1.f : FP8 ? fmaxf(scale * kLog2e, FLT_MIN) : scale * kLog2e;
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int c = 0; c < kColumnsOf; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);

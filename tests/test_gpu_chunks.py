@@ -242,6 +242,20 @@ def test_rows_do_not_depend_on_lse_or_order(hz, rl, cuda_device):
     compare(got, got_lse, reference(turned[0], [rows[i] for i in (2, 0, 1)], turned[1:], [1200, 500, 65], [1, 9, 40], "10", 16, 112, 0, None, False))
 
 
+@pytest.mark.parametrize("counts", [[3, 2], [150, 3]])
+@pytest.mark.parametrize("k_scale", [1e-12, 1e-36])
+def test_queries_of_zeros_over_tiny_codes(hz, cuda_device, counts, k_scale):
+    """An 8-bit cache whose scale times the queries' own leaves fp32: a query of zeros weighs every key that it sees the same."""
+    dev, Hkv, Hq, D, lens = cuda_device, 2, 8, 128, [70, 20]
+    cache = hz.PagedCache(1, Hkv, Hq, D, 2, 8, 256, [1, 0], 16, 112, device=dev, k_scale=[k_scale] * 2, v_scale=scales(Hkv, True)[1])
+    slots, rows = fill(cache, lens, Hkv, D, 3, dev)
+    x = rand_bf16((sum(counts), Hq + 2 * Hkv, D), 4).to(dev)
+    q = torch.zeros_like(x[:, :Hq].contiguous())
+    out, lse = cache.attend_chunks(0, slots, counts, q, x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:])
+    assert cache.status() == 0
+    compare(out, lse, reference(q, rows, (x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]), lens, counts, "10", 16, 112, 0, None, True))
+
+
 WRITES = [
     # Hkv, D, mask, sink, window, fp8, lengths, then counts call by call
     (2, 64, "10", 4, 60, False, [[1, 63, 64, 65, 0], [64, 1, 0, 200, 3], [130, 130, 130, 1, 1]]),

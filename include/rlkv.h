@@ -440,7 +440,7 @@ int rlkv_debug_paged_cut(const int* lens, int n, int n_full, int n_comp, int cap
  * lens[i] tokens and counts[i] new ones, n_full full and n_comp compressed heads of `group` query heads.  The work is a flat
  * sequence of key tiles: sequence by sequence, tile of queries by tile, the full heads and then the compressed ones.  shape 0: the
  * queries of 32 / group tokens and 64 keys to a tile, 1: 128 / group and 64, 2: 2 * (128 / group) and 128; -1: as the call would
- * choose.  CTA c takes the tiles from
+ * choose on a 16-bit cache of head_dim 128, -2: on an 8-bit one.  CTA c takes the tiles from
  * at_out[4c..4c+3] = (sequence, query tile, head, key tile) up to at_out[4c+4..4c+7], c < *ctas_out; the last entry names
  * sequence n (host int[4 * (max_ctas + 1)]). */
 int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full, int n_comp, int group, int sink, int window,

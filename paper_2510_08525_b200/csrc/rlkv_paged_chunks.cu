@@ -130,14 +130,17 @@ int plan_chunks(ChunkArgs& a, int shape, int max_ctas, int min_tiles, int extra)
     return most;
 }
 
-// The shape of a launch.  32 rows where every chunk's queries of a KV head fit them.  Two sub-tiles of 128 where most key tiles
-// belong to chunks that fill more than one, and the launch gives every SM 16 such tiles of 128 keys and more: 64 tokens of each of
-// 32 sequences on 8064 take 303 us so and 360 with one sub-tile, a prompt of 8192 tokens 483 and 550; 300 tokens alone 30 and 21,
-// three times 100 on 500 32 and 25, 512 beside 47 single tokens 140 and 97.
-int choose_shape(const ChunkArgs& a, int sms)
+// The shape of a launch.  32 rows where every chunk's queries of a KV head fit them.  Two sub-tiles of 128 are for launches most of whose
+// key tiles belong to chunks that fill more than one: on an 8-bit cache for all of these, since a tile's codes are decoded once for
+// both (us with one sub-tile and so: a prompt of 8192 tokens 877 and 651, 512 tokens on 3400 65 and 57, three times 100 on 500 31
+// and 30), in 16 bits where the K and V rows are too many for the L2, in which the other tiles of rows would find them (four times
+// 512 on 8192 300 and 270, 64 of each of 32 sequences on 8064 341 and 272) and every SM has 32 such tiles of 128 keys (64 tokens on 40000 62 and 65), or where it has 100 (2048 on 8192 280 and 282,
+// under the power cap 320 and 315, a prompt of 8192 497 and 490); but 512 on 8192 78 and 81, four times 512 on 3400 111 and 117.
+constexpr long long kNearL2 = 80ll << 20;
+int choose_shape(const ChunkArgs& a, int sms, int head_dim, bool fp8)
 {
     const long long ring = a.sink + a.window;
-    long long small = 0, large = 0;  // key rows times row tiles of 128
+    long long small = 0, large = 0, shared = 0;  // key rows times row tiles of 128; rows that several of these read
     bool few = true;
     for (int i = 0; i < a.seqs.n; ++i) {
         const int m = a.seqs.start[i + 1] - a.seqs.start[i];
@@ -145,8 +148,11 @@ int choose_shape(const ChunkArgs& a, int sms)
         const long long rows = (long long)a.n_full * (a.seqs.len[i] + m / 2) + (long long)a.n_comp * ring;
         const int tiles = (int)(((long long)m * a.group + 127) / 128);
         (tiles > 1 ? large : small) += rows * tiles;
+        if (tiles > 1) shared += rows;
     }
-    return few ? 0 : large > small && large / 256 >= 16ll * sms ? 2 : 1;
+    if (few) return 0;
+    if (large <= small) return 1;
+    return fp8 || large / 256 >= (shared * head_dim * 4 > kNearL2 ? 32ll : 100ll) * sms ? 2 : 1;
 }
 
 }  // namespace
@@ -248,7 +254,7 @@ int rlkv_paged_chunk_attention(rlkv_paged* p, int layer, const int* slots, const
         a.v_scale[h] = p->fp8 ? p->v_scale[(size_t)layer * p->kv_heads + h] : 1.f;
     }
     const int sms = p->sm_count < kMaxChunkCtas / 2 ? p->sm_count : kMaxChunkCtas / 2;
-    const int shape = choose_shape(a, sms);
+    const int shape = choose_shape(a, sms, p->head_dim, p->fp8);
     const long long room = (long long)(p->chunk_bytes / (2 * sizeof(float) * chunk_record_floats(p->head_dim, shape)));  // CTAs it has records for
     int ctas = shape == 2 ? sms : 2 * sms;
     if (ctas > room) ctas = room < 1 ? 1 : (int)room;
@@ -379,7 +385,7 @@ int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full,
     a.group = group;
     a.sink = sink;
     a.window = window;
-    if (shape < 0) shape = choose_shape(a, kMaxChunkCtas / 2);
+    if (shape < 0) shape = choose_shape(a, kMaxChunkCtas / 2, 128, shape == -2);
     if (shape > 2) return RLKV_EINVAL;
     plan_chunks(a, shape, max_ctas, kMinChunkTiles, unit_tiles(shape, false));
     for (int c = 0; c <= a.ctas; ++c) {

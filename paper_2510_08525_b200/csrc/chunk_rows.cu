@@ -69,8 +69,10 @@ __device__ __forceinline__ void transpose4(uint32_t (&w)[4])
     w[3] = __byte_perm(c, d, 0x7632);
 }
 
-// Measured (us on the GPU; 8 heads of 128, 4 full): 24 requests of 843 tokens on average into an 8-bit cache 17.2 with V codes stored
-// byte by byte; 16384 tokens of one request (6 full) in 16 bits 19.9 with one row at a time.
+// Bound by memory where the rows are many, else by the launch.  A thread's loads all go out before its first store, and V codes are
+// turned four tokens by four elements in registers.  Measured (us on the GPU; 8 heads of 128, 4 full): 24 requests of 843 tokens on
+// average into an 8-bit cache 15.9 (10.9 at a copy's rate; with V codes stored byte by byte 17.2); 16384 tokens of one request (6 full)
+// in 16 bits 12.7 (101 MB, some of which stay in the L2; with one row at a time 19.9).
 template <int D, bool FP8>
 __global__ void __launch_bounds__(256) write_chunks_kernel(const __grid_constant__ ChunkRowsArgs a, const __grid_constant__ ChunkPages pages)
 {
@@ -200,7 +202,8 @@ __global__ void __launch_bounds__(256) write_chunks_kernel(const __grid_constant
     }
 }
 
-// Measured (us on the GPU): the 24 requests above 28.2 with V codes gathered byte by byte.
+// As above, the other way round.  Measured (us on the GPU): the 24 requests above 24.5 (16.3 at a copy's rate; with V codes gathered
+// byte by byte 28.2), the second half of the 16384 tokens 7.5 (59 MB, read out of the L2; one row at a time 11.4).
 template <int D, bool FP8>
 __global__ void __launch_bounds__(256) read_rows_kernel(const __grid_constant__ ChunkRowsArgs a, const __grid_constant__ ChunkPages pages)
 {

@@ -43,7 +43,8 @@ struct Eight {
 // operations, both elements of a pair in one lane, running pointers, and copies to shared memory that go out while the token before
 // is worked on in place of loads whose registers wait.  8192 tokens of 32 / 8 heads of 128: loads of four heads at a time took 43 us
 // forward and 79 backward (117 and 151 registers: too few loads in flight); eight elements a lane, the pairs' others by shuffles, 36
-// and 65 (250 and then 190 instructions for 512 bytes; half of the issue slots).
+// and 65 (250 and then 190 instructions for 512 bytes; half of the issue slots); this, 31.6 and 45.5 (168 and 252 MB: 5.3 and 5.5 TB/s,
+// 81 and 84 % of a copy's rate; half of the issue slots still).
 template <int D>
 struct Lane {
     static constexpr int kLanes = D / 16, kRows = 32 / kLanes;  // of a row, rows of a warp

@@ -234,8 +234,9 @@ __global__ void __launch_bounds__(256, 2) norm_rotary_kernel(const __grid_consta
     }
 }
 
-// The same walk.  A lane adds up its eight columns of dw over all steps, and the block's sums go to `partials`, whose order the
-// launch fixes.
+// The same walk.  A lane adds up its columns of dw over all steps, and the block's sums go to `partials`; the last block of the
+// queries' and of the keys' to arrive adds them up, in the order of the blocks whichever it is.  (A kernel of its own behind this one, with
+// its launch: 1777 tokens of 8 / 2 heads of 64, forward and backward, 21.4 us a pass, so 19.2; 8192 of 32 / 8 of 128 84.0 and 82.6.)
 template <int D, int STEPS>
 __global__ void __launch_bounds__(256, 2) norm_rotary_backward_kernel(const __grid_constant__ NormRotaryArgs a, const int q_groups)
 {
@@ -331,7 +332,6 @@ __global__ void __launch_bounds__(256, 2) norm_rotary_backward_kernel(const __gr
         then = further;
     }
     if (!a.partials) return;
-    grid_dep_launch();
     float(*sums)[D] = reinterpret_cast<float(*)[D]>(memory);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -343,39 +343,46 @@ __global__ void __launch_bounds__(256, 2) norm_rotary_backward_kernel(const __gr
     __syncthreads();  // (no copy is on its way any more: those behind the last token copy nothing)
     if (lane.row == 0) lane.store(sums[warp], du, dv);
     __syncthreads();
+    float* to = is_q ? a.dq_weight : a.dk_weight;
+    if (!to) return;
     if (threadIdx.x < D) {
         float all = 0.f;
 #pragma unroll
         for (int x = 0; x < 8; ++x) all += sums[x][threadIdx.x];
         a.partials[((long long)blockIdx.y * gridDim.x + blockIdx.x) * D + threadIdx.x] = all;
     }
-}
-
-// dw of the queries' norm (blockIdx.y 0) and the keys' (1): eight columns a block, the blocks' sums added up in a fixed order.
-__global__ void __launch_bounds__(256) norm_weights_kernel(const float* partials, int q_blocks, int k_blocks, int head_dim, float* dq_weight, float* dk_weight)
-{
-    __shared__ float sums[32][9];
-    grid_dep_wait();
-    const bool is_q = blockIdx.y == 0;
-    float* to = is_q ? dq_weight : dk_weight;
-    if (!to) return;
-    const int n = is_q ? q_blocks : k_blocks, c = threadIdx.x & 7, r = threadIdx.x >> 3;
-    const float* p = partials + (is_q ? 0 : (long long)q_blocks * head_dim) + blockIdx.x * 8 + c;
-    float s = 0.f;
-#pragma unroll 8
-    for (int b = r; b < n; b += 32) s += p[(long long)b * head_dim];
-    sums[r][c] = s;
-    __syncthreads();
-    if (threadIdx.x < 8) {
-        float all = 0.f;
+    const int blocks = (is_q ? q_groups : (int)gridDim.y - q_groups) * gridDim.x;
+    __threadfence();
+    __syncthreads();  // (every thread's sum is out before the block counts as arrived)
+    if (__syncthreads_or(threadIdx.x == 0 && atomicAdd(a.arrived + (is_q ? 0 : 1), 1) == blocks - 1) == 0) return;
+    __threadfence();
+    if (threadIdx.x == 0) a.arrived[is_q ? 0 : 1] = 0;  // for the next launch
+    constexpr int kPer = D / 4, kSlices = 256 / kPer;     // threads of a block's sums, blocks at a time
+    const int c = threadIdx.x % kPer, slice = threadIdx.x / kPer;
+    const float4* from = reinterpret_cast<const float4*>(a.partials + (is_q ? 0 : (long long)q_groups * gridDim.x * D)) + c;
+    float4 all = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = slice; i0 < blocks; i0 += 16 * kSlices) {  // sixteen loads on the way
+        float4 x[16];
 #pragma unroll
-        for (int x = 0; x < 32; ++x) all += sums[x][c];
-        to[blockIdx.x * 8 + c] = all;
+        for (int j = 0; j < 16; ++j)
+            x[j] = i0 + j * kSlices < blocks ? __ldcg(from + (long long)(i0 + j * kSlices) * kPer) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) all = make_float4(all.x + x[j].x, all.y + x[j].y, all.z + x[j].z, all.w + x[j].w);
+    }
+    float4* meet = reinterpret_cast<float4*>(memory);
+    meet[slice * kPer + c] = all;  // (the block's own sums have been read)
+    __syncthreads();
+    if (threadIdx.x < D) {
+        float w = 0.f;
+#pragma unroll
+        for (int x = 0; x < kSlices; ++x) w += reinterpret_cast<const float*>(meet)[x * D + threadIdx.x];
+        to[threadIdx.x] = w;
     }
 }
 
-// How a launch is cut: two steps of heads to a token where that leaves the GPU filled (they share the angles and what a token
-// costs beside its rows), else one; at most two blocks on every SM.
+// How a launch is cut: two steps of heads to a token where there are so many and that leaves the GPU filled (they share the angles and
+// what a token costs beside its rows), else one (8 / 2 heads of 64, a step half empty: 13.9 us on the GPU, so 12.0); at most two
+// blocks on every SM.
 struct Cut {
     int steps, q_groups, groups, columns;
 };
@@ -384,7 +391,7 @@ Cut cut_heads(const NormRotaryArgs& a)
     const int rows = a.head_dim == 128 ? 4 : 8, tiles = (a.n + 7) / 8, most = 148 * 2;
     Cut c;
     auto groups = [&](int heads) { return (a.q_heads + heads - 1) / heads + (a.kv_heads + heads - 1) / heads; };
-    c.steps = (long long)tiles * groups(2 * rows) >= most || groups(rows) > most ? 2 : 1;
+    c.steps = a.q_heads > rows && ((long long)tiles * groups(2 * rows) >= most || groups(rows) > most) ? 2 : 1;
     c.q_groups = (a.q_heads + c.steps * rows - 1) / (c.steps * rows);
     c.groups = groups(c.steps * rows);
     c.columns = most / c.groups < tiles ? most / c.groups : tiles;
@@ -427,19 +434,8 @@ cudaError_t launch_norm_rotary_backward(const NormRotaryArgs& args, cudaStream_t
     NormRotaryArgs a = args;
     const Cut c = cut_heads(a);
     if (!a.dq_weight && !a.dk_weight) a.partials = nullptr;
-    cudaError_t e = a.head_dim == 128 ? (c.steps == 2 ? launch_backward_steps<128, 2>(a, c, stream) : launch_backward_steps<128, 1>(a, c, stream))
-                                      : (c.steps == 2 ? launch_backward_steps<64, 2>(a, c, stream) : launch_backward_steps<64, 1>(a, c, stream));
-    if (e != cudaSuccess || !a.partials) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.head_dim / 8, 2);
-    cfg.blockDim = dim3(256);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, norm_weights_kernel, (const float*)a.partials, c.columns * c.q_groups, c.columns * (c.groups - c.q_groups), a.head_dim, a.dq_weight, a.dk_weight);
+    return a.head_dim == 128 ? (c.steps == 2 ? launch_backward_steps<128, 2>(a, c, stream) : launch_backward_steps<128, 1>(a, c, stream))
+                             : (c.steps == 2 ? launch_backward_steps<64, 2>(a, c, stream) : launch_backward_steps<64, 1>(a, c, stream));
 }
 
 cudaError_t prepare_norm_backward()

@@ -163,6 +163,7 @@ struct NormRotaryArgs {
     const int* position;                 // device, [n], or null: token i at position i
     int n, q_heads, kv_heads, head_dim;
     float* partials;                     // [kMaxNormBlocks][head_dim]
+    int* arrived;                        // [2], 0 between launches: blocks of the queries and of the keys that are done
     float *dq_weight, *dk_weight;
 };
 constexpr int kMaxNormBlocks = 148 * 2;

@@ -12,6 +12,8 @@
 
 using namespace rlkv;
 
+constexpr int kNormArrivals = 16;  // counters of the norms' gradients in the status area
+
 struct rlkv_prompt {
     int layers, kv_heads, q_heads, head_dim, max_tokens, sink, window, device;
     float softcap;
@@ -313,6 +315,7 @@ int rlkv_prompt_rotate_backward(rlkv_prompt* p, int layer, const void* q, int64_
     a.dq_weight = dq_weight;
     a.dk_weight = dk_weight;
     a.partials = reinterpret_cast<float*>(p->dev_base + p->off_norms);
+    a.arrived = reinterpret_cast<int*>(p->dev_base) + kNormArrivals;
     DeviceGuard g(p->device);
     if (!g.ok) return RLKV_ECUDA;
     RLKV_CUDA(launch_norm_rotary_backward(a, static_cast<cudaStream_t>(stream)));

@@ -11,7 +11,9 @@ using namespace rlkv;
 namespace {
 
 constexpr int kMaxChunkTokens = 1 << 24;  // of one call
-constexpr int kMinChunkTiles = 4;         // key tiles of a CTA's range, at least
+// Keys of a CTA's range, at least: three times 100 tokens on 500, 8 bits, tiles of 128, 30 us with 512, 27 so; tiles of 64: 27 to 28 us
+// for 512 on 1000 with 64 to 512, 31 with 768.
+constexpr int kMinChunkKeys = 256;
 
 // What a unit's start and end -- its queries' way to shared memory, the first product, its results -- count as in key tiles.  Measured
 // over counts from 1 to 14: 32 rows a unit, 16 bits: 48 single tokens on 3400 each 58 us with 3, 52 with 6, 54 with 10, four drafted
@@ -258,7 +260,7 @@ int rlkv_paged_chunk_attention(rlkv_paged* p, int layer, const int* slots, const
     const long long room = (long long)(p->chunk_bytes / (2 * sizeof(float) * chunk_record_floats(p->head_dim, shape)));  // CTAs it has records for
     int ctas = shape == 2 ? sms : 2 * sms;
     if (ctas > room) ctas = room < 1 ? 1 : (int)room;
-    const int pieces = plan_chunks(a, shape, ctas, kMinChunkTiles, unit_tiles(shape, p->fp8));
+    const int pieces = plan_chunks(a, shape, ctas, kMinChunkKeys / chunk_keys(shape), unit_tiles(shape, p->fp8));
     const int keys = chunk_keys(shape);
     ChunkMaps m;
     int e = encode_heads_map(&m.q, q, total, p->q_heads, p->head_dim, q_stride, a.group, (shape == 0 ? 32 : 128) / a.group);
@@ -387,7 +389,7 @@ int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full,
     a.window = window;
     if (shape < 0) shape = choose_shape(a, kMaxChunkCtas / 2, 128, shape == -2);
     if (shape > 2) return RLKV_EINVAL;
-    plan_chunks(a, shape, max_ctas, kMinChunkTiles, unit_tiles(shape, false));
+    plan_chunks(a, shape, max_ctas, kMinChunkKeys / chunk_keys(shape), unit_tiles(shape, false));
     for (int c = 0; c <= a.ctas; ++c) {
         at_out[4 * c] = a.at[c].seq;
         at_out[4 * c + 1] = a.at[c].row_tile;

@@ -38,7 +38,7 @@
 // Measured on one B200 (us on the GPU; 32 / 8 heads of 128, 6 of 8 full, unless said otherwise): five drafted tokens on 8192 14.5
 // (latency of one wave and of the join); four of each of 32 sequences of 8064 on average, 16 bits 129 (819 MB: 6.3 TB/s), 8 bits 106
 // (410 MB: the products, the decoding and the softmax of a tile share an SM's shared memory and issue slots); 512 beside 47 single
-// tokens of 2900 on average (28 / 4 heads, 3 of 4 full, capped) 87; 2048 on 8192, all full, 267 in bursts (1.16 PFLOP/s, 69 % of a large
+// tokens of 2900 on average (28 / 4 heads, 3 of 4 full, capped) 87, in 8 bits 134 as two launches; 2048 on 8192, all full, 267 in bursts (1.16 PFLOP/s, 69 % of a large
 // library product's burst rate), 8 bits 384 (one product per 128 keys; 395 with one per page).
 //
 // Tried and not taken: units of at most 32 rows four times in the tile of SHAPE 1 too, where they stand beside larger ones (512 beside
@@ -386,7 +386,7 @@ struct Walk {
     {
         if (same_unit(at, end) && at.tile >= end.tile) return false;
         s.start = a.seqs.start[at.seq];
-        s.m = a.seqs.start[at.seq + 1] - s.start;
+        s.m = a.seqs.count[at.seq];
         s.len = a.seqs.len[at.seq];
         s.slot = a.seqs.slot[at.seq];
         s.full = at.head < a.n_full;
@@ -408,8 +408,7 @@ struct Walk {
                 at.head = 0;
                 if (++at.row_tile * SUBS * tokens >= s.m) {
                     at.row_tile = 0;
-                    do ++at.seq;
-                    while (at.seq < a.seqs.n && a.seqs.start[at.seq + 1] == a.seqs.start[at.seq]);
+                    ++at.seq;
                 }
             }
         }
@@ -1138,7 +1137,7 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
     const ChunkPos b = a.at[c], before = a.at[c - 1];
     if (b.tile == 0 || b.seq >= a.seqs.n || (same_unit(before, b) && before.tile > 0)) return;
     const int tokens = kRecordRows / a.group, w = blockIdx.y / 4, row0 = blockIdx.y % 4 * 32;
-    const int start = a.seqs.start[b.seq], m = a.seqs.start[b.seq + 1] - start;
+    const int start = a.seqs.start[b.seq], m = a.seqs.count[b.seq];
     const int from = (b.row_tile * (SHAPE == 2 ? 2 : 1) + w) * tokens;
     if (row0 / a.group >= tokens || from + row0 / a.group >= m) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;

@@ -74,8 +74,15 @@ __host__ __device__ inline bool same_unit(const ChunkPos& a, const ChunkPos& b)
 }
 constexpr int kMaxChunkCtas = 2 * 148;
 
+// The chunks of a launch: entry i's `count[i]` tokens lie from packed token start[i] on.
+struct ChunkList {
+    int n;
+    int start[kMaxPagedBatch], count[kMaxPagedBatch], len[kMaxPagedBatch];
+    unsigned short slot[kMaxPagedBatch];
+};
+
 struct ChunkArgs {
-    ChunkSeqs seqs;
+    ChunkList seqs;
     const int* page_table;
     int table_stride, n_pages;
     long long full_row0, comp_row0;  // 16-bit pool: first rows of the layer's regions, as in PagedArgs

@@ -91,11 +91,11 @@ void fill_rows_args(rlkv_paged* p, int layer, ChunkRowsArgs& a)
 int plan_chunks(ChunkArgs& a, int shape, int max_ctas, int min_tiles, int extra)
 {
     const int keys = chunk_keys(shape), tokens = chunk_tokens(shape, a.group);
-    const ChunkSeqs& s = a.seqs;
+    const ChunkList& s = a.seqs;
     auto unit = [&](int i, int j, bool full) {
-        return chunk_unit(s.len[i], s.start[i + 1] - s.start[i], j, tokens, keys, full, a.sink, a.window).tiles + extra;
+        return chunk_unit(s.len[i], s.count[i], j, tokens, keys, full, a.sink, a.window).tiles + extra;
     };
-    auto row_tiles = [&](int i) { return (s.start[i + 1] - s.start[i] + tokens - 1) / tokens; };
+    auto row_tiles = [&](int i) { return (s.count[i] + tokens - 1) / tokens; };
     long long all = 0;
     for (int i = 0; i < s.n; ++i)
         for (int j = 0; j < row_tiles(i); ++j) {
@@ -135,9 +135,11 @@ int plan_chunks(ChunkArgs& a, int shape, int max_ctas, int min_tiles, int extra)
 // The shape of a launch.  32 rows where every chunk's queries of a KV head fit them.  Two sub-tiles of 128 are for launches most of whose
 // key tiles belong to chunks that fill more than one: on an 8-bit cache for all of these, since a tile's codes are decoded once for
 // both (us with one sub-tile and so: a prompt of 8192 tokens 877 and 651, 512 tokens on 3400 65 and 57, three times 100 on 500 31
-// and 30), in 16 bits where the K and V rows are too many for the L2, in which the other tiles of rows would find them (four times
-// 512 on 8192 300 and 270, 64 of each of 32 sequences on 8064 341 and 272) and every SM has 32 such tiles of 128 keys (64 tokens on 40000 62 and 65), or where it has 100 (2048 on 8192 280 and 282,
-// under the power cap 320 and 315, a prompt of 8192 497 and 490); but 512 on 8192 78 and 81, four times 512 on 3400 111 and 117.
+// and 30), but few others beside them, whose tiles are as long (512 tokens on 3400 beside 11 single ones 94 and 110); in 16 bits where
+// the K and V rows are too many for the L2, in which the other tiles of rows would find them (four times 512 on 8192 300 and 270, 64
+// of each of 32 sequences on 8064 341 and 272) and every SM has 32 such tiles of 128 keys (64 tokens on 40000 62 and 65), or where it
+// has 100 (2048 on 8192 280 and 282, under the power cap 320 and 315, a prompt of 8192 497 and 490); but 512 on 8192 78 and 81, four
+// times 512 on 3400 111 and 117.
 constexpr long long kNearL2 = 80ll << 20;
 int choose_shape(const ChunkArgs& a, int sms, int head_dim, bool fp8)
 {
@@ -145,7 +147,7 @@ int choose_shape(const ChunkArgs& a, int sms, int head_dim, bool fp8)
     long long small = 0, large = 0, shared = 0;  // key rows times row tiles of 128; rows that several of these read
     bool few = true;
     for (int i = 0; i < a.seqs.n; ++i) {
-        const int m = a.seqs.start[i + 1] - a.seqs.start[i];
+        const int m = a.seqs.count[i];
         if (m > chunk_tokens(0, a.group)) few = false;
         const long long rows = (long long)a.n_full * (a.seqs.len[i] + m / 2) + (long long)a.n_comp * ring;
         const int tiles = (int)(((long long)m * a.group + 127) / 128);
@@ -153,8 +155,38 @@ int choose_shape(const ChunkArgs& a, int sms, int head_dim, bool fp8)
         if (tiles > 1) shared += rows;
     }
     if (few) return 0;
-    if (large <= small) return 1;
+    if (large <= (fp8 ? 4 * small : small)) return 1;
     return fp8 || large / 256 >= (shared * head_dim * 4 > kNearL2 ? 32ll : 100ll) * sms ? 2 : 1;
+}
+
+// Whether chunks of at most 32 rows and the others go out as two launches, each in its own shape.  In 16 bits one launch is shorter
+// (one kind's products run beside the other's stream: 512 tokens on 3400 beside 47 single ones on 1700 71 us, apart 52 and 36); in 8
+// bits its one sub-tile is not (139 us, as two 130; on 3400 all 172 and 154; 1024 tokens of a new prompt beside 47 126 and 107), unless
+// either kind is little (40 tokens on 100 beside 16 single ones on 2000 46, apart 34 and 15; 300 on 3400 beside 23, all full, 116 and 118).
+bool two_launches(const ChunkSeqs& s, const ChunkArgs& a, int sms, bool fp8)
+{
+    if (!fp8) return false;
+    long long few = 0, more = 0;  // key rows times row tiles of 128
+    for (int i = 0; i < s.n; ++i) {
+        const int m = s.start[i + 1] - s.start[i];
+        const long long rows = (long long)a.n_full * (s.len[i] + m / 2) + (long long)a.n_comp * (a.sink + a.window);
+        if (m > 0) (m * a.group <= 32 ? few : more) += rows * (((long long)m * a.group + 127) / 128);
+    }
+    return few / 256 >= 6ll * sms && more / 256 >= 2ll * sms;
+}
+
+// The chunks of a launch, 0: all, 1: those of at most 32 rows, 2: the others; empty ones in none.
+void pick_chunks(const ChunkSeqs& s, int group, int pick, ChunkList& l)
+{
+    l.n = 0;
+    for (int i = 0; i < s.n; ++i) {
+        const int m = s.start[i + 1] - s.start[i];
+        if (m == 0 || (pick && (m * group <= 32) != (pick == 1))) continue;
+        l.start[l.n] = s.start[i];
+        l.count[l.n] = m;
+        l.len[l.n] = s.len[i];
+        l.slot[l.n++] = s.slot[i];
+    }
 }
 
 }  // namespace
@@ -216,12 +248,13 @@ int rlkv_paged_rotate_chunks(rlkv_paged* p, int layer, const int* slots, const i
 int rlkv_paged_chunk_attention(rlkv_paged* p, int layer, const int* slots, const int* counts, int n, const void* q, int64_t q_stride,
                                const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* out, float* lse, void* stream)
 {
+    ChunkSeqs s;
     ChunkArgs a;
-    const int rc = check_chunks(p, layer, slots, nullptr, counts, n, false, a.seqs);
+    const int rc = check_chunks(p, layer, slots, nullptr, counts, n, false, s);
     if (rc) return rc;
     if (!check_stride(p, p->q_heads, q_stride) || !check_stride(p, p->kv_heads, k_stride) || !check_stride(p, p->kv_heads, v_stride))
         return RLKV_EINVAL;
-    const int total = a.seqs.start[n];
+    const int total = s.start[n];
     if (total == 0) return RLKV_OK;
     if (!q || !k || !v || !out || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3))
         return RLKV_EINVAL;
@@ -256,22 +289,28 @@ int rlkv_paged_chunk_attention(rlkv_paged* p, int layer, const int* slots, const
         a.v_scale[h] = p->fp8 ? p->v_scale[(size_t)layer * p->kv_heads + h] : 1.f;
     }
     const int sms = p->sm_count < kMaxChunkCtas / 2 ? p->sm_count : kMaxChunkCtas / 2;
-    const int shape = choose_shape(a, sms, p->head_dim, p->fp8);
-    const long long room = (long long)(p->chunk_bytes / (2 * sizeof(float) * chunk_record_floats(p->head_dim, shape)));  // CTAs it has records for
-    int ctas = shape == 2 ? sms : 2 * sms;
-    if (ctas > room) ctas = room < 1 ? 1 : (int)room;
-    const int pieces = plan_chunks(a, shape, ctas, kMinChunkKeys / chunk_keys(shape), unit_tiles(shape, p->fp8));
-    const int keys = chunk_keys(shape);
-    ChunkMaps m;
-    int e = encode_heads_map(&m.q, q, total, p->q_heads, p->head_dim, q_stride, a.group, (shape == 0 ? 32 : 128) / a.group);
-    if (!e) e = encode_heads_map(&m.k, k, total, p->kv_heads, p->head_dim, k_stride, 1, keys);
-    if (!e) e = encode_heads_map(&m.v, v, total, p->kv_heads, p->head_dim, v_stride, 1, keys);
-    if (!e && !p->fp8) e = encode_heads_map(&m.pool, dev_at<__nv_bfloat16>(p, p->off_pool), p->pool_rows, 1, p->head_dim, p->head_dim, 1, kTile);
-    else if (!e) m.pool = shape == 2 ? p->map_codes : p->map_k;
-    if (e) return e;
-    RLKV_CUDA(launch_chunk_attention(a, m, p->head_dim, shape, pieces, static_cast<cudaStream_t>(stream)));
-    p->launches += pieces > 1 ? 2 : 1;
-    return RLKV_OK;
+    auto launch = [&](int pick) -> int {
+        pick_chunks(s, a.group, pick, a.seqs);
+        const int shape = choose_shape(a, sms, p->head_dim, p->fp8);
+        const long long room = (long long)(p->chunk_bytes / (2 * sizeof(float) * chunk_record_floats(p->head_dim, shape)));  // CTAs it has records for
+        int ctas = shape == 2 ? sms : 2 * sms;
+        if (ctas > room) ctas = room < 1 ? 1 : (int)room;
+        const int pieces = plan_chunks(a, shape, ctas, kMinChunkKeys / chunk_keys(shape), unit_tiles(shape, p->fp8));
+        const int keys = chunk_keys(shape);
+        ChunkMaps m;
+        int e = encode_heads_map(&m.q, q, total, p->q_heads, p->head_dim, q_stride, a.group, (shape == 0 ? 32 : 128) / a.group);
+        if (!e) e = encode_heads_map(&m.k, k, total, p->kv_heads, p->head_dim, k_stride, 1, keys);
+        if (!e) e = encode_heads_map(&m.v, v, total, p->kv_heads, p->head_dim, v_stride, 1, keys);
+        if (!e && !p->fp8) e = encode_heads_map(&m.pool, dev_at<__nv_bfloat16>(p, p->off_pool), p->pool_rows, 1, p->head_dim, p->head_dim, 1, kTile);
+        else if (!e) m.pool = shape == 2 ? p->map_codes : p->map_k;
+        if (e) return e;
+        RLKV_CUDA(launch_chunk_attention(a, m, p->head_dim, shape, pieces, static_cast<cudaStream_t>(stream)));
+        p->launches += pieces > 1 ? 2 : 1;
+        return RLKV_OK;
+    };
+    if (!two_launches(s, a, sms, p->fp8)) return launch(0);
+    const int e = launch(1);
+    return e ? e : launch(2);
 }
 
 int rlkv_paged_append_chunks(rlkv_paged* p, int layer, const int* slots, const int* counts, int n, const void* k, int64_t k_stride,
@@ -377,11 +416,11 @@ int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full,
         if (lens[i] < 0 || counts[i] < 0) return RLKV_EINVAL;
         a.seqs.len[i] = lens[i];
         a.seqs.start[i] = (int)total;
+        a.seqs.count[i] = counts[i];
         total += counts[i];
         if (total > kMaxChunkTokens) return RLKV_EINVAL;
     }
     if (total < 1) return RLKV_EINVAL;
-    a.seqs.start[n] = (int)total;
     a.n_full = n_full;
     a.n_comp = n_comp;
     a.group = group;

@@ -204,6 +204,29 @@ def test_many_sequences(hz, cuda_device):
         compare(out, lse, reference(q, rows, (k, v), lens, counts, "1010", 16, 112, 0, slopes, fp8))
 
 
+@pytest.mark.parametrize("cap,biased", [(0, False), (0, True), (30.0, False)])
+def test_small_and_large_chunks_on_an_8_bit_cache(hz, cuda_device, cap, biased):
+    """Enough of both for a launch of each: the same results whatever their order, and whatever stands between them."""
+    lens = [1750 + 3 * i for i in range(26)] + [900, 64, 300, 0]
+    counts = [1 + i % 8 for i in range(26)] + [512, 0, 9, 33]
+    order = [28, 0, 1, 26, 27] + list(range(2, 20)) + [29] + list(range(20, 26))
+    lens, counts = [lens[i] for i in order], [counts[i] for i in order]
+    mask = "110111"
+    rows = [m * 4 <= 32 for m in counts]
+    assert sum(n * 5 for n, r in zip(lens, rows) if r) >= 6 * 148 * 256 and sum(n * 5 * 16 for n, r in zip(lens, rows) if not r) >= 2 * 148 * 256
+    cache, slots, held, slopes, q, k, v = build(hz, cuda_device, 6, 24, 128, mask, 16, 112, lens, counts, cap, biased, True)
+    out, lse = cache.attend_chunks(0, slots, counts, q, k, v)
+    assert cache.status() == 0
+    compare(out, lse, reference(q, held, (k, v), lens, counts, mask, 16, 112, cap, slopes, True))
+    again, lse2 = cache.attend_chunks(0, slots, counts, q.contiguous(), k.contiguous(), v.contiguous())
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    few = [i for i, m in enumerate(counts) if 0 < m <= 8]          # alone they go out in the launch they have here
+    parts = [list(x.split(counts)) for x in (q, k, v, out, lse)]
+    small = [torch.cat([x[i] for i in few]) for x in parts]
+    alone, lse3 = cache.attend_chunks(0, [slots[i] for i in few], [counts[i] for i in few], *small[:3])
+    assert torch.equal(alone, small[3]) and torch.equal(lse3, small[4])
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("counts", [[3, 1, 4], [200, 1, 90]])
 @pytest.mark.parametrize("cap", [0.0, 20.0])

@@ -24,6 +24,8 @@
 //   last four        8-bit caches: V codes to fp16
 //
 // The running maximum of a row moves only when it would grow by more than 2^8 (its effect cancels in O / l, which are fp32).
+// Every row sees its own token at least, so that l is above 0, unless scores are not finite: those rows become NaN, in one piece or
+// in many (a maximum passes over NaN, a sum does not).
 // P is rounded to bf16 for the product, half a step 2^-8 of each weight; l sums the fp32 values.
 //
 // An 8-bit cache.  Scores come from the K codes as they lie, on the products of 8-bit operands: the queries are split into two E4M3
@@ -698,16 +700,16 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
 #pragma unroll
                 for (int x = 0; x < 4; ++x) all = fmaxf(all, at[x * 32 + lane]);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) total_l += at[x * 32 + lane] == -INFINITY ? 0.f : at[128 + x * 32 + lane] * ex2(at[x * 32 + lane] - all);
+                for (int x = 0; x < 4; ++x) total_l += at[128 + x * 32 + lane] * (at[x * 32 + lane] == -INFINITY ? 0.f : ex2(at[x * 32 + lane] - all));
                 const bool whole = g.record < 0;
-                const float f = m == -INFINITY ? 0.f : ex2(m - all) * unit, inv = whole ? (total_l > 0.f ? 1.f / total_l : 0.f) : 1.f;
+                const float f = m == -INFINITY ? 0.f : ex2(m - all) * unit, inv = whole ? 1.f / total_l : 1.f;
                 float* rec = a.records + (long long)max(g.record, 0) * chunk_record_floats(D, SHAPE);
                 if (warp == 0) {
                     if (!whole) {
                         rec[D * 32 + lane] = all;
                         rec[(D + 1) * 32 + lane] = total_l;
                     } else if (mine && a.lse) {
-                        a.lse[at_head] = total_l > 0.f ? (all + log2f(total_l)) * kLn2 : -INFINITY;
+                        a.lse[at_head] = (all + log2f(total_l)) * kLn2;
                     }
                 }
                 constexpr int kHalf = D / 8, kMine = D / 32;  // groups of four columns in a half, and a warp's of them
@@ -744,8 +746,8 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                 }
             } else if (!busy) {
             } else if (g.record < 0) {
-                const float inv = l > 0.f ? unit / l : 0.f;
-                if (mine && a.lse) a.lse[at_head] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                const float inv = unit / l;
+                if (mine && a.lse) a.lse[at_head] = (m + log2f(l)) * kLn2;
                 // through shared memory (the sub-tile's queries are not needed any more), so that whole rows go out
                 uint8_t* stage = smem + w * C::kQBytes + (warp & 3) * 32 * D * 2;
                 constexpr int kChunks = D / 8, kPerStore = 32 / kChunks;  // 16-byte pieces of a row, rows per store instruction
@@ -1154,6 +1156,7 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
         for (int u = 0; u < kAtOnce; ++u) {
             const int k = k0 + u * kPieces;
             pm[u] = -INFINITY;
+            pl[u] = 0.f;
             if (k > last) continue;
             const int slot = k > c - 1 || same_unit(before, b) ? 2 * k : 2 * k + 1;
             const float* rec = a.records + (long long)slot * chunk_record_floats(D, SHAPE) + (long long)w * kRows * (D + 2);
@@ -1165,7 +1168,7 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
         }
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-            if (pm[u] == -INFINITY) continue;  // the row sees none of the piece's keys
+            if (pm[u] == -INFINITY && pl[u] == 0.f) continue;  // the row sees none of the piece's keys (of NaN scores, the sum is NaN)
             const float to = fmaxf(mx, pm[u]), old = mx == -INFINITY ? 0.f : ex2(mx - to), f = ex2(pm[u] - to);
             mx = to;
             l = l * old + pl[u] * f;
@@ -1195,7 +1198,7 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
         f[k] = t == -INFINITY ? 0.f : ex2(t - all);
         total += sum[k * RUNS][r] * f[k];
     }
-    const float inv = total > 0.f ? 1.f / total : 0.f;
+    const float inv = 1.f / total;
     const int head = a.head_of_slot[b.head] * a.group + (row0 + r) % a.group;
     const long long at_head = (long long)(start + i) * a.q_heads + head;
 #pragma unroll
@@ -1208,7 +1211,7 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
         *reinterpret_cast<uint2*>(a.out + at_head * D + (blockIdx.z * RUNS + run) * RUN + x0) =
             make_uint2(bf16x2(y[0] * inv, y[1] * inv), bf16x2(y[2] * inv, y[3] * inv));
     }
-    if (a.lse && blockIdx.z == 0 && x0 == 0) a.lse[at_head] = total > 0.f ? (all + log2f(total)) * kLn2 : -INFINITY;
+    if (a.lse && blockIdx.z == 0 && x0 == 0) a.lse[at_head] = (all + log2f(total)) * kLn2;
 }
 
 template <int D, int SHAPE, bool FP8>

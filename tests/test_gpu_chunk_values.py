@@ -1,0 +1,47 @@
+"""Attention of chunks where the queries' values are not those of a standard normal row."""
+import pytest
+import torch
+
+from test_gpu_chunks import build, hz  # noqa: F401
+from test_gpu_parity import rand_bf16
+
+pytestmark = pytest.mark.gpu
+
+CHANNEL = 37
+
+
+def with_channel(hz, dev, lens, counts, fp8, cached, own, mask="10", cap=0.0, seed=100):  # noqa: F811
+    """As build, but every key holds the same number in one channel: `cached` those that the cache holds, `own` the chunks'."""
+    Hkv, Hq, D, S, W = len(mask), 4 * len(mask), 128, 16, 112
+    cache, slots, rows, _, q, k, v = build(hz, dev, Hkv, Hq, D, mask, S, W, [0] * len(lens), counts, cap, False, fp8, seed=seed, room=max(lens) + max(counts))
+    rows = []
+    for i, (s, n) in enumerate(zip(slots, lens)):
+        kk, vv = rand_bf16((n, Hkv, D), seed + 2 * i).to(dev), rand_bf16((n, Hkv, D), seed + 2 * i + 1).to(dev)
+        kk[..., CHANNEL] = cached
+        if n:
+            cache.prefill(0, s, kk, vv)
+        rows.append((kk, vv))
+    q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+    k[..., CHANNEL] = own
+    return cache, slots, rows, q, k, v
+
+
+BAD = [float("inf"), float("-inf"), float("nan")]
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("lens,counts", [([40, 0], [3, 2]), ([9000, 17], [4, 1]), ([700, 5], [40, 3]), ([6000, 100], [300, 3])])
+def test_queries_that_are_not_finite(hz, cuda_device, fp8, lens, counts):  # noqa: F811
+    """An infinite or NaN query gives NaN, as the formula does, whether its keys lie in one piece or in many; the other rows do not change.
+    (Every score of one sign of infinity: there is no largest that is finite, either.)"""
+    cache, slots, rows, q, k, v = with_channel(hz, cuda_device, lens, counts, fp8, 1.0, 1.0)
+    want, want_lse = cache.attend_chunks(0, slots, counts, q, k, v)
+    for bad in BAD[2:] if fp8 else BAD:
+        for token, head in ((1, 0), (2, 7), (counts[0] - 1, 4)):
+            x = q.clone()
+            x[token, head, CHANNEL] = bad
+            out, lse = cache.attend_chunks(0, slots, counts, x, k, v)
+            assert cache.status() == 0
+            assert bool(out[token, head].isnan().all()) and not bool(lse[token, head].isfinite())
+            out[token, head], lse[token, head] = want[token, head], want_lse[token, head]
+            assert torch.equal(out, want) and torch.equal(lse, want_lse)

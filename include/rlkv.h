@@ -350,7 +350,8 @@ int rlkv_paged_rotate_chunks(rlkv_paged* cache, int layer, const int* slots, con
  * exp(score), or NULL.  Every sum has a fixed order: the same call on the same cache gives the same bits.  (What a call keeps
  * between its CTAs lies in 39 MB -- 20 at head_dim 64 -- that rlkv_paged_create allocates beside the cache's buffer; if it cannot, the
  * decode launches' scratch serves, and large calls use fewer CTAs.)  Values of a sequence's own rows are
- * assumed finite; what rows of other sequences or of pages' unused parts hold has no effect. */
+ * assumed finite; what rows of other sequences or of pages' unused parts hold has no effect.  A query that is not finite gives a
+ * result that is not (under a cap an infinite one scores the cap). */
 int rlkv_paged_chunk_attention(rlkv_paged* cache, int layer, const int* slots, const int* counts, int n, const void* q,
                                int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* out,
                                float* lse, void* stream);

@@ -190,7 +190,8 @@ __device__ __forceinline__ void values4(uint32_t codes, float2& f, float2& g)
 // A query row of 128 bf16 elements in shared memory (two runs of 128 bytes, swizzled by the row) becomes, in place, two rows of
 // E4M3: x 2^e = a + b, a rounded to four bits, b what is left.  2^e brings the largest element to 128 .. 256; a bf16 number has
 // eight bits, so a + b is exact down to 2^-10 of the largest element and off by at most 2^-18 of it below -- less than what
-// bf16 itself leaves of such an element next to it.  Returns 2^-e.
+// bf16 itself leaves of such an element next to it.  Returns 2^-e, and of a row with an infinite element (a code stands for its sign)
+// infinity: its scores are infinite, or NaN against keys of zero, as they would be of the queries as given.
 __device__ __forceinline__ float split_row(uint8_t* q, int row)
 {
     uint4* at[2] = {reinterpret_cast<uint4*>(q + row * 128), reinterpret_cast<uint4*>(q + kQBlock + row * 128)};
@@ -203,7 +204,7 @@ __device__ __forceinline__ float split_row(uint8_t* q, int row)
     for (int i = 0; i < 64; ++i) top = __hmax2(top, __habs2(p[i]));
     const float big = fmaxf(__low2float(top), __high2float(top));
     const int exponent = min(max((__float_as_int(big) >> 23 & 255) - 134, -126), 120);  // of the largest element's distance from 2^7
-    const float up = __int_as_float((127 - exponent) << 23), down = __int_as_float((127 + exponent) << 23);
+    const float up = __int_as_float((127 - exponent) << 23), down = big == INFINITY ? INFINITY : __int_as_float((127 + exponent) << 23);
 #pragma unroll
     for (int c = 0; c < 8; ++c) {  // sixteen elements: sixteen bytes of a and of b
         uint32_t a[4], b[4];

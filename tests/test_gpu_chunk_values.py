@@ -1,8 +1,8 @@
-"""Attention of chunks where the queries' values are not those of a standard normal row."""
+"""Attention of chunks where the queries' values are those of no standard normal row."""
 import pytest
 import torch
 
-from test_gpu_chunks import build, hz  # noqa: F401
+from test_gpu_chunks import build, hz, reference  # noqa: F401
 from test_gpu_parity import rand_bf16
 
 pytestmark = pytest.mark.gpu
@@ -36,7 +36,7 @@ def test_queries_that_are_not_finite(hz, cuda_device, fp8, lens, counts):  # noq
     (Every score of one sign of infinity: there is no largest that is finite, either.)"""
     cache, slots, rows, q, k, v = with_channel(hz, cuda_device, lens, counts, fp8, 1.0, 1.0)
     want, want_lse = cache.attend_chunks(0, slots, counts, q, k, v)
-    for bad in BAD[2:] if fp8 else BAD:
+    for bad in BAD:
         for token, head in ((1, 0), (2, 7), (counts[0] - 1, 4)):
             x = q.clone()
             x[token, head, CHANNEL] = bad
@@ -45,3 +45,19 @@ def test_queries_that_are_not_finite(hz, cuda_device, fp8, lens, counts):  # noq
             assert bool(out[token, head].isnan().all()) and not bool(lse[token, head].isfinite())
             out[token, head], lse[token, head] = want[token, head], want_lse[token, head]
             assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("lens,counts", [([40, 0], [3, 2]), ([9000, 17], [4, 1]), ([700, 5], [40, 3])])
+def test_infinite_queries_under_a_cap(hz, cuda_device, fp8, lens, counts):  # noqa: F811
+    """A capped score of an infinite query is the cap: all keys weigh the same."""
+    cache, slots, rows, q, k, v = with_channel(hz, cuda_device, lens, counts, fp8, 1.0, 1.0, cap=30.0)
+    for bad in BAD[:2]:
+        x = q.clone()
+        x[2, 5, CHANNEL] = bad
+        out, lse = cache.attend_chunks(0, slots, counts, x, k, v)
+        assert cache.status() == 0
+        ref, size, ref_lse, top = reference(x, rows, (k, v), lens, counts, "10", 16, 112, 30.0, None, fp8)
+        err = (out.double() - ref).abs()
+        assert bool((err <= (2.0 ** -8 + 2.0 ** -14) * size + 2.0 ** -8 * ref.abs() + 1e-6).all())
+        assert bool(((lse.double() - ref_lse).abs() <= 2.0 ** -15 + 2.0 ** -22 * (ref_lse.abs() + top)).all())

@@ -28,8 +28,8 @@
 // in many (a maximum passes over NaN, a sum does not).
 // P is rounded to bf16 for the product, half a step 2^-8 of each weight; l sums the fp32 values.
 //
-// An 8-bit cache.  Scores come from the K codes as they lie, on the products of 8-bit operands: the queries are split into two E4M3
-// numbers (split_row), which costs the same products as bf16 would.  V codes (they lie transposed, an element's tokens contiguous)
+// An 8-bit cache.  Scores come from the K codes as they lie, on the products of 8-bit operands: the queries are split into an E4M3
+// and an E5M2 number (split_row), which costs the same products as bf16 would.  V codes (they lie transposed, an element's tokens contiguous)
 // are decoded by four warps, to fp16, which holds them exactly and which one instruction converts two of; so P is fp16 there, with
 // its reference 2^7 below a row's largest score: P from 2^15 down to 2^-14 keeps eleven bits, the step below that is 2^-31 of the
 // largest weight.  (Both operands decoded to bf16 by their bits: 250 us for four drafted tokens of 32 sequences; V only 137; V by
@@ -143,8 +143,11 @@ __device__ __forceinline__ void load_page(uint32_t dst, const CUtensorMap* map, 
                  : "memory");
 }
 
-// E4M3 x E4M3 -> fp32, 32 elements of the contraction; both operands in shared memory, rows of 128 bytes.
-__host__ __device__ constexpr uint32_t instr_desc8(int m, int n) { return 1u << 4 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24; }
+// E4M3 (`wide`: E5M2) x E4M3 -> fp32, 32 elements of the contraction; both operands in shared memory, rows of 128 bytes.
+__host__ __device__ constexpr uint32_t instr_desc8(int m, int n, bool wide)
+{
+    return 1u << 4 | (wide ? 1u << 7 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
+}
 __device__ __forceinline__ void mma_ss8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
 {
     asm volatile(
@@ -179,6 +182,15 @@ __device__ __forceinline__ uint32_t codes4(float2 f, float2 g)
         : "f"(f.x), "f"(f.y), "f"(g.x), "f"(g.y));
     return d;
 }
+// Four numbers to E5M2.
+__device__ __forceinline__ uint32_t wide_codes4(float2 f, float2 g)
+{
+    uint32_t d;
+    asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e5m2x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e5m2x2.f32 b, %4, %3;\n\tmov.b32 %0, {a, b};\n\t}"
+        : "=r"(d)
+        : "f"(f.x), "f"(f.y), "f"(g.x), "f"(g.y));
+    return d;
+}
 __device__ __forceinline__ void values4(uint32_t codes, float2& f, float2& g)
 {
     uint32_t a, b;
@@ -188,9 +200,12 @@ __device__ __forceinline__ void values4(uint32_t codes, float2& f, float2& g)
 }
 
 // A query row of 128 bf16 elements in shared memory (two runs of 128 bytes, swizzled by the row) becomes, in place, two rows of
-// E4M3: x 2^e = a + b, a rounded to four bits, b what is left.  2^e brings the largest element to 128 .. 256; a bf16 number has
-// eight bits, so a + b is exact down to 2^-10 of the largest element and off by at most 2^-18 of it below -- less than what
-// bf16 itself leaves of such an element next to it.  Returns 2^-e, and of a row with an infinite element (a code stands for its sign)
+// 8-bit numbers: x 2^e = a + b, a rounded to E4M3, b what is left, to E5M2.  2^e brings the largest element to 128 .. 256.  A bf16
+// number has eight bits; where a is a normal number of four, b has at most three, which E5M2 holds down to 2^-16: a + b is exact down
+// to 2^-13 of the largest element.  Below, b is at most 2^-10 and off by 2^-14: 2^-21 of the largest element.  (With b in E4M3 too, whose
+// step ends at 2^-9, it was 2^-18, and one channel 1000 or 3000 times the others cost them: out over 4096 keys off by 2.6e-3 and 9.0e-3
+// of its norm, so 1.65e-3 with either -- its own rounding; lse of five keys 4.5e-3 and 2.4e-2, so 9e-5 and 6e-4; the same time.)
+// Returns 2^-e, and of a row with an infinite element (a code stands for its sign)
 // infinity: its scores are infinite, or NaN against keys of zero, as they would be of the queries as given.
 __device__ __forceinline__ float split_row(uint8_t* q, int row)
 {
@@ -215,7 +230,7 @@ __device__ __forceinline__ float split_row(uint8_t* q, int row)
             g = mul2(g, make_float2(up, up));
             a[i] = codes4(f, g);
             values4(a[i], r, t);
-            b[i] = codes4(make_float2(f.x - r.x, f.y - r.y), make_float2(g.x - t.x, g.y - t.y));
+            b[i] = wide_codes4(make_float2(f.x - r.x, f.y - r.y), make_float2(g.x - t.x, g.y - t.y));
         }
         at[0][c ^ (row & 7)] = make_uint4(a[0], a[1], a[2], a[3]);
         at[1][c ^ (row & 7)] = make_uint4(b[0], b[1], b[2], b[3]);
@@ -908,7 +923,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
         W walk(a);
         Segment g;
         constexpr uint32_t kQK = instr_desc(kRows, KEYS, false), kPV = instr_desc(kRows, D, true), kPVt = instr_desc(kRows, D, false) & ~(1u << 7 | 1u << 10);  // (fp16)
-        constexpr uint32_t kQK8 = instr_desc8(kRows, KEYS);
+        constexpr uint32_t kQK8 = instr_desc8(kRows, KEYS, false), kQK8Wide = instr_desc8(kRows, KEYS, true);
         int used[2] = {0, 0};               // P tiles multiplied so far (SUBS 1: used[0])
         int base = 0, dbase = 0;            // stages and decoded tiles so far
         int segs[2] = {0, 0}, split[2] = {0, 0};  // segments of each sub-tile, those whose queries were split
@@ -953,7 +968,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkArgs a, const __grid_constan
                     if (elect_one()) {
 #pragma unroll
                         for (int x = 0; x < 8; ++x)  // the queries' first and second parts
-                            mma_ss8(to, q + ((x / 4 * kQBlock + x % 4 * 32) >> 4), k + (x % 4 * 32 >> 4), kQK8, x > 0);
+                            mma_ss8(to, q + ((x / 4 * kQBlock + x % 4 * 32) >> 4), k + (x % 4 * 32 >> 4), x < 4 ? kQK8 : kQK8Wide, x > 0);
                         commit(smem_u32(&sh.s_full[place]));
                     }
                 } else if (elect_one()) {

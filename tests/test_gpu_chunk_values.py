@@ -1,8 +1,16 @@
-"""Attention of chunks where the queries' values are those of no standard normal row."""
+"""Attention of chunks where the queries' values are not those of a standard normal row: one channel far above the others, infinities
+and NaN.
+
+Tolerances.  An 8-bit cache takes the queries as two numbers, E4M3 and E5M2, at a power of two that brings a row's largest element to
+128 .. 256.  Four bits go to the first; what is left has three or fewer while the element is 2^-13 of the largest or more, which E5M2
+holds; below, the first is a multiple of 2^-9, and what it leaves, 2^-10 at most, is rounded to three bits, by 2^-14 at most: 2^-21 of the
+largest element.  So a score is off by at most 2^-21 max |q| sum |k| / sqrt(D), and, as a sum of D products in fp32, by (D + 4) 2^-24 of
+sum |q k| / sqrt(D).  lse is off by as much as its scores, by 2^-15 of the exponentials and their sum, and by its own rounding; a weight
+relatively by twice as much (numerator and sum)."""
 import pytest
 import torch
 
-from test_gpu_chunks import build, hz, reference  # noqa: F401
+from test_gpu_chunks import as_held, build, hz, reference  # noqa: F401
 from test_gpu_parity import rand_bf16
 
 pytestmark = pytest.mark.gpu
@@ -24,6 +32,34 @@ def with_channel(hz, dev, lens, counts, fp8, cached, own, mask="10", cap=0.0, se
     q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
     k[..., CHANNEL] = own
     return cache, slots, rows, q, k, v
+
+
+@pytest.mark.parametrize("factor", [300.0, 1000.0, -3000.0])
+@pytest.mark.parametrize("lens,counts", [([5, 3, 70, 1], [3, 1, 4, 8]), ([5, 129], [300, 1]), ([64, 3], [33, 9])])
+def test_queries_with_one_large_channel(hz, cuda_device, factor, lens, counts):  # noqa: F811
+    """The channel is the same in all cached keys, so that it has no say in their weights; the chunk's own keys have it the other way round, so
+    that the weights are those of the scores from the 8-bit codes."""
+    sign = 1.0 if factor > 0 else -1.0
+    cache, slots, rows, q, k, v = with_channel(hz, cuda_device, lens, counts, True, sign, -sign)
+    q[..., CHANNEL] = factor
+    out, lse = cache.attend_chunks(0, slots, counts, q, k, v)
+    assert cache.status() == 0
+    ref, size, ref_lse, top = reference(q, rows, (k, v), lens, counts, "10", 16, 112, 0, None, True)
+    # sum |k| and sum |q k| of the largest key of each sequence
+    big, both, at = torch.zeros_like(ref_lse), torch.zeros_like(ref_lse), 0
+    for (kk, _), m in zip(rows, counts):
+        held = as_held(kk, True, 2, 0).abs()
+        rows_q = q[at:at + m].double().abs().view(m, 2, 4, 128)
+        big[at:at + m] = held.sum(-1).amax(0).repeat_interleave(4)
+        both[at:at + m] = torch.einsum("ihgd,jhd->ihgj", rows_q, held).amax(-1).reshape(m, 8)
+        at += m
+    score = (2.0 ** -21 * abs(factor) * big + 132 * 2.0 ** -24 * both) / 128 ** 0.5
+    err = (lse.double() - ref_lse).abs()
+    bound = score + 2.0 ** -15 + 2.0 ** -22 * (ref_lse.abs() + top)
+    assert bool((err <= bound).all()), float((err / bound).max())
+    err = (out.double() - ref).abs()
+    bound = (2.0 ** -8 + 2.0 ** -14 + 2 * score[..., None]) * size + 2.0 ** -8 * ref.abs() + 1e-6
+    assert bool((err <= bound).all()), float((err / bound).max())
 
 
 BAD = [float("inf"), float("-inf"), float("nan")]

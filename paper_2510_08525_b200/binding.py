@@ -143,6 +143,7 @@ def _ptr(x) -> int:
 class Handle(int):
     """The address of a cache or prompt handle, with the shape and the GPU it was created with: what a call reads and writes
     goes by them, so they are what the call's arrays are checked against.  (An address alone, like a tensor's, is taken as it is.)"""
+    norms = None, None  # weights of the queries' and of the keys' norm, None: not set
 
 
 def _handle(address, layers, kv_heads, q_heads, head_dim) -> Handle:
@@ -607,7 +608,8 @@ def _set_norms(call, handle, q_weight, k_weight, eps) -> None:
             raise ValueError("a norm's weights are fp32 [layers][head_dim]")
     _check(call(handle, _ptr(q_weight), _ptr(k_weight), float(eps)))
     if isinstance(handle, Handle):
-        handle.norms = q_weight, k_weight  # (the launches read them: they live as long as the handle, or until others are set)
+        # (the launches read them: they live as long as the handle, or until others are set)
+        handle.norms = tuple(None if isinstance(w, int) and not w else w for w in (q_weight, k_weight))
 
 
 def rlkv_paged_set_norms(cache, q_weight, k_weight, eps=1e-6) -> None:

@@ -296,10 +296,10 @@ class PromptAttention:
         return q_out, k_out
 
     def rotate_backward(self, layer, q, k, dq_out, dk_out, positions=None, weights=True):
-        """Returns dq, dk and, with `weights`, the gradients of the norms' weights."""
+        """Returns dq, dk and, with `weights`, the gradients of the queries' and the keys' norm (None of one that is not set)."""
         _check_rows(self, q, k, k)
         dq, dk = (torch.zeros(x.shape, dtype=torch.bfloat16, device=self.device) for x in (q, k))
-        dw = [torch.empty(self.head_dim, dtype=torch.float32, device=self.device) for _ in range(2)] if weights else [None, None]
+        dw = [torch.empty(self.head_dim, dtype=torch.float32, device=self.device) if weights and w is not None else None for w in self.handle.norms]
         rl.rlkv_prompt_rotate_backward(self.handle, layer, q, k, positions, dq_out, dk_out, dq, dk, *dw)
         return (dq, dk, *dw) if weights else (dq, dk)
 

@@ -1,0 +1,32 @@
+"""PromptAttention.rotate and rotate_backward as a model calls them: whichever of rotation and norms it has."""
+import pytest
+import torch
+
+from test_gpu_norm_rotary import EPS, backward64, hz, weights  # noqa: F401
+from test_gpu_parity import rand_bf16
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("norms,rot", [("qk", 128), ("q", 128), ("k", 64), ("", 128), ("q", 0), ("k", 0)])
+def test_gradients_of_the_norms_that_are_set(hz, cuda_device, norms, rot):  # noqa: F811
+    """The default call returns the gradient of each norm that is set and None of the others (tolerances: test_gpu_norm_rotary)."""
+    dev, n, Hq, Hkv, D = cuda_device, 70, 8, 2, 128
+    p = hz.PromptAttention(1, Hkv, Hq, D, n, [1] * Hkv, 4, 60, device=dev)
+    if rot:
+        p.set_rotary(hz.rotary_table(n, rot, device=dev), rot)
+    qw, kw = weights(1, D, 5, dev)
+    qw, kw = qw if "q" in norms else None, kw if "k" in norms else None
+    p.set_norms(qw, kw, EPS)
+    q, k = rand_bf16((n, Hq, D), 1).to(dev), rand_bf16((n, Hkv, D), 2).to(dev)
+    dq_out, dk_out = rand_bf16((n, Hq, D), 3).to(dev), rand_bf16((n, Hkv, D), 4).to(dev)
+    dq, dk, dqw, dkw = p.rotate_backward(0, q, k, dq_out, dk_out)
+    pos = torch.arange(n).numpy()
+    for x, w, dy, dx, dw in ((q, qw, dq_out, dq, dqw), (k, kw, dk_out, dk, dkw)):
+        want, size, want_w, size_w = backward64(x, None if w is None else w[0], pos, rot, False, dy)
+        assert bool(((dx.double().cpu() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -19 * size + 2.0 ** -133).all())
+        assert (dw is None) == (w is None)
+        if w is not None:
+            terms = x.shape[0] * x.shape[1]
+            assert bool(((dw.double().cpu() - want_w).abs() <= ((terms / 256 + 32) * 2.0 ** -24 + 2.0 ** -19) * size_w + 1e-30).all())
+    assert all(torch.equal(a, b) for a, b in zip(p.rotate_backward(0, q, k, dq_out, dk_out, weights=False), (dq, dk)))

@@ -144,6 +144,7 @@ class Handle(int):
     """The address of a cache or prompt handle, with the shape and the GPU it was created with: what a call reads and writes
     goes by them, so they are what the call's arrays are checked against.  (An address alone, like a tensor's, is taken as it is.)"""
     norms = None, None  # weights of the queries' and of the keys' norm, None: not set
+    positions = None    # rows of a prompt handle's table of angles, None: no rotation
 
 
 def _handle(address, layers, kv_heads, q_heads, head_dim) -> Handle:
@@ -779,7 +780,7 @@ def rlkv_prompt_set_rotary(prompt, table, positions, rot_dim, interleaved=False)
     _check_table(table, min(rot_dim, 128), positions)
     _check(lib.rlkv_prompt_set_rotary(prompt, _ptr(table), positions, rot_dim, int(bool(interleaved))))
     if isinstance(prompt, Handle):
-        prompt.rotary = table
+        prompt.rotary, prompt.positions = table, positions if _ptr(table) else None
 
 
 def rlkv_prompt_set_norms(prompt, q_weight, k_weight, eps=1e-6) -> None:

@@ -288,17 +288,23 @@ class PromptAttention:
         """As PagedCache.set_norms."""
         rl.rlkv_prompt_set_norms(self.handle, q_weight, k_weight, eps)
 
+    def _results(self, q, k, positions):
+        """Memory for rows like q's and k's; cleared where a token's position may be of no document, whose rows the kernels leave."""
+        past = self.handle.positions is not None and q.shape[0] > self.handle.positions
+        new = torch.empty if positions is None and not past else torch.zeros
+        return [new(x.shape, dtype=torch.bfloat16, device=self.device) for x in (q, k)]
+
     def rotate(self, layer, q, k, positions=None):
-        """q and k normalised and rotated by their positions (int32; rows of tokens at negative ones are zero)."""
+        """q and k normalised and rotated by their positions (int32; rows of tokens at negative ones, or past the table, are zero)."""
         _check_rows(self, q, k, k)
-        q_out, k_out = (torch.zeros(x.shape, dtype=torch.bfloat16, device=self.device) for x in (q, k))
+        q_out, k_out = self._results(q, k, positions)
         rl.rlkv_prompt_rotate(self.handle, layer, q, k, positions, q_out, k_out)
         return q_out, k_out
 
     def rotate_backward(self, layer, q, k, dq_out, dk_out, positions=None, weights=True):
         """Returns dq, dk and, with `weights`, the gradients of the queries' and the keys' norm (None of one that is not set)."""
         _check_rows(self, q, k, k)
-        dq, dk = (torch.zeros(x.shape, dtype=torch.bfloat16, device=self.device) for x in (q, k))
+        dq, dk = self._results(q, k, positions)
         dw = [torch.empty(self.head_dim, dtype=torch.float32, device=self.device) if weights and w is not None else None for w in self.handle.norms]
         rl.rlkv_prompt_rotate_backward(self.handle, layer, q, k, positions, dq_out, dk_out, dq, dk, *dw)
         return (dq, dk, *dw) if weights else (dq, dk)

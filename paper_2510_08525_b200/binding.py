@@ -159,7 +159,7 @@ def _stream(s, of=None, x=None) -> int:
     """A stream's handle.  None: the current stream of the call's GPU, so that the calls on one cache go to one stream -- that of
     `of`, a Handle or a tensor in device memory, else that of the tensor x, else the current device."""
     if s is None:
-        device = of.device if type(of) is Handle else None
+        device = of.device if isinstance(of, Handle) else None
         if device is None:
             device = _gpu_of(of)
             if device is None:
@@ -503,7 +503,7 @@ def _on_device(x) -> bool:
 def _shape_of(handle, x):
     """q_heads, kv_heads, head_dim and GPU that a call's tensors are held to: the handle's; of an address alone no heads are known
     (0), and the GPU is that of the tensor x (None where x is an address too)."""
-    if type(handle) is Handle:
+    if isinstance(handle, Handle):
         return handle.q_heads, handle.kv_heads, handle.head_dim, handle.device
     return 0, 0, 0, _gpu_of(x)
 
@@ -631,7 +631,7 @@ def _chunks(slots, counts, *more):
 
 def _width(handle, heads, of):
     """Elements of a token's rows: the handle's, or those of a tensor."""
-    if type(handle) is Handle:
+    if isinstance(handle, Handle):
         return getattr(handle, heads) * handle.head_dim
     return 0 if of is None or isinstance(of, int) else of.shape[1] * of.shape[2]
 

@@ -245,6 +245,15 @@ int rlkv_prompt_set_norms(rlkv_prompt* p, const float* q_weight, const float* k_
     return RLKV_OK;
 }
 
+// Strides of rows of queries and keys: 0 stands for contiguous tokens, 2^30 elements are the most, so that no token's offset leaves 64 bits.
+static bool row_strides(const rlkv_prompt* p, int64_t& q_stride, int64_t& k_stride)
+{
+    const int64_t q_row = (int64_t)p->q_heads * p->head_dim, kv_row = (int64_t)p->kv_heads * p->head_dim, most = (int64_t)1 << 30;
+    if (!q_stride) q_stride = q_row;
+    if (!k_stride) k_stride = kv_row;
+    return q_stride >= q_row && k_stride >= kv_row && q_stride % 8 == 0 && k_stride % 8 == 0 && q_stride <= most && k_stride <= most;
+}
+
 // What the two directions share.
 static int norm_rotary_args(const rlkv_prompt* p, int layer, const void* q, int64_t q_stride, const void* k, int64_t k_stride, int tokens,
                             const int* positions, NormRotaryArgs& a)
@@ -253,10 +262,7 @@ static int norm_rotary_args(const rlkv_prompt* p, int layer, const void* q, int6
         (reinterpret_cast<uintptr_t>(positions) & 3))
         return RLKV_EINVAL;
     if (!p->rotary && !p->q_norm && !p->k_norm) return RLKV_EINVAL;
-    const int64_t q_row = (int64_t)p->q_heads * p->head_dim, kv_row = (int64_t)p->kv_heads * p->head_dim;
-    if (!q_stride) q_stride = q_row;
-    if (!k_stride) k_stride = kv_row;
-    if (q_stride < q_row || k_stride < kv_row || q_stride % 8 || k_stride % 8) return RLKV_EINVAL;
+    if (!row_strides(p, q_stride, k_stride)) return RLKV_EINVAL;
     memset(&a, 0, sizeof a);
     a.q = static_cast<const __nv_bfloat16*>(q);
     a.k = static_cast<const __nv_bfloat16*>(k);
@@ -302,10 +308,7 @@ int rlkv_prompt_rotate_backward(rlkv_prompt* p, int layer, const void* q, int64_
     if (!dq_out || !dk_out || !dq || !dk || !aligned16(dq_out) || !aligned16(dk_out) || !aligned16(dq) || !aligned16(dk)) return RLKV_EINVAL;
     if ((reinterpret_cast<uintptr_t>(dq_weight) | reinterpret_cast<uintptr_t>(dk_weight)) & 3) return RLKV_EINVAL;
     if ((dq_weight && !p->q_norm) || (dk_weight && !p->k_norm)) return RLKV_EINVAL;
-    const int64_t q_row = (int64_t)p->q_heads * p->head_dim, kv_row = (int64_t)p->kv_heads * p->head_dim;
-    if (!dq_stride) dq_stride = q_row;
-    if (!dk_stride) dk_stride = kv_row;
-    if (dq_stride < q_row || dk_stride < kv_row || dq_stride % 8 || dk_stride % 8) return RLKV_EINVAL;
+    if (!row_strides(p, dq_stride, dk_stride)) return RLKV_EINVAL;
     a.dq_out = static_cast<const __nv_bfloat16*>(dq_out);
     a.dk_out = static_cast<const __nv_bfloat16*>(dk_out);
     a.dq = static_cast<__nv_bfloat16*>(dq);

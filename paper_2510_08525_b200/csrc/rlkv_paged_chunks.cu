@@ -141,15 +141,20 @@ int plan_chunks(ChunkArgs& a, int shape, int max_ctas, int min_tiles, int extra)
 // has 100 (2048 on 8192 280 and 282, under the power cap 320 and 315, a prompt of 8192 497 and 490); but 512 on 8192 78 and 81, four
 // times 512 on 3400 111 and 117.
 constexpr long long kNearL2 = 80ll << 20;
+// Key rows that a chunk of m tokens meets over all heads, on average over its tokens: of a ring no more than the sequence has.
+long long key_rows(const ChunkArgs& a, int len, int m)
+{
+    const long long held = (long long)len + m / 2, ring = a.sink + a.window;
+    return a.n_full * held + a.n_comp * (held < ring ? held : ring);
+}
 int choose_shape(const ChunkArgs& a, int sms, int head_dim, bool fp8)
 {
-    const long long ring = a.sink + a.window;
     long long small = 0, large = 0, shared = 0;  // key rows times row tiles of 128; rows that several of these read
     bool few = true;
     for (int i = 0; i < a.seqs.n; ++i) {
         const int m = a.seqs.count[i];
         if (m > chunk_tokens(0, a.group)) few = false;
-        const long long rows = (long long)a.n_full * (a.seqs.len[i] + m / 2) + (long long)a.n_comp * ring;
+        const long long rows = key_rows(a, a.seqs.len[i], m);
         const int tiles = (int)(((long long)m * a.group + 127) / 128);
         (tiles > 1 ? large : small) += rows * tiles;
         if (tiles > 1) shared += rows;
@@ -169,7 +174,7 @@ bool two_launches(const ChunkSeqs& s, const ChunkArgs& a, int sms, bool fp8)
     long long few = 0, more = 0;  // key rows times row tiles of 128
     for (int i = 0; i < s.n; ++i) {
         const int m = s.start[i + 1] - s.start[i];
-        const long long rows = (long long)a.n_full * (s.len[i] + m / 2) + (long long)a.n_comp * (a.sink + a.window);
+        const long long rows = key_rows(a, s.len[i], m);
         if (m > 0) (m * a.group <= 32 ? few : more) += rows * (((long long)m * a.group + 127) / 128);
     }
     return few / 256 >= 6ll * sms && more / 256 >= 2ll * sms;

@@ -86,3 +86,13 @@ def test_refusals(binding):
         assert e.value.code == binding.RLKV_EINVAL
     with pytest.raises(binding.RlkvError):
         binding.rlkv_debug_chunk_plan([1], [1], 1, 0, 4, 0, 1, 1, 297)
+
+
+@pytest.mark.parametrize("shape", [-1, -2])
+@pytest.mark.parametrize("lens,counts", [([0] * 16, [240] * 16), ([0, 30, 5, 100], [700, 1, 90, 33]), ([100] * 40, [1] * 39 + [300])])
+def test_a_window_that_no_query_reaches_changes_nothing(binding, lens, counts, shape):
+    """A sequence is counted with the rows it has, not with those its rings have room for."""
+    reach = max(n + m for n, m in zip(lens, counts))
+    plans = [binding.rlkv_debug_chunk_plan(lens, counts, 2, 6, 4, 16, window, shape) for window in (reach, reach + 1, 4 * reach, 20000)]
+    for plan in plans[1:]:
+        np.testing.assert_array_equal(plans[0], plan)

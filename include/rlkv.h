@@ -245,7 +245,8 @@ int rlkv_step_host(rlkv_cache* cache, const void* k_host, const void* v_host, co
  * decode step can serve any subset of the open slots, each at its own length.
  * Limits: max_seq_len <= 65536 tokens; at most min(max_seqs, 512) sequences per call; the other
  * shape limits of rlkv_cache_create.  Device memory: rlkv_paged_size bytes, library- or caller-owned
- * as for rlkv_cache_create.  Errors leave the cache unchanged. */
+ * as for rlkv_cache_create; and, of a cache that attends chunks (rlkv_paged_chunk_attention), their scratch, see
+ * rlkv_paged_set_chunk_scratch.  Errors leave the cache unchanged. */
 typedef struct rlkv_paged rlkv_paged;
 int rlkv_paged_size(int layers, int kv_heads, int q_heads, int head_dim, int max_seqs, int n_pages,
                     int max_seq_len, const uint8_t* head_is_full, int sink, int window,
@@ -347,14 +348,21 @@ int rlkv_paged_rotate_chunks(rlkv_paged* cache, int layer, const int* slots, con
  * that its first tokens see.)  Scores as rlkv_paged_set_scores says.  The chunk's own keys and values are taken as they are given,
  * those of an 8-bit cache as it holds them.  The cache does not change; a sequence may hold nothing yet.
  * out: device bf16 [tokens][q_heads][head_dim] (fp32 accumulation, rounded once); lse: device fp32 [tokens][q_heads], log sum
- * exp(score), or NULL.  Every sum has a fixed order: the same call on the same cache gives the same bits.  (What a call keeps
- * between its CTAs lies in 39 MB -- 20 at head_dim 64 -- that rlkv_paged_create allocates beside the cache's buffer; if it cannot, the
- * decode launches' scratch serves, and large calls use fewer CTAs.)  Values of a sequence's own rows are
+ * exp(score), or NULL.  Every sum has a fixed order: the same call on the same cache gives the same bits.  Values of a sequence's own rows are
  * assumed finite; what rows of other sequences or of pages' unused parts hold has no effect.  A query that is not finite gives a
  * result that is not (under a cap an infinite one scores the cap). */
 int rlkv_paged_chunk_attention(rlkv_paged* cache, int layer, const int* slots, const int* counts, int n, const void* q,
                                int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* out,
                                float* lse, void* stream);
+/* What a call keeps between its CTAs: 39 MB for the largest (20 at head_dim 64; rlkv_paged_chunk_scratch_size, whatever the cache holds).
+ * In a cache whose decode launches keep as much it lies in the cache's buffer.  For others the first rlkv_paged_chunk_attention allocates it
+ * beside the buffer, until rlkv_paged_destroy -- in a captured call, too --, unless the caller has given memory of its own; if there is
+ * none left, what the decode launches have serves, with fewer CTAs to a call.
+ * scratch: DEVICE memory of `bytes` bytes on the cache's GPU, 16-byte aligned, the caller's, for this cache's calls alone, to outlive them
+ * and what was captured of them; fewer bytes than rlkv_paged_chunk_scratch_size do, with fewer CTAs to a call (of the same inputs, results
+ * to rounding).  NULL: as without. */
+int rlkv_paged_chunk_scratch_size(const rlkv_paged* cache, size_t* bytes_out);
+int rlkv_paged_set_chunk_scratch(rlkv_paged* cache, void* scratch, size_t bytes);
 /* Appends the chunks: the cache's bytes are those of counts[i] single appends to slots[i].  Pages are taken from the free list
  * sequence by sequence.  RLKV_EFULL (nothing appended for any sequence) if it cannot serve every new page.  A captured call
  * stores its tokens where they belonged at its capture, as often as it is replayed. */

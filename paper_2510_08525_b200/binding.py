@@ -74,6 +74,8 @@ SIGNATURES = {
     "rlkv_paged_set_norms": (_ci, [_vp, _vp, _vp, ctypes.c_float]),
     "rlkv_paged_rotate_chunks": (_ci, [_vp, _ci, _vp, _vp, _ci, _vp, _i64, _vp, _i64, _vp, _vp, _vp]),
     "rlkv_paged_chunk_attention": (_ci, [_vp, _ci, _vp, _vp, _ci, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp]),
+    "rlkv_paged_chunk_scratch_size": (_ci, [_vp, ctypes.POINTER(_sz)]),
+    "rlkv_paged_set_chunk_scratch": (_ci, [_vp, _vp, _sz]),
     "rlkv_paged_append_chunks": (_ci, [_vp, _ci, _vp, _vp, _ci, _vp, _i64, _vp, _i64, _vp]),
     "rlkv_paged_read": (_ci, [_vp, _ci, _vp, _vp, _vp, _ci, _vp, _vp, _vp]),
     "rlkv_paged_decode_attention": (_ci, [_vp, _ci, _vp, _ci, _vp, _vp, _vp]),
@@ -653,6 +655,21 @@ def rlkv_paged_chunk_attention(cache, layer, slots, counts, q, k, v, out, lse=No
     _check(lib.rlkv_paged_chunk_attention(cache, layer, _host(s), _host(m), s.size, *_rows(q, n, hq, d, gpu), *_rows(k, n, hkv, d, gpu),
                                           *_rows(v, n, hkv, d, gpu), _room(out, n * width, gpu=gpu),
                                           _room(lse, n * width // d if d else 0, "float32", gpu), _stream(stream, cache, k)))
+
+
+def rlkv_paged_chunk_scratch_size(cache) -> int:
+    out = _sz(0)
+    _check(lib.rlkv_paged_chunk_scratch_size(cache, ctypes.byref(out)))
+    return int(out.value)
+
+
+def rlkv_paged_set_chunk_scratch(cache, scratch, nbytes=None) -> None:
+    """scratch: a contiguous tensor in the memory of the cache's GPU, an address with its bytes, or None: the library's own."""
+    if nbytes is None:
+        nbytes = 0 if scratch is None else scratch.numel() * scratch.element_size()
+    _check(lib.rlkv_paged_set_chunk_scratch(cache, _ptr(scratch), int(nbytes)))
+    if isinstance(cache, Handle):
+        cache.scratch = scratch  # (the launches write it: it lives as long as the handle, or until another is set)
 
 
 def rlkv_paged_append_chunks(cache, layer, slots, counts, k, v, stream=None) -> None:

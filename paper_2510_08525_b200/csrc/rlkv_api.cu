@@ -802,8 +802,8 @@ int rlkv_cache_create_fp8(rlkv_cache** out, int layers, int kv_heads, int q_head
     }
     c->fp8_staging = c->dev_base + z.paged;
     const int pages = batch * ((max_len + kTile - 1) / kTile);
-    rc = rlkv::paged_create_for_batch(&c->fp8, layers, kv_heads, q_heads, head_dim, batch, pages, max_len, head_is_full, sink,
-                                      window, k_scale, v_scale, c->dev_base, z.paged);
+    rc = rlkv_paged_create_fp8(&c->fp8, layers, kv_heads, q_heads, head_dim, batch, pages, max_len, head_is_full, sink,
+                               window, k_scale, v_scale, c->dev_base, z.paged);
     if (rc) return fail(rc);
     c->fp8_slots.assign(batch, -1);
     for (int b = 0; b < batch; ++b) {

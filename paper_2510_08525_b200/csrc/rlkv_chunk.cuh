@@ -108,7 +108,9 @@ __host__ __device__ constexpr int chunk_keys(int shape) { return shape == 2 ? 12
 __host__ __device__ constexpr int chunk_tokens(int shape, int group) { return shape == 2 ? 2 * (128 / group) : (shape == 1 ? 128 : 32) / group; }
 // Floats of one record: of each sub-tile of R rows (32 or 128) [head_dim / 4][R] float4, then [2][R] maximum and sum.
 __host__ __device__ constexpr long long chunk_record_floats(int head_dim, int shape) { return (shape == 2 ? 256ll : shape == 1 ? 128 : 32) * (head_dim + 2); }
+// Two records a CTA, of the largest launches: kMaxChunkCtas of 128 rows, or half as many of 256.
 inline size_t chunk_record_bytes(int head_dim) { return (size_t)2 * kMaxChunkCtas * chunk_record_floats(head_dim, 1) * sizeof(float); }
+static_assert(chunk_record_floats(128, 2) == 2 * chunk_record_floats(128, 1) && chunk_record_floats(128, 0) <= chunk_record_floats(128, 1), "records");
 
 // Status codes (device error word of the cache): which wait of the chunk kernel ran out.
 enum : int { kChunkWaitLoad = 201, kChunkWaitProduct = 202, kChunkWaitSoftmax = 203, kChunkWaitStage = 204, kChunkWaitDrain = 205,

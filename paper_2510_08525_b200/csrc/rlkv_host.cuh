@@ -123,10 +123,6 @@ namespace rlkv {
 int paged_prefill_strided(rlkv_paged* p, int layer, int slot, const void* k, const void* v, int n_tokens,
                           long long entry_stride, void* stream);
 uint64_t paged_launch_count(const rlkv_paged* p);
-// rlkv_paged_create_fp8 for that cache, which attends no chunks: without their scratch.
-int paged_create_for_batch(rlkv_paged** out, int layers, int kv_heads, int q_heads, int head_dim, int max_seqs, int n_pages, int max_seq_len,
-                           const uint8_t* head_is_full, int sink, int window, const float* k_scale, const float* v_scale,
-                           void* device_buf, size_t device_buf_bytes);
 
 struct DeviceGuard {
     int prev = -1;

@@ -217,7 +217,7 @@ int rlkv_paged_size_fp8(int layers, int kv_heads, int q_heads, int head_dim, int
 
 static int paged_create(rlkv_paged** out, int layers, int kv_heads, int q_heads, int head_dim, int max_seqs, int n_pages,
                         int max_seq_len, const uint8_t* head_is_full, int sink, int window, const float* k_scale,
-                        const float* v_scale, void* device_buf, size_t device_buf_bytes, bool chunks = true)
+                        const float* v_scale, void* device_buf, size_t device_buf_bytes)
 {
     if (!out) return RLKV_EINVAL;
     *out = nullptr;
@@ -309,19 +309,7 @@ static int paged_create(rlkv_paged** out, int layers, int kv_heads, int q_heads,
         if (!rc) rc = encode_byte_rows_tensor_map(&p->map_codes, p->dev_base + p->off_pool8, 128, p->pages8 * 128, kTile);
         if (rc) return fail(rc);
     }
-    // The records of attention on chunks have memory of their own, which the buffer does not count; where there is none left they
-    // share the decode launches' partial records (calls on one cache are ordered), with fewer CTAs to a launch.
-    p->chunk_records = dev_at<float>(p, p->off_partials);
-    p->chunk_bytes = p->total - p->off_partials;
-    if (chunks && chunk_record_bytes(head_dim) > p->chunk_bytes) {
-        void* mem = nullptr;
-        if (cudaMalloc(&mem, chunk_record_bytes(head_dim)) == cudaSuccess) {
-            p->chunk_records = p->own_records = static_cast<float*>(mem);
-            p->chunk_bytes = chunk_record_bytes(head_dim);
-        } else {
-            cudaGetLastError();
-        }
-    }
+    rlkv_paged_set_chunk_scratch(p, nullptr, 0);
     *out = p;
     return RLKV_OK;
 }
@@ -342,19 +330,6 @@ int rlkv_paged_create_fp8(rlkv_paged** out, int layers, int kv_heads, int q_head
     return paged_create(out, layers, kv_heads, q_heads, head_dim, max_seqs, n_pages, max_seq_len, head_is_full, sink, window,
                         k_scale, v_scale, device_buf, device_buf_bytes);
 }
-
-}  // extern "C"
-
-int rlkv::paged_create_for_batch(rlkv_paged** out, int layers, int kv_heads, int q_heads, int head_dim, int max_seqs, int n_pages, int max_seq_len,
-                                 const uint8_t* head_is_full, int sink, int window, const float* k_scale, const float* v_scale,
-                                 void* device_buf, size_t device_buf_bytes)
-{
-    if (!k_scale || !v_scale) return RLKV_EINVAL;
-    return paged_create(out, layers, kv_heads, q_heads, head_dim, max_seqs, n_pages, max_seq_len, head_is_full, sink, window, k_scale, v_scale,
-                        device_buf, device_buf_bytes, false);
-}
-
-extern "C" {
 
 int rlkv_paged_destroy(rlkv_paged* p)
 {

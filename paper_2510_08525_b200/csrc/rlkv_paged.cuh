@@ -33,8 +33,9 @@ struct rlkv_paged {
     size_t off_pool, off_tables, off_head_table, off_layer_desc, off_slopes, off_page_table, off_tickets, off_status, off_partials, total;
     uint8_t* dev_base;
     bool owns_buffer;
-    float *chunk_records, *own_records;  // scratch of rlkv_paged_chunk_attention; what of it has memory of its own (or null)
+    float *chunk_records, *own_records;  // scratch of rlkv_paged_chunk_attention; the library's own, once it is taken (or null)
     size_t chunk_bytes;
+    bool chunk_settled;           // false: the next call that attends chunks takes own_records first
     CUtensorMap tmap;
     uint64_t launches;
     const float* rotary;          // rlkv_paged_set_rotary: the caller's table of angles (device), null: none set

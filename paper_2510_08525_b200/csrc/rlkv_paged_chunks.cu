@@ -194,9 +194,45 @@ void pick_chunks(const ChunkSeqs& s, int group, int pick, ChunkList& l)
     }
 }
 
+// Records for every CTA of a launch, before the first call: memory of the library's own where the decode launches' records, which serve
+// calls on the same cache in turn, take less.  (In a captured call, too: the allocation is no part of the graph.)  Where there is
+// none left those serve, with fewer CTAs to a launch, from then on.
+void settle_scratch(rlkv_paged* p)
+{
+    if (p->chunk_settled) return;
+    p->chunk_settled = true;
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    void* mem = nullptr;
+    if (cudaMalloc(&mem, chunk_record_bytes(p->head_dim)) == cudaSuccess) {
+        p->chunk_records = p->own_records = static_cast<float*>(mem);
+        p->chunk_bytes = chunk_record_bytes(p->head_dim);
+    } else {
+        cudaGetLastError();
+    }
+    cudaThreadExchangeStreamCaptureMode(&mode);
+}
+
 }  // namespace
 
 extern "C" {
+
+int rlkv_paged_chunk_scratch_size(const rlkv_paged* p, size_t* bytes_out)
+{
+    if (!p || !bytes_out) return RLKV_EINVAL;
+    *bytes_out = chunk_record_bytes(p->head_dim);
+    return RLKV_OK;
+}
+
+int rlkv_paged_set_chunk_scratch(rlkv_paged* p, void* scratch, size_t bytes)
+{
+    if (!p || (scratch && !on_device(scratch, p->device))) return RLKV_EINVAL;
+    const size_t all = chunk_record_bytes(p->head_dim), decode = p->total - p->off_partials;
+    p->chunk_settled = scratch || p->own_records || decode >= all;
+    p->chunk_records = scratch ? static_cast<float*>(scratch) : p->own_records ? p->own_records : dev_at<float>(p, p->off_partials);
+    p->chunk_bytes = scratch ? bytes : p->own_records ? all : decode;
+    return RLKV_OK;
+}
 
 int rlkv_paged_set_norms(rlkv_paged* p, const float* q_weight, const float* k_weight, float eps)
 {
@@ -286,6 +322,7 @@ int rlkv_paged_chunk_attention(rlkv_paged* p, int layer, const int* slots, const
     a.slopes = p->biased ? dev_at<float>(p, p->off_slopes) + (size_t)layer * p->q_heads : nullptr;
     a.out = static_cast<__nv_bfloat16*>(out);
     a.lse = lse;
+    settle_scratch(p);
     a.records = p->chunk_records;
     a.status = dev_at<int>(p, p->off_status);
     for (int h = 0; h < p->kv_heads; ++h) {
@@ -297,9 +334,9 @@ int rlkv_paged_chunk_attention(rlkv_paged* p, int layer, const int* slots, const
     auto launch = [&](int pick) -> int {
         pick_chunks(s, a.group, pick, a.seqs);
         const int shape = choose_shape(a, sms, p->head_dim, p->fp8);
-        const long long room = (long long)(p->chunk_bytes / (2 * sizeof(float) * chunk_record_floats(p->head_dim, shape)));  // CTAs it has records for
+        const long long room = (long long)(p->chunk_bytes / (2 * sizeof(float) * chunk_record_floats(p->head_dim, shape)));  // CTAs there are records for
         int ctas = shape == 2 ? sms : 2 * sms;
-        if (ctas > room) ctas = room < 1 ? 1 : (int)room;
+        if (ctas > room) ctas = room < 1 ? 1 : (int)room;  // (one alone cuts no unit: it leaves no record)
         const int pieces = plan_chunks(a, shape, ctas, kMinChunkKeys / chunk_keys(shape), unit_tiles(shape, p->fp8));
         const int keys = chunk_keys(shape);
         ChunkMaps m;

@@ -33,3 +33,11 @@ def test_the_stream_is_that_of_a_derived_handles_gpu(binding, monkeypatch):  # n
     h.device = 3
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 100 + device, raising=False)
     assert binding._stream(None, h) == 103
+
+
+def test_scratch_calls_refuse_without_a_handle(binding):  # noqa: F811
+    for call in (lambda: binding.rlkv_paged_chunk_scratch_size(0), lambda: binding.rlkv_paged_set_chunk_scratch(0, None),
+                 lambda: binding.rlkv_paged_set_chunk_scratch(0, 4096, 1 << 20)):
+        with pytest.raises(binding.RlkvError) as e:
+            call()
+        assert e.value.code == binding.RLKV_EINVAL

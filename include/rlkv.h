@@ -448,12 +448,17 @@ int rlkv_debug_paged_cut(const int* lens, int n, int n_full, int n_comp, int cap
 /* How rlkv_paged_chunk_attention cuts a call's work for at most max_ctas CTAs (up to 296), host arithmetic only: n sequences of
  * lens[i] tokens and counts[i] new ones, n_full full and n_comp compressed heads of `group` query heads.  The work is a flat
  * sequence of key tiles: sequence by sequence, tile of queries by tile, the full heads and then the compressed ones.  shape 0: the
- * queries of 32 / group tokens and 64 keys to a tile, 1: 128 / group and 64, 2: 2 * (128 / group) and 128; -1: as the call would
- * choose on a 16-bit cache of head_dim 128, -2: on an 8-bit one.  CTA c takes the tiles from
+ * queries of 32 / group tokens and 64 keys to a tile, 1: 128 / group and 64, 2: 2 * (128 / group) and 128; -1: the shape that
+ * a call of one launch has on a 16-bit cache of head_dim 128, -2: on an 8-bit one.  A unit's fixed cost is that of a 16-bit cache.  CTA c takes the tiles from
  * at_out[4c..4c+3] = (sequence, query tile, head, key tile) up to at_out[4c+4..4c+7], c < *ctas_out; the last entry names
  * sequence n (host int[4 * (max_ctas + 1)]). */
 int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full, int n_comp, int group, int sink, int window,
                           int shape, int max_ctas, int* ctas_out, int* at_out);
+/* The launches of such a call as it makes them, on a cache of head_dim (64, 128), in 8 bits if fp8, with all the scratch that it can use: how
+ * many there are -- one; two of an 8-bit cache's where small and large chunks are both many, the small first --, and of launch `which` its
+ * shape and its ranges, as above, of the chunks that are in it (host int[4 * 297]). */
+int rlkv_debug_chunk_launch(const int* lens, const int* counts, int n, int n_full, int n_comp, int group, int sink, int window,
+                            int head_dim, int fp8, int which, int* launches_out, int* shape_out, int* ctas_out, int* at_out);
 
 /* ---- attention over whole prompts -------------------------------------------------------------------
  * What a prompt (or a training sample) needs before its tokens are decoded: every token attends the tokens

@@ -96,6 +96,8 @@ SIGNATURES = {
     "rlkv_prompt_rotate_backward": (_ci, [_vp, _ci, _vp, _i64, _vp, _i64, _ci, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp]),
     "rlkv_prompt_kernel_status": (_ci, [_vp, ctypes.POINTER(_ci)]),
     "rlkv_debug_chunk_plan": (_ci, [_vp, _vp, _ci, _ci, _ci, _ci, _ci, _ci, _ci, _ci, ctypes.POINTER(_ci), _vp]),
+    "rlkv_debug_chunk_launch": (_ci, [_vp, _vp, _ci, _ci, _ci, _ci, _ci, _ci, _ci, _ci, _ci, ctypes.POINTER(_ci), ctypes.POINTER(_ci),
+                                      ctypes.POINTER(_ci), _vp]),
     "rlkv_debug_paged_cut": (_ci, [_vp, _ci, _ci, _ci, _ci, _ci, _ci, _ci, _ci, ctypes.POINTER(_ci), ctypes.POINTER(_ci)]),
     "rlkv_debug_paged_schedule": (_ci, [_vp, _ci, _ci, _ci, _ci, _ci, _ci, ctypes.POINTER(_ci), _vp, _vp, _vp]),
 }
@@ -851,6 +853,17 @@ def rlkv_debug_chunk_plan(lens, counts, n_full, n_comp, group, sink, window, sha
     _check(lib.rlkv_debug_chunk_plan(ln.ctypes.data, m.ctypes.data, ln.size, n_full, n_comp, group, sink, window, shape, max_ctas,
                                      ctypes.byref(ctas), at.ctypes.data))
     return at[:ctas.value + 1]
+
+
+def rlkv_debug_chunk_launch(lens, counts, n_full, n_comp, group, sink, window, head_dim=128, fp8=False, which=0):
+    """The number of a call's launches, and of launch `which` its shape and its ranges, as rlkv_debug_chunk_plan returns them."""
+    ln, m, number, shape, ctas = _slots(lens), _slots(counts), _ci(0), _ci(0), _ci(0)
+    if ln.size != m.size:
+        raise ValueError("lens and counts must have an entry for each sequence")
+    at = np.zeros((297, 4), dtype=np.int32)
+    _check(lib.rlkv_debug_chunk_launch(ln.ctypes.data, m.ctypes.data, ln.size, n_full, n_comp, group, sink, window, head_dim, int(bool(fp8)), which,
+                                       ctypes.byref(number), ctypes.byref(shape), ctypes.byref(ctas), at.ctypes.data))
+    return number.value, shape.value, at[:ctas.value + 1]
 
 
 def rlkv_debug_paged_cut(lens, n_full, n_comp, cap, ctas, fp8=False, scored=False, in_step=False):

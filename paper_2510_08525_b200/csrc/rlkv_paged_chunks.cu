@@ -180,18 +180,74 @@ bool two_launches(const ChunkSeqs& s, const ChunkArgs& a, int sms, bool fp8)
     return few / 256 >= 6ll * sms && more / 256 >= 2ll * sms;
 }
 
-// The chunks of a launch, 0: all, 1: those of at most 32 rows, 2: the others; empty ones in none.
-void pick_chunks(const ChunkSeqs& s, int group, int pick, ChunkList& l)
+// The chunks of a launch, 0: all, 1: those of at most 32 rows, 2: the others; empty ones in none.  entries: where each stands in the call
+// (or null).
+void pick_chunks(const ChunkSeqs& s, int group, int pick, ChunkList& l, int* entries)
 {
     l.n = 0;
     for (int i = 0; i < s.n; ++i) {
         const int m = s.start[i + 1] - s.start[i];
         if (m == 0 || (pick && (m * group <= 32) != (pick == 1))) continue;
+        if (entries) entries[l.n] = i;
         l.start[l.n] = s.start[i];
         l.count[l.n] = m;
         l.len[l.n] = s.len[i];
         l.slot[l.n++] = s.slot[i];
     }
+}
+
+// Launch `which` of a call's (two: the small chunks and the others): its chunks, its shape and its CTAs' ranges, with records in `bytes`.
+struct Cut {
+    int shape, pieces;
+};
+Cut cut_launch(const ChunkSeqs& s, ChunkArgs& a, bool two, int which, int sms, int head_dim, bool fp8, size_t bytes, int* entries)
+{
+    Cut c;
+    pick_chunks(s, a.group, two ? 1 + which : 0, a.seqs, entries);
+    c.shape = choose_shape(a, sms, head_dim, fp8);
+    const long long room = (long long)(bytes / (2 * sizeof(float) * chunk_record_floats(head_dim, c.shape)));  // CTAs there are records for
+    int ctas = c.shape == 2 ? sms : 2 * sms;
+    if (ctas > room) ctas = room < 1 ? 1 : (int)room;  // (one alone cuts no unit: it leaves no record)
+    c.pieces = plan_chunks(a, c.shape, ctas, kMinChunkKeys / chunk_keys(c.shape), unit_tiles(c.shape, fp8));
+    return c;
+}
+
+// A boundary per CTA and the end, four numbers each; sequences as in the call.
+void write_ranges(const ChunkArgs& a, const int* entries, int n, int* at_out)
+{
+    for (int c = 0; c <= a.ctas; ++c) {
+        const int seq = a.at[c].seq;
+        at_out[4 * c] = !entries ? seq : seq < a.seqs.n ? entries[seq] : n;
+        at_out[4 * c + 1] = a.at[c].row_tile;
+        at_out[4 * c + 2] = a.at[c].head;
+        at_out[4 * c + 3] = a.at[c].tile;
+    }
+}
+
+// The arguments that the two below share, checked.
+int debug_args(const int* lens, const int* counts, int n, int n_full, int n_comp, int group, int sink, int window, ChunkSeqs& s, ChunkArgs& a)
+{
+    if (!lens || !counts || n < 1 || n > kMaxPagedBatch || n_full < 0 || n_comp < 0 || n_full + n_comp < 1 || group < 1 || group > kMaxGroup ||
+        sink < 0 || window < 1)
+        return RLKV_EINVAL;
+    s.n = n;
+    long long total = 0;
+    for (int i = 0; i < n; ++i) {
+        if (lens[i] < 0 || counts[i] < 0) return RLKV_EINVAL;
+        s.len[i] = lens[i];
+        s.start[i] = (int)total;
+        s.slot[i] = 0;
+        total += counts[i];
+        if (total > kMaxChunkTokens) return RLKV_EINVAL;
+    }
+    if (total < 1) return RLKV_EINVAL;
+    s.start[n] = (int)total;
+    a.n_full = n_full;
+    a.n_comp = n_comp;
+    a.group = group;
+    a.sink = sink;
+    a.window = window;
+    return RLKV_OK;
 }
 
 // Records for every CTA of a launch, before the first call: memory of the library's own where the decode launches' records, which serve
@@ -331,28 +387,21 @@ int rlkv_paged_chunk_attention(rlkv_paged* p, int layer, const int* slots, const
         a.v_scale[h] = p->fp8 ? p->v_scale[(size_t)layer * p->kv_heads + h] : 1.f;
     }
     const int sms = p->sm_count < kMaxChunkCtas / 2 ? p->sm_count : kMaxChunkCtas / 2;
-    auto launch = [&](int pick) -> int {
-        pick_chunks(s, a.group, pick, a.seqs);
-        const int shape = choose_shape(a, sms, p->head_dim, p->fp8);
-        const long long room = (long long)(p->chunk_bytes / (2 * sizeof(float) * chunk_record_floats(p->head_dim, shape)));  // CTAs there are records for
-        int ctas = shape == 2 ? sms : 2 * sms;
-        if (ctas > room) ctas = room < 1 ? 1 : (int)room;  // (one alone cuts no unit: it leaves no record)
-        const int pieces = plan_chunks(a, shape, ctas, kMinChunkKeys / chunk_keys(shape), unit_tiles(shape, p->fp8));
-        const int keys = chunk_keys(shape);
+    const bool two = two_launches(s, a, sms, p->fp8);
+    for (int which = 0; which < 1 + two; ++which) {
+        const Cut cut = cut_launch(s, a, two, which, sms, p->head_dim, p->fp8, p->chunk_bytes, nullptr);
+        const int keys = chunk_keys(cut.shape);
         ChunkMaps m;
-        int e = encode_heads_map(&m.q, q, total, p->q_heads, p->head_dim, q_stride, a.group, (shape == 0 ? 32 : 128) / a.group);
+        int e = encode_heads_map(&m.q, q, total, p->q_heads, p->head_dim, q_stride, a.group, (cut.shape == 0 ? 32 : 128) / a.group);
         if (!e) e = encode_heads_map(&m.k, k, total, p->kv_heads, p->head_dim, k_stride, 1, keys);
         if (!e) e = encode_heads_map(&m.v, v, total, p->kv_heads, p->head_dim, v_stride, 1, keys);
         if (!e && !p->fp8) e = encode_heads_map(&m.pool, dev_at<__nv_bfloat16>(p, p->off_pool), p->pool_rows, 1, p->head_dim, p->head_dim, 1, kTile);
-        else if (!e) m.pool = shape == 2 ? p->map_codes : p->map_k;
+        else if (!e) m.pool = cut.shape == 2 ? p->map_codes : p->map_k;
         if (e) return e;
-        RLKV_CUDA(launch_chunk_attention(a, m, p->head_dim, shape, pieces, static_cast<cudaStream_t>(stream)));
-        p->launches += pieces > 1 ? 2 : 1;
-        return RLKV_OK;
-    };
-    if (!two_launches(s, a, sms, p->fp8)) return launch(0);
-    const int e = launch(1);
-    return e ? e : launch(2);
+        RLKV_CUDA(launch_chunk_attention(a, m, p->head_dim, cut.shape, cut.pieces, static_cast<cudaStream_t>(stream)));
+        p->launches += cut.pieces > 1 ? 2 : 1;
+    }
+    return RLKV_OK;
 }
 
 int rlkv_paged_append_chunks(rlkv_paged* p, int layer, const int* slots, const int* counts, int n, const void* k, int64_t k_stride,
@@ -448,35 +497,40 @@ int rlkv_paged_read(rlkv_paged* p, int layer, const int* slots, const int* first
 int rlkv_debug_chunk_plan(const int* lens, const int* counts, int n, int n_full, int n_comp, int group, int sink, int window, int shape,
                           int max_ctas, int* ctas_out, int* at_out)
 {
-    if (!lens || !counts || n < 1 || n > kMaxPagedBatch || n_full < 0 || n_comp < 0 || n_full + n_comp < 1 || group < 1 || group > kMaxGroup ||
-        sink < 0 || window < 1 || max_ctas < 1 || max_ctas > kMaxChunkCtas || !ctas_out || !at_out)
-        return RLKV_EINVAL;
+    if (max_ctas < 1 || max_ctas > kMaxChunkCtas || !ctas_out || !at_out) return RLKV_EINVAL;
+    ChunkSeqs s;
     ChunkArgs a;
+    const int rc = debug_args(lens, counts, n, n_full, n_comp, group, sink, window, s, a);
+    if (rc) return rc;
     a.seqs.n = n;
-    long long total = 0;
     for (int i = 0; i < n; ++i) {
-        if (lens[i] < 0 || counts[i] < 0) return RLKV_EINVAL;
         a.seqs.len[i] = lens[i];
-        a.seqs.start[i] = (int)total;
+        a.seqs.start[i] = s.start[i];
         a.seqs.count[i] = counts[i];
-        total += counts[i];
-        if (total > kMaxChunkTokens) return RLKV_EINVAL;
     }
-    if (total < 1) return RLKV_EINVAL;
-    a.n_full = n_full;
-    a.n_comp = n_comp;
-    a.group = group;
-    a.sink = sink;
-    a.window = window;
     if (shape < 0) shape = choose_shape(a, kMaxChunkCtas / 2, 128, shape == -2);
     if (shape > 2) return RLKV_EINVAL;
     plan_chunks(a, shape, max_ctas, kMinChunkKeys / chunk_keys(shape), unit_tiles(shape, false));
-    for (int c = 0; c <= a.ctas; ++c) {
-        at_out[4 * c] = a.at[c].seq;
-        at_out[4 * c + 1] = a.at[c].row_tile;
-        at_out[4 * c + 2] = a.at[c].head;
-        at_out[4 * c + 3] = a.at[c].tile;
-    }
+    write_ranges(a, nullptr, n, at_out);
+    *ctas_out = a.ctas;
+    return RLKV_OK;
+}
+
+int rlkv_debug_chunk_launch(const int* lens, const int* counts, int n, int n_full, int n_comp, int group, int sink, int window, int head_dim,
+                            int fp8, int which, int* launches_out, int* shape_out, int* ctas_out, int* at_out)
+{
+    if ((head_dim != 64 && head_dim != 128) || (fp8 && head_dim != 128) || !launches_out || !shape_out || !ctas_out || !at_out) return RLKV_EINVAL;
+    ChunkSeqs s;
+    ChunkArgs a;
+    const int rc = debug_args(lens, counts, n, n_full, n_comp, group, sink, window, s, a);
+    if (rc) return rc;
+    const int sms = kMaxChunkCtas / 2;
+    const bool two = two_launches(s, a, sms, fp8 != 0);
+    if (which < 0 || which > (two ? 1 : 0)) return RLKV_EINVAL;
+    int entries[kMaxPagedBatch];
+    *shape_out = cut_launch(s, a, two, which, sms, head_dim, fp8 != 0, chunk_record_bytes(head_dim), entries).shape;
+    write_ranges(a, entries, n, at_out);
+    *launches_out = two ? 2 : 1;
     *ctas_out = a.ctas;
     return RLKV_OK;
 }

@@ -40,12 +40,12 @@
 // Measured on one B200 (us on the GPU; 32 / 8 heads of 128, 6 of 8 full, unless said otherwise): five drafted tokens on 8192 14.5
 // (latency of one wave and of the join); four of each of 32 sequences of 8064 on average, 16 bits 129 (819 MB: 6.3 TB/s), 8 bits 106
 // (410 MB: the products, the decoding and the softmax of a tile share an SM's shared memory and issue slots); 512 beside 47 single
-// tokens of 2900 on average (28 / 4 heads, 3 of 4 full, capped) 87, in 8 bits 134 as two launches; 2048 on 8192, all full, 267 in bursts (1.16 PFLOP/s, 69 % of a large
+// tokens of 3400 on average (28 / 4 heads, 3 of 4 full, capped) 86 (alone 42 and 55), in 8 bits, as two launches, 135 (68 and 59); 2048 on 8192, all full, 267 in bursts (1.16 PFLOP/s, 69 % of a large
 // library product's burst rate), 8 bits 384 (one product per 128 keys; 395 with one per page).
 //
 // Tried and not taken: units of at most 32 rows four times in the tile of SHAPE 1 too, where they stand beside larger ones (512 beside
 // 47 88 -> 116, in 8 bits 144 -> 207: the code of both costs the softmax its registers); the two kinds as two launches at once on two
-// streams (70.9 -> 113 and more) or one behind the other; ranges that weigh tiles of few rows less or more (equal weights are best).
+// streams (70.9 -> 113 and more), and in 16 bits one behind the other (8-bit caches have them so, see two_launches in rlkv_paged_chunks.cu); ranges that weigh tiles of few rows less or more (equal weights are best).
 #include <cuda_fp16.h>
 #include <float.h>
 

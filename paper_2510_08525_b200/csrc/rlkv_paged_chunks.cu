@@ -138,8 +138,8 @@ int plan_chunks(ChunkArgs& a, int shape, int max_ctas, int min_tiles, int extra)
 // and 30), but few others beside them, whose tiles are as long (512 tokens on 3400 beside 11 single ones 94 and 110); in 16 bits where
 // the K and V rows are too many for the L2, in which the other tiles of rows would find them (four times 512 on 8192 300 and 270, 64
 // of each of 32 sequences on 8064 341 and 272) and every SM has 32 such tiles of 128 keys (64 tokens on 40000 62 and 65), or where it
-// has 100 (2048 on 8192 280 and 282, under the power cap 320 and 315, a prompt of 8192 497 and 490); but 512 on 8192 78 and 81, four
-// times 512 on 3400 111 and 117.
+// has 100 (2048 on 8192 280 and 282, under the power cap 320 and 315, a prompt of 8192 497 and 490; eight times 512 on 3400, 6 of 8 full,
+// 203 and 209: near this line the two are within 3 %, either way); but 512 on 8192 78 and 81, four times 512 on 3400 111 and 117.
 constexpr long long kNearL2 = 80ll << 20;
 // Key rows that a chunk of m tokens meets over all heads, on average over its tokens: of a ring no more than the sequence has.
 long long key_rows(const ChunkArgs& a, int len, int m)

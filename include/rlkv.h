@@ -346,7 +346,8 @@ int rlkv_paged_rotate_chunks(rlkv_paged* cache, int layer, const int* slots, con
  * sequence of len tokens stands at position len + i and sees key j <= len + i -- a full head every one, a compressed head
  * those with j < sink or j > len + i - window.  (That is why the chunk is not appended first: a ring would have dropped keys
  * that its first tokens see.)  Scores as rlkv_paged_set_scores says.  The chunk's own keys and values are taken as they are given,
- * those of an 8-bit cache as it holds them, against queries that are exact to 2^-21 of a row's largest element.  The cache does not change; a sequence may hold nothing yet.
+ * those of an 8-bit cache as it holds them, against queries that are exact to 2^-21 of a row's largest element.  The cache does not
+ * change; a sequence may hold nothing yet.
  * out: device bf16 [tokens][q_heads][head_dim] (fp32 accumulation, rounded once); lse: device fp32 [tokens][q_heads], log sum
  * exp(score), or NULL.  Every sum has a fixed order: the same call on the same cache gives the same bits.  Values of a sequence's own rows are
  * assumed finite; what rows of other sequences or of pages' unused parts hold has no effect.  A query that is not finite gives a
